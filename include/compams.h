@@ -422,6 +422,87 @@ int compams_blocksign_sweep_static_limits(int64_t* max_workers, int64_t* max_til
  */
 int compams_collect(float* row, const float* const* tensors, const int64_t* offsets, int32_t count, void* cuda_stream);
 
+/*
+ * Operators for the layers of a model whose n workers' micro-batches run as one batch: activations are [n, rows, h] with the worker on
+ * the leading axis, and a weight's gradient stays apart by worker, as the rows of the gradient buffer that compams_step takes.
+ *
+ * Element (i, j, c) of an input lies at p + i * worker_stride + j * row_stride + c elements of its type; the strides, in elements,
+ * are the caller's (0 repeats a worker or a row), columns are packed. Outputs are packed [n, rows, h] and may not overlap inputs.
+ * 1 <= n <= 65535, n * rows < 2^31 (rows = 0: nothing to do, gradients of weights become 0), 1 <= h < 2^31 - 4096; pointers are aligned to
+ * their element, and where all rows start on 16-byte boundaries accesses are 16 bytes wide. Work is enqueued on cuda_stream, in the
+ * current device, and nothing is allocated. Errors: INVALID_ARG, TOO_LARGE, CUDA.
+ *
+ * Dropout. Element c of row j of worker first_worker + i is kept where a 16-bit number u >= t = round(65536 p), and then multiplied
+ * by 65536 / (65536 - t); dropped elements are 0, whatever they were. u is a half of a word of the Philox4x32-10 block at counter
+ * (c / 8, j, worker, call) under key (seed mod 2^32, seed div 2^32): word (c % 8) / 2, its low half where c is even. The mask is
+ * found again from these numbers wherever it is needed and never stored. call counts a program's uses of the generator;
+ * call_device, if not null, points to one device int64 that is added to it (modulo 2^32), so that a captured graph draws anew at
+ * each replay; it has to hold the same value in a backward pass as in its forward pass.
+ */
+enum compams_type { COMPAMS_F32 = 0, COMPAMS_BF16 = 1, COMPAMS_F16 = 2 };
+
+/* y = dropout(x); also dx = dropout(dy). 0 <= p <= 1. */
+int compams_dropout(void* y, const void* x, int32_t type, int32_t n, int64_t rows, int64_t h, int64_t worker_stride,
+                    int64_t row_stride, double p, uint64_t seed, uint32_t call, const int64_t* call_device, uint32_t first_worker,
+                    void* cuda_stream);
+
+/*
+ * Layer norm over the h columns: y = (v - mean) / sqrt(var + eps) * weight + bias, with v = x, or, where residual is given,
+ * v = s = residual + dropout(x), which is rounded to residual_type and written to s.
+ *   type            of x and y; residual_type: of residual and s, the same or COMPAMS_F32.
+ *   stats           device float [n * rows][2], 8-byte aligned: mean and 1 / sqrt(var + eps) for the backward pass; may be null.
+ *   weight, bias    device fp32; element c of worker i at i * stride + c (stride 0: one for all workers); null: 1 and 0.
+ */
+int compams_norm_forward(void* y, void* s, float* stats, const void* x, const void* residual, int32_t type, int32_t residual_type,
+                         int32_t n, int64_t rows, int64_t h, int64_t x_worker_stride, int64_t x_row_stride,
+                         int64_t residual_worker_stride, int64_t residual_row_stride, const float* weight, int64_t weight_stride,
+                         const float* bias, int64_t bias_stride, float eps, double p, uint64_t seed, uint32_t call,
+                         const int64_t* call_device, uint32_t first_worker, void* cuda_stream);
+
+/*
+ * Its gradients. v and stats are the forward pass's (v = x, or s where `added`), v_type is v's; dy has `type`, ds v_type.
+ *   added = 0       dx: gradient of x. ds and dresidual are null, p is 0.
+ *   added = 1       dresidual = gradient of v + ds (ds null: none), in v_type; dx = dropout of it, in `type`.
+ *   dx, dresidual, dweight, dbias   each may be null: not wanted.
+ *   dweight, dbias  packed fp32 [n, h], row i summed over the rows of worker i alone, in a fixed order; sum_workers: [h], over all workers.
+ *   workspace       device, 16-byte aligned, at least compams_norm_workspace_bytes of the current device; used during the call's
+ *                   device work only. Not needed without dweight and dbias.
+ */
+int compams_norm_backward(void* dx, void* dresidual, float* dweight, float* dbias, int32_t sum_workers, const void* dy, const void* ds,
+                          const void* v, const float* stats, int32_t type, int32_t v_type, int32_t n, int64_t rows, int64_t h,
+                          int64_t dy_worker_stride, int64_t dy_row_stride, int64_t ds_worker_stride, int64_t ds_row_stride,
+                          int64_t v_worker_stride, int64_t v_row_stride, const float* weight, int64_t weight_stride, int32_t added,
+                          double p, uint64_t seed, uint32_t call, const int64_t* call_device, uint32_t first_worker, void* workspace,
+                          size_t workspace_bytes, void* cuda_stream);
+int compams_norm_workspace_bytes(size_t* bytes, int32_t n, int64_t rows, int64_t h);
+
+/*
+ * Low-rank adapters beside a projection: y = base + scale (dropout(x) A^T) B^T, worker (or request) by worker.
+ *   type            of x, base, dy and of the results; x is [n, rows, in], base [n, rows, out] (null: 0) and y packed [n, rows, out].
+ *   a, b            device fp32, A [rank, in] and B [out, rank]: rows packed, row_stride apart; worker i's at i * worker_stride (0: one
+ *                   for all). 1 <= rank <= 1024.
+ *   t               device, packed fp32 [n, rows, rank]: receives dropout(x) A^T, which the backward pass takes.
+ * The dropout is that of element (i, j, c) of x, as above.
+ */
+int compams_adapter_forward(void* y, float* t, const void* x, const void* base, int32_t type, int32_t n, int64_t rows, int64_t in,
+                            int64_t out, int32_t rank, int64_t x_worker_stride, int64_t x_row_stride, int64_t base_worker_stride,
+                            int64_t base_row_stride, const float* a, int64_t a_worker_stride, int64_t a_row_stride, const float* b,
+                            int64_t b_worker_stride, int64_t b_row_stride, float scale, double p, uint64_t seed, uint32_t call,
+                            const int64_t* call_device, uint32_t first_worker, void* cuda_stream);
+
+/*
+ * Its gradients (base's is dy itself). dx: packed [n, rows, in]; da: packed fp32 [n, rank, in]; db: packed fp32 [n, out, rank]; each may
+ * be null: not wanted. sum_workers: da [rank, in] and db [out, rank], summed over the workers. Sums run in a fixed order.
+ *   workspace       device, 16-byte aligned, at least compams_adapter_workspace_bytes; used during the call's device work only.
+ */
+int compams_adapter_backward(void* dx, float* da, float* db, int32_t sum_workers, const void* dy, const void* x, const float* t,
+                             int32_t type, int32_t n, int64_t rows, int64_t in, int64_t out, int32_t rank, int64_t dy_worker_stride,
+                             int64_t dy_row_stride, int64_t x_worker_stride, int64_t x_row_stride, const float* a,
+                             int64_t a_worker_stride, int64_t a_row_stride, const float* b, int64_t b_worker_stride,
+                             int64_t b_row_stride, float scale, double p, uint64_t seed, uint32_t call, const int64_t* call_device,
+                             uint32_t first_worker, void* workspace, size_t workspace_bytes, void* cuda_stream);
+int compams_adapter_workspace_bytes(size_t* bytes, int32_t n, int64_t rows, int64_t in, int64_t out, int32_t rank);
+
 /* Static strings (never null). */
 const char* compams_error_string(int status);
 const char* compams_kernel_name(int32_t kernel);

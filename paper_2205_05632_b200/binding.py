@@ -119,6 +119,23 @@ def load_library() -> ctypes.CDLL:
     L.compams_blocksign_sweep_static_limits.argtypes = [c.POINTER(c.c_int64), c.POINTER(c.c_int64)]
     L.compams_collect.restype = c.c_int
     L.compams_collect.argtypes = [c.c_void_p, c.POINTER(c.c_void_p), c.POINTER(c.c_int64), c.c_int32, c.c_void_p]
+    P, I32, I64, U32, U64 = c.c_void_p, c.c_int32, c.c_int64, c.c_uint32, c.c_uint64
+    drop = [c.c_double, U64, U32, P, U32]  # p, seed, call, call_device, first_worker
+    L.compams_dropout.restype = c.c_int
+    L.compams_dropout.argtypes = [P, P, I32, I32, I64, I64, I64, I64] + drop + [P]
+    L.compams_norm_forward.restype = c.c_int
+    L.compams_norm_forward.argtypes = [P] * 5 + [I32] * 3 + [I64] * 6 + [P, I64, P, I64, c.c_float] + drop + [P]
+    L.compams_norm_backward.restype = c.c_int
+    L.compams_norm_backward.argtypes = [P] * 4 + [I32] + [P] * 4 + [I32] * 3 + [I64] * 8 + [P, I64, I32] + drop + [P, c.c_size_t, P]
+    L.compams_norm_workspace_bytes.restype = c.c_int
+    L.compams_norm_workspace_bytes.argtypes = [c.POINTER(c.c_size_t), I32, I64, I64]
+    L.compams_adapter_forward.restype = c.c_int
+    L.compams_adapter_forward.argtypes = [P] * 4 + [I32] * 2 + [I64] * 3 + [I32] + [I64] * 4 + [P, I64, I64] * 2 + [c.c_float] + drop + [P]
+    L.compams_adapter_backward.restype = c.c_int
+    L.compams_adapter_backward.argtypes = ([P] * 3 + [I32] + [P] * 3 + [I32] * 2 + [I64] * 3 + [I32] + [I64] * 4 + [P, I64, I64] * 2
+                                           + [c.c_float] + drop + [P, c.c_size_t, P])
+    L.compams_adapter_workspace_bytes.restype = c.c_int
+    L.compams_adapter_workspace_bytes.argtypes = [c.POINTER(c.c_size_t), I32, I64, I64, I64, I32]
     L.compams_error_string.restype = c.c_char_p
     L.compams_error_string.argtypes = [c.c_int]
     L.compams_kernel_name.restype = c.c_char_p

@@ -12,13 +12,15 @@
 using namespace compams;
 
 namespace {
-
 thread_local std::string g_last_cuda_error;
+}
 
-int cuda_fail(cudaError_t e, const char* what) {
+int compams::cuda_fail(cudaError_t e, const char* what) {
     g_last_cuda_error = std::string(what) + ": " + cudaGetErrorString(e);
     return COMPAMS_ERR_CUDA;
 }
+
+namespace {
 
 #define CU(call)                                          \
     do {                                                  \

@@ -11,6 +11,9 @@
 
 namespace compams {
 
+// Notes a CUDA error's text for compams_last_cuda_error and gives the status to return.
+int cuda_fail(cudaError_t e, const char* what);
+
 constexpr int kSmallMax = 4096;    // Top-k blocks up to this size are selected inside one CTA's shared memory
 constexpr int kBins1 = 2048;       // radix pass 1: key bits 30..20
 constexpr int kBins23 = 1024;      // radix passes 2, 3: key bits 19..10, 9..0

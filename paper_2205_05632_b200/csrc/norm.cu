@@ -1,0 +1,594 @@
+// dropout, layer norm, and dropout + residual sum + layer norm on [n, rows, h] activations: forward and backward, with the
+// gradient of the weight and the bias kept apart by worker.
+//
+//   s = residual + dropout(x)             (or s = x)        kept in the residual's type
+//   y = (s - mean) rstd w + b,            mean and variance over the h columns, rstd = 1 / sqrt(var + eps)
+//   backward:  g = dy w,  xhat = (s - mean) rstd,
+//   ds_all = rstd (g - mean(g) - xhat mean(g xhat)) + ds,   dresidual = ds_all,  dx = dropout(ds_all) with the same mask
+//   dw_i = sum over the rows of worker i of dy xhat,        db_i = sum of dy
+//
+// All bound by memory. Sums and statistics are fp32, the variance is summed over differences from the mean (the row stays in
+// registers), weights, biases and their gradients are fp32 as the optimizer keeps them.
+#include "context.h"
+#include "rows.cuh"
+
+namespace compams {
+namespace {
+
+struct NormArgs {
+    const void* x;         // forward: x; backward: dy
+    const void* residual;  // forward: the residual; backward: ds (may be null)
+    const void* v;         // backward: the normalised values (x or s)
+    void* y;               // forward: y; backward: dx (may be null)
+    void* s;               // forward: s; backward: dresidual (may be null)
+    float2* stats;         // mean and rstd of every row; forward: may be null
+    const float* weight;   // may be null: ones
+    const float* bias;     // may be null: zeros
+    float* partial;        // backward: [n, chunks, 2, h] sums over the rows of a chunk; null: not wanted
+    int64_t x_ws, x_rs, r_ws, r_rs, v_ws, v_rs, weight_ws, bias_ws;
+    uint32_t rows;         // per worker
+    uint32_t total;        // n * rows
+    int32_t h;
+    uint32_t chunks;       // backward: CTAs per worker
+    float eps;
+    Drop drop;
+};
+
+__device__ __forceinline__ float warp_sum(float x) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    return x;
+}
+// The sum over the W warps of a row; the same order on every warp. `scratch`: W floats that no one reads any more.
+template <int W>
+__device__ __forceinline__ float row_sum(float x, float* scratch, int warp) {
+    x = warp_sum(x);
+    if (W == 1) return x;
+    if ((threadIdx.x & 31) == 0) scratch[warp] = x;
+    __syncthreads();
+    float s = 0.0f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) s += scratch[w];
+    return s;
+}
+
+constexpr int kRowsOfOneWarp = 8;  // rows of a CTA whose warps take a row each
+
+template <int W>
+constexpr int norm_threads() { return W == 1 ? 32 * kRowsOfOneWarp : 32 * W; }
+
+// ---- forward ---------------------------------------------------------------------------------------------------------------
+
+// W warps to a row, NG spans to a warp; the row lies in registers between the sums.
+template <typename TX, typename TR, int W, int NG, bool VEC, bool ADD>
+__global__ void __launch_bounds__(norm_threads<W>()) norm_forward_kernel(const __grid_constant__ NormArgs a) {
+    __shared__ float scratch[2][W];
+    const int lane = threadIdx.x & 31, warp = W == 1 ? 0 : (int)(threadIdx.x >> 5);
+    const uint32_t m = W == 1 ? blockIdx.x * kRowsOfOneWarp + (threadIdx.x >> 5) : blockIdx.x;
+    if (m >= a.total) return;  // a whole warp, and only where W is 1
+    const uint32_t i = m / a.rows, j = m - i * a.rows;
+    const TX* x = (const TX*)a.x + (int64_t)i * a.x_ws + (int64_t)j * a.x_rs;
+    float v[NG][8];
+#pragma unroll
+    for (int q = 0; q < NG; ++q) span_load<TX, VEC>(x, (q * W + warp) * kSpan, a.h, lane, v[q]);
+    if (ADD) {
+        const TR* r = (const TR*)a.residual + (int64_t)i * a.r_ws + (int64_t)j * a.r_rs;
+        TR* s = (TR*)a.s + (int64_t)m * a.h;
+        const uint32_t call = drop_call(a.drop);
+#pragma unroll
+        for (int q = 0; q < NG; ++q) {
+            const int c0 = (q * W + warp) * kSpan;
+            if (c0 >= a.h) break;
+            float add[8];
+            span_load<TR, VEC>(r, c0, a.h, lane, add);
+            if (a.drop.on) span_drop<VEC>(a.drop, c0, j, a.drop.worker + i, call, lane, v[q]);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[q][k] = to_float(from_float<TR>(v[q][k] + add[k]));
+            span_store<TR, VEC>(s, c0, a.h, lane, v[q]);
+        }
+    }
+    float sum = 0.0f;
+#pragma unroll
+    for (int q = 0; q < NG; ++q)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum += v[q][k];  // 0 beyond h
+    const float mean = row_sum<W>(sum, scratch[0], warp) / (float)a.h;
+    float square = 0.0f;
+#pragma unroll
+    for (int q = 0; q < NG; ++q)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const bool in = span_column<VEC>((q * W + warp) * kSpan, lane, k) < a.h;
+            v[q][k] -= mean;
+            square = fmaf(in ? v[q][k] : 0.0f, v[q][k], square);
+        }
+    const float rstd = 1.0f / sqrtf(row_sum<W>(square, scratch[1], warp) / (float)a.h + a.eps);
+    if (a.stats && warp == 0 && lane == 0) a.stats[m] = make_float2(mean, rstd);
+    const float* weight = a.weight ? a.weight + (int64_t)i * a.weight_ws : nullptr;
+    const float* bias = a.bias ? a.bias + (int64_t)i * a.bias_ws : nullptr;
+    TX* y = (TX*)a.y + (int64_t)m * a.h;
+#pragma unroll
+    for (int q = 0; q < NG; ++q) {
+        const int c0 = (q * W + warp) * kSpan;
+        if (c0 >= a.h) break;
+        float w[8], b[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) b[k] = 0.0f, w[k] = 1.0f;
+        if (weight) span_load<float, VEC>(weight, c0, a.h, lane, w);
+        if (bias) span_load<float, VEC>(bias, c0, a.h, lane, b);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[q][k] = fmaf(v[q][k] * rstd, w[k], b[k]);
+        span_store<TX, VEC>(y, c0, a.h, lane, v[q]);
+    }
+}
+
+// Rows too long for registers: the row is read again for each sum, from the L2 as a rule.
+template <typename TX, typename TR, bool ADD>
+__global__ void __launch_bounds__(512) norm_forward_long_kernel(const __grid_constant__ NormArgs a) {
+    constexpr int W = 16;
+    __shared__ float scratch[2][W];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint32_t m = blockIdx.x, i = m / a.rows, j = m - i * a.rows;
+    const TX* x = (const TX*)a.x + (int64_t)i * a.x_ws + (int64_t)j * a.x_rs;
+    // where there is a sum s it is written first, and read again by the thread that wrote it
+    TR* s = (TR*)a.s + (int64_t)m * a.h;
+    const TR* r = (const TR*)a.residual + (int64_t)i * a.r_ws + (int64_t)j * a.r_rs;
+    const uint32_t call = drop_call(a.drop);
+    float sum = 0.0f;
+    for (int c0 = warp * kSpan; c0 < a.h; c0 += W * kSpan) {
+        float v[8], add[8];
+        span_load<TX, false>(x, c0, a.h, lane, v);
+        if (ADD) {
+            span_load<TR, false>(r, c0, a.h, lane, add);
+            if (a.drop.on) span_drop<false>(a.drop, c0, j, a.drop.worker + i, call, lane, v);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = to_float(from_float<TR>(v[k] + add[k]));
+            span_store<TR, false>(s, c0, a.h, lane, v);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum += v[k];
+    }
+    const float mean = row_sum<W>(sum, scratch[0], warp) / (float)a.h;
+    float square = 0.0f;
+    for (int c = warp * kSpan + lane; c < a.h; c += (c - lane) % kSpan == kSpan - 32 ? (W - 1) * kSpan + 32 : 32) {
+        const float v = (ADD ? to_float(s[c]) : to_float(__ldg(x + c))) - mean;
+        square = fmaf(v, v, square);
+    }
+    const float rstd = 1.0f / sqrtf(row_sum<W>(square, scratch[1], warp) / (float)a.h + a.eps);
+    if (a.stats && threadIdx.x == 0) a.stats[m] = make_float2(mean, rstd);
+    const float* weight = a.weight ? a.weight + (int64_t)i * a.weight_ws : nullptr;
+    const float* bias = a.bias ? a.bias + (int64_t)i * a.bias_ws : nullptr;
+    TX* y = (TX*)a.y + (int64_t)m * a.h;
+    for (int c = warp * kSpan + lane; c < a.h; c += (c - lane) % kSpan == kSpan - 32 ? (W - 1) * kSpan + 32 : 32) {
+        const float v = (ADD ? to_float(s[c]) : to_float(__ldg(x + c))) - mean;
+        y[c] = from_float<TX>(fmaf(v * rstd, weight ? __ldg(weight + c) : 1.0f, bias ? __ldg(bias + c) : 0.0f));
+    }
+}
+
+// ---- backward --------------------------------------------------------------------------------------------------------------
+
+// A CTA goes through the rows of one chunk of one worker and keeps the sums of dy xhat and dy of its columns in registers.
+template <typename TX, typename TR, int W, int NG, bool VEC, bool ADD>
+__global__ void __launch_bounds__(norm_threads<W>()) norm_backward_kernel(const __grid_constant__ NormArgs a) {
+    constexpr int kSlots = W == 1 ? kRowsOfOneWarp : 1;
+    __shared__ float scratch[2][2][W];
+    __shared__ float joined[W == 1 ? NG * kSpan : 1];
+    const int lane = threadIdx.x & 31, warp = W == 1 ? 0 : (int)(threadIdx.x >> 5), slot = W == 1 ? (int)(threadIdx.x >> 5) : 0;
+    const uint32_t i = blockIdx.x / a.chunks, chunk = blockIdx.x - i * a.chunks;
+    const uint32_t j0 = (uint32_t)((uint64_t)a.rows * chunk / a.chunks), j1 = (uint32_t)((uint64_t)a.rows * (chunk + 1) / a.chunks);
+    const float* weight = a.weight ? a.weight + (int64_t)i * a.weight_ws : nullptr;
+    const uint32_t call = drop_call(a.drop);
+    float dw[NG][8], db[NG][8];
+#pragma unroll
+    for (int q = 0; q < NG; ++q)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) dw[q][k] = db[q][k] = 0.0f;
+    int turn = 0;
+    for (uint32_t j = j0 + slot; j < j1; j += kSlots, turn ^= 1) {
+        const uint32_t m = i * a.rows + j;
+        const TX* dy = (const TX*)a.x + (int64_t)i * a.x_ws + (int64_t)j * a.x_rs;
+        const TR* v = (const TR*)a.v + (int64_t)i * a.v_ws + (int64_t)j * a.v_rs;
+        float g[NG][8], xhat[NG][8];
+        const float2 st = a.stats[m];
+        float c1 = 0.0f, c2 = 0.0f;
+#pragma unroll
+        for (int q = 0; q < NG; ++q) {
+            span_load<TX, VEC>(dy, (q * W + warp) * kSpan, a.h, lane, g[q]);
+            span_load<TR, VEC>(v, (q * W + warp) * kSpan, a.h, lane, xhat[q], st.x);
+        }
+#pragma unroll
+        for (int q = 0; q < NG; ++q) {
+            const int c0 = (q * W + warp) * kSpan;
+            float w[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) w[k] = 1.0f;
+            if (weight) span_load<float, VEC>(weight, c0, a.h, lane, w);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                xhat[q][k] = (xhat[q][k] - st.x) * st.y;
+                db[q][k] += g[q][k];
+                dw[q][k] = fmaf(g[q][k], xhat[q][k], dw[q][k]);
+                g[q][k] *= w[k];
+                c1 += g[q][k];
+                c2 = fmaf(g[q][k], xhat[q][k], c2);
+            }
+        }
+        if (!a.y && !a.s) continue;
+        c1 = warp_sum(c1);
+        c2 = warp_sum(c2);
+        if (W > 1) {
+            if (lane == 0) {
+                scratch[turn][0][warp] = c1;
+                scratch[turn][1][warp] = c2;
+            }
+            __syncthreads();  // the next row writes the other half, and the one after it only behind the next row's barrier
+            c1 = c2 = 0.0f;
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                c1 += scratch[turn][0][w];
+                c2 += scratch[turn][1][w];
+            }
+        }
+        c1 /= (float)a.h;
+        c2 /= (float)a.h;
+        const TR* more = ADD && a.residual ? (const TR*)a.residual + (int64_t)i * a.r_ws + (int64_t)j * a.r_rs : nullptr;
+#pragma unroll
+        for (int q = 0; q < NG; ++q) {
+            const int c0 = (q * W + warp) * kSpan;
+            if (c0 >= a.h) break;
+            float add[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) add[k] = 0.0f;
+            if (more) span_load<TR, VEC>(more, c0, a.h, lane, add);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) g[q][k] = fmaf(st.y, g[q][k] - c1 - xhat[q][k] * c2, add[k]);
+            if (ADD && a.s) span_store<TR, VEC>((TR*)a.s + (int64_t)m * a.h, c0, a.h, lane, g[q]);
+            if (ADD && a.drop.on && a.y) span_drop<VEC>(a.drop, c0, j, a.drop.worker + i, call, lane, g[q]);
+            if (a.y) span_store<TX, VEC>((TX*)a.y + (int64_t)m * a.h, c0, a.h, lane, g[q]);
+        }
+    }
+    if (!a.partial) return;
+    float* out = a.partial + (int64_t)blockIdx.x * 2 * a.h;
+    if constexpr (W > 1) {
+#pragma unroll
+        for (int q = 0; q < NG; ++q)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int c = span_column<VEC>((q * W + warp) * kSpan, lane, k);
+                if (c < a.h) {
+                    out[c] = dw[q][k];
+                    out[a.h + c] = db[q][k];
+                }
+            }
+    } else {  // warps with rows of their own: their sums joined one warp after the other
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            for (int s = 0; s < kSlots; ++s) {
+                if (slot == s) {
+#pragma unroll
+                    for (int q = 0; q < NG; ++q)
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            const int at = span_column<VEC>(q * kSpan, lane, k);
+                            const float x = which ? db[q][k] : dw[q][k];
+                            joined[at] = s == 0 ? x : joined[at] + x;
+                        }
+                }
+                __syncthreads();
+            }
+            for (int c = threadIdx.x; c < a.h; c += blockDim.x) out[which * a.h + c] = joined[c];
+            __syncthreads();
+        }
+    }
+}
+
+// Rows too long for registers: one kernel for the rows' sums and dx, one for the columns' sums.
+template <typename TX, typename TR, bool ADD>
+__global__ void __launch_bounds__(512) norm_backward_long_kernel(const __grid_constant__ NormArgs a) {
+    constexpr int W = 16;
+    __shared__ float scratch[2][W];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint32_t m = blockIdx.x, i = m / a.rows, j = m - i * a.rows;
+    const TX* dy = (const TX*)a.x + (int64_t)i * a.x_ws + (int64_t)j * a.x_rs;
+    const TR* v = (const TR*)a.v + (int64_t)i * a.v_ws + (int64_t)j * a.v_rs;
+    const float* weight = a.weight ? a.weight + (int64_t)i * a.weight_ws : nullptr;
+    const uint32_t call = drop_call(a.drop);
+    const float2 st = a.stats[m];
+    float c1 = 0.0f, c2 = 0.0f;
+    for (int c0 = warp * kSpan; c0 < a.h; c0 += W * kSpan)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int c = span_column<false>(c0, lane, k);
+            if (c < a.h) {
+                const float g = to_float(__ldg(dy + c)) * (weight ? __ldg(weight + c) : 1.0f);
+                c1 += g;
+                c2 = fmaf(g, (to_float(__ldg(v + c)) - st.x) * st.y, c2);
+            }
+        }
+    c1 = row_sum<W>(c1, scratch[0], warp) / (float)a.h;
+    c2 = row_sum<W>(c2, scratch[1], warp) / (float)a.h;
+    const TR* more = ADD && a.residual ? (const TR*)a.residual + (int64_t)i * a.r_ws + (int64_t)j * a.r_rs : nullptr;
+    for (int c0 = warp * kSpan; c0 < a.h; c0 += W * kSpan) {
+        float g[8], xhat[8], add[8], w[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) add[k] = 0.0f, w[k] = 1.0f;
+        span_load<TX, false>(dy, c0, a.h, lane, g);
+        span_load<TR, false>(v, c0, a.h, lane, xhat, st.x);
+        if (weight) span_load<float, false>(weight, c0, a.h, lane, w);
+        if (more) span_load<TR, false>(more, c0, a.h, lane, add);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) g[k] = fmaf(st.y, g[k] * w[k] - c1 - (xhat[k] - st.x) * st.y * c2, add[k]);
+        if (ADD && a.s) span_store<TR, false>((TR*)a.s + (int64_t)m * a.h, c0, a.h, lane, g);
+        if (ADD && a.drop.on && a.y) span_drop<false>(a.drop, c0, j, a.drop.worker + i, call, lane, g);
+        if (a.y) span_store<TX, false>((TX*)a.y + (int64_t)m * a.h, c0, a.h, lane, g);
+    }
+}
+
+template <typename TX, typename TR>
+__global__ void __launch_bounds__(256) norm_columns_kernel(const __grid_constant__ NormArgs a) {
+    const uint32_t tiles = (uint32_t)(a.h + 255) / 256, at = blockIdx.x / tiles;
+    const uint32_t i = at / a.chunks, chunk = at - i * a.chunks;
+    const uint32_t j0 = (uint32_t)((uint64_t)a.rows * chunk / a.chunks), j1 = (uint32_t)((uint64_t)a.rows * (chunk + 1) / a.chunks);
+    const int c = (int)((blockIdx.x - at * tiles) * 256 + threadIdx.x);
+    if (c >= a.h) return;
+    const TX* dy = (const TX*)a.x + (int64_t)i * a.x_ws + c;
+    const TR* v = (const TR*)a.v + (int64_t)i * a.v_ws + c;
+    float dw = 0.0f, db = 0.0f;
+    for (uint32_t j = j0; j < j1; ++j) {
+        const float2 st = a.stats[i * a.rows + j];
+        const float g = to_float(__ldg(dy + (int64_t)j * a.x_rs));
+        dw = fmaf(g, (to_float(__ldg(v + (int64_t)j * a.v_rs)) - st.x) * st.y, dw);
+        db += g;
+    }
+    float* out = a.partial + (int64_t)at * 2 * a.h;
+    out[c] = dw;
+    out[a.h + c] = db;
+}
+
+// Sums the chunks of a worker (or of all) in their order: 32 columns by 8 shares of the chunks, the shares joined in shared memory.
+__global__ void __launch_bounds__(256) norm_join_kernel(const float* __restrict__ partial, float* dweight, float* dbias, int32_t h,
+                                                        uint32_t chunks) {
+    __shared__ float share[8][33];
+    dependency_wait();
+    const int c = (int)(blockIdx.x * 32 + threadIdx.x);
+    float* out = blockIdx.z ? dbias : dweight;
+    if (!out) return;
+    float s = 0.0f;
+    if (c < h) {
+        const float* p = partial + ((int64_t)blockIdx.y * chunks * 2 + blockIdx.z) * h + c;
+        for (uint32_t q = threadIdx.y; q < chunks; q += 8) s += __ldcg(p + (int64_t)q * 2 * h);
+    }
+    share[threadIdx.y][threadIdx.x] = s;
+    __syncthreads();
+    if (threadIdx.y == 0 && c < h) {
+        for (int k = 1; k < 8; ++k) s += share[k][threadIdx.x];
+        out[(int64_t)blockIdx.y * h + c] = s;
+    }
+}
+
+// ---- dropout ---------------------------------------------------------------------------------------------------------------
+
+// A warp per span of a row.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(256) dropout_kernel(const T* __restrict__ x, T* __restrict__ y, int64_t ws, int64_t rs, uint32_t rows,
+                                                      uint32_t total, int32_t h, uint32_t spans, const __grid_constant__ Drop d) {
+    const int lane = threadIdx.x & 31;
+    const uint64_t at = (uint64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const uint64_t m64 = at / spans;
+    if (m64 >= total) return;
+    const uint32_t m = (uint32_t)m64, i = m / rows, j = m - i * rows;
+    const int c0 = (int)(at - m64 * spans) * kSpan;
+    float v[8];
+    span_load<T, VEC>(x + (int64_t)i * ws + (int64_t)j * rs, c0, h, lane, v);
+    if (d.on) span_drop<VEC>(d, c0, j, d.worker + i, drop_call(d), lane, v);
+    span_store<T, VEC>(y + (int64_t)m * h, c0, h, lane, v);
+}
+
+// ---- host ------------------------------------------------------------------------------------------------------------------
+
+constexpr int kLongest = 16 * 4 * kSpan;  // columns of a row that is kept in registers
+
+struct Shape {
+    int32_t n;
+    int64_t rows, h;
+    bool ok() const {
+        return n >= 1 && n <= 65535 && rows >= 0 && h >= 1 && h < ((int64_t)1 << 31) - 16 * kSpan && rows <= (int64_t)0x7fffffff / n;
+    }
+};
+
+uint32_t backward_chunks(const Shape& z) {
+    int device = 0, sms = 148;
+    if (cudaGetDevice(&device) == cudaSuccess) cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
+    cudaGetLastError();
+    const int64_t per_row_warp = z.h <= 4 * kSpan ? kRowsOfOneWarp : 1;
+    int64_t c = (2 * (int64_t)sms + z.n - 1) / z.n;
+    const int64_t most = (z.rows + per_row_warp - 1) / per_row_warp;
+    if (c > most) c = most;
+    return (uint32_t)(c < 1 ? 1 : c);
+}
+
+template <typename F>
+int by_types(int32_t x, int32_t r, F f) {  // r: x's type or fp32
+    if (x == kTypeF32) return f(float(), float());
+    if (x == kTypeBF16) return r == kTypeF32 ? f(__nv_bfloat16(), float()) : f(__nv_bfloat16(), __nv_bfloat16());
+    return r == kTypeF32 ? f(__half(), float()) : f(__half(), __half());
+}
+
+int launched(cudaError_t e, const char* what) { return e == cudaSuccess ? COMPAMS_OK : cuda_fail(e, what); }
+
+template <typename TX, typename TR, bool ADD>
+int forward(const NormArgs& a, bool vec, cudaStream_t stream) {
+    const int spans = (a.h + kSpan - 1) / kSpan;
+    cudaError_t e = cudaSuccess;
+    auto go = [&](auto kernel, int W) {
+        const uint32_t per = W == 1 ? kRowsOfOneWarp : 1;
+        e = launch_plain(kernel, dim3((a.total + per - 1) / per), dim3(W == 1 ? 32 * kRowsOfOneWarp : 32 * W), 0, stream, a);
+    };
+    // a few rows leave SMs idle: then as many warps as a row has spans, the shortest way through one row
+    const bool few = a.total <= 2 * 148;
+    if (a.h > kLongest) {
+        e = launch_plain(norm_forward_long_kernel<TX, TR, ADD>, dim3(a.total), dim3(512), 0, stream, a);
+    } else if (vec) {
+        if (few && spans > 1 && spans <= 16) go(norm_forward_kernel<TX, TR, 16, 1, true, ADD>, 16);
+        else if (spans <= 1) go(norm_forward_kernel<TX, TR, 1, 1, true, ADD>, 1);
+        else if (spans <= 2) go(norm_forward_kernel<TX, TR, 1, 2, true, ADD>, 1);
+        else if (spans <= 4) go(norm_forward_kernel<TX, TR, 1, 4, true, ADD>, 1);
+        else if (spans <= 16) go(norm_forward_kernel<TX, TR, 4, 4, true, ADD>, 4);
+        else if (spans <= 32) go(norm_forward_kernel<TX, TR, 8, 4, true, ADD>, 8);
+        else go(norm_forward_kernel<TX, TR, 16, 4, true, ADD>, 16);
+    } else {
+        if (spans <= 4) go(norm_forward_kernel<TX, TR, 1, 4, false, ADD>, 1);
+        else if (spans <= 16) go(norm_forward_kernel<TX, TR, 4, 4, false, ADD>, 4);
+        else go(norm_forward_kernel<TX, TR, 16, 4, false, ADD>, 16);
+    }
+    return launched(e, "norm_forward");
+}
+
+template <typename TX, typename TR, bool ADD>
+int backward(const NormArgs& a, int n, bool vec, cudaStream_t stream) {
+    const int spans = (a.h + kSpan - 1) / kSpan;
+    cudaError_t e = cudaSuccess;
+    auto go = [&](auto kernel, int W) {
+        e = launch_plain(kernel, dim3((uint32_t)n * a.chunks), dim3(W == 1 ? 32 * kRowsOfOneWarp : 32 * W), 0, stream, a);
+    };
+    if (a.h > kLongest) {
+        if (a.y || a.s) e = launch_plain(norm_backward_long_kernel<TX, TR, ADD>, dim3(a.total), dim3(512), 0, stream, a);
+        if (e == cudaSuccess && a.partial)
+            e = launch_plain(norm_columns_kernel<TX, TR>, dim3((uint32_t)(a.h + 255) / 256 * (uint32_t)n * a.chunks), dim3(256), 0, stream, a);
+    } else if (vec) {
+        if (spans <= 1) go(norm_backward_kernel<TX, TR, 1, 1, true, ADD>, 1);
+        else if (spans <= 2) go(norm_backward_kernel<TX, TR, 1, 2, true, ADD>, 1);
+        else if (spans <= 4) go(norm_backward_kernel<TX, TR, 1, 4, true, ADD>, 1);
+        else if (spans <= 8) go(norm_backward_kernel<TX, TR, 8, 1, true, ADD>, 8);
+        else if (spans <= 16) go(norm_backward_kernel<TX, TR, 16, 1, true, ADD>, 16);
+        else if (spans <= 32) go(norm_backward_kernel<TX, TR, 16, 2, true, ADD>, 16);
+        else go(norm_backward_kernel<TX, TR, 16, 4, true, ADD>, 16);
+    } else {
+        if (spans <= 4) go(norm_backward_kernel<TX, TR, 1, 4, false, ADD>, 1);
+        else if (spans <= 16) go(norm_backward_kernel<TX, TR, 16, 1, false, ADD>, 16);
+        else go(norm_backward_kernel<TX, TR, 16, 4, false, ADD>, 16);
+    }
+    return launched(e, "norm_backward");
+}
+
+bool vector_parameter(const float* p, int64_t ws) {
+    return !p || (((reinterpret_cast<uintptr_t>(p) | (uint64_t)(ws * 4)) & 15u) == 0);
+}
+bool float_aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+}  // namespace
+}  // namespace compams
+
+using namespace compams;
+
+extern "C" {
+
+int compams_dropout(void* y, const void* x, int32_t type, int32_t n, int64_t rows, int64_t h, int64_t worker_stride, int64_t row_stride,
+                    double p, uint64_t seed, uint32_t call, const int64_t* call_device, uint32_t first_worker, void* cuda_stream) {
+    const Shape z{n, rows, h};
+    Drop d;
+    if (!z.ok() || !type_known(type) || !make_drop(d, p, seed, call, call_device, first_worker)) return COMPAMS_ERR_INVALID_ARG;
+    if (rows == 0) return COMPAMS_OK;
+    const Rows in{x, worker_stride, row_stride, type}, out = packed(y, rows, h, type);
+    if (!x || !y || !in.element_aligned() || !out.element_aligned()) return COMPAMS_ERR_INVALID_ARG;
+    const bool vec = h % 8 == 0 && in.aligned() && out.aligned();
+    const uint32_t spans = (uint32_t)((h + kSpan - 1) / kSpan), total = (uint32_t)(n * rows);
+    const uint64_t ctas = ((uint64_t)total * spans + 7) / 8;
+    if (ctas > 0x7fffffffu) return COMPAMS_ERR_TOO_LARGE;
+    return by_types(type, type, [&](auto t, auto) {
+        using T = decltype(t);
+        auto kernel = vec ? dropout_kernel<T, true> : dropout_kernel<T, false>;
+        return launched(launch_plain(kernel, dim3((uint32_t)ctas), dim3(256), 0, (cudaStream_t)cuda_stream, (const T*)x, (T*)y, worker_stride,
+                                     row_stride, (uint32_t)rows, total, (int32_t)h, spans, d),
+                        "dropout");
+    });
+}
+
+int compams_norm_forward(void* y, void* s, float* stats, const void* x, const void* residual, int32_t type, int32_t residual_type,
+                         int32_t n, int64_t rows, int64_t h, int64_t x_worker_stride, int64_t x_row_stride,
+                         int64_t residual_worker_stride, int64_t residual_row_stride, const float* weight, int64_t weight_stride,
+                         const float* bias, int64_t bias_stride, float eps, double p, uint64_t seed, uint32_t call,
+                         const int64_t* call_device, uint32_t first_worker, void* cuda_stream) {
+    const Shape z{n, rows, h};
+    NormArgs a = {};
+    if (!z.ok() || !type_known(type) || !make_drop(a.drop, p, seed, call, call_device, first_worker) || !(eps >= 0.0f))
+        return COMPAMS_ERR_INVALID_ARG;
+    const bool add = residual != nullptr;
+    if (add ? residual_type != type && residual_type != kTypeF32 : s != nullptr || p != 0.0) return COMPAMS_ERR_INVALID_ARG;
+    if (rows == 0) return COMPAMS_OK;
+    const Rows in{x, x_worker_stride, x_row_stride, type}, out = packed(y, rows, h, type);
+    const Rows res{residual, residual_worker_stride, residual_row_stride, residual_type}, sum = packed(s, rows, h, residual_type);
+    if (!x || !y || (add && !s) || !in.element_aligned() || !out.element_aligned() || !float_aligned(weight) || !float_aligned(bias) ||
+        (reinterpret_cast<uintptr_t>(stats) & 7u) || (add && (!res.element_aligned() || !sum.element_aligned())))
+        return COMPAMS_ERR_INVALID_ARG;
+    const bool vec = h % 8 == 0 && in.aligned() && out.aligned() && (!add || (res.aligned() && sum.aligned())) &&
+                     vector_parameter(weight, weight_stride) && vector_parameter(bias, bias_stride);
+    a.x = x; a.residual = residual; a.y = y; a.s = s; a.stats = (float2*)stats; a.weight = weight; a.bias = bias;
+    a.x_ws = x_worker_stride; a.x_rs = x_row_stride; a.r_ws = residual_worker_stride; a.r_rs = residual_row_stride;
+    a.weight_ws = weight_stride; a.bias_ws = bias_stride;
+    a.rows = (uint32_t)rows; a.total = (uint32_t)(n * rows); a.h = (int32_t)h; a.eps = eps;
+    return by_types(type, add ? residual_type : type, [&](auto tx, auto tr) {
+        using TX = decltype(tx);
+        using TR = decltype(tr);
+        if (add) return forward<TX, TR, true>(a, vec, (cudaStream_t)cuda_stream);
+        return forward<TX, TX, false>(a, vec, (cudaStream_t)cuda_stream);
+    });
+}
+
+int compams_norm_workspace_bytes(size_t* bytes, int32_t n, int64_t rows, int64_t h) {
+    const Shape z{n, rows, h};
+    if (!bytes || !z.ok()) return COMPAMS_ERR_INVALID_ARG;
+    *bytes = (size_t)n * backward_chunks(z) * 2 * (size_t)h * sizeof(float);
+    return COMPAMS_OK;
+}
+
+int compams_norm_backward(void* dx, void* dresidual, float* dweight, float* dbias, int32_t sum_workers, const void* dy, const void* ds,
+                          const void* v, const float* stats, int32_t type, int32_t v_type, int32_t n, int64_t rows, int64_t h,
+                          int64_t dy_worker_stride, int64_t dy_row_stride, int64_t ds_worker_stride, int64_t ds_row_stride,
+                          int64_t v_worker_stride, int64_t v_row_stride, const float* weight, int64_t weight_stride, int32_t added,
+                          double p, uint64_t seed, uint32_t call, const int64_t* call_device, uint32_t first_worker, void* workspace,
+                          size_t workspace_bytes, void* cuda_stream) {
+    const Shape z{n, rows, h};
+    NormArgs a = {};
+    if (!z.ok() || !type_known(type) || !make_drop(a.drop, p, seed, call, call_device, first_worker)) return COMPAMS_ERR_INVALID_ARG;
+    const bool add = added != 0;
+    if (add ? v_type != type && v_type != kTypeF32 : v_type != type || ds || dresidual || p != 0.0) return COMPAMS_ERR_INVALID_ARG;
+    const bool sums = dweight || dbias;
+    const uint32_t chunks = backward_chunks(z);
+    if ((uint64_t)n * chunks * (uint64_t)((h + 255) / 256) > 0x7fffffffu) return COMPAMS_ERR_TOO_LARGE;
+    if (sums && (!workspace || workspace_bytes < (size_t)n * chunks * 2 * (size_t)h * sizeof(float) ||
+                 (reinterpret_cast<uintptr_t>(workspace) & 15u) || !float_aligned(dweight) || !float_aligned(dbias)))
+        return COMPAMS_ERR_INVALID_ARG;
+    const cudaStream_t stream = (cudaStream_t)cuda_stream;
+    if (rows == 0) {
+        const size_t bytes = (size_t)(sum_workers ? 1 : n) * (size_t)h * sizeof(float);
+        cudaError_t e = dweight ? cudaMemsetAsync(dweight, 0, bytes, stream) : cudaSuccess;
+        if (e == cudaSuccess && dbias) e = cudaMemsetAsync(dbias, 0, bytes, stream);
+        return launched(e, "norm_backward");
+    }
+    const Rows gin{dy, dy_worker_stride, dy_row_stride, type}, gsum{ds, ds_worker_stride, ds_row_stride, v_type};
+    const Rows vin{v, v_worker_stride, v_row_stride, v_type}, out = packed(dx, rows, h, type), rout = packed(dresidual, rows, h, v_type);
+    if (!dy || !v || !stats || (reinterpret_cast<uintptr_t>(stats) & 7u) || !float_aligned(weight) || !gin.element_aligned() ||
+        !gsum.element_aligned() || !vin.element_aligned() || !out.element_aligned() || !rout.element_aligned())
+        return COMPAMS_ERR_INVALID_ARG;
+    const bool vec = h % 8 == 0 && gin.aligned() && vin.aligned() && (!ds || gsum.aligned()) && out.aligned() && rout.aligned() &&
+                     vector_parameter(weight, weight_stride);
+    a.x = dy; a.residual = ds; a.v = v; a.y = dx; a.s = dresidual; a.stats = (float2*)stats; a.weight = weight;
+    a.partial = sums ? (float*)workspace : nullptr;
+    a.x_ws = dy_worker_stride; a.x_rs = dy_row_stride; a.r_ws = ds_worker_stride; a.r_rs = ds_row_stride;
+    a.v_ws = v_worker_stride; a.v_rs = v_row_stride; a.weight_ws = weight_stride;
+    a.rows = (uint32_t)rows; a.total = (uint32_t)(n * rows); a.h = (int32_t)h; a.chunks = chunks;
+    const int rc = by_types(type, v_type, [&](auto tx, auto tr) {
+        using TX = decltype(tx);
+        using TR = decltype(tr);
+        if (add) return backward<TX, TR, true>(a, n, vec, stream);
+        return backward<TX, TX, false>(a, n, vec, stream);
+    });
+    if (rc != COMPAMS_OK || !sums) return rc;
+    const uint32_t groups = sum_workers ? 1u : (uint32_t)n, per = sum_workers ? (uint32_t)n * chunks : chunks;
+    return launched(launch_after(norm_join_kernel, dim3((uint32_t)((h + 31) / 32), groups, 2), dim3(32, 8), stream,
+                                 (const float*)workspace, dweight, dbias, (int32_t)h, per),
+                    "norm_join");
+}
+
+}  // extern "C"

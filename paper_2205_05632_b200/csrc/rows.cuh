@@ -1,0 +1,205 @@
+// What the operators on [n, rows, h] activations share: element types, spans of 256 columns, the dropout mask.
+//
+// The leading axis is the worker's, so element (i, j, c) is column c of row j of worker i; rows are packed (column stride 1), the
+// other two strides are the caller's. A warp takes a span of 256 columns at a time, eight per lane. Where every row starts on a
+// 16-byte boundary and h is a multiple of 8 (VEC) they are eight neighbours, read and written 16 bytes at a time; elsewhere they are
+// every 32nd column, one element per access, so that a warp's accesses stay contiguous.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+namespace compams {
+
+constexpr int kSpan = 256;
+
+// ---- element types ---------------------------------------------------------------------------------------------------------
+
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
+template <typename T> __device__ __forceinline__ T from_float(float x);
+template <> __device__ __forceinline__ float from_float<float>(float x) { return x; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+template <> __device__ __forceinline__ __half from_float<__half>(float x) { return __float2half_rn(x); }
+
+__device__ __forceinline__ void unpack(uint32_t w, float& a, float& b, __nv_bfloat16) {
+    a = __uint_as_float(w << 16);
+    b = __uint_as_float(w & 0xffff0000u);
+}
+__device__ __forceinline__ void unpack(uint32_t w, float& a, float& b, __half) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+    a = f.x;
+    b = f.y;
+}
+__device__ __forceinline__ uint32_t pack(float a, float b, __nv_bfloat16) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ uint32_t pack(float a, float b, __half) {
+    const __half2 v = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// Eight neighbours on a 16-byte boundary, as they lie in memory: 16 bytes of a 16-bit type, 32 of fp32.
+template <typename T> struct Raw8 { uint4 q; };
+template <> struct Raw8<float> { float4 a, b; };
+
+template <typename T> __device__ __forceinline__ Raw8<T> raw_load(const T* p) { return {__ldg(reinterpret_cast<const uint4*>(p))}; }
+template <> __device__ __forceinline__ Raw8<float> raw_load<float>(const float* p) {
+    return {__ldg(reinterpret_cast<const float4*>(p)), __ldg(reinterpret_cast<const float4*>(p) + 1)};
+}
+template <typename T> __device__ __forceinline__ void raw_floats(const Raw8<T>& r, float (&v)[8]) {
+    unpack(r.q.x, v[0], v[1], T());
+    unpack(r.q.y, v[2], v[3], T());
+    unpack(r.q.z, v[4], v[5], T());
+    unpack(r.q.w, v[6], v[7], T());
+}
+template <> __device__ __forceinline__ void raw_floats<float>(const Raw8<float>& r, float (&v)[8]) {
+    v[0] = r.a.x; v[1] = r.a.y; v[2] = r.a.z; v[3] = r.a.w;
+    v[4] = r.b.x; v[5] = r.b.y; v[6] = r.b.z; v[7] = r.b.w;
+}
+template <typename T> __device__ __forceinline__ void store8(T* p, const float (&v)[8]) {
+    uint4 q;
+    q.x = pack(v[0], v[1], T());
+    q.y = pack(v[2], v[3], T());
+    q.z = pack(v[4], v[5], T());
+    q.w = pack(v[6], v[7], T());
+    *reinterpret_cast<uint4*>(p) = q;
+}
+template <> __device__ __forceinline__ void store8<float>(float* p, const float (&v)[8]) {
+    reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+}
+
+// ---- spans -----------------------------------------------------------------------------------------------------------------
+
+// The column of a lane's value k in the span that starts at column c0.
+template <bool VEC> __device__ __forceinline__ int span_column(int c0, int lane, int k) {
+    return VEC ? c0 + lane * 8 + k : c0 + k * 32 + lane;
+}
+// A lane's values of a span; `beyond` stands in the columns from h on.
+template <typename T, bool VEC>
+__device__ __forceinline__ void span_load(const T* __restrict__ row, int c0, int h, int lane, float (&v)[8], float beyond = 0.0f) {
+    if (VEC) {
+        if (c0 + lane * 8 < h) {
+            raw_floats<T>(raw_load<T>(row + c0 + lane * 8), v);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = beyond;
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int c = c0 + k * 32 + lane;
+            v[k] = c < h ? to_float(__ldg(row + c)) : beyond;
+        }
+    }
+}
+template <typename T, bool VEC>
+__device__ __forceinline__ void span_store(T* __restrict__ row, int c0, int h, int lane, const float (&v)[8]) {
+    if (VEC) {
+        if (c0 + lane * 8 < h) store8<T>(row + c0 + lane * 8, v);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int c = c0 + k * 32 + lane;
+            if (c < h) row[c] = from_float<T>(v[k]);
+        }
+    }
+}
+
+// ---- dropout ---------------------------------------------------------------------------------------------------------------
+
+// Element c of row j of worker i is kept where a 16-bit number u is at least t = round(65536 p), and then multiplied by
+// 65536 / (65536 - t), so that the expectation is exact for the share that is really dropped. u is a half of a word of the
+// Philox4x32-10 block (Salmon, Moraes, Dror, Shaw, SC 2011) at counter (c / 8, j, i, call) under the seed's two halves as key:
+// word (c % 8) / 2, its low half where c is even. Any kernel finds any element's bit again from its place, so a mask is never
+// stored. Sixteen bits per element make one block serve eight, the elements of one 16-byte access: about 10 instructions an element,
+// against the 22 or so that a sweep which reads and writes 2 bytes an element has time for at the memory's rate.
+struct Drop {
+    uint32_t key[20];         // the ten rounds' keys
+    uint32_t threshold;       // t in the upper 16 bits; all ones: everything is dropped
+    float factor;             // 65536 / (65536 - t)
+    uint32_t call;            // added to *call_device
+    uint32_t worker;          // the number of the first worker
+    const int64_t* call_device;  // may be null
+    int32_t on;               // 0: t is 0, nothing is dropped
+};
+
+__device__ __forceinline__ uint32_t drop_call(const Drop& d) {
+    return d.call + (d.on && d.call_device ? (uint32_t)*d.call_device : 0u);
+}
+
+// The eight bits of columns 8 group ... 8 group + 7.
+__device__ __forceinline__ uint32_t drop_bits(const Drop& d, uint32_t group, uint32_t row, uint32_t worker, uint32_t call) {
+    uint32_t c0 = group, c1 = row, c2 = worker, c3 = call;
+#pragma unroll
+    for (int r = 0; r < 10; ++r) {
+        const uint64_t a = (uint64_t)0xD2511F53u * c0, b = (uint64_t)0xCD9E8D57u * c2;
+        c0 = (uint32_t)(b >> 32) ^ c1 ^ d.key[2 * r];
+        c1 = (uint32_t)b;
+        c2 = (uint32_t)(a >> 32) ^ c3 ^ d.key[2 * r + 1];
+        c3 = (uint32_t)a;
+    }
+    const uint32_t w[4] = {c0, c1, c2, c3}, t = d.threshold;
+    uint32_t bits = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if ((w[k] << 16) >= t) bits |= 1u << (2 * k);
+        if ((w[k] & 0xffff0000u) >= t) bits |= 2u << (2 * k);
+    }
+    return bits;
+}
+
+// Dropout of a lane's values of a span; the whole warp takes part.
+template <bool VEC>
+__device__ __forceinline__ void span_drop(const Drop& d, int c0, uint32_t row, uint32_t worker, uint32_t call, int lane, float (&v)[8]) {
+    const uint32_t bits = drop_bits(d, (uint32_t)(c0 >> 3) + lane, row, worker, call);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const bool keep = VEC ? (bits >> k) & 1u : (__shfl_sync(0xffffffffu, bits, k * 4 + (lane >> 3)) >> (lane & 7)) & 1u;
+        v[k] = keep ? v[k] * d.factor : 0.0f;
+    }
+}
+
+// Fills a Drop from the arguments of a call; false where they are out of range.
+inline bool make_drop(Drop& d, double p, uint64_t seed, uint32_t call, const int64_t* call_device, uint32_t worker) {
+    if (!(p >= 0.0 && p <= 1.0) || (reinterpret_cast<uintptr_t>(call_device) & 7u)) return false;
+    const uint32_t t = (uint32_t)(65536.0 * p + 0.5);
+    for (uint32_t r = 0; r < 10; ++r) {
+        d.key[2 * r] = (uint32_t)seed + r * 0x9E3779B9u;
+        d.key[2 * r + 1] = (uint32_t)(seed >> 32) + r * 0xBB67AE85u;
+    }
+    d.threshold = t < 65536u ? t << 16 : 0xffffffffu;
+    d.factor = t < 65536u ? (float)(65536.0 / (65536.0 - t)) : 0.0f;
+    d.call = call;
+    d.worker = worker;
+    d.call_device = call_device;
+    d.on = t > 0;
+    return true;
+}
+
+// ---- host ------------------------------------------------------------------------------------------------------------------
+
+enum : int32_t { kTypeF32 = 0, kTypeBF16 = 1, kTypeF16 = 2 };
+
+inline int type_bytes(int32_t type) { return type == kTypeF32 ? 4 : 2; }
+inline bool type_known(int32_t type) { return type >= kTypeF32 && type <= kTypeF16; }
+
+// A [n, rows, h] operand as the entry points take it.
+struct Rows {
+    const void* p;
+    int64_t worker_stride, row_stride;
+    int32_t type;
+    bool aligned() const {  // every row on a 16-byte boundary
+        const int64_t e = type_bytes(type);
+        return ((reinterpret_cast<uintptr_t>(p) | (uint64_t)(worker_stride * e) | (uint64_t)(row_stride * e)) & 15u) == 0;
+    }
+    bool element_aligned() const { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(type_bytes(type) - 1)) == 0; }
+};
+inline Rows packed(const void* p, int64_t rows, int64_t h, int32_t type) { return {p, rows * h, h, type}; }
+
+}  // namespace compams

@@ -49,6 +49,7 @@ class CompAMSOptimizer:
         places = [int(o) for o, size in zip(self.offsets, sizes) if size] + [self.d]
         self._places = (ctypes.c_int64 * len(places))(*places)
         self._addresses = (ctypes.c_void_p * len(self._pieces))()
+        self._leaves = None  # worker_parameters(): made when they are first asked for
         blocks = np.array([0, self.d], dtype=np.int64) if whole_vector else self.offsets
         with torch.cuda.device(dev):
             self.opt = CompAMS(self.n, self.d, blocks, compressor, k_ratio, lr, beta1, beta2, eps)
@@ -81,6 +82,34 @@ class CompAMSOptimizer:
                                                   len(addresses), stream), "compams_collect")
         for p in self.params:
             p.grad = None
+
+    def worker_parameters(self) -> List[torch.Tensor]:
+        """For models that run the n workers' micro-batches as one batch (the operators of .layers, or torch's batched products): per
+        parameter a leaf [n, *shape] whose n rows are all the parameter itself, so that they move with theta, and whose .grad keeps the
+        workers' gradients apart. The same leaves at every call; collect_all() takes their gradients."""
+        if self._leaves is None:
+            self._leaves = [self.theta[lo:hi].view(p.shape).expand(self.n, *p.shape).requires_grad_()
+                            for p, lo, hi in zip(self.params, self.offsets[:-1], self.offsets[1:])]
+        return self._leaves
+
+    def collect_all(self) -> None:
+        """All rows of G <- the gradients that worker_parameters() accumulated since the last call; they are cleared."""
+        leaves = self.worker_parameters()
+        dev = self.G.device
+        grads = []
+        for leaf, (_, nbytes) in zip((w for w in leaves if w.numel()), self._pieces):
+            g = leaf.grad
+            if g is not None and (g.dtype != torch.float32 or g.device != dev or not g.is_contiguous() or g.is_neg()):
+                g = g.to(dev, torch.float32).resolve_neg().contiguous()
+            grads.append((g, nbytes))
+        with torch.cuda.device(dev):
+            stream = torch.cuda.current_stream(dev).cuda_stream
+            for i in range(self.n):
+                self._addresses[:] = [None if g is None else g.data_ptr() + i * nbytes for g, nbytes in grads]
+                _check(load_library().compams_collect(self.G.data_ptr() + 4 * self.d * i, self._addresses, self._places,
+                                                      len(grads), stream), "compams_collect")
+        for leaf in leaves:
+            leaf.grad = None
 
     def step(self) -> None:
         self.opt.step(self.G, self.theta)
