@@ -482,18 +482,20 @@ int compams_norm_workspace_bytes(size_t* bytes, int32_t n, int64_t rows, int64_t
  *   a, b            device fp32, A [rank, in] and B [out, rank]: rows packed, row_stride apart; worker i's at i * worker_stride (0: one
  *                   for all). 1 <= rank <= 1024.
  *   t               device, packed fp32 [n, rows, rank]: receives dropout(x) A^T, which the backward pass takes.
+ *   workspace       device, 16-byte aligned, at least compams_adapter_workspace_bytes; used during the call's device work only.
  * The dropout is that of element (i, j, c) of x, as above.
  */
 int compams_adapter_forward(void* y, float* t, const void* x, const void* base, int32_t type, int32_t n, int64_t rows, int64_t in,
                             int64_t out, int32_t rank, int64_t x_worker_stride, int64_t x_row_stride, int64_t base_worker_stride,
                             int64_t base_row_stride, const float* a, int64_t a_worker_stride, int64_t a_row_stride, const float* b,
                             int64_t b_worker_stride, int64_t b_row_stride, float scale, double p, uint64_t seed, uint32_t call,
-                            const int64_t* call_device, uint32_t first_worker, void* cuda_stream);
+                            const int64_t* call_device, uint32_t first_worker, void* workspace, size_t workspace_bytes,
+                            void* cuda_stream);
 
 /*
  * Its gradients (base's is dy itself). dx: packed [n, rows, in]; da: packed fp32 [n, rank, in]; db: packed fp32 [n, out, rank]; each may
  * be null: not wanted. sum_workers: da [rank, in] and db [out, rank], summed over the workers. Sums run in a fixed order.
- *   workspace       device, 16-byte aligned, at least compams_adapter_workspace_bytes; used during the call's device work only.
+ *   workspace       as above.
  */
 int compams_adapter_backward(void* dx, float* da, float* db, int32_t sum_workers, const void* dy, const void* x, const float* t,
                              int32_t type, int32_t n, int64_t rows, int64_t in, int64_t out, int32_t rank, int64_t dy_worker_stride,
@@ -501,7 +503,9 @@ int compams_adapter_backward(void* dx, float* da, float* db, int32_t sum_workers
                              int64_t a_worker_stride, int64_t a_row_stride, const float* b, int64_t b_worker_stride,
                              int64_t b_row_stride, float scale, double p, uint64_t seed, uint32_t call, const int64_t* call_device,
                              uint32_t first_worker, void* workspace, size_t workspace_bytes, void* cuda_stream);
-int compams_adapter_workspace_bytes(size_t* bytes, int32_t n, int64_t rows, int64_t in, int64_t out, int32_t rank);
+/* shared: both worker strides of A and B are 0, or n is 1. sum_workers matters to the backward pass alone. */
+int compams_adapter_workspace_bytes(size_t* bytes, int32_t n, int64_t rows, int64_t in, int64_t out, int32_t rank, int32_t shared,
+                                    int32_t backward, int32_t sum_workers);
 
 /* Static strings (never null). */
 const char* compams_error_string(int status);

@@ -287,6 +287,11 @@ def _stacked(w: torch.Tensor) -> Tuple[int, int, int]:
     return (w.data_ptr(), w.stride(0), w.stride(1)) if w.dim() == 3 else (w.data_ptr(), 0, w.stride(0))
 
 
+def _shared(a: torch.Tensor, b: torch.Tensor) -> int:
+    """Whether all workers have one adapter, as the library counts it."""
+    return int(a.dim() == 2 or a.shape[0] == 1 or (a.stride(0) == 0 and b.stride(0) == 0))
+
+
 def _adapter_forward(x, base, a, b, scale, drop):
     n, rank, out = x.shape[0], a.shape[-2], b.shape[-2]
     y = torch.empty(*x.shape[:-1], out, dtype=x.dtype, device=x.device)
@@ -296,8 +301,9 @@ def _adapter_forward(x, base, a, b, scale, drop):
         z, zws, zrs = None, 0, 0
         if base is not None:
             z, _, zws, zrs = _rows(base)
+        work = _workspace("compams_adapter_workspace_bytes", x.device, n, rows, x.shape[-1], out, rank, _shared(a, b), 0, 0)
         _run("compams_adapter_forward", x.device, y.data_ptr(), t.data_ptr(), v.data_ptr(), _ptr(z), _TYPES[x.dtype], n, rows,
-             x.shape[-1], out, rank, ws, rs, zws, zrs, *_stacked(a), *_stacked(b), scale, *drop.args())
+             x.shape[-1], out, rank, ws, rs, zws, zrs, *_stacked(a), *_stacked(b), scale, *drop.args(), _ptr(work), work.numel())
     return y, t
 
 
@@ -322,7 +328,8 @@ class _AdapterFunction(torch.autograd.Function):
         if x.numel() and (needs_x or needs_a or needs_b):
             g, rows, gws, grs = _rows(dy)
             v, _, ws, rs = _rows(x)
-            work = _workspace("compams_adapter_workspace_bytes", x.device, n, rows, h, out, rank)
+            work = _workspace("compams_adapter_workspace_bytes", x.device, n, rows, h, out, rank, _shared(a, b), 1,
+                              0 if a.dim() == 3 else 1)
             _run("compams_adapter_backward", x.device, _ptr(dx), _ptr(da), _ptr(db), 0 if a.dim() == 3 else 1, g.data_ptr(),
                  v.data_ptr(), t.data_ptr(), _TYPES[x.dtype], n, rows, h, out, rank, gws, grs, ws, rs, *_stacked(a), *_stacked(b),
                  ctx.scale, *ctx.drop.args(), work.data_ptr(), work.numel())

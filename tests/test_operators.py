@@ -88,12 +88,12 @@ def test_norm_backward_refuses(lib, bad):
 
 def adapter_args(**kw):
     v = dict(y=A, t=A, x=A, base=A, type=1, n=2, rows=3, inn=8, out=8, rank=4, xws=24, xrs=8, bws=24, brs=8, a=A, aws=0, ars=8, b=A, bbws=0, bbrs=4,
-             scale=1.0, p=0.0, seed=1, call=0, call_device=None, worker=0, stream=None)
+             scale=1.0, p=0.0, seed=1, call=0, call_device=None, worker=0, work=A, bytes=1 << 30, stream=None)
     v.update(kw)
     return list(v.values())
 
 
-@pytest.mark.parametrize("bad", [dict(y=None), dict(t=None), dict(x=None), dict(a=None), dict(b=None), dict(type=4), dict(n=0), dict(rows=-1), dict(inn=0),
+@pytest.mark.parametrize("bad", [dict(y=None), dict(work=None), dict(bytes=16), dict(work=A + 8), dict(t=None), dict(x=None), dict(a=None), dict(b=None), dict(type=4), dict(n=0), dict(rows=-1), dict(inn=0),
                                  dict(out=0), dict(rank=0), dict(rank=1025), dict(p=2.0), dict(a=A + 2), dict(b=A + 1), dict(t=A + 2), dict(x=A + 1),
                                  dict(base=A + 1), dict(y=A + 1)])
 def test_adapter_forward_refuses(lib, bad):
@@ -124,5 +124,6 @@ def test_workspaces(lib):
     assert lib.compams_norm_workspace_bytes(ctypes.byref(need), 4, 100, 512) == 0 and need.value >= 4 * 2 * 512 * 4
     assert lib.compams_norm_workspace_bytes(None, 4, 100, 512) == -1
     assert lib.compams_norm_workspace_bytes(ctypes.byref(need), 0, 100, 512) == -1
-    assert lib.compams_adapter_workspace_bytes(ctypes.byref(need), 4, 100, 512, 256, 16) == 0 and need.value >= 4 * 100 * 16 * 4
-    assert lib.compams_adapter_workspace_bytes(ctypes.byref(need), 4, 100, 512, 256, 0) == -1
+    assert lib.compams_adapter_workspace_bytes(ctypes.byref(need), 4, 100, 512, 256, 16, 1, 1, 0) == 0 and need.value >= 4 * 100 * 16 * 4
+    assert lib.compams_adapter_workspace_bytes(ctypes.byref(need), 4, 1, 512, 256, 16, 0, 0, 0) == 0 and need.value == 0
+    assert lib.compams_adapter_workspace_bytes(ctypes.byref(need), 4, 100, 512, 256, 0, 1, 1, 0) == -1
