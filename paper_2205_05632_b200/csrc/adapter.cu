@@ -13,13 +13,18 @@
 // A product with an activation costs 2 rank operations for each element that is read once, so at the usual ranks it is bound by
 // memory, and the kernels are built around 16-byte loads of the activation that become matrix operands where they arrive, in
 // registers: a sum's terms and a product's columns may be numbered as one likes, so the eight neighbours that a lane loads are taken as
-// the places of the operand that this lane has to hold. No shared memory stands between memory and mma.sync; the factors wait in the
-// order of the lanes' registers ("frag") and come through the L1.
+// the places of the operand that this lane has to hold. No exchange between lanes stands between memory and mma.sync; the factors and t
+// wait in the order of the lanes' registers and come through the L1.
 //
 // Precision. mma.sync multiplies bf16 exactly and adds in fp32. An fp32 number is the sum of three bf16 numbers, its planes (8 bits
 // each, cut, not rounded: the rest after each cut is exact, nothing overflows); fp16 needs two and bf16 is one. Products of planes
 // i and j are formed for i + j <= 2, which leaves out less than 3 * 2^-24 of a product: as fp32 arithmetic does. Where the result is
 // a 16-bit number (y, dx) i + j <= 1 suffice: 3 * 2^-16 of a product, an eighth of half a step of fp16, 2^-6 of one of bf16.
+#include <cooperative_groups.h>
+#include <string.h>
+
+#include <type_traits>
+
 #include "context.h"
 #include "rows.cuh"
 
@@ -34,17 +39,19 @@ struct Factor {  // A or B^T
 struct AdapterArgs {
     const void* x;  // down, outer: the rows; up: the base (may be null)
     void* y;        // up: the result
-    const float* t;
-    float* out;     // down: t; outer: the result, or the partial sums [n, chunks, rank * h]
-    const uint4* frag;
+    const float* t; // the kernels for a few rows: t
+    float* out;     // down: t (may be null); outer: the result, or the partial sums [n, chunks, rank * h]
+    const uint4* frag;       // down, up: the factor's fragments
+    uint4* t_up;             // t as an operand of up: written by down, read by up
+    uint2* t_outer;          // t as an operand of outer: written by down (may be null), read by outer
     Factor f;
     int64_t x_ws, x_rs;
-    int64_t frag_ws;   // 16-byte words of a group's fragments
-    uint32_t rows, total;
-    uint32_t group_rows;  // rows that share a factor: a worker's, or all
-    uint32_t tiles;       // down: row tiles of a group; up: row chunks of a group
+    int64_t frag_ws;   // 16-byte words of a worker's fragments; 0: one factor for all
+    uint32_t rows;
+    uint32_t tiles;    // down: row tiles of a worker; up: row chunks of a worker
     int32_t h, rank;
-    uint32_t chunks;
+    uint32_t chunks;   // outer: row chunks of a worker
+    int32_t split;     // down: CTAs of a cluster, which share out the columns
     float scale;
     Drop drop;
 };
@@ -140,18 +147,54 @@ __host__ __device__ inline int64_t up_frag_words(int64_t h, int rank) {
     return (h + kUpColumns - 1) / kUpColumns * ((rank + 15) / 16) * kPlanes * 64;
 }
 
-// A block per 8 fragments; one lane writes its share of the planes of one fragment.
+// t as an operand, 16 rows of a worker at a time:
+//   up:    [16 rows][16 ranks][plane][lane g, t] = rows g and g + 8, ranks 4 t ... 4 t + 3
+//   outer: [16 rows][8 ranks][plane][lane g, t] = rows 4 t ... 4 t + 3, rank g
+__host__ __device__ inline int64_t t_up_words(int64_t rows, int rank) {  // of 16 bytes, a worker's
+    return (rows + 15) / 16 * ((rank + 15) / 16) * kPlanes * 32;
+}
+__host__ __device__ inline int64_t t_outer_words(int64_t rows, int rank) {  // of 8 bytes, a worker's
+    return (rows + 15) / 16 * ((rank + 7) / 8) * kPlanes * 32;
+}
+
+// Four numbers of t as an operand of outer.
+__device__ __forceinline__ void store_t_outer(uint2* at, const float (&v)[4]) {
+    uint32_t lo[kPlanes], hi[kPlanes];
+    split2<kPlanes>(v[0], v[1], lo);
+    split2<kPlanes>(v[2], v[3], hi);
+#pragma unroll
+    for (int p = 0; p < kPlanes; ++p) at[p * 32] = make_uint2(lo[p], hi[p]);
+}
+
+// A warp per fragment; a lane writes its share of the planes.
 //   down: [column block][8 ranks][plane][lane g, t] = rank 8 b + g, columns 8 t ... 8 t + 7
 //   up:   [column block][16 ranks][plane][half][lane g, t] = for two of the four products q, column 8 (g / 2) + 2 q + g % 2, ranks 4 t ... 4 t + 3
+// and, in the backward pass, the forward pass's t for outer.
 struct PrepareArgs {
     Factor down, up;
     uint4 *down_frag, *up_frag;
+    const float* t;
+    uint2* t_outer;
     int32_t down_h, up_h, rank;
-    uint32_t down_count, up_count;  // fragments of a group
+    uint32_t rows;
+    uint32_t down_count, up_count, t_count;  // fragments of a worker
+    int32_t shared;  // the factors' fragments are those of worker 0
 };
 __global__ void __launch_bounds__(256) adapter_prepare_kernel(const __grid_constant__ PrepareArgs a) {
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     uint32_t at = blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (at < a.t_count) {
+        const int ranks = (a.rank + 7) / 8, j = (int)(at % ranks) * 8 + g;
+        const uint32_t row = at / ranks * 16 + 4 * t;
+        float v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            v[k] = row + k < a.rows && j < a.rank ? __ldg(a.t + ((int64_t)blockIdx.y * a.rows + row + k) * a.rank + j) : 0.0f;
+        store_t_outer(a.t_outer + blockIdx.y * t_outer_words(a.rows, a.rank) + (int64_t)at * kPlanes * 32 + lane, v);
+        return;
+    }
+    at -= a.t_count;
+    if (a.shared && blockIdx.y) return;
     if (at < a.down_count) {
         const int ranks = (a.rank + 7) / 8, j = (int)(at % ranks) * 8 + g, c = (int)(at / ranks) * kDownColumns + 8 * t;
         const float* f = a.down.p + (int64_t)blockIdx.y * a.down.ws;
@@ -192,111 +235,256 @@ __global__ void __launch_bounds__(256) adapter_prepare_kernel(const __grid_const
     }
 }
 
+// ---- rings of asynchronous copies ------------------------------------------------------------------------------------------
+
+// Every lane copies what it will need of an activation into places of shared memory that it alone reads, kStages - 1 steps ahead, so
+// that no registers wait for memory; place: [stage][slot][thread], 16 bytes each. What the warps of a CTA share (the factor's fragments,
+// t's) is copied by all of them into a stage of the same step. Per step: wait for the step's copies, a barrier, behind which the stage of
+// the step before is free and is filled again, then the products.
+constexpr int kStages = 3;
+template <int SLOTS>
+__device__ __forceinline__ uint4* ring_at(char* smem, int stage, int slot) {
+    return reinterpret_cast<uint4*>(smem) + (stage * SLOTS + slot) * 256 + threadIdx.x;
+}
+__device__ __forceinline__ void copy16(void* shared, const void* global, bool there) {  // zeros where it is not
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(shared)), "l"(global),
+                 "r"(there ? 16 : 0)
+                 : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+template <int N, typename T>
+__device__ __forceinline__ Raw8<T> ring_raw(char* smem, int stage, int slot) {  // slot: of the first 16 bytes
+    Raw8<T> r;
+    uint4 q[sizeof(r) / 16];
+#pragma unroll
+    for (int k = 0; k < (int)sizeof(r) / 16; ++k) q[k] = *ring_at<N>(smem, stage, slot + k);
+    memcpy(&r, q, sizeof(r));
+    return r;
+}
+
 // ---- down ------------------------------------------------------------------------------------------------------------------
 
-// A CTA per 16 MT rows and 8 NT rank indices; its warps take every eighth block of 32 columns, so that the CTA reads 512 bytes of a row
-// at a time, and join their sums at the end, in order.
-template <typename T, bool VEC, int MT, int NT>
-__global__ void __launch_bounds__(256) adapter_down_kernel(const __grid_constant__ AdapterArgs a) {
-    __shared__ float joined[8][16][NT * 8 + 1];
+// A warp takes MT blocks of 16 rows and 8 NT rank indices; WK warps of a CTA share out the columns of their rows, and so do the CTAs of a
+// cluster. With many rows WK is 1 and the eight warps, of different rows, share the fragments, which pass through shared memory. A few
+// rows need WK = 8 to occupy the SMs; every warp then fetches fragments of its own. The sums of the warps and of the CTAs are
+// joined in their order, through the CTAs' shared memory, and leave as t and as the operands that up and outer take.
+template <typename T>
+__host__ __device__ constexpr int down_step() { return sizeof(T) == 4 ? 1 : 2; }  // blocks of 32 columns in a step
+template <typename T, bool VEC, int NT, int WK, int MT>
+__host__ __device__ constexpr int down_ring() { return VEC ? kStages * 2 * MT * down_step<T>() * (int)sizeof(Raw8<T>) * 256 : 0; }
+template <typename T, bool VEC, int NT, int WK, int MT>
+__host__ __device__ constexpr int down_shared() {
+    const int rings = down_ring<T, VEC, NT, WK, MT>() + (WK == 1 ? kStages * down_step<T>() * NT * kPlanes * 512 : 0);
+    const int join = (8 * MT + 1) * 16 * (NT * 8 + 1) * 4;
+    return rings > join ? rings : join;
+}
+
+template <typename T, bool VEC, int NT, int WK, int MT>
+__global__ void __launch_bounds__(256, MT == 1 ? 2 : 1) adapter_down_kernel(const __grid_constant__ AdapterArgs a) {
+    extern __shared__ __align__(16) char smem[];
     dependency_wait();
-    constexpr int PX = Planes<T>::count;
+    constexpr int PX = Planes<T>::count, KB = down_step<T>(), S16 = (int)sizeof(Raw8<T>) / 16, SLOTS = 2 * MT * KB * S16;
+    constexpr int BLOCKS = 8 * MT / WK;  // of 16 rows, a CTA's
+    uint4* stages = reinterpret_cast<uint4*>(smem + down_ring<T, VEC, NT, WK, MT>());
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-    const uint32_t group = blockIdx.x / a.tiles, row0 = (blockIdx.x - group * a.tiles) * 16 * MT;
+    const uint32_t tile = blockIdx.x / a.split, i = tile / a.tiles;
+    const int part = (int)(blockIdx.x - tile * a.split);
+    const uint32_t block0 = (tile - i * a.tiles) * BLOCKS;  // the first block of rows
+    const uint32_t row0 = (block0 + warp / WK * MT) * 16;
     const int n0 = blockIdx.y * NT, ntiles = (a.rank + 7) / 8;
     const uint32_t call = drop_call(a.drop);
     const T* row[MT][2];
-    uint32_t wi[MT][2], wj[MT][2];
     bool in[MT][2];
 #pragma unroll
     for (int q = 0; q < MT; ++q)
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             const uint32_t r = row0 + q * 16 + half * 8 + g;
-            in[q][half] = r < a.group_rows;
-            const uint32_t m = group * a.group_rows + (in[q][half] ? r : 0);
-            wi[q][half] = m / a.rows;
-            wj[q][half] = m - wi[q][half] * a.rows;
-            row[q][half] = (const T*)a.x + (int64_t)wi[q][half] * a.x_ws + (int64_t)wj[q][half] * a.x_rs;
+            in[q][half] = r < a.rows;
+            row[q][half] = (const T*)a.x + (int64_t)i * a.x_ws + (int64_t)(in[q][half] ? r : 0) * a.x_rs;
         }
-    const uint4* frag = a.frag + (int64_t)group * a.frag_ws + lane;
-    const int blocks = (a.h + kDownColumns - 1) / kDownColumns;
+    const uint4* frag = a.frag + (int64_t)i * a.frag_ws;
+    const int blocks = (a.h + kDownColumns - 1) / kDownColumns, steps = (blocks + KB - 1) / KB, stride = a.split * WK;
     float acc[MT][NT][4] = {};
-    Raw8<T> next[MT][2];
-#pragma unroll
-    for (int q = 0; q < MT; ++q)
-#pragma unroll
-        for (int half = 0; half < 2; ++half)
-            next[q][half] = raw_columns<T, VEC>(row[q][half], warp * kDownColumns + 8 * t, in[q][half] ? a.h : 0);
-    for (int b = warp; b < blocks; b += 8) {
-        uint32_t w[MT][2][PX][4];
+    Raw8<T> next[MT][2][KB];
+    auto fetch = [&](int step, int stage) {
 #pragma unroll
         for (int q = 0; q < MT; ++q)
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const Raw8<T> now = next[q][half];
-                next[q][half] = raw_columns<T, VEC>(row[q][half], (b + 8) * kDownColumns + 8 * t, in[q][half] ? a.h : 0);
-                uint32_t bits = 0xffu;
-                if (a.drop.on) bits = drop_bits(a.drop, b * (kDownColumns / 8) + t, wj[q][half], a.drop.worker + wi[q][half], call);
-                raw_planes<T>(now, a.drop.on, bits, w[q][half]);
-            }
+            for (int half = 0; half < 2; ++half)
 #pragma unroll
-        for (int j = 0; j < NT; ++j) {
-            if (n0 + j >= ntiles) break;
-            uint4 f[kPlanes];
+                for (int k = 0; k < KB; ++k) {
+                    const int c = (step * KB + k) * kDownColumns + 8 * t;
+                    const bool there = step < steps && in[q][half] && c < a.h;
+                    if constexpr (VEC) {
 #pragma unroll
-            for (int p = 0; p < kPlanes; ++p) f[p] = frag[((int64_t)(b * ntiles + n0 + j) * kPlanes + p) * 32];
-#pragma unroll
-            for (int q = 0; q < MT; ++q) {
-                float c[4];
-                bool first = true;
-#pragma unroll
-                for (int sum = kPlanes - 1; sum >= 0; --sum)  // the planes' indices together: the smallest products first
-#pragma unroll
-                    for (int px = 0; px < PX; ++px) {
-                        const int p = sum - px;
-                        if (p < 0) break;
-                        if (first) mma_first(c, w[q][0][px][0], w[q][1][px][0], w[q][0][px][1], w[q][1][px][1], f[p].x, f[p].y);
-                        else mma(c, w[q][0][px][0], w[q][1][px][0], w[q][0][px][1], w[q][1][px][1], f[p].x, f[p].y);
-                        mma(c, w[q][0][px][2], w[q][1][px][2], w[q][0][px][3], w[q][1][px][3], f[p].z, f[p].w);
-                        first = false;
+                        for (int v = 0; v < S16; ++v)
+                            copy16(ring_at<SLOTS>(smem, stage, ((q * 2 + half) * KB + k) * S16 + v),
+                                   there ? reinterpret_cast<const char*>(row[q][half] + c) + 16 * v : a.x, there);
+                    } else {
+                        next[q][half][k] = raw_columns<T, false>(row[q][half], c, there ? a.h : 0);
                     }
+                }
+    };
+    auto fetch_shared = [&](int step, int stage) {
+        if constexpr (WK == 1) {
+            uint4* to = stages + stage * (KB * NT * kPlanes * 32);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) acc[q][j][k] += c[k];
+            for (int e = threadIdx.x; e < KB * NT * kPlanes * 32; e += 256) {
+                const int k = e / (NT * kPlanes * 32), rest = e - k * (NT * kPlanes * 32), b = step * KB + k;
+                if (b < blocks && n0 + rest / (kPlanes * 32) < ntiles) copy16(to + e, frag + (int64_t)(b * ntiles + n0) * kPlanes * 32 + rest, true);
+            }
+        }
+        copies_commit();
+    };
+    const int first = part * WK + warp % WK;
+    if constexpr (VEC) {
+        for (int s = 0; s < kStages - 1; ++s) {
+            fetch(first + s * stride, s);
+            fetch_shared(first + s * stride, s);
+        }
+    } else {
+        fetch(first, 0);
+        for (int s = 0; s < kStages - 1; ++s) fetch_shared(first + s * stride, s);
+    }
+    int stage = 0;
+    for (int step = first; step < steps; step += stride) {
+        copies_wait<kStages - 2>();
+        if constexpr (WK == 1) __syncthreads();  // (the steps of all warps are the same)
+        else __syncwarp();
+        const int behind = stage == 0 ? kStages - 1 : stage - 1;
+        uint32_t w[MT][2][KB][PX][4];
+#pragma unroll
+        for (int q = 0; q < MT; ++q)
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int k = 0; k < KB; ++k) {
+                    Raw8<T> now;
+                    if constexpr (VEC) now = ring_raw<SLOTS, T>(smem, stage, ((q * 2 + half) * KB + k) * S16);
+                    else now = next[q][half][k];
+                    uint32_t bits = 0xffu;
+                    if (a.drop.on)
+                        bits = drop_bits(a.drop, (step * KB + k) * (kDownColumns / 8) + t, row0 + q * 16 + half * 8 + g, a.drop.worker + i,
+                                         call);
+                    raw_planes<T>(now, a.drop.on, bits, w[q][half][k]);
+                }
+        if constexpr (VEC) fetch(step + (kStages - 1) * stride, behind);
+        else fetch(step + stride, 0);
+        fetch_shared(step + (kStages - 1) * stride, behind);
+        const uint4* here = stages + stage * (KB * NT * kPlanes * 32) + lane;
+        stage = stage + 1 == kStages ? 0 : stage + 1;
+#pragma unroll
+        for (int k = 0; k < KB; ++k) {
+            const int b = step * KB + k;
+            if (b >= blocks) break;
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                if (n0 + j >= ntiles) break;
+                uint4 f[kPlanes];
+#pragma unroll
+                for (int p = 0; p < kPlanes; ++p)
+                    f[p] = WK == 1 ? here[((k * NT + j) * kPlanes + p) * 32] : frag[((int64_t)(b * ntiles + n0 + j) * kPlanes + p) * 32 + lane];
+#pragma unroll
+                for (int q = 0; q < MT; ++q) {
+                    float c[4];
+                    bool start = true;
+#pragma unroll
+                    for (int sum = kPlanes - 1; sum >= 0; --sum)  // the planes' indices together: the smallest products first
+#pragma unroll
+                        for (int px = 0; px < PX; ++px) {
+                            const int p = sum - px;
+                            if (p < 0) break;
+                            if (start) mma_first(c, w[q][0][k][px][0], w[q][1][k][px][0], w[q][0][k][px][1], w[q][1][k][px][1], f[p].x, f[p].y);
+                            else mma(c, w[q][0][k][px][0], w[q][1][k][px][0], w[q][0][k][px][1], w[q][1][k][px][1], f[p].x, f[p].y);
+                            mma(c, w[q][0][k][px][2], w[q][1][k][px][2], w[q][0][k][px][3], w[q][1][k][px][3], f[p].z, f[p].w);
+                            start = false;
+                        }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[q][j][e] += c[e];
+                }
             }
         }
     }
-    const float scale = a.scale * (a.drop.on ? a.drop.factor : 1.0f);
+    // joined[warp][MT][row][rank], then whole[row][rank] of one block of rows
+    constexpr int L = NT * 8 + 1, B = 16 * L;
+    float* joined = reinterpret_cast<float*>(smem);
+    float* whole = joined + 8 * MT * B;
+    copies_wait<0>();
+    __syncthreads();  // the rings' memory is taken over
 #pragma unroll
-    for (int q = 0; q < MT; ++q) {
-        if (q) __syncthreads();
+    for (int q = 0; q < MT; ++q)
 #pragma unroll
         for (int j = 0; j < NT; ++j)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) joined[warp][g + (k >> 1) * 8][j * 8 + 2 * t + (k & 1)] = acc[q][j][k];
-        __syncthreads();
-        for (int e = threadIdx.x; e < 16 * NT * 8; e += 256) {
-            const int r = e / (NT * 8), j = e - r * (NT * 8);
-            const uint32_t at = row0 + q * 16 + r;
-            if (at < a.group_rows && n0 * 8 + j < a.rank) {
-                float s = 0.0f;
+            for (int e = 0; e < 4; ++e) joined[(warp * MT + q) * B + (g + (e >> 1) * 8) * L + j * 8 + 2 * t + (e & 1)] = acc[q][j][e];
+    __syncthreads();
+    if (WK > 1) {
+        static_assert(WK == 1 || MT == 1, "");
+        for (int e = threadIdx.x; e < B; e += 256) {
+            float v = joined[e];
 #pragma unroll
-                for (int w = 0; w < 8; ++w) s += joined[w][r][j];
-                a.out[((int64_t)group * a.group_rows + at) * a.rank + n0 * 8 + j] = scale * s;
-            }
+            for (int w = 1; w < WK; ++w) v += joined[w * B + e];
+            joined[e] = v;
         }
     }
+    cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
+    cluster.sync();
+    const float scale = a.scale * (a.drop.on ? a.drop.factor : 1.0f);
+    const int ranks = (a.rank + 15) / 16;
+    for (int b = part; b < BLOCKS; b += a.split) {
+        const uint32_t block = block0 + b;
+        if (block * 16 >= a.rows) break;
+        for (int e = threadIdx.x; e < B; e += 256) {
+            float v = 0.0f;
+            for (int s = 0; s < a.split; ++s) v += cluster.map_shared_rank(joined, s)[b * WK * B + e];
+            whole[e] = scale * v;
+        }
+        __syncthreads();
+        if (a.out)
+            for (int e = threadIdx.x; e < 16 * NT * 8; e += 256) {
+                const int r = e / (NT * 8), j = e - r * (NT * 8);
+                if (block * 16 + r < a.rows && n0 * 8 + j < a.rank)
+                    a.out[((int64_t)i * a.rows + block * 16 + r) * a.rank + n0 * 8 + j] = whole[r * L + j];
+            }
+        for (int q = warp; q < (NT + 1) / 2; q += 8) {  // 16 rank indices each
+            if (n0 / 2 + q >= ranks) break;
+            uint32_t v[2][2][kPlanes];  // [rows g, g + 8][pair of ranks]
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int pair = 0; pair < 2; ++pair) {
+                    const int j = q * 16 + 4 * t + 2 * pair;
+                    const float* at = whole + (g + half * 8) * L + j;
+                    split2<kPlanes>(j < NT * 8 ? at[0] : 0.0f, j < NT * 8 ? at[1] : 0.0f, v[half][pair]);
+                }
+            uint4* out = a.t_up + i * t_up_words(a.rows, a.rank) + ((int64_t)block * ranks + n0 / 2 + q) * kPlanes * 32 + lane;
+#pragma unroll
+            for (int p = 0; p < kPlanes; ++p) out[p * 32] = make_uint4(v[0][0][p], v[1][0][p], v[0][1][p], v[1][1][p]);
+        }
+        if (a.t_outer)
+            for (int q = warp; q < NT; q += 8) {
+                if (n0 + q >= ntiles) break;
+                float v[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v[k] = whole[(4 * t + k) * L + q * 8 + g];
+                store_t_outer(a.t_outer + i * t_outer_words(a.rows, a.rank) + ((int64_t)block * ntiles + n0 + q) * kPlanes * 32 + lane, v);
+            }
+        __syncthreads();
+    }
+    cluster.sync();  // the others may still be reading
 }
 
-// A few rows that share a factor: bound by the factor, which is read once, in fp32 as it lies. A CTA per rank index.
+// A few rows to a worker: bound by the factor, which is read once, in fp32 as it lies. A CTA per worker and rank index.
 constexpr int kFewRows = 4;
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) adapter_down_few_kernel(const __grid_constant__ AdapterArgs a) {
     __shared__ float joined[8][kFewRows];
-    dependency_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, j = blockIdx.x;
-    const uint32_t group = blockIdx.y, call = drop_call(a.drop);
-    const float* f = a.f.p + (int64_t)group * a.f.ws + j * a.f.sj;
+    const uint32_t i = blockIdx.y, call = drop_call(a.drop);
+    const float* f = a.f.p + (int64_t)i * a.f.ws + j * a.f.sj;
     float acc[kFewRows] = {};
     for (int c0 = warp * kSpan; c0 < a.h; c0 += 8 * kSpan) {
         float w[8];
@@ -307,11 +495,10 @@ __global__ void __launch_bounds__(256) adapter_down_few_kernel(const __grid_cons
         }
 #pragma unroll
         for (int r = 0; r < kFewRows; ++r) {
-            if (r >= (int)a.group_rows) break;
-            const uint32_t m = group * a.group_rows + r, i = m / a.rows, jr = m - i * a.rows;
+            if (r >= (int)a.rows) break;
             float v[8];
-            span_load<T, VEC>((const T*)a.x + (int64_t)i * a.x_ws + (int64_t)jr * a.x_rs, c0, a.h, lane, v);
-            if (a.drop.on) span_drop<VEC>(a.drop, c0, jr, a.drop.worker + i, call, lane, v);
+            span_load<T, VEC>((const T*)a.x + (int64_t)i * a.x_ws + (int64_t)r * a.x_rs, c0, a.h, lane, v);
+            if (a.drop.on) span_drop<VEC>(a.drop, c0, r, a.drop.worker + i, call, lane, v);
 #pragma unroll
             for (int k = 0; k < 8; ++k)
                 if (span_column<VEC>(c0, lane, k) < a.h) acc[r] = fmaf(v[k], w[k], acc[r]);
@@ -324,126 +511,157 @@ __global__ void __launch_bounds__(256) adapter_down_few_kernel(const __grid_cons
         if (lane == 0) joined[warp][r] = acc[r];
     }
     __syncthreads();
-    if (threadIdx.x < kFewRows && threadIdx.x < a.group_rows) {
+    if (threadIdx.x < kFewRows && threadIdx.x < a.rows) {
         float s = 0.0f;
 #pragma unroll
         for (int w = 0; w < 8; ++w) s += joined[w][threadIdx.x];
-        a.out[((int64_t)group * a.group_rows + threadIdx.x) * a.rank + j] = a.scale * s;
+        a.out[((int64_t)i * a.rows + threadIdx.x) * a.rank + j] = a.scale * s;
     }
 }
 
 // ---- up --------------------------------------------------------------------------------------------------------------------
 
-// A warp per 32 columns goes through the rows of a chunk, 16 MT at a time; the eight warps of a CTA are neighbours and meet at the
-// same rows of t in the L1. PT: planes of t and of the factor.
-template <typename T, bool VEC, int MT, int PT>
+// A warp per 32 columns goes through the blocks of 16 rows of a chunk; the eight warps of a CTA are neighbours and share t, which passes
+// through shared memory. RB: blocks of 16 rank indices, whose fragments of the factor stay in registers (0: any number; fragments and t are
+// fetched again for each block of rows). PT: planes of t and of the factor.
+template <typename T, bool VEC, int RB, int PT>
+__host__ __device__ constexpr int up_ring() { return VEC ? kStages * 2 * (int)sizeof(Raw8<T>) * 256 : 0; }
+template <typename T, bool VEC, int RB, int PT>
+__host__ __device__ constexpr int up_shared() { return up_ring<T, VEC, RB, PT>() + kStages * RB * PT * 512; }
+
+template <typename T, bool VEC, int RB, int PT>
 __global__ void __launch_bounds__(256) adapter_up_kernel(const __grid_constant__ AdapterArgs a) {
+    extern __shared__ __align__(16) char smem[];
+    constexpr int S16 = (int)sizeof(Raw8<T>) / 16, SLOTS = 2 * S16;
     dependency_wait();
+    uint4* stages = reinterpret_cast<uint4*>(smem + up_ring<T, VEC, RB, PT>());
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const uint32_t group = blockIdx.y / a.tiles, chunk = blockIdx.y - group * a.tiles;
+    const uint32_t i = blockIdx.y / a.tiles, chunk = blockIdx.y - i * a.tiles;
     const int cb = blockIdx.x * 8 + (threadIdx.x >> 5), c = cb * kUpColumns + 8 * t;
-    if (cb * kUpColumns >= a.h) return;
-    const int ranks = (a.rank + 15) / 16;
-    const uint32_t steps = (a.group_rows + 16 * MT - 1) / (16 * MT);
-    const uint32_t s0 = (uint32_t)((uint64_t)steps * chunk / a.tiles), s1 = (uint32_t)((uint64_t)steps * (chunk + 1) / a.tiles);
+    const bool mine = cb * kUpColumns < a.h;  // a whole warp
+    const int ranks = RB ? RB : (a.rank + 15) / 16;
+    const uint32_t blocks = (a.rows + 15) / 16;
+    const uint32_t b0 = (uint32_t)((uint64_t)blocks * chunk / a.tiles), b1 = (uint32_t)((uint64_t)blocks * (chunk + 1) / a.tiles);
     const uint32_t call = drop_call(a.drop);
-    const uint4* frag = a.frag + (int64_t)group * a.frag_ws + (int64_t)cb * ranks * kPlanes * 64 + lane;
-    const bool four = (a.rank & 3) == 0 && (reinterpret_cast<uintptr_t>(a.t) & 15u) == 0;
-    for (uint32_t s = s0; s < s1; ++s) {
-        uint32_t m[MT][2], wi[MT][2], wj[MT][2];
-        bool in[MT][2];
-        Raw8<T> base[MT][2];
+    const uint4* frag = a.frag + (int64_t)i * a.frag_ws + (int64_t)(mine ? cb : 0) * ranks * kPlanes * 64 + lane;
+    const uint4* tt = a.t_up + i * t_up_words(a.rows, a.rank);
+    uint4 f[RB ? RB : 1][PT][2];
+    auto factor = [&](int r, uint4 (&to)[PT][2]) {
 #pragma unroll
-        for (int q = 0; q < MT; ++q)
+        for (int p = 0; p < PT; ++p) {
+            to[p][0] = frag[((int64_t)r * kPlanes + p) * 64];
+            to[p][1] = frag[((int64_t)r * kPlanes + p) * 64 + 32];
+        }
+    };
+    if constexpr (RB > 0)
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const uint32_t r = (s * MT + q) * 16 + half * 8 + g;
-                in[q][half] = r < a.group_rows;
-                m[q][half] = group * a.group_rows + (in[q][half] ? r : 0);
-                wi[q][half] = m[q][half] / a.rows;
-                wj[q][half] = m[q][half] - wi[q][half] * a.rows;
-                base[q][half] = raw_columns<T, VEC>((const T*)a.x + (int64_t)wi[q][half] * a.x_ws + (int64_t)wj[q][half] * a.x_rs, c,
-                                                    a.x && in[q][half] ? a.h : 0);
+        for (int r = 0; r < RB; ++r) factor(r, f[r]);
+    Raw8<T> next[2];
+    auto fetch = [&](uint32_t b, int stage) {
+        if constexpr (RB > 0) {
+#pragma unroll
+            for (int e = threadIdx.x; e < RB * PT * 32; e += 256) {
+                const int r = e / (PT * 32), rest = e - r * (PT * 32);
+                if (b < b1) copy16(stages + stage * (RB * PT * 32) + e, tt + ((int64_t)b * ranks + r) * kPlanes * 32 + rest, true);
             }
-        float acc[MT][4][4] = {};
-        for (int b = 0; b < ranks; ++b) {
-            uint32_t w[MT][2][2][PT];
-#pragma unroll
-            for (int q = 0; q < MT; ++q)
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const float* p = a.t + (int64_t)m[q][half] * a.rank + b * 16 + 4 * t;
-                    float v[4];
-                    if (four) {
-                        const float4 f = in[q][half] && b * 16 + 4 * t < a.rank ? *reinterpret_cast<const float4*>(p) : make_float4(0.f, 0.f, 0.f, 0.f);
-                        v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
-                    } else {
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) v[k] = in[q][half] && b * 16 + 4 * t + k < a.rank ? p[k] : 0.0f;
-                    }
-                    split2<PT>(v[0], v[1], w[q][half][0]);
-                    split2<PT>(v[2], v[3], w[q][half][1]);
-                }
-            uint4 f[PT][2];
-#pragma unroll
-            for (int p = 0; p < PT; ++p) {
-                f[p][0] = frag[((int64_t)b * kPlanes + p) * 64];
-                f[p][1] = frag[((int64_t)b * kPlanes + p) * 64 + 32];
-            }
-#pragma unroll
-            for (int q = 0; q < MT; ++q)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    float d[4] = {};
-                    float(&sum)[4] = PT == 3 ? d : acc[q][k];  // a 16-bit result can stand one running sum
-#pragma unroll
-                    for (int both = PT - 1; both >= 0; --both)
-#pragma unroll
-                        for (int pt = 0; pt <= both; ++pt) {
-                            const uint4 e = f[both - pt][k >> 1];
-                            mma(sum, w[q][0][0][pt], w[q][1][0][pt], w[q][0][1][pt], w[q][1][1][pt], k & 1 ? e.z : e.x, k & 1 ? e.w : e.y);
-                        }
-                    if (PT == 3)
-#pragma unroll
-                        for (int v = 0; v < 4; ++v) acc[q][k][v] += d[v];
-                }
         }
 #pragma unroll
-        for (int q = 0; q < MT; ++q)
+        for (int half = 0; half < 2; ++half) {
+            const uint32_t j = b * 16 + half * 8 + g;
+            const bool in = a.x && b < b1 && j < a.rows && c < a.h;
+            const T* from = (const T*)a.x + (int64_t)i * a.x_ws + (int64_t)(in ? j : 0) * a.x_rs;
+            if constexpr (VEC) {
+                if (a.x)
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                if (!in[q][half] || c >= a.h) continue;
-                float v[8];
-                raw_floats<T>(base[q][half], v);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) v[k] = fmaf(a.scale, acc[q][k >> 1][half * 2 + (k & 1)], v[k]);
-                if (a.drop.on) {
-                    const uint32_t bits = drop_bits(a.drop, (uint32_t)c >> 3, wj[q][half], a.drop.worker + wi[q][half], call);
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) v[k] = (bits >> k) & 1u ? v[k] * a.drop.factor : 0.0f;
-                }
-                T* y = (T*)a.y + (int64_t)m[q][half] * a.h + c;
-                if (VEC) {
-                    store8<T>(y, v);
-                } else {
-#pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        if (c + k < a.h) y[k] = from_float<T>(v[k]);
-                }
+                    for (int q = 0; q < S16; ++q)
+                        copy16(ring_at<SLOTS>(smem, stage, half * S16 + q), in ? reinterpret_cast<const char*>(from + c) + 16 * q : a.x, in);
+            } else {
+                next[half] = raw_columns<T, false>(from, c, in ? a.h : 0);
             }
+        }
+        copies_commit();
+    };
+    if constexpr (VEC) {
+        for (int s = 0; s < kStages - 1; ++s) fetch(b0 + s, s);
+    } else {
+        fetch(b0, 0);
+    }
+    int stage = 0;
+    for (uint32_t b = b0; b < b1; ++b) {
+        copies_wait<VEC ? kStages - 2 : 0>();
+        __syncthreads();
+        Raw8<T> base[2] = {};
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            if constexpr (VEC) {
+                if (a.x) base[half] = ring_raw<SLOTS, T>(smem, stage, half * S16);
+            } else {
+                base[half] = next[half];
+            }
+        }
+        const uint4* here = stages + stage * (RB * PT * 32) + lane;
+        if constexpr (VEC) fetch(b + kStages - 1, stage == 0 ? kStages - 1 : stage - 1);
+        else fetch(b + 1, stage + 1 == kStages ? 0 : stage + 1);
+        stage = stage + 1 == kStages ? 0 : stage + 1;
+        if (!mine) continue;
+        float acc[4][4] = {};
+#pragma unroll(RB ? RB : 1)
+        for (int r = 0; r < ranks; ++r) {
+            uint4 w[PT];
+            if constexpr (RB == 0) factor(r, f[0]);
+#pragma unroll
+            for (int p = 0; p < PT; ++p) w[p] = RB ? here[(r * PT + p) * 32] : tt[((int64_t)(b * ranks + r) * kPlanes + p) * 32 + lane];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                float d[4] = {};
+                float(&sum)[4] = PT == 3 ? d : acc[k];  // a 16-bit result can stand one running sum
+#pragma unroll
+                for (int both = PT - 1; both >= 0; --both)
+#pragma unroll
+                    for (int pt = 0; pt <= both; ++pt) {
+                        const uint4 e = f[RB ? r : 0][both - pt][k >> 1];
+                        mma(sum, w[pt].x, w[pt].y, w[pt].z, w[pt].w, k & 1 ? e.z : e.x, k & 1 ? e.w : e.y);
+                    }
+                if (PT == 3)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) acc[k][v] += d[v];
+            }
+        }
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const uint32_t j = b * 16 + half * 8 + g;
+            if (j >= a.rows || c >= a.h) continue;
+            float v[8];
+            raw_floats<T>(base[half], v);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = fmaf(a.scale, acc[k >> 1][half * 2 + (k & 1)], v[k]);
+            if (a.drop.on) {
+                const uint32_t bits = drop_bits(a.drop, (uint32_t)c >> 3, j, a.drop.worker + i, call);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] = (bits >> k) & 1u ? v[k] * a.drop.factor : 0.0f;
+            }
+            T* y = (T*)a.y + ((int64_t)i * a.rows + j) * a.h + c;
+            if (VEC) {
+                store8<T>(y, v);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (c + k < a.h) y[k] = from_float<T>(v[k]);
+            }
+        }
     }
 }
 
-// A few rows that share a factor: a warp per span of the columns, the factor read once in fp32.
+// A few rows to a worker: a lane per column, the factor read once in fp32.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) adapter_up_few_kernel(const __grid_constant__ AdapterArgs a) {
     dependency_wait();
     const int lane = threadIdx.x & 31, c0 = (blockIdx.x * 8 + (int)(threadIdx.x >> 5)) * 32;
-    const uint32_t group = blockIdx.y;
+    const uint32_t i = blockIdx.y;
     const int c = c0 + lane;
     if (c0 >= a.h) return;
-    const float* f = a.f.p + (int64_t)group * a.f.ws + c * a.f.sc;
-    const float* t = a.t + (int64_t)group * a.group_rows * a.rank;
+    const float* f = a.f.p + (int64_t)i * a.f.ws + c * a.f.sc;
+    const float* t = a.t + (int64_t)i * a.rows * a.rank;
     float acc[kFewRows] = {};
     const bool four = a.f.sj == 1 && ((reinterpret_cast<uintptr_t>(a.f.p) | (uint64_t)a.f.ws * 4 | (uint64_t)a.f.sc * 4) & 15u) == 0 && (a.rank & 3) == 0;
     if (c < a.h) {
@@ -460,118 +678,227 @@ __global__ void __launch_bounds__(256) adapter_up_few_kernel(const __grid_consta
             for (int r = 0; r < kFewRows; ++r)
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
-                    if (r < (int)a.group_rows && j + k < a.rank) acc[r] = fmaf(t[r * a.rank + j + k], w[k], acc[r]);
+                    if (r < (int)a.rows && j + k < a.rank) acc[r] = fmaf(t[r * a.rank + j + k], w[k], acc[r]);
         }
     }
     const uint32_t call = drop_call(a.drop);
 #pragma unroll
     for (int r = 0; r < kFewRows; ++r) {
-        if (r >= (int)a.group_rows) break;
-        const uint32_t m = group * a.group_rows + r, i = m / a.rows, j = m - i * a.rows;
+        if (r >= (int)a.rows) break;
         float v = a.scale * acc[r];
-        if (c < a.h && a.x) v += to_float(__ldg((const T*)a.x + (int64_t)i * a.x_ws + (int64_t)j * a.x_rs + c));
+        if (c < a.h && a.x) v += to_float(__ldg((const T*)a.x + (int64_t)i * a.x_ws + (int64_t)r * a.x_rs + c));
         if (a.drop.on) {
-            const uint32_t bits = drop_bits(a.drop, (uint32_t)c >> 3, j, a.drop.worker + i, call);
+            const uint32_t bits = drop_bits(a.drop, (uint32_t)c >> 3, r, a.drop.worker + i, call);
             v = (bits >> (c & 7)) & 1u ? v * a.drop.factor : 0.0f;
         }
-        if (c < a.h) ((T*)a.y)[(int64_t)m * a.h + c] = from_float<T>(v);
+        if (c < a.h) ((T*)a.y)[((int64_t)i * a.rows + r) * a.h + c] = from_float<T>(v);
     }
 }
 
 // ---- outer -----------------------------------------------------------------------------------------------------------------
 
-// A CTA per 128 columns, 8 NT rank indices and chunk of a worker's rows: two warps side by side, four that share out the rows and
-// join their sums in order. A lane loads eight neighbours of four rows; pairs of rows become the operand's pairs by byte permutes.
-constexpr int kOuterColumns = 128;
+// A CTA per 256 columns, 8 NT rank indices and chunk of a worker's rows: four warps side by side, two that share out the blocks of 16 rows
+// and join their sums. A lane takes eight neighbours of four rows; pairs of rows become the operand's pairs by byte permutes. The side by
+// side warps share t, which passes through shared memory.
+constexpr int kOuterColumns = 256;
+template <typename T, bool VEC, int NT>
+__host__ __device__ constexpr int outer_ring() { return VEC ? kStages * 4 * (int)sizeof(Raw8<T>) * 256 : 0; }
+template <typename T, bool VEC, int NT>
+__host__ __device__ constexpr int outer_shared() {
+    const int rings = outer_ring<T, VEC, NT>() + kStages * 2 * NT * kPlanes * 256, join = 4 * 4 * NT * 4 * 32 * 4;
+    return rings > join ? rings : join;
+}
 template <typename T, bool VEC, int NT>
 __global__ void __launch_bounds__(256) adapter_outer_kernel(const __grid_constant__ AdapterArgs a) {
-    constexpr int PX = Planes<T>::count;
-    __shared__ float joined[kOuterColumns][NT * 8 + 1];
+    extern __shared__ __align__(16) char smem[];
+    constexpr int PX = Planes<T>::count, S16 = (int)sizeof(Raw8<T>) / 16, SLOTS = 4 * S16;
     dependency_wait();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3, side = warp & 1, turn = warp >> 1;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3, side = warp & 3, turn = warp >> 2;
     const uint32_t i = blockIdx.y / a.chunks, chunk = blockIdx.y - i * a.chunks;
-    const int groups = (a.rank + NT * 8 - 1) / (NT * 8), column = blockIdx.x / groups, n0 = (blockIdx.x - column * groups) * NT * 8;
-    const int cc = column * kOuterColumns, c = cc + side * 64 + 8 * g;
-    const uint32_t steps = (a.rows + 15) / 16;
-    const uint32_t s0 = (uint32_t)((uint64_t)steps * chunk / a.chunks), s1 = (uint32_t)((uint64_t)steps * (chunk + 1) / a.chunks);
+    const int ntiles = (a.rank + 7) / 8, groups = (ntiles + NT - 1) / NT, column = blockIdx.x / groups;
+    const int n0 = (blockIdx.x - column * groups) * NT;
+    const int c = column * kOuterColumns + side * 64 + 8 * g;
+    const uint32_t blocks = (a.rows + 15) / 16;
+    const uint32_t s0 = (uint32_t)((uint64_t)blocks * chunk / a.chunks), s1 = (uint32_t)((uint64_t)blocks * (chunk + 1) / a.chunks);
     const uint32_t call = drop_call(a.drop);
     const T* x = (const T*)a.x + (int64_t)i * a.x_ws;
-    const float* tt = a.t + (int64_t)i * a.rows * a.rank + n0 + g;
+    const uint4* tt = reinterpret_cast<const uint4*>(a.t_outer + i * t_outer_words(a.rows, a.rank));
+    uint4* stages = reinterpret_cast<uint4*>(smem + outer_ring<T, VEC, NT>());
+    constexpr int STAGE = 2 * NT * kPlanes * 16;  // words of 16 bytes: the fragments of the two blocks of rows of a step
     float acc[4][NT][4] = {};
     Raw8<T> next[4];
-    float tnext[NT][4];
-    auto fetch = [&](uint32_t s) {
+    auto fetch = [&](uint32_t s, int stage) {  // s: the warp's block of rows
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const uint32_t j = s * 16 + 4 * t + r;
-            const bool in = s < s1 && j < a.rows;
-            next[r] = raw_columns<T, VEC>(x + (int64_t)(in ? j : 0) * a.x_rs, c, in ? a.h : 0);
+            const bool there = s < s1 && j < a.rows && c < a.h;
+            const T* from = x + (int64_t)(there ? j : 0) * a.x_rs;
+            if constexpr (VEC) {
 #pragma unroll
-            for (int q = 0; q < NT; ++q) tnext[q][r] = in && n0 + q * 8 + g < a.rank ? tt[(int64_t)j * a.rank + q * 8] : 0.0f;
+                for (int q = 0; q < S16; ++q)
+                    copy16(ring_at<SLOTS>(smem, stage, r * S16 + q), there ? reinterpret_cast<const char*>(from + c) + 16 * q : a.x, there);
+            } else {
+                next[r] = raw_columns<T, false>(from, c, there ? a.h : 0);
+            }
         }
     };
-    fetch(s0 + turn);
-    for (uint32_t s = s0 + turn; s < s1; s += 4) {
-        uint32_t w[4][PX][4], f[NT][2][kPlanes];
+    auto fetch_shared = [&](uint32_t s, int stage) {  // s: the first block of rows of the step
+#pragma unroll
+        for (int e = threadIdx.x; e < STAGE; e += 256) {
+            const int which = e / (STAGE / 2), rest = e - which * (STAGE / 2);
+            if (s + which < s1 && n0 + rest / (kPlanes * 16) < ntiles)
+                copy16(stages + stage * STAGE + e, tt + ((int64_t)(s + which) * ntiles + n0) * kPlanes * 16 + rest, true);
+        }
+        copies_commit();
+    };
+    if constexpr (VEC) {
+        for (int s = 0; s < kStages - 1; ++s) {
+            fetch(s0 + turn + 2 * s, s);
+            fetch_shared(s0 + 2 * s, s);
+        }
+    } else {
+        fetch(s0 + turn, 0);
+        for (int s = 0; s < kStages - 1; ++s) fetch_shared(s0 + 2 * s, s);
+    }
+    int stage = 0;
+    for (uint32_t first = s0; first < s1; first += 2) {
+        copies_wait<kStages - 2>();
+        __syncthreads();
+        const uint32_t s = first + turn;
+        const int behind = stage == 0 ? kStages - 1 : stage - 1;
+        uint32_t w[4][PX][4];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
+            Raw8<T> now;
+            if constexpr (VEC) now = ring_raw<SLOTS, T>(smem, stage, r * S16);
+            else now = next[r];
             uint32_t bits = 0xffu;
             if (a.drop.on) bits = drop_bits(a.drop, (uint32_t)c >> 3, s * 16 + 4 * t + r, a.drop.worker + i, call);
-            raw_planes<T>(next[r], a.drop.on, bits, w[r]);
+            raw_planes<T>(now, a.drop.on, bits, w[r]);
         }
+        if constexpr (VEC) fetch(s + 2 * (kStages - 1), behind);
+        else fetch(s + 2, 0);
+        fetch_shared(first + 2 * (kStages - 1), behind);
+        const uint2* here = reinterpret_cast<const uint2*>(stages + stage * STAGE + turn * (STAGE / 2)) + lane;
+        stage = stage + 1 == kStages ? 0 : stage + 1;
+        if (s >= s1) continue;
+        uint32_t e[4][PX][4];
 #pragma unroll
-        for (int q = 0; q < NT; ++q) {
-            split2<kPlanes>(tnext[q][0], tnext[q][1], f[q][0]);
-            split2<kPlanes>(tnext[q][2], tnext[q][3], f[q][1]);
-        }
-        fetch(s + 4);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            uint32_t e[PX][4];
+        for (int k = 0; k < 4; ++k)
 #pragma unroll
             for (int px = 0; px < PX; ++px)
 #pragma unroll
                 for (int pair = 0; pair < 4; ++pair)
-                    e[px][pair] = __byte_perm(w[pair & 2][px][k], w[(pair & 2) + 1][px][k], pair & 1 ? 0x7632 : 0x5410);
+                    e[k][px][pair] = __byte_perm(w[pair & 2][px][k], w[(pair & 2) + 1][px][k], pair & 1 ? 0x7632 : 0x5410);
 #pragma unroll
-            for (int q = 0; q < NT; ++q) {
+        for (int q = 0; q < NT; ++q) {
+            if (n0 + q >= ntiles) break;
+            uint2 f[kPlanes];
+#pragma unroll
+            for (int p = 0; p < kPlanes; ++p) f[p] = here[(q * kPlanes + p) * 32];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
                 float d[4];
-                bool first = true;
+                bool start = true;
 #pragma unroll
                 for (int both = kPlanes - 1; both >= 0; --both)
 #pragma unroll
                     for (int px = 0; px < PX; ++px) {
                         const int p = both - px;
                         if (p < 0) break;
-                        if (first) mma_first(d, e[px][0], e[px][1], e[px][2], e[px][3], f[q][0][p], f[q][1][p]);
-                        else mma(d, e[px][0], e[px][1], e[px][2], e[px][3], f[q][0][p], f[q][1][p]);
-                        first = false;
+                        if (start) mma_first(d, e[k][px][0], e[k][px][1], e[k][px][2], e[k][px][3], f[p].x, f[p].y);
+                        else mma(d, e[k][px][0], e[k][px][1], e[k][px][2], e[k][px][3], f[p].x, f[p].y);
+                        start = false;
                     }
 #pragma unroll
                 for (int v = 0; v < 4; ++v) acc[k][q][v] += d[v];
             }
         }
     }
-    for (int w = 0; w < 4; ++w) {
-        if (turn == w) {
+    copies_wait<0>();
+    __syncthreads();  // the rings' memory is taken over
+    float* joined = reinterpret_cast<float*>(smem) + side * 4 * NT * 4 * 32 + lane;
+    if (turn == 1)
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
+        for (int k = 0; k < 4; ++k)
 #pragma unroll
-                for (int q = 0; q < NT; ++q)
+            for (int q = 0; q < NT; ++q)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        float& at = joined[side * 64 + 8 * g + 2 * k + (e >> 1)][q * 8 + 2 * t + (e & 1)];
-                        at = w == 0 ? acc[k][q][e] : at + acc[k][q][e];
-                    }
-        }
-        __syncthreads();
-    }
+                for (int v = 0; v < 4; ++v) joined[((k * NT + q) * 4 + v) * 32] = acc[k][q][v];
+    __syncthreads();
+    if (turn == 1) return;
     const float scale = a.scale * (a.drop.on ? a.drop.factor : 1.0f);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int q = 0; q < NT; ++q)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) acc[k][q][v] = scale * (acc[k][q][v] + joined[((k * NT + q) * 4 + v) * 32]);
+    // a lane holds columns c ... c + 7 of two neighbouring rank indices
     float* out = a.out + (int64_t)blockIdx.y * a.rank * a.h;
-    const bool ranks_packed = a.f.sj == 1;
-    for (int e = threadIdx.x; e < kOuterColumns * NT * 8; e += 256) {
-        const int k = ranks_packed ? e / (NT * 8) : e % kOuterColumns, j = ranks_packed ? e % (NT * 8) : e / kOuterColumns;
-        if (cc + k < a.h && n0 + j < a.rank) out[(n0 + j) * a.f.sj + (cc + k) * a.f.sc] = scale * joined[k][j];
+    const bool ranks_packed = a.f.sj == 1, aligned = (reinterpret_cast<uintptr_t>(out) & 15u) == 0;
+#pragma unroll
+    for (int q = 0; q < NT; ++q) {
+        const int j = (n0 + q) * 8 + 2 * t;
+        if (j >= a.rank) break;
+        if (ranks_packed) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                if (c + k >= a.h) break;
+                float* at = out + (int64_t)(c + k) * a.f.sc + j;
+                if (aligned && !(a.rank & 1)) {
+                    *reinterpret_cast<float2*>(at) = make_float2(acc[k >> 1][q][(k & 1) * 2], acc[k >> 1][q][(k & 1) * 2 + 1]);
+                } else {
+                    at[0] = acc[k >> 1][q][(k & 1) * 2];
+                    if (j + 1 < a.rank) at[1] = acc[k >> 1][q][(k & 1) * 2 + 1];
+                }
+            }
+        } else {
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                if (j + r >= a.rank) break;
+                float* at = out + (int64_t)(j + r) * a.f.sj + c;
+                if (aligned && !(a.h & 3)) {
+#pragma unroll
+                    for (int k = 0; k < 8; k += 4)
+                        if (c + k < a.h)
+                            *reinterpret_cast<float4*>(at + k) = make_float4(acc[k >> 1][q][r], acc[k >> 1][q][2 + r], acc[(k >> 1) + 1][q][r],
+                                                                             acc[(k >> 1) + 1][q][2 + r]);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        if (c + k < a.h) at[k] = acc[k >> 1][q][(k & 1) * 2 + r];
+                }
+            }
+        }
+    }
+}
+
+// A few rows to a worker: a lane per column, bound by the gradient that it writes.
+template <typename T>
+__global__ void __launch_bounds__(256) adapter_outer_few_kernel(const __grid_constant__ AdapterArgs a) {
+    dependency_wait();
+    const int c = blockIdx.x * 256 + threadIdx.x;
+    const uint32_t i = blockIdx.y, call = drop_call(a.drop);
+    if (c >= a.h) return;
+    float v[kFewRows] = {};
+#pragma unroll
+    for (int r = 0; r < kFewRows; ++r) {
+        if (r >= (int)a.rows) break;
+        v[r] = to_float(__ldg((const T*)a.x + (int64_t)i * a.x_ws + (int64_t)r * a.x_rs + c));
+        if (a.drop.on) {
+            const uint32_t bits = drop_bits(a.drop, (uint32_t)c >> 3, r, a.drop.worker + i, call);
+            v[r] = (bits >> (c & 7)) & 1u ? v[r] * a.drop.factor : 0.0f;
+        }
+    }
+    const float* t = a.t + (int64_t)i * a.rows * a.rank;
+    float* out = a.out + (int64_t)i * a.rank * a.h;
+    for (int j = 0; j < a.rank; ++j) {
+        float s = 0.0f;
+#pragma unroll
+        for (int r = 0; r < kFewRows; ++r)
+            if (r < (int)a.rows) s = fmaf(t[r * a.rank + j], v[r], s);
+        out[j * a.f.sj + c * a.f.sc] = a.scale * s;
     }
 }
 
@@ -602,17 +929,18 @@ struct AdapterShape {
     uint32_t total() const { return (uint32_t)(n * rows); }
 };
 
-// Whether the rows that share a factor are few enough for the kernels that read the factor as it lies: with a tile of 16 rows of which
-// four are there, three quarters of the products are of zeros, and the fragments are written and read again for them.
-bool few(const AdapterShape& z, bool shared) { return (shared ? (int64_t)z.n * z.rows : z.rows) <= kFewRows; }
+// Whether a worker's rows are few enough for the kernels that read the factor as it lies: with a tile of 16 rows of which four are
+// there, three quarters of the products are of zeros, and the fragments are written and read again for them.
+bool few(const AdapterShape& z) { return z.rows <= kFewRows; }
 
-int outer_ranks(int rank) { return rank <= 8 ? 1 : rank <= 16 ? 2 : 4; }  // NT
+int outer_ranks(int rank) { return rank <= 8 ? 1 : rank <= 16 ? 2 : rank <= 32 ? 4 : 8; }  // NT
 
-// Chunks of a worker's rows: as many as give each SM about four CTAs, of 64 rows at least.
+// Chunks of a worker's rows: as many as give each SM about two CTAs, of 64 rows at least.
 uint32_t outer_chunks(const AdapterShape& z, int64_t h) {
+    if (few(z)) return 1;
     const int nt = outer_ranks(z.rank) * 8;
     const int64_t tiles = (h + kOuterColumns - 1) / kOuterColumns * ((z.rank + nt - 1) / nt) * z.n;
-    int64_t c = 148 * 4 / tiles;
+    int64_t c = (148 * 2 + tiles - 1) / tiles;
     const int64_t most = (z.rows + 63) / 64;
     if (c > most) c = most;
     if (c > 65535 / z.n) c = 65535 / z.n;
@@ -623,124 +951,214 @@ int64_t outer_floats(const AdapterShape& z, int64_t h, bool sum_workers) {
     return c == 1 && (!sum_workers || z.n == 1) ? 0 : (int64_t)z.n * c * z.rank * h;
 }
 
+template <int V>
+using Int = std::integral_constant<int, V>;
 template <typename F>
 int by_type(int32_t type, F f) {
     return type == kTypeF32 ? f(float()) : type == kTypeBF16 ? f(__nv_bfloat16()) : f(__half());
 }
 int launched(cudaError_t e, const char* what) { return e == cudaSuccess ? COMPAMS_OK : cuda_fail(e, what); }
 
-AdapterArgs arguments(const AdapterShape& z, Rows x, int64_t h, bool shared, float scale, const Drop& d) {
+// A launch behind another of the same call (or the first), with dynamic shared memory and a cluster along x.
+template <typename... KArgs, typename... Args>
+cudaError_t launch_next(void (*kernel)(KArgs...), dim3 grid, int cluster, size_t shared, bool first, cudaStream_t stream, Args... args) {
+    if (shared > 48 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared);
+        if (e != cudaSuccess) return e;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(256);
+    cfg.dynamicSmemBytes = shared;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    int count = 0;
+    if (!first) {
+        attr[count].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[count++].val.programmaticStreamSerializationAllowed = 1;
+    }
+    if (cluster > 1) {
+        attr[count].id = cudaLaunchAttributeClusterDimension;
+        attr[count].val.clusterDim.x = (unsigned)cluster;
+        attr[count].val.clusterDim.y = 1;
+        attr[count++].val.clusterDim.z = 1;
+    }
+    cfg.attrs = attr;
+    cfg.numAttrs = count;
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
+}
+
+// Where t goes to and comes from: fp32, and the operands of up and outer.
+struct Low {
+    float* t;
+    uint4* up;
+    uint2* outer;
+};
+
+AdapterArgs arguments(const AdapterShape& z, Rows x, int64_t h, const Low& low, float scale, const Drop& d) {
     AdapterArgs a = {};
-    a.x = x.p; a.x_ws = x.worker_stride; a.x_rs = x.row_stride; a.rows = (uint32_t)z.rows; a.total = z.total();
-    a.group_rows = shared ? a.total : a.rows;
+    a.x = x.p; a.x_ws = x.worker_stride; a.x_rs = x.row_stride; a.rows = (uint32_t)z.rows;
+    a.t = low.t; a.t_up = low.up; a.t_outer = low.outer;
     a.h = (int32_t)h; a.rank = z.rank; a.scale = scale; a.drop = d;
     return a;
 }
 
 int prepare(const AdapterShape& z, bool shared, Factor down, int64_t down_h, uint4* down_frag, Factor up, int64_t up_h, uint4* up_frag,
-            cudaStream_t stream) {
-    PrepareArgs p = {down, up, down_frag, up_frag, (int32_t)down_h, (int32_t)up_h, z.rank, 0, 0};
+            const float* t, uint2* t_outer, cudaStream_t stream) {
+    PrepareArgs p = {down, up, down_frag, up_frag, t, t_outer, (int32_t)down_h, (int32_t)up_h, z.rank, (uint32_t)z.rows, 0, 0, 0, shared};
     if (down_frag) p.down_count = (uint32_t)((down_h + kDownColumns - 1) / kDownColumns * ((z.rank + 7) / 8));
     if (up_frag) p.up_count = (uint32_t)((up_h + kUpColumns - 1) / kUpColumns * ((z.rank + 15) / 16));
-    const uint64_t ctas = ((uint64_t)p.down_count + p.up_count + 7) / 8;
+    if (t_outer) p.t_count = (uint32_t)((z.rows + 15) / 16 * ((z.rank + 7) / 8));
+    const uint64_t ctas = ((uint64_t)p.down_count + p.up_count + p.t_count + 7) / 8;
     if (ctas > 0x0fffffffu) return COMPAMS_ERR_TOO_LARGE;
-    return launched(launch_plain(adapter_prepare_kernel, dim3((uint32_t)ctas, shared ? 1 : (uint32_t)z.n), dim3(256), 0, stream, p),
-                    "adapter_prepare");
+    const uint32_t workers = shared && !t_outer ? 1 : (uint32_t)z.n;
+    return launched(launch_next(adapter_prepare_kernel, dim3((uint32_t)ctas, workers), 1, 0, true, stream, p), "adapter_prepare");
 }
 
-int down(float* out, Rows x, const AdapterShape& z, int64_t h, bool shared, Factor f, const uint4* frag, float scale, const Drop& d,
+int down(Low low, Rows x, const AdapterShape& z, int64_t h, bool shared, Factor f, const uint4* frag, float scale, const Drop& d,
          cudaStream_t stream) {
-    AdapterArgs a = arguments(z, x, h, shared, scale, d);
-    a.out = out; a.f = f; a.frag = frag; a.frag_ws = shared ? 0 : down_frag_words(h, z.rank);
-    const uint32_t groups = shared ? 1 : (uint32_t)z.n;
+    AdapterArgs a = arguments(z, x, h, low, scale, d);
+    a.out = low.t; a.f = f; a.frag = frag; a.frag_ws = shared ? 0 : down_frag_words(h, z.rank);
     const bool vec = h % 8 == 0 && x.aligned();
     return by_type(x.type, [&](auto t) {
         using T = decltype(t);
         if (!frag) {
             auto kernel = vec ? adapter_down_few_kernel<T, true> : adapter_down_few_kernel<T, false>;
-            return launched(launch_plain(kernel, dim3((uint32_t)z.rank, groups), dim3(256), 0, stream, a), "adapter_down");
+            return launched(launch_next(kernel, dim3((uint32_t)z.rank, (uint32_t)z.n), 1, 0, true, stream, a), "adapter_down");
         }
         const int ntiles = (z.rank + 7) / 8;
-        auto go = [&](auto kernel, int mt, int nt) {
-            a.tiles = (a.group_rows + 16 * mt - 1) / (16 * mt);
-            const uint64_t ctas = (uint64_t)a.tiles * groups;
+        auto go = [&](auto kernel, int nt, int wk, int mt, int shared_bytes) {
+            const int per = 16 * 8 * mt / wk;
+            a.tiles = (a.rows + per - 1) / per;
+            // columns shared out over as many CTAs (of a cluster) as give each SM two, four steps each at least
+            const uint64_t tiles = (uint64_t)a.tiles * z.n * ((ntiles + nt - 1) / nt);
+            const int64_t steps = (h + 32 * down_step<T>() - 1) / (32 * down_step<T>()) / wk;
+            a.split = 1;
+            while (a.split < 8 && tiles * a.split < 2 * 148 / mt && steps >= 8 * a.split) a.split *= 2;
+            const uint64_t ctas = (uint64_t)a.tiles * z.n * a.split;
             if (ctas > 0x7fffffffu) return (int)COMPAMS_ERR_TOO_LARGE;
-            return launched(launch_after(kernel, dim3((uint32_t)ctas, (ntiles + nt - 1) / nt), dim3(256), stream, a), "adapter_down");
+            return launched(launch_next(kernel, dim3((uint32_t)ctas, (ntiles + nt - 1) / nt), a.split, shared_bytes, false, stream, a),
+                            "adapter_down");
         };
-        if (ntiles <= 1) return vec ? go(adapter_down_kernel<T, true, 1, 1>, 1, 1) : go(adapter_down_kernel<T, false, 1, 1>, 1, 1);
-        if (ntiles <= 2) return vec ? go(adapter_down_kernel<T, true, 1, 2>, 1, 2) : go(adapter_down_kernel<T, false, 1, 2>, 1, 2);
-        if (ntiles <= 4) return vec ? go(adapter_down_kernel<T, true, 1, 4>, 1, 4) : go(adapter_down_kernel<T, false, 1, 4>, 1, 4);
-        return vec ? go(adapter_down_kernel<T, true, 2, 8>, 2, 8) : go(adapter_down_kernel<T, false, 2, 8>, 2, 8);
+        auto pick = [&](auto v, auto k, auto n, auto m) {
+            constexpr bool V = decltype(v)::value;
+            constexpr int WK = decltype(k)::value, NT = decltype(n)::value, MT = decltype(m)::value;
+            return go(adapter_down_kernel<T, V, NT, WK, MT>, NT, WK, MT, down_shared<T, V, NT, WK, MT>());
+        };
+        auto by_ranks = [&](auto v, auto k) {
+            if (ntiles <= 1) return pick(v, k, Int<1>(), Int<1>());
+            if (ntiles <= 2) return pick(v, k, Int<2>(), Int<1>());
+            if (ntiles <= 4) return pick(v, k, Int<4>(), Int<1>());
+            // many rank indices: two blocks of rows to a warp, or the fragments' way through shared memory is the limit
+            if constexpr (decltype(k)::value == 1) return pick(v, k, Int<8>(), Int<2>());
+            else return pick(v, k, Int<8>(), Int<1>());
+        };
+        // eight blocks of rows to a CTA where that leaves CTAs for all SMs, the columns shared out eightfold
+        const bool many = (z.rows + 127) / 128 * z.n * 8 >= 148;
+        if (many) return vec ? by_ranks(Int<1>(), Int<1>()) : by_ranks(Int<0>(), Int<1>());
+        return vec ? by_ranks(Int<1>(), Int<8>()) : by_ranks(Int<0>(), Int<8>());
     });
 }
 
-int up(void* y, Rows base, const float* t, const AdapterShape& z, int64_t h, bool shared, Factor f, const uint4* frag, float scale,
-       const Drop& d, cudaStream_t stream) {
-    AdapterArgs a = arguments(z, base, h, shared, scale, d);
-    a.y = y; a.t = t; a.f = f; a.frag = frag; a.frag_ws = shared ? 0 : up_frag_words(h, z.rank);
-    const uint32_t groups = shared ? 1 : (uint32_t)z.n;
+int up(void* y, Rows base, Low low, const AdapterShape& z, int64_t h, bool shared, Factor f, const uint4* frag, float scale, const Drop& d,
+       cudaStream_t stream) {
+    AdapterArgs a = arguments(z, base, h, low, scale, d);
+    a.y = y; a.f = f; a.frag = frag; a.frag_ws = shared ? 0 : up_frag_words(h, z.rank);
     const bool vec = h % 8 == 0 && (!base.p || base.aligned()) && packed(y, z.rows, h, base.type).aligned();
     return by_type(base.type, [&](auto tt) {
         using T = decltype(tt);
+        const uint32_t columns = (uint32_t)((h + 8 * kUpColumns - 1) / (8 * kUpColumns));
         if (!frag) {
             auto kernel = vec ? adapter_up_few_kernel<T, true> : adapter_up_few_kernel<T, false>;
-            return launched(launch_after(kernel, dim3((uint32_t)((h + 255) / 256), groups), dim3(256), stream, a), "adapter_up");
+            return launched(launch_next(kernel, dim3(columns, (uint32_t)z.n), 1, 0, false, stream, a), "adapter_up");
         }
-        constexpr int MT = sizeof(T) == 4 ? 1 : 2, PT = sizeof(T) == 4 ? 3 : 2;
-        // row chunks: as many as give each SM about eight CTAs
-        const uint32_t columns = (uint32_t)((h + 8 * kUpColumns - 1) / (8 * kUpColumns)), steps = (a.group_rows + 16 * MT - 1) / (16 * MT);
-        uint64_t c = 148 * 8 / ((uint64_t)columns * groups) + 1;
-        if (c > steps) c = steps;
-        if (c > 65535 / groups) c = 65535 / groups;
+        constexpr int PT = sizeof(T) == 4 ? 3 : 2;
+        // row chunks: as many as give each SM about four CTAs
+        const uint32_t blocks = (a.rows + 15) / 16, n = (uint32_t)z.n;
+        uint64_t c = 148 * 4 / ((uint64_t)columns * n) + 1;
+        if (c > blocks) c = blocks;
+        if (c > 65535 / n) c = 65535 / n;
         a.tiles = (uint32_t)c;
-        auto kernel = vec ? adapter_up_kernel<T, true, MT, PT> : adapter_up_kernel<T, false, MT, PT>;
-        return launched(launch_after(kernel, dim3(columns, groups * a.tiles), dim3(256), stream, a), "adapter_up");
+        auto go = [&](auto v, auto r) {
+            constexpr bool V = decltype(v)::value;
+            constexpr int RB = decltype(r)::value;
+            return launched(launch_next(adapter_up_kernel<T, V, RB, PT>, dim3(columns, n * a.tiles), 1, up_shared<T, V, RB, PT>(), false,
+                                        stream, a),
+                            "adapter_up");
+        };
+        auto by_ranks = [&](auto v) {
+            const int ranks = (z.rank + 15) / 16;
+            if (ranks == 1) return go(v, Int<1>());
+            if (ranks == 2) return go(v, Int<2>());
+            if constexpr (PT == 2)
+                if (ranks == 4) return go(v, Int<4>());
+            return go(v, Int<0>());
+        };
+        return vec ? by_ranks(Int<1>()) : by_ranks(Int<0>());
     });
 }
 
 // out(j, c) at j * sj + c * sc of every worker's rank * h floats.
-int outer(float* out, bool sum_workers, Rows x, const float* t, const AdapterShape& z, int64_t h, int64_t sj, int64_t sc, float scale,
+int outer(float* out, bool sum_workers, Rows x, Low low, const AdapterShape& z, int64_t h, int64_t sj, int64_t sc, float scale,
           const Drop& d, float* partial, bool first, cudaStream_t stream) {
-    AdapterArgs a = arguments(z, x, h, false, scale, d);
-    a.t = t; a.f = {nullptr, 0, sj, sc}; a.chunks = outer_chunks(z, h);
+    AdapterArgs a = arguments(z, x, h, low, scale, d);
+    a.f = {nullptr, 0, sj, sc}; a.chunks = outer_chunks(z, h);
     const bool straight = outer_floats(z, h, sum_workers) == 0;
     a.out = straight ? out : partial;
-    const int nt = outer_ranks(z.rank);
-    const uint64_t tiles = (uint64_t)((h + kOuterColumns - 1) / kOuterColumns) * ((z.rank + 8 * nt - 1) / (8 * nt));
-    if (tiles > 0x7fffffffu) return COMPAMS_ERR_TOO_LARGE;
     const int rc = by_type(x.type, [&](auto tt) {
         using T = decltype(tt);
+        if (few(z))
+            return launched(launch_next(adapter_outer_few_kernel<T>, dim3((uint32_t)((h + 255) / 256), (uint32_t)z.n), 1, 0, first, stream, a),
+                            "adapter_outer");
+        const int nt = outer_ranks(z.rank);
+        const uint64_t tiles = (uint64_t)((h + kOuterColumns - 1) / kOuterColumns) * ((z.rank + 8 * nt - 1) / (8 * nt));
+        if (tiles > 0x7fffffffu) return (int)COMPAMS_ERR_TOO_LARGE;
         const bool vec = h % 8 == 0 && x.aligned();
-        auto kernel = nt == 1 ? (vec ? adapter_outer_kernel<T, true, 1> : adapter_outer_kernel<T, false, 1>)
-                    : nt == 2 ? (vec ? adapter_outer_kernel<T, true, 2> : adapter_outer_kernel<T, false, 2>)
-                              : (vec ? adapter_outer_kernel<T, true, 4> : adapter_outer_kernel<T, false, 4>);
-        const dim3 grid((uint32_t)tiles, (uint32_t)z.n * a.chunks);
-        return launched(first ? launch_plain(kernel, grid, dim3(256), 0, stream, a) : launch_after(kernel, grid, dim3(256), stream, a),
-                        "adapter_outer");
+        auto go = [&](auto v, auto m) {
+            constexpr bool V = decltype(v)::value;
+            constexpr int NT = decltype(m)::value;
+            return launched(launch_next(adapter_outer_kernel<T, V, NT>, dim3((uint32_t)tiles, (uint32_t)z.n * a.chunks), 1,
+                                        outer_shared<T, V, NT>(), first, stream, a),
+                            "adapter_outer");
+        };
+        auto by_ranks = [&](auto v) {
+            return nt == 1 ? go(v, Int<1>()) : nt == 2 ? go(v, Int<2>()) : nt == 4 ? go(v, Int<4>()) : go(v, Int<8>());
+        };
+        return vec ? by_ranks(Int<1>()) : by_ranks(Int<0>());
     });
     if (rc != COMPAMS_OK || straight) return rc;
     const int64_t len = z.rank * h;
-    return launched(launch_after(adapter_join_kernel, dim3((uint32_t)((len + 255) / 256), sum_workers ? 1 : (uint32_t)z.n), dim3(256),
-                                 stream, (const float*)partial, out, len, sum_workers ? z.n * a.chunks : a.chunks),
+    return launched(launch_next(adapter_join_kernel, dim3((uint32_t)((len + 255) / 256), sum_workers ? 1 : (uint32_t)z.n), 1, 0, false,
+                                stream, (const float*)partial, out, len, sum_workers ? z.n * a.chunks : a.chunks),
                     "adapter_join");
 }
 
 bool float_aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
-int64_t padded(int64_t floats) { return (floats + 63) / 64 * 64; }
 
-// The workspace: fragments of the two factors, and, for the backward pass, dt and the partial sums.
+// The workspace: fragments of the two factors, t (dt in the backward pass) as operands, and, in the backward pass, the forward pass's t
+// as an operand of outer and the partial sums; offsets in bytes.
 struct Places {
-    int64_t down, up, dt, partial, bytes;  // offsets in bytes
+    int64_t down, up, t, t_up, t_outer, saved, partial, bytes;
 };
 Places places(const AdapterShape& z, bool shared, bool backward, bool sum_workers) {
-    const int64_t groups = shared ? 1 : z.n;
-    const bool frags = !few(z, shared);
+    const int64_t factors = shared ? 1 : z.n;
+    const bool frags = !few(z);
     Places p = {};
-    p.up = p.down + (frags ? groups * down_frag_words(backward ? z.out : z.in, z.rank) * 16 : 0);
-    p.dt = p.up + (frags ? groups * up_frag_words(backward ? z.in : z.out, z.rank) * 16 : 0);
-    p.partial = p.dt + (backward ? padded((int64_t)z.total() * z.rank) * 4 : 0);
+    int64_t at = 0;
+    auto take = [&](int64_t bytes) {
+        const int64_t here = at;
+        at += (bytes + 255) / 256 * 256;
+        return here;
+    };
+    p.down = take(frags ? factors * down_frag_words(backward ? z.out : z.in, z.rank) * 16 : 0);
+    p.up = take(frags ? factors * up_frag_words(backward ? z.in : z.out, z.rank) * 16 : 0);
+    p.t = take(backward && !frags ? (int64_t)z.total() * z.rank * 4 : 0);
+    p.t_up = take(frags ? z.n * t_up_words(z.rows, z.rank) * 16 : 0);
+    p.t_outer = take(frags && backward ? z.n * t_outer_words(z.rows, z.rank) * 8 : 0);
+    p.saved = take(frags && backward ? z.n * t_outer_words(z.rows, z.rank) * 8 : 0);
     const int64_t fa = backward ? outer_floats(z, z.in, sum_workers) : 0, fb = backward ? outer_floats(z, z.out, sum_workers) : 0;
-    p.bytes = p.partial + (fa > fb ? fa : fb) * 4;
+    p.partial = take((fa > fb ? fa : fb) * 4);
+    p.bytes = at;
     return p;
 }
 
@@ -755,7 +1173,7 @@ int compams_adapter_workspace_bytes(size_t* bytes, int32_t n, int64_t rows, int6
                                     int32_t backward, int32_t sum_workers) {
     const AdapterShape z{n, rows, in, out, rank};
     if (!bytes || !z.ok()) return COMPAMS_ERR_INVALID_ARG;
-    *bytes = (size_t)places(z, shared != 0, backward != 0, sum_workers != 0).bytes;
+    *bytes = (size_t)places(z, shared != 0 || n == 1, backward != 0, sum_workers != 0).bytes;
     return COMPAMS_OK;
 }
 
@@ -780,15 +1198,18 @@ int compams_adapter_forward(void* y, float* t, const void* x, const void* base, 
         return COMPAMS_ERR_INVALID_ARG;
     const cudaStream_t stream = (cudaStream_t)cuda_stream;
     const Factor fa{a, a_worker_stride, a_row_stride, 1}, fb{b, b_worker_stride, 1, b_row_stride};
+    char* work = (char*)workspace;
+    Low low = {t, nullptr, nullptr};
     uint4 *down_frag = nullptr, *up_frag = nullptr;
     int rc = COMPAMS_OK;
-    if (!few(z, shared)) {
-        down_frag = (uint4*)((char*)workspace + at.down);
-        up_frag = (uint4*)((char*)workspace + at.up);
-        rc = prepare(z, shared, fa, in, down_frag, fb, out, up_frag, stream);
+    if (!few(z)) {
+        down_frag = (uint4*)(work + at.down);
+        up_frag = (uint4*)(work + at.up);
+        low.up = (uint4*)(work + at.t_up);
+        rc = prepare(z, shared, fa, in, down_frag, fb, out, up_frag, nullptr, nullptr, stream);
     }
-    if (rc == COMPAMS_OK) rc = down(t, xin, z, in, shared, fa, down_frag, 1.0f, d, stream);
-    if (rc == COMPAMS_OK) rc = up(y, bin, t, z, out, shared, fb, up_frag, scale, none, stream);
+    if (rc == COMPAMS_OK) rc = down(low, xin, z, in, shared, fa, down_frag, 1.0f, d, stream);
+    if (rc == COMPAMS_OK) rc = up(y, bin, low, z, out, shared, fb, up_frag, scale, none, stream);
     return rc;
 }
 
@@ -819,19 +1240,28 @@ int compams_adapter_backward(void* dx, float* da, float* db, int32_t sum_workers
         !packed(dx, rows, in, type).element_aligned())
         return COMPAMS_ERR_INVALID_ARG;
     const Factor fa{a, a_worker_stride, a_row_stride, 1}, fb{b, b_worker_stride, 1, b_row_stride};
-    float* dt = (float*)((char*)workspace + at.dt);
-    float* partial = (float*)((char*)workspace + at.partial);
+    char* work = (char*)workspace;
+    float* partial = (float*)(work + at.partial);
+    Low low = {few(z) ? (float*)(work + at.t) : nullptr, nullptr, nullptr}, saved = {const_cast<float*>(t), nullptr, nullptr};
     uint4 *down_frag = nullptr, *up_frag = nullptr;
     int rc = COMPAMS_OK;
-    if (!few(z, shared) && (dx || da)) {
-        down_frag = (uint4*)((char*)workspace + at.down);
-        up_frag = dx ? (uint4*)((char*)workspace + at.up) : nullptr;
-        rc = prepare(z, shared, fb, out, down_frag, fa, in, up_frag, stream);
+    bool first = true;
+    if (!few(z)) {
+        if (dx || da) down_frag = (uint4*)(work + at.down);
+        if (dx) up_frag = (uint4*)(work + at.up);
+        low.up = (uint4*)(work + at.t_up);
+        if (da) low.outer = (uint2*)(work + at.t_outer);
+        if (db) saved.outer = (uint2*)(work + at.saved);
+        rc = prepare(z, shared, fb, out, down_frag, fa, in, up_frag, t, saved.outer, stream);
+        first = false;
     }
-    if (rc == COMPAMS_OK && (dx || da)) rc = down(dt, gin, z, out, shared, fb, down_frag, scale, none, stream);
-    if (rc == COMPAMS_OK && db) rc = outer(db, sum_workers, gin, t, z, out, 1, rank, scale, none, partial, !(dx || da), stream);
-    if (rc == COMPAMS_OK && da) rc = outer(da, sum_workers, xin, dt, z, in, in, 1, 1.0f, d, partial, false, stream);
-    if (rc == COMPAMS_OK && dx) rc = up(dx, {nullptr, 0, 0, type}, dt, z, in, shared, fa, up_frag, 1.0f, d, stream);
+    if (rc == COMPAMS_OK && (dx || da)) {
+        rc = down(low, gin, z, out, shared, fb, down_frag, scale, none, stream);
+        first = false;
+    }
+    if (rc == COMPAMS_OK && db) rc = outer(db, sum_workers, gin, saved, z, out, 1, rank, scale, none, partial, first, stream);
+    if (rc == COMPAMS_OK && da) rc = outer(da, sum_workers, xin, low, z, in, in, 1, 1.0f, d, partial, false, stream);
+    if (rc == COMPAMS_OK && dx) rc = up(dx, {nullptr, 0, 0, type}, low, z, in, shared, fa, up_frag, 1.0f, d, stream);
     return rc;
 }
 

@@ -87,7 +87,7 @@ def test_norm_backward_refuses(lib, bad):
 
 
 def adapter_args(**kw):
-    v = dict(y=A, t=A, x=A, base=A, type=1, n=2, rows=3, inn=8, out=8, rank=4, xws=24, xrs=8, bws=24, brs=8, a=A, aws=0, ars=8, b=A, bbws=0, bbrs=4,
+    v = dict(y=A, t=A, x=A, base=A, type=1, n=2, rows=30, inn=8, out=8, rank=4, xws=240, xrs=8, bws=240, brs=8, a=A, aws=0, ars=8, b=A, bbws=0, bbrs=4,
              scale=1.0, p=0.0, seed=1, call=0, call_device=None, worker=0, work=A, bytes=1 << 30, stream=None)
     v.update(kw)
     return list(v.values())
@@ -101,7 +101,7 @@ def test_adapter_forward_refuses(lib, bad):
 
 
 def adapter_backward_args(**kw):
-    v = dict(dx=A, da=A, db=A, sum=0, dy=A, x=A, t=A, type=1, n=2, rows=3, inn=8, out=8, rank=4, gws=24, grs=8, xws=24, xrs=8, a=A, aws=0, ars=8, b=A,
+    v = dict(dx=A, da=A, db=A, sum=0, dy=A, x=A, t=A, type=1, n=2, rows=30, inn=8, out=8, rank=4, gws=240, grs=8, xws=240, xrs=8, a=A, aws=0, ars=8, b=A,
              bws=0, brs=4, scale=1.0, p=0.0, seed=1, call=0, call_device=None, worker=0, work=A, bytes=1 << 30, stream=None)
     v.update(kw)
     return list(v.values())
