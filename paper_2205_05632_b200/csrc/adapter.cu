@@ -108,15 +108,15 @@ __device__ __forceinline__ Raw8<T> raw_columns(const T* __restrict__ row, int c,
     }
     return r;
 }
-// Their planes, as pairs; elements whose bit is 0 are 0.
+// Their planes, as pairs; dropped elements are 0.
 template <typename T>
-__device__ __forceinline__ void raw_planes(const Raw8<T>& r, bool drop, uint32_t bits, uint32_t (&w)[Planes<T>::count][4]) {
+__device__ __forceinline__ void raw_planes(const Raw8<T>& r, const Drop& d, const uint4& u, uint32_t (&w)[Planes<T>::count][4]) {
     float v[8];
     raw_floats<T>(r, v);
-    if (drop)
+    if (d.on)
 #pragma unroll
         for (int k = 0; k < 8; ++k)
-            if (!((bits >> k) & 1u)) v[k] = 0.0f;
+            if (!drop_keeps(d, u, k)) v[k] = 0.0f;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         uint32_t p[Planes<T>::count];
@@ -126,12 +126,14 @@ __device__ __forceinline__ void raw_planes(const Raw8<T>& r, bool drop, uint32_t
     }
 }
 template <>
-__device__ __forceinline__ void raw_planes<__nv_bfloat16>(const Raw8<__nv_bfloat16>& r, bool drop, uint32_t bits, uint32_t (&w)[1][4]) {
+__device__ __forceinline__ void raw_planes<__nv_bfloat16>(const Raw8<__nv_bfloat16>& r, const Drop& d, const uint4& u, uint32_t (&w)[1][4]) {
     w[0][0] = r.q.x; w[0][1] = r.q.y; w[0][2] = r.q.z; w[0][3] = r.q.w;
-    if (drop)
+    if (d.on)
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-            w[0][q] &= ((bits >> (2 * q)) & 1u ? 0xffffu : 0u) | ((bits >> (2 * q + 1)) & 1u ? 0xffff0000u : 0u);
+        for (int q = 0; q < 4; ++q) {
+            if (!drop_keeps(d, u, 2 * q)) w[0][q] &= 0xffff0000u;
+            if (!drop_keeps(d, u, 2 * q + 1)) w[0][q] &= 0xffffu;
+        }
 }
 
 // ---- the factors as operands -----------------------------------------------------------------------------------------------
@@ -140,22 +142,29 @@ constexpr int kPlanes = 3;
 constexpr int kDownColumns = 32;  // columns of a fragment of "down": 8 per lane of a quad
 constexpr int kUpColumns = 32;    // columns of a fragment of "up": four 8-column products, whose columns interleave by pairs
 
-__host__ __device__ inline int64_t down_frag_words(int64_t h, int rank) {  // of 16 bytes
-    return (h + kDownColumns - 1) / kDownColumns * ((rank + 7) / 8) * kPlanes * 32;
-}
+// Rank indices are taken in groups of NT tiles of 8: all of them up to 64, 64 at a time beyond. Fragments of a group are padded to whole
+// groups and an even number of column blocks, so that the loops over them have no ends to look for; what is padded is 0.
+__host__ __device__ inline int group_tiles(int rank) { return rank <= 8 ? 1 : rank <= 16 ? 2 : rank <= 32 ? 4 : 8; }  // NT
+__host__ __device__ inline int rank_groups(int rank) { return rank <= 64 ? 1 : (rank + 63) / 64; }
+__host__ __device__ inline int rank_tiles(int rank) { return rank_groups(rank) * group_tiles(rank); }
+__host__ __device__ inline int down_blocks(int64_t h) { return (int)((h + 2 * kDownColumns - 1) / (2 * kDownColumns) * 2); }
+
+// Words of 16 bytes, a worker's:
+//   down: [group][column block][tile][plane][lane g, t] = rank 8 tile + g, columns 8 t ... 8 t + 7
+//   up:   [column block][16 ranks][plane][half][lane g, t] = for two of the four products q, column 8 (g / 2) + 2 q + g % 2, ranks 4 t ... 4 t + 3
+__host__ __device__ inline int64_t down_frag_words(int64_t h, int rank) { return (int64_t)down_blocks(h) * rank_tiles(rank) * kPlanes * 32; }
 __host__ __device__ inline int64_t up_frag_words(int64_t h, int rank) {
     return (h + kUpColumns - 1) / kUpColumns * ((rank + 15) / 16) * kPlanes * 64;
 }
-
 // t as an operand, 16 rows of a worker at a time:
-//   up:    [16 rows][16 ranks][plane][lane g, t] = rows g and g + 8, ranks 4 t ... 4 t + 3
-//   outer: [16 rows][8 ranks][plane][lane g, t] = rows 4 t ... 4 t + 3, rank g
-__host__ __device__ inline int64_t t_up_words(int64_t rows, int rank) {  // of 16 bytes, a worker's
-    return (rows + 15) / 16 * ((rank + 15) / 16) * kPlanes * 32;
+//   up:    [16 rows][16 ranks][plane][lane g, t] = rows g and g + 8, ranks 4 t ... 4 t + 3 (16 bytes); as many planes as up multiplies
+//   outer: [group][16 rows][tile][plane][lane g, t] = rows 4 t ... 4 t + 3, rank g (8 bytes)
+__host__ __device__ inline int64_t t_up_words(int64_t rows, int rank, int planes) {
+    return (rows + 15) / 16 * ((rank + 15) / 16) * planes * 32;
 }
-__host__ __device__ inline int64_t t_outer_words(int64_t rows, int rank) {  // of 8 bytes, a worker's
-    return (rows + 15) / 16 * ((rank + 7) / 8) * kPlanes * 32;
-}
+__host__ __device__ inline int64_t t_outer_words(int64_t rows, int rank) { return (rows + 15) / 16 * rank_tiles(rank) * kPlanes * 16; }
+template <typename T>
+__host__ __device__ constexpr int up_planes() { return sizeof(T) == 4 ? 3 : 2; }
 
 // Four numbers of t as an operand of outer.
 __device__ __forceinline__ void store_t_outer(uint2* at, const float (&v)[4]) {
@@ -166,10 +175,7 @@ __device__ __forceinline__ void store_t_outer(uint2* at, const float (&v)[4]) {
     for (int p = 0; p < kPlanes; ++p) at[p * 32] = make_uint2(lo[p], hi[p]);
 }
 
-// A warp per fragment; a lane writes its share of the planes.
-//   down: [column block][8 ranks][plane][lane g, t] = rank 8 b + g, columns 8 t ... 8 t + 7
-//   up:   [column block][16 ranks][plane][half][lane g, t] = for two of the four products q, column 8 (g / 2) + 2 q + g % 2, ranks 4 t ... 4 t + 3
-// and, in the backward pass, the forward pass's t for outer.
+// A warp per fragment; a lane writes its share of the planes. In the backward pass the forward pass's t becomes an operand of outer too.
 struct PrepareArgs {
     Factor down, up;
     uint4 *down_frag, *up_frag;
@@ -184,19 +190,22 @@ __global__ void __launch_bounds__(256) adapter_prepare_kernel(const __grid_const
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     uint32_t at = blockIdx.x * 8 + (threadIdx.x >> 5);
     if (at < a.t_count) {
-        const int ranks = (a.rank + 7) / 8, j = (int)(at % ranks) * 8 + g;
-        const uint32_t row = at / ranks * 16 + 4 * t;
+        const uint32_t nt = group_tiles(a.rank), blocks = (a.rows + 15) / 16, tile = at % nt, block = at / nt % blocks, group = at / nt / blocks;
+        const int j = (int)(group * nt + tile) * 8 + g;
+        const uint32_t row = block * 16 + 4 * t;
         float v[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k)
             v[k] = row + k < a.rows && j < a.rank ? __ldg(a.t + ((int64_t)blockIdx.y * a.rows + row + k) * a.rank + j) : 0.0f;
-        store_t_outer(a.t_outer + blockIdx.y * t_outer_words(a.rows, a.rank) + (int64_t)at * kPlanes * 32 + lane, v);
+        store_t_outer(a.t_outer + blockIdx.y * t_outer_words(a.rows, a.rank) * 2 + (int64_t)at * kPlanes * 32 + lane, v);
         return;
     }
     at -= a.t_count;
     if (a.shared && blockIdx.y) return;
     if (at < a.down_count) {
-        const int ranks = (a.rank + 7) / 8, j = (int)(at % ranks) * 8 + g, c = (int)(at / ranks) * kDownColumns + 8 * t;
+        const uint32_t nt = group_tiles(a.rank), blocks = down_blocks(a.down_h), tile = at % nt, block = at / nt % blocks, group = at / nt / blocks;
+        const int j = (int)(group * nt + tile) * 8 + g;
+        const int64_t c = (int64_t)block * kDownColumns + 8 * t;
         const float* f = a.down.p + (int64_t)blockIdx.y * a.down.ws;
         uint32_t w[4][kPlanes];
 #pragma unroll
@@ -293,7 +302,7 @@ __global__ void __launch_bounds__(256, MT == 1 ? 2 : 1) adapter_down_kernel(cons
     const int part = (int)(blockIdx.x - tile * a.split);
     const uint32_t block0 = (tile - i * a.tiles) * BLOCKS;  // the first block of rows
     const uint32_t row0 = (block0 + warp / WK * MT) * 16;
-    const int n0 = blockIdx.y * NT, ntiles = (a.rank + 7) / 8;
+    const int n0 = blockIdx.y * NT;
     const uint32_t call = drop_call(a.drop);
     const T* row[MT][2];
     bool in[MT][2];
@@ -305,8 +314,8 @@ __global__ void __launch_bounds__(256, MT == 1 ? 2 : 1) adapter_down_kernel(cons
             in[q][half] = r < a.rows;
             row[q][half] = (const T*)a.x + (int64_t)i * a.x_ws + (int64_t)(in[q][half] ? r : 0) * a.x_rs;
         }
-    const uint4* frag = a.frag + (int64_t)i * a.frag_ws;
-    const int blocks = (a.h + kDownColumns - 1) / kDownColumns, steps = (blocks + KB - 1) / KB, stride = a.split * WK;
+    const int steps = down_blocks(a.h) / KB, stride = a.split * WK;
+    const uint4* frag = a.frag + (int64_t)i * a.frag_ws + (int64_t)blockIdx.y * steps * (KB * NT * kPlanes * 32);
     float acc[MT][NT][4] = {};
     Raw8<T> next[MT][2][KB];
     auto fetch = [&](int step, int stage) {
@@ -331,11 +340,10 @@ __global__ void __launch_bounds__(256, MT == 1 ? 2 : 1) adapter_down_kernel(cons
     auto fetch_shared = [&](int step, int stage) {
         if constexpr (WK == 1) {
             uint4* to = stages + stage * (KB * NT * kPlanes * 32);
+            const uint4* from = frag + (int64_t)step * (KB * NT * kPlanes * 32);
+            if (step < steps)
 #pragma unroll
-            for (int e = threadIdx.x; e < KB * NT * kPlanes * 32; e += 256) {
-                const int k = e / (NT * kPlanes * 32), rest = e - k * (NT * kPlanes * 32), b = step * KB + k;
-                if (b < blocks && n0 + rest / (kPlanes * 32) < ntiles) copy16(to + e, frag + (int64_t)(b * ntiles + n0) * kPlanes * 32 + rest, true);
-            }
+                for (int e = threadIdx.x; e < KB * NT * kPlanes * 32; e += 256) copy16(to + e, from + e, true);
         }
         copies_commit();
     };
@@ -365,28 +373,24 @@ __global__ void __launch_bounds__(256, MT == 1 ? 2 : 1) adapter_down_kernel(cons
                     Raw8<T> now;
                     if constexpr (VEC) now = ring_raw<SLOTS, T>(smem, stage, ((q * 2 + half) * KB + k) * S16);
                     else now = next[q][half][k];
-                    uint32_t bits = 0xffu;
+                    uint4 u = {};
                     if (a.drop.on)
-                        bits = drop_bits(a.drop, (step * KB + k) * (kDownColumns / 8) + t, row0 + q * 16 + half * 8 + g, a.drop.worker + i,
-                                         call);
-                    raw_planes<T>(now, a.drop.on, bits, w[q][half][k]);
+                        u = drop_words(a.drop, (step * KB + k) * (kDownColumns / 8) + t, row0 + q * 16 + half * 8 + g, a.drop.worker + i, call);
+                    raw_planes<T>(now, a.drop, u, w[q][half][k]);
                 }
         if constexpr (VEC) fetch(step + (kStages - 1) * stride, behind);
         else fetch(step + stride, 0);
         fetch_shared(step + (kStages - 1) * stride, behind);
-        const uint4* here = stages + stage * (KB * NT * kPlanes * 32) + lane;
+        const uint4 *here = stages + stage * (KB * NT * kPlanes * 32) + lane, *mine = frag + (int64_t)step * (KB * NT * kPlanes * 32) + lane;
         stage = stage + 1 == kStages ? 0 : stage + 1;
 #pragma unroll
         for (int k = 0; k < KB; ++k) {
-            const int b = step * KB + k;
-            if (b >= blocks) break;
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
-                if (n0 + j >= ntiles) break;
                 uint4 f[kPlanes];
 #pragma unroll
                 for (int p = 0; p < kPlanes; ++p)
-                    f[p] = WK == 1 ? here[((k * NT + j) * kPlanes + p) * 32] : frag[((int64_t)(b * ntiles + n0 + j) * kPlanes + p) * 32 + lane];
+                    f[p] = WK == 1 ? here[((k * NT + j) * kPlanes + p) * 32] : mine[((k * NT + j) * kPlanes + p) * 32];
 #pragma unroll
                 for (int q = 0; q < MT; ++q) {
                     float c[4];
@@ -460,17 +464,19 @@ __global__ void __launch_bounds__(256, MT == 1 ? 2 : 1) adapter_down_kernel(cons
                     const float* at = whole + (g + half * 8) * L + j;
                     split2<kPlanes>(j < NT * 8 ? at[0] : 0.0f, j < NT * 8 ? at[1] : 0.0f, v[half][pair]);
                 }
-            uint4* out = a.t_up + i * t_up_words(a.rows, a.rank) + ((int64_t)block * ranks + n0 / 2 + q) * kPlanes * 32 + lane;
+            constexpr int PT = up_planes<T>();
+            uint4* out = a.t_up + i * t_up_words(a.rows, a.rank, PT) + ((int64_t)block * ranks + n0 / 2 + q) * PT * 32 + lane;
 #pragma unroll
-            for (int p = 0; p < kPlanes; ++p) out[p * 32] = make_uint4(v[0][0][p], v[1][0][p], v[0][1][p], v[1][1][p]);
+            for (int p = 0; p < PT; ++p) out[p * 32] = make_uint4(v[0][0][p], v[1][0][p], v[0][1][p], v[1][1][p]);
         }
         if (a.t_outer)
             for (int q = warp; q < NT; q += 8) {
-                if (n0 + q >= ntiles) break;
                 float v[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) v[k] = whole[(4 * t + k) * L + q * 8 + g];
-                store_t_outer(a.t_outer + i * t_outer_words(a.rows, a.rank) + ((int64_t)block * ntiles + n0 + q) * kPlanes * 32 + lane, v);
+                store_t_outer(a.t_outer + i * t_outer_words(a.rows, a.rank) * 2 +
+                                  (((int64_t)blockIdx.y * ((a.rows + 15) / 16) + block) * NT + q) * kPlanes * 32 + lane,
+                              v);
             }
         __syncthreads();
     }
@@ -521,20 +527,22 @@ __global__ void __launch_bounds__(256) adapter_down_few_kernel(const __grid_cons
 
 // ---- up --------------------------------------------------------------------------------------------------------------------
 
-// A warp per 32 columns goes through the blocks of 16 rows of a chunk; the eight warps of a CTA are neighbours and share t, which passes
-// through shared memory. RB: blocks of 16 rank indices, whose fragments of the factor stay in registers (0: any number; fragments and t are
-// fetched again for each block of rows). PT: planes of t and of the factor.
-template <typename T, bool VEC, int RB, int PT>
-__host__ __device__ constexpr int up_ring() { return VEC ? kStages * 2 * (int)sizeof(Raw8<T>) * 256 : 0; }
-template <typename T, bool VEC, int RB, int PT>
-__host__ __device__ constexpr int up_shared() { return up_ring<T, VEC, RB, PT>() + kStages * RB * PT * 512; }
+// A warp per 32 columns goes through the blocks of 16 rows of a chunk, MB at a time; the eight warps of a CTA are neighbours and share
+// t, which passes through shared memory. RB: blocks of 16 rank indices, whose fragments of the factor stay in registers (0: any number;
+// fragments and t are fetched again for each block of rows).
+template <typename T, int RB>
+__host__ __device__ constexpr int up_rows() { return (RB == 1 || RB == 2) && sizeof(T) == 2 ? 2 : 1; }  // MB
+template <typename T, bool VEC, int RB>
+__host__ __device__ constexpr int up_ring() { return VEC ? kStages * 2 * up_rows<T, RB>() * (int)sizeof(Raw8<T>) * 256 : 0; }
+template <typename T, bool VEC, int RB>
+__host__ __device__ constexpr int up_shared() { return up_ring<T, VEC, RB>() + kStages * up_rows<T, RB>() * RB * up_planes<T>() * 512; }
 
-template <typename T, bool VEC, int RB, int PT>
-__global__ void __launch_bounds__(256) adapter_up_kernel(const __grid_constant__ AdapterArgs a) {
+template <typename T, bool VEC, int RB>
+__global__ void __launch_bounds__(256, 2) adapter_up_kernel(const __grid_constant__ AdapterArgs a) {
     extern __shared__ __align__(16) char smem[];
-    constexpr int S16 = (int)sizeof(Raw8<T>) / 16, SLOTS = 2 * S16;
+    constexpr int S16 = (int)sizeof(Raw8<T>) / 16, PT = up_planes<T>(), MB = up_rows<T, RB>(), SLOTS = 2 * MB * S16, STAGE = MB * RB * PT * 32;
     dependency_wait();
-    uint4* stages = reinterpret_cast<uint4*>(smem + up_ring<T, VEC, RB, PT>());
+    uint4* stages = reinterpret_cast<uint4*>(smem + up_ring<T, VEC, RB>());
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const uint32_t i = blockIdx.y / a.tiles, chunk = blockIdx.y - i * a.tiles;
     const int cb = blockIdx.x * 8 + (threadIdx.x >> 5), c = cb * kUpColumns + 8 * t;
@@ -544,7 +552,7 @@ __global__ void __launch_bounds__(256) adapter_up_kernel(const __grid_constant__
     const uint32_t b0 = (uint32_t)((uint64_t)blocks * chunk / a.tiles), b1 = (uint32_t)((uint64_t)blocks * (chunk + 1) / a.tiles);
     const uint32_t call = drop_call(a.drop);
     const uint4* frag = a.frag + (int64_t)i * a.frag_ws + (int64_t)(mine ? cb : 0) * ranks * kPlanes * 64 + lane;
-    const uint4* tt = a.t_up + i * t_up_words(a.rows, a.rank);
+    const uint4* tt = a.t_up + i * t_up_words(a.rows, a.rank, PT);
     uint4 f[RB ? RB : 1][PT][2];
     auto factor = [&](int r, uint4 (&to)[PT][2]) {
 #pragma unroll
@@ -556,99 +564,109 @@ __global__ void __launch_bounds__(256) adapter_up_kernel(const __grid_constant__
     if constexpr (RB > 0)
 #pragma unroll
         for (int r = 0; r < RB; ++r) factor(r, f[r]);
-    Raw8<T> next[2];
+    const T* x = (const T*)a.x + (int64_t)i * a.x_ws + c;
+    T* y = (T*)a.y + (int64_t)i * a.rows * a.h + c;
+    Raw8<T> next[MB][2];
     auto fetch = [&](uint32_t b, int stage) {
         if constexpr (RB > 0) {
+            const uint4* from = tt + (int64_t)b * (RB * PT * 32);
+            const int have = b < b1 ? (b + MB <= b1 ? STAGE : RB * PT * 32) : 0;
 #pragma unroll
-            for (int e = threadIdx.x; e < RB * PT * 32; e += 256) {
-                const int r = e / (PT * 32), rest = e - r * (PT * 32);
-                if (b < b1) copy16(stages + stage * (RB * PT * 32) + e, tt + ((int64_t)b * ranks + r) * kPlanes * 32 + rest, true);
-            }
+            for (int e = threadIdx.x; e < STAGE; e += 256)
+                if (e < have) copy16(stages + stage * STAGE + e, from + e, true);
         }
+        if (a.x) {
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const uint32_t j = b * 16 + half * 8 + g;
-            const bool in = a.x && b < b1 && j < a.rows && c < a.h;
-            const T* from = (const T*)a.x + (int64_t)i * a.x_ws + (int64_t)(in ? j : 0) * a.x_rs;
-            if constexpr (VEC) {
-                if (a.x)
+            for (int q = 0; q < MB; ++q)
 #pragma unroll
-                    for (int q = 0; q < S16; ++q)
-                        copy16(ring_at<SLOTS>(smem, stage, half * S16 + q), in ? reinterpret_cast<const char*>(from + c) + 16 * q : a.x, in);
-            } else {
-                next[half] = raw_columns<T, false>(from, c, in ? a.h : 0);
-            }
+                for (int half = 0; half < 2; ++half) {
+                    const uint32_t j = (b + q) * 16 + half * 8 + g;
+                    const bool in = b + q < b1 && j < a.rows && c < a.h;
+                    const T* from = in ? x + (int64_t)j * a.x_rs : (const T*)a.x;
+                    if constexpr (VEC) {
+#pragma unroll
+                        for (int v = 0; v < S16; ++v)
+                            copy16(ring_at<SLOTS>(smem, stage, (q * 2 + half) * S16 + v), reinterpret_cast<const char*>(from) + 16 * v, in);
+                    } else {
+                        next[q][half] = raw_columns<T, false>(from - c, c, in ? a.h : 0);
+                    }
+                }
         }
         copies_commit();
     };
     if constexpr (VEC) {
-        for (int s = 0; s < kStages - 1; ++s) fetch(b0 + s, s);
+        for (int s = 0; s < kStages - 1; ++s) fetch(b0 + s * MB, s);
     } else {
         fetch(b0, 0);
     }
     int stage = 0;
-    for (uint32_t b = b0; b < b1; ++b) {
+    for (uint32_t b = b0; b < b1; b += MB) {
         copies_wait<VEC ? kStages - 2 : 0>();
         __syncthreads();
-        Raw8<T> base[2] = {};
+        Raw8<T> base[MB][2] = {};
+        if (a.x)
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            if constexpr (VEC) {
-                if (a.x) base[half] = ring_raw<SLOTS, T>(smem, stage, half * S16);
-            } else {
-                base[half] = next[half];
-            }
-        }
-        const uint4* here = stages + stage * (RB * PT * 32) + lane;
-        if constexpr (VEC) fetch(b + kStages - 1, stage == 0 ? kStages - 1 : stage - 1);
-        else fetch(b + 1, stage + 1 == kStages ? 0 : stage + 1);
+            for (int q = 0; q < MB; ++q)
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    if constexpr (VEC) base[q][half] = ring_raw<SLOTS, T>(smem, stage, (q * 2 + half) * S16);
+                    else base[q][half] = next[q][half];
+                }
+        const uint4* here = stages + stage * STAGE + lane;
+        if constexpr (VEC) fetch(b + (kStages - 1) * MB, stage == 0 ? kStages - 1 : stage - 1);
+        else fetch(b + MB, stage + 1 == kStages ? 0 : stage + 1);
         stage = stage + 1 == kStages ? 0 : stage + 1;
         if (!mine) continue;
-        float acc[4][4] = {};
+        float acc[MB][4][4] = {};
 #pragma unroll(RB ? RB : 1)
         for (int r = 0; r < ranks; ++r) {
-            uint4 w[PT];
+            uint4 w[MB][PT];
             if constexpr (RB == 0) factor(r, f[0]);
 #pragma unroll
-            for (int p = 0; p < PT; ++p) w[p] = RB ? here[(r * PT + p) * 32] : tt[((int64_t)(b * ranks + r) * kPlanes + p) * 32 + lane];
+            for (int q = 0; q < MB; ++q)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                float d[4] = {};
-                float(&sum)[4] = PT == 3 ? d : acc[k];  // a 16-bit result can stand one running sum
+                for (int p = 0; p < PT; ++p) w[q][p] = RB ? here[((q * RB + r) * PT + p) * 32] : tt[((int64_t)(b * ranks + r) * PT + p) * 32 + lane];
+            float d[MB][4][4] = {};
+            auto& sum = PT == 3 ? d : acc;  // a 16-bit result can stand one running sum
 #pragma unroll
-                for (int both = PT - 1; both >= 0; --both)
+            for (int both = PT - 1; both >= 0; --both)
 #pragma unroll
-                    for (int pt = 0; pt <= both; ++pt) {
-                        const uint4 e = f[RB ? r : 0][both - pt][k >> 1];
-                        mma(sum, w[pt].x, w[pt].y, w[pt].z, w[pt].w, k & 1 ? e.z : e.x, k & 1 ? e.w : e.y);
-                    }
-                if (PT == 3)
+                for (int pt = 0; pt <= both; ++pt)
 #pragma unroll
-                    for (int v = 0; v < 4; ++v) acc[k][v] += d[v];
-            }
+                    for (int q = 0; q < MB; ++q)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const uint4 e = f[RB ? r : 0][both - pt][k >> 1];
+                            mma(sum[q][k], w[q][pt].x, w[q][pt].y, w[q][pt].z, w[q][pt].w, k & 1 ? e.z : e.x, k & 1 ? e.w : e.y);
+                        }
+            if (PT == 3)
+#pragma unroll
+                for (int q = 0; q < MB; ++q)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) acc[q][k][v] += d[q][k][v];
         }
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const uint32_t j = b * 16 + half * 8 + g;
-            if (j >= a.rows || c >= a.h) continue;
-            float v[8];
-            raw_floats<T>(base[half], v);
+        for (int q = 0; q < MB; ++q)
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = fmaf(a.scale, acc[k >> 1][half * 2 + (k & 1)], v[k]);
-            if (a.drop.on) {
-                const uint32_t bits = drop_bits(a.drop, (uint32_t)c >> 3, j, a.drop.worker + i, call);
+            for (int half = 0; half < 2; ++half) {
+                const uint32_t j = (b + q) * 16 + half * 8 + g;
+                if ((MB > 1 && b + q >= b1) || j >= a.rows || c >= a.h) continue;
+                float v[8];
+                raw_floats<T>(base[q][half], v);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) v[k] = (bits >> k) & 1u ? v[k] * a.drop.factor : 0.0f;
+                for (int k = 0; k < 8; ++k) v[k] = fmaf(a.scale, acc[q][k >> 1][half * 2 + (k & 1)], v[k]);
+                if (a.drop.on) drop8(a.drop, drop_words(a.drop, (uint32_t)c >> 3, j, a.drop.worker + i, call), v);
+                T* to = y + (int64_t)j * a.h;
+                if (VEC) {
+                    store8<T>(to, v);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        if (c + k < a.h) to[k] = from_float<T>(v[k]);
+                }
             }
-            T* y = (T*)a.y + ((int64_t)i * a.rows + j) * a.h + c;
-            if (VEC) {
-                store8<T>(y, v);
-            } else {
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    if (c + k < a.h) y[k] = from_float<T>(v[k]);
-            }
-        }
     }
 }
 
@@ -715,14 +733,13 @@ __global__ void __launch_bounds__(256) adapter_outer_kernel(const __grid_constan
     dependency_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3, side = warp & 3, turn = warp >> 2;
     const uint32_t i = blockIdx.y / a.chunks, chunk = blockIdx.y - i * a.chunks;
-    const int ntiles = (a.rank + 7) / 8, groups = (ntiles + NT - 1) / NT, column = blockIdx.x / groups;
-    const int n0 = (blockIdx.x - column * groups) * NT;
+    const int groups = rank_groups(a.rank), column = blockIdx.x / groups, group = blockIdx.x - column * groups, n0 = group * NT;
     const int c = column * kOuterColumns + side * 64 + 8 * g;
     const uint32_t blocks = (a.rows + 15) / 16;
     const uint32_t s0 = (uint32_t)((uint64_t)blocks * chunk / a.chunks), s1 = (uint32_t)((uint64_t)blocks * (chunk + 1) / a.chunks);
     const uint32_t call = drop_call(a.drop);
     const T* x = (const T*)a.x + (int64_t)i * a.x_ws;
-    const uint4* tt = reinterpret_cast<const uint4*>(a.t_outer + i * t_outer_words(a.rows, a.rank));
+    const uint4* tt = reinterpret_cast<const uint4*>(a.t_outer) + i * t_outer_words(a.rows, a.rank) + (int64_t)group * blocks * (NT * kPlanes * 16);
     uint4* stages = reinterpret_cast<uint4*>(smem + outer_ring<T, VEC, NT>());
     constexpr int STAGE = 2 * NT * kPlanes * 16;  // words of 16 bytes: the fragments of the two blocks of rows of a step
     float acc[4][NT][4] = {};
@@ -743,12 +760,11 @@ __global__ void __launch_bounds__(256) adapter_outer_kernel(const __grid_constan
         }
     };
     auto fetch_shared = [&](uint32_t s, int stage) {  // s: the first block of rows of the step
+        const uint4* from = tt + (int64_t)s * (STAGE / 2);
+        const int have = s < s1 ? (s + 2 <= s1 ? STAGE : STAGE / 2) : 0;
 #pragma unroll
-        for (int e = threadIdx.x; e < STAGE; e += 256) {
-            const int which = e / (STAGE / 2), rest = e - which * (STAGE / 2);
-            if (s + which < s1 && n0 + rest / (kPlanes * 16) < ntiles)
-                copy16(stages + stage * STAGE + e, tt + ((int64_t)(s + which) * ntiles + n0) * kPlanes * 16 + rest, true);
-        }
+        for (int e = threadIdx.x; e < STAGE; e += 256)
+            if (e < have) copy16(stages + stage * STAGE + e, from + e, true);
         copies_commit();
     };
     if constexpr (VEC) {
@@ -772,9 +788,9 @@ __global__ void __launch_bounds__(256) adapter_outer_kernel(const __grid_constan
             Raw8<T> now;
             if constexpr (VEC) now = ring_raw<SLOTS, T>(smem, stage, r * S16);
             else now = next[r];
-            uint32_t bits = 0xffu;
-            if (a.drop.on) bits = drop_bits(a.drop, (uint32_t)c >> 3, s * 16 + 4 * t + r, a.drop.worker + i, call);
-            raw_planes<T>(now, a.drop.on, bits, w[r]);
+            uint4 u = {};
+            if (a.drop.on) u = drop_words(a.drop, (uint32_t)c >> 3, s * 16 + 4 * t + r, a.drop.worker + i, call);
+            raw_planes<T>(now, a.drop, u, w[r]);
         }
         if constexpr (VEC) fetch(s + 2 * (kStages - 1), behind);
         else fetch(s + 2, 0);
@@ -792,7 +808,6 @@ __global__ void __launch_bounds__(256) adapter_outer_kernel(const __grid_constan
                     e[k][px][pair] = __byte_perm(w[pair & 2][px][k], w[(pair & 2) + 1][px][k], pair & 1 ? 0x7632 : 0x5410);
 #pragma unroll
         for (int q = 0; q < NT; ++q) {
-            if (n0 + q >= ntiles) break;
             uint2 f[kPlanes];
 #pragma unroll
             for (int p = 0; p < kPlanes; ++p) f[p] = here[(q * kPlanes + p) * 32];
@@ -933,13 +948,10 @@ struct AdapterShape {
 // there, three quarters of the products are of zeros, and the fragments are written and read again for them.
 bool few(const AdapterShape& z) { return z.rows <= kFewRows; }
 
-int outer_ranks(int rank) { return rank <= 8 ? 1 : rank <= 16 ? 2 : rank <= 32 ? 4 : 8; }  // NT
-
 // Chunks of a worker's rows: as many as give each SM about two CTAs, of 64 rows at least.
 uint32_t outer_chunks(const AdapterShape& z, int64_t h) {
     if (few(z)) return 1;
-    const int nt = outer_ranks(z.rank) * 8;
-    const int64_t tiles = (h + kOuterColumns - 1) / kOuterColumns * ((z.rank + nt - 1) / nt) * z.n;
+    const int64_t tiles = (h + kOuterColumns - 1) / kOuterColumns * rank_groups(z.rank) * z.n;
     int64_t c = (148 * 2 + tiles - 1) / tiles;
     const int64_t most = (z.rows + 63) / 64;
     if (c > most) c = most;
@@ -1006,9 +1018,9 @@ AdapterArgs arguments(const AdapterShape& z, Rows x, int64_t h, const Low& low, 
 int prepare(const AdapterShape& z, bool shared, Factor down, int64_t down_h, uint4* down_frag, Factor up, int64_t up_h, uint4* up_frag,
             const float* t, uint2* t_outer, cudaStream_t stream) {
     PrepareArgs p = {down, up, down_frag, up_frag, t, t_outer, (int32_t)down_h, (int32_t)up_h, z.rank, (uint32_t)z.rows, 0, 0, 0, shared};
-    if (down_frag) p.down_count = (uint32_t)((down_h + kDownColumns - 1) / kDownColumns * ((z.rank + 7) / 8));
+    if (down_frag) p.down_count = (uint32_t)(down_blocks(down_h) * rank_tiles(z.rank));
     if (up_frag) p.up_count = (uint32_t)((up_h + kUpColumns - 1) / kUpColumns * ((z.rank + 15) / 16));
-    if (t_outer) p.t_count = (uint32_t)((z.rows + 15) / 16 * ((z.rank + 7) / 8));
+    if (t_outer) p.t_count = (uint32_t)((z.rows + 15) / 16 * rank_tiles(z.rank));
     const uint64_t ctas = ((uint64_t)p.down_count + p.up_count + p.t_count + 7) / 8;
     if (ctas > 0x0fffffffu) return COMPAMS_ERR_TOO_LARGE;
     const uint32_t workers = shared && !t_outer ? 1 : (uint32_t)z.n;
@@ -1026,29 +1038,30 @@ int down(Low low, Rows x, const AdapterShape& z, int64_t h, bool shared, Factor 
             auto kernel = vec ? adapter_down_few_kernel<T, true> : adapter_down_few_kernel<T, false>;
             return launched(launch_next(kernel, dim3((uint32_t)z.rank, (uint32_t)z.n), 1, 0, true, stream, a), "adapter_down");
         }
-        const int ntiles = (z.rank + 7) / 8;
-        auto go = [&](auto kernel, int nt, int wk, int mt, int shared_bytes) {
+        const uint32_t groups = rank_groups(z.rank);
+        auto go = [&](auto kernel, int wk, int mt, int shared_bytes) {
             const int per = 16 * 8 * mt / wk;
             a.tiles = (a.rows + per - 1) / per;
             // columns shared out over as many CTAs (of a cluster) as give each SM two, four steps each at least
-            const uint64_t tiles = (uint64_t)a.tiles * z.n * ((ntiles + nt - 1) / nt);
+            const uint64_t tiles = (uint64_t)a.tiles * z.n * groups;
             const int64_t steps = (h + 32 * down_step<T>() - 1) / (32 * down_step<T>()) / wk;
             a.split = 1;
             while (a.split < 8 && tiles * a.split < 2 * 148 / mt && steps >= 8 * a.split) a.split *= 2;
             const uint64_t ctas = (uint64_t)a.tiles * z.n * a.split;
             if (ctas > 0x7fffffffu) return (int)COMPAMS_ERR_TOO_LARGE;
-            return launched(launch_next(kernel, dim3((uint32_t)ctas, (ntiles + nt - 1) / nt), a.split, shared_bytes, false, stream, a),
+            return launched(launch_next(kernel, dim3((uint32_t)ctas, groups), a.split, shared_bytes, false, stream, a),
                             "adapter_down");
         };
         auto pick = [&](auto v, auto k, auto n, auto m) {
             constexpr bool V = decltype(v)::value;
             constexpr int WK = decltype(k)::value, NT = decltype(n)::value, MT = decltype(m)::value;
-            return go(adapter_down_kernel<T, V, NT, WK, MT>, NT, WK, MT, down_shared<T, V, NT, WK, MT>());
+            return go(adapter_down_kernel<T, V, NT, WK, MT>, WK, MT, down_shared<T, V, NT, WK, MT>());
         };
         auto by_ranks = [&](auto v, auto k) {
-            if (ntiles <= 1) return pick(v, k, Int<1>(), Int<1>());
-            if (ntiles <= 2) return pick(v, k, Int<2>(), Int<1>());
-            if (ntiles <= 4) return pick(v, k, Int<4>(), Int<1>());
+            const int nt = group_tiles(z.rank);
+            if (nt == 1) return pick(v, k, Int<1>(), Int<1>());
+            if (nt == 2) return pick(v, k, Int<2>(), Int<1>());
+            if (nt == 4) return pick(v, k, Int<4>(), Int<1>());
             // many rank indices: two blocks of rows to a warp, or the fragments' way through shared memory is the limit
             if constexpr (decltype(k)::value == 1) return pick(v, k, Int<8>(), Int<2>());
             else return pick(v, k, Int<8>(), Int<1>());
@@ -1072,7 +1085,6 @@ int up(void* y, Rows base, Low low, const AdapterShape& z, int64_t h, bool share
             auto kernel = vec ? adapter_up_few_kernel<T, true> : adapter_up_few_kernel<T, false>;
             return launched(launch_next(kernel, dim3(columns, (uint32_t)z.n), 1, 0, false, stream, a), "adapter_up");
         }
-        constexpr int PT = sizeof(T) == 4 ? 3 : 2;
         // row chunks: as many as give each SM about four CTAs
         const uint32_t blocks = (a.rows + 15) / 16, n = (uint32_t)z.n;
         uint64_t c = 148 * 4 / ((uint64_t)columns * n) + 1;
@@ -1082,7 +1094,7 @@ int up(void* y, Rows base, Low low, const AdapterShape& z, int64_t h, bool share
         auto go = [&](auto v, auto r) {
             constexpr bool V = decltype(v)::value;
             constexpr int RB = decltype(r)::value;
-            return launched(launch_next(adapter_up_kernel<T, V, RB, PT>, dim3(columns, n * a.tiles), 1, up_shared<T, V, RB, PT>(), false,
+            return launched(launch_next(adapter_up_kernel<T, V, RB>, dim3(columns, n * a.tiles), 1, up_shared<T, V, RB>(), false,
                                         stream, a),
                             "adapter_up");
         };
@@ -1090,7 +1102,7 @@ int up(void* y, Rows base, Low low, const AdapterShape& z, int64_t h, bool share
             const int ranks = (z.rank + 15) / 16;
             if (ranks == 1) return go(v, Int<1>());
             if (ranks == 2) return go(v, Int<2>());
-            if constexpr (PT == 2)
+            if constexpr (sizeof(T) == 2)
                 if (ranks == 4) return go(v, Int<4>());
             return go(v, Int<0>());
         };
@@ -1110,8 +1122,8 @@ int outer(float* out, bool sum_workers, Rows x, Low low, const AdapterShape& z, 
         if (few(z))
             return launched(launch_next(adapter_outer_few_kernel<T>, dim3((uint32_t)((h + 255) / 256), (uint32_t)z.n), 1, 0, first, stream, a),
                             "adapter_outer");
-        const int nt = outer_ranks(z.rank);
-        const uint64_t tiles = (uint64_t)((h + kOuterColumns - 1) / kOuterColumns) * ((z.rank + 8 * nt - 1) / (8 * nt));
+        const int nt = group_tiles(z.rank);
+        const uint64_t tiles = (uint64_t)((h + kOuterColumns - 1) / kOuterColumns) * rank_groups(z.rank);
         if (tiles > 0x7fffffffu) return (int)COMPAMS_ERR_TOO_LARGE;
         const bool vec = h % 8 == 0 && x.aligned();
         auto go = [&](auto v, auto m) {
@@ -1153,9 +1165,9 @@ Places places(const AdapterShape& z, bool shared, bool backward, bool sum_worker
     p.down = take(frags ? factors * down_frag_words(backward ? z.out : z.in, z.rank) * 16 : 0);
     p.up = take(frags ? factors * up_frag_words(backward ? z.in : z.out, z.rank) * 16 : 0);
     p.t = take(backward && !frags ? (int64_t)z.total() * z.rank * 4 : 0);
-    p.t_up = take(frags ? z.n * t_up_words(z.rows, z.rank) * 16 : 0);
-    p.t_outer = take(frags && backward ? z.n * t_outer_words(z.rows, z.rank) * 8 : 0);
-    p.saved = take(frags && backward ? z.n * t_outer_words(z.rows, z.rank) * 8 : 0);
+    p.t_up = take(frags ? z.n * t_up_words(z.rows, z.rank, kPlanes) * 16 : 0);
+    p.t_outer = take(frags && backward ? z.n * t_outer_words(z.rows, z.rank) * 16 : 0);
+    p.saved = take(frags && backward ? z.n * t_outer_words(z.rows, z.rank) * 16 : 0);
     const int64_t fa = backward ? outer_floats(z, z.in, sum_workers) : 0, fb = backward ? outer_floats(z, z.out, sum_workers) : 0;
     p.partial = take((fa > fb ? fa : fb) * 4);
     p.bytes = at;

@@ -121,7 +121,7 @@ __device__ __forceinline__ void span_store(T* __restrict__ row, int c0, int h, i
 // against the 22 or so that a sweep which reads and writes 2 bytes an element has time for at the memory's rate.
 struct Drop {
     uint32_t key[20];         // the ten rounds' keys
-    uint32_t threshold;       // t in the upper 16 bits; all ones: everything is dropped
+    uint32_t limit;           // t in the upper 16 bits, less 1; all ones: everything is dropped
     float factor;             // 65536 / (65536 - t)
     uint32_t call;            // added to *call_device
     uint32_t worker;          // the number of the first worker
@@ -133,8 +133,8 @@ __device__ __forceinline__ uint32_t drop_call(const Drop& d) {
     return d.call + (d.on && d.call_device ? (uint32_t)*d.call_device : 0u);
 }
 
-// The eight bits of columns 8 group ... 8 group + 7.
-__device__ __forceinline__ uint32_t drop_bits(const Drop& d, uint32_t group, uint32_t row, uint32_t worker, uint32_t call) {
+// The block of columns 8 group ... 8 group + 7.
+__device__ __forceinline__ uint4 drop_words(const Drop& d, uint32_t group, uint32_t row, uint32_t worker, uint32_t call) {
     uint32_t c0 = group, c1 = row, c2 = worker, c3 = call;
 #pragma unroll
     for (int r = 0; r < 10; ++r) {
@@ -144,24 +144,35 @@ __device__ __forceinline__ uint32_t drop_bits(const Drop& d, uint32_t group, uin
         c2 = (uint32_t)(a >> 32) ^ c3 ^ d.key[2 * r + 1];
         c3 = (uint32_t)a;
     }
-    const uint32_t w[4] = {c0, c1, c2, c3}, t = d.threshold;
+    return make_uint4(c0, c1, c2, c3);
+}
+// Whether element k of the eight is kept: its half, in the upper 16 bits, is above the limit, whatever the lower 16 are.
+__device__ __forceinline__ bool drop_keeps(const Drop& d, const uint4& u, int k) {
+    const uint32_t w = k < 2 ? u.x : k < 4 ? u.y : k < 6 ? u.z : u.w;
+    return (k & 1 ? w : w << 16) > d.limit;
+}
+__device__ __forceinline__ void drop8(const Drop& d, const uint4& u, float (&v)[8]) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = drop_keeps(d, u, k) ? v[k] * d.factor : 0.0f;
+}
+__device__ __forceinline__ uint32_t drop_bits(const Drop& d, uint32_t group, uint32_t row, uint32_t worker, uint32_t call) {
+    const uint4 u = drop_words(d, group, row, worker, call);
     uint32_t bits = 0;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        if ((w[k] << 16) >= t) bits |= 1u << (2 * k);
-        if ((w[k] & 0xffff0000u) >= t) bits |= 2u << (2 * k);
-    }
+    for (int k = 0; k < 8; ++k) bits |= drop_keeps(d, u, k) ? 1u << k : 0u;
     return bits;
 }
 
 // Dropout of a lane's values of a span; the whole warp takes part.
 template <bool VEC>
 __device__ __forceinline__ void span_drop(const Drop& d, int c0, uint32_t row, uint32_t worker, uint32_t call, int lane, float (&v)[8]) {
-    const uint32_t bits = drop_bits(d, (uint32_t)(c0 >> 3) + lane, row, worker, call);
+    if (VEC) {
+        drop8(d, drop_words(d, (uint32_t)(c0 >> 3) + lane, row, worker, call), v);
+    } else {
+        const uint32_t bits = drop_bits(d, (uint32_t)(c0 >> 3) + lane, row, worker, call);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        const bool keep = VEC ? (bits >> k) & 1u : (__shfl_sync(0xffffffffu, bits, k * 4 + (lane >> 3)) >> (lane & 7)) & 1u;
-        v[k] = keep ? v[k] * d.factor : 0.0f;
+        for (int k = 0; k < 8; ++k)
+            v[k] = (__shfl_sync(0xffffffffu, bits, k * 4 + (lane >> 3)) >> (lane & 7)) & 1u ? v[k] * d.factor : 0.0f;
     }
 }
 
@@ -173,7 +184,7 @@ inline bool make_drop(Drop& d, double p, uint64_t seed, uint32_t call, const int
         d.key[2 * r] = (uint32_t)seed + r * 0x9E3779B9u;
         d.key[2 * r + 1] = (uint32_t)(seed >> 32) + r * 0xBB67AE85u;
     }
-    d.threshold = t < 65536u ? t << 16 : 0xffffffffu;
+    d.limit = t < 65536u ? (t << 16) - 1u : 0xffffffffu;
     d.factor = t < 65536u ? (float)(65536.0 / (65536.0 - t)) : 0.0f;
     d.call = call;
     d.worker = worker;
