@@ -25,6 +25,7 @@ The operators run on the current stream of x's device. They are differentiable o
 from __future__ import annotations
 
 import ctypes
+import functools
 from typing import Optional, Tuple, Union
 
 import torch
@@ -67,10 +68,11 @@ def _activation(x: torch.Tensor) -> None:
 
 def _factor(w: torch.Tensor, x: torch.Tensor, inner: Tuple[int, ...], what: str) -> torch.Tensor:
     """A float32 parameter of shape `inner`, for all workers or ([n, *inner]) for each; its last axis packed."""
-    if not isinstance(w, torch.Tensor) or w.device != x.device or w.dtype != torch.float32 or (
-            tuple(w.shape) != inner and tuple(w.shape) != (x.shape[0],) + inner):
+    if not isinstance(w, torch.Tensor) or w.dtype is not torch.float32 or w.device != x.device or (
+            w.shape != inner and w.shape != (x.shape[0], *inner)):
         raise CompAMSError("%s must be a float32 tensor %s or %s on %s" % (what, list(inner), [x.shape[0], *inner], x.device))
-    w = w.resolve_neg()
+    if w.is_neg():
+        w = w.resolve_neg()
     return w if w.stride(-1) == 1 or w.shape[-1] == 1 else w.contiguous()
 
 
@@ -101,25 +103,66 @@ class _Drop:
         return self.p, self.seed, self.call, None if self.tensor is None else self.tensor.data_ptr(), self.worker
 
 
+class _Nothing:
+    """No dropout."""
+    tensor = None
+
+    @staticmethod
+    def args():
+        return 0.0, 0, 0, None, 0
+
+
+_NOTHING = _Nothing()
+
+
 def _run(name: str, device: torch.device, *args) -> None:
     fn = getattr(load_library(), name)
-    if torch.cuda.current_device() == device.index:
-        rc = fn(*args, torch.cuda.current_stream(device).cuda_stream)
+    index = device.index
+    if torch.cuda.current_device() == index:
+        rc = fn(*args, _stream(index))
     else:
         with torch.cuda.device(device):
-            rc = fn(*args, torch.cuda.current_stream(device).cuda_stream)
+            rc = fn(*args, _stream(index))
     if rc:
         _check(rc, name)
 
 
-def _workspace(name: str, device: torch.device, *shape) -> torch.Tensor:
+def _stream(index: int) -> int:
+    """The current stream of a device, as the library takes it. (torch.cuda.current_stream(index).cuda_stream is the same number and
+    takes 2 us, a tenth of a single token's layer norm.)"""
+    return torch._C._cuda_getCurrentRawStream(index)
+
+
+@functools.lru_cache(maxsize=1024)
+def _workspace_bytes(name: str, device: torch.device, *shape) -> int:
     need = ctypes.c_size_t(0)
-    fn = getattr(load_library(), name)
     with torch.cuda.device(device):
-        rc = fn(ctypes.byref(need), *shape)
+        rc = getattr(load_library(), name)(ctypes.byref(need), *shape)
     if rc:
         _check(rc, name)
-    return torch.empty(need.value, dtype=torch.uint8, device=device)
+    return need.value
+
+
+def _workspace(name: str, like: torch.Tensor, *shape) -> torch.Tensor:
+    return like.new_empty(_workspace_bytes(name, like.device, *shape), dtype=torch.uint8)
+
+
+def _once(backward):
+    """A backward pass that is not differentiable itself. (torch's once_differentiable costs 8 us, and says no more than this where no
+    graph of the backward pass is asked for.)"""
+    guarded = torch.autograd.function.once_differentiable(backward)
+
+    def run(ctx, *grads):
+        return guarded(ctx, *grads) if torch.is_grad_enabled() else backward(ctx, *grads)
+
+    return run
+
+
+def _empty(like: torch.Tensor, dtype: Optional[torch.dtype] = None) -> torch.Tensor:
+    """Packed, of the same shape."""
+    if dtype is None or dtype == like.dtype:
+        return torch.empty_like(like) if like.is_contiguous() else like.new_empty(like.shape)
+    return like.new_empty(like.shape, dtype=dtype)
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -134,7 +177,7 @@ def _wants_gradient(*tensors) -> bool:
 
 
 def _dropout(x: torch.Tensor, drop: _Drop) -> torch.Tensor:
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    y = _empty(x)
     if x.numel():
         v, rows, ws, rs = _rows(x)
         _run("compams_dropout", x.device, y.data_ptr(), v.data_ptr(), _TYPES[x.dtype], x.shape[0], rows, x.shape[-1], ws, rs,
@@ -150,7 +193,7 @@ class _DropoutFunction(torch.autograd.Function):
         return _dropout(x, drop)
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
+    @_once
     def backward(ctx, dy):
         ctx.saved_tensors  # raises where the device-held call has been changed since
         return _dropout(dy, ctx.drop), None
@@ -168,9 +211,9 @@ def dropout(x: torch.Tensor, p: float, seed: int = 0, call: Call = 0, worker: in
 
 
 def _norm_forward(x, residual, weight, bias, eps, drop, keep_stats):
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    s = None if residual is None else torch.empty(x.shape, dtype=residual.dtype, device=x.device)
-    stats = torch.empty(x.numel() // x.shape[-1], 2, dtype=torch.float32, device=x.device) if keep_stats else None
+    y = _empty(x)
+    s = None if residual is None else _empty(x, residual.dtype)
+    stats = x.new_empty((x.numel() // x.shape[-1], 2), dtype=torch.float32) if keep_stats else None
     if x.numel():
         v, rows, ws, rs = _rows(x)
         r, rws, rrs = None, 0, 0
@@ -187,19 +230,19 @@ def _norm_backward(ctx, dy, ds, v, stats, weight, added):
     needs_x, needs_r, needs_w, needs_b = ctx.wanted
     device, n, h = v.device, v.shape[0], v.shape[-1]
     apart = ctx.apart  # the workers' gradients stay apart
-    dx = torch.empty(v.shape, dtype=ctx.dtype, device=device) if needs_x else None
-    dres = torch.empty(v.shape, dtype=v.dtype, device=device) if needs_r else None
-    make = torch.empty if v.numel() else torch.zeros
-    dw = make(*((n, h) if apart else (h,)), dtype=torch.float32, device=device) if needs_w else None
-    db = make(*((n, h) if apart else (h,)), dtype=torch.float32, device=device) if needs_b else None
+    dx = _empty(v, ctx.dtype) if needs_x else None
+    dres = _empty(v) if needs_r else None
+    make = v.new_empty if v.numel() else v.new_zeros
+    dw = make((n, h) if apart else (h,), dtype=torch.float32) if needs_w else None
+    db = make((n, h) if apart else (h,), dtype=torch.float32) if needs_b else None
     if v.numel():
-        dy = torch.zeros(v.shape, dtype=ctx.dtype, device=device) if dy is None else dy
+        dy = v.new_zeros(v.shape, dtype=ctx.dtype) if dy is None else dy
         g, rows, gws, grs = _rows(dy)
         w, _, vws, vrs = _rows(v)
         e, ews, ers = None, 0, 0
         if ds is not None:
             e, _, ews, ers = _rows(ds)
-        work = _workspace("compams_norm_workspace_bytes", device, n, rows, h) if needs_w or needs_b else None
+        work = _workspace("compams_norm_workspace_bytes", v, n, rows, h) if needs_w or needs_b else None
         _run("compams_norm_backward", device, _ptr(dx), _ptr(dres), _ptr(dw), _ptr(db), 0 if apart else 1, g.data_ptr(), _ptr(e),
              w.data_ptr(), stats.data_ptr(), _TYPES[ctx.dtype], _TYPES[v.dtype], n, rows, h, gws, grs, ews, ers, vws, vrs,
              *_affine(weight), 1 if added else 0, *ctx.drop.args(), _ptr(work), 0 if work is None else work.numel())
@@ -208,19 +251,19 @@ def _norm_backward(ctx, dy, ds, v, stats, weight, added):
 
 class _LayerNormFunction(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, weight, bias, eps, drop):
-        y, _, stats = _norm_forward(x, None, weight, bias, eps, drop, True)
+    def forward(ctx, x, weight, bias, eps):
+        y, _, stats = _norm_forward(x, None, weight, bias, eps, _NOTHING, True)
         ctx.save_for_backward(x, stats, *([weight] if weight is not None else []))
-        ctx.drop, ctx.dtype, ctx.apart = drop, x.dtype, any(t is not None and t.dim() == 2 for t in (weight, bias))
+        ctx.drop, ctx.dtype, ctx.apart = _NOTHING, x.dtype, any(t is not None and t.dim() == 2 for t in (weight, bias))
         return y
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
+    @_once
     def backward(ctx, dy):
         x, stats, *weight = ctx.saved_tensors
         ctx.wanted = (ctx.needs_input_grad[0], False, *ctx.needs_input_grad[1:3])
         dx, _, dw, db = _norm_backward(ctx, dy, None, x, stats, weight[0] if weight else None, False)
-        return dx, dw, db, None, None
+        return dx, dw, db, None
 
 
 class _AddNormFunction(torch.autograd.Function):
@@ -234,7 +277,7 @@ class _AddNormFunction(torch.autograd.Function):
         return y, s
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
+    @_once
     def backward(ctx, dy, ds):
         s, stats, *more = ctx.saved_tensors
         ctx.wanted = ctx.needs_input_grad[:4]
@@ -260,10 +303,9 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
     [h] or [n, h]."""
     _activation(x)
     weight, bias, eps = _norm_parameters(x, weight, bias, eps)
-    drop = _Drop(x, 0.0, 0, 0, 0)
     if _wants_gradient(x, weight, bias):
-        return _LayerNormFunction.apply(x, weight, bias, eps, drop)
-    return _norm_forward(x, None, weight, bias, eps, drop, False)[0]
+        return _LayerNormFunction.apply(x, weight, bias, eps)
+    return _norm_forward(x, None, weight, bias, eps, _NOTHING, False)[0]
 
 
 def dropout_add_layer_norm(x: torch.Tensor, residual: torch.Tensor, weight: Optional[torch.Tensor] = None,
@@ -294,14 +336,14 @@ def _shared(a: torch.Tensor, b: torch.Tensor) -> int:
 
 def _adapter_forward(x, base, a, b, scale, drop):
     n, rank, out = x.shape[0], a.shape[-2], b.shape[-2]
-    y = torch.empty(*x.shape[:-1], out, dtype=x.dtype, device=x.device)
-    t = torch.empty(x.numel() // x.shape[-1], rank, dtype=torch.float32, device=x.device)
+    y = x.new_empty((*x.shape[:-1], out)) if base is None else _empty(base)
+    t = x.new_empty((x.numel() // x.shape[-1], rank), dtype=torch.float32)
     if x.numel():
         v, rows, ws, rs = _rows(x)
         z, zws, zrs = None, 0, 0
         if base is not None:
             z, _, zws, zrs = _rows(base)
-        work = _workspace("compams_adapter_workspace_bytes", x.device, n, rows, x.shape[-1], out, rank, _shared(a, b), 0, 0)
+        work = _workspace("compams_adapter_workspace_bytes", x, n, rows, x.shape[-1], out, rank, _shared(a, b), 0, 0)
         _run("compams_adapter_forward", x.device, y.data_ptr(), t.data_ptr(), v.data_ptr(), _ptr(z), _TYPES[x.dtype], n, rows,
              x.shape[-1], out, rank, ws, rs, zws, zrs, *_stacked(a), *_stacked(b), scale, *drop.args(), _ptr(work), work.numel())
     return y, t
@@ -316,19 +358,19 @@ class _AdapterFunction(torch.autograd.Function):
         return y
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
+    @_once
     def backward(ctx, dy):
         x, t, a, b = ctx.saved_tensors[:4]
         needs_x, needs_base, needs_a, needs_b = ctx.needs_input_grad[:4]
         n, h, rank, out = x.shape[0], x.shape[-1], a.shape[-2], b.shape[-2]
-        make = torch.empty if x.numel() else torch.zeros
-        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if needs_x else None
-        da = make(a.shape, dtype=torch.float32, device=x.device) if needs_a else None
-        db = make(b.shape, dtype=torch.float32, device=x.device) if needs_b else None
+        make = a.new_empty if x.numel() else a.new_zeros
+        dx = _empty(x) if needs_x else None
+        da = make(a.shape) if needs_a else None
+        db = make(b.shape) if needs_b else None
         if x.numel() and (needs_x or needs_a or needs_b):
             g, rows, gws, grs = _rows(dy)
             v, _, ws, rs = _rows(x)
-            work = _workspace("compams_adapter_workspace_bytes", x.device, n, rows, h, out, rank, _shared(a, b), 1,
+            work = _workspace("compams_adapter_workspace_bytes", x, n, rows, h, out, rank, _shared(a, b), 1,
                               0 if a.dim() == 3 else 1)
             _run("compams_adapter_backward", x.device, _ptr(dx), _ptr(da), _ptr(db), 0 if a.dim() == 3 else 1, g.data_ptr(),
                  v.data_ptr(), t.data_ptr(), _TYPES[x.dtype], n, rows, h, out, rank, gws, grs, ws, rs, *_stacked(a), *_stacked(b),
