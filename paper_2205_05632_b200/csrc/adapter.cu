@@ -255,14 +255,6 @@ template <int SLOTS>
 __device__ __forceinline__ uint4* ring_at(char* smem, int stage, int slot) {
     return reinterpret_cast<uint4*>(smem) + (stage * SLOTS + slot) * 256 + threadIdx.x;
 }
-__device__ __forceinline__ void copy16(void* shared, const void* global, bool there) {  // zeros where it is not
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(shared)), "l"(global),
-                 "r"(there ? 16 : 0)
-                 : "memory");
-}
-__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 template <int N, typename T>
 __device__ __forceinline__ Raw8<T> ring_raw(char* smem, int stage, int slot) {  // slot: of the first 16 bytes
     Raw8<T> r;

@@ -9,6 +9,10 @@
 //
 // All bound by memory. Sums and statistics are fp32, the variance is summed over differences from the mean (the row stays in
 // registers), weights, biases and their gradients are fp32 as the optimizer keeps them.
+#include <string.h>
+
+#include <type_traits>
+
 #include "context.h"
 #include "rows.cuh"
 
@@ -55,7 +59,7 @@ __device__ __forceinline__ float row_sum(float x, float* scratch, int warp) {
 constexpr int kRowsOfOneWarp = 8;  // rows of a CTA whose warps take a row each
 
 template <int W>
-constexpr int norm_threads() { return W == 1 ? 32 * kRowsOfOneWarp : 32 * W; }
+__host__ __device__ constexpr int norm_threads() { return W == 1 ? 32 * kRowsOfOneWarp : 32 * W; }
 
 // ---- forward ---------------------------------------------------------------------------------------------------------------
 
@@ -167,99 +171,174 @@ __global__ void __launch_bounds__(512) norm_forward_long_kernel(const __grid_con
 
 // ---- backward --------------------------------------------------------------------------------------------------------------
 
-// A CTA goes through the rows of one chunk of one worker and keeps the sums of dy xhat and dy of its columns in registers.
+// A CTA goes through the rows of one chunk of one worker and keeps the sums of dy xhat and dy of its columns in registers, the weight too.
+// W warps to a row, NG spans to a warp. Where rows are aligned (VEC) every lane copies what it will need of the next rows into places of
+// shared memory that it alone reads, two rows ahead, so that the two sums that a row waits for (one barrier) do not
+// stop the loads: [stage][operand][span][16 bytes][thread]. With several spans to a warp the values are taken from there a second time
+// behind the barrier instead of being held, and with four the weight is read again for each row: registers are what bounds the CTAs
+// of an SM.
+template <typename TX, typename TR, int W, int NG, bool ADD>
+__host__ __device__ constexpr int backward_ring() {  // 16-byte slots of a lane in a stage
+    return NG * ((int)sizeof(Raw8<TX>) + (ADD ? 2 : 1) * (int)sizeof(Raw8<TR>)) / 16;
+}
+// Stages of it: three where an SM has the room, or two; none for the longest rows of fp32, which are read where they are used.
+template <typename TX, typename TR, int W, int NG, bool VEC, bool ADD>
+__host__ __device__ constexpr int backward_stages() {
+    const int bytes = backward_ring<TX, TR, W, NG, ADD>() * 16 * norm_threads<W>();
+    return !VEC || 2 * bytes > 200 * 1024 ? 0 : 3 * bytes > 200 * 1024 ? 2 : 3;
+}
+template <typename TX, typename TR, int W, int NG, bool VEC, bool ADD>
+__host__ __device__ constexpr int backward_shared() {
+    return backward_stages<TX, TR, W, NG, VEC, ADD>() * backward_ring<TX, TR, W, NG, ADD>() * 16 * norm_threads<W>();
+}
+
 template <typename TX, typename TR, int W, int NG, bool VEC, bool ADD>
 __global__ void __launch_bounds__(norm_threads<W>()) norm_backward_kernel(const __grid_constant__ NormArgs a) {
-    constexpr int kSlots = W == 1 ? kRowsOfOneWarp : 1;
+    extern __shared__ __align__(16) char smem[];
+    constexpr int kSlots = W == 1 ? kRowsOfOneWarp : 1, kThreadsHere = norm_threads<W>();
+    constexpr int SX = (int)sizeof(Raw8<TX>) / 16, SR = (int)sizeof(Raw8<TR>) / 16, RING = backward_ring<TX, TR, W, NG, ADD>();
+    constexpr int kStages = backward_stages<TX, TR, W, NG, VEC, ADD>();
     __shared__ float scratch[2][2][W];
     __shared__ float joined[W == 1 ? NG * kSpan : 1];
     const int lane = threadIdx.x & 31, warp = W == 1 ? 0 : (int)(threadIdx.x >> 5), slot = W == 1 ? (int)(threadIdx.x >> 5) : 0;
     const uint32_t i = blockIdx.x / a.chunks, chunk = blockIdx.x - i * a.chunks;
     const uint32_t j0 = (uint32_t)((uint64_t)a.rows * chunk / a.chunks), j1 = (uint32_t)((uint64_t)a.rows * (chunk + 1) / a.chunks);
-    const float* weight = a.weight ? a.weight + (int64_t)i * a.weight_ws : nullptr;
     const uint32_t call = drop_call(a.drop);
-    float dw[NG][8], db[NG][8];
+    const TX* dy = (const TX*)a.x + (int64_t)i * a.x_ws;
+    const TR* v = (const TR*)a.v + (int64_t)i * a.v_ws;
+    const TR* more = ADD && a.residual ? (const TR*)a.residual + (int64_t)i * a.r_ws : nullptr;
+    constexpr bool kHold = NG == 1, kHoldWeight = NG <= 2;
+    float held[kHoldWeight ? NG : 1][8], dw[NG][8], db[NG][8];
+    auto weight = [&](int q, float (&w)[8]) {
 #pragma unroll
-    for (int q = 0; q < NG; ++q)
+        for (int k = 0; k < 8; ++k) w[k] = 1.0f;
+        if (a.weight) span_load<float, VEC>(a.weight + (int64_t)i * a.weight_ws, (q * W + warp) * kSpan, a.h, lane, w);
+    };
+#pragma unroll
+    for (int q = 0; q < NG; ++q) {
 #pragma unroll
         for (int k = 0; k < 8; ++k) dw[q][k] = db[q][k] = 0.0f;
-    int turn = 0;
+        if (kHoldWeight) weight(q, held[kHoldWeight ? q : 0]);
+    }
+    auto place = [&](int stage, int at) { return reinterpret_cast<uint4*>(smem) + (stage * RING + at) * kThreadsHere + threadIdx.x; };
+    auto fetch = [&](uint32_t j, int stage) {
+        if constexpr (kStages > 0) {
+#pragma unroll
+            for (int q = 0; q < NG; ++q) {
+                const int c = (q * W + warp) * kSpan + lane * 8;
+                if (j < j1 && c < a.h) {
+                    const char* gx = reinterpret_cast<const char*>(dy + (int64_t)j * a.x_rs + c);
+                    const char* gv = reinterpret_cast<const char*>(v + (int64_t)j * a.v_rs + c);
+#pragma unroll
+                    for (int k = 0; k < SX; ++k) copy16(place(stage, q * SX + k), gx + 16 * k);
+#pragma unroll
+                    for (int k = 0; k < SR; ++k) copy16(place(stage, NG * SX + q * SR + k), gv + 16 * k);
+                    if (ADD && more) {
+                        const char* gr = reinterpret_cast<const char*>(more + (int64_t)j * a.r_rs + c);
+#pragma unroll
+                        for (int k = 0; k < SR; ++k) copy16(place(stage, NG * (SX + SR) + q * SR + k), gr + 16 * k);
+                    }
+                }
+            }
+            copies_commit();
+        }
+    };
+    // a lane's values of span q, `beyond` in the columns from h on
+    auto take = [&](auto type, const auto* row, int stage, int at, int q, float beyond, float (&to)[8]) {
+        using T = decltype(type);
+        const int c0 = (q * W + warp) * kSpan;
+        if constexpr (kStages > 0) {
+            if (c0 + lane * 8 < a.h) {
+                Raw8<T> r;
+                uint4 u[sizeof(r) / 16];
+#pragma unroll
+                for (int k = 0; k < (int)sizeof(r) / 16; ++k) u[k] = *place(stage, at + q * (int)sizeof(r) / 16 + k);
+                memcpy(&r, u, sizeof(r));
+                raw_floats<T>(r, to);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) to[k] = beyond;
+            }
+        } else {
+            span_load<T, VEC>(row, c0, a.h, lane, to, beyond);
+        }
+    };
+    for (int k = 0; k + 1 < kStages; ++k) fetch(j0 + slot + k * kSlots, k);
+    int turn = 0, stage = 0;
+    float2 next = j0 + slot < j1 ? a.stats[i * a.rows + j0 + slot] : make_float2(0.0f, 0.0f);
     for (uint32_t j = j0 + slot; j < j1; j += kSlots, turn ^= 1) {
         const uint32_t m = i * a.rows + j;
-        const TX* dy = (const TX*)a.x + (int64_t)i * a.x_ws + (int64_t)j * a.x_rs;
-        const TR* v = (const TR*)a.v + (int64_t)i * a.v_ws + (int64_t)j * a.v_rs;
-        float g[NG][8], xhat[NG][8];
-        const float2 st = a.stats[m];
-        float c1 = 0.0f, c2 = 0.0f;
-#pragma unroll
-        for (int q = 0; q < NG; ++q) {
-            span_load<TX, VEC>(dy, (q * W + warp) * kSpan, a.h, lane, g[q]);
-            span_load<TR, VEC>(v, (q * W + warp) * kSpan, a.h, lane, xhat[q], st.x);
-        }
-#pragma unroll
-        for (int q = 0; q < NG; ++q) {
-            const int c0 = (q * W + warp) * kSpan;
+        const float2 st = next;
+        if (j + kSlots < j1) next = a.stats[m + kSlots];
+        if constexpr (kStages > 0) fetch(j + (kStages - 1) * kSlots, stage == 0 ? kStages - 1 : stage - 1);
+        if constexpr (kStages > 0) copies_wait<kStages - 1>();  // a lane's own
+        float g[8], xhat[8], c1 = 0.0f, c2 = 0.0f;
+        // dy w and xhat of span q; the first time its share of the sums
+        auto values = [&](int q, bool first) {
+            take(TX(), dy + (int64_t)j * a.x_rs, stage, 0, q, 0.0f, g);
+            take(TR(), v + (int64_t)j * a.v_rs, stage, NG * SX, q, st.x, xhat);
             float w[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) w[k] = 1.0f;
-            if (weight) span_load<float, VEC>(weight, c0, a.h, lane, w);
+            if (!kHoldWeight) weight(q, w);
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                xhat[q][k] = (xhat[q][k] - st.x) * st.y;
-                db[q][k] += g[q][k];
-                dw[q][k] = fmaf(g[q][k], xhat[q][k], dw[q][k]);
-                g[q][k] *= w[k];
-                c1 += g[q][k];
-                c2 = fmaf(g[q][k], xhat[q][k], c2);
+                xhat[k] = (xhat[k] - st.x) * st.y;
+                if (first) {
+                    db[q][k] += g[k];
+                    dw[q][k] = fmaf(g[k], xhat[k], dw[q][k]);
+                }
+                g[k] *= kHoldWeight ? held[kHoldWeight ? q : 0][k] : w[k];
+                if (first) {
+                    c1 += g[k];
+                    c2 = fmaf(g[k], xhat[k], c2);
+                }
+            }
+        };
+#pragma unroll
+        for (int q = 0; q < NG; ++q) values(q, true);
+        if (a.y || (ADD && a.s)) {
+            c1 = warp_sum(c1);
+            c2 = warp_sum(c2);
+            if (W > 1) {
+                if (lane == 0) {
+                    scratch[turn][0][warp] = c1;
+                    scratch[turn][1][warp] = c2;
+                }
+                __syncthreads();  // the next row writes the other half, and the one after it only behind the next row's barrier
+                c1 = c2 = 0.0f;
+#pragma unroll
+                for (int k = 0; k < W; ++k) {
+                    c1 += scratch[turn][0][k];
+                    c2 += scratch[turn][1][k];
+                }
+            }
+            c1 *= 1.0f / (float)a.h;
+            c2 *= 1.0f / (float)a.h;
+#pragma unroll
+            for (int q = 0; q < NG; ++q) {
+                const int c0 = (q * W + warp) * kSpan;
+                if (c0 >= a.h) break;
+                if (!kHold) values(q, false);
+                float add[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) add[k] = 0.0f;
+                if (ADD && more) take(TR(), more + (int64_t)j * a.r_rs, stage, NG * (SX + SR), q, 0.0f, add);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) g[k] = fmaf(st.y, g[k] - c1 - xhat[k] * c2, add[k]);
+                if (ADD && a.s) span_store<TR, VEC>((TR*)a.s + (int64_t)m * a.h, c0, a.h, lane, g);
+                if (ADD && a.drop.on && a.y) span_drop<VEC>(a.drop, c0, j, a.drop.worker + i, call, lane, g);
+                if (a.y) span_store<TX, VEC>((TX*)a.y + (int64_t)m * a.h, c0, a.h, lane, g);
             }
         }
-        if (!a.y && !a.s) continue;
-        c1 = warp_sum(c1);
-        c2 = warp_sum(c2);
-        if (W > 1) {
-            if (lane == 0) {
-                scratch[turn][0][warp] = c1;
-                scratch[turn][1][warp] = c2;
-            }
-            __syncthreads();  // the next row writes the other half, and the one after it only behind the next row's barrier
-            c1 = c2 = 0.0f;
-#pragma unroll
-            for (int w = 0; w < W; ++w) {
-                c1 += scratch[turn][0][w];
-                c2 += scratch[turn][1][w];
-            }
-        }
-        c1 /= (float)a.h;
-        c2 /= (float)a.h;
-        const TR* more = ADD && a.residual ? (const TR*)a.residual + (int64_t)i * a.r_ws + (int64_t)j * a.r_rs : nullptr;
-#pragma unroll
-        for (int q = 0; q < NG; ++q) {
-            const int c0 = (q * W + warp) * kSpan;
-            if (c0 >= a.h) break;
-            float add[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) add[k] = 0.0f;
-            if (more) span_load<TR, VEC>(more, c0, a.h, lane, add);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) g[q][k] = fmaf(st.y, g[q][k] - c1 - xhat[q][k] * c2, add[k]);
-            if (ADD && a.s) span_store<TR, VEC>((TR*)a.s + (int64_t)m * a.h, c0, a.h, lane, g[q]);
-            if (ADD && a.drop.on && a.y) span_drop<VEC>(a.drop, c0, j, a.drop.worker + i, call, lane, g[q]);
-            if (a.y) span_store<TX, VEC>((TX*)a.y + (int64_t)m * a.h, c0, a.h, lane, g[q]);
-        }
+        stage = stage + 1 == kStages ? 0 : stage + 1;
     }
     if (!a.partial) return;
     float* out = a.partial + (int64_t)blockIdx.x * 2 * a.h;
     if constexpr (W > 1) {
 #pragma unroll
-        for (int q = 0; q < NG; ++q)
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const int c = span_column<VEC>((q * W + warp) * kSpan, lane, k);
-                if (c < a.h) {
-                    out[c] = dw[q][k];
-                    out[a.h + c] = db[q][k];
-                }
-            }
+        for (int q = 0; q < NG; ++q) {
+            span_store<float, VEC>(out, (q * W + warp) * kSpan, a.h, lane, dw[q]);
+            span_store<float, VEC>(out + a.h, (q * W + warp) * kSpan, a.h, lane, db[q]);
+        }
     } else {  // warps with rows of their own: their sums joined one warp after the other
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
@@ -368,20 +447,40 @@ __global__ void __launch_bounds__(256) norm_join_kernel(const float* __restrict_
 
 // ---- dropout ---------------------------------------------------------------------------------------------------------------
 
-// A warp per span of a row.
-template <typename T, bool VEC>
+// A warp takes four spans, one after the other in the order of memory; their loads stand before the first mask. U: a number of spans.
+constexpr int kDropSpans = 4;
+template <typename T, bool VEC, typename U>
 __global__ void __launch_bounds__(256) dropout_kernel(const T* __restrict__ x, T* __restrict__ y, int64_t ws, int64_t rs, uint32_t rows,
                                                       uint32_t total, int32_t h, uint32_t spans, const __grid_constant__ Drop d) {
     const int lane = threadIdx.x & 31;
-    const uint64_t at = (uint64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-    const uint64_t m64 = at / spans;
-    if (m64 >= total) return;
-    const uint32_t m = (uint32_t)m64, i = m / rows, j = m - i * rows;
-    const int c0 = (int)(at - m64 * spans) * kSpan;
-    float v[8];
-    span_load<T, VEC>(x + (int64_t)i * ws + (int64_t)j * rs, c0, h, lane, v);
-    if (d.on) span_drop<VEC>(d, c0, j, d.worker + i, drop_call(d), lane, v);
-    span_store<T, VEC>(y + (int64_t)m * h, c0, h, lane, v);
+    const U at = ((U)blockIdx.x * 8 + (threadIdx.x >> 5)) * kDropSpans;
+    uint32_t m = (uint32_t)(at / spans), span = (uint32_t)(at - (U)m * spans), i = m / rows, j = m - i * rows;
+    const uint32_t call = drop_call(d);
+    float v[kDropSpans][8];
+    uint32_t worker[kDropSpans], row[kDropSpans];
+    int c0[kDropSpans];
+    T* to[kDropSpans];
+#pragma unroll
+    for (int k = 0; k < kDropSpans; ++k) {
+        c0[k] = m < total ? (int)span * kSpan : h;
+        worker[k] = i;
+        row[k] = j;
+        to[k] = y + (int64_t)m * h;
+        span_load<T, VEC>(x + (int64_t)i * ws + (int64_t)j * rs, c0[k], h, lane, v[k]);
+        if (++span == spans) {
+            span = 0;
+            ++m;
+            if (++j == rows) {
+                j = 0;
+                ++i;
+            }
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kDropSpans; ++k) {
+        if (d.on) span_drop<VEC>(d, c0[k], row[k], d.worker + worker[k], call, lane, v[k]);
+        span_store<T, VEC>(to[k], c0[k], h, lane, v[k]);
+    }
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------------
@@ -396,16 +495,25 @@ struct Shape {
     }
 };
 
+// Warps to a row of the backward pass.
+int backward_warps(int64_t h) {
+    const int64_t spans = (h + kSpan - 1) / kSpan;
+    return spans <= 1 ? 1 : spans <= 2 ? 2 : spans <= 4 ? 4 : spans <= 16 ? 8 : 16;
+}
+// Chunks of a worker's rows: CTAs for about 32 warps on each SM, of eight rows at least (16 where a warp takes a row).
 uint32_t backward_chunks(const Shape& z) {
     int device = 0, sms = 148;
     if (cudaGetDevice(&device) == cudaSuccess) cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
     cudaGetLastError();
-    const int64_t per_row_warp = z.h <= 4 * kSpan ? kRowsOfOneWarp : 1;
-    int64_t c = (2 * (int64_t)sms + z.n - 1) / z.n;
-    const int64_t most = (z.rows + per_row_warp - 1) / per_row_warp;
+    const int w = backward_warps(z.h), each = w == 1 ? 32 / kRowsOfOneWarp : 32 / w;
+    int64_t c = ((int64_t)sms * each + z.n - 1) / z.n;
+    const int64_t least = w == 1 ? 16 : 8, most = (z.rows + least - 1) / least;
     if (c > most) c = most;
     return (uint32_t)(c < 1 ? 1 : c);
 }
+
+template <int V>
+using Int = std::integral_constant<int, V>;
 
 template <typename F>
 int by_types(int32_t x, int32_t r, F f) {  // r: x's type or fp32
@@ -448,25 +556,32 @@ template <typename TX, typename TR, bool ADD>
 int backward(const NormArgs& a, int n, bool vec, cudaStream_t stream) {
     const int spans = (a.h + kSpan - 1) / kSpan;
     cudaError_t e = cudaSuccess;
-    auto go = [&](auto kernel, int W) {
-        e = launch_plain(kernel, dim3((uint32_t)n * a.chunks), dim3(W == 1 ? 32 * kRowsOfOneWarp : 32 * W), 0, stream, a);
+    auto go = [&](auto w, auto g, auto v) {
+        constexpr int W = decltype(w)::value, NG = decltype(g)::value;
+        constexpr bool V = decltype(v)::value;
+        auto kernel = norm_backward_kernel<TX, TR, W, NG, V, ADD>;
+        constexpr int shared = backward_shared<TX, TR, W, NG, V, ADD>();
+        if (shared > 32 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, shared);
+        if (e == cudaSuccess) e = launch_plain(kernel, dim3((uint32_t)n * a.chunks), dim3(norm_threads<W>()), shared, stream, a);
     };
     if (a.h > kLongest) {
         if (a.y || a.s) e = launch_plain(norm_backward_long_kernel<TX, TR, ADD>, dim3(a.total), dim3(512), 0, stream, a);
         if (e == cudaSuccess && a.partial)
             e = launch_plain(norm_columns_kernel<TX, TR>, dim3((uint32_t)(a.h + 255) / 256 * (uint32_t)n * a.chunks), dim3(256), 0, stream, a);
     } else if (vec) {
-        if (spans <= 1) go(norm_backward_kernel<TX, TR, 1, 1, true, ADD>, 1);
-        else if (spans <= 2) go(norm_backward_kernel<TX, TR, 1, 2, true, ADD>, 1);
-        else if (spans <= 4) go(norm_backward_kernel<TX, TR, 1, 4, true, ADD>, 1);
-        else if (spans <= 8) go(norm_backward_kernel<TX, TR, 8, 1, true, ADD>, 8);
-        else if (spans <= 16) go(norm_backward_kernel<TX, TR, 16, 1, true, ADD>, 16);
-        else if (spans <= 32) go(norm_backward_kernel<TX, TR, 16, 2, true, ADD>, 16);
-        else go(norm_backward_kernel<TX, TR, 16, 4, true, ADD>, 16);
+        if (spans <= 1) go(Int<1>(), Int<1>(), Int<1>());
+        else if (spans <= 2) go(Int<2>(), Int<1>(), Int<1>());
+        else if (spans <= 4) go(Int<4>(), Int<1>(), Int<1>());
+        else if (spans <= 8) go(Int<8>(), Int<1>(), Int<1>());
+        else if (spans <= 16) go(Int<8>(), Int<2>(), Int<1>());
+        else if (spans <= 32) go(Int<16>(), Int<2>(), Int<1>());
+        else go(Int<16>(), Int<4>(), Int<1>());
     } else {
-        if (spans <= 4) go(norm_backward_kernel<TX, TR, 1, 4, false, ADD>, 1);
-        else if (spans <= 16) go(norm_backward_kernel<TX, TR, 16, 1, false, ADD>, 16);
-        else go(norm_backward_kernel<TX, TR, 16, 4, false, ADD>, 16);
+        if (spans <= 1) go(Int<1>(), Int<1>(), Int<0>());
+        else if (spans <= 2) go(Int<2>(), Int<1>(), Int<0>());
+        else if (spans <= 4) go(Int<4>(), Int<1>(), Int<0>());
+        else if (spans <= 16) go(Int<8>(), Int<2>(), Int<0>());
+        else go(Int<16>(), Int<4>(), Int<0>());
     }
     return launched(e, "norm_backward");
 }
@@ -493,11 +608,13 @@ int compams_dropout(void* y, const void* x, int32_t type, int32_t n, int64_t row
     if (!x || !y || !in.element_aligned() || !out.element_aligned()) return COMPAMS_ERR_INVALID_ARG;
     const bool vec = h % 8 == 0 && in.aligned() && out.aligned();
     const uint32_t spans = (uint32_t)((h + kSpan - 1) / kSpan), total = (uint32_t)(n * rows);
-    const uint64_t ctas = ((uint64_t)total * spans + 7) / 8;
+    const uint64_t all = (uint64_t)total * spans, per = 8 * kDropSpans, ctas = (all + per - 1) / per;
     if (ctas > 0x7fffffffu) return COMPAMS_ERR_TOO_LARGE;
+    const bool wide = all > 0xffffffffu - per;
     return by_types(type, type, [&](auto t, auto) {
         using T = decltype(t);
-        auto kernel = vec ? dropout_kernel<T, true> : dropout_kernel<T, false>;
+        auto kernel = vec ? (wide ? dropout_kernel<T, true, uint64_t> : dropout_kernel<T, true, uint32_t>)
+                          : (wide ? dropout_kernel<T, false, uint64_t> : dropout_kernel<T, false, uint32_t>);
         return launched(launch_plain(kernel, dim3((uint32_t)ctas), dim3(256), 0, (cudaStream_t)cuda_stream, (const T*)x, (T*)y, worker_stride,
                                      row_stride, (uint32_t)rows, total, (int32_t)h, spans, d),
                         "dropout");

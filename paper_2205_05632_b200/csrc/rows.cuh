@@ -74,6 +74,18 @@ template <> __device__ __forceinline__ void store8<float>(float* p, const float 
     reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
 }
 
+// ---- asynchronous copies -----------------------------------------------------------------------------------------------------
+
+// Asynchronous copies of 16 bytes into shared memory; zeros where `there` is false (an address in bounds all the same).
+__device__ __forceinline__ void copy16(void* shared, const void* global, bool there = true) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(shared)), "l"(global),
+                 "r"(there ? 16 : 0)
+                 : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
 // ---- spans -----------------------------------------------------------------------------------------------------------------
 
 // The column of a lane's value k in the span that starts at column c0.
