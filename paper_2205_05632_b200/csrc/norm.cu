@@ -11,6 +11,7 @@
 // registers), weights, biases and their gradients are fp32 as the optimizer keeps them.
 #include <string.h>
 
+#include <atomic>
 #include <type_traits>
 
 #include "context.h"
@@ -61,68 +62,169 @@ constexpr int kRowsOfOneWarp = 8;  // rows of a CTA whose warps take a row each
 template <int W>
 __host__ __device__ constexpr int norm_threads() { return W == 1 ? 32 * kRowsOfOneWarp : 32 * W; }
 
+// CTAs that the registers of an SM have to hold, so that their barriers fall at different times: 24 warps' (16 where the backward
+// pass with its third input would not fit 80 registers a thread, and where rows are read element by element).
+template <int W, int NG, bool VEC, bool MORE>
+__host__ __device__ constexpr int norm_ctas() {
+    return W == 16 ? 1 : (VEC && !(MORE && NG > 1) ? 24 : 16) / (W == 1 ? kRowsOfOneWarp : W);
+}
+
+// ---- a CTA's rows ----------------------------------------------------------------------------------------------------------
+
+// A CTA goes through the rows of one chunk of one worker, W warps to a row, NG spans to a warp, and keeps in registers what all rows share.
+// Where rows are aligned (VEC) every lane copies what it will need of the next rows into places of shared memory that it
+// alone reads, kStages - 1 rows ahead, so that the sums that a row waits for (one barrier) do not stop the loads. Place:
+// [stage][slot][thread], 16 bytes each; SLOTS: of a lane in a stage. Three stages where an SM has the room, or two; none for
+// the longest rows of fp32, which are read where they are used.
+template <int W, int SLOTS, bool VEC>
+__host__ __device__ constexpr int row_stages() {
+    const int bytes = SLOTS * 16 * norm_threads<W>();
+    return !VEC || 2 * bytes > 200 * 1024 ? 0 : 3 * bytes > 200 * 1024 ? 2 : 3;
+}
+template <int W, int SLOTS, bool VEC>
+__host__ __device__ constexpr int row_shared() { return row_stages<W, SLOTS, VEC>() * SLOTS * 16 * norm_threads<W>(); }
+template <typename T>
+__host__ __device__ constexpr int raw_slots() { return (int)sizeof(Raw8<T>) / 16; }
+
+template <int W, int SLOTS>
+__device__ __forceinline__ uint4* row_place(char* smem, int stage, int slot) {
+    return reinterpret_cast<uint4*>(smem) + (stage * SLOTS + slot) * norm_threads<W>() + threadIdx.x;
+}
+template <typename T, int W, int SLOTS>
+__device__ __forceinline__ void row_copy(char* smem, int stage, int slot, const T* from) {
+#pragma unroll
+    for (int k = 0; k < raw_slots<T>(); ++k) copy16(row_place<W, SLOTS>(smem, stage, slot + k), reinterpret_cast<const char*>(from) + 16 * k);
+}
+// A lane's values of the span from column c0 on, `beyond` in the columns from h on.
+template <typename T, int W, int SLOTS, bool VEC, bool RING>
+__device__ __forceinline__ void row_take(char* smem, int stage, int slot, const T* row, int c0, int h, int lane, float beyond, float (&to)[8]) {
+    if constexpr (RING) {
+        if (c0 + lane * 8 < h) {
+            Raw8<T> r;
+            uint4 u[raw_slots<T>()];
+#pragma unroll
+            for (int k = 0; k < raw_slots<T>(); ++k) u[k] = *row_place<W, SLOTS>(smem, stage, slot + k);
+            memcpy(&r, u, sizeof(r));
+            raw_floats<T>(r, to);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) to[k] = beyond;
+        }
+    } else {
+        span_load<T, VEC>(row, c0, h, lane, to, beyond);
+    }
+}
+
 // ---- forward ---------------------------------------------------------------------------------------------------------------
 
-// W warps to a row, NG spans to a warp; the row lies in registers between the sums.
+template <typename TX, typename TR, int NG, bool ADD>
+__host__ __device__ constexpr int forward_slots() { return NG * (raw_slots<TX>() + (ADD ? raw_slots<TR>() : 0)); }
+
+// Every warp finds the mean and the sum of squares about it of its own columns; the barrier passes these on, and each warp
+// joins them (Chan, Golub, LeVeque 1979: the squares about the common mean are those about the parts' means and n_w (mean_w -
+// mean)^2 more).
 template <typename TX, typename TR, int W, int NG, bool VEC, bool ADD>
-__global__ void __launch_bounds__(norm_threads<W>()) norm_forward_kernel(const __grid_constant__ NormArgs a) {
-    __shared__ float scratch[2][W];
-    const int lane = threadIdx.x & 31, warp = W == 1 ? 0 : (int)(threadIdx.x >> 5);
-    const uint32_t m = W == 1 ? blockIdx.x * kRowsOfOneWarp + (threadIdx.x >> 5) : blockIdx.x;
-    if (m >= a.total) return;  // a whole warp, and only where W is 1
-    const uint32_t i = m / a.rows, j = m - i * a.rows;
-    const TX* x = (const TX*)a.x + (int64_t)i * a.x_ws + (int64_t)j * a.x_rs;
-    float v[NG][8];
-#pragma unroll
-    for (int q = 0; q < NG; ++q) span_load<TX, VEC>(x, (q * W + warp) * kSpan, a.h, lane, v[q]);
-    if (ADD) {
-        const TR* r = (const TR*)a.residual + (int64_t)i * a.r_ws + (int64_t)j * a.r_rs;
-        TR* s = (TR*)a.s + (int64_t)m * a.h;
-        const uint32_t call = drop_call(a.drop);
-#pragma unroll
-        for (int q = 0; q < NG; ++q) {
-            const int c0 = (q * W + warp) * kSpan;
-            if (c0 >= a.h) break;
-            float add[8];
-            span_load<TR, VEC>(r, c0, a.h, lane, add);
-            if (a.drop.on) span_drop<VEC>(a.drop, c0, j, a.drop.worker + i, call, lane, v[q]);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) v[q][k] = to_float(from_float<TR>(v[q][k] + add[k]));
-            span_store<TR, VEC>(s, c0, a.h, lane, v[q]);
-        }
-    }
-    float sum = 0.0f;
-#pragma unroll
-    for (int q = 0; q < NG; ++q)
-#pragma unroll
-        for (int k = 0; k < 8; ++k) sum += v[q][k];  // 0 beyond h
-    const float mean = row_sum<W>(sum, scratch[0], warp) / (float)a.h;
-    float square = 0.0f;
-#pragma unroll
-    for (int q = 0; q < NG; ++q)
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const bool in = span_column<VEC>((q * W + warp) * kSpan, lane, k) < a.h;
-            v[q][k] -= mean;
-            square = fmaf(in ? v[q][k] : 0.0f, v[q][k], square);
-        }
-    const float rstd = 1.0f / sqrtf(row_sum<W>(square, scratch[1], warp) / (float)a.h + a.eps);
-    if (a.stats && warp == 0 && lane == 0) a.stats[m] = make_float2(mean, rstd);
+__global__ void __launch_bounds__(norm_threads<W>(), norm_ctas<W, NG, VEC, false>()) norm_forward_kernel(const __grid_constant__ NormArgs a) {
+    extern __shared__ __align__(16) char smem[];
+    constexpr int kRows = W == 1 ? kRowsOfOneWarp : 1, SLOTS = forward_slots<TX, TR, NG, ADD>(), kStages = row_stages<W, SLOTS, VEC>();
+    constexpr bool RING = kStages > 0, kHold = NG <= 2;
+    __shared__ float2 scratch[2][W];
+    const int lane = threadIdx.x & 31, warp = W == 1 ? 0 : (int)(threadIdx.x >> 5), slot = W == 1 ? (int)(threadIdx.x >> 5) : 0;
+    const uint32_t i = blockIdx.x / a.chunks, chunk = blockIdx.x - i * a.chunks;
+    const uint32_t j0 = (uint32_t)((uint64_t)a.rows * chunk / a.chunks), j1 = (uint32_t)((uint64_t)a.rows * (chunk + 1) / a.chunks);
+    const uint32_t call = drop_call(a.drop);
+    const TX* x = (const TX*)a.x + (int64_t)i * a.x_ws;
+    const TR* residual = ADD ? (const TR*)a.residual + (int64_t)i * a.r_ws : nullptr;
     const float* weight = a.weight ? a.weight + (int64_t)i * a.weight_ws : nullptr;
     const float* bias = a.bias ? a.bias + (int64_t)i * a.bias_ws : nullptr;
-    TX* y = (TX*)a.y + (int64_t)m * a.h;
-#pragma unroll
-    for (int q = 0; q < NG; ++q) {
+    auto affine = [&](int q, float (&w)[8], float (&b)[8]) {
         const int c0 = (q * W + warp) * kSpan;
-        if (c0 >= a.h) break;
-        float w[8], b[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) b[k] = 0.0f, w[k] = 1.0f;
         if (weight) span_load<float, VEC>(weight, c0, a.h, lane, w);
         if (bias) span_load<float, VEC>(bias, c0, a.h, lane, b);
+    };
+    auto fetch = [&](uint32_t j, int stage) {
+        if constexpr (RING) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[q][k] = fmaf(v[q][k] * rstd, w[k], b[k]);
-        span_store<TX, VEC>(y, c0, a.h, lane, v[q]);
+            for (int q = 0; q < NG; ++q) {
+                const int c = (q * W + warp) * kSpan + lane * 8;
+                if (j < j1 && c < a.h) {
+                    row_copy<TX, W, SLOTS>(smem, stage, q * raw_slots<TX>(), x + (int64_t)j * a.x_rs + c);
+                    if (ADD) row_copy<TR, W, SLOTS>(smem, stage, NG * raw_slots<TX>() + q * raw_slots<TR>(), residual + (int64_t)j * a.r_rs + c);
+                }
+            }
+            copies_commit();
+        }
+    };
+    for (int k = 0; k + 1 < kStages; ++k) fetch(j0 + slot + k * kRows, k);
+    float w[kHold ? NG : 1][8], b[kHold ? NG : 1][8];
+    if (kHold)
+#pragma unroll
+        for (int q = 0; q < NG; ++q) affine(q, w[kHold ? q : 0], b[kHold ? q : 0]);
+    // columns of this warp's own, and of warp k
+    auto columns = [&](int k) {
+        int c = 0;
+#pragma unroll
+        for (int q = 0; q < NG; ++q) c += min(max(a.h - (q * W + k) * kSpan, 0), kSpan);
+        return (float)c;
+    };
+    const float own = columns(warp), per_own = own > 0.0f ? 1.0f / own : 0.0f, per_row = 1.0f / (float)a.h;
+    const float lane_columns = lane < W ? columns(lane) : 0.0f;
+    int turn = 0, stage = 0;
+    for (uint32_t j = j0 + slot; j < j1; j += kRows, turn ^= 1) {
+        const uint32_t m = i * a.rows + j;
+        if constexpr (RING) {
+            fetch(j + (kStages - 1) * kRows, stage == 0 ? kStages - 1 : stage - 1);
+            copies_wait<kStages - 1>();  // a lane's own
+        }
+        float v[NG][8], sum = 0.0f;
+#pragma unroll
+        for (int q = 0; q < NG; ++q) {
+            const int c0 = (q * W + warp) * kSpan;
+            row_take<TX, W, SLOTS, VEC, RING>(smem, stage, q * raw_slots<TX>(), x + (int64_t)j * a.x_rs, c0, a.h, lane, 0.0f, v[q]);
+            if (ADD && c0 < a.h) {
+                float add[8];
+                row_take<TR, W, SLOTS, VEC, RING>(smem, stage, NG * raw_slots<TX>() + q * raw_slots<TR>(), residual + (int64_t)j * a.r_rs, c0,
+                                                  a.h, lane, 0.0f, add);
+                if (a.drop.on) span_drop<VEC>(a.drop, c0, j, a.drop.worker + i, call, lane, v[q]);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[q][k] = to_float(from_float<TR>(v[q][k] + add[k]));
+                span_store<TR, VEC>((TR*)a.s + (int64_t)m * a.h, c0, a.h, lane, v[q]);
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sum += v[q][k];  // 0 beyond h
+        }
+        stage = stage + 1 == kStages ? 0 : stage + 1;
+        float mean = warp_sum(sum) * per_own, square = 0.0f;
+#pragma unroll
+        for (int q = 0; q < NG; ++q)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float d = span_column<VEC>((q * W + warp) * kSpan, lane, k) < a.h ? v[q][k] - mean : 0.0f;
+                square = fmaf(d, d, square);
+            }
+        square = warp_sum(square);
+        if (W > 1) {
+            if (lane == 0) scratch[turn][warp] = make_float2(mean, square);
+            __syncthreads();  // the next row writes the other half, and the one after it only behind the next row's barrier
+            // lane k joins warp k's; the sums are the same tree in every warp
+            const float2 part = lane < W ? scratch[turn][lane] : make_float2(0.0f, 0.0f);
+            mean = warp_sum(lane_columns * part.x) * per_row;
+            const float d = part.x - mean;
+            square = warp_sum(fmaf(lane_columns * d, d, part.y));
+        }
+        const float rstd = 1.0f / sqrtf(square * per_row + a.eps);
+        if (a.stats && warp == 0 && lane == 0) a.stats[m] = make_float2(mean, rstd);
+#pragma unroll
+        for (int q = 0; q < NG; ++q) {
+            const int c0 = (q * W + warp) * kSpan;
+            if (c0 >= a.h) break;
+            if (!kHold) affine(q, w[0], b[0]);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[q][k] = fmaf((v[q][k] - mean) * rstd, w[kHold ? q : 0][k], b[kHold ? q : 0][k]);
+            span_store<TX, VEC>((TX*)a.y + (int64_t)m * a.h, c0, a.h, lane, v[q]);
+        }
     }
 }
 
@@ -171,33 +273,18 @@ __global__ void __launch_bounds__(512) norm_forward_long_kernel(const __grid_con
 
 // ---- backward --------------------------------------------------------------------------------------------------------------
 
-// A CTA goes through the rows of one chunk of one worker and keeps the sums of dy xhat and dy of its columns in registers, the weight too.
-// W warps to a row, NG spans to a warp. Where rows are aligned (VEC) every lane copies what it will need of the next rows into places of
-// shared memory that it alone reads, two rows ahead, so that the two sums that a row waits for (one barrier) do not
-// stop the loads: [stage][operand][span][16 bytes][thread]. With several spans to a warp the values are taken from there a second time
-// behind the barrier instead of being held, and with four the weight is read again for each row: registers are what bounds the CTAs
-// of an SM.
-template <typename TX, typename TR, int W, int NG, bool ADD>
-__host__ __device__ constexpr int backward_ring() {  // 16-byte slots of a lane in a stage
-    return NG * ((int)sizeof(Raw8<TX>) + (ADD ? 2 : 1) * (int)sizeof(Raw8<TR>)) / 16;
-}
-// Stages of it: three where an SM has the room, or two; none for the longest rows of fp32, which are read where they are used.
-template <typename TX, typename TR, int W, int NG, bool VEC, bool ADD>
-__host__ __device__ constexpr int backward_stages() {
-    const int bytes = backward_ring<TX, TR, W, NG, ADD>() * 16 * norm_threads<W>();
-    return !VEC || 2 * bytes > 200 * 1024 ? 0 : 3 * bytes > 200 * 1024 ? 2 : 3;
-}
-template <typename TX, typename TR, int W, int NG, bool VEC, bool ADD>
-__host__ __device__ constexpr int backward_shared() {
-    return backward_stages<TX, TR, W, NG, VEC, ADD>() * backward_ring<TX, TR, W, NG, ADD>() * 16 * norm_threads<W>();
-}
+template <typename TX, typename TR, int NG, bool ADD>
+__host__ __device__ constexpr int backward_slots() { return NG * (raw_slots<TX>() + (ADD ? 2 : 1) * raw_slots<TR>()); }
 
+// The sums of dy xhat and dy of a chunk's rows stay in registers, the weight too. With several spans to a warp the values are taken
+// a second time behind the barrier instead of being held, and with four the weight is read again for each row: registers are what
+// bounds the CTAs of an SM.
 template <typename TX, typename TR, int W, int NG, bool VEC, bool ADD>
-__global__ void __launch_bounds__(norm_threads<W>()) norm_backward_kernel(const __grid_constant__ NormArgs a) {
+__global__ void __launch_bounds__(norm_threads<W>(), norm_ctas<W, NG, VEC, ADD>()) norm_backward_kernel(const __grid_constant__ NormArgs a) {
     extern __shared__ __align__(16) char smem[];
-    constexpr int kSlots = W == 1 ? kRowsOfOneWarp : 1, kThreadsHere = norm_threads<W>();
-    constexpr int SX = (int)sizeof(Raw8<TX>) / 16, SR = (int)sizeof(Raw8<TR>) / 16, RING = backward_ring<TX, TR, W, NG, ADD>();
-    constexpr int kStages = backward_stages<TX, TR, W, NG, VEC, ADD>();
+    constexpr int kSlots = W == 1 ? kRowsOfOneWarp : 1, SX = raw_slots<TX>(), SR = raw_slots<TR>();
+    constexpr int SLOTS = backward_slots<TX, TR, NG, ADD>(), kStages = row_stages<W, SLOTS, VEC>();
+    constexpr bool RING = kStages > 0;
     __shared__ float scratch[2][2][W];
     __shared__ float joined[W == 1 ? NG * kSpan : 1];
     const int lane = threadIdx.x & 31, warp = W == 1 ? 0 : (int)(threadIdx.x >> 5), slot = W == 1 ? (int)(threadIdx.x >> 5) : 0;
@@ -220,47 +307,18 @@ __global__ void __launch_bounds__(norm_threads<W>()) norm_backward_kernel(const 
         for (int k = 0; k < 8; ++k) dw[q][k] = db[q][k] = 0.0f;
         if (kHoldWeight) weight(q, held[kHoldWeight ? q : 0]);
     }
-    auto place = [&](int stage, int at) { return reinterpret_cast<uint4*>(smem) + (stage * RING + at) * kThreadsHere + threadIdx.x; };
     auto fetch = [&](uint32_t j, int stage) {
-        if constexpr (kStages > 0) {
+        if constexpr (RING) {
 #pragma unroll
             for (int q = 0; q < NG; ++q) {
                 const int c = (q * W + warp) * kSpan + lane * 8;
                 if (j < j1 && c < a.h) {
-                    const char* gx = reinterpret_cast<const char*>(dy + (int64_t)j * a.x_rs + c);
-                    const char* gv = reinterpret_cast<const char*>(v + (int64_t)j * a.v_rs + c);
-#pragma unroll
-                    for (int k = 0; k < SX; ++k) copy16(place(stage, q * SX + k), gx + 16 * k);
-#pragma unroll
-                    for (int k = 0; k < SR; ++k) copy16(place(stage, NG * SX + q * SR + k), gv + 16 * k);
-                    if (ADD && more) {
-                        const char* gr = reinterpret_cast<const char*>(more + (int64_t)j * a.r_rs + c);
-#pragma unroll
-                        for (int k = 0; k < SR; ++k) copy16(place(stage, NG * (SX + SR) + q * SR + k), gr + 16 * k);
-                    }
+                    row_copy<TX, W, SLOTS>(smem, stage, q * SX, dy + (int64_t)j * a.x_rs + c);
+                    row_copy<TR, W, SLOTS>(smem, stage, NG * SX + q * SR, v + (int64_t)j * a.v_rs + c);
+                    if (ADD && more) row_copy<TR, W, SLOTS>(smem, stage, NG * (SX + SR) + q * SR, more + (int64_t)j * a.r_rs + c);
                 }
             }
             copies_commit();
-        }
-    };
-    // a lane's values of span q, `beyond` in the columns from h on
-    auto take = [&](auto type, const auto* row, int stage, int at, int q, float beyond, float (&to)[8]) {
-        using T = decltype(type);
-        const int c0 = (q * W + warp) * kSpan;
-        if constexpr (kStages > 0) {
-            if (c0 + lane * 8 < a.h) {
-                Raw8<T> r;
-                uint4 u[sizeof(r) / 16];
-#pragma unroll
-                for (int k = 0; k < (int)sizeof(r) / 16; ++k) u[k] = *place(stage, at + q * (int)sizeof(r) / 16 + k);
-                memcpy(&r, u, sizeof(r));
-                raw_floats<T>(r, to);
-            } else {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) to[k] = beyond;
-            }
-        } else {
-            span_load<T, VEC>(row, c0, a.h, lane, to, beyond);
         }
     };
     for (int k = 0; k + 1 < kStages; ++k) fetch(j0 + slot + k * kSlots, k);
@@ -270,13 +328,16 @@ __global__ void __launch_bounds__(norm_threads<W>()) norm_backward_kernel(const 
         const uint32_t m = i * a.rows + j;
         const float2 st = next;
         if (j + kSlots < j1) next = a.stats[m + kSlots];
-        if constexpr (kStages > 0) fetch(j + (kStages - 1) * kSlots, stage == 0 ? kStages - 1 : stage - 1);
-        if constexpr (kStages > 0) copies_wait<kStages - 1>();  // a lane's own
+        if constexpr (RING) {
+            fetch(j + (kStages - 1) * kSlots, stage == 0 ? kStages - 1 : stage - 1);
+            copies_wait<kStages - 1>();  // a lane's own
+        }
         float g[8], xhat[8], c1 = 0.0f, c2 = 0.0f;
         // dy w and xhat of span q; the first time its share of the sums
         auto values = [&](int q, bool first) {
-            take(TX(), dy + (int64_t)j * a.x_rs, stage, 0, q, 0.0f, g);
-            take(TR(), v + (int64_t)j * a.v_rs, stage, NG * SX, q, st.x, xhat);
+            const int c0 = (q * W + warp) * kSpan;
+            row_take<TX, W, SLOTS, VEC, RING>(smem, stage, q * SX, dy + (int64_t)j * a.x_rs, c0, a.h, lane, 0.0f, g);
+            row_take<TR, W, SLOTS, VEC, RING>(smem, stage, NG * SX + q * SR, v + (int64_t)j * a.v_rs, c0, a.h, lane, st.x, xhat);
             float w[8];
             if (!kHoldWeight) weight(q, w);
 #pragma unroll
@@ -321,7 +382,8 @@ __global__ void __launch_bounds__(norm_threads<W>()) norm_backward_kernel(const 
                 float add[8];
 #pragma unroll
                 for (int k = 0; k < 8; ++k) add[k] = 0.0f;
-                if (ADD && more) take(TR(), more + (int64_t)j * a.r_rs, stage, NG * (SX + SR), q, 0.0f, add);
+                if (ADD && more)
+                    row_take<TR, W, SLOTS, VEC, RING>(smem, stage, NG * (SX + SR) + q * SR, more + (int64_t)j * a.r_rs, c0, a.h, lane, 0.0f, add);
 #pragma unroll
                 for (int k = 0; k < 8; ++k) g[k] = fmaf(st.y, g[k] - c1 - xhat[k] * c2, add[k]);
                 if (ADD && a.s) span_store<TR, VEC>((TR*)a.s + (int64_t)m * a.h, c0, a.h, lane, g);
@@ -447,39 +509,90 @@ __global__ void __launch_bounds__(256) norm_join_kernel(const float* __restrict_
 
 // ---- dropout ---------------------------------------------------------------------------------------------------------------
 
-// A warp takes four spans, one after the other in the order of memory; their loads stand before the first mask. U: a number of spans.
+// A CTA takes a stretch of spans in the order of memory, a warp four of 32 at a time; the next four are on their way while these are done.
+// U: a number of spans. (32 spans) further is `span` spans, `row` rows and `worker` workers further.
 constexpr int kDropSpans = 4;
-template <typename T, bool VEC, typename U>
-__global__ void __launch_bounds__(256) dropout_kernel(const T* __restrict__ x, T* __restrict__ y, int64_t ws, int64_t rs, uint32_t rows,
-                                                      uint32_t total, int32_t h, uint32_t spans, const __grid_constant__ Drop d) {
-    const int lane = threadIdx.x & 31;
-    const U at = ((U)blockIdx.x * 8 + (threadIdx.x >> 5)) * kDropSpans;
-    uint32_t m = (uint32_t)(at / spans), span = (uint32_t)(at - (U)m * spans), i = m / rows, j = m - i * rows;
-    const uint32_t call = drop_call(d);
-    float v[kDropSpans][8];
-    uint32_t worker[kDropSpans], row[kDropSpans];
-    int c0[kDropSpans];
-    T* to[kDropSpans];
+struct DropoutArgs {
+    const void* x;
+    void* y;
+    int64_t ws, rs;
+    uint64_t steps, ctas;  // of 32 spans
+    uint32_t rows, total;
+    int32_t h;
+    uint32_t spans;                       // of a row
+    uint32_t step_span, step_row, step_j, step_worker;  // step_row rows = step_worker workers and step_j rows
+    Drop drop;
+};
+template <typename T, bool VEC>  // a lane's values of a span, as they lie in memory
+struct Held {
+    Raw8<T> r;
+    __device__ __forceinline__ void load(const T* row, int c0, int h, int lane) {
+        r = {};
+        if (c0 + lane * 8 < h) r = raw_load<T>(row + c0 + lane * 8);
+    }
+    __device__ __forceinline__ void floats(float (&v)[8]) const { raw_floats<T>(r, v); }
+};
+template <typename T>
+struct Held<T, false> {
+    float x[8];
+    __device__ __forceinline__ void load(const T* row, int c0, int h, int lane) { span_load<T, false>(row, c0, h, lane, x); }
+    __device__ __forceinline__ void floats(float (&v)[8]) const {
 #pragma unroll
-    for (int k = 0; k < kDropSpans; ++k) {
-        c0[k] = m < total ? (int)span * kSpan : h;
-        worker[k] = i;
-        row[k] = j;
-        to[k] = y + (int64_t)m * h;
-        span_load<T, VEC>(x + (int64_t)i * ws + (int64_t)j * rs, c0[k], h, lane, v[k]);
-        if (++span == spans) {
+        for (int k = 0; k < 8; ++k) v[k] = x[k];
+    }
+};
+template <typename T, bool VEC, typename U>
+__global__ void __launch_bounds__(256) dropout_kernel(const __grid_constant__ DropoutArgs a) {
+    const int lane = threadIdx.x & 31;
+    const U s0 = (U)(a.steps * blockIdx.x / a.ctas), s1 = (U)(a.steps * (blockIdx.x + 1) / a.ctas);
+    const U at = s0 * 32 + (threadIdx.x >> 5) * kDropSpans;
+    uint32_t m = (uint32_t)(at / a.spans), span = (uint32_t)(at - (U)m * a.spans), i = m / a.rows, j = m - i * a.rows;
+    const uint32_t call = drop_call(a.drop);
+    // the place of span k of the four, which are neighbours
+    auto place = [&](uint32_t& m, uint32_t& span, uint32_t& i, uint32_t& j) {
+        if (++span == a.spans) {
             span = 0;
             ++m;
-            if (++j == rows) {
+            if (++j == a.rows) {
                 j = 0;
                 ++i;
             }
         }
-    }
+    };
+    Held<T, VEC> next[kDropSpans];
+    auto load = [&](uint32_t m, uint32_t span, uint32_t i, uint32_t j) {
 #pragma unroll
-    for (int k = 0; k < kDropSpans; ++k) {
-        if (d.on) span_drop<VEC>(d, c0[k], row[k], d.worker + worker[k], call, lane, v[k]);
-        span_store<T, VEC>(to[k], c0[k], h, lane, v[k]);
+        for (int k = 0; k < kDropSpans; ++k) {
+            next[k].load((const T*)a.x + (int64_t)i * a.ws + (int64_t)j * a.rs, m < a.total ? (int)span * kSpan : a.h, a.h, lane);
+            place(m, span, i, j);
+        }
+    };
+    load(m, span, i, j);
+    for (U s = s0; s < s1; ++s) {
+        Held<T, VEC> now[kDropSpans];
+#pragma unroll
+        for (int k = 0; k < kDropSpans; ++k) now[k] = next[k];
+        uint32_t tm = m, tspan = span, ti = i, tj = j;
+        m += a.step_row, span += a.step_span, i += a.step_worker, j += a.step_j;
+        if (span >= a.spans) {
+            span -= a.spans;
+            ++m;
+            ++j;
+        }
+        if (j >= a.rows) {
+            j -= a.rows;
+            ++i;
+        }
+        if (s + 1 < s1) load(m, span, i, j);
+#pragma unroll
+        for (int k = 0; k < kDropSpans; ++k) {
+            const int c0 = tm < a.total ? (int)tspan * kSpan : a.h;
+            float v[8];
+            now[k].floats(v);
+            if (a.drop.on) span_drop<VEC>(a.drop, c0, tj, a.drop.worker + ti, call, lane, v);
+            span_store<T, VEC>((T*)a.y + (int64_t)tm * a.h, c0, a.h, lane, v);
+            place(tm, tspan, ti, tj);
+        }
     }
 }
 
@@ -495,18 +608,34 @@ struct Shape {
     }
 };
 
-// Warps to a row of the backward pass.
-int backward_warps(int64_t h) {
-    const int64_t spans = (h + kSpan - 1) / kSpan;
-    return spans <= 1 ? 1 : spans <= 2 ? 2 : spans <= 4 ? 4 : spans <= 16 ? 8 : 16;
-}
-// Chunks of a worker's rows: CTAs for about 32 warps on each SM, of eight rows at least (16 where a warp takes a row).
-uint32_t backward_chunks(const Shape& z) {
+int multiprocessors() {
     int device = 0, sms = 148;
     if (cudaGetDevice(&device) == cudaSuccess) cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
     cudaGetLastError();
-    const int w = backward_warps(z.h), each = w == 1 ? 32 / kRowsOfOneWarp : 32 / w;
-    int64_t c = ((int64_t)sms * each + z.n - 1) / z.n;
+    return sms;
+}
+// CTAs of a kernel that an SM holds at once. Asked once for every kernel and device.
+template <auto kernel>
+cudaError_t resident(int threads, int shared, int* count) {
+    static std::atomic<int> known[64];
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    *count = device < 64 ? known[device].load(std::memory_order_relaxed) : 0;
+    if (*count) return cudaSuccess;
+    if (shared > 32 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, shared);
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(count, kernel, threads, shared);
+    if (e == cudaSuccess && *count < 1) e = cudaErrorInvalidConfiguration;
+    if (e == cudaSuccess && device < 64) known[device].store(*count, std::memory_order_relaxed);
+    return e;
+}
+
+// Chunks of a worker's rows: at most as many as give every SM 32 warps, of eight rows at least (16 where a warp takes a row); the
+// partial sums of so many fit the workspace. Fewer where an SM holds fewer CTAs: then all run at once.
+uint32_t most_chunks(const Shape& z) {
+    const int64_t spans = (z.h + kSpan - 1) / kSpan;
+    const int w = spans <= 1 ? 1 : spans <= 2 ? 2 : spans <= 4 ? 4 : spans <= 16 ? 8 : 16, each = w == 1 ? 32 / kRowsOfOneWarp : 32 / w;
+    int64_t c = ((int64_t)multiprocessors() * each + z.n - 1) / z.n;
     const int64_t least = w == 1 ? 16 : 8, most = (z.rows + least - 1) / least;
     if (c > most) c = most;
     return (uint32_t)(c < 1 ? 1 : c);
@@ -524,45 +653,64 @@ int by_types(int32_t x, int32_t r, F f) {  // r: x's type or fp32
 
 int launched(cudaError_t e, const char* what) { return e == cudaSuccess ? COMPAMS_OK : cuda_fail(e, what); }
 
-template <typename TX, typename TR, bool ADD>
-int forward(const NormArgs& a, bool vec, cudaStream_t stream) {
-    const int spans = (a.h + kSpan - 1) / kSpan;
-    cudaError_t e = cudaSuccess;
-    auto go = [&](auto kernel, int W) {
-        const uint32_t per = W == 1 ? kRowsOfOneWarp : 1;
-        e = launch_plain(kernel, dim3((a.total + per - 1) / per), dim3(W == 1 ? 32 * kRowsOfOneWarp : 32 * W), 0, stream, a);
-    };
-    // a few rows leave SMs idle: then as many warps as a row has spans, the shortest way through one row
-    const bool few = a.total <= 2 * 148;
-    if (a.h > kLongest) {
-        e = launch_plain(norm_forward_long_kernel<TX, TR, ADD>, dim3(a.total), dim3(512), 0, stream, a);
-    } else if (vec) {
-        if (few && spans > 1 && spans <= 16) go(norm_forward_kernel<TX, TR, 16, 1, true, ADD>, 16);
-        else if (spans <= 1) go(norm_forward_kernel<TX, TR, 1, 1, true, ADD>, 1);
-        else if (spans <= 2) go(norm_forward_kernel<TX, TR, 1, 2, true, ADD>, 1);
-        else if (spans <= 4) go(norm_forward_kernel<TX, TR, 1, 4, true, ADD>, 1);
-        else if (spans <= 16) go(norm_forward_kernel<TX, TR, 4, 4, true, ADD>, 4);
-        else if (spans <= 32) go(norm_forward_kernel<TX, TR, 8, 4, true, ADD>, 8);
-        else go(norm_forward_kernel<TX, TR, 16, 4, true, ADD>, 16);
-    } else {
-        if (spans <= 4) go(norm_forward_kernel<TX, TR, 1, 4, false, ADD>, 1);
-        else if (spans <= 16) go(norm_forward_kernel<TX, TR, 4, 4, false, ADD>, 4);
-        else go(norm_forward_kernel<TX, TR, 16, 4, false, ADD>, 16);
-    }
-    return launched(e, "norm_forward");
+// One wave of CTAs: as many chunks as run at once, no more than `most`, each of one row at least.
+uint32_t chunks_at_once(int count, int n, int64_t rows, int64_t per, int64_t most) {
+    int64_t c = (int64_t)multiprocessors() * count / n;
+    if (c > most) c = most;
+    if (c > (rows + per - 1) / per) c = (rows + per - 1) / per;
+    return (uint32_t)(c < 1 ? 1 : c);
 }
 
 template <typename TX, typename TR, bool ADD>
-int backward(const NormArgs& a, int n, bool vec, cudaStream_t stream) {
+int forward(NormArgs a, int n, bool vec, cudaStream_t stream) {
     const int spans = (a.h + kSpan - 1) / kSpan;
     cudaError_t e = cudaSuccess;
     auto go = [&](auto w, auto g, auto v) {
         constexpr int W = decltype(w)::value, NG = decltype(g)::value;
         constexpr bool V = decltype(v)::value;
+        auto kernel = norm_forward_kernel<TX, TR, W, NG, V, ADD>;
+        constexpr int shared = row_shared<W, forward_slots<TX, TR, NG, ADD>(), V>();
+        int count = 0;
+        e = resident<norm_forward_kernel<TX, TR, W, NG, V, ADD>>(norm_threads<W>(), shared, &count);
+        if (e != cudaSuccess) return;
+        a.chunks = chunks_at_once(count, n, a.rows, W == 1 ? kRowsOfOneWarp : 1, 0x7fffffff / n);
+        e = launch_plain(kernel, dim3((uint32_t)n * a.chunks), dim3(norm_threads<W>()), shared, stream, a);
+    };
+    if (a.h > kLongest) {
+        e = launch_plain(norm_forward_long_kernel<TX, TR, ADD>, dim3(a.total), dim3(512), 0, stream, a);
+    } else if (vec) {
+        if (spans <= 1) go(Int<1>(), Int<1>(), Int<1>());
+        else if (spans <= 2) go(Int<2>(), Int<1>(), Int<1>());
+        else if (spans <= 4) go(Int<4>(), Int<1>(), Int<1>());
+        else if (spans <= 8) go(Int<8>(), Int<1>(), Int<1>());
+        else if (spans <= 16) go(Int<8>(), Int<2>(), Int<1>());
+        else if (spans <= 32) go(Int<16>(), Int<2>(), Int<1>());
+        else go(Int<16>(), Int<4>(), Int<1>());
+    } else {
+        if (spans <= 1) go(Int<1>(), Int<1>(), Int<0>());
+        else if (spans <= 2) go(Int<2>(), Int<1>(), Int<0>());
+        else if (spans <= 4) go(Int<4>(), Int<1>(), Int<0>());
+        else if (spans <= 16) go(Int<8>(), Int<2>(), Int<0>());
+        else go(Int<16>(), Int<4>(), Int<0>());
+    }
+    return launched(e, "norm_forward");
+}
+
+template <typename TX, typename TR, bool ADD>
+int backward(NormArgs& a, int n, bool vec, cudaStream_t stream) {
+    const int spans = (a.h + kSpan - 1) / kSpan;
+    const uint32_t most = a.chunks;
+    cudaError_t e = cudaSuccess;
+    auto go = [&](auto w, auto g, auto v) {
+        constexpr int W = decltype(w)::value, NG = decltype(g)::value;
+        constexpr bool V = decltype(v)::value;
         auto kernel = norm_backward_kernel<TX, TR, W, NG, V, ADD>;
-        constexpr int shared = backward_shared<TX, TR, W, NG, V, ADD>();
-        if (shared > 32 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, shared);
-        if (e == cudaSuccess) e = launch_plain(kernel, dim3((uint32_t)n * a.chunks), dim3(norm_threads<W>()), shared, stream, a);
+        constexpr int shared = row_shared<W, backward_slots<TX, TR, NG, ADD>(), V>();
+        int count = 0;
+        e = resident<norm_backward_kernel<TX, TR, W, NG, V, ADD>>(norm_threads<W>(), shared, &count);
+        if (e != cudaSuccess) return;
+        a.chunks = chunks_at_once(count, n, a.rows, W == 1 ? kRowsOfOneWarp : 1, most);
+        e = launch_plain(kernel, dim3((uint32_t)n * a.chunks), dim3(norm_threads<W>()), shared, stream, a);
     };
     if (a.h > kLongest) {
         if (a.y || a.s) e = launch_plain(norm_backward_long_kernel<TX, TR, ADD>, dim3(a.total), dim3(512), 0, stream, a);
@@ -607,17 +755,27 @@ int compams_dropout(void* y, const void* x, int32_t type, int32_t n, int64_t row
     const Rows in{x, worker_stride, row_stride, type}, out = packed(y, rows, h, type);
     if (!x || !y || !in.element_aligned() || !out.element_aligned()) return COMPAMS_ERR_INVALID_ARG;
     const bool vec = h % 8 == 0 && in.aligned() && out.aligned();
-    const uint32_t spans = (uint32_t)((h + kSpan - 1) / kSpan), total = (uint32_t)(n * rows);
-    const uint64_t all = (uint64_t)total * spans, per = 8 * kDropSpans, ctas = (all + per - 1) / per;
-    if (ctas > 0x7fffffffu) return COMPAMS_ERR_TOO_LARGE;
-    const bool wide = all > 0xffffffffu - per;
+    DropoutArgs a = {};
+    a.x = x; a.y = y; a.ws = worker_stride; a.rs = row_stride; a.rows = (uint32_t)rows; a.total = (uint32_t)(n * rows); a.h = (int32_t)h;
+    a.spans = (uint32_t)((h + kSpan - 1) / kSpan);
+    a.step_row = 32 / a.spans; a.step_span = 32 % a.spans; a.step_worker = a.step_row / a.rows; a.step_j = a.step_row % a.rows;
+    a.drop = d;
+    const uint64_t all = (uint64_t)a.total * a.spans;
+    a.steps = (all + 31) / 32;
     return by_types(type, type, [&](auto t, auto) {
         using T = decltype(t);
-        auto kernel = vec ? (wide ? dropout_kernel<T, true, uint64_t> : dropout_kernel<T, true, uint32_t>)
-                          : (wide ? dropout_kernel<T, false, uint64_t> : dropout_kernel<T, false, uint32_t>);
-        return launched(launch_plain(kernel, dim3((uint32_t)ctas), dim3(256), 0, (cudaStream_t)cuda_stream, (const T*)x, (T*)y, worker_stride,
-                                     row_stride, (uint32_t)rows, total, (int32_t)h, spans, d),
-                        "dropout");
+        auto go = [&](auto v, auto u) {
+            constexpr bool V = decltype(v)::value;
+            using U = decltype(u);
+            int count = 0;
+            cudaError_t e = resident<dropout_kernel<T, V, U>>(256, 0, &count);
+            if (e != cudaSuccess) return cuda_fail(e, "dropout");
+            a.ctas = (uint64_t)multiprocessors() * count;
+            if (a.ctas > a.steps) a.ctas = a.steps;
+            return launched(launch_plain(dropout_kernel<T, V, U>, dim3((uint32_t)a.ctas), dim3(256), 0, (cudaStream_t)cuda_stream, a), "dropout");
+        };
+        const bool wide = all > 0xffffffffu - 64;
+        return vec ? (wide ? go(Int<1>(), uint64_t()) : go(Int<1>(), uint32_t())) : (wide ? go(Int<0>(), uint64_t()) : go(Int<0>(), uint32_t()));
     });
 }
 
@@ -647,15 +805,15 @@ int compams_norm_forward(void* y, void* s, float* stats, const void* x, const vo
     return by_types(type, add ? residual_type : type, [&](auto tx, auto tr) {
         using TX = decltype(tx);
         using TR = decltype(tr);
-        if (add) return forward<TX, TR, true>(a, vec, (cudaStream_t)cuda_stream);
-        return forward<TX, TX, false>(a, vec, (cudaStream_t)cuda_stream);
+        if (add) return forward<TX, TR, true>(a, n, vec, (cudaStream_t)cuda_stream);
+        return forward<TX, TX, false>(a, n, vec, (cudaStream_t)cuda_stream);
     });
 }
 
 int compams_norm_workspace_bytes(size_t* bytes, int32_t n, int64_t rows, int64_t h) {
     const Shape z{n, rows, h};
     if (!bytes || !z.ok()) return COMPAMS_ERR_INVALID_ARG;
-    *bytes = (size_t)n * backward_chunks(z) * 2 * (size_t)h * sizeof(float);
+    *bytes = (size_t)n * most_chunks(z) * 2 * (size_t)h * sizeof(float);
     return COMPAMS_OK;
 }
 
@@ -671,7 +829,7 @@ int compams_norm_backward(void* dx, void* dresidual, float* dweight, float* dbia
     const bool add = added != 0;
     if (add ? v_type != type && v_type != kTypeF32 : v_type != type || ds || dresidual || p != 0.0) return COMPAMS_ERR_INVALID_ARG;
     const bool sums = dweight || dbias;
-    const uint32_t chunks = backward_chunks(z);
+    const uint32_t chunks = most_chunks(z);
     if ((uint64_t)n * chunks * (uint64_t)((h + 255) / 256) > 0x7fffffffu) return COMPAMS_ERR_TOO_LARGE;
     if (sums && (!workspace || workspace_bytes < (size_t)n * chunks * 2 * (size_t)h * sizeof(float) ||
                  (reinterpret_cast<uintptr_t>(workspace) & 15u) || !float_aligned(dweight) || !float_aligned(dbias)))
@@ -702,7 +860,7 @@ int compams_norm_backward(void* dx, void* dresidual, float* dweight, float* dbia
         return backward<TX, TX, false>(a, n, vec, stream);
     });
     if (rc != COMPAMS_OK || !sums) return rc;
-    const uint32_t groups = sum_workers ? 1u : (uint32_t)n, per = sum_workers ? (uint32_t)n * chunks : chunks;
+    const uint32_t groups = sum_workers ? 1u : (uint32_t)n, per = sum_workers ? (uint32_t)n * a.chunks : a.chunks;
     return launched(launch_after(norm_join_kernel, dim3((uint32_t)((h + 31) / 32), groups, 2), dim3(32, 8), stream,
                                  (const float*)workspace, dweight, dbias, (int32_t)h, per),
                     "norm_join");
