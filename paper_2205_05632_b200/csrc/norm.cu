@@ -44,6 +44,13 @@ __device__ __forceinline__ float warp_sum(float x) {
     for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
     return x;
 }
+// Over W neighbouring lanes.
+template <int W>
+__device__ __forceinline__ float few_sum(float x) {
+#pragma unroll
+    for (int o = W / 2; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    return x;
+}
 // The sum over the W warps of a row; the same order on every warp. `scratch`: W floats that no one reads any more.
 template <int W>
 __device__ __forceinline__ float row_sum(float x, float* scratch, int warp) {
@@ -97,7 +104,7 @@ __device__ __forceinline__ void row_copy(char* smem, int stage, int slot, const 
 }
 // A lane's values of the span from column c0 on, `beyond` in the columns from h on.
 template <typename T, int W, int SLOTS, bool VEC, bool RING>
-__device__ __forceinline__ void row_take(char* smem, int stage, int slot, const T* row, int c0, int h, int lane, float beyond, float (&to)[8]) {
+__device__ __forceinline__ void row_take(char* smem, int stage, int slot, const T* row, int c0, int h, int lane, float beyond, Pair (&to)[4]) {
     if constexpr (RING) {
         if (c0 + lane * 8 < h) {
             Raw8<T> r;
@@ -105,10 +112,10 @@ __device__ __forceinline__ void row_take(char* smem, int stage, int slot, const 
 #pragma unroll
             for (int k = 0; k < raw_slots<T>(); ++k) u[k] = *row_place<W, SLOTS>(smem, stage, slot + k);
             memcpy(&r, u, sizeof(r));
-            raw_floats<T>(r, to);
+            raw_pairs<T>(r, to);
         } else {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) to[k] = beyond;
+            for (int p = 0; p < 4; ++p) to[p] = pair(beyond);
         }
     } else {
         span_load<T, VEC>(row, c0, h, lane, to, beyond);
@@ -137,10 +144,10 @@ __global__ void __launch_bounds__(norm_threads<W>(), norm_ctas<W, NG, VEC, false
     const TR* residual = ADD ? (const TR*)a.residual + (int64_t)i * a.r_ws : nullptr;
     const float* weight = a.weight ? a.weight + (int64_t)i * a.weight_ws : nullptr;
     const float* bias = a.bias ? a.bias + (int64_t)i * a.bias_ws : nullptr;
-    auto affine = [&](int q, float (&w)[8], float (&b)[8]) {
+    auto affine = [&](int q, Pair (&w)[4], Pair (&b)[4]) {
         const int c0 = (q * W + warp) * kSpan;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) b[k] = 0.0f, w[k] = 1.0f;
+        for (int p = 0; p < 4; ++p) b[p] = pair(0.0f), w[p] = pair(1.0f);
         if (weight) span_load<float, VEC>(weight, c0, a.h, lane, w);
         if (bias) span_load<float, VEC>(bias, c0, a.h, lane, b);
     };
@@ -158,7 +165,7 @@ __global__ void __launch_bounds__(norm_threads<W>(), norm_ctas<W, NG, VEC, false
         }
     };
     for (int k = 0; k + 1 < kStages; ++k) fetch(j0 + slot + k * kRows, k);
-    float w[kHold ? NG : 1][8], b[kHold ? NG : 1][8];
+    Pair w[kHold ? NG : 1][4], b[kHold ? NG : 1][4];
     if (kHold)
 #pragma unroll
         for (int q = 0; q < NG; ++q) affine(q, w[kHold ? q : 0], b[kHold ? q : 0]);
@@ -170,7 +177,7 @@ __global__ void __launch_bounds__(norm_threads<W>(), norm_ctas<W, NG, VEC, false
         return (float)c;
     };
     const float own = columns(warp), per_own = own > 0.0f ? 1.0f / own : 0.0f, per_row = 1.0f / (float)a.h;
-    const float lane_columns = lane < W ? columns(lane) : 0.0f;
+    const float lane_columns = columns(lane % W);
     int turn = 0, stage = 0;
     for (uint32_t j = j0 + slot; j < j1; j += kRows, turn ^= 1) {
         const uint32_t m = i * a.rows + j;
@@ -178,51 +185,59 @@ __global__ void __launch_bounds__(norm_threads<W>(), norm_ctas<W, NG, VEC, false
             fetch(j + (kStages - 1) * kRows, stage == 0 ? kStages - 1 : stage - 1);
             copies_wait<kStages - 1>();  // a lane's own
         }
-        float v[NG][8], sum = 0.0f;
+        Pair v[NG][4], sum = pair(0.0f);
 #pragma unroll
         for (int q = 0; q < NG; ++q) {
             const int c0 = (q * W + warp) * kSpan;
             row_take<TX, W, SLOTS, VEC, RING>(smem, stage, q * raw_slots<TX>(), x + (int64_t)j * a.x_rs, c0, a.h, lane, 0.0f, v[q]);
             if (ADD && c0 < a.h) {
-                float add[8];
+                Pair more[4];
                 row_take<TR, W, SLOTS, VEC, RING>(smem, stage, NG * raw_slots<TX>() + q * raw_slots<TR>(), residual + (int64_t)j * a.r_rs, c0,
-                                                  a.h, lane, 0.0f, add);
+                                                  a.h, lane, 0.0f, more);
                 if (a.drop.on) span_drop<VEC>(a.drop, c0, j, a.drop.worker + i, call, lane, v[q]);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) v[q][k] = to_float(from_float<TR>(v[q][k] + add[k]));
-                span_store<TR, VEC>((TR*)a.s + (int64_t)m * a.h, c0, a.h, lane, v[q]);
+                for (int p = 0; p < 4; ++p) v[q][p] = add(v[q][p], more[p]);
+                span_store<TR, VEC, true>((TR*)a.s + (int64_t)m * a.h, c0, a.h, lane, v[q]);
             }
 #pragma unroll
-            for (int k = 0; k < 8; ++k) sum += v[q][k];  // 0 beyond h
+            for (int p = 0; p < 4; ++p) sum = add(sum, v[q][p]);  // 0 beyond h
         }
         stage = stage + 1 == kStages ? 0 : stage + 1;
-        float mean = warp_sum(sum) * per_own, square = 0.0f;
+        const float mean = warp_sum(joint(sum)) * per_own;
+        Pair squares = pair(0.0f);
 #pragma unroll
-        for (int q = 0; q < NG; ++q)
+        for (int q = 0; q < NG; ++q) {
+            const int c0 = (q * W + warp) * kSpan;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const float d = span_column<VEC>((q * W + warp) * kSpan, lane, k) < a.h ? v[q][k] - mean : 0.0f;
-                square = fmaf(d, d, square);
+            for (int p = 0; p < 4; ++p) {
+                if (VEC) {
+                    v[q][p] = add(v[q][p], pair(c0 + lane * 8 < a.h ? -mean : 0.0f));
+                } else {
+                    v[q][p] = add(v[q][p], pair(c0 + 64 * p + lane < a.h ? -mean : 0.0f, c0 + 64 * p + 32 + lane < a.h ? -mean : 0.0f));
+                }
+                squares = fma(v[q][p], v[q][p], squares);
             }
-        square = warp_sum(square);
+        }
+        float square = warp_sum(joint(squares)), off = 0.0f, centre = mean;  // off: of the warp's mean from the row's
         if (W > 1) {
             if (lane == 0) scratch[turn][warp] = make_float2(mean, square);
             __syncthreads();  // the next row writes the other half, and the one after it only behind the next row's barrier
-            // lane k joins warp k's; the sums are the same tree in every warp
-            const float2 part = lane < W ? scratch[turn][lane] : make_float2(0.0f, 0.0f);
-            mean = warp_sum(lane_columns * part.x) * per_row;
-            const float d = part.x - mean;
-            square = warp_sum(fmaf(lane_columns * d, d, part.y));
+            const float2 part = scratch[turn][lane % W];  // every W lanes join the W warps' in the same way
+            centre = few_sum<W>(lane_columns * part.x) * per_row;
+            const float d = part.x - centre;
+            square = few_sum<W>(fmaf(lane_columns * d, d, part.y));
+            off = mean - centre;
         }
         const float rstd = 1.0f / sqrtf(square * per_row + a.eps);
-        if (a.stats && warp == 0 && lane == 0) a.stats[m] = make_float2(mean, rstd);
+        if (a.stats && warp == 0 && lane == 0) a.stats[m] = make_float2(centre, rstd);
+        const Pair factor = pair(rstd), offset = pair(off * rstd);
 #pragma unroll
         for (int q = 0; q < NG; ++q) {
             const int c0 = (q * W + warp) * kSpan;
             if (c0 >= a.h) break;
             if (!kHold) affine(q, w[0], b[0]);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[q][k] = fmaf((v[q][k] - mean) * rstd, w[kHold ? q : 0][k], b[kHold ? q : 0][k]);
+            for (int p = 0; p < 4; ++p) v[q][p] = fma(fma(v[q][p], factor, offset), w[kHold ? q : 0][p], b[kHold ? q : 0][p]);
             span_store<TX, VEC>((TX*)a.y + (int64_t)m * a.h, c0, a.h, lane, v[q]);
         }
     }
@@ -280,12 +295,12 @@ __host__ __device__ constexpr int backward_slots() { return NG * (raw_slots<TX>(
 // a second time behind the barrier instead of being held, and with four the weight is read again for each row: registers are what
 // bounds the CTAs of an SM.
 template <typename TX, typename TR, int W, int NG, bool VEC, bool ADD>
-__global__ void __launch_bounds__(norm_threads<W>(), norm_ctas<W, NG, VEC, ADD>()) norm_backward_kernel(const __grid_constant__ NormArgs a) {
+__global__ void __launch_bounds__(norm_threads<W>(), norm_ctas<W, NG, VEC, true>()) norm_backward_kernel(const __grid_constant__ NormArgs a) {
     extern __shared__ __align__(16) char smem[];
     constexpr int kSlots = W == 1 ? kRowsOfOneWarp : 1, SX = raw_slots<TX>(), SR = raw_slots<TR>();
     constexpr int SLOTS = backward_slots<TX, TR, NG, ADD>(), kStages = row_stages<W, SLOTS, VEC>();
     constexpr bool RING = kStages > 0;
-    __shared__ float scratch[2][2][W];
+    __shared__ float2 scratch[2][W];
     __shared__ float joined[W == 1 ? NG * kSpan : 1];
     const int lane = threadIdx.x & 31, warp = W == 1 ? 0 : (int)(threadIdx.x >> 5), slot = W == 1 ? (int)(threadIdx.x >> 5) : 0;
     const uint32_t i = blockIdx.x / a.chunks, chunk = blockIdx.x - i * a.chunks;
@@ -295,16 +310,16 @@ __global__ void __launch_bounds__(norm_threads<W>(), norm_ctas<W, NG, VEC, ADD>(
     const TR* v = (const TR*)a.v + (int64_t)i * a.v_ws;
     const TR* more = ADD && a.residual ? (const TR*)a.residual + (int64_t)i * a.r_ws : nullptr;
     constexpr bool kHold = NG == 1, kHoldWeight = NG <= 2;
-    float held[kHoldWeight ? NG : 1][8], dw[NG][8], db[NG][8];
-    auto weight = [&](int q, float (&w)[8]) {
+    Pair held[kHoldWeight ? NG : 1][4], dw[NG][4], db[NG][4];
+    auto weight = [&](int q, Pair (&w)[4]) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) w[k] = 1.0f;
+        for (int p = 0; p < 4; ++p) w[p] = pair(1.0f);
         if (a.weight) span_load<float, VEC>(a.weight + (int64_t)i * a.weight_ws, (q * W + warp) * kSpan, a.h, lane, w);
     };
 #pragma unroll
     for (int q = 0; q < NG; ++q) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) dw[q][k] = db[q][k] = 0.0f;
+        for (int p = 0; p < 4; ++p) dw[q][p] = db[q][p] = pair(0.0f);
         if (kHoldWeight) weight(q, held[kHoldWeight ? q : 0]);
     }
     auto fetch = [&](uint32_t j, int stage) {
@@ -323,6 +338,7 @@ __global__ void __launch_bounds__(norm_threads<W>(), norm_ctas<W, NG, VEC, ADD>(
     };
     for (int k = 0; k + 1 < kStages; ++k) fetch(j0 + slot + k * kSlots, k);
     int turn = 0, stage = 0;
+    const float per_row = 1.0f / (float)a.h;
     float2 next = j0 + slot < j1 ? a.stats[i * a.rows + j0 + slot] : make_float2(0.0f, 0.0f);
     for (uint32_t j = j0 + slot; j < j1; j += kSlots, turn ^= 1) {
         const uint32_t m = i * a.rows + j;
@@ -332,60 +348,55 @@ __global__ void __launch_bounds__(norm_threads<W>(), norm_ctas<W, NG, VEC, ADD>(
             fetch(j + (kStages - 1) * kSlots, stage == 0 ? kStages - 1 : stage - 1);
             copies_wait<kStages - 1>();  // a lane's own
         }
-        float g[8], xhat[8], c1 = 0.0f, c2 = 0.0f;
+        Pair g[4], xhat[4], sum1 = pair(0.0f), sum2 = pair(0.0f);
+        const Pair rstd = pair(st.y), shift = pair(-st.x * st.y);
         // dy w and xhat of span q; the first time its share of the sums
         auto values = [&](int q, bool first) {
             const int c0 = (q * W + warp) * kSpan;
             row_take<TX, W, SLOTS, VEC, RING>(smem, stage, q * SX, dy + (int64_t)j * a.x_rs, c0, a.h, lane, 0.0f, g);
             row_take<TR, W, SLOTS, VEC, RING>(smem, stage, NG * SX + q * SR, v + (int64_t)j * a.v_rs, c0, a.h, lane, st.x, xhat);
-            float w[8];
+            Pair w[4];
             if (!kHoldWeight) weight(q, w);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                xhat[k] = (xhat[k] - st.x) * st.y;
+            for (int p = 0; p < 4; ++p) {
+                xhat[p] = fma(xhat[p], rstd, shift);
                 if (first) {
-                    db[q][k] += g[k];
-                    dw[q][k] = fmaf(g[k], xhat[k], dw[q][k]);
+                    db[q][p] = add(db[q][p], g[p]);
+                    dw[q][p] = fma(g[p], xhat[p], dw[q][p]);
                 }
-                g[k] *= kHoldWeight ? held[kHoldWeight ? q : 0][k] : w[k];
+                g[p] = mul(g[p], kHoldWeight ? held[kHoldWeight ? q : 0][p] : w[p]);
                 if (first) {
-                    c1 += g[k];
-                    c2 = fmaf(g[k], xhat[k], c2);
+                    sum1 = add(sum1, g[p]);
+                    sum2 = fma(g[p], xhat[p], sum2);
                 }
             }
         };
 #pragma unroll
         for (int q = 0; q < NG; ++q) values(q, true);
         if (a.y || (ADD && a.s)) {
-            c1 = warp_sum(c1);
-            c2 = warp_sum(c2);
+            float c1 = warp_sum(joint(sum1)), c2 = warp_sum(joint(sum2));
             if (W > 1) {
-                if (lane == 0) {
-                    scratch[turn][0][warp] = c1;
-                    scratch[turn][1][warp] = c2;
-                }
+                if (lane == 0) scratch[turn][warp] = make_float2(c1, c2);
                 __syncthreads();  // the next row writes the other half, and the one after it only behind the next row's barrier
-                c1 = c2 = 0.0f;
-#pragma unroll
-                for (int k = 0; k < W; ++k) {
-                    c1 += scratch[turn][0][k];
-                    c2 += scratch[turn][1][k];
-                }
+                const float2 part = scratch[turn][lane % W];
+                c1 = few_sum<W>(part.x);
+                c2 = few_sum<W>(part.y);
             }
-            c1 *= 1.0f / (float)a.h;
-            c2 *= 1.0f / (float)a.h;
+            // rstd (g - c1 - xhat c2)
+            const Pair less = pair(-c1 * per_row * st.y), along = pair(-c2 * per_row * st.y);
 #pragma unroll
             for (int q = 0; q < NG; ++q) {
                 const int c0 = (q * W + warp) * kSpan;
                 if (c0 >= a.h) break;
                 if (!kHold) values(q, false);
-                float add[8];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) add[k] = 0.0f;
-                if (ADD && more)
-                    row_take<TR, W, SLOTS, VEC, RING>(smem, stage, NG * (SX + SR) + q * SR, more + (int64_t)j * a.r_rs, c0, a.h, lane, 0.0f, add);
+                for (int p = 0; p < 4; ++p) g[p] = fma(xhat[p], along, fma(g[p], rstd, less));
+                if (ADD && more) {
+                    Pair r[4];
+                    row_take<TR, W, SLOTS, VEC, RING>(smem, stage, NG * (SX + SR) + q * SR, more + (int64_t)j * a.r_rs, c0, a.h, lane, 0.0f, r);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) g[k] = fmaf(st.y, g[k] - c1 - xhat[k] * c2, add[k]);
+                    for (int p = 0; p < 4; ++p) g[p] = add(g[p], r[p]);
+                }
                 if (ADD && a.s) span_store<TR, VEC>((TR*)a.s + (int64_t)m * a.h, c0, a.h, lane, g);
                 if (ADD && a.drop.on && a.y) span_drop<VEC>(a.drop, c0, j, a.drop.worker + i, call, lane, g);
                 if (a.y) span_store<TX, VEC>((TX*)a.y + (int64_t)m * a.h, c0, a.h, lane, g);
@@ -409,10 +420,14 @@ __global__ void __launch_bounds__(norm_threads<W>(), norm_ctas<W, NG, VEC, ADD>(
 #pragma unroll
                     for (int q = 0; q < NG; ++q)
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            const int at = span_column<VEC>(q * kSpan, lane, k);
-                            const float x = which ? db[q][k] : dw[q][k];
-                            joined[at] = s == 0 ? x : joined[at] + x;
+                        for (int p = 0; p < 4; ++p) {
+                            float x[2];
+                            halves(which ? db[q][p] : dw[q][p], x[0], x[1]);
+#pragma unroll
+                            for (int k = 0; k < 2; ++k) {
+                                const int at = span_column<VEC>(q * kSpan, lane, 2 * p + k);
+                                joined[at] = s == 0 ? x[k] : joined[at] + x[k];
+                            }
                         }
                 }
                 __syncthreads();
@@ -530,15 +545,15 @@ struct Held {
         r = {};
         if (c0 + lane * 8 < h) r = raw_load<T>(row + c0 + lane * 8);
     }
-    __device__ __forceinline__ void floats(float (&v)[8]) const { raw_floats<T>(r, v); }
+    __device__ __forceinline__ void pairs(Pair (&v)[4]) const { raw_pairs<T>(r, v); }
 };
 template <typename T>
 struct Held<T, false> {
-    float x[8];
+    Pair x[4];
     __device__ __forceinline__ void load(const T* row, int c0, int h, int lane) { span_load<T, false>(row, c0, h, lane, x); }
-    __device__ __forceinline__ void floats(float (&v)[8]) const {
+    __device__ __forceinline__ void pairs(Pair (&v)[4]) const {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = x[k];
+        for (int p = 0; p < 4; ++p) v[p] = x[p];
     }
 };
 template <typename T, bool VEC, typename U>
@@ -587,8 +602,8 @@ __global__ void __launch_bounds__(256) dropout_kernel(const __grid_constant__ Dr
 #pragma unroll
         for (int k = 0; k < kDropSpans; ++k) {
             const int c0 = tm < a.total ? (int)tspan * kSpan : a.h;
-            float v[8];
-            now[k].floats(v);
+            Pair v[4];
+            now[k].pairs(v);
             if (a.drop.on) span_drop<VEC>(a.drop, c0, tj, a.drop.worker + ti, call, lane, v);
             span_store<T, VEC>((T*)a.y + (int64_t)tm * a.h, c0, a.h, lane, v);
             place(tm, tspan, ti, tj);

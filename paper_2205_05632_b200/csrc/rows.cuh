@@ -74,6 +74,41 @@ template <> __device__ __forceinline__ void store8<float>(float* p, const float 
     reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
 }
 
+// ---- pairs -------------------------------------------------------------------------------------------------------------------
+
+// Two fp32 numbers that one instruction adds or multiplies, each rounded as by itself: the kernels below are bound by what the SMs can
+// issue where they are not by memory.
+struct Pair {
+    uint64_t u;
+};
+__device__ __forceinline__ Pair pair(float a, float b) {
+    Pair r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r.u) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ Pair pair(float a) { return pair(a, a); }
+__device__ __forceinline__ void halves(Pair x, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x.u)); }
+__device__ __forceinline__ float joint(Pair x) {
+    float a, b;
+    halves(x, a, b);
+    return a + b;
+}
+__device__ __forceinline__ Pair add(Pair a, Pair b) {
+    Pair r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.u) : "l"(a.u), "l"(b.u));
+    return r;
+}
+__device__ __forceinline__ Pair mul(Pair a, Pair b) {
+    Pair r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.u) : "l"(a.u), "l"(b.u));
+    return r;
+}
+__device__ __forceinline__ Pair fma(Pair a, Pair b, Pair c) {
+    Pair r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.u) : "l"(a.u), "l"(b.u), "l"(c.u));
+    return r;
+}
+
 // ---- asynchronous copies -----------------------------------------------------------------------------------------------------
 
 // Asynchronous copies of 16 bytes into shared memory; zeros where `there` is false (an address in bounds all the same).
@@ -119,6 +154,63 @@ __device__ __forceinline__ void span_store(T* __restrict__ row, int c0, int h, i
         for (int k = 0; k < 8; ++k) {
             const int c = c0 + k * 32 + lane;
             if (c < h) row[c] = from_float<T>(v[k]);
+        }
+    }
+}
+
+// The same in pairs: a lane's values 2 p and 2 p + 1.
+template <typename T> __device__ __forceinline__ void raw_pairs(const Raw8<T>& r, Pair (&v)[4]) {
+    float x[8];
+    raw_floats<T>(r, x);
+#pragma unroll
+    for (int p = 0; p < 4; ++p) v[p] = pair(x[2 * p], x[2 * p + 1]);
+}
+template <typename T> __device__ __forceinline__ Raw8<T> pack_pairs(const Pair (&v)[4]) {
+    float x[8];
+#pragma unroll
+    for (int p = 0; p < 4; ++p) halves(v[p], x[2 * p], x[2 * p + 1]);
+    return {make_uint4(pack(x[0], x[1], T()), pack(x[2], x[3], T()), pack(x[4], x[5], T()), pack(x[6], x[7], T()))};
+}
+template <> __device__ __forceinline__ Raw8<float> pack_pairs<float>(const Pair (&v)[4]) {
+    Raw8<float> r;
+    halves(v[0], r.a.x, r.a.y);
+    halves(v[1], r.a.z, r.a.w);
+    halves(v[2], r.b.x, r.b.y);
+    halves(v[3], r.b.z, r.b.w);
+    return r;
+}
+template <typename T> __device__ __forceinline__ void raw_store(T* p, const Raw8<T>& r) { *reinterpret_cast<uint4*>(p) = r.q; }
+template <> __device__ __forceinline__ void raw_store<float>(float* p, const Raw8<float>& r) {
+    reinterpret_cast<float4*>(p)[0] = r.a;
+    reinterpret_cast<float4*>(p)[1] = r.b;
+}
+template <typename T, bool VEC>
+__device__ __forceinline__ void span_load(const T* __restrict__ row, int c0, int h, int lane, Pair (&v)[4], float beyond = 0.0f) {
+    float x[8];
+    span_load<T, VEC>(row, c0, h, lane, x, beyond);
+#pragma unroll
+    for (int p = 0; p < 4; ++p) v[p] = pair(x[2 * p], x[2 * p + 1]);
+}
+// Rounds to T and stores; v becomes what was stored where KEEP.
+template <typename T, bool VEC, bool KEEP = false>
+__device__ __forceinline__ void span_store(T* __restrict__ row, int c0, int h, int lane, Pair (&v)[4]) {
+    if constexpr (VEC) {
+        const Raw8<T> r = pack_pairs<T>(v);
+        if (c0 + lane * 8 < h) raw_store<T>(row + c0 + lane * 8, r);
+        if (KEEP) raw_pairs<T>(r, v);
+    } else {
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+            float x[2];
+            halves(v[p], x[0], x[1]);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const T t = from_float<T>(x[k]);
+                const int c = c0 + (2 * p + k) * 32 + lane;
+                if (c < h) row[c] = t;
+                x[k] = to_float(t);
+            }
+            if (KEEP) v[p] = pair(x[0], x[1]);
         }
     }
 }
@@ -185,6 +277,27 @@ __device__ __forceinline__ void span_drop(const Drop& d, int c0, uint32_t row, u
 #pragma unroll
         for (int k = 0; k < 8; ++k)
             v[k] = (__shfl_sync(0xffffffffu, bits, k * 4 + (lane >> 3)) >> (lane & 7)) & 1u ? v[k] * d.factor : 0.0f;
+    }
+}
+
+template <bool VEC>
+__device__ __forceinline__ void span_drop(const Drop& d, int c0, uint32_t row, uint32_t worker, uint32_t call, int lane, Pair (&v)[4]) {
+    const uint4 u = drop_words(d, (uint32_t)(c0 >> 3) + lane, row, worker, call);
+    uint32_t bits = 0;
+    if (!VEC)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) bits |= drop_keeps(d, u, k) ? 1u << k : 0u;
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        float x[2];
+        halves(mul(v[p], pair(d.factor)), x[0], x[1]);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int e = 2 * p + k;
+            const bool keep = VEC ? drop_keeps(d, u, e) : (__shfl_sync(0xffffffffu, bits, e * 4 + (lane >> 3)) >> (lane & 7)) & 1u;
+            x[k] = keep ? x[k] : 0.0f;
+        }
+        v[p] = pair(x[0], x[1]);
     }
 }
 
