@@ -23,6 +23,7 @@
 #include <cooperative_groups.h>
 #include <string.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "context.h"
@@ -243,6 +244,14 @@ __global__ void __launch_bounds__(256) adapter_prepare_kernel(const __grid_const
         out[p * 64 + 32] = make_uint4(w[2][0][p], w[2][1][p], w[3][0][p], w[3][1][p]);
     }
 }
+
+}  // namespace
+}  // namespace compams
+
+#include "adapter_tensor.cuh"
+
+namespace compams {
+namespace {
 
 // ---- rings of asynchronous copies ------------------------------------------------------------------------------------------
 
@@ -940,9 +949,29 @@ struct AdapterShape {
 // there, three quarters of the products are of zeros, and the fragments are written and read again for them.
 bool few(const AdapterShape& z) { return z.rows <= kFewRows; }
 
+// Whether the products run on tcgen05.mma.
+bool on_tensor(const AdapterShape& z, int32_t type) {
+    return type == kTypeBF16 && z.rank > tensor::kRank / 2 && z.rank <= tensor::kRank && z.rows >= 64;
+}
+
+// The number of parts, of 1 ... most, at which the slowest of `slots` places ends first: waves of tiles * parts CTAs, each a part's
+// share of `work` and `fixed` more.
+int64_t parts_of(int64_t tiles, int64_t slots, int64_t work, double fixed, int64_t most, bool powers) {
+    int64_t best = 1;
+    double least = 0.0;
+    for (int64_t c = 1; c <= most && c <= work; c = powers ? 2 * c : c + 1) {
+        const double cost = (double)((tiles * c + slots - 1) / slots) * ((double)((work + c - 1) / c) + fixed);
+        if (c == 1 || cost < least * 0.999) best = c, least = cost;
+    }
+    return best;
+}
+
 // Chunks of a worker's rows: as many as give each SM about two CTAs, of 64 rows at least.
-uint32_t outer_chunks(const AdapterShape& z, int64_t h) {
+uint32_t outer_chunks(const AdapterShape& z, int64_t h, int32_t type) {
     if (few(z)) return 1;
+    // (partial sums beyond the first cost as much as `rank` rows of bf16)
+    if (on_tensor(z, type))
+        return (uint32_t)parts_of((h + 255) / 256 * z.n, 148, (z.rows + 63) / 64, 4.0, std::min<int64_t>(65535 / z.n, 8), false);
     const int64_t tiles = (h + kOuterColumns - 1) / kOuterColumns * rank_groups(z.rank) * z.n;
     int64_t c = (148 * 2 + tiles - 1) / tiles;
     const int64_t most = (z.rows + 63) / 64;
@@ -950,8 +979,8 @@ uint32_t outer_chunks(const AdapterShape& z, int64_t h) {
     if (c > 65535 / z.n) c = 65535 / z.n;
     return (uint32_t)(c < 1 ? 1 : c);
 }
-int64_t outer_floats(const AdapterShape& z, int64_t h, bool sum_workers) {
-    const uint32_t c = outer_chunks(z, h);
+int64_t outer_floats(const AdapterShape& z, int64_t h, bool sum_workers, int32_t type) {
+    const uint32_t c = outer_chunks(z, h, type);
     return c == 1 && (!sum_workers || z.n == 1) ? 0 : (int64_t)z.n * c * z.rank * h;
 }
 
@@ -1007,8 +1036,57 @@ AdapterArgs arguments(const AdapterShape& z, Rows x, int64_t h, const Low& low, 
     return a;
 }
 
+// The three products on tcgen05.mma; the images stand where the fragments do.
+int tensor_prepare(const AdapterShape& z, bool shared, Factor down, int64_t down_h, void* down_image, Factor up, int64_t up_h, void* up_image,
+                   const float* t, void* t_image, cudaStream_t stream) {
+    tensor::PrepareArgs p = {down, up, (char*)down_image, (char*)up_image, t, (char*)t_image, (int32_t)down_h, (int32_t)up_h, z.rank,
+                             (uint32_t)z.rows, 0, 0, 0, shared};
+    if (down_image) p.down_count = (uint32_t)((down_h + 63) / 64 * 512);
+    if (up_image) p.up_count = (uint32_t)((up_h + 127) / 128 * 1024);
+    if (t_image) p.t_count = (uint32_t)((z.rows + 63) / 64 * 512);
+    const uint64_t ctas = ((uint64_t)p.down_count + p.up_count + p.t_count + 255) / 256;
+    if (ctas > 0x00ffffffu) return COMPAMS_ERR_TOO_LARGE;
+    const uint32_t workers = shared && !t_image ? 1 : (uint32_t)z.n;
+    return launched(launch_next(tensor::prepare_kernel, dim3((uint32_t)ctas, workers), 1, 0, true, stream, p), "adapter_prepare");
+}
+
+int tensor_down(Low low, Rows x, const AdapterShape& z, int64_t h, bool shared, const uint4* image, float scale, const Drop& d,
+                cudaStream_t stream) {
+    tensor::Args a = {};
+    a.x = x.p; a.x_ws = x.worker_stride; a.x_rs = x.row_stride; a.image = (const char*)image; a.image_ws = shared ? 0 : tensor::down_image(h);
+    a.t_up = (char*)low.up; a.t_outer = (char*)low.outer; a.out = low.t; a.rows = (uint32_t)z.rows; a.h = (int32_t)h; a.rank = z.rank;
+    a.tiles = (a.rows + 255) / 256; a.scale = scale; a.drop = d;
+    a.split = (int32_t)parts_of((int64_t)a.tiles * z.n, 148, (h + 63) / 64, 4.0, 4, true);
+    const uint64_t ctas = (uint64_t)a.tiles * z.n * a.split;
+    if (ctas > 0x7fffffffu) return COMPAMS_ERR_TOO_LARGE;
+    auto kernel = h % 8 == 0 && x.aligned() ? tensor::down_kernel<true> : tensor::down_kernel<false>;
+    return launched(launch_next(kernel, dim3((uint32_t)ctas), a.split, tensor::kShared, false, stream, a), "adapter_down");
+}
+
+int tensor_up(void* y, Rows base, Low low, const AdapterShape& z, int64_t h, bool shared, const uint4* image, float scale, const Drop& d,
+              cudaStream_t stream) {
+    tensor::UpArgs a = {};
+    a.base = base.p; a.y = y; a.image = (const char*)image; a.t_up = (const char*)low.up; a.base_ws = base.worker_stride;
+    a.base_rs = base.row_stride; a.image_ws = shared ? 0 : tensor::up_image(h); a.rows = (uint32_t)z.rows; a.h = (int32_t)h; a.scale = scale;
+    a.drop = d;
+    const int64_t columns = (h + 127) / 128, blocks = (z.rows + 127) / 128;
+    a.chunks = (uint32_t)parts_of(columns * z.n, 2 * 148, blocks, 0.5, 65535 / z.n, false);
+    const bool vec = h % 8 == 0 && (!base.p || base.aligned()) && packed(y, z.rows, h, base.type).aligned();
+    auto kernel = vec ? tensor::up_kernel<true> : tensor::up_kernel<false>;
+    return launched(launch_next(kernel, dim3((uint32_t)columns, (uint32_t)z.n * a.chunks), 1, tensor::kUpShared, false, stream, a), "adapter_up");
+}
+
+cudaError_t tensor_outer(AdapterArgs& b, Rows x, Low low, const AdapterShape& z, int64_t h, bool first, cudaStream_t stream) {
+    tensor::Args a = {};
+    a.x = b.x; a.x_ws = b.x_ws; a.x_rs = b.x_rs; a.image = (const char*)low.outer; a.image_ws = tensor::t_outer_image(z.rows); a.out = b.out;
+    a.sj = b.f.sj; a.sc = b.f.sc; a.rows = b.rows; a.h = b.h; a.rank = b.rank; a.chunks = b.chunks; a.scale = b.scale; a.drop = b.drop;
+    auto kernel = h % 8 == 0 && x.aligned() ? tensor::outer_kernel<true> : tensor::outer_kernel<false>;
+    return launch_next(kernel, dim3((uint32_t)((h + 255) / 256), (uint32_t)z.n * a.chunks), 1, tensor::kShared, first, stream, a);
+}
+
 int prepare(const AdapterShape& z, bool shared, Factor down, int64_t down_h, uint4* down_frag, Factor up, int64_t up_h, uint4* up_frag,
-            const float* t, uint2* t_outer, cudaStream_t stream) {
+            const float* t, uint2* t_outer, int32_t type, cudaStream_t stream) {
+    if (on_tensor(z, type)) return tensor_prepare(z, shared, down, down_h, down_frag, up, up_h, up_frag, t, t_outer, stream);
     PrepareArgs p = {down, up, down_frag, up_frag, t, t_outer, (int32_t)down_h, (int32_t)up_h, z.rank, (uint32_t)z.rows, 0, 0, 0, shared};
     if (down_frag) p.down_count = (uint32_t)(down_blocks(down_h) * rank_tiles(z.rank));
     if (up_frag) p.up_count = (uint32_t)((up_h + kUpColumns - 1) / kUpColumns * ((z.rank + 15) / 16));
@@ -1021,6 +1099,7 @@ int prepare(const AdapterShape& z, bool shared, Factor down, int64_t down_h, uin
 
 int down(Low low, Rows x, const AdapterShape& z, int64_t h, bool shared, Factor f, const uint4* frag, float scale, const Drop& d,
          cudaStream_t stream) {
+    if (on_tensor(z, x.type)) return tensor_down(low, x, z, h, shared, frag, scale, d, stream);
     AdapterArgs a = arguments(z, x, h, low, scale, d);
     a.out = low.t; a.f = f; a.frag = frag; a.frag_ws = shared ? 0 : down_frag_words(h, z.rank);
     const bool vec = h % 8 == 0 && x.aligned();
@@ -1067,6 +1146,7 @@ int down(Low low, Rows x, const AdapterShape& z, int64_t h, bool shared, Factor 
 
 int up(void* y, Rows base, Low low, const AdapterShape& z, int64_t h, bool shared, Factor f, const uint4* frag, float scale, const Drop& d,
        cudaStream_t stream) {
+    if (on_tensor(z, base.type)) return tensor_up(y, base, low, z, h, shared, frag, scale, d, stream);
     AdapterArgs a = arguments(z, base, h, low, scale, d);
     a.y = y; a.f = f; a.frag = frag; a.frag_ws = shared ? 0 : up_frag_words(h, z.rank);
     const bool vec = h % 8 == 0 && (!base.p || base.aligned()) && packed(y, z.rows, h, base.type).aligned();
@@ -1106,14 +1186,15 @@ int up(void* y, Rows base, Low low, const AdapterShape& z, int64_t h, bool share
 int outer(float* out, bool sum_workers, Rows x, Low low, const AdapterShape& z, int64_t h, int64_t sj, int64_t sc, float scale,
           const Drop& d, float* partial, bool first, cudaStream_t stream) {
     AdapterArgs a = arguments(z, x, h, low, scale, d);
-    a.f = {nullptr, 0, sj, sc}; a.chunks = outer_chunks(z, h);
-    const bool straight = outer_floats(z, h, sum_workers) == 0;
+    a.f = {nullptr, 0, sj, sc}; a.chunks = outer_chunks(z, h, x.type);
+    const bool straight = outer_floats(z, h, sum_workers, x.type) == 0;
     a.out = straight ? out : partial;
     const int rc = by_type(x.type, [&](auto tt) {
         using T = decltype(tt);
         if (few(z))
             return launched(launch_next(adapter_outer_few_kernel<T>, dim3((uint32_t)((h + 255) / 256), (uint32_t)z.n), 1, 0, first, stream, a),
                             "adapter_outer");
+        if (on_tensor(z, x.type)) return launched(tensor_outer(a, x, low, z, h, first, stream), "adapter_outer");
         const int nt = group_tiles(z.rank);
         const uint64_t tiles = (uint64_t)((h + kOuterColumns - 1) / kOuterColumns) * rank_groups(z.rank);
         if (tiles > 0x7fffffffu) return (int)COMPAMS_ERR_TOO_LARGE;
@@ -1154,14 +1235,24 @@ Places places(const AdapterShape& z, bool shared, bool backward, bool sum_worker
         at += (bytes + 255) / 256 * 256;
         return here;
     };
-    p.down = take(frags ? factors * down_frag_words(backward ? z.out : z.in, z.rank) * 16 : 0);
-    p.up = take(frags ? factors * up_frag_words(backward ? z.in : z.out, z.rank) * 16 : 0);
+    // (the larger of the fragments and the images, so that the size does not depend on the type)
+    auto either = [&](int64_t words, int64_t image) { return words * 16 > image ? words * 16 : image; };
+    const int64_t dh = backward ? z.out : z.in, uh = backward ? z.in : z.out;
+    if (frags) {
+        p.down = take(factors * either(down_frag_words(dh, z.rank), tensor::down_image(dh)));
+        p.up = take(factors * either(up_frag_words(uh, z.rank), tensor::up_image(uh)));
+        p.t_up = take(z.n * either(t_up_words(z.rows, z.rank, kPlanes), tensor::t_up_image(z.rows)));
+    }
+    if (frags && backward) {
+        p.t_outer = take(z.n * either(t_outer_words(z.rows, z.rank), tensor::t_outer_image(z.rows)));
+        p.saved = take(z.n * either(t_outer_words(z.rows, z.rank), tensor::t_outer_image(z.rows)));
+    }
     p.t = take(backward && !frags ? (int64_t)z.total() * z.rank * 4 : 0);
-    p.t_up = take(frags ? z.n * t_up_words(z.rows, z.rank, kPlanes) * 16 : 0);
-    p.t_outer = take(frags && backward ? z.n * t_outer_words(z.rows, z.rank) * 16 : 0);
-    p.saved = take(frags && backward ? z.n * t_outer_words(z.rows, z.rank) * 16 : 0);
-    const int64_t fa = backward ? outer_floats(z, z.in, sum_workers) : 0, fb = backward ? outer_floats(z, z.out, sum_workers) : 0;
-    p.partial = take((fa > fb ? fa : fb) * 4);
+    int64_t most = 0;
+    if (backward)
+        for (int32_t type : {kTypeF32, kTypeBF16})
+            for (int64_t h : {z.in, z.out}) most = std::max(most, outer_floats(z, h, sum_workers, type));
+    p.partial = take(most * 4);
     p.bytes = at;
     return p;
 }
@@ -1210,7 +1301,7 @@ int compams_adapter_forward(void* y, float* t, const void* x, const void* base, 
         down_frag = (uint4*)(work + at.down);
         up_frag = (uint4*)(work + at.up);
         low.up = (uint4*)(work + at.t_up);
-        rc = prepare(z, shared, fa, in, down_frag, fb, out, up_frag, nullptr, nullptr, stream);
+        rc = prepare(z, shared, fa, in, down_frag, fb, out, up_frag, nullptr, nullptr, type, stream);
     }
     if (rc == COMPAMS_OK) rc = down(low, xin, z, in, shared, fa, down_frag, 1.0f, d, stream);
     if (rc == COMPAMS_OK) rc = up(y, bin, low, z, out, shared, fb, up_frag, scale, none, stream);
@@ -1256,7 +1347,7 @@ int compams_adapter_backward(void* dx, float* da, float* db, int32_t sum_workers
         low.up = (uint4*)(work + at.t_up);
         if (da) low.outer = (uint2*)(work + at.t_outer);
         if (db) saved.outer = (uint2*)(work + at.saved);
-        rc = prepare(z, shared, fb, out, down_frag, fa, in, up_frag, t, saved.outer, stream);
+        rc = prepare(z, shared, fb, out, down_frag, fa, in, up_frag, t, saved.outer, type, stream);
         first = false;
     }
     if (rc == COMPAMS_OK && (dx || da)) {

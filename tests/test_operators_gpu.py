@@ -270,7 +270,8 @@ def test_norm_gradients_against_differences():
 
 ADAPTERS = [(1, 1, 1, 1, 1), (3, 5, 7, 9, 2), (2, 1, 64, 40, 8), (32, 1, 256, 264, 16), (2, 33, 100, 77, 3), (1, 70, 520, 1001, 12),
             (4, 16, 128, 128, 16), (2, 129, 264, 136, 17), (1, 200, 96, 1032, 64), (2, 40, 300, 200, 100), (1, 24, 2048, 64, 128),
-            (3, 65, 192, 320, 32), (1, 1100, 64, 72, 4), (1, 5, 40, 33, 300), (2, 0, 8, 8, 4)]
+            (3, 65, 192, 320, 32), (1, 1100, 64, 72, 4), (1, 5, 40, 33, 300), (2, 0, 8, 8, 4),
+            (2, 300, 264, 136, 40), (1, 130, 1032, 520, 64), (3, 64, 72, 88, 33), (1, 1000, 256, 2048, 64), (2, 257, 200, 129, 48), (5, 512, 4096, 1024, 64)]
 
 
 def adapter_case(g, n, rows, h, out, rank, dtype, form):
