@@ -994,14 +994,15 @@ int launched(cudaError_t e, const char* what) { return e == cudaSuccess ? COMPAM
 
 // A launch behind another of the same call (or the first), with dynamic shared memory and a cluster along x.
 template <typename... KArgs, typename... Args>
-cudaError_t launch_next(void (*kernel)(KArgs...), dim3 grid, int cluster, size_t shared, bool first, cudaStream_t stream, Args... args) {
+cudaError_t launch_sized(void (*kernel)(KArgs...), dim3 grid, int threads, int cluster, size_t shared, bool first, cudaStream_t stream,
+                         Args... args) {
     if (shared > 48 * 1024) {
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared);
         if (e != cudaSuccess) return e;
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
-    cfg.blockDim = dim3(256);
+    cfg.blockDim = dim3(threads);
     cfg.dynamicSmemBytes = shared;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
@@ -1019,6 +1020,11 @@ cudaError_t launch_next(void (*kernel)(KArgs...), dim3 grid, int cluster, size_t
     cfg.attrs = attr;
     cfg.numAttrs = count;
     return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
+}
+
+template <typename... KArgs, typename... Args>
+cudaError_t launch_next(void (*kernel)(KArgs...), dim3 grid, int cluster, size_t shared, bool first, cudaStream_t stream, Args... args) {
+    return launch_sized(kernel, grid, 256, cluster, shared, first, stream, args...);
 }
 
 // Where t goes to and comes from: fp32, and the operands of up and outer.
@@ -1060,7 +1066,7 @@ int tensor_down(Low low, Rows x, const AdapterShape& z, int64_t h, bool shared, 
     const uint64_t ctas = (uint64_t)a.tiles * z.n * a.split;
     if (ctas > 0x7fffffffu) return COMPAMS_ERR_TOO_LARGE;
     auto kernel = h % 8 == 0 && x.aligned() ? tensor::down_kernel<true> : tensor::down_kernel<false>;
-    return launched(launch_next(kernel, dim3((uint32_t)ctas), a.split, tensor::kShared, false, stream, a), "adapter_down");
+    return launched(launch_sized(kernel, dim3((uint32_t)ctas), tensor::kThreads, a.split, tensor::kShared, false, stream, a), "adapter_down");
 }
 
 int tensor_up(void* y, Rows base, Low low, const AdapterShape& z, int64_t h, bool shared, const uint4* image, float scale, const Drop& d,
@@ -1081,7 +1087,7 @@ cudaError_t tensor_outer(AdapterArgs& b, Rows x, Low low, const AdapterShape& z,
     a.x = b.x; a.x_ws = b.x_ws; a.x_rs = b.x_rs; a.image = (const char*)low.outer; a.image_ws = tensor::t_outer_image(z.rows); a.out = b.out;
     a.sj = b.f.sj; a.sc = b.f.sc; a.rows = b.rows; a.h = b.h; a.rank = b.rank; a.chunks = b.chunks; a.scale = b.scale; a.drop = b.drop;
     auto kernel = h % 8 == 0 && x.aligned() ? tensor::outer_kernel<true> : tensor::outer_kernel<false>;
-    return launch_next(kernel, dim3((uint32_t)((h + 255) / 256), (uint32_t)z.n * a.chunks), 1, tensor::kShared, first, stream, a);
+    return launch_sized(kernel, dim3((uint32_t)((h + 255) / 256), (uint32_t)z.n * a.chunks), tensor::kThreads, 1, tensor::kShared, first, stream, a);
 }
 
 int prepare(const AdapterShape& z, bool shared, Factor down, int64_t down_h, uint4* down_frag, Factor up, int64_t up_h, uint4* up_frag,

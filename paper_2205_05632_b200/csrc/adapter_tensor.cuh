@@ -7,9 +7,9 @@
 // and the sum runs along them (K-major); outer: the sum runs over the rows, the tile is read across them (MN-major), and t
 // comes turned, [plane, rank][row].
 //
-// All 256 threads copy (cp.async straight into the swizzle; where dropout masks an activation the thread that copied a chunk does so in
-// place), one issues the products, which run while the next tiles are being fetched. The tensor cores cut their sums, so after every four
-// tiles of 64 the sums go to fp32 registers by rounded additions.
+// 256 threads copy (cp.async straight into the swizzle; where dropout masks an activation the thread that copied a chunk does so in place), a
+// thread of a ninth warp copies the planes in bulk and issues the products; mbarriers pass the stages between them. The tensor cores cut
+// their sums, so after every kFlush tiles of 64 the sums go to fp32 registers by rounded additions.
 #pragma once
 
 #include "rows.cuh"
@@ -23,8 +23,8 @@ constexpr int kN = 3 * kRank;              // planes side by side
 constexpr int kTileBytes = 128 * 128;      // 128 rows of 64 elements, or 64 rows of 128
 constexpr int kPlanesBytes = kN * 128;     // planes: 192 rows of 64 elements
 constexpr int kStageBytes = 2 * kTileBytes + kPlanesBytes;
-constexpr int kStages = 3;
-constexpr int kFlush = 4;                  // tiles between two additions to the registers
+constexpr int kStages = 4;
+constexpr int kFlush = 8;                  // tiles between two additions to the registers
 constexpr int kShared = 1024 + kStages * kStageBytes;
 constexpr uint32_t kColumns = 512;         // of tensor memory: 2 x 192 used, a power of two taken
 
@@ -43,13 +43,14 @@ __device__ __forceinline__ uint32_t swizzled(uint32_t row, uint32_t chunk) { ret
 
 __device__ __forceinline__ uint32_t shared_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
-__device__ __forceinline__ void barrier_init(uint32_t bar) {
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar) : "memory");
+__device__ __forceinline__ void barrier_init(uint32_t bar, uint32_t count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
 }
+__device__ __forceinline__ void barrier_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 // Waits for the phase of this parity to end; gives up after a number of tries, each of which the hardware may hold for a while.
 __device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity) {
     uint32_t there = 0;
-    for (int tries = 0; tries < (1 << 16) && !there; ++tries)
+    for (int tries = 0; tries < (1 << 14) && !there; ++tries)
         asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
                      : "=r"(there)
                      : "r"(bar), "r"(parity)
@@ -95,9 +96,14 @@ __device__ __forceinline__ void columns32(uint32_t at, float (&v)[32]) {
           "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]),
           "=r"(r[31])
         : "r"(at));
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
     for (int k = 0; k < 32; ++k) v[k] = __uint_as_float(r[k]);
+}
+// Behind it the values are there.
+__device__ __forceinline__ void columns_wait(float (&v)[32]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int k = 0; k < 32; ++k) asm volatile("" : "+f"(v[k]));
 }
 
 // Set where a wait gave up, which no size or input should bring about; the results of that call are then worthless.
@@ -195,138 +201,18 @@ struct Args {
     Drop drop;
 };
 
-// A thread's eight chunks of 16 bytes of a stage's activation tiles: chunk index e = thread + 256 k of [2 tiles][rows][chunks].
-// down: a tile has 128 rows of 8 chunks, both 64 columns wide. outer: a tile has 64 rows and 2 x 8 chunks, 128 columns wide, as
-// two halves of 64 rows x 8 chunks.
-template <bool ACROSS>
-__device__ __forceinline__ void chunk_place(int e, uint32_t& row, uint32_t& chunk, uint32_t& at) {
-    if (ACROSS) {  // 32 chunks of a row are neighbours in memory
-        row = (uint32_t)e >> 5;
-        const uint32_t c = (uint32_t)e & 31u;
-        chunk = c;  // of 256 columns
-        at = (c >> 3) * 8192u + swizzled(row, c & 7u);
-    } else {
-        row = (uint32_t)e >> 3;
-        chunk = (uint32_t)e & 7u;
-        at = (row >> 7) * kTileBytes + swizzled(row & 127u, chunk);
-    }
-}
-
-// The sums of two tiles along `steps` stages: sums[r] of a thread is rank r of row 128 (warp / 4) + 32 (warp % 4) + lane of the 256.
-// ACROSS = false: 256 rows from row0 on, stages along the columns; true: 256 columns from column0 on, stages along the rows.
-template <bool VEC, bool ACROSS>
-__device__ __forceinline__ void sum_tiles(const Args& a, uint32_t worker, uint32_t row0, int column0, int first, int stride, int last, char* smem,
-                                          uint32_t memory, uint32_t bars, float (&sums)[kRank]) {
-    const int warp = threadIdx.x >> 5;
-    const __nv_bfloat16* x = (const __nv_bfloat16*)a.x + (int64_t)worker * a.x_ws;
-    const char* image = a.image + (int64_t)worker * a.image_ws;
-    const uint32_t call = drop_call(a.drop);
-    bool lost = false;  // a wait gave up
-    auto fetch = [&](int step, int stage) {
-        if (step < last) {
-            char* to = smem + stage * kStageBytes;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                uint32_t r, c, at;
-                chunk_place<ACROSS>(threadIdx.x + 256 * k, r, c, at);
-                const uint32_t row = ACROSS ? (uint32_t)step * 64 + r : row0 + r;
-                const int64_t col = (ACROSS ? (int64_t)column0 : (int64_t)step * 64) + c * 8;
-                const bool in = row < a.rows && col < a.h;
-                const __nv_bfloat16* from = in ? x + (int64_t)row * a.x_rs + col : (const __nv_bfloat16*)a.x;
-                if constexpr (VEC) {
-                    copy16(to + at, from, in);
-                } else {
-                    *reinterpret_cast<uint4*>(to + at) = raw_columns<__nv_bfloat16, false>(from - (in ? col : 0), (int)col, in ? a.h : 0).q;
-                }
-            }
-            const char* planes = image + (int64_t)step * kPlanesBytes;
-#pragma unroll
-            for (int k = 0; k < kPlanesBytes / 16 / 256; ++k)
-                copy16(to + 2 * kTileBytes + (threadIdx.x + 256 * k) * 16, planes + (threadIdx.x + 256 * k) * 16);
-        }
-        copies_commit();
-    };
-    auto mask = [&](int step, int stage) {  // the chunks that this thread copied
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            uint32_t r, c, at;
-            chunk_place<ACROSS>(threadIdx.x + 256 * k, r, c, at);
-            const uint32_t row = ACROSS ? (uint32_t)step * 64 + r : row0 + r;
-            const uint32_t group = (ACROSS ? (uint32_t)column0 / 8 : (uint32_t)step * 8) + c;
-            const uint4 u = drop_words(a.drop, group, row, a.drop.worker + worker, call);
-            uint4* place = reinterpret_cast<uint4*>(smem + stage * kStageBytes + at);
-            Raw8<__nv_bfloat16> raw = {*place};
-            uint32_t w[1][4];
-            raw_planes<__nv_bfloat16>(raw, a.drop, u, w);
-            *place = make_uint4(w[0][0], w[0][1], w[0][2], w[0][3]);
-        }
-    };
-    // the tiles' sums go from tensor memory to the registers, the planes' together
-    auto flush = [&]() {
-        const uint32_t at = memory + ((uint32_t)(warp & 3) << 21) + (uint32_t)(warp >> 2) * kN;
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            float part[32], v[32];
-            columns32(at + 2 * kRank + half * 32, part);
-            columns32(at + kRank + half * 32, v);
-#pragma unroll
-            for (int k = 0; k < 32; ++k) part[k] += v[k];
-            columns32(at + half * 32, v);
-#pragma unroll
-            for (int k = 0; k < 32; ++k) sums[half * 32 + k] += part[k] + v[k];
-        }
-    };
-#pragma unroll
-    for (int r = 0; r < kRank; ++r) sums[r] = 0.0f;
-    uint32_t done = 0, joined = 0;  // phases of the stages' barriers, a bit each, and of the flush's
-    for (int s = 0; s < kStages - 1; ++s) fetch(first + s * stride, s);
-    int stage = 0, since = 0, turn = 0;
-    for (int step = first; step < last; step += stride, ++turn) {
-        copies_wait<kStages - 2>();
-        if (a.drop.on) mask(step, stage);
-        fence_shared();
-        fence_before();
-        if (__syncthreads_or(lost)) break;
-        if (threadIdx.x == 0) {
-            fence_after();
-            const uint32_t tiles = shared_address(smem + stage * kStageBytes), planes = tiles + 2 * kTileBytes;
-#pragma unroll
-            for (int m = 0; m < 2; ++m)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {  // 16 of the 64
-                    const uint64_t left = ACROSS ? operand(tiles + m * kTileBytes + k * 2048, 8192) : operand(tiles + m * kTileBytes + k * 32, 16);
-                    product(memory + m * kN, left, operand(planes + k * 32, 16), instruction(kN, ACROSS, false), since > 0 || k > 0);
-                }
-            products_done(bars + 8 * stage);
-        }
-        // the stage before is free once its products are done, and is filled for the step after the next
-        const int behind = stage == 0 ? kStages - 1 : stage - 1;
-        if (turn > 0) {
-            lost |= !barrier_wait(bars + 8 * behind, done >> behind & 1u);
-            done ^= 1u << behind;
-        }
-        fetch(step + (kStages - 1) * stride, behind);
-        if (++since == kFlush || step + stride >= last) {
-            since = 0;
-            if (threadIdx.x == 0) products_done(bars + 8 * kStages);
-            lost |= !barrier_wait(bars + 8 * kStages, joined);
-            joined ^= 1u;
-            fence_after();
-            flush();
-        }
-        stage = stage + 1 == kStages ? 0 : stage + 1;
-    }
-    copies_wait<0>();
-    fence_before();
-    if (__syncthreads_or(lost) && threadIdx.x == 0) gave_up = 1;
-}
+// The barriers: a stage is full (256 threads' chunks and the planes), a stage is empty (its products are done); the sums are ready, the
+// sums are drained.
+enum : int { kFull = 0, kEmpty = kStages, kReady = 2 * kStages, kDrained = 2 * kStages + 1, kBars = 2 * kStages + 2 };
+constexpr int kThreads = 288;
 
 // Shared memory from its first 1024-byte boundary on, tensor memory and the barriers. The shared word that takes the address is the
 // caller's.
 __device__ __forceinline__ char* tensor_begin(char* smem, uint64_t* bars, uint32_t* word, uint32_t columns, uint32_t& memory) {
     if (threadIdx.x < 32) memory_alloc(shared_address(word), columns);
     if (threadIdx.x == 0) {
-        for (int k = 0; k <= kStages; ++k) barrier_init(shared_address(bars + k));
+        for (int k = 0; k < kBars; ++k)
+            barrier_init(shared_address(bars + k), k < kEmpty ? 257u : k == kDrained ? 256u : 1u);
         fence_shared();
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -343,33 +229,183 @@ __device__ __forceinline__ void tensor_end(uint32_t memory, uint32_t columns) {
     if (threadIdx.x < 32) memory_free(memory, columns);
 }
 
+// The ninth warp's part: planes and products of the steps first, first + stride, ... below last.
+template <bool ACROSS>
+__device__ __forceinline__ void issue_products_alone(const char* image, int first, int stride, int last, char* smem, uint32_t memory, uint32_t bars) {
+    bool lost = false;
+    auto planes = [&](int step, int stage) {
+        if (step >= last) return;
+        const uint32_t bar = bars + 8 * (kFull + stage);
+        mbar_expect(bar, kPlanesBytes);
+        bulk_load(smem + stage * kStageBytes + 2 * kTileBytes, image + (int64_t)step * kPlanesBytes, kPlanesBytes, bar);
+    };
+    for (int s = 0; s < kStages - 1; ++s) planes(first + s * stride, s);
+    int stage = 0, since = 0;
+    uint32_t full = 0, empty = 0, drained = 1;  // phases; nothing is to be drained at first
+    for (int step = first, turn = 0; step < last && !lost; step += stride, ++turn) {
+        if (since == 0) {
+            if (turn > 0) lost = !barrier_wait(bars + 8 * kDrained, drained);
+            drained ^= 1u;
+        }
+        lost = lost || !barrier_wait(bars + 8 * (kFull + stage), full >> stage & 1u);
+        full ^= 1u << stage;
+        if (lost) break;
+        fence_after();
+        const uint32_t tiles = shared_address(smem + stage * kStageBytes), right = tiles + 2 * kTileBytes;
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {  // 16 of the 64
+                const uint64_t left = ACROSS ? operand(tiles + m * kTileBytes + k * 2048, 8192) : operand(tiles + m * kTileBytes + k * 32, 16);
+                product(memory + m * kN, left, operand(right + k * 32, 16), instruction(kN, ACROSS, false), since > 0 || k > 0);
+            }
+        products_done(bars + 8 * (kEmpty + stage));
+        if (++since == kFlush || step + stride >= last) {
+            since = 0;
+            products_done(bars + 8 * kReady);
+        }
+        const int behind = stage == 0 ? kStages - 1 : stage - 1;
+        if (turn > 0) {
+            lost = !barrier_wait(bars + 8 * (kEmpty + behind), empty >> behind & 1u);
+            empty ^= 1u << behind;
+        }
+        if (!lost) planes(step + (kStages - 1) * stride, behind);
+        stage = stage + 1 == kStages ? 0 : stage + 1;
+    }
+    if (lost) gave_up = 1;
+}
+
+template <bool ACROSS>
+__device__ __forceinline__ void issue_products(const char* image, int first, int stride, int last, char* smem, uint32_t memory, uint32_t bars) {
+    if (threadIdx.x == 256) issue_products_alone<ACROSS>(image, first, stride, last, smem, memory, bars);
+    __syncwarp();
+}
+
+// The first eight warps' part: the sums of two tiles along the steps; sums[r] of a thread is rank r of row 128 (warp / 4) + 32 (warp % 4) +
+// lane of the 256. ACROSS = false: 256 rows from row0 on, steps of 64 along the columns; true: 256 columns from column0 on, steps of
+// 64 along the rows. A thread has a column of eight chunks, every 32nd row's (or 8th row's): its addresses are a start and a stride.
+template <bool VEC, bool ACROSS>
+__device__ __forceinline__ void sum_tiles(const Args& a, uint32_t worker, uint32_t row0, int column0, int first, int stride, int last, char* smem,
+                                          uint32_t memory, uint32_t bars, float (&sums)[kRank]) {
+    constexpr uint32_t kRows = ACROSS ? 8 : 32, kPlace = ACROSS ? 1024 : 4096;  // from one of a thread's chunks to the next
+    const int warp = threadIdx.x >> 5;
+    const uint32_t r0 = ACROSS ? threadIdx.x >> 5 : threadIdx.x >> 3, c0 = ACROSS ? threadIdx.x & 31u : threadIdx.x & 7u;
+    char* at0 = smem + (ACROSS ? (c0 >> 3) * 8192u + swizzled(r0, c0 & 7u) : swizzled(r0, c0));
+    const int64_t step_rows = ACROSS ? 64 : 0, step_columns = ACROSS ? 0 : 64;
+    const uint32_t row1 = (ACROSS ? 0 : row0) + r0;        // of step 0 and the first chunk
+    const int64_t column1 = (ACROSS ? column0 : 0) + (int64_t)c0 * 8;
+    const __nv_bfloat16* x = (const __nv_bfloat16*)a.x + (int64_t)worker * a.x_ws;
+    const uint32_t call = drop_call(a.drop);
+    bool lost = false;  // a wait gave up
+    auto fetch = [&](int step, int stage) {
+        if (step < last) {
+            const int64_t column = column1 + step * step_columns;
+            const uint32_t row = row1 + (uint32_t)(step * step_rows);
+            const __nv_bfloat16* from = x + (int64_t)row * a.x_rs + column;
+            const bool in = column < a.h;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const bool there = in && row + k * kRows < a.rows;
+                char* to = at0 + stage * kStageBytes + k * kPlace;
+                if constexpr (VEC) {
+                    copy16(to, there ? (const void*)(from + k * kRows * a.x_rs) : a.x, there);
+                } else {
+                    *reinterpret_cast<uint4*>(to) = raw_columns<__nv_bfloat16, false>(
+                        there ? from + k * kRows * a.x_rs - column : (const __nv_bfloat16*)a.x, (int)column, there ? a.h : 0).q;
+                }
+            }
+        }
+        copies_commit();
+    };
+    auto mask = [&](int step, int stage) {  // the chunks that this thread copied
+        const uint32_t row = row1 + (uint32_t)(step * step_rows), group = (uint32_t)((column1 + step * step_columns) >> 3);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const uint4 u = drop_words(a.drop, group, row + k * kRows, a.drop.worker + worker, call);
+            uint4* place = reinterpret_cast<uint4*>(at0 + stage * kStageBytes + k * kPlace);
+            const Raw8<__nv_bfloat16> raw = {*place};
+            uint32_t w[1][4];
+            raw_planes<__nv_bfloat16>(raw, a.drop, u, w);
+            *place = make_uint4(w[0][0], w[0][1], w[0][2], w[0][3]);
+        }
+    };
+    // the tiles' sums go from tensor memory to the registers, the planes' together
+    auto flush = [&]() {
+        const uint32_t at = memory + ((uint32_t)(warp & 3) << 21) + (uint32_t)(warp >> 2) * kN;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            float v[32], w[32];
+            columns32(at + 2 * kRank + half * 32, v);
+            columns32(at + kRank + half * 32, w);
+            columns_wait(v);
+            columns_wait(w);
+#pragma unroll
+            for (int k = 0; k < 32; ++k) w[k] += v[k];
+            columns32(at + half * 32, v);
+            columns_wait(v);
+#pragma unroll
+            for (int k = 0; k < 32; ++k) sums[half * 32 + k] += v[k] + w[k];
+        }
+    };
+#pragma unroll
+    for (int r = 0; r < kRank; ++r) sums[r] = 0.0f;
+    for (int s = 0; s < kStages - 1; ++s) fetch(first + s * stride, s);
+    int stage = 0, since = 0;
+    uint32_t empty = 0, ready = 0;  // phases
+    for (int step = first, turn = 0; step < last; step += stride, ++turn) {
+        copies_wait<kStages - 2>();
+        if (a.drop.on) mask(step, stage);
+        fence_shared();
+        barrier_arrive(bars + 8 * (kFull + stage));
+        // the stage before is free once its products are done
+        const int behind = stage == 0 ? kStages - 1 : stage - 1;
+        if (turn > 0) {
+            lost = lost || !barrier_wait(bars + 8 * (kEmpty + behind), empty >> behind & 1u);
+            empty ^= 1u << behind;
+        }
+        fetch(step + (kStages - 1) * stride, behind);
+        if (++since == kFlush || step + stride >= last) {
+            since = 0;
+            lost = lost || !barrier_wait(bars + 8 * kReady, ready);
+            ready ^= 1u;
+            fence_after();
+            flush();
+            fence_before();
+            barrier_arrive(bars + 8 * kDrained);
+        }
+        stage = stage + 1 == kStages ? 0 : stage + 1;
+    }
+    copies_wait<0>();
+    if (lost) gave_up = 1;
+}
+
 // A CTA takes 256 rows of a worker and its share of the columns.
 template <bool VEC>
-__global__ void __launch_bounds__(256, 1) down_kernel(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(kThreads, 1) down_kernel(const __grid_constant__ Args a) {
     extern __shared__ __align__(16) char dynamic[];
-    __shared__ uint64_t bars[kStages + 1];
+    __shared__ uint64_t bars[kBars];
     __shared__ uint32_t word;
     dependency_wait();
     uint32_t memory;
     char* smem = tensor_begin(dynamic, bars, &word, kColumns, memory);
     const uint32_t tile = blockIdx.x / a.split, i = tile / a.tiles, row0 = (tile - i * a.tiles) * 256;
     const int part = (int)(blockIdx.x - tile * a.split), steps = (a.h + 63) / 64;
+    const bool main = threadIdx.x < 256;
     float sums[kRank];
-    sum_tiles<VEC, false>(a, i, row0, 0, part, a.split, steps, smem, memory, shared_address(bars), sums);
+    if (main) sum_tiles<VEC, false>(a, i, row0, 0, part, a.split, steps, smem, memory, shared_address(bars), sums);
+    else issue_products<false>(a.image + (int64_t)i * a.image_ws, part, a.split, steps, smem, memory, shared_address(bars));
     tensor_end(memory, kColumns);
     // this CTA's sums, then its share of the rows, joined over the cluster in order
     constexpr int L = kRank + 1;
     float *mine = reinterpret_cast<float*>(smem), *whole = mine + 256 * L;
-    {
-        float* at = mine + ((threadIdx.x >> 7) * 128 + (threadIdx.x & 127)) * L;
+    if (main)
 #pragma unroll
-        for (int r = 0; r < kRank; ++r) at[r] = sums[r];
-    }
+        for (int r = 0; r < kRank; ++r) mine[threadIdx.x * L + r] = sums[r];
     cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
     cluster.sync();
     const float scale = a.scale * (a.drop.on ? a.drop.factor : 1.0f);
     const int share = 256 / a.split, from = part * share;  // split is a power of two up to 4: a share is 64 rows at least
-    for (int e = threadIdx.x; e < share * kRank; e += 256) {
+    for (int e = threadIdx.x; e < share * kRank; e += kThreads) {
         const int r = e / kRank, j = e % kRank;
         float v = 0.0f;
         for (int s = 0; s < a.split; ++s) v += cluster.map_shared_rank(mine, s)[(from + r) * L + j];
@@ -378,11 +414,11 @@ __global__ void __launch_bounds__(256, 1) down_kernel(const __grid_constant__ Ar
     __syncthreads();
     const uint32_t first = row0 + from;  // a multiple of 64
     if (a.out)
-        for (int e = threadIdx.x; e < share * kRank; e += 256) {
+        for (int e = threadIdx.x; e < share * kRank; e += kThreads) {
             const int r = e / kRank, j = e % kRank;
             if (first + r < a.rows && j < a.rank) a.out[((int64_t)i * a.rows + first + r) * a.rank + j] = whole[r * L + j];
         }
-    for (int e = threadIdx.x; e < share * 8; e += 256) {  // a row's eight ranks
+    for (int e = threadIdx.x; e < share * 8; e += kThreads) {  // a row's eight ranks
         const int r = e >> 3, c = e & 7;
         const uint32_t row = first + r;
         if (row >= (a.rows + 127) / 128 * 128) break;
@@ -396,7 +432,7 @@ __global__ void __launch_bounds__(256, 1) down_kernel(const __grid_constant__ Ar
         *reinterpret_cast<uint4*>(out + kTileBytes) = w[1];
     }
     if (a.t_outer)
-        for (int e = threadIdx.x; e < share * 8; e += 256) {  // a rank's eight rows
+        for (int e = threadIdx.x; e < share * 8; e += kThreads) {  // a rank's eight rows
             const int j = e & 63, r = (e >> 6) * 8;
             const uint32_t row = first + r;
             if (row >= (a.rows + 63) / 64 * 64) break;
@@ -414,9 +450,9 @@ __global__ void __launch_bounds__(256, 1) down_kernel(const __grid_constant__ Ar
 
 // A CTA takes 256 columns and a chunk of a worker's rows.
 template <bool VEC>
-__global__ void __launch_bounds__(256, 1) outer_kernel(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(kThreads, 1) outer_kernel(const __grid_constant__ Args a) {
     extern __shared__ __align__(16) char dynamic[];
-    __shared__ uint64_t bars[kStages + 1];
+    __shared__ uint64_t bars[kBars];
     __shared__ uint32_t word;
     dependency_wait();
     uint32_t memory;
@@ -424,10 +460,11 @@ __global__ void __launch_bounds__(256, 1) outer_kernel(const __grid_constant__ A
     const uint32_t i = blockIdx.y / a.chunks, chunk = blockIdx.y - i * a.chunks, blocks = (a.rows + 63) / 64;
     const int s0 = (int)((uint64_t)blocks * chunk / a.chunks), s1 = (int)((uint64_t)blocks * (chunk + 1) / a.chunks);
     float sums[kRank];
-    sum_tiles<VEC, true>(a, i, 0, (int)blockIdx.x * 256, s0, 1, s1, smem, memory, shared_address(bars), sums);
+    if (threadIdx.x < 256) sum_tiles<VEC, true>(a, i, 0, (int)blockIdx.x * 256, s0, 1, s1, smem, memory, shared_address(bars), sums);
+    else issue_products<true>(a.image + (int64_t)i * a.image_ws, s0, 1, s1, smem, memory, shared_address(bars));
     tensor_end(memory, kColumns);
     const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (c >= a.h) return;
+    if (threadIdx.x >= 256 || c >= a.h) return;
     const float scale = a.scale * (a.drop.on ? a.drop.factor : 1.0f);
     float* out = a.out + (int64_t)blockIdx.y * a.rank * a.h + c * a.sc;
     if (a.sj == 1 && (a.rank & 3) == 0 && (reinterpret_cast<uintptr_t>(a.out) & 15u) == 0) {
@@ -446,7 +483,8 @@ __global__ void __launch_bounds__(256, 1) outer_kernel(const __grid_constant__ A
 
 // A CTA takes 128 columns, whose planes of the factor stay in shared memory, and goes through the 128-row tiles of a chunk: the tile's
 // planes of t and of the base by copies, 12 products of 16 rank indices (the planes' indices together at most 1), the
-// result into the base's place in shared memory and from there to memory by rows. Two CTAs of an SM keep memory and tensor cores busy.
+// result into the base's place in shared memory and from there to memory by rows. Behind the products t's place is free for the next base,
+// which is on its way during the rest of the tile, and behind the stores the tile's place for the next t. Two CTAs to an SM.
 constexpr int kUpShared = 1024 + 2 * 2 * kTileBytes + 2 * kTileBytes;
 constexpr uint32_t kUpColumns = 128;
 
@@ -464,46 +502,43 @@ struct UpArgs {
 template <bool VEC>
 __global__ void __launch_bounds__(256, 2) up_kernel(const __grid_constant__ UpArgs a) {
     extern __shared__ __align__(16) char dynamic[];
-    __shared__ uint64_t bars[kStages + 1];
+    __shared__ uint64_t bars[kBars];
     __shared__ uint32_t word;
     bool lost = false;  // a wait gave up
     dependency_wait();
     uint32_t memory;
     char* smem = tensor_begin(dynamic, bars, &word, kUpColumns, memory);
-    char *planes = smem, *t = smem + 2 * kTileBytes, *tile = smem + 4 * kTileBytes;  // tile: 128 rows of 16 chunks, chunk c at c ^ (row % 8)
+    // tile: 128 rows of 16 chunks, chunk c at c ^ (row % 8)
+    char *planes = smem, *t = smem + 2 * kTileBytes, *tile = smem + 4 * kTileBytes;
     const uint32_t i = blockIdx.y / a.chunks, chunk = blockIdx.y - i * a.chunks, blocks = (a.rows + 127) / 128;
     const uint32_t b0 = (uint32_t)((uint64_t)blocks * chunk / a.chunks), b1 = (uint32_t)((uint64_t)blocks * (chunk + 1) / a.chunks);
     const int c0 = (int)blockIdx.x * 128, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t call = drop_call(a.drop), bar = shared_address(bars);
+    const uint32_t call = drop_call(a.drop), bar = shared_address(bars + kReady);
     auto linear = [&](char* to, const char* from) {  // two planes
 #pragma unroll
         for (int k = 0; k < 2 * kTileBytes / 16 / 256; ++k) copy16(to + (threadIdx.x + 256 * k) * 16, from + (threadIdx.x + 256 * k) * 16);
     };
-    auto place = [&](int e, uint32_t& row, int& col) {  // of a thread's chunk of the tile
-        row = (uint32_t)e >> 4;
-        const uint32_t c = (uint32_t)e & 15u;
-        col = c0 + (int)c * 8;
-        return tile + row * 256u + ((c ^ (row & 7u)) << 4);
-    };
-    auto fetch_base = [&](uint32_t b) {
+    // a thread has a column of eight chunks of a tile, every 16th row's
+    const uint32_t r0 = threadIdx.x >> 4, at0 = r0 * 256u + (((threadIdx.x & 15u) ^ (r0 & 7u)) << 4);
+    const int column = c0 + (int)(threadIdx.x & 15u) * 8;
+    const __nv_bfloat16* base = (const __nv_bfloat16*)a.base + (int64_t)i * a.base_ws + column;
+    __nv_bfloat16* y = (__nv_bfloat16*)a.y + (int64_t)i * a.rows * a.h + column;
+    auto fetch_base = [&](uint32_t b, char* tile) {
         if (!a.base) return;
+        const __nv_bfloat16* from = base + (int64_t)(b * 128 + r0) * a.base_rs;
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            uint32_t r;
-            int col;
-            char* to = place(threadIdx.x + 256 * k, r, col);
-            const uint32_t row = b * 128 + r;
-            const bool in = row < a.rows && col < a.h;
-            const __nv_bfloat16* from = (const __nv_bfloat16*)a.base + (in ? (int64_t)i * a.base_ws + (int64_t)row * a.base_rs : 0);
-            if constexpr (VEC) copy16(to, from + (in ? col : 0), in);
-            else *reinterpret_cast<uint4*>(to) = raw_columns<__nv_bfloat16, false>(from, col, in ? a.h : 0).q;
+            const bool in = column < a.h && b * 128 + r0 + 16 * k < a.rows;
+            if constexpr (VEC) copy16(tile + at0 + k * 4096, in ? (const void*)(from + k * 16 * a.base_rs) : a.base, in);
+            else *reinterpret_cast<uint4*>(tile + at0 + k * 4096) = raw_columns<__nv_bfloat16, false>(
+                     in ? from + k * 16 * a.base_rs - column : (const __nv_bfloat16*)a.base, column, in ? a.h : 0).q;
         }
     };
     const char* t_image = a.t_up + i * t_up_image(a.rows);
     linear(planes, a.image + (int64_t)i * a.image_ws + (int64_t)blockIdx.x * (2 * kTileBytes));
     if (b0 < b1) {
         linear(t, t_image + (int64_t)b0 * (2 * kTileBytes));
-        fetch_base(b0);
+        fetch_base(b0, tile);
     }
     copies_commit();
     uint32_t phase = 0;
@@ -527,7 +562,7 @@ __global__ void __launch_bounds__(256, 2) up_kernel(const __grid_constant__ UpAr
         lost |= !barrier_wait(bar, phase);
         phase ^= 1u;
         fence_after();
-        if (b + 1 < b1) linear(t, t_image + (int64_t)(b + 1) * (2 * kTileBytes));
+        if (b + 1 < b1) fetch_base(b + 1, t);
         // a lane's row: 64 columns from 64 (warp / 4) on
         const uint32_t r = (uint32_t)(warp & 3) * 32 + lane, row = b * 128 + r;
 #pragma unroll
@@ -535,6 +570,7 @@ __global__ void __launch_bounds__(256, 2) up_kernel(const __grid_constant__ UpAr
             const int first = (warp >> 2) * 64 + half * 32;
             float v[32];
             columns32(memory + ((uint32_t)(warp & 3) << 21) + first, v);
+            columns_wait(v);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const uint32_t c = (uint32_t)(first >> 3) + k;
@@ -553,26 +589,27 @@ __global__ void __launch_bounds__(256, 2) up_kernel(const __grid_constant__ UpAr
             if (threadIdx.x == 0) gave_up = 1;
             break;
         }
+        __nv_bfloat16* to = y + (int64_t)(b * 128 + r0) * a.h;
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            uint32_t q;
-            int col;
-            const uint4 u = *reinterpret_cast<const uint4*>(place(threadIdx.x + 256 * k, q, col));
-            if (b * 128 + q >= a.rows || col >= a.h) continue;
-            __nv_bfloat16* to = (__nv_bfloat16*)a.y + ((int64_t)i * a.rows + b * 128 + q) * a.h + col;
+            const uint4 u = *reinterpret_cast<const uint4*>(tile + at0 + k * 4096);
+            if (b * 128 + r0 + 16 * k >= a.rows || column >= a.h) continue;
             if (VEC) {
-                *reinterpret_cast<uint4*>(to) = u;
+                *reinterpret_cast<uint4*>(to + (int64_t)k * 16 * a.h) = u;
             } else {
                 __nv_bfloat16 s[8];
                 memcpy(s, &u, sizeof(s));
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    if (col + e < a.h) to[e] = s[e];
+                    if (column + e < a.h) to[(int64_t)k * 16 * a.h + e] = s[e];
             }
         }
-        // (a thread fills the chunks that it has just read)
-        if (b + 1 < b1) fetch_base(b + 1);
+        __syncthreads();
+        if (b + 1 < b1) linear(tile, t_image + (int64_t)(b + 1) * (2 * kTileBytes));
         copies_commit();
+        char* other = t;
+        t = tile;
+        tile = other;
     }
     copies_wait<0>();
     tensor_end(memory, kUpColumns);
