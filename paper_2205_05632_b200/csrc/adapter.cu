@@ -951,7 +951,7 @@ bool few(const AdapterShape& z) { return z.rows <= kFewRows; }
 
 // Whether the products run on tcgen05.mma.
 bool on_tensor(const AdapterShape& z, int32_t type) {
-    return type == kTypeBF16 && z.rank > tensor::kRank / 2 && z.rank <= tensor::kRank && z.rows >= 64;
+    return type == kTypeBF16 && z.rank <= tensor::kMostRank && z.rows >= 64;
 }
 
 // The number of parts, of 1 ... most, at which the slowest of `slots` places ends first: waves of tiles * parts CTAs, each a part's
@@ -1042,52 +1042,99 @@ AdapterArgs arguments(const AdapterShape& z, Rows x, int64_t h, const Low& low, 
     return a;
 }
 
+template <typename F>
+int by_rank(const AdapterShape& z, F f) {
+    const int r = tensor::padded_rank(z.rank);
+    return r == 16 ? f(Int<16>()) : r == 32 ? f(Int<32>()) : f(Int<64>());
+}
+
+// A map of x for boxes of 64 columns and `box` rows, in the 128-byte swizzle; false where TMA cannot address x.
+bool box_map(CUtensorMap* map, Rows x, const AdapterShape& z, int64_t h, uint32_t box) {
+    *map = {};
+    if (h % 8 != 0 || !x.aligned() || x.row_stride < h || (z.n > 1 && x.worker_stride < 1) || x.row_stride >= (int64_t)1 << 38 ||
+        x.worker_stride >= (int64_t)1 << 38)
+        return false;
+    // the encoder is the driver's; it is asked for once
+    using Encode = decltype(&cuTensorMapEncodeTiled);
+    static const Encode encode = [] {
+        void* f = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess)
+            f = nullptr;
+        return (Encode)f;
+    }();
+    if (!encode) return false;
+    const cuuint64_t size[3] = {(cuuint64_t)h, (cuuint64_t)z.rows, (cuuint64_t)z.n};
+    const cuuint64_t stride[2] = {(cuuint64_t)x.row_stride * 2, (cuuint64_t)(z.n > 1 ? x.worker_stride : x.row_stride * z.rows) * 2};
+    const cuuint32_t extent[3] = {64, box, 1}, every[3] = {1, 1, 1};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(x.p), size, stride, extent, every, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // The three products on tcgen05.mma; the images stand where the fragments do.
 int tensor_prepare(const AdapterShape& z, bool shared, Factor down, int64_t down_h, void* down_image, Factor up, int64_t up_h, void* up_image,
                    const float* t, void* t_image, cudaStream_t stream) {
     tensor::PrepareArgs p = {down, up, (char*)down_image, (char*)up_image, t, (char*)t_image, (int32_t)down_h, (int32_t)up_h, z.rank,
                              (uint32_t)z.rows, 0, 0, 0, shared};
-    if (down_image) p.down_count = (uint32_t)((down_h + 63) / 64 * 512);
-    if (up_image) p.up_count = (uint32_t)((up_h + 127) / 128 * 1024);
-    if (t_image) p.t_count = (uint32_t)((z.rows + 63) / 64 * 512);
+    const int r = tensor::padded_rank(z.rank);
+    if (down_image) p.down_count = (uint32_t)((down_h + 63) / 64 * 8 * r);
+    if (up_image) p.up_count = (uint32_t)((up_h + 127) / 128 * 16 * r);
+    if (t_image) p.t_count = (uint32_t)((z.rows + 63) / 64 * 8 * r);
     const uint64_t ctas = ((uint64_t)p.down_count + p.up_count + p.t_count + 255) / 256;
     if (ctas > 0x00ffffffu) return COMPAMS_ERR_TOO_LARGE;
     const uint32_t workers = shared && !t_image ? 1 : (uint32_t)z.n;
-    return launched(launch_next(tensor::prepare_kernel, dim3((uint32_t)ctas, workers), 1, 0, true, stream, p), "adapter_prepare");
+    return by_rank(z, [&](auto v) {
+        return launched(launch_next(tensor::prepare_kernel<decltype(v)::value>, dim3((uint32_t)ctas, workers), 1, 0, true, stream, p), "adapter_prepare");
+    });
 }
 
 int tensor_down(Low low, Rows x, const AdapterShape& z, int64_t h, bool shared, const uint4* image, float scale, const Drop& d,
                 cudaStream_t stream) {
     tensor::Args a = {};
-    a.x = x.p; a.x_ws = x.worker_stride; a.x_rs = x.row_stride; a.image = (const char*)image; a.image_ws = shared ? 0 : tensor::down_image(h);
+    a.x = x.p; a.x_ws = x.worker_stride; a.x_rs = x.row_stride; a.image = (const char*)image; a.image_ws = shared ? 0 : tensor::down_image(h, z.rank);
     a.t_up = (char*)low.up; a.t_outer = (char*)low.outer; a.out = low.t; a.rows = (uint32_t)z.rows; a.h = (int32_t)h; a.rank = z.rank;
     a.tiles = (a.rows + 255) / 256; a.scale = scale; a.drop = d;
     a.split = (int32_t)parts_of((int64_t)a.tiles * z.n, 148, (h + 63) / 64, 4.0, 4, true);
     const uint64_t ctas = (uint64_t)a.tiles * z.n * a.split;
     if (ctas > 0x7fffffffu) return COMPAMS_ERR_TOO_LARGE;
-    auto kernel = h % 8 == 0 && x.aligned() ? tensor::down_kernel<true> : tensor::down_kernel<false>;
-    return launched(launch_sized(kernel, dim3((uint32_t)ctas), tensor::kThreads, a.split, tensor::kShared, false, stream, a), "adapter_down");
+    return by_rank(z, [&](auto v) {
+        constexpr int R = decltype(v)::value;
+        CUtensorMap map;
+        auto kernel = box_map(&map, x, z, h, 128) ? tensor::down_kernel<R, true> : tensor::down_kernel<R, false>;
+        return launched(launch_sized(kernel, dim3((uint32_t)ctas), tensor::kThreads, a.split, tensor::By<R>::kShared, false, stream, a, map),
+                        "adapter_down");
+    });
 }
 
 int tensor_up(void* y, Rows base, Low low, const AdapterShape& z, int64_t h, bool shared, const uint4* image, float scale, const Drop& d,
               cudaStream_t stream) {
     tensor::UpArgs a = {};
     a.base = base.p; a.y = y; a.image = (const char*)image; a.t_up = (const char*)low.up; a.base_ws = base.worker_stride;
-    a.base_rs = base.row_stride; a.image_ws = shared ? 0 : tensor::up_image(h); a.rows = (uint32_t)z.rows; a.h = (int32_t)h; a.scale = scale;
+    a.base_rs = base.row_stride; a.image_ws = shared ? 0 : tensor::up_image(h, z.rank); a.rows = (uint32_t)z.rows; a.h = (int32_t)h; a.scale = scale;
     a.drop = d;
-    const int64_t columns = (h + 127) / 128, blocks = (z.rows + 127) / 128;
+    const int64_t wide = tensor::padded_rank(z.rank) == 64 ? tensor::up_columns<64>() : tensor::up_columns<16>();
+    const int64_t columns = (h + wide - 1) / wide, blocks = (z.rows + 127) / 128;
     a.chunks = (uint32_t)parts_of(columns * z.n, 2 * 148, blocks, 0.5, 65535 / z.n, false);
     const bool vec = h % 8 == 0 && (!base.p || base.aligned()) && packed(y, z.rows, h, base.type).aligned();
-    auto kernel = vec ? tensor::up_kernel<true> : tensor::up_kernel<false>;
-    return launched(launch_next(kernel, dim3((uint32_t)columns, (uint32_t)z.n * a.chunks), 1, tensor::kUpShared, false, stream, a), "adapter_up");
+    return by_rank(z, [&](auto v) {
+        constexpr int R = decltype(v)::value;
+        auto kernel = vec ? tensor::up_kernel<R, true> : tensor::up_kernel<R, false>;
+        return launched(launch_next(kernel, dim3((uint32_t)columns, (uint32_t)z.n * a.chunks), 1, tensor::up_shared<R>(), false, stream, a), "adapter_up");
+    });
 }
 
-cudaError_t tensor_outer(AdapterArgs& b, Rows x, Low low, const AdapterShape& z, int64_t h, bool first, cudaStream_t stream) {
+int tensor_outer(const AdapterArgs& b, Rows x, Low low, const AdapterShape& z, int64_t h, bool first, cudaStream_t stream) {
     tensor::Args a = {};
-    a.x = b.x; a.x_ws = b.x_ws; a.x_rs = b.x_rs; a.image = (const char*)low.outer; a.image_ws = tensor::t_outer_image(z.rows); a.out = b.out;
+    a.x = b.x; a.x_ws = b.x_ws; a.x_rs = b.x_rs; a.image = (const char*)low.outer; a.image_ws = tensor::t_outer_image(z.rows, z.rank); a.out = b.out;
     a.sj = b.f.sj; a.sc = b.f.sc; a.rows = b.rows; a.h = b.h; a.rank = b.rank; a.chunks = b.chunks; a.scale = b.scale; a.drop = b.drop;
-    auto kernel = h % 8 == 0 && x.aligned() ? tensor::outer_kernel<true> : tensor::outer_kernel<false>;
-    return launch_sized(kernel, dim3((uint32_t)((h + 255) / 256), (uint32_t)z.n * a.chunks), tensor::kThreads, 1, tensor::kShared, first, stream, a);
+    return by_rank(z, [&](auto v) {
+        constexpr int R = decltype(v)::value;
+        CUtensorMap map;
+        auto kernel = box_map(&map, x, z, h, 64) ? tensor::outer_kernel<R, true> : tensor::outer_kernel<R, false>;
+        return launched(launch_sized(kernel, dim3((uint32_t)((h + 255) / 256), (uint32_t)z.n * a.chunks), tensor::kThreads, 1, tensor::By<R>::kShared,
+                                     first, stream, a, map),
+                        "adapter_outer");
+    });
 }
 
 int prepare(const AdapterShape& z, bool shared, Factor down, int64_t down_h, uint4* down_frag, Factor up, int64_t up_h, uint4* up_frag,
@@ -1200,7 +1247,7 @@ int outer(float* out, bool sum_workers, Rows x, Low low, const AdapterShape& z, 
         if (few(z))
             return launched(launch_next(adapter_outer_few_kernel<T>, dim3((uint32_t)((h + 255) / 256), (uint32_t)z.n), 1, 0, first, stream, a),
                             "adapter_outer");
-        if (on_tensor(z, x.type)) return launched(tensor_outer(a, x, low, z, h, first, stream), "adapter_outer");
+        if (on_tensor(z, x.type)) return tensor_outer(a, x, low, z, h, first, stream);
         const int nt = group_tiles(z.rank);
         const uint64_t tiles = (uint64_t)((h + kOuterColumns - 1) / kOuterColumns) * rank_groups(z.rank);
         if (tiles > 0x7fffffffu) return (int)COMPAMS_ERR_TOO_LARGE;
@@ -1245,13 +1292,13 @@ Places places(const AdapterShape& z, bool shared, bool backward, bool sum_worker
     auto either = [&](int64_t words, int64_t image) { return words * 16 > image ? words * 16 : image; };
     const int64_t dh = backward ? z.out : z.in, uh = backward ? z.in : z.out;
     if (frags) {
-        p.down = take(factors * either(down_frag_words(dh, z.rank), tensor::down_image(dh)));
-        p.up = take(factors * either(up_frag_words(uh, z.rank), tensor::up_image(uh)));
-        p.t_up = take(z.n * either(t_up_words(z.rows, z.rank, kPlanes), tensor::t_up_image(z.rows)));
+        p.down = take(factors * either(down_frag_words(dh, z.rank), tensor::down_image(dh, z.rank)));
+        p.up = take(factors * either(up_frag_words(uh, z.rank), tensor::up_image(uh, z.rank)));
+        p.t_up = take(z.n * either(t_up_words(z.rows, z.rank, kPlanes), tensor::t_up_image(z.rows, z.rank)));
     }
     if (frags && backward) {
-        p.t_outer = take(z.n * either(t_outer_words(z.rows, z.rank), tensor::t_outer_image(z.rows)));
-        p.saved = take(z.n * either(t_outer_words(z.rows, z.rank), tensor::t_outer_image(z.rows)));
+        p.t_outer = take(z.n * either(t_outer_words(z.rows, z.rank), tensor::t_outer_image(z.rows, z.rank)));
+        p.saved = take(z.n * either(t_outer_words(z.rows, z.rank), tensor::t_outer_image(z.rows, z.rank)));
     }
     p.t = take(backward && !frags ? (int64_t)z.total() * z.rank * 4 : 0);
     int64_t most = 0;

@@ -1,16 +1,21 @@
-// The adapters' three products on tcgen05.mma, for bfloat16 activations and ranks from 33 to 64, where mma.sync is bound by its own
-// rate (550 TFLOP/s measured, a third of tcgen05's) instead of by memory.
+// The adapters' three products on tcgen05.mma, for bfloat16 activations and ranks up to 64. mma.sync is bound by its own rate (550
+// TFLOP/s measured, a third of tcgen05's) from about rank 32 on, and below by the instructions that bring operands to registers.
 //
-// The planes of an fp32 operand are stacked along N: a tile of an activation, 128 x 64, is multiplied by [3 x 64] rows of planes at once, so
+// The planes of an fp32 operand are stacked along N: a tile of an activation, 128 x 64, is multiplied by [3 x R] rows of planes at once (R: the rank, padded to 16, 32 or 64), so
 // it is an operand once and the planes' sums stand beside each other in tensor memory. Operands lie in shared memory in the
 // 128-byte swizzle: rows of 128 bytes (64 elements), whose 16-byte chunk c lies at chunk c ^ (row % 8). down: the rows are the activation's
 // and the sum runs along them (K-major); outer: the sum runs over the rows, the tile is read across them (MN-major), and t
 // comes turned, [plane, rank][row].
 //
-// 256 threads copy (cp.async straight into the swizzle; where dropout masks an activation the thread that copied a chunk does so in place), a
-// thread of a ninth warp copies the planes in bulk and issues the products; mbarriers pass the stages between them. The tensor cores cut
-// their sums, so after every kFlush tiles of 64 the sums go to fp32 registers by rounded additions.
+// One thread of a ninth warp brings the tiles (TMA, into the swizzle; the planes, already in its order, in bulk) and issues the products; it
+// waits for nobody else unless dropout masks the activation, which the 256 threads of the other warps do in place. (With tiles copied by
+// all threads, cp.async and a fence to the tensor cores' proxy for each, a stage took 1 us however many were under way: the fence
+// waits for all of a thread's copies.) The tensor cores cut their sums, so after every kFlush tiles of 64 the sums go to fp32 registers by
+// rounded additions, which is the other warps' work. Activations that TMA cannot address (odd widths, other strides) are
+// brought by these warps, element by element.
 #pragma once
+
+#include <cuda.h>  // CUtensorMap
 
 #include "rows.cuh"
 
@@ -18,24 +23,38 @@ namespace compams {
 namespace {
 namespace tensor {
 
-constexpr int kRank = 64;                  // rank indices, padded
-constexpr int kN = 3 * kRank;              // planes side by side
+constexpr int kMostRank = 64;
 constexpr int kTileBytes = 128 * 128;      // 128 rows of 64 elements, or 64 rows of 128
-constexpr int kPlanesBytes = kN * 128;     // planes: 192 rows of 64 elements
-constexpr int kStageBytes = 2 * kTileBytes + kPlanesBytes;
-constexpr int kStages = 4;
 constexpr int kFlush = 8;                  // tiles between two additions to the registers
-constexpr int kShared = 1024 + kStages * kStageBytes;
-constexpr uint32_t kColumns = 512;         // of tensor memory: 2 x 192 used, a power of two taken
+
+// What goes by the padded rank.
+__host__ __device__ inline int padded_rank(int rank) { return rank <= 16 ? 16 : rank <= 32 ? 32 : 64; }
+template <int R>
+struct By {
+    static constexpr int kN = 3 * R;                       // planes side by side
+    static constexpr int kPlanesBytes = kN * 128;          // planes: rows of 64 elements
+    static constexpr int kStageBytes = 2 * kTileBytes + kPlanesBytes;
+    static constexpr int kStages = R == 64 ? 4 : 5;        // what 227 KB hold
+    static constexpr int kShared = 1024 + kStages * kStageBytes;
+    static constexpr uint32_t kColumns = R == 64 ? 512 : R == 32 ? 256 : 128;  // of tensor memory: 2 kN used, a power of two taken
+    // up: two planes of 128 rows; up to 32 they share the rows' 128 bytes
+    static constexpr int kUpTiles = R == 64 ? 2 : 1, kUpBytes = kUpTiles * kTileBytes;
+    static constexpr uint32_t kUpPlane = R == 64 ? kTileBytes : 2 * R;  // from plane 0 to plane 1
+    // The barriers: what is brought to a stage has landed; 256 threads have done their part on it; its products are done; the sums are
+    // ready, and drained.
+    static constexpr int kLanded = 0, kTouched = kStages, kEmpty = 2 * kStages, kReady = 3 * kStages, kDrained = 3 * kStages + 1,
+                         kBars = 3 * kStages + 2;
+};
 
 // ---- images of the fp32 operands in global memory, in the order of shared memory --------------------------------------------
 
-// A factor for down: [64 columns][plane, rank][64 columns]; for up: [128 columns][plane 0, 1][column][rank]; bytes of a worker's.
-__host__ __device__ inline int64_t down_image(int64_t h) { return (h + 63) / 64 * kPlanesBytes; }
-__host__ __device__ inline int64_t up_image(int64_t h) { return (h + 127) / 128 * (2 * kTileBytes); }
-// t for outer: [64 rows][plane, rank][row]; for up: [128 rows][plane 0, 1][row][rank].
-__host__ __device__ inline int64_t t_outer_image(int64_t rows) { return (rows + 63) / 64 * kPlanesBytes; }
-__host__ __device__ inline int64_t t_up_image(int64_t rows) { return (rows + 127) / 128 * (2 * kTileBytes); }
+// A factor for down: [64 columns][plane, rank][64 columns]; for up: [128 columns][plane 0, 1][column][rank] (the planes within a column's
+// 128 bytes up to 32 ranks); bytes of a worker's.
+__host__ __device__ inline int64_t down_image(int64_t h, int rank) { return (h + 63) / 64 * (3 * 128 * padded_rank(rank)); }
+__host__ __device__ inline int64_t up_image(int64_t h, int rank) { return (h + 127) / 128 * (kTileBytes << (padded_rank(rank) == 64)); }
+// t for outer: [64 rows][plane, rank][row]; for up: [128 rows], as a factor's columns.
+__host__ __device__ inline int64_t t_outer_image(int64_t rows, int rank) { return down_image(rows, rank); }
+__host__ __device__ inline int64_t t_up_image(int64_t rows, int rank) { return up_image(rows, rank); }
 
 __device__ __forceinline__ uint32_t swizzled(uint32_t row, uint32_t chunk) { return row * 128u + ((chunk ^ (row & 7u)) << 4); }
 
@@ -85,25 +104,33 @@ __device__ __forceinline__ void product(uint32_t d, uint64_t a, uint64_t b, uint
 __device__ __forceinline__ void products_done(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
-// 32 columns of a lane's row.
-__device__ __forceinline__ void columns32(uint32_t at, float (&v)[32]) {
-    uint32_t r[32];
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,"
-        "%26,%27,%28,%29,%30,%31}, [%32];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
-          "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
-          "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]),
-          "=r"(r[31])
-        : "r"(at));
-#pragma unroll
-    for (int k = 0; k < 32; ++k) v[k] = __uint_as_float(r[k]);
+// A box of a 3-d map, which is in parameter space, to shared memory.
+__device__ __forceinline__ void box_load(uint32_t to, const CUtensorMap* map, int column, int row, int worker, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(to),
+                 "l"(map), "r"(column), "r"(row), "r"(worker), "r"(bar)
+                 : "memory");
 }
 // Behind it the values are there.
-__device__ __forceinline__ void columns_wait(float (&v)[32]) {
+template <int N>
+__device__ __forceinline__ void columns_wait(float (&v)[N]) {
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
-    for (int k = 0; k < 32; ++k) asm volatile("" : "+f"(v[k]));
+    for (int k = 0; k < N; ++k) asm volatile("" : "+f"(v[k]));
+}
+
+// N columns of a lane's row, 16 at a time.
+template <int N>
+__device__ __forceinline__ void columns(uint32_t at, float (&v)[N]) {
+#pragma unroll
+    for (int k = 0; k < N; k += 16) {
+        uint32_t r[16];
+        asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                     : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+                       "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                     : "r"(at + k));
+#pragma unroll
+        for (int e = 0; e < 16; ++e) v[k + e] = __uint_as_float(r[e]);
+    }
 }
 
 // Set where a wait gave up, which no size or input should bring about; the results of that call are then worthless.
@@ -118,6 +145,14 @@ __device__ __forceinline__ void planes8(const float (&v)[8], uint4 (&out)[3]) {
     for (int p = 0; p < 3; ++p) out[p] = make_uint4(w[0][p], w[1][p], w[2][p], w[3][p]);
 }
 
+// The first two planes of eight ranks of a row (a column of the factor) in an image for up.
+template <int R>
+__device__ __forceinline__ void store_up(char* tile, uint32_t row, uint32_t c, const uint4 (&w)[3]) {
+#pragma unroll
+    for (uint32_t p = 0; p < 2; ++p)
+        *reinterpret_cast<uint4*>(tile + (R == 64 ? p * kTileBytes + swizzled(row, c) : swizzled(row, p * (R / 8) + c))) = w[p];
+}
+
 // ---- prepare ---------------------------------------------------------------------------------------------------------------
 
 struct PrepareArgs {
@@ -130,21 +165,22 @@ struct PrepareArgs {
     int32_t shared;
 };
 // A thread per chunk of 16 bytes.
+template <int R>
 __global__ void __launch_bounds__(256) prepare_kernel(const __grid_constant__ PrepareArgs a) {
     uint32_t at = blockIdx.x * 256 + threadIdx.x;
     float v[8];
     uint4 w[3];
     if (at < a.t_count) {  // [64 rows][8 rows][rank]: neighbouring threads read neighbouring ranks
-        const uint32_t rank = at & 63u, c = at >> 6 & 7u, block = at >> 9;
+        const uint32_t rank = at % R, c = at / R % 8u, block = at / (8 * R);
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
             const uint32_t row = block * 64 + c * 8 + k;
             v[k] = row < a.rows && (int)rank < a.rank ? __ldg(a.t + ((int64_t)blockIdx.y * a.rows + row) * a.rank + rank) : 0.0f;
         }
         planes8(v, w);
-        char* out = a.t_image + blockIdx.y * t_outer_image(a.rows) + (int64_t)block * kPlanesBytes;
+        char* out = a.t_image + blockIdx.y * t_outer_image(a.rows, R) + (int64_t)block * By<R>::kPlanesBytes;
 #pragma unroll
-        for (int p = 0; p < 3; ++p) *reinterpret_cast<uint4*>(out + swizzled(p * kRank + rank, c)) = w[p];
+        for (int p = 0; p < 3; ++p) *reinterpret_cast<uint4*>(out + swizzled(p * R + rank, c)) = w[p];
         return;
     }
     at -= a.t_count;
@@ -152,7 +188,7 @@ __global__ void __launch_bounds__(256) prepare_kernel(const __grid_constant__ Pr
     if (at < a.down_count) {
         // the faster index is the one along which the factor is packed
         const bool ranks_packed = a.down.sj == 1;
-        const uint32_t rank = ranks_packed ? at & 63u : at >> 3 & 63u, c = ranks_packed ? at >> 6 & 7u : at & 7u, block = at >> 9;
+        const uint32_t rank = ranks_packed ? at % R : at / 8 % R, c = ranks_packed ? at / R % 8u : at % 8u, block = at / (8 * R);
         const float* f = a.down.p + (int64_t)blockIdx.y * a.down.ws;
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
@@ -160,15 +196,16 @@ __global__ void __launch_bounds__(256) prepare_kernel(const __grid_constant__ Pr
             v[k] = (int)rank < a.rank && col < a.down_h ? __ldg(f + rank * a.down.sj + col * a.down.sc) : 0.0f;
         }
         planes8(v, w);
-        char* out = a.down_image + blockIdx.y * down_image(a.down_h) + (int64_t)block * kPlanesBytes;
+        char* out = a.down_image + blockIdx.y * down_image(a.down_h, R) + (int64_t)block * By<R>::kPlanesBytes;
 #pragma unroll
-        for (int p = 0; p < 3; ++p) *reinterpret_cast<uint4*>(out + swizzled(p * kRank + rank, c)) = w[p];
+        for (int p = 0; p < 3; ++p) *reinterpret_cast<uint4*>(out + swizzled(p * R + rank, c)) = w[p];
         return;
     }
     at -= a.down_count;
     if (at >= a.up_count) return;
     const bool ranks_packed = a.up.sj == 1;
-    const uint32_t col = ranks_packed ? at >> 3 & 127u : at & 127u, c = ranks_packed ? at & 7u : at >> 7 & 7u, block = at >> 10;
+    constexpr uint32_t C = R / 8;  // chunks of a plane's row
+    const uint32_t col = ranks_packed ? at / C % 128u : at % 128u, c = ranks_packed ? at % C : at / 128 % C, block = at / (128 * C);
     const float* f = a.up.p + (int64_t)blockIdx.y * a.up.ws;
     const int64_t column = (int64_t)block * 128 + col;
 #pragma unroll
@@ -177,9 +214,7 @@ __global__ void __launch_bounds__(256) prepare_kernel(const __grid_constant__ Pr
         v[k] = rank < a.rank && column < a.up_h ? __ldg(f + rank * a.up.sj + column * a.up.sc) : 0.0f;
     }
     planes8(v, w);
-    char* out = a.up_image + blockIdx.y * up_image(a.up_h) + (int64_t)block * (2 * kTileBytes);
-#pragma unroll
-    for (int p = 0; p < 2; ++p) *reinterpret_cast<uint4*>(out + p * kTileBytes + swizzled(col, c)) = w[p];
+    store_up<R>(a.up_image + blockIdx.y * up_image(a.up_h, R) + (int64_t)block * By<R>::kUpBytes, col, c, w);
 }
 
 // ---- down and outer --------------------------------------------------------------------------------------------------------
@@ -201,18 +236,15 @@ struct Args {
     Drop drop;
 };
 
-// The barriers: a stage is full (256 threads' chunks and the planes), a stage is empty (its products are done); the sums are ready, the
-// sums are drained.
-enum : int { kFull = 0, kEmpty = kStages, kReady = 2 * kStages, kDrained = 2 * kStages + 1, kBars = 2 * kStages + 2 };
 constexpr int kThreads = 288;
 
-// Shared memory from its first 1024-byte boundary on, tensor memory and the barriers. The shared word that takes the address is the
-// caller's.
-__device__ __forceinline__ char* tensor_begin(char* smem, uint64_t* bars, uint32_t* word, uint32_t columns, uint32_t& memory) {
+// Tensor memory and the barriers. The shared word that takes the address is the caller's.
+template <int R>
+__device__ __forceinline__ void tensor_begin(uint64_t* bars, uint32_t* word, uint32_t columns, uint32_t& memory) {
     if (threadIdx.x < 32) memory_alloc(shared_address(word), columns);
     if (threadIdx.x == 0) {
-        for (int k = 0; k < kBars; ++k)
-            barrier_init(shared_address(bars + k), k < kEmpty ? 257u : k == kDrained ? 256u : 1u);
+        for (int k = 0; k < By<R>::kBars; ++k)
+            barrier_init(shared_address(bars + k), (k >= By<R>::kTouched && k < By<R>::kEmpty) || k == By<R>::kDrained ? 256u : 1u);
         fence_shared();
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -220,8 +252,9 @@ __device__ __forceinline__ char* tensor_begin(char* smem, uint64_t* bars, uint32
     __syncthreads();
     fence_after();
     memory = *word;
-    return smem + ((1024u - (shared_address(smem) & 1023u)) & 1023u);
 }
+// From its first 1024-byte boundary on.
+__device__ __forceinline__ char* aligned(char* smem) { return smem + ((1024u - (shared_address(smem) & 1023u)) & 1023u); }
 __device__ __forceinline__ void tensor_end(uint32_t memory, uint32_t columns) {
     fence_before();
     __syncthreads();
@@ -229,197 +262,208 @@ __device__ __forceinline__ void tensor_end(uint32_t memory, uint32_t columns) {
     if (threadIdx.x < 32) memory_free(memory, columns);
 }
 
-// The ninth warp's part: planes and products of the steps first, first + stride, ... below last.
-template <bool ACROSS>
-__device__ __forceinline__ void issue_products_alone(const char* image, int first, int stride, int last, char* smem, uint32_t memory, uint32_t bars) {
+// What both parts walk: steps first, first + stride, ... below last of 64 columns (down: 256 rows from row0 on) or 64 rows (outer,
+// ACROSS: 256 columns from column0 on).
+struct Walk {
+    uint32_t worker, row0;
+    int column0, first, stride, last;
+};
+
+// The ninth warp's part. MAPPED: the activation is brought by TMA.
+template <int R, bool MAPPED, bool ACROSS>
+__device__ __forceinline__ void issue_alone(const Args& a, const CUtensorMap* map, const Walk& k, char* smem, uint32_t memory, uint32_t bars) {
+    using B = By<R>;
+    const char* image = a.image + (int64_t)k.worker * a.image_ws;
+    const bool touched = !MAPPED || a.drop.on;
     bool lost = false;
-    auto planes = [&](int step, int stage) {
-        if (step >= last) return;
-        const uint32_t bar = bars + 8 * (kFull + stage);
-        mbar_expect(bar, kPlanesBytes);
-        bulk_load(smem + stage * kStageBytes + 2 * kTileBytes, image + (int64_t)step * kPlanesBytes, kPlanesBytes, bar);
+    auto bring = [&](int step, int stage) {
+        if (step >= k.last) return;
+        const uint32_t bar = bars + 8 * (B::kLanded + stage), to = shared_address(smem + stage * B::kStageBytes);
+        mbar_expect(bar, B::kPlanesBytes + (MAPPED ? 2 * kTileBytes : 0));
+        if (MAPPED) {
+            if (ACROSS) {
+#pragma unroll
+                for (int c = 0; c < 4; ++c) box_load(to + c * 8192, map, k.column0 + c * 64, step * 64, (int)k.worker, bar);
+            } else {
+#pragma unroll
+                for (int m = 0; m < 2; ++m) box_load(to + m * kTileBytes, map, step * 64, (int)k.row0 + m * 128, (int)k.worker, bar);
+            }
+        }
+        bulk_load(smem + stage * B::kStageBytes + 2 * kTileBytes, image + (int64_t)step * B::kPlanesBytes, B::kPlanesBytes, bar);
     };
-    for (int s = 0; s < kStages - 1; ++s) planes(first + s * stride, s);
+    for (int s = 0; s < B::kStages - 1; ++s) bring(k.first + s * k.stride, s);
     int stage = 0, since = 0;
-    uint32_t full = 0, empty = 0, drained = 1;  // phases; nothing is to be drained at first
-    for (int step = first, turn = 0; step < last && !lost; step += stride, ++turn) {
+    uint32_t here = 0, empty = 0, drained = 1;  // phases; nothing is to be drained at first
+    for (int step = k.first, turn = 0; step < k.last; step += k.stride, ++turn) {
         if (since == 0) {
-            if (turn > 0) lost = !barrier_wait(bars + 8 * kDrained, drained);
+            if (turn > 0) lost = !barrier_wait(bars + 8 * B::kDrained, drained);
             drained ^= 1u;
         }
-        lost = lost || !barrier_wait(bars + 8 * (kFull + stage), full >> stage & 1u);
-        full ^= 1u << stage;
+        lost = lost || !barrier_wait(bars + 8 * (B::kLanded + stage), here >> stage & 1u);
+        if (touched) lost = lost || !barrier_wait(bars + 8 * (B::kTouched + stage), here >> stage & 1u);
+        here ^= 1u << stage;
         if (lost) break;
         fence_after();
-        const uint32_t tiles = shared_address(smem + stage * kStageBytes), right = tiles + 2 * kTileBytes;
+        const uint32_t tiles = shared_address(smem + stage * B::kStageBytes), right = tiles + 2 * kTileBytes;
 #pragma unroll
         for (int m = 0; m < 2; ++m)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {  // 16 of the 64
-                const uint64_t left = ACROSS ? operand(tiles + m * kTileBytes + k * 2048, 8192) : operand(tiles + m * kTileBytes + k * 32, 16);
-                product(memory + m * kN, left, operand(right + k * 32, 16), instruction(kN, ACROSS, false), since > 0 || k > 0);
+            for (int q = 0; q < 4; ++q) {  // 16 of the 64
+                const uint64_t left = ACROSS ? operand(tiles + m * kTileBytes + q * 2048, 8192) : operand(tiles + m * kTileBytes + q * 32, 16);
+                product(memory + m * B::kN, left, operand(right + q * 32, 16), instruction(B::kN, ACROSS, false), since > 0 || q > 0);
             }
-        products_done(bars + 8 * (kEmpty + stage));
-        if (++since == kFlush || step + stride >= last) {
+        products_done(bars + 8 * (B::kEmpty + stage));
+        if (++since == kFlush || step + k.stride >= k.last) {
             since = 0;
-            products_done(bars + 8 * kReady);
+            products_done(bars + 8 * B::kReady);
         }
-        const int behind = stage == 0 ? kStages - 1 : stage - 1;
+        // the stage before is free once its products are done
+        const int behind = stage == 0 ? B::kStages - 1 : stage - 1;
         if (turn > 0) {
-            lost = !barrier_wait(bars + 8 * (kEmpty + behind), empty >> behind & 1u);
+            lost = !barrier_wait(bars + 8 * (B::kEmpty + behind), empty >> behind & 1u);
             empty ^= 1u << behind;
+            if (lost) break;
         }
-        if (!lost) planes(step + (kStages - 1) * stride, behind);
-        stage = stage + 1 == kStages ? 0 : stage + 1;
+        bring(step + (B::kStages - 1) * k.stride, behind);
+        stage = stage + 1 == B::kStages ? 0 : stage + 1;
     }
     if (lost) gave_up = 1;
 }
-
-template <bool ACROSS>
-__device__ __forceinline__ void issue_products(const char* image, int first, int stride, int last, char* smem, uint32_t memory, uint32_t bars) {
-    if (threadIdx.x == 256) issue_products_alone<ACROSS>(image, first, stride, last, smem, memory, bars);
+template <int R, bool MAPPED, bool ACROSS>
+__device__ __forceinline__ void issue(const Args& a, const CUtensorMap* map, const Walk& k, char* smem, uint32_t memory, uint32_t bars) {
+    if (threadIdx.x == 256) issue_alone<R, MAPPED, ACROSS>(a, map, k, smem, memory, bars);
     __syncwarp();
 }
 
-// The first eight warps' part: the sums of two tiles along the steps; sums[r] of a thread is rank r of row 128 (warp / 4) + 32 (warp % 4) +
-// lane of the 256. ACROSS = false: 256 rows from row0 on, steps of 64 along the columns; true: 256 columns from column0 on, steps of
-// 64 along the rows. A thread has a column of eight chunks, every 32nd row's (or 8th row's): its addresses are a start and a stride.
-template <bool VEC, bool ACROSS>
-__device__ __forceinline__ void sum_tiles(const Args& a, uint32_t worker, uint32_t row0, int column0, int first, int stride, int last, char* smem,
-                                          uint32_t memory, uint32_t bars, float (&sums)[kRank]) {
+// The first eight warps' part: sums[r] of a thread is rank r of row 128 (warp / 4) + 32 (warp % 4) + lane of the 256. Where there is
+// something to do on the tiles a thread has a column of eight chunks, every 32nd row's (or 8th row's).
+template <int R, bool MAPPED, bool ACROSS>
+__device__ __forceinline__ void sum_tiles(const Args& a, const Walk& k, char* smem, uint32_t memory, uint32_t bars, float (&sums)[R]) {
+    using B = By<R>;
     constexpr uint32_t kRows = ACROSS ? 8 : 32, kPlace = ACROSS ? 1024 : 4096;  // from one of a thread's chunks to the next
     const int warp = threadIdx.x >> 5;
     const uint32_t r0 = ACROSS ? threadIdx.x >> 5 : threadIdx.x >> 3, c0 = ACROSS ? threadIdx.x & 31u : threadIdx.x & 7u;
     char* at0 = smem + (ACROSS ? (c0 >> 3) * 8192u + swizzled(r0, c0 & 7u) : swizzled(r0, c0));
-    const int64_t step_rows = ACROSS ? 64 : 0, step_columns = ACROSS ? 0 : 64;
-    const uint32_t row1 = (ACROSS ? 0 : row0) + r0;        // of step 0 and the first chunk
-    const int64_t column1 = (ACROSS ? column0 : 0) + (int64_t)c0 * 8;
-    const __nv_bfloat16* x = (const __nv_bfloat16*)a.x + (int64_t)worker * a.x_ws;
+    const __nv_bfloat16* x = (const __nv_bfloat16*)a.x + (int64_t)k.worker * a.x_ws;
     const uint32_t call = drop_call(a.drop);
+    const bool touch = !MAPPED || a.drop.on;
     bool lost = false;  // a wait gave up
-    auto fetch = [&](int step, int stage) {
-        if (step < last) {
-            const int64_t column = column1 + step * step_columns;
-            const uint32_t row = row1 + (uint32_t)(step * step_rows);
-            const __nv_bfloat16* from = x + (int64_t)row * a.x_rs + column;
-            const bool in = column < a.h;
+    auto flush = [&]() {  // from tensor memory to the registers, the planes' together
+        const uint32_t at = memory + ((uint32_t)(warp & 3) << 21) + (uint32_t)(warp >> 2) * B::kN;
+        constexpr int H = R == 64 ? 32 : R;  // columns at a time
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const bool there = in && row + k * kRows < a.rows;
-                char* to = at0 + stage * kStageBytes + k * kPlace;
-                if constexpr (VEC) {
-                    copy16(to, there ? (const void*)(from + k * kRows * a.x_rs) : a.x, there);
-                } else {
-                    *reinterpret_cast<uint4*>(to) = raw_columns<__nv_bfloat16, false>(
-                        there ? from + k * kRows * a.x_rs - column : (const __nv_bfloat16*)a.x, (int)column, there ? a.h : 0).q;
-                }
-            }
-        }
-        copies_commit();
-    };
-    auto mask = [&](int step, int stage) {  // the chunks that this thread copied
-        const uint32_t row = row1 + (uint32_t)(step * step_rows), group = (uint32_t)((column1 + step * step_columns) >> 3);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const uint4 u = drop_words(a.drop, group, row + k * kRows, a.drop.worker + worker, call);
-            uint4* place = reinterpret_cast<uint4*>(at0 + stage * kStageBytes + k * kPlace);
-            const Raw8<__nv_bfloat16> raw = {*place};
-            uint32_t w[1][4];
-            raw_planes<__nv_bfloat16>(raw, a.drop, u, w);
-            *place = make_uint4(w[0][0], w[0][1], w[0][2], w[0][3]);
-        }
-    };
-    // the tiles' sums go from tensor memory to the registers, the planes' together
-    auto flush = [&]() {
-        const uint32_t at = memory + ((uint32_t)(warp & 3) << 21) + (uint32_t)(warp >> 2) * kN;
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            float v[32], w[32];
-            columns32(at + 2 * kRank + half * 32, v);
-            columns32(at + kRank + half * 32, w);
+        for (int from = 0; from < R; from += H) {
+            float v[H], w[H];
+            columns(at + 2 * R + from, v);
+            columns(at + R + from, w);
             columns_wait(v);
             columns_wait(w);
 #pragma unroll
-            for (int k = 0; k < 32; ++k) w[k] += v[k];
-            columns32(at + half * 32, v);
+            for (int e = 0; e < H; ++e) w[e] += v[e];
+            columns(at + from, v);
             columns_wait(v);
 #pragma unroll
-            for (int k = 0; k < 32; ++k) sums[half * 32 + k] += v[k] + w[k];
+            for (int e = 0; e < H; ++e) sums[from + e] += v[e] + w[e];
         }
     };
 #pragma unroll
-    for (int r = 0; r < kRank; ++r) sums[r] = 0.0f;
-    for (int s = 0; s < kStages - 1; ++s) fetch(first + s * stride, s);
+    for (int r = 0; r < R; ++r) sums[r] = 0.0f;
     int stage = 0, since = 0;
-    uint32_t empty = 0, ready = 0;  // phases
-    for (int step = first, turn = 0; step < last; step += stride, ++turn) {
-        copies_wait<kStages - 2>();
-        if (a.drop.on) mask(step, stage);
-        fence_shared();
-        barrier_arrive(bars + 8 * (kFull + stage));
-        // the stage before is free once its products are done
-        const int behind = stage == 0 ? kStages - 1 : stage - 1;
-        if (turn > 0) {
-            lost = lost || !barrier_wait(bars + 8 * (kEmpty + behind), empty >> behind & 1u);
-            empty ^= 1u << behind;
+    uint32_t here = 0, empty = 0, ready = 0;  // phases
+    for (int step = k.first, turn = 0; step < k.last; step += k.stride, ++turn) {
+        if (touch) {
+            char* at = at0 + stage * B::kStageBytes;
+            const uint32_t row = (ACROSS ? (uint32_t)step * 64 : k.row0) + r0;
+            const int64_t column = (ACROSS ? (int64_t)k.column0 : (int64_t)step * 64) + c0 * 8;
+            if (MAPPED) {
+                lost = lost || !barrier_wait(bars + 8 * (B::kLanded + stage), here >> stage & 1u);
+            } else if (turn >= B::kStages) {
+                lost = lost || !barrier_wait(bars + 8 * (B::kEmpty + stage), empty >> stage & 1u);
+                empty ^= 1u << stage;
+            }
+            here ^= 1u << stage;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                uint4* place = reinterpret_cast<uint4*>(at + e * kPlace);
+                Raw8<__nv_bfloat16> raw;
+                if (MAPPED) {
+                    raw.q = *place;
+                } else {
+                    const bool in = row + e * kRows < a.rows;
+                    raw = raw_columns<__nv_bfloat16, false>(x + (in ? (int64_t)(row + e * kRows) * a.x_rs : 0), (int)min(column, (int64_t)a.h),
+                                                            in ? a.h : 0);
+                }
+                if (a.drop.on) {
+                    const uint4 u = drop_words(a.drop, (uint32_t)(column >> 3), row + e * kRows, a.drop.worker + k.worker, call);
+                    uint32_t w[1][4];
+                    raw_planes<__nv_bfloat16>(raw, a.drop, u, w);
+                    raw.q = make_uint4(w[0][0], w[0][1], w[0][2], w[0][3]);
+                }
+                *place = raw.q;
+            }
+            fence_shared();
+            barrier_arrive(bars + 8 * (B::kTouched + stage));
         }
-        fetch(step + (kStages - 1) * stride, behind);
-        if (++since == kFlush || step + stride >= last) {
+        if (++since == kFlush || step + k.stride >= k.last) {
             since = 0;
-            lost = lost || !barrier_wait(bars + 8 * kReady, ready);
+            lost = lost || !barrier_wait(bars + 8 * B::kReady, ready);
             ready ^= 1u;
             fence_after();
             flush();
             fence_before();
-            barrier_arrive(bars + 8 * kDrained);
+            barrier_arrive(bars + 8 * B::kDrained);
         }
-        stage = stage + 1 == kStages ? 0 : stage + 1;
+        stage = stage + 1 == B::kStages ? 0 : stage + 1;
     }
-    copies_wait<0>();
     if (lost) gave_up = 1;
 }
 
 // A CTA takes 256 rows of a worker and its share of the columns.
-template <bool VEC>
-__global__ void __launch_bounds__(kThreads, 1) down_kernel(const __grid_constant__ Args a) {
+template <int R, bool MAPPED>
+__global__ void __launch_bounds__(kThreads, 1) down_kernel(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap map) {
     extern __shared__ __align__(16) char dynamic[];
-    __shared__ uint64_t bars[kBars];
+    __shared__ uint64_t bars[By<R>::kBars];
     __shared__ uint32_t word;
     dependency_wait();
     uint32_t memory;
-    char* smem = tensor_begin(dynamic, bars, &word, kColumns, memory);
+    char* smem = aligned(dynamic);
+    tensor_begin<R>(bars, &word, By<R>::kColumns, memory);
     const uint32_t tile = blockIdx.x / a.split, i = tile / a.tiles, row0 = (tile - i * a.tiles) * 256;
     const int part = (int)(blockIdx.x - tile * a.split), steps = (a.h + 63) / 64;
     const bool main = threadIdx.x < 256;
-    float sums[kRank];
-    if (main) sum_tiles<VEC, false>(a, i, row0, 0, part, a.split, steps, smem, memory, shared_address(bars), sums);
-    else issue_products<false>(a.image + (int64_t)i * a.image_ws, part, a.split, steps, smem, memory, shared_address(bars));
-    tensor_end(memory, kColumns);
+    float sums[R];
+    const Walk walk = {i, row0, 0, part, a.split, steps};
+    if (main) sum_tiles<R, MAPPED, false>(a, walk, smem, memory, shared_address(bars), sums);
+    else issue<R, MAPPED, false>(a, &map, walk, smem, memory, shared_address(bars));
+    tensor_end(memory, By<R>::kColumns);
     // this CTA's sums, then its share of the rows, joined over the cluster in order
-    constexpr int L = kRank + 1;
+    constexpr int L = R + 1;
     float *mine = reinterpret_cast<float*>(smem), *whole = mine + 256 * L;
     if (main)
 #pragma unroll
-        for (int r = 0; r < kRank; ++r) mine[threadIdx.x * L + r] = sums[r];
+        for (int r = 0; r < R; ++r) mine[threadIdx.x * L + r] = sums[r];
     cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
     cluster.sync();
     const float scale = a.scale * (a.drop.on ? a.drop.factor : 1.0f);
-    const int share = 256 / a.split, from = part * share;  // split is a power of two up to 4: a share is 64 rows at least
-    for (int e = threadIdx.x; e < share * kRank; e += kThreads) {
-        const int r = e / kRank, j = e % kRank;
-        float v = 0.0f;
-        for (int s = 0; s < a.split; ++s) v += cluster.map_shared_rank(mine, s)[(from + r) * L + j];
+    const int share = 256 / a.split, from = part * share;  // split is a power of two up to 8: a share is 32 rows at least
+    for (int e = threadIdx.x; e < share * R; e += kThreads) {
+        const int r = e / R, j = e % R;
+        float part[8], v = 0.0f;
+#pragma unroll
+        for (int s = 0; s < 8; ++s) part[s] = s < a.split ? cluster.map_shared_rank(mine, s)[(from + r) * L + j] : 0.0f;
+#pragma unroll
+        for (int s = 0; s < 8; ++s) v += part[s];
         whole[r * L + j] = scale * v;
     }
     __syncthreads();
     const uint32_t first = row0 + from;  // a multiple of 64
     if (a.out)
-        for (int e = threadIdx.x; e < share * kRank; e += kThreads) {
-            const int r = e / kRank, j = e % kRank;
+        for (int e = threadIdx.x; e < share * R; e += kThreads) {
+            const int r = e / R, j = e % R;
             if (first + r < a.rows && j < a.rank) a.out[((int64_t)i * a.rows + first + r) * a.rank + j] = whole[r * L + j];
         }
-    for (int e = threadIdx.x; e < share * 8; e += kThreads) {  // a row's eight ranks
-        const int r = e >> 3, c = e & 7;
+    for (int e = threadIdx.x; e < share * (R / 8); e += kThreads) {  // a row's eight ranks
+        const int r = e / (R / 8), c = e % (R / 8);
         const uint32_t row = first + r;
         if (row >= (a.rows + 127) / 128 * 128) break;
         float v[8];
@@ -427,13 +471,11 @@ __global__ void __launch_bounds__(kThreads, 1) down_kernel(const __grid_constant
         for (int k = 0; k < 8; ++k) v[k] = whole[r * L + c * 8 + k];
         uint4 w[3];
         planes8(v, w);
-        char* out = a.t_up + i * t_up_image(a.rows) + (int64_t)(row >> 7) * (2 * kTileBytes) + swizzled(row & 127u, c);
-        *reinterpret_cast<uint4*>(out) = w[0];
-        *reinterpret_cast<uint4*>(out + kTileBytes) = w[1];
+        store_up<R>(a.t_up + i * t_up_image(a.rows, R) + (int64_t)(row >> 7) * By<R>::kUpBytes, row & 127u, c, w);
     }
     if (a.t_outer)
-        for (int e = threadIdx.x; e < share * 8; e += kThreads) {  // a rank's eight rows
-            const int j = e & 63, r = (e >> 6) * 8;
+        for (int e = threadIdx.x; e < share / 8 * R; e += kThreads) {  // a rank's eight rows
+            const int j = e % R, r = e / R * 8;
             const uint32_t row = first + r;
             if (row >= (a.rows + 63) / 64 * 64) break;
             float v[8];
@@ -441,52 +483,55 @@ __global__ void __launch_bounds__(kThreads, 1) down_kernel(const __grid_constant
             for (int k = 0; k < 8; ++k) v[k] = whole[(r + k) * L + j];
             uint4 w[3];
             planes8(v, w);
-            char* out = a.t_outer + i * t_outer_image(a.rows) + (int64_t)(row >> 6) * kPlanesBytes;
+            char* out = a.t_outer + i * t_outer_image(a.rows, R) + (int64_t)(row >> 6) * By<R>::kPlanesBytes;
 #pragma unroll
-            for (int p = 0; p < 3; ++p) *reinterpret_cast<uint4*>(out + swizzled(p * kRank + j, (row >> 3) & 7u)) = w[p];
+            for (int p = 0; p < 3; ++p) *reinterpret_cast<uint4*>(out + swizzled(p * R + j, (row >> 3) & 7u)) = w[p];
         }
     cluster.sync();  // the others may still be reading
 }
 
 // A CTA takes 256 columns and a chunk of a worker's rows.
-template <bool VEC>
-__global__ void __launch_bounds__(kThreads, 1) outer_kernel(const __grid_constant__ Args a) {
+template <int R, bool MAPPED>
+__global__ void __launch_bounds__(kThreads, 1) outer_kernel(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap map) {
     extern __shared__ __align__(16) char dynamic[];
-    __shared__ uint64_t bars[kBars];
+    __shared__ uint64_t bars[By<R>::kBars];
     __shared__ uint32_t word;
     dependency_wait();
     uint32_t memory;
-    char* smem = tensor_begin(dynamic, bars, &word, kColumns, memory);
+    char* smem = aligned(dynamic);
+    tensor_begin<R>(bars, &word, By<R>::kColumns, memory);
     const uint32_t i = blockIdx.y / a.chunks, chunk = blockIdx.y - i * a.chunks, blocks = (a.rows + 63) / 64;
     const int s0 = (int)((uint64_t)blocks * chunk / a.chunks), s1 = (int)((uint64_t)blocks * (chunk + 1) / a.chunks);
-    float sums[kRank];
-    if (threadIdx.x < 256) sum_tiles<VEC, true>(a, i, 0, (int)blockIdx.x * 256, s0, 1, s1, smem, memory, shared_address(bars), sums);
-    else issue_products<true>(a.image + (int64_t)i * a.image_ws, s0, 1, s1, smem, memory, shared_address(bars));
-    tensor_end(memory, kColumns);
+    float sums[R];
+    const Walk walk = {i, 0, (int)blockIdx.x * 256, s0, 1, s1};
+    if (threadIdx.x < 256) sum_tiles<R, MAPPED, true>(a, walk, smem, memory, shared_address(bars), sums);
+    else issue<R, MAPPED, true>(a, &map, walk, smem, memory, shared_address(bars));
+    tensor_end(memory, By<R>::kColumns);
     const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (threadIdx.x >= 256 || c >= a.h) return;
     const float scale = a.scale * (a.drop.on ? a.drop.factor : 1.0f);
     float* out = a.out + (int64_t)blockIdx.y * a.rank * a.h + c * a.sc;
     if (a.sj == 1 && (a.rank & 3) == 0 && (reinterpret_cast<uintptr_t>(a.out) & 15u) == 0) {
 #pragma unroll
-        for (int r = 0; r < kRank; r += 4)
+        for (int r = 0; r < R; r += 4)
             if (r < a.rank)
                 *reinterpret_cast<float4*>(out + r) = make_float4(scale * sums[r], scale * sums[r + 1], scale * sums[r + 2], scale * sums[r + 3]);
     } else {
 #pragma unroll
-        for (int r = 0; r < kRank; ++r)
+        for (int r = 0; r < R; ++r)
             if (r < a.rank) out[r * a.sj] = scale * sums[r];
     }
 }
 
 // ---- up --------------------------------------------------------------------------------------------------------------------
 
-// A CTA takes 128 columns, whose planes of the factor stay in shared memory, and goes through the 128-row tiles of a chunk: the tile's
-// planes of t and of the base by copies, 12 products of 16 rank indices (the planes' indices together at most 1), the
-// result into the base's place in shared memory and from there to memory by rows. Behind the products t's place is free for the next base,
-// which is on its way during the rest of the tile, and behind the stores the tile's place for the next t. Two CTAs to an SM.
-constexpr int kUpShared = 1024 + 2 * 2 * kTileBytes + 2 * kTileBytes;
-constexpr uint32_t kUpColumns = 128;
+// A CTA takes CN columns, whose planes of the factor stay in shared memory, and goes through the 128-row tiles of a chunk: the planes of t
+// and the base of the next tile are on their way while this one is done; products of 16 rank indices (the planes' indices together at
+// most 1); the result into the base's place in shared memory and from there to memory by rows. Two CTAs to an SM.
+template <int R>
+__host__ __device__ constexpr int up_columns() { return R == 64 ? 64 : 128; }  // CN: what two CTAs' shared memory holds
+template <int R>
+__host__ __device__ constexpr int up_shared() { return By<R>::kUpTiles * up_columns<R>() * 128 + 2 * By<R>::kUpBytes + 2 * 256 * up_columns<R>() + 256; }
 
 struct UpArgs {
     const void* base;  // may be null
@@ -499,82 +544,102 @@ struct UpArgs {
     Drop drop;
 };
 
-template <bool VEC>
+template <int R, bool VEC>
 __global__ void __launch_bounds__(256, 2) up_kernel(const __grid_constant__ UpArgs a) {
-    extern __shared__ __align__(16) char dynamic[];
-    __shared__ uint64_t bars[kBars];
-    __shared__ uint32_t word;
+    extern __shared__ __align__(1024) char smem[];  // (all of it: nothing static, so it starts on the boundary, and two CTAs fit)
+    using B = By<R>;
+    constexpr int CN = up_columns<R>(), kRow = 2 * CN, kPlaneBytes = CN * 128;  // bytes of a tile's row; of a plane of the factor (R = 64)
+    constexpr uint32_t kMemory = CN;
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + up_shared<R>() - 256);
+    uint32_t* word = reinterpret_cast<uint32_t*>(bars + B::kBars);
     bool lost = false;  // a wait gave up
     dependency_wait();
     uint32_t memory;
-    char* smem = tensor_begin(dynamic, bars, &word, kUpColumns, memory);
-    // tile: 128 rows of 16 chunks, chunk c at c ^ (row % 8)
-    char *planes = smem, *t = smem + 2 * kTileBytes, *tile = smem + 4 * kTileBytes;
+    tensor_begin<R>(bars, word, kMemory, memory);
+    // tile: 128 rows, chunk c at c ^ (row % 8)
+    char *planes = smem, *t0 = smem + B::kUpTiles * kPlaneBytes, *tile0 = t0 + 2 * B::kUpBytes;
     const uint32_t i = blockIdx.y / a.chunks, chunk = blockIdx.y - i * a.chunks, blocks = (a.rows + 127) / 128;
     const uint32_t b0 = (uint32_t)((uint64_t)blocks * chunk / a.chunks), b1 = (uint32_t)((uint64_t)blocks * (chunk + 1) / a.chunks);
-    const int c0 = (int)blockIdx.x * 128, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t call = drop_call(a.drop), bar = shared_address(bars + kReady);
-    auto linear = [&](char* to, const char* from) {  // two planes
+    const int c0 = (int)blockIdx.x * CN, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t call = drop_call(a.drop), bar = shared_address(bars + B::kReady);
+    const __nv_bfloat16* base = (const __nv_bfloat16*)a.base + (int64_t)i * a.base_ws;
+    __nv_bfloat16* y = (__nv_bfloat16*)a.y + (int64_t)i * a.rows * a.h;
+    const char* t_image = a.t_up + i * t_up_image(a.rows, R);
+    // What a thread brings to a tile it takes away too. VEC: a column of chunks, every (256 / chunks of a row)-th row's; elsewhere a warp has
+    // every eighth row and a lane every 32nd element.
+    constexpr uint32_t kChunks = CN / 8, kRows = 256 / kChunks;
+    const uint32_t r0 = threadIdx.x / kChunks, q0 = threadIdx.x % kChunks, at0 = r0 * kRow + ((q0 ^ (r0 & 7u)) << 4);
+    const int column = c0 + (int)q0 * 8;
+    auto element = [&](uint32_t row, uint32_t c) { return row * kRow + (((c >> 3) ^ (row & 7u)) << 4) + (c & 7u) * 2; };
+    auto fetch = [&](uint32_t b, uint32_t turn) {
+        if (b < b1) {
+            char *t = t0 + (turn & 1u) * B::kUpBytes, *tile = tile0 + (turn & 1u) * (128 * kRow);
+            const char* from = t_image + (int64_t)b * B::kUpBytes;
 #pragma unroll
-        for (int k = 0; k < 2 * kTileBytes / 16 / 256; ++k) copy16(to + (threadIdx.x + 256 * k) * 16, from + (threadIdx.x + 256 * k) * 16);
-    };
-    // a thread has a column of eight chunks of a tile, every 16th row's
-    const uint32_t r0 = threadIdx.x >> 4, at0 = r0 * 256u + (((threadIdx.x & 15u) ^ (r0 & 7u)) << 4);
-    const int column = c0 + (int)(threadIdx.x & 15u) * 8;
-    const __nv_bfloat16* base = (const __nv_bfloat16*)a.base + (int64_t)i * a.base_ws + column;
-    __nv_bfloat16* y = (__nv_bfloat16*)a.y + (int64_t)i * a.rows * a.h + column;
-    auto fetch_base = [&](uint32_t b, char* tile) {
-        if (!a.base) return;
-        const __nv_bfloat16* from = base + (int64_t)(b * 128 + r0) * a.base_rs;
+            for (int k = 0; k < B::kUpBytes / 16 / 256; ++k) copy16(t + (threadIdx.x + 256 * k) * 16, from + (threadIdx.x + 256 * k) * 16);
+            if (a.base) {
+                if constexpr (VEC) {
+                    const __nv_bfloat16* x = base + (int64_t)(b * 128 + r0) * a.base_rs + column;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const bool in = column < a.h && b * 128 + r0 + 16 * k < a.rows;
-            if constexpr (VEC) copy16(tile + at0 + k * 4096, in ? (const void*)(from + k * 16 * a.base_rs) : a.base, in);
-            else *reinterpret_cast<uint4*>(tile + at0 + k * 4096) = raw_columns<__nv_bfloat16, false>(
-                     in ? from + k * 16 * a.base_rs - column : (const __nv_bfloat16*)a.base, column, in ? a.h : 0).q;
+                    for (uint32_t k = 0; k < 128 / kRows; ++k) {
+                        const bool in = column < a.h && b * 128 + r0 + kRows * k < a.rows;
+                        copy16(tile + at0 + k * kRows * kRow, in ? (const void*)(x + k * kRows * a.base_rs) : a.base, in);
+                    }
+                } else {
+                    for (uint32_t r = warp; r < 128; r += 8)
+#pragma unroll
+                        for (int c = lane; c < CN; c += 32)
+                            if (b * 128 + r < a.rows && c0 + c < a.h)
+                                *reinterpret_cast<__nv_bfloat16*>(tile + element(r, c)) = __ldg(base + (int64_t)(b * 128 + r) * a.base_rs + c0 + c);
+                }
+            }
         }
+        copies_commit();
     };
-    const char* t_image = a.t_up + i * t_up_image(a.rows);
-    linear(planes, a.image + (int64_t)i * a.image_ws + (int64_t)blockIdx.x * (2 * kTileBytes));
-    if (b0 < b1) {
-        linear(t, t_image + (int64_t)b0 * (2 * kTileBytes));
-        fetch_base(b0, tile);
+    {
+        const char* from = a.image + (int64_t)i * a.image_ws + (int64_t)(c0 / 128) * B::kUpBytes + c0 % 128 * 128;
+#pragma unroll
+        for (int p = 0; p < B::kUpTiles; ++p)
+#pragma unroll
+            for (int k = 0; k < kPlaneBytes / 16 / 256; ++k)
+                copy16(planes + p * kPlaneBytes + (threadIdx.x + 256 * k) * 16, from + p * kTileBytes + (threadIdx.x + 256 * k) * 16);
     }
-    copies_commit();
-    uint32_t phase = 0;
-    for (uint32_t b = b0; b < b1; ++b) {
-        copies_wait<0>();
+    fetch(b0, 0);
+    uint32_t turn = 0;
+    for (uint32_t b = b0; b < b1; ++b, ++turn) {
+        fetch(b + 1, turn + 1);
+        copies_wait<1>();
         fence_shared();
         fence_before();
         __syncthreads();
+        char* tile = tile0 + (turn & 1u) * (128 * kRow);
         if (threadIdx.x == 0) {
             fence_after();
-            const uint32_t left = shared_address(t), right = shared_address(planes);
+            const uint32_t left = shared_address(t0 + (turn & 1u) * B::kUpBytes), right = shared_address(planes);
+            constexpr uint32_t kRightPlane = R == 64 ? kPlaneBytes : 2 * R;
 #pragma unroll
             for (int q = 0; q < 3; ++q) {  // (0, 1), (1, 0), (0, 0): the smallest first
-                const uint32_t l = left + (q == 1 ? kTileBytes : 0), r = right + (q == 0 ? kTileBytes : 0);
+                const uint32_t l = left + (q == 1 ? B::kUpPlane : 0), r = right + (q == 0 ? kRightPlane : 0);
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    product(memory, operand(l + k * 32, 16), operand(r + k * 32, 16), instruction(128, false, false), q > 0 || k > 0);
+                for (int k = 0; k < R / 16; ++k)
+                    product(memory, operand(l + k * 32, 16), operand(r + k * 32, 16), instruction(CN, false, false), q > 0 || k > 0);
             }
             products_done(bar);
         }
-        lost |= !barrier_wait(bar, phase);
-        phase ^= 1u;
-        fence_after();
-        if (b + 1 < b1) fetch_base(b + 1, t);
-        // a lane's row: 64 columns from 64 (warp / 4) on
+        // a lane's row: CN / 2 columns from CN / 2 (warp / 4) on
         const uint32_t r = (uint32_t)(warp & 3) * 32 + lane, row = b * 128 + r;
+        lost = lost || !barrier_wait(bar, turn & 1u);
+        fence_after();
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int first = (warp >> 2) * 64 + half * 32;
+        for (int part = 0; part < CN / 64; ++part) {
+            const int first = (warp >> 2) * (CN / 2) + part * 32;
             float v[32];
-            columns32(memory + ((uint32_t)(warp & 3) << 21) + first, v);
+            columns(memory + ((uint32_t)(warp & 3) << 21) + first, v);
             columns_wait(v);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const uint32_t c = (uint32_t)(first >> 3) + k;
-                uint4* at = reinterpret_cast<uint4*>(tile + r * 256u + ((c ^ (r & 7u)) << 4));
+                uint4* at = reinterpret_cast<uint4*>(tile + r * kRow + ((c ^ (r & 7u)) << 4));
                 float x[8] = {};
                 if (a.base) raw_floats<__nv_bfloat16>({*at}, x);
 #pragma unroll
@@ -585,34 +650,25 @@ __global__ void __launch_bounds__(256, 2) up_kernel(const __grid_constant__ UpAr
             }
         }
         fence_before();
-        if (__syncthreads_or(lost)) {
-            if (threadIdx.x == 0) gave_up = 1;
-            break;
-        }
-        __nv_bfloat16* to = y + (int64_t)(b * 128 + r0) * a.h;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const uint4 u = *reinterpret_cast<const uint4*>(tile + at0 + k * 4096);
-            if (b * 128 + r0 + 16 * k >= a.rows || column >= a.h) continue;
-            if (VEC) {
-                *reinterpret_cast<uint4*>(to + (int64_t)k * 16 * a.h) = u;
-            } else {
-                __nv_bfloat16 s[8];
-                memcpy(s, &u, sizeof(s));
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (column + e < a.h) to[(int64_t)k * 16 * a.h + e] = s[e];
-            }
-        }
         __syncthreads();
-        if (b + 1 < b1) linear(tile, t_image + (int64_t)(b + 1) * (2 * kTileBytes));
-        copies_commit();
-        char* other = t;
-        t = tile;
-        tile = other;
+        if constexpr (VEC) {
+            __nv_bfloat16* to = y + (int64_t)(b * 128 + r0) * a.h + column;
+#pragma unroll
+            for (uint32_t k = 0; k < 128 / kRows; ++k) {
+                const uint4 u = *reinterpret_cast<const uint4*>(tile + at0 + k * kRows * kRow);
+                if (column < a.h && b * 128 + r0 + kRows * k < a.rows) *reinterpret_cast<uint4*>(to + (int64_t)k * kRows * a.h) = u;
+            }
+        } else {
+            for (uint32_t q = warp; q < 128; q += 8)
+#pragma unroll
+                for (int c = lane; c < CN; c += 32)
+                    if (b * 128 + q < a.rows && c0 + c < a.h)
+                        y[(int64_t)(b * 128 + q) * a.h + c0 + c] = *reinterpret_cast<const __nv_bfloat16*>(tile + element(q, c));
+        }
     }
     copies_wait<0>();
-    tensor_end(memory, kUpColumns);
+    if (lost) gave_up = 1;
+    tensor_end(memory, kMemory);
 }
 
 }  // namespace tensor
