@@ -7,8 +7,9 @@
 // and the sum runs along them (K-major); outer: the sum runs over the rows, the tile is read across them (MN-major), and t
 // comes turned, [plane, rank][row].
 //
-// One thread of a ninth warp brings the tiles (TMA, into the swizzle; the planes, already in its order, in bulk) and issues the products; it
-// waits for nobody else unless dropout masks the activation, which the 256 threads of the other warps do in place. (With tiles copied by
+// One thread of a ninth warp issues the products and one of a tenth brings the tiles (TMA, into the swizzle; the planes, already in its
+// order, in bulk): a stage costs the one 0.35 us and the other 0.2 us, whatever the rank, and one thread for both held the rest up. They wait
+// for nobody else unless dropout masks the activation, which the 256 threads of the other warps do in place. (With tiles copied by
 // all threads, cp.async and a fence to the tensor cores' proxy for each, a stage took 1 us however many were under way: the fence
 // waits for all of a thread's copies.) The tensor cores cut their sums, so after every kFlush tiles of 64 the sums go to fp32 registers by
 // rounded additions, which is the other warps' work. Activations that TMA cannot address (odd widths, other strides) are
@@ -236,7 +237,7 @@ struct Args {
     Drop drop;
 };
 
-constexpr int kThreads = 288;
+constexpr int kThreads = 320;
 
 // Tensor memory and the barriers. The shared word that takes the address is the caller's.
 template <int R>
@@ -269,15 +270,18 @@ struct Walk {
     int column0, first, stride, last;
 };
 
-// The ninth warp's part. MAPPED: the activation is brought by TMA.
+// The tenth warp's part. MAPPED: the activation is brought by TMA.
 template <int R, bool MAPPED, bool ACROSS>
-__device__ __forceinline__ void issue_alone(const Args& a, const CUtensorMap* map, const Walk& k, char* smem, uint32_t memory, uint32_t bars) {
+__device__ __forceinline__ void bring(const Args& a, const CUtensorMap* map, const Walk& k, char* smem, uint32_t bars) {
     using B = By<R>;
     const char* image = a.image + (int64_t)k.worker * a.image_ws;
-    const bool touched = !MAPPED || a.drop.on;
-    bool lost = false;
-    auto bring = [&](int step, int stage) {
-        if (step >= k.last) return;
+    int stage = 0;
+    uint32_t empty = 1;  // the phase to wait for: of a stage's first round none
+    for (int step = k.first, turn = 0; step < k.last; step += k.stride, ++turn) {
+        if (turn >= B::kStages && !barrier_wait(bars + 8 * (B::kEmpty + stage), empty)) {
+            gave_up = 1;
+            return;
+        }
         const uint32_t bar = bars + 8 * (B::kLanded + stage), to = shared_address(smem + stage * B::kStageBytes);
         mbar_expect(bar, B::kPlanesBytes + (MAPPED ? 2 * kTileBytes : 0));
         if (MAPPED) {
@@ -290,48 +294,57 @@ __device__ __forceinline__ void issue_alone(const Args& a, const CUtensorMap* ma
             }
         }
         bulk_load(smem + stage * B::kStageBytes + 2 * kTileBytes, image + (int64_t)step * B::kPlanesBytes, B::kPlanesBytes, bar);
-    };
-    for (int s = 0; s < B::kStages - 1; ++s) bring(k.first + s * k.stride, s);
+        if (++stage == B::kStages) {
+            stage = 0;
+            empty ^= 1u;
+        }
+    }
+}
+
+// The ninth warp's part.
+template <int R, bool MAPPED, bool ACROSS>
+__device__ __forceinline__ void issue(const Args& a, const Walk& k, char* smem, uint32_t memory, uint32_t bars) {
+    using B = By<R>;
+    const bool touched = !MAPPED || a.drop.on;
+    const uint32_t tiles = shared_address(smem);
+    const uint64_t left0 = operand(tiles, ACROSS ? 8192 : 16), right0 = operand(tiles + 2 * kTileBytes, 16);
     int stage = 0, since = 0;
-    uint32_t here = 0, empty = 0, drained = 1;  // phases; nothing is to be drained at first
+    uint32_t here = 0, drained = 1;  // phases; nothing is to be drained at first
     for (int step = k.first, turn = 0; step < k.last; step += k.stride, ++turn) {
+        bool ok = true;
         if (since == 0) {
-            if (turn > 0) lost = !barrier_wait(bars + 8 * B::kDrained, drained);
+            if (turn > 0) ok = barrier_wait(bars + 8 * B::kDrained, drained);
             drained ^= 1u;
         }
-        lost = lost || !barrier_wait(bars + 8 * (B::kLanded + stage), here >> stage & 1u);
-        if (touched) lost = lost || !barrier_wait(bars + 8 * (B::kTouched + stage), here >> stage & 1u);
-        here ^= 1u << stage;
-        if (lost) break;
+        ok = ok && barrier_wait(bars + 8 * (B::kLanded + stage), here) && (!touched || barrier_wait(bars + 8 * (B::kTouched + stage), here));
+        if (!ok) {
+            gave_up = 1;
+            return;
+        }
         fence_after();
-        const uint32_t tiles = shared_address(smem + stage * B::kStageBytes), right = tiles + 2 * kTileBytes;
+        // addresses count 16 bytes in the operands' lowest bits
+        const uint64_t left = left0 + (uint32_t)(stage * (B::kStageBytes / 16)), right = right0 + (uint32_t)(stage * (B::kStageBytes / 16));
 #pragma unroll
-        for (int m = 0; m < 2; ++m)
+        for (int q = 0; q < 4; ++q)  // 16 of the 64
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {  // 16 of the 64
-                const uint64_t left = ACROSS ? operand(tiles + m * kTileBytes + q * 2048, 8192) : operand(tiles + m * kTileBytes + q * 32, 16);
-                product(memory + m * B::kN, left, operand(right + q * 32, 16), instruction(B::kN, ACROSS, false), since > 0 || q > 0);
-            }
+            for (int m = 0; m < 2; ++m)
+                product(memory + m * B::kN, left + (m * kTileBytes + q * (ACROSS ? 2048 : 32)) / 16, right + q * 2, instruction(B::kN, ACROSS, false),
+                        q > 0 || since > 0);
         products_done(bars + 8 * (B::kEmpty + stage));
         if (++since == kFlush || step + k.stride >= k.last) {
             since = 0;
             products_done(bars + 8 * B::kReady);
         }
-        // the stage before is free once its products are done
-        const int behind = stage == 0 ? B::kStages - 1 : stage - 1;
-        if (turn > 0) {
-            lost = !barrier_wait(bars + 8 * (B::kEmpty + behind), empty >> behind & 1u);
-            empty ^= 1u << behind;
-            if (lost) break;
+        if (++stage == B::kStages) {
+            stage = 0;
+            here ^= 1u;
         }
-        bring(step + (B::kStages - 1) * k.stride, behind);
-        stage = stage + 1 == B::kStages ? 0 : stage + 1;
     }
-    if (lost) gave_up = 1;
 }
 template <int R, bool MAPPED, bool ACROSS>
-__device__ __forceinline__ void issue(const Args& a, const CUtensorMap* map, const Walk& k, char* smem, uint32_t memory, uint32_t bars) {
-    if (threadIdx.x == 256) issue_alone<R, MAPPED, ACROSS>(a, map, k, smem, memory, bars);
+__device__ __forceinline__ void feed(const Args& a, const CUtensorMap* map, const Walk& k, char* smem, uint32_t memory, uint32_t bars) {
+    if (threadIdx.x == 256) issue<R, MAPPED, ACROSS>(a, k, smem, memory, bars);
+    if (threadIdx.x == 288) bring<R, MAPPED, ACROSS>(a, map, k, smem, bars);
     __syncwarp();
 }
 
@@ -434,7 +447,7 @@ __global__ void __launch_bounds__(kThreads, 1) down_kernel(const __grid_constant
     float sums[R];
     const Walk walk = {i, row0, 0, part, a.split, steps};
     if (main) sum_tiles<R, MAPPED, false>(a, walk, smem, memory, shared_address(bars), sums);
-    else issue<R, MAPPED, false>(a, &map, walk, smem, memory, shared_address(bars));
+    else feed<R, MAPPED, false>(a, &map, walk, smem, memory, shared_address(bars));
     tensor_end(memory, By<R>::kColumns);
     // this CTA's sums, then its share of the rows, joined over the cluster in order
     constexpr int L = R + 1;
@@ -505,7 +518,7 @@ __global__ void __launch_bounds__(kThreads, 1) outer_kernel(const __grid_constan
     float sums[R];
     const Walk walk = {i, 0, (int)blockIdx.x * 256, s0, 1, s1};
     if (threadIdx.x < 256) sum_tiles<R, MAPPED, true>(a, walk, smem, memory, shared_address(bars), sums);
-    else issue<R, MAPPED, true>(a, &map, walk, smem, memory, shared_address(bars));
+    else feed<R, MAPPED, true>(a, &map, walk, smem, memory, shared_address(bars));
     tensor_end(memory, By<R>::kColumns);
     const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (threadIdx.x >= 256 || c >= a.h) return;
