@@ -1077,7 +1077,7 @@ int tensor_prepare(const AdapterShape& z, bool shared, Factor down, int64_t down
     tensor::PrepareArgs p = {down, up, (char*)down_image, (char*)up_image, t, (char*)t_image, (int32_t)down_h, (int32_t)up_h, z.rank,
                              (uint32_t)z.rows, 0, 0, 0, shared};
     const int r = tensor::padded_rank(z.rank);
-    if (down_image) p.down_count = (uint32_t)((down_h + 63) / 64 * 8 * r);
+    if (down_image) p.down_count = (uint32_t)((down_h + 127) / 128 * 16 * r);
     if (up_image) p.up_count = (uint32_t)((up_h + 127) / 128 * 16 * r);
     if (t_image) p.t_count = (uint32_t)((z.rows + 63) / 64 * 8 * r);
     const uint64_t ctas = ((uint64_t)p.down_count + p.up_count + p.t_count + 255) / 256;
@@ -1093,15 +1093,17 @@ int tensor_down(Low low, Rows x, const AdapterShape& z, int64_t h, bool shared, 
     tensor::Args a = {};
     a.x = x.p; a.x_ws = x.worker_stride; a.x_rs = x.row_stride; a.image = (const char*)image; a.image_ws = shared ? 0 : tensor::down_image(h, z.rank);
     a.t_up = (char*)low.up; a.t_outer = (char*)low.outer; a.out = low.t; a.rows = (uint32_t)z.rows; a.h = (int32_t)h; a.rank = z.rank;
-    a.tiles = (a.rows + 255) / 256; a.scale = scale; a.drop = d;
-    a.split = (int32_t)parts_of((int64_t)a.tiles * z.n, 148, (h + 63) / 64, 4.0, 4, true);
-    const uint64_t ctas = (uint64_t)a.tiles * z.n * a.split;
-    if (ctas > 0x7fffffffu) return COMPAMS_ERR_TOO_LARGE;
+    a.scale = scale; a.drop = d;
     return by_rank(z, [&](auto v) {
         constexpr int R = decltype(v)::value;
+        using P = tensor::Pipe<R, false>;
+        a.tiles = (a.rows + P::kRows - 1) / P::kRows;
+        a.split = (int32_t)parts_of((int64_t)a.tiles * z.n, 148, (h + P::kStep - 1) / P::kStep, 4.0, 4, true);
+        const uint64_t ctas = (uint64_t)a.tiles * z.n * a.split;
+        if (ctas > 0x7fffffffu) return (int)COMPAMS_ERR_TOO_LARGE;
         CUtensorMap map;
         auto kernel = box_map(&map, x, z, h, 128) ? tensor::down_kernel<R, true> : tensor::down_kernel<R, false>;
-        return launched(launch_sized(kernel, dim3((uint32_t)ctas), tensor::kThreads, a.split, tensor::By<R>::kShared, false, stream, a, map),
+        return launched(launch_sized(kernel, dim3((uint32_t)ctas), tensor::kThreads, a.split, P::kShared, false, stream, a, map),
                         "adapter_down");
     });
 }
@@ -1131,7 +1133,7 @@ int tensor_outer(const AdapterArgs& b, Rows x, Low low, const AdapterShape& z, i
         constexpr int R = decltype(v)::value;
         CUtensorMap map;
         auto kernel = box_map(&map, x, z, h, 64) ? tensor::outer_kernel<R, true> : tensor::outer_kernel<R, false>;
-        return launched(launch_sized(kernel, dim3((uint32_t)((h + 255) / 256), (uint32_t)z.n * a.chunks), tensor::kThreads, 1, tensor::By<R>::kShared,
+        return launched(launch_sized(kernel, dim3((uint32_t)((h + 255) / 256), (uint32_t)z.n * a.chunks), tensor::kThreads, 1, tensor::Pipe<R, true>::kShared,
                                      first, stream, a, map),
                         "adapter_outer");
     });

@@ -34,13 +34,21 @@ template <int R>
 struct By {
     static constexpr int kN = 3 * R;                       // planes side by side
     static constexpr int kPlanesBytes = kN * 128;          // planes: rows of 64 elements
-    static constexpr int kStageBytes = 2 * kTileBytes + kPlanesBytes;
-    static constexpr int kStages = R == 64 ? 4 : 5;        // what 227 KB hold
-    static constexpr int kShared = 1024 + kStages * kStageBytes;
     static constexpr uint32_t kColumns = R == 64 ? 512 : R == 32 ? 256 : 128;  // of tensor memory: 2 kN used, a power of two taken
     // up: two planes of 128 rows; up to 32 they share the rows' 128 bytes
     static constexpr int kUpTiles = R == 64 ? 2 : 1, kUpBytes = kUpTiles * kTileBytes;
     static constexpr uint32_t kUpPlane = R == 64 ? kTileBytes : 2 * R;  // from plane 0 to plane 1
+};
+// The stages of down (ACROSS = false) and outer: two tiles of the activation, which go to a sum each, and planes. outer: 64 rows of 256
+// columns. down: 64 columns of 256 rows, or, up to rank 32, 128 columns of 128 rows (WIDE), whose two sums are of the same rows and are
+// added in the end: twice as many CTAs for a few thousand rows (4096 x 4096, rank 16: 15.5 -> 13.7 us), for planes read twice as often.
+template <int R, bool ACROSS>
+struct Pipe {
+    static constexpr bool kWide = !ACROSS && R <= 32;
+    static constexpr int kRows = ACROSS ? 0 : kWide ? 128 : 256, kStep = kWide ? 128 : 64;  // down: rows of a CTA; columns (outer: rows) of a step
+    static constexpr int kPlanesBytes = By<R>::kPlanesBytes * (kWide ? 2 : 1), kStageBytes = 2 * kTileBytes + kPlanesBytes;
+    static constexpr int kStages = kStageBytes * 5 > 225 * 1024 ? 4 : 5;  // what 227 KB hold
+    static constexpr int kShared = 1024 + kStages * kStageBytes;
     // The barriers: what is brought to a stage has landed; 256 threads have done their part on it; its products are done; the sums are
     // ready, and drained.
     static constexpr int kLanded = 0, kTouched = kStages, kEmpty = 2 * kStages, kReady = 3 * kStages, kDrained = 3 * kStages + 1,
@@ -49,12 +57,12 @@ struct By {
 
 // ---- images of the fp32 operands in global memory, in the order of shared memory --------------------------------------------
 
-// A factor for down: [64 columns][plane, rank][64 columns]; for up: [128 columns][plane 0, 1][column][rank] (the planes within a column's
+// A factor for down: [64 columns, an even number of times][plane, rank][64 columns]; for up: [128 columns][plane 0, 1][column][rank] (the planes within a column's
 // 128 bytes up to 32 ranks); bytes of a worker's.
-__host__ __device__ inline int64_t down_image(int64_t h, int rank) { return (h + 63) / 64 * (3 * 128 * padded_rank(rank)); }
+__host__ __device__ inline int64_t down_image(int64_t h, int rank) { return (h + 127) / 128 * (2 * 3 * 128 * padded_rank(rank)); }
 __host__ __device__ inline int64_t up_image(int64_t h, int rank) { return (h + 127) / 128 * (kTileBytes << (padded_rank(rank) == 64)); }
 // t for outer: [64 rows][plane, rank][row]; for up: [128 rows], as a factor's columns.
-__host__ __device__ inline int64_t t_outer_image(int64_t rows, int rank) { return down_image(rows, rank); }
+__host__ __device__ inline int64_t t_outer_image(int64_t rows, int rank) { return (rows + 63) / 64 * (3 * 128 * padded_rank(rank)); }
 __host__ __device__ inline int64_t t_up_image(int64_t rows, int rank) { return up_image(rows, rank); }
 
 __device__ __forceinline__ uint32_t swizzled(uint32_t row, uint32_t chunk) { return row * 128u + ((chunk ^ (row & 7u)) << 4); }
@@ -240,12 +248,12 @@ struct Args {
 constexpr int kThreads = 320;
 
 // Tensor memory and the barriers. The shared word that takes the address is the caller's.
-template <int R>
+template <typename P>
 __device__ __forceinline__ void tensor_begin(uint64_t* bars, uint32_t* word, uint32_t columns, uint32_t& memory) {
     if (threadIdx.x < 32) memory_alloc(shared_address(word), columns);
     if (threadIdx.x == 0) {
-        for (int k = 0; k < By<R>::kBars; ++k)
-            barrier_init(shared_address(bars + k), (k >= By<R>::kTouched && k < By<R>::kEmpty) || k == By<R>::kDrained ? 256u : 1u);
+        for (int k = 0; k < P::kBars; ++k)
+            barrier_init(shared_address(bars + k), (k >= P::kTouched && k < P::kEmpty) || k == P::kDrained ? 256u : 1u);
         fence_shared();
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -263,7 +271,7 @@ __device__ __forceinline__ void tensor_end(uint32_t memory, uint32_t columns) {
     if (threadIdx.x < 32) memory_free(memory, columns);
 }
 
-// What both parts walk: steps first, first + stride, ... below last of 64 columns (down: 256 rows from row0 on) or 64 rows (outer,
+// What the parts walk: steps first, first + stride, ... below last along the columns (down: rows from row0 on) or along the rows (outer,
 // ACROSS: 256 columns from column0 on).
 struct Walk {
     uint32_t worker, row0;
@@ -273,28 +281,29 @@ struct Walk {
 // The tenth warp's part. MAPPED: the activation is brought by TMA.
 template <int R, bool MAPPED, bool ACROSS>
 __device__ __forceinline__ void bring(const Args& a, const CUtensorMap* map, const Walk& k, char* smem, uint32_t bars) {
-    using B = By<R>;
+    using P = Pipe<R, ACROSS>;
     const char* image = a.image + (int64_t)k.worker * a.image_ws;
     int stage = 0;
     uint32_t empty = 1;  // the phase to wait for: of a stage's first round none
     for (int step = k.first, turn = 0; step < k.last; step += k.stride, ++turn) {
-        if (turn >= B::kStages && !barrier_wait(bars + 8 * (B::kEmpty + stage), empty)) {
+        if (turn >= P::kStages && !barrier_wait(bars + 8 * (P::kEmpty + stage), empty)) {
             gave_up = 1;
             return;
         }
-        const uint32_t bar = bars + 8 * (B::kLanded + stage), to = shared_address(smem + stage * B::kStageBytes);
-        mbar_expect(bar, B::kPlanesBytes + (MAPPED ? 2 * kTileBytes : 0));
+        const uint32_t bar = bars + 8 * (P::kLanded + stage), to = shared_address(smem + stage * P::kStageBytes);
+        mbar_expect(bar, P::kPlanesBytes + (MAPPED ? 2 * kTileBytes : 0));
         if (MAPPED) {
             if (ACROSS) {
 #pragma unroll
                 for (int c = 0; c < 4; ++c) box_load(to + c * 8192, map, k.column0 + c * 64, step * 64, (int)k.worker, bar);
             } else {
 #pragma unroll
-                for (int m = 0; m < 2; ++m) box_load(to + m * kTileBytes, map, step * 64, (int)k.row0 + m * 128, (int)k.worker, bar);
+                for (int m = 0; m < 2; ++m)
+                    box_load(to + m * kTileBytes, map, step * P::kStep + (P::kWide ? m * 64 : 0), (int)k.row0 + (P::kWide ? 0 : m * 128), (int)k.worker, bar);
             }
         }
-        bulk_load(smem + stage * B::kStageBytes + 2 * kTileBytes, image + (int64_t)step * B::kPlanesBytes, B::kPlanesBytes, bar);
-        if (++stage == B::kStages) {
+        bulk_load(smem + stage * P::kStageBytes + 2 * kTileBytes, image + (int64_t)step * P::kPlanesBytes, P::kPlanesBytes, bar);
+        if (++stage == P::kStages) {
             stage = 0;
             empty ^= 1u;
         }
@@ -304,7 +313,7 @@ __device__ __forceinline__ void bring(const Args& a, const CUtensorMap* map, con
 // The ninth warp's part.
 template <int R, bool MAPPED, bool ACROSS>
 __device__ __forceinline__ void issue(const Args& a, const Walk& k, char* smem, uint32_t memory, uint32_t bars) {
-    using B = By<R>;
+    using P = Pipe<R, ACROSS>;
     const bool touched = !MAPPED || a.drop.on;
     const uint32_t tiles = shared_address(smem);
     const uint64_t left0 = operand(tiles, ACROSS ? 8192 : 16), right0 = operand(tiles + 2 * kTileBytes, 16);
@@ -313,29 +322,29 @@ __device__ __forceinline__ void issue(const Args& a, const Walk& k, char* smem, 
     for (int step = k.first, turn = 0; step < k.last; step += k.stride, ++turn) {
         bool ok = true;
         if (since == 0) {
-            if (turn > 0) ok = barrier_wait(bars + 8 * B::kDrained, drained);
+            if (turn > 0) ok = barrier_wait(bars + 8 * P::kDrained, drained);
             drained ^= 1u;
         }
-        ok = ok && barrier_wait(bars + 8 * (B::kLanded + stage), here) && (!touched || barrier_wait(bars + 8 * (B::kTouched + stage), here));
+        ok = ok && barrier_wait(bars + 8 * (P::kLanded + stage), here) && (!touched || barrier_wait(bars + 8 * (P::kTouched + stage), here));
         if (!ok) {
             gave_up = 1;
             return;
         }
         fence_after();
         // addresses count 16 bytes in the operands' lowest bits
-        const uint64_t left = left0 + (uint32_t)(stage * (B::kStageBytes / 16)), right = right0 + (uint32_t)(stage * (B::kStageBytes / 16));
+        const uint64_t left = left0 + (uint32_t)(stage * (P::kStageBytes / 16)), right = right0 + (uint32_t)(stage * (P::kStageBytes / 16));
 #pragma unroll
         for (int q = 0; q < 4; ++q)  // 16 of the 64
 #pragma unroll
             for (int m = 0; m < 2; ++m)
-                product(memory + m * B::kN, left + (m * kTileBytes + q * (ACROSS ? 2048 : 32)) / 16, right + q * 2, instruction(B::kN, ACROSS, false),
+                product(memory + m * By<R>::kN, left + (m * kTileBytes + q * (ACROSS ? 2048 : 32)) / 16, right + (P::kWide ? m * By<R>::kPlanesBytes / 16 : 0) + q * 2, instruction(By<R>::kN, ACROSS, false),
                         q > 0 || since > 0);
-        products_done(bars + 8 * (B::kEmpty + stage));
+        products_done(bars + 8 * (P::kEmpty + stage));
         if (++since == kFlush || step + k.stride >= k.last) {
             since = 0;
-            products_done(bars + 8 * B::kReady);
+            products_done(bars + 8 * P::kReady);
         }
-        if (++stage == B::kStages) {
+        if (++stage == P::kStages) {
             stage = 0;
             here ^= 1u;
         }
@@ -348,11 +357,11 @@ __device__ __forceinline__ void feed(const Args& a, const CUtensorMap* map, cons
     __syncwarp();
 }
 
-// The first eight warps' part: sums[r] of a thread is rank r of row 128 (warp / 4) + 32 (warp % 4) + lane of the 256. Where there is
+// The first eight warps' part: sums[r] of a thread is rank r of row (outer: column) 32 (warp % 4) + lane of tile warp / 4. Where there is
 // something to do on the tiles a thread has a column of eight chunks, every 32nd row's (or 8th row's).
 template <int R, bool MAPPED, bool ACROSS>
 __device__ __forceinline__ void sum_tiles(const Args& a, const Walk& k, char* smem, uint32_t memory, uint32_t bars, float (&sums)[R]) {
-    using B = By<R>;
+    using P = Pipe<R, ACROSS>;
     constexpr uint32_t kRows = ACROSS ? 8 : 32, kPlace = ACROSS ? 1024 : 4096;  // from one of a thread's chunks to the next
     const int warp = threadIdx.x >> 5;
     const uint32_t r0 = ACROSS ? threadIdx.x >> 5 : threadIdx.x >> 3, c0 = ACROSS ? threadIdx.x & 31u : threadIdx.x & 7u;
@@ -362,7 +371,7 @@ __device__ __forceinline__ void sum_tiles(const Args& a, const Walk& k, char* sm
     const bool touch = !MAPPED || a.drop.on;
     bool lost = false;  // a wait gave up
     auto flush = [&]() {  // from tensor memory to the registers, the planes' together
-        const uint32_t at = memory + ((uint32_t)(warp & 3) << 21) + (uint32_t)(warp >> 2) * B::kN;
+        const uint32_t at = memory + ((uint32_t)(warp & 3) << 21) + (uint32_t)(warp >> 2) * By<R>::kN;
         constexpr int H = R == 64 ? 32 : R;  // columns at a time
 #pragma unroll
         for (int from = 0; from < R; from += H) {
@@ -385,29 +394,31 @@ __device__ __forceinline__ void sum_tiles(const Args& a, const Walk& k, char* sm
     uint32_t here = 0, empty = 0, ready = 0;  // phases
     for (int step = k.first, turn = 0; step < k.last; step += k.stride, ++turn) {
         if (touch) {
-            char* at = at0 + stage * B::kStageBytes;
+            char* at = at0 + stage * P::kStageBytes;
             const uint32_t row = (ACROSS ? (uint32_t)step * 64 : k.row0) + r0;
-            const int64_t column = (ACROSS ? (int64_t)k.column0 : (int64_t)step * 64) + c0 * 8;
+            const int64_t column0 = (ACROSS ? (int64_t)k.column0 : (int64_t)step * P::kStep) + c0 * 8;
             if (MAPPED) {
-                lost = lost || !barrier_wait(bars + 8 * (B::kLanded + stage), here >> stage & 1u);
-            } else if (turn >= B::kStages) {
-                lost = lost || !barrier_wait(bars + 8 * (B::kEmpty + stage), empty >> stage & 1u);
+                lost = lost || !barrier_wait(bars + 8 * (P::kLanded + stage), here >> stage & 1u);
+            } else if (turn >= P::kStages) {
+                lost = lost || !barrier_wait(bars + 8 * (P::kEmpty + stage), empty >> stage & 1u);
                 empty ^= 1u << stage;
             }
             here ^= 1u << stage;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 uint4* place = reinterpret_cast<uint4*>(at + e * kPlace);
+                const uint32_t j = row + (P::kWide ? e & 3 : e) * kRows;
+                const int64_t column = column0 + (P::kWide ? (e >> 2) * 64 : 0);
                 Raw8<__nv_bfloat16> raw;
                 if (MAPPED) {
                     raw.q = *place;
                 } else {
-                    const bool in = row + e * kRows < a.rows;
-                    raw = raw_columns<__nv_bfloat16, false>(x + (in ? (int64_t)(row + e * kRows) * a.x_rs : 0), (int)min(column, (int64_t)a.h),
+                    const bool in = j < a.rows;
+                    raw = raw_columns<__nv_bfloat16, false>(x + (in ? (int64_t)j * a.x_rs : 0), (int)min(column, (int64_t)a.h),
                                                             in ? a.h : 0);
                 }
                 if (a.drop.on) {
-                    const uint4 u = drop_words(a.drop, (uint32_t)(column >> 3), row + e * kRows, a.drop.worker + k.worker, call);
+                    const uint4 u = drop_words(a.drop, (uint32_t)(column >> 3), j, a.drop.worker + k.worker, call);
                     uint32_t w[1][4];
                     raw_planes<__nv_bfloat16>(raw, a.drop, u, w);
                     raw.q = make_uint4(w[0][0], w[0][1], w[0][2], w[0][3]);
@@ -415,34 +426,35 @@ __device__ __forceinline__ void sum_tiles(const Args& a, const Walk& k, char* sm
                 *place = raw.q;
             }
             fence_shared();
-            barrier_arrive(bars + 8 * (B::kTouched + stage));
+            barrier_arrive(bars + 8 * (P::kTouched + stage));
         }
         if (++since == kFlush || step + k.stride >= k.last) {
             since = 0;
-            lost = lost || !barrier_wait(bars + 8 * B::kReady, ready);
+            lost = lost || !barrier_wait(bars + 8 * P::kReady, ready);
             ready ^= 1u;
             fence_after();
             flush();
             fence_before();
-            barrier_arrive(bars + 8 * B::kDrained);
+            barrier_arrive(bars + 8 * P::kDrained);
         }
-        stage = stage + 1 == B::kStages ? 0 : stage + 1;
+        stage = stage + 1 == P::kStages ? 0 : stage + 1;
     }
     if (lost) gave_up = 1;
 }
 
-// A CTA takes 256 rows of a worker and its share of the columns.
+// A CTA takes 256 rows of a worker, or 128 (WIDE), and its share of the columns.
 template <int R, bool MAPPED>
 __global__ void __launch_bounds__(kThreads, 1) down_kernel(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap map) {
     extern __shared__ __align__(16) char dynamic[];
-    __shared__ uint64_t bars[By<R>::kBars];
+    using P = Pipe<R, false>;
+    __shared__ uint64_t bars[P::kBars];
     __shared__ uint32_t word;
     dependency_wait();
     uint32_t memory;
     char* smem = aligned(dynamic);
-    tensor_begin<R>(bars, &word, By<R>::kColumns, memory);
-    const uint32_t tile = blockIdx.x / a.split, i = tile / a.tiles, row0 = (tile - i * a.tiles) * 256;
-    const int part = (int)(blockIdx.x - tile * a.split), steps = (a.h + 63) / 64;
+    tensor_begin<P>(bars, &word, By<R>::kColumns, memory);
+    const uint32_t tile = blockIdx.x / a.split, i = tile / a.tiles, row0 = (tile - i * a.tiles) * P::kRows;
+    const int part = (int)(blockIdx.x - tile * a.split), steps = (a.h + P::kStep - 1) / P::kStep;
     const bool main = threadIdx.x < 256;
     float sums[R];
     const Walk walk = {i, row0, 0, part, a.split, steps};
@@ -458,18 +470,21 @@ __global__ void __launch_bounds__(kThreads, 1) down_kernel(const __grid_constant
     cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
     cluster.sync();
     const float scale = a.scale * (a.drop.on ? a.drop.factor : 1.0f);
-    const int share = 256 / a.split, from = part * share;  // split is a power of two up to 8: a share is 32 rows at least
+    const int share = P::kRows / a.split, from = part * share;  // split is a power of two up to 8: a share is 16 rows at least
     for (int e = threadIdx.x; e < share * R; e += kThreads) {
         const int r = e / R, j = e % R;
-        float part[8], v = 0.0f;
+        float sum[8], v = 0.0f;
 #pragma unroll
-        for (int s = 0; s < 8; ++s) part[s] = s < a.split ? cluster.map_shared_rank(mine, s)[(from + r) * L + j] : 0.0f;
+        for (int s = 0; s < 8; ++s) {
+            const float* at = s < a.split ? cluster.map_shared_rank(mine, s) + (from + r) * L + j : nullptr;
+            sum[s] = at ? (P::kWide ? at[0] + at[128 * L] : at[0]) : 0.0f;
+        }
 #pragma unroll
-        for (int s = 0; s < 8; ++s) v += part[s];
+        for (int s = 0; s < 8; ++s) v += sum[s];
         whole[r * L + j] = scale * v;
     }
     __syncthreads();
-    const uint32_t first = row0 + from;  // a multiple of 64
+    const uint32_t first = row0 + from;  // a multiple of 16
     if (a.out)
         for (int e = threadIdx.x; e < share * R; e += kThreads) {
             const int r = e / R, j = e % R;
@@ -507,12 +522,13 @@ __global__ void __launch_bounds__(kThreads, 1) down_kernel(const __grid_constant
 template <int R, bool MAPPED>
 __global__ void __launch_bounds__(kThreads, 1) outer_kernel(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap map) {
     extern __shared__ __align__(16) char dynamic[];
-    __shared__ uint64_t bars[By<R>::kBars];
+    using P = Pipe<R, true>;
+    __shared__ uint64_t bars[P::kBars];
     __shared__ uint32_t word;
     dependency_wait();
     uint32_t memory;
     char* smem = aligned(dynamic);
-    tensor_begin<R>(bars, &word, By<R>::kColumns, memory);
+    tensor_begin<P>(bars, &word, By<R>::kColumns, memory);
     const uint32_t i = blockIdx.y / a.chunks, chunk = blockIdx.y - i * a.chunks, blocks = (a.rows + 63) / 64;
     const int s0 = (int)((uint64_t)blocks * chunk / a.chunks), s1 = (int)((uint64_t)blocks * (chunk + 1) / a.chunks);
     float sums[R];
@@ -563,18 +579,19 @@ __global__ void __launch_bounds__(256, 2) up_kernel(const __grid_constant__ UpAr
     using B = By<R>;
     constexpr int CN = up_columns<R>(), kRow = 2 * CN, kPlaneBytes = CN * 128;  // bytes of a tile's row; of a plane of the factor (R = 64)
     constexpr uint32_t kMemory = CN;
+    using P = Pipe<R, true>;
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + up_shared<R>() - 256);
-    uint32_t* word = reinterpret_cast<uint32_t*>(bars + B::kBars);
+    uint32_t* word = reinterpret_cast<uint32_t*>(bars + P::kBars);
     bool lost = false;  // a wait gave up
     dependency_wait();
     uint32_t memory;
-    tensor_begin<R>(bars, word, kMemory, memory);
+    tensor_begin<P>(bars, word, kMemory, memory);
     // tile: 128 rows, chunk c at c ^ (row % 8)
     char *planes = smem, *t0 = smem + B::kUpTiles * kPlaneBytes, *tile0 = t0 + 2 * B::kUpBytes;
     const uint32_t i = blockIdx.y / a.chunks, chunk = blockIdx.y - i * a.chunks, blocks = (a.rows + 127) / 128;
     const uint32_t b0 = (uint32_t)((uint64_t)blocks * chunk / a.chunks), b1 = (uint32_t)((uint64_t)blocks * (chunk + 1) / a.chunks);
     const int c0 = (int)blockIdx.x * CN, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t call = drop_call(a.drop), bar = shared_address(bars + B::kReady);
+    const uint32_t call = drop_call(a.drop), bar = shared_address(bars + P::kReady);
     const __nv_bfloat16* base = (const __nv_bfloat16*)a.base + (int64_t)i * a.base_ws;
     __nv_bfloat16* y = (__nv_bfloat16*)a.y + (int64_t)i * a.rows * a.h;
     const char* t_image = a.t_up + i * t_up_image(a.rows, R);
