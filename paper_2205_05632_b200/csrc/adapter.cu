@@ -24,6 +24,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <atomic>
 #include <type_traits>
 
 #include "context.h"
@@ -992,12 +993,26 @@ int by_type(int32_t type, F f) {
 }
 int launched(cudaError_t e, const char* what) { return e == cudaSuccess ? COMPAMS_OK : cuda_fail(e, what); }
 
+// Lets a kernel have more than 48 KB of shared memory: asked once for every kernel and device (a kernel's size is always the same).
+cudaError_t allow_shared(const void* kernel, size_t bytes) {
+    static std::atomic<uint64_t> known[1024];
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    const uint64_t key = (uint64_t)(uintptr_t)kernel ^ (uint64_t)(device + 1) << 56;
+    std::atomic<uint64_t>& slot = known[(key * 0x9E3779B97F4A7C15ull) >> 54];
+    if (slot.load(std::memory_order_relaxed) == key) return cudaSuccess;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e == cudaSuccess) slot.store(key, std::memory_order_relaxed);
+    return e;
+}
+
 // A launch behind another of the same call (or the first), with dynamic shared memory and a cluster along x.
 template <typename... KArgs, typename... Args>
 cudaError_t launch_sized(void (*kernel)(KArgs...), dim3 grid, int threads, int cluster, size_t shared, bool first, cudaStream_t stream,
                          Args... args) {
     if (shared > 48 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared);
+        const cudaError_t e = allow_shared((const void*)kernel, shared);
         if (e != cudaSuccess) return e;
     }
     cudaLaunchConfig_t cfg = {};
