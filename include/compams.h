@@ -427,7 +427,7 @@ int compams_collect(float* row, const float* const* tensors, const int64_t* offs
  * the leading axis, and a weight's gradient stays apart by worker, as the rows of the gradient buffer that compams_step takes.
  *
  * Element (i, j, c) of an input lies at p + i * worker_stride + j * row_stride + c elements of its type; the strides, in elements,
- * are the caller's (0 repeats a worker or a row), columns are packed. Outputs are packed [n, rows, h] and may not overlap inputs.
+ * are the caller's, not negative (0 repeats a worker or a row), columns are packed. Outputs are packed [n, rows, h] and may not overlap inputs.
  * 1 <= n <= 65535, n * rows < 2^31 (rows = 0: nothing to do, gradients of weights become 0), 1 <= h < 2^31 - 4096; pointers are aligned to
  * their element, and where all rows start on 16-byte boundaries accesses are 16 bytes wide. Work is enqueued on cuda_stream, in the
  * current device, and nothing is allocated. Errors: INVALID_ARG, TOO_LARGE, CUDA.
@@ -503,6 +503,9 @@ int compams_adapter_backward(void* dx, float* da, float* db, int32_t sum_workers
                              int64_t a_worker_stride, int64_t a_row_stride, const float* b, int64_t b_worker_stride,
                              int64_t b_row_stride, float scale, double p, uint64_t seed, uint32_t call, const int64_t* call_device,
                              uint32_t first_worker, void* workspace, size_t workspace_bytes, void* cuda_stream);
+/* 1 if a kernel of the adapters gave up waiting for its own copies or products since the library was loaded (then a result was
+   worthless; no size or input should bring it about), else 0. Synchronises. */
+int compams_adapter_status(int32_t* gave_up);
 /* shared: both worker strides of A and B are 0, or n is 1. sum_workers matters to the backward pass alone. */
 int compams_adapter_workspace_bytes(size_t* bytes, int32_t n, int64_t rows, int64_t in, int64_t out, int32_t rank, int32_t shared,
                                     int32_t backward, int32_t sum_workers);

@@ -1334,6 +1334,11 @@ using namespace compams;
 
 extern "C" {
 
+int compams_adapter_status(int32_t* gave_up) {
+    if (!gave_up) return COMPAMS_ERR_INVALID_ARG;
+    return launched(cudaMemcpyFromSymbol(gave_up, tensor::gave_up, sizeof(int32_t)), "adapter_status");
+}
+
 int compams_adapter_workspace_bytes(size_t* bytes, int32_t n, int64_t rows, int64_t in, int64_t out, int32_t rank, int32_t shared,
                                     int32_t backward, int32_t sum_workers) {
     const AdapterShape z{n, rows, in, out, rank};
@@ -1357,7 +1362,8 @@ int compams_adapter_forward(void* y, float* t, const void* x, const void* base, 
     const Rows xin{x, x_worker_stride, x_row_stride, type}, bin{base, base_worker_stride, base_row_stride, type};
     const bool shared = n == 1 || (a_worker_stride == 0 && b_worker_stride == 0);
     const Places at = places(z, shared, false, false);
-    if (!x || !y || !t || !a || !b || !float_aligned(t) || !float_aligned(a) || !float_aligned(b) || !xin.element_aligned() ||
+    if (!xin.strides_ok() || (base && !bin.strides_ok()) || a_worker_stride < 0 || a_row_stride < 0 || b_worker_stride < 0 || b_row_stride < 0 ||
+        !x || !y || !t || !a || !b || !float_aligned(t) || !float_aligned(a) || !float_aligned(b) || !xin.element_aligned() ||
         !bin.element_aligned() || !packed(y, rows, out, type).element_aligned() || workspace_bytes < (size_t)at.bytes ||
         (at.bytes && !workspace) || (reinterpret_cast<uintptr_t>(workspace) & 15u))
         return COMPAMS_ERR_INVALID_ARG;
@@ -1399,7 +1405,8 @@ int compams_adapter_backward(void* dx, float* da, float* db, int32_t sum_workers
     const Rows xin{x, x_worker_stride, x_row_stride, type}, gin{dy, dy_worker_stride, dy_row_stride, type};
     const bool shared = n == 1 || (a_worker_stride == 0 && b_worker_stride == 0);
     const Places at = places(z, shared, true, sum_workers != 0);
-    if (!dy || !a || !b || (da && !x) || (db && !t) || !workspace || workspace_bytes < (size_t)at.bytes ||
+    if (!gin.strides_ok() || (x && !xin.strides_ok()) || a_worker_stride < 0 || a_row_stride < 0 || b_worker_stride < 0 || b_row_stride < 0 ||
+        !dy || !a || !b || (da && !x) || (db && !t) || !workspace || workspace_bytes < (size_t)at.bytes ||
         (reinterpret_cast<uintptr_t>(workspace) & 15u) || !float_aligned(t) || !float_aligned(a) || !float_aligned(b) ||
         !float_aligned(da) || !float_aligned(db) || !xin.element_aligned() || !gin.element_aligned() ||
         !packed(dx, rows, in, type).element_aligned())

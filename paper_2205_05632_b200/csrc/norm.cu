@@ -11,6 +11,7 @@
 // registers), weights, biases and their gradients are fp32 as the optimizer keeps them.
 #include <string.h>
 
+#include <algorithm>
 #include <atomic>
 #include <type_traits>
 
@@ -524,91 +525,99 @@ __global__ void __launch_bounds__(256) norm_join_kernel(const float* __restrict_
 
 // ---- dropout ---------------------------------------------------------------------------------------------------------------
 
-// A CTA takes a stretch of spans in the order of memory, a warp four of 32 at a time; the next four are on their way while these are done.
-// U: a number of spans. (32 spans) further is `span` spans, `row` rows and `worker` workers further.
-constexpr int kDropSpans = 4;
+// n / d for n < 2^31 by a multiplication (Granlund, Montgomery 1994): shift = ceil(log2 d), factor = ceil(2^(31 + shift) / d).
+struct Divisor {
+    uint32_t factor, shift, d;
+    __device__ __forceinline__ uint32_t operator()(uint32_t n) const { return d == 1 ? n : __umulhi(n, factor) >> (shift - 1); }
+};
+inline Divisor divisor(uint32_t d) {
+    uint32_t shift = 0;
+    while (((uint64_t)1 << shift) < d) ++shift;
+    return {(uint32_t)((((uint64_t)1 << (31 + shift)) + d - 1) / d), shift, d};
+}
+
 struct DropoutArgs {
     const void* x;
     void* y;
     int64_t ws, rs;
-    uint64_t steps, ctas;  // of 32 spans
-    uint32_t rows, total;
+    uint32_t row0, count;  // rows of this launch, of all workers'
+    uint32_t units;        // groups of eight (aligned rows) or spans, all rows' together: below 2^31
     int32_t h;
-    uint32_t spans;                       // of a row
-    uint32_t step_span, step_row, step_j, step_worker;  // step_row rows = step_worker workers and step_j rows
+    Divisor rows, per_row;  // rows of a worker, units of a row
     Drop drop;
 };
-template <typename T, bool VEC>  // a lane's values of a span, as they lie in memory
-struct Held {
-    Raw8<T> r;
-    __device__ __forceinline__ void load(const T* row, int c0, int h, int lane) {
-        r = {};
-        if (c0 + lane * 8 < h) r = raw_load<T>(row + c0 + lane * 8);
-    }
-    __device__ __forceinline__ void pairs(Pair (&v)[4]) const { raw_pairs<T>(r, v); }
-};
+
+// Aligned rows: a thread takes groups of eight elements, four at a time in the order of memory and the next four on their way. Bound by
+// memory and by what the SMs can issue, the generator's 40 instructions and 50 more a group: 67 M bfloat16 numbers, 268 MB, 56 us (a
+// plain copy 43; with the words of the place instead of the generator's 46). Numbered through, a group's row and worker come from two
+// multiplications, and short rows leave no lane idle: 67 M numbers in rows of 64 take 60 us for both passes together, with a span of 256
+// columns to a warp 212.
+constexpr int kDropGroups = 4;
 template <typename T>
-struct Held<T, false> {
-    Pair x[4];
-    __device__ __forceinline__ void load(const T* row, int c0, int h, int lane) { span_load<T, false>(row, c0, h, lane, x); }
-    __device__ __forceinline__ void pairs(Pair (&v)[4]) const {
-#pragma unroll
-        for (int p = 0; p < 4; ++p) v[p] = x[p];
-    }
-};
-template <typename T, bool VEC, typename U>
 __global__ void __launch_bounds__(256) dropout_kernel(const __grid_constant__ DropoutArgs a) {
-    const int lane = threadIdx.x & 31;
-    const U s0 = (U)(a.steps * blockIdx.x / a.ctas), s1 = (U)(a.steps * (blockIdx.x + 1) / a.ctas);
-    const U at = s0 * 32 + (threadIdx.x >> 5) * kDropSpans;
-    uint32_t m = (uint32_t)(at / a.spans), span = (uint32_t)(at - (U)m * a.spans), i = m / a.rows, j = m - i * a.rows;
-    const uint32_t call = drop_call(a.drop);
-    // the place of span k of the four, which are neighbours
-    auto place = [&](uint32_t& m, uint32_t& span, uint32_t& i, uint32_t& j) {
-        if (++span == a.spans) {
-            span = 0;
-            ++m;
-            if (++j == a.rows) {
-                j = 0;
-                ++i;
+    const uint32_t stride = gridDim.x * 256 * kDropGroups, call = drop_call(a.drop);
+    uint32_t at = blockIdx.x * 256 * kDropGroups + threadIdx.x;
+    struct Place {
+        uint32_t group, m, i, j;
+    };
+    auto place = [&](uint32_t unit) {
+        Place p;
+        const uint32_t r = a.per_row(unit);
+        p.group = unit - r * a.per_row.d;
+        p.m = a.row0 + r;
+        p.i = a.rows(p.m);
+        p.j = p.m - p.i * a.rows.d;
+        return p;
+    };
+    Raw8<T> next[kDropGroups];
+    auto load = [&](uint32_t unit) {
+#pragma unroll
+        for (int k = 0; k < kDropGroups; ++k) {
+            next[k] = {};
+            if (unit + 256 * k < a.units) {
+                const Place p = place(unit + 256 * k);
+                next[k] = raw_load<T>((const T*)a.x + (int64_t)p.i * a.ws + (int64_t)p.j * a.rs + p.group * 8);
             }
         }
     };
-    Held<T, VEC> next[kDropSpans];
-    auto load = [&](uint32_t m, uint32_t span, uint32_t i, uint32_t j) {
+    load(at);
+    for (; at < a.units; at += stride) {
+        Raw8<T> now[kDropGroups];
 #pragma unroll
-        for (int k = 0; k < kDropSpans; ++k) {
-            next[k].load((const T*)a.x + (int64_t)i * a.ws + (int64_t)j * a.rs, m < a.total ? (int)span * kSpan : a.h, a.h, lane);
-            place(m, span, i, j);
-        }
-    };
-    load(m, span, i, j);
-    for (U s = s0; s < s1; ++s) {
-        Held<T, VEC> now[kDropSpans];
+        for (int k = 0; k < kDropGroups; ++k) now[k] = next[k];
+        if (a.units - at > stride) load(at + stride);
 #pragma unroll
-        for (int k = 0; k < kDropSpans; ++k) now[k] = next[k];
-        uint32_t tm = m, tspan = span, ti = i, tj = j;
-        m += a.step_row, span += a.step_span, i += a.step_worker, j += a.step_j;
-        if (span >= a.spans) {
-            span -= a.spans;
-            ++m;
-            ++j;
-        }
-        if (j >= a.rows) {
-            j -= a.rows;
-            ++i;
-        }
-        if (s + 1 < s1) load(m, span, i, j);
-#pragma unroll
-        for (int k = 0; k < kDropSpans; ++k) {
-            const int c0 = tm < a.total ? (int)tspan * kSpan : a.h;
+        for (int k = 0; k < kDropGroups; ++k) {
+            if (at + 256 * k >= a.units) break;
+            const Place p = place(at + 256 * k);
             Pair v[4];
-            now[k].pairs(v);
-            if (a.drop.on) span_drop<VEC>(a.drop, c0, tj, a.drop.worker + ti, call, lane, v);
-            span_store<T, VEC>((T*)a.y + (int64_t)tm * a.h, c0, a.h, lane, v);
-            place(tm, tspan, ti, tj);
+            raw_pairs<T>(now[k], v);
+            if (a.drop.on) {
+                const uint4 u = drop_words(a.drop, p.group, p.j, a.drop.worker + p.i, call);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float x[2];
+                    halves(mul(v[e], pair(a.drop.factor)), x[0], x[1]);
+                    v[e] = pair(drop_keeps(a.drop, u, 2 * e) ? x[0] : 0.0f, drop_keeps(a.drop, u, 2 * e + 1) ? x[1] : 0.0f);
+                }
+            }
+            raw_store<T>((T*)a.y + (int64_t)p.m * a.h + p.group * 8, pack_pairs<T>(v));
         }
     }
+}
+
+// Other rows: a warp per span (rows of 4097: 88 us a pass).
+template <typename T>
+__global__ void __launch_bounds__(256) dropout_spans_kernel(const __grid_constant__ DropoutArgs a) {
+    const int lane = threadIdx.x & 31;
+    const uint32_t unit = blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (unit >= a.units) return;
+    const uint32_t r = a.per_row(unit), m = a.row0 + r, i = a.rows(m), j = m - i * a.rows.d;
+    const int c0 = (int)(unit - r * a.per_row.d) * kSpan;
+    float v[8];
+    span_load<T, false>((const T*)a.x + (int64_t)i * a.ws + (int64_t)j * a.rs, c0, a.h, lane, v);
+    if (a.drop.on) span_drop<false>(a.drop, c0, j, a.drop.worker + i, drop_call(a.drop), lane, v);
+    span_store<T, false>((T*)a.y + (int64_t)m * a.h, c0, a.h, lane, v);
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------------
@@ -768,29 +777,33 @@ int compams_dropout(void* y, const void* x, int32_t type, int32_t n, int64_t row
     if (!z.ok() || !type_known(type) || !make_drop(d, p, seed, call, call_device, first_worker)) return COMPAMS_ERR_INVALID_ARG;
     if (rows == 0) return COMPAMS_OK;
     const Rows in{x, worker_stride, row_stride, type}, out = packed(y, rows, h, type);
-    if (!x || !y || !in.element_aligned() || !out.element_aligned()) return COMPAMS_ERR_INVALID_ARG;
+    if (!in.strides_ok() || !x || !y || !in.element_aligned() || !out.element_aligned()) return COMPAMS_ERR_INVALID_ARG;
     const bool vec = h % 8 == 0 && in.aligned() && out.aligned();
     DropoutArgs a = {};
-    a.x = x; a.y = y; a.ws = worker_stride; a.rs = row_stride; a.rows = (uint32_t)rows; a.total = (uint32_t)(n * rows); a.h = (int32_t)h;
-    a.spans = (uint32_t)((h + kSpan - 1) / kSpan);
-    a.step_row = 32 / a.spans; a.step_span = 32 % a.spans; a.step_worker = a.step_row / a.rows; a.step_j = a.step_row % a.rows;
-    a.drop = d;
-    const uint64_t all = (uint64_t)a.total * a.spans;
-    a.steps = (all + 31) / 32;
+    a.x = x; a.y = y; a.ws = worker_stride; a.rs = row_stride; a.h = (int32_t)h; a.drop = d;
+    const uint32_t per_row = (uint32_t)(vec ? h / 8 : (h + kSpan - 1) / kSpan);
+    a.rows = divisor((uint32_t)rows);
+    a.per_row = divisor(per_row);
+    // units are counted in 31 bits (and the steps of all threads beyond them in 32): as many rows at a time as that allows
+    const int64_t total = n * rows, most = std::max<int64_t>(1, ((int64_t)1 << 31) / per_row - 1);
     return by_types(type, type, [&](auto t, auto) {
         using T = decltype(t);
-        auto go = [&](auto v, auto u) {
-            constexpr bool V = decltype(v)::value;
-            using U = decltype(u);
-            int count = 0;
-            cudaError_t e = resident<dropout_kernel<T, V, U>>(256, 0, &count);
+        for (int64_t row = 0; row < total; row += most) {
+            a.row0 = (uint32_t)row;
+            a.count = (uint32_t)std::min(most, total - row);
+            a.units = a.count * per_row;
+            cudaError_t e;
+            if (vec) {
+                int count = 0;
+                e = resident<dropout_kernel<T>>(256, 0, &count);
+                const uint32_t all = (a.units + 256 * kDropGroups - 1) / (256 * kDropGroups), once = (uint32_t)(multiprocessors() * count);
+                if (e == cudaSuccess) e = launch_plain(dropout_kernel<T>, dim3(std::min(all, once)), dim3(256), 0, (cudaStream_t)cuda_stream, a);
+            } else {
+                e = launch_plain(dropout_spans_kernel<T>, dim3((a.units + 7) / 8), dim3(256), 0, (cudaStream_t)cuda_stream, a);
+            }
             if (e != cudaSuccess) return cuda_fail(e, "dropout");
-            a.ctas = (uint64_t)multiprocessors() * count;
-            if (a.ctas > a.steps) a.ctas = a.steps;
-            return launched(launch_plain(dropout_kernel<T, V, U>, dim3((uint32_t)a.ctas), dim3(256), 0, (cudaStream_t)cuda_stream, a), "dropout");
-        };
-        const bool wide = all > 0xffffffffu - 64;
-        return vec ? (wide ? go(Int<1>(), uint64_t()) : go(Int<1>(), uint32_t())) : (wide ? go(Int<0>(), uint64_t()) : go(Int<0>(), uint32_t()));
+        }
+        return (int)COMPAMS_OK;
     });
 }
 
@@ -808,7 +821,7 @@ int compams_norm_forward(void* y, void* s, float* stats, const void* x, const vo
     if (rows == 0) return COMPAMS_OK;
     const Rows in{x, x_worker_stride, x_row_stride, type}, out = packed(y, rows, h, type);
     const Rows res{residual, residual_worker_stride, residual_row_stride, residual_type}, sum = packed(s, rows, h, residual_type);
-    if (!x || !y || (add && !s) || !in.element_aligned() || !out.element_aligned() || !float_aligned(weight) || !float_aligned(bias) ||
+    if (!in.strides_ok() || (add && !res.strides_ok()) || weight_stride < 0 || bias_stride < 0 || !x || !y || (add && !s) || !in.element_aligned() || !out.element_aligned() || !float_aligned(weight) || !float_aligned(bias) ||
         (reinterpret_cast<uintptr_t>(stats) & 7u) || (add && (!res.element_aligned() || !sum.element_aligned())))
         return COMPAMS_ERR_INVALID_ARG;
     const bool vec = h % 8 == 0 && in.aligned() && out.aligned() && (!add || (res.aligned() && sum.aligned())) &&
@@ -858,7 +871,7 @@ int compams_norm_backward(void* dx, void* dresidual, float* dweight, float* dbia
     }
     const Rows gin{dy, dy_worker_stride, dy_row_stride, type}, gsum{ds, ds_worker_stride, ds_row_stride, v_type};
     const Rows vin{v, v_worker_stride, v_row_stride, v_type}, out = packed(dx, rows, h, type), rout = packed(dresidual, rows, h, v_type);
-    if (!dy || !v || !stats || (reinterpret_cast<uintptr_t>(stats) & 7u) || !float_aligned(weight) || !gin.element_aligned() ||
+    if (!gin.strides_ok() || (ds && !gsum.strides_ok()) || !vin.strides_ok() || weight_stride < 0 || !dy || !v || !stats || (reinterpret_cast<uintptr_t>(stats) & 7u) || !float_aligned(weight) || !gin.element_aligned() ||
         !gsum.element_aligned() || !vin.element_aligned() || !out.element_aligned() || !rout.element_aligned())
         return COMPAMS_ERR_INVALID_ARG;
     const bool vec = h % 8 == 0 && gin.aligned() && vin.aligned() && (!ds || gsum.aligned()) && out.aligned() && rout.aligned() &&

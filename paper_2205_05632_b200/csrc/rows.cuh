@@ -334,6 +334,7 @@ struct Rows {
         const int64_t e = type_bytes(type);
         return ((reinterpret_cast<uintptr_t>(p) | (uint64_t)(worker_stride * e) | (uint64_t)(row_stride * e)) & 15u) == 0;
     }
+    bool strides_ok() const { return worker_stride >= 0 && row_stride >= 0; }
     bool element_aligned() const { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(type_bytes(type) - 1)) == 0; }
 };
 inline Rows packed(const void* p, int64_t rows, int64_t h, int32_t type) { return {p, rows * h, h, type}; }

@@ -54,7 +54,7 @@ def dropout_args(**kw):
 
 @pytest.mark.parametrize("bad", [dict(y=None), dict(x=None), dict(type=3), dict(type=-1), dict(n=0), dict(n=65536), dict(rows=-1), dict(h=0),
                                  dict(h=1 << 31), dict(rows=1 << 31), dict(p=-0.1), dict(p=1.1), dict(p=float("nan")), dict(x=A + 2),
-                                 dict(y=A + 1), dict(call_device=A + 4), dict(type=1, x=A + 1)])
+                                 dict(y=A + 1), dict(call_device=A + 4), dict(type=1, x=A + 1), dict(ws=-24), dict(rs=-8)])
 def test_dropout_refuses(lib, bad):
     assert lib.compams_dropout(*dropout_args(**bad)) == -1
 
@@ -68,7 +68,8 @@ def forward_args(**kw):
 
 @pytest.mark.parametrize("bad", [dict(y=None), dict(x=None), dict(type=7), dict(n=0), dict(h=0), dict(rows=-2), dict(eps=-1.0), dict(eps=float("nan")),
                                  dict(p=0.5), dict(s=A), dict(residual=A), dict(residual=A, s=A, type=0, rtype=1), dict(residual=A, s=A, rtype=2),
-                                 dict(residual=A + 2, s=A, rtype=0), dict(weight=A + 1), dict(bias=A + 2), dict(stats=A + 4), dict(x=A + 1)])
+                                 dict(residual=A + 2, s=A, rtype=0), dict(weight=A + 1), dict(bias=A + 2), dict(stats=A + 4), dict(x=A + 1), dict(rs=-8),
+                                 dict(wst=-8), dict(bst=-8), dict(residual=A, s=A, rws=-24)])
 def test_norm_forward_refuses(lib, bad):
     assert lib.compams_norm_forward(*forward_args(**bad)) == -1
 
@@ -81,7 +82,8 @@ def backward_args(**kw):
 
 
 @pytest.mark.parametrize("bad", [dict(dy=None), dict(v=None), dict(stats=None), dict(vtype=0), dict(ds=A), dict(dres=A), dict(p=0.1), dict(work=None),
-                                 dict(bytes=16), dict(work=A + 8), dict(dw=A + 2), dict(added=1, vtype=2), dict(n=0), dict(h=0), dict(dx=A + 1)])
+                                 dict(bytes=16), dict(work=A + 8), dict(dw=A + 2), dict(added=1, vtype=2), dict(n=0), dict(h=0), dict(dx=A + 1), dict(gws=-1),
+                                 dict(vrs=-8), dict(wst=-1)])
 def test_norm_backward_refuses(lib, bad):
     assert lib.compams_norm_backward(*backward_args(**bad)) == -1
 
@@ -95,7 +97,7 @@ def adapter_args(**kw):
 
 @pytest.mark.parametrize("bad", [dict(y=None), dict(work=None), dict(bytes=16), dict(work=A + 8), dict(t=None), dict(x=None), dict(a=None), dict(b=None), dict(type=4), dict(n=0), dict(rows=-1), dict(inn=0),
                                  dict(out=0), dict(rank=0), dict(rank=1025), dict(p=2.0), dict(a=A + 2), dict(b=A + 1), dict(t=A + 2), dict(x=A + 1),
-                                 dict(base=A + 1), dict(y=A + 1)])
+                                 dict(base=A + 1), dict(y=A + 1), dict(xrs=-8), dict(bws=-1), dict(aws=-1), dict(ars=-8), dict(bbws=-1), dict(bbrs=-4)])
 def test_adapter_forward_refuses(lib, bad):
     assert lib.compams_adapter_forward(*adapter_args(**bad)) == -1
 
@@ -108,7 +110,8 @@ def adapter_backward_args(**kw):
 
 
 @pytest.mark.parametrize("bad", [dict(dy=None), dict(x=None), dict(t=None), dict(a=None), dict(b=None), dict(work=None), dict(bytes=64), dict(work=A + 4),
-                                 dict(rank=0), dict(da=A + 2), dict(db=A + 1), dict(dx=A + 1), dict(dy=A + 1)])
+                                 dict(rank=0), dict(da=A + 2), dict(db=A + 1), dict(dx=A + 1), dict(dy=A + 1), dict(grs=-8), dict(xws=-1),
+                                 dict(ars=-1), dict(bws=-1)])
 def test_adapter_backward_refuses(lib, bad):
     assert lib.compams_adapter_backward(*adapter_backward_args(**bad)) == -1
 

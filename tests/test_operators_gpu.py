@@ -324,10 +324,10 @@ def test_adapter_without_a_base_and_with_few_gradients(dtype):
     assert torch.equal(got, dy)
 
 
-@pytest.mark.parametrize("rows", [1, 48])
-def test_adapter_layouts(rows):
+@pytest.mark.parametrize("rows,rank", [(1, 8), (48, 8), (80, 8), (130, 40)])
+def test_adapter_layouts(rows, rank):
     g = gen(14)
-    n, h, out, rank = 3, 64, 80, 8
+    n, h, out = 3, 64, 80
     (x, base, a, b), dy, a64, b64 = adapter_case(g, n, rows, h, out, rank, BF16, "own")
     one = torch.ones(n, rows, h).double()
     _, want, _, tol = R.adapter(R.d(x), R.d(base), a64, b64, 1.0, one)
@@ -348,6 +348,15 @@ def test_adapter_layouts(rows):
     turned = [x.detach().transpose(0, 1).contiguous().transpose(0, 1), base.detach(), a.detach().transpose(1, 2).contiguous().transpose(1, 2),
               b.detach().transpose(1, 2).contiguous().transpose(1, 2)]
     R.check(low_rank_adapter(*turned), want, tol, "turned")
+    # repeated workers and rows
+    for v, z in ((x.detach()[:1].expand(n, rows, h), base.detach()), (x.detach()[:, :1].expand(n, rows, h), base.detach()[:, :1].expand(n, rows, out))):
+        _, want, _, tol = R.adapter(R.d(v), R.d(z), a64, b64, 1.0, one)
+        v, f, q = v.requires_grad_(), a.detach().requires_grad_(), b.detach().requires_grad_()
+        y = low_rank_adapter(v, z, f, q)
+        R.check(y, want, tol, "repeated")
+        (wx, _, tx), (wa, ta), (wb, tb) = R.adapter_gradients(R.d(dy[:, :1]).expand(n, rows, out), R.d(v), a64, b64, 1.0, one)
+        dx, da, db = torch.autograd.grad(y, (v, f, q), dy[:, :1].expand(n, rows, out))
+        R.check(dx, wx, tx, "dx"), R.check(da, wa, ta, "dA"), R.check(db, wb, tb, "dB")
 
 
 def test_adapter_dropped_values_do_not_matter():
@@ -397,6 +406,41 @@ def test_adapter_values_of_any_size():
         R.check(dx, wx, tx, "dx"), R.check(da, wa, ta, "dA"), R.check(db, wb, tb, "dB")
 
 
+def test_no_wait_gave_up():
+    import ctypes
+    from paper_2205_05632_b200 import load_library
+    low_rank_adapter(rand(gen(), 1, 64, 64, dtype=BF16), None, rand(gen(), 16, 64), rand(gen(), 64, 16))
+    gave_up = ctypes.c_int32(-1)
+    assert load_library().compams_adapter_status(ctypes.byref(gave_up)) == 0 and gave_up.value == 0
+
+
+@pytest.mark.parametrize("rank", [16, 32, 64, 65])
+@pytest.mark.parametrize("rows", [63, 64, 65, 127, 128, 129, 255, 256, 257, 513])
+def test_adapter_rows_around_the_tiles(rows, rank):
+    n, h, out = 2, 136, 264
+    (x, base, a, b), dy, a64, b64 = adapter_case(gen(21), n, rows, h, out, rank, BF16, "apart")
+    y = low_rank_adapter(x, base, a, b, p=0.5, seed=2)
+    f = R.factor(n, rows, h, 0.5, 2)
+    _, want, _, tol = R.adapter(R.d(x), R.d(base), a64, b64, 1.0, f)
+    R.check(y, want, tol, "y")
+    dx, da, db = torch.autograd.grad(y, (x, a, b), dy)
+    (wx, _, tx), (wa, ta), (wb, tb) = R.adapter_gradients(R.d(dy), R.d(x), a64, b64, 1.0, f)
+    R.check(dx, wx, tx, "dx"), R.check(da, wa, ta, "dA"), R.check(db, wb, tb, "dB")
+
+
+@pytest.mark.parametrize("h,out", [(8, 8), (56, 64), (64, 120), (72, 128), (120, 136), (128, 256), (136, 264), (1000, 65), (257, 1), (1, 129)])
+def test_adapter_columns_around_the_tiles(h, out):
+    for rank in (4, 30, 50):
+        (x, base, a, b), dy, a64, b64 = adapter_case(gen(22), 2, 70, h, out, rank, BF16, "own")
+        y = low_rank_adapter(x, base, a, b, p=0.25, seed=2)
+        f = R.factor(2, 70, h, 0.25, 2)
+        _, want, _, tol = R.adapter(R.d(x), R.d(base), a64, b64, 1.0, f)
+        R.check(y, want, tol, "y")
+        dx, da, db = torch.autograd.grad(y, (x, a, b), dy)
+        (wx, _, tx), (wa, ta), (wb, tb) = R.adapter_gradients(R.d(dy), R.d(x), a64, b64, 1.0, f)
+        R.check(dx, wx, tx, "dx"), R.check(da, wa, ta, "dA"), R.check(db, wb, tb, "dB")
+
+
 # ---- together --------------------------------------------------------------------------------------------------------------
 
 
@@ -421,9 +465,10 @@ def test_results_do_not_change_from_run_to_run_and_streams_are_kept(dtype):
         assert all(torch.equal(p, q) for p, q in zip(first, other))
 
 
-def test_forward_and_backward_in_a_graph():
+@pytest.mark.parametrize("rows", [3, 50, 200])
+def test_forward_and_backward_in_a_graph(rows):
     g = gen(19)
-    (x, base, a, b), dy, _, _ = adapter_case(g, 2, 50, 136, 72, 8, BF16, "apart")
+    (x, base, a, b), dy, _, _ = adapter_case(g, 2, rows, 136, 72, 8, BF16, "apart")
     w, bias, _, _ = parameters(g, 2, 72, "apart")
     counter = torch.zeros(1, dtype=torch.int64, device="cuda")
 
