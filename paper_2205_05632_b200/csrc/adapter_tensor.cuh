@@ -1,19 +1,18 @@
 // The adapters' three products on tcgen05.mma, for bfloat16 activations and ranks up to 64. mma.sync is bound by its own rate (550
 // TFLOP/s measured, a third of tcgen05's) from about rank 32 on, and below by the instructions that bring operands to registers.
 //
-// The planes of an fp32 operand are stacked along N: a tile of an activation, 128 x 64, is multiplied by [3 x R] rows of planes at once (R: the rank, padded to 16, 32 or 64), so
-// it is an operand once and the planes' sums stand beside each other in tensor memory. Operands lie in shared memory in the
-// 128-byte swizzle: rows of 128 bytes (64 elements), whose 16-byte chunk c lies at chunk c ^ (row % 8). down: the rows are the activation's
-// and the sum runs along them (K-major); outer: the sum runs over the rows, the tile is read across them (MN-major), and t
-// comes turned, [plane, rank][row].
+// The planes of an fp32 operand are stacked along N: a tile of an activation, 128 x 64, is multiplied by [3 x R] rows of planes at
+// once (R: the rank, padded to 16, 32 or 64), so it is an operand once and the planes' sums stand beside each other in tensor memory.
+// Operands lie in shared memory in the 128-byte swizzle: rows of 128 bytes (64 elements), whose 16-byte chunk c lies at chunk
+// c ^ (row % 8). down: the rows are the activation's and the sum runs along them (K-major); outer: the sum runs over the rows, the tile
+// is read across them (MN-major), and t comes turned, [plane, rank][row].
 //
 // One thread of a ninth warp issues the products and one of a tenth brings the tiles (TMA, into the swizzle; the planes, already in its
-// order, in bulk): a stage costs the one 0.35 us and the other 0.2 us, whatever the rank, and one thread for both held the rest up. They wait
-// for nobody else unless dropout masks the activation, which the 256 threads of the other warps do in place. (With tiles copied by
-// all threads, cp.async and a fence to the tensor cores' proxy for each, a stage took 1 us however many were under way: the fence
-// waits for all of a thread's copies.) The tensor cores cut their sums, so after every kFlush tiles of 64 the sums go to fp32 registers by
-// rounded additions, which is the other warps' work. Activations that TMA cannot address (odd widths, other strides) are
-// brought by these warps, element by element.
+// order, in bulk): a stage costs the one 0.35 us and the other 0.2 us, whatever the rank. One thread for both, waits included, held
+// every stage to 0.8 to 1.1 us. They wait for nobody else unless dropout masks the activation, which the 256 threads of the other warps
+// do in place. The tensor cores cut their sums, so after every kFlush tiles of 64 the sums go to fp32 registers by rounded additions,
+// which is the other warps' work. Activations that TMA cannot address (odd widths, other strides) are brought by these warps, element by
+// element.
 #pragma once
 
 #include <cuda.h>  // CUtensorMap
@@ -26,7 +25,9 @@ namespace tensor {
 
 constexpr int kMostRank = 64;
 constexpr int kTileBytes = 128 * 128;      // 128 rows of 64 elements, or 64 rows of 128
-constexpr int kFlush = 8;                  // tiles between two additions to the registers
+// Tiles between two additions to the registers. The largest error of dA, 2048 rows x 4096, rank 64, against its largest value: 4.3e-7 with
+// 4, 8.8e-7 with 8, and 1.8e-6 for torch's fp32 product.
+constexpr int kFlush = 8;
 
 // What goes by the padded rank.
 __host__ __device__ inline int padded_rank(int rank) { return rank <= 16 ? 16 : rank <= 32 ? 32 : 64; }

@@ -65,7 +65,10 @@ __device__ __forceinline__ float row_sum(float x, float* scratch, int warp) {
     return s;
 }
 
-constexpr int kRowsOfOneWarp = 8;  // rows of a CTA whose warps take a row each
+constexpr int kRowsOfOneWarp = 8;  // warps of a CTA whose warps share no row
+// Rows of such a CTA, L lanes to a row: 32, or as many as the eights of an aligned short row need.
+template <int W, int L>
+__host__ __device__ constexpr int norm_rows() { return W == 1 ? kRowsOfOneWarp * (32 / L) : 1; }
 
 template <int W>
 __host__ __device__ constexpr int norm_threads() { return W == 1 ? 32 * kRowsOfOneWarp : 32 * W; }
@@ -130,14 +133,16 @@ __host__ __device__ constexpr int forward_slots() { return NG * (raw_slots<TX>()
 
 // Every warp finds the mean and the sum of squares about it of its own columns; the barrier passes these on, and each warp
 // joins them (Chan, Golub, LeVeque 1979: the squares about the common mean are those about the parts' means and n_w (mean_w -
-// mean)^2 more).
-template <typename TX, typename TR, int W, int NG, bool VEC, bool ADD>
+// mean)^2 more), so a row costs one barrier and its values stay in registers. Bound by memory: 16384 rows of 4096 in bfloat16, 268 MB,
+// 48 us (5.6 TB/s; a plain copy takes 42); with dropout and the residual, 32768 rows, 1.07 GB, 198 us (5.4 TB/s). One row of 4096 takes
+// 3 us, which is the latency of its loads and the barrier.
+template <typename TX, typename TR, int W, int NG, int L, bool VEC, bool ADD>
 __global__ void __launch_bounds__(norm_threads<W>(), norm_ctas<W, NG, VEC, false>()) norm_forward_kernel(const __grid_constant__ NormArgs a) {
     extern __shared__ __align__(16) char smem[];
-    constexpr int kRows = W == 1 ? kRowsOfOneWarp : 1, SLOTS = forward_slots<TX, TR, NG, ADD>(), kStages = row_stages<W, SLOTS, VEC>();
+    constexpr int kRows = norm_rows<W, L>(), SLOTS = forward_slots<TX, TR, NG, ADD>(), kStages = row_stages<W, SLOTS, VEC>();
     constexpr bool RING = kStages > 0, kHold = NG <= 2;
     __shared__ float2 scratch[2][W];
-    const int lane = threadIdx.x & 31, warp = W == 1 ? 0 : (int)(threadIdx.x >> 5), slot = W == 1 ? (int)(threadIdx.x >> 5) : 0;
+    const int lane = (int)threadIdx.x % L, warp = W == 1 ? 0 : (int)(threadIdx.x >> 5), slot = W == 1 ? (int)threadIdx.x / L : 0;
     const uint32_t i = blockIdx.x / a.chunks, chunk = blockIdx.x - i * a.chunks;
     const uint32_t j0 = (uint32_t)((uint64_t)a.rows * chunk / a.chunks), j1 = (uint32_t)((uint64_t)a.rows * (chunk + 1) / a.chunks);
     const uint32_t call = drop_call(a.drop);
@@ -180,8 +185,9 @@ __global__ void __launch_bounds__(norm_threads<W>(), norm_ctas<W, NG, VEC, false
     const float own = columns(warp), per_own = own > 0.0f ? 1.0f / own : 0.0f, per_row = 1.0f / (float)a.h;
     const float lane_columns = columns(lane % W);
     int turn = 0, stage = 0;
-    for (uint32_t j = j0 + slot; j < j1; j += kRows, turn ^= 1) {
+    for (uint32_t j = j0 + slot; j - slot % (32 / L) < j1; j += kRows, turn ^= 1) {
         const uint32_t m = i * a.rows + j;
+        const int h = L == 32 || j < j1 ? a.h : 0;  // a warp's rows go on together; the ones behind the chunk's last are empty
         if constexpr (RING) {
             fetch(j + (kStages - 1) * kRows, stage == 0 ? kStages - 1 : stage - 1);
             copies_wait<kStages - 1>();  // a lane's own
@@ -190,21 +196,21 @@ __global__ void __launch_bounds__(norm_threads<W>(), norm_ctas<W, NG, VEC, false
 #pragma unroll
         for (int q = 0; q < NG; ++q) {
             const int c0 = (q * W + warp) * kSpan;
-            row_take<TX, W, SLOTS, VEC, RING>(smem, stage, q * raw_slots<TX>(), x + (int64_t)j * a.x_rs, c0, a.h, lane, 0.0f, v[q]);
-            if (ADD && c0 < a.h) {
+            row_take<TX, W, SLOTS, VEC, RING>(smem, stage, q * raw_slots<TX>(), x + (int64_t)j * a.x_rs, c0, h, lane, 0.0f, v[q]);
+            if (ADD && c0 < h) {
                 Pair more[4];
                 row_take<TR, W, SLOTS, VEC, RING>(smem, stage, NG * raw_slots<TX>() + q * raw_slots<TR>(), residual + (int64_t)j * a.r_rs, c0,
-                                                  a.h, lane, 0.0f, more);
+                                                  h, lane, 0.0f, more);
                 if (a.drop.on) span_drop<VEC>(a.drop, c0, j, a.drop.worker + i, call, lane, v[q]);
 #pragma unroll
                 for (int p = 0; p < 4; ++p) v[q][p] = add(v[q][p], more[p]);
-                span_store<TR, VEC, true>((TR*)a.s + (int64_t)m * a.h, c0, a.h, lane, v[q]);
+                span_store<TR, VEC, true>((TR*)a.s + (int64_t)m * a.h, c0, h, lane, v[q]);
             }
 #pragma unroll
             for (int p = 0; p < 4; ++p) sum = add(sum, v[q][p]);  // 0 beyond h
         }
         stage = stage + 1 == kStages ? 0 : stage + 1;
-        const float mean = warp_sum(joint(sum)) * per_own;
+        const float mean = few_sum<L>(joint(sum)) * per_own;
         Pair squares = pair(0.0f);
 #pragma unroll
         for (int q = 0; q < NG; ++q) {
@@ -212,14 +218,14 @@ __global__ void __launch_bounds__(norm_threads<W>(), norm_ctas<W, NG, VEC, false
 #pragma unroll
             for (int p = 0; p < 4; ++p) {
                 if (VEC) {
-                    v[q][p] = add(v[q][p], pair(c0 + lane * 8 < a.h ? -mean : 0.0f));
+                    v[q][p] = add(v[q][p], pair(c0 + lane * 8 < h ? -mean : 0.0f));
                 } else {
                     v[q][p] = add(v[q][p], pair(c0 + 64 * p + lane < a.h ? -mean : 0.0f, c0 + 64 * p + 32 + lane < a.h ? -mean : 0.0f));
                 }
                 squares = fma(v[q][p], v[q][p], squares);
             }
         }
-        float square = warp_sum(joint(squares)), off = 0.0f, centre = mean;  // off: of the warp's mean from the row's
+        float square = few_sum<L>(joint(squares)), off = 0.0f, centre = mean;  // off: of the warp's mean from the row's
         if (W > 1) {
             if (lane == 0) scratch[turn][warp] = make_float2(mean, square);
             __syncthreads();  // the next row writes the other half, and the one after it only behind the next row's barrier
@@ -230,21 +236,21 @@ __global__ void __launch_bounds__(norm_threads<W>(), norm_ctas<W, NG, VEC, false
             off = mean - centre;
         }
         const float rstd = 1.0f / sqrtf(square * per_row + a.eps);
-        if (a.stats && warp == 0 && lane == 0) a.stats[m] = make_float2(centre, rstd);
+        if (a.stats && warp == 0 && lane == 0 && h) a.stats[m] = make_float2(centre, rstd);
         const Pair factor = pair(rstd), offset = pair(off * rstd);
 #pragma unroll
         for (int q = 0; q < NG; ++q) {
             const int c0 = (q * W + warp) * kSpan;
-            if (c0 >= a.h) break;
+            if (c0 >= h) break;
             if (!kHold) affine(q, w[0], b[0]);
 #pragma unroll
             for (int p = 0; p < 4; ++p) v[q][p] = fma(fma(v[q][p], factor, offset), w[kHold ? q : 0][p], b[kHold ? q : 0][p]);
-            span_store<TX, VEC>((TX*)a.y + (int64_t)m * a.h, c0, a.h, lane, v[q]);
+            span_store<TX, VEC>((TX*)a.y + (int64_t)m * a.h, c0, h, lane, v[q]);
         }
     }
 }
 
-// Rows too long for registers: the row is read again for each sum, from the L2 as a rule.
+// Rows too long for registers (above 16384 columns): a CTA to a row, which is read again for each sum, from the L2 as a rule.
 template <typename TX, typename TR, bool ADD>
 __global__ void __launch_bounds__(512) norm_forward_long_kernel(const __grid_constant__ NormArgs a) {
     constexpr int W = 16;
@@ -294,16 +300,18 @@ __host__ __device__ constexpr int backward_slots() { return NG * (raw_slots<TX>(
 
 // The sums of dy xhat and dy of a chunk's rows stay in registers, the weight too. With several spans to a warp the values are taken
 // a second time behind the barrier instead of being held, and with four the weight is read again for each row: registers are what
-// bounds the CTAs of an SM.
-template <typename TX, typename TR, int W, int NG, bool VEC, bool ADD>
+// bounds the CTAs of an SM. 16384 rows of 4096 in bfloat16, 403 MB, take 77 us (5.2 TB/s); with dropout, the second incoming gradient
+// and the residual's, 32768 rows, 1.34 GB, 230 us (5.8 TB/s). 8192 rows of 16000, four spans to a warp, take 427 us with the forward
+// pass, 2.6 times the bytes' time: the weights are read again from the L2 for each row.
+template <typename TX, typename TR, int W, int NG, int L, bool VEC, bool ADD>
 __global__ void __launch_bounds__(norm_threads<W>(), norm_ctas<W, NG, VEC, true>()) norm_backward_kernel(const __grid_constant__ NormArgs a) {
     extern __shared__ __align__(16) char smem[];
-    constexpr int kSlots = W == 1 ? kRowsOfOneWarp : 1, SX = raw_slots<TX>(), SR = raw_slots<TR>();
+    constexpr int kSlots = norm_rows<W, L>(), SX = raw_slots<TX>(), SR = raw_slots<TR>();
     constexpr int SLOTS = backward_slots<TX, TR, NG, ADD>(), kStages = row_stages<W, SLOTS, VEC>();
     constexpr bool RING = kStages > 0;
     __shared__ float2 scratch[2][W];
     __shared__ float joined[W == 1 ? NG * kSpan : 1];
-    const int lane = threadIdx.x & 31, warp = W == 1 ? 0 : (int)(threadIdx.x >> 5), slot = W == 1 ? (int)(threadIdx.x >> 5) : 0;
+    const int lane = (int)threadIdx.x % L, warp = W == 1 ? 0 : (int)(threadIdx.x >> 5), slot = W == 1 ? (int)threadIdx.x / L : 0;
     const uint32_t i = blockIdx.x / a.chunks, chunk = blockIdx.x - i * a.chunks;
     const uint32_t j0 = (uint32_t)((uint64_t)a.rows * chunk / a.chunks), j1 = (uint32_t)((uint64_t)a.rows * (chunk + 1) / a.chunks);
     const uint32_t call = drop_call(a.drop);
@@ -341,8 +349,9 @@ __global__ void __launch_bounds__(norm_threads<W>(), norm_ctas<W, NG, VEC, true>
     int turn = 0, stage = 0;
     const float per_row = 1.0f / (float)a.h;
     float2 next = j0 + slot < j1 ? a.stats[i * a.rows + j0 + slot] : make_float2(0.0f, 0.0f);
-    for (uint32_t j = j0 + slot; j < j1; j += kSlots, turn ^= 1) {
+    for (uint32_t j = j0 + slot; j - slot % (32 / L) < j1; j += kSlots, turn ^= 1) {
         const uint32_t m = i * a.rows + j;
+        const int h = L == 32 || j < j1 ? a.h : 0;  // as in the forward pass: empty, so all its sums and terms are zeros
         const float2 st = next;
         if (j + kSlots < j1) next = a.stats[m + kSlots];
         if constexpr (RING) {
@@ -354,8 +363,8 @@ __global__ void __launch_bounds__(norm_threads<W>(), norm_ctas<W, NG, VEC, true>
         // dy w and xhat of span q; the first time its share of the sums
         auto values = [&](int q, bool first) {
             const int c0 = (q * W + warp) * kSpan;
-            row_take<TX, W, SLOTS, VEC, RING>(smem, stage, q * SX, dy + (int64_t)j * a.x_rs, c0, a.h, lane, 0.0f, g);
-            row_take<TR, W, SLOTS, VEC, RING>(smem, stage, NG * SX + q * SR, v + (int64_t)j * a.v_rs, c0, a.h, lane, st.x, xhat);
+            row_take<TX, W, SLOTS, VEC, RING>(smem, stage, q * SX, dy + (int64_t)j * a.x_rs, c0, h, lane, 0.0f, g);
+            row_take<TR, W, SLOTS, VEC, RING>(smem, stage, NG * SX + q * SR, v + (int64_t)j * a.v_rs, c0, h, lane, st.x, xhat);
             Pair w[4];
             if (!kHoldWeight) weight(q, w);
 #pragma unroll
@@ -375,7 +384,7 @@ __global__ void __launch_bounds__(norm_threads<W>(), norm_ctas<W, NG, VEC, true>
 #pragma unroll
         for (int q = 0; q < NG; ++q) values(q, true);
         if (a.y || (ADD && a.s)) {
-            float c1 = warp_sum(joint(sum1)), c2 = warp_sum(joint(sum2));
+            float c1 = few_sum<L>(joint(sum1)), c2 = few_sum<L>(joint(sum2));
             if (W > 1) {
                 if (lane == 0) scratch[turn][warp] = make_float2(c1, c2);
                 __syncthreads();  // the next row writes the other half, and the one after it only behind the next row's barrier
@@ -388,19 +397,19 @@ __global__ void __launch_bounds__(norm_threads<W>(), norm_ctas<W, NG, VEC, true>
 #pragma unroll
             for (int q = 0; q < NG; ++q) {
                 const int c0 = (q * W + warp) * kSpan;
-                if (c0 >= a.h) break;
+                if (c0 >= h) break;
                 if (!kHold) values(q, false);
 #pragma unroll
                 for (int p = 0; p < 4; ++p) g[p] = fma(xhat[p], along, fma(g[p], rstd, less));
                 if (ADD && more) {
                     Pair r[4];
-                    row_take<TR, W, SLOTS, VEC, RING>(smem, stage, NG * (SX + SR) + q * SR, more + (int64_t)j * a.r_rs, c0, a.h, lane, 0.0f, r);
+                    row_take<TR, W, SLOTS, VEC, RING>(smem, stage, NG * (SX + SR) + q * SR, more + (int64_t)j * a.r_rs, c0, h, lane, 0.0f, r);
 #pragma unroll
                     for (int p = 0; p < 4; ++p) g[p] = add(g[p], r[p]);
                 }
-                if (ADD && a.s) span_store<TR, VEC>((TR*)a.s + (int64_t)m * a.h, c0, a.h, lane, g);
+                if (ADD && a.s) span_store<TR, VEC>((TR*)a.s + (int64_t)m * a.h, c0, h, lane, g);
                 if (ADD && a.drop.on && a.y) span_drop<VEC>(a.drop, c0, j, a.drop.worker + i, call, lane, g);
-                if (a.y) span_store<TX, VEC>((TX*)a.y + (int64_t)m * a.h, c0, a.h, lane, g);
+                if (a.y) span_store<TX, VEC>((TX*)a.y + (int64_t)m * a.h, c0, h, lane, g);
             }
         }
         stage = stage + 1 == kStages ? 0 : stage + 1;
@@ -413,11 +422,28 @@ __global__ void __launch_bounds__(norm_threads<W>(), norm_ctas<W, NG, VEC, true>
             span_store<float, VEC>(out, (q * W + warp) * kSpan, a.h, lane, dw[q]);
             span_store<float, VEC>(out + a.h, (q * W + warp) * kSpan, a.h, lane, db[q]);
         }
-    } else {  // warps with rows of their own: their sums joined one warp after the other
+    } else {  // warps with rows of their own: their sums joined, those of a warp's rows first, then one warp after the other
+#pragma unroll
+        for (int o = L; o < 32; o <<= 1)
+#pragma unroll
+            for (int p = 0; p < 4; ++p)
+#pragma unroll
+                for (int q = 0; q < NG; ++q) {
+                    float x[2], y[2];
+                    halves(dw[q][p], x[0], x[1]);
+                    halves(db[q][p], y[0], y[1]);
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        x[k] += __shfl_xor_sync(0xffffffffu, x[k], o);
+                        y[k] += __shfl_xor_sync(0xffffffffu, y[k], o);
+                    }
+                    dw[q][p] = pair(x[0], x[1]);
+                    db[q][p] = pair(y[0], y[1]);
+                }
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
-            for (int s = 0; s < kSlots; ++s) {
-                if (slot == s) {
+            for (int s = 0; s < kRowsOfOneWarp; ++s) {
+                if ((int)threadIdx.x / 32 == s && (int)threadIdx.x % 32 < L) {
 #pragma unroll
                     for (int q = 0; q < NG; ++q)
 #pragma unroll
@@ -502,7 +528,8 @@ __global__ void __launch_bounds__(256) norm_columns_kernel(const __grid_constant
     out[a.h + c] = db;
 }
 
-// Sums the chunks of a worker (or of all) in their order: 32 columns by 8 shares of the chunks, the shares joined in shared memory.
+// Sums the chunks of a worker (or of all) in their order, so that the result does not depend on which CTA was first, as it would with
+// atomics: 32 columns by 8 shares of the chunks, the shares joined in shared memory. 8 workers of 4096 columns 5 us, some 20 MB from the L2.
 __global__ void __launch_bounds__(256) norm_join_kernel(const float* __restrict__ partial, float* dweight, float* dbias, int32_t h,
                                                         uint32_t chunks) {
     __shared__ float share[8][33];
@@ -685,75 +712,74 @@ uint32_t chunks_at_once(int count, int n, int64_t rows, int64_t per, int64_t mos
     return (uint32_t)(c < 1 ? 1 : c);
 }
 
+// f(warps of a row, spans of a warp, aligned, lanes of a row): a span to a warp as far as eight warps go, so that few values are kept by
+// each thread; then two and four. A warp takes several aligned short rows: 262144 bfloat16 rows of 64, both passes, 41 us with eight
+// lanes to a row, 118 with 32; of 128, 74 us with 16 lanes; of 200, with 32 as their groups of eight need, 129. Rows that are not
+// aligned go the same way: 16384 of 4097, 427 us with two spans to 16 warps, 664 with four.
+template <typename F>
+void by_width(int32_t h, bool vec, F f) {
+    const int spans = (h + kSpan - 1) / kSpan;
+    auto of = [&](auto v) {
+        const Int<32> l;
+        if (spans <= 1) f(Int<1>(), Int<1>(), v, l);
+        else if (spans <= 2) f(Int<2>(), Int<1>(), v, l);
+        else if (spans <= 4) f(Int<4>(), Int<1>(), v, l);
+        else if (spans <= 8) f(Int<8>(), Int<1>(), v, l);
+        else if (spans <= 16) f(Int<8>(), Int<2>(), v, l);
+        else if (spans <= 32) f(Int<16>(), Int<2>(), v, l);
+        else f(Int<16>(), Int<4>(), v, l);
+    };
+    if (vec && h <= 64) f(Int<1>(), Int<1>(), Int<1>(), Int<8>());
+    else if (vec && h <= 128) f(Int<1>(), Int<1>(), Int<1>(), Int<16>());
+    else if (vec) of(Int<1>());
+    else of(Int<0>());
+}
+
 template <typename TX, typename TR, bool ADD>
 int forward(NormArgs a, int n, bool vec, cudaStream_t stream) {
-    const int spans = (a.h + kSpan - 1) / kSpan;
     cudaError_t e = cudaSuccess;
-    auto go = [&](auto w, auto g, auto v) {
+    auto go = [&](auto w, auto g, auto v, auto l) {
         constexpr int W = decltype(w)::value, NG = decltype(g)::value;
         constexpr bool V = decltype(v)::value;
-        auto kernel = norm_forward_kernel<TX, TR, W, NG, V, ADD>;
+        constexpr int L = decltype(l)::value;
+        auto kernel = norm_forward_kernel<TX, TR, W, NG, L, V, ADD>;
         constexpr int shared = row_shared<W, forward_slots<TX, TR, NG, ADD>(), V>();
         int count = 0;
-        e = resident<norm_forward_kernel<TX, TR, W, NG, V, ADD>>(norm_threads<W>(), shared, &count);
+        e = resident<norm_forward_kernel<TX, TR, W, NG, L, V, ADD>>(norm_threads<W>(), shared, &count);
         if (e != cudaSuccess) return;
-        a.chunks = chunks_at_once(count, n, a.rows, W == 1 ? kRowsOfOneWarp : 1, 0x7fffffff / n);
+        a.chunks = chunks_at_once(count, n, a.rows, norm_rows<W, L>(), 0x7fffffff / n);
         e = launch_plain(kernel, dim3((uint32_t)n * a.chunks), dim3(norm_threads<W>()), shared, stream, a);
     };
     if (a.h > kLongest) {
         e = launch_plain(norm_forward_long_kernel<TX, TR, ADD>, dim3(a.total), dim3(512), 0, stream, a);
-    } else if (vec) {
-        if (spans <= 1) go(Int<1>(), Int<1>(), Int<1>());
-        else if (spans <= 2) go(Int<2>(), Int<1>(), Int<1>());
-        else if (spans <= 4) go(Int<4>(), Int<1>(), Int<1>());
-        else if (spans <= 8) go(Int<8>(), Int<1>(), Int<1>());
-        else if (spans <= 16) go(Int<8>(), Int<2>(), Int<1>());
-        else if (spans <= 32) go(Int<16>(), Int<2>(), Int<1>());
-        else go(Int<16>(), Int<4>(), Int<1>());
     } else {
-        if (spans <= 1) go(Int<1>(), Int<1>(), Int<0>());
-        else if (spans <= 2) go(Int<2>(), Int<1>(), Int<0>());
-        else if (spans <= 4) go(Int<4>(), Int<1>(), Int<0>());
-        else if (spans <= 16) go(Int<8>(), Int<2>(), Int<0>());
-        else go(Int<16>(), Int<4>(), Int<0>());
+        by_width(a.h, vec, go);
     }
     return launched(e, "norm_forward");
 }
 
 template <typename TX, typename TR, bool ADD>
 int backward(NormArgs& a, int n, bool vec, cudaStream_t stream) {
-    const int spans = (a.h + kSpan - 1) / kSpan;
     const uint32_t most = a.chunks;
     cudaError_t e = cudaSuccess;
-    auto go = [&](auto w, auto g, auto v) {
+    auto go = [&](auto w, auto g, auto v, auto l) {
         constexpr int W = decltype(w)::value, NG = decltype(g)::value;
         constexpr bool V = decltype(v)::value;
-        auto kernel = norm_backward_kernel<TX, TR, W, NG, V, ADD>;
+        constexpr int L = decltype(l)::value;
+        auto kernel = norm_backward_kernel<TX, TR, W, NG, L, V, ADD>;
         constexpr int shared = row_shared<W, backward_slots<TX, TR, NG, ADD>(), V>();
         int count = 0;
-        e = resident<norm_backward_kernel<TX, TR, W, NG, V, ADD>>(norm_threads<W>(), shared, &count);
+        e = resident<norm_backward_kernel<TX, TR, W, NG, L, V, ADD>>(norm_threads<W>(), shared, &count);
         if (e != cudaSuccess) return;
-        a.chunks = chunks_at_once(count, n, a.rows, W == 1 ? kRowsOfOneWarp : 1, most);
+        a.chunks = chunks_at_once(count, n, a.rows, norm_rows<W, L>(), most);
         e = launch_plain(kernel, dim3((uint32_t)n * a.chunks), dim3(norm_threads<W>()), shared, stream, a);
     };
     if (a.h > kLongest) {
         if (a.y || a.s) e = launch_plain(norm_backward_long_kernel<TX, TR, ADD>, dim3(a.total), dim3(512), 0, stream, a);
         if (e == cudaSuccess && a.partial)
             e = launch_plain(norm_columns_kernel<TX, TR>, dim3((uint32_t)(a.h + 255) / 256 * (uint32_t)n * a.chunks), dim3(256), 0, stream, a);
-    } else if (vec) {
-        if (spans <= 1) go(Int<1>(), Int<1>(), Int<1>());
-        else if (spans <= 2) go(Int<2>(), Int<1>(), Int<1>());
-        else if (spans <= 4) go(Int<4>(), Int<1>(), Int<1>());
-        else if (spans <= 8) go(Int<8>(), Int<1>(), Int<1>());
-        else if (spans <= 16) go(Int<8>(), Int<2>(), Int<1>());
-        else if (spans <= 32) go(Int<16>(), Int<2>(), Int<1>());
-        else go(Int<16>(), Int<4>(), Int<1>());
     } else {
-        if (spans <= 1) go(Int<1>(), Int<1>(), Int<0>());
-        else if (spans <= 2) go(Int<2>(), Int<1>(), Int<0>());
-        else if (spans <= 4) go(Int<4>(), Int<1>(), Int<0>());
-        else if (spans <= 16) go(Int<8>(), Int<2>(), Int<0>());
-        else go(Int<16>(), Int<4>(), Int<0>());
+        by_width(a.h, vec, go);
     }
     return launched(e, "norm_backward");
 }

@@ -19,7 +19,8 @@ def rand(g, *shape, dtype=F32, sigma=1.0):
 
 # (n, rows, h): one element, short and odd rows, the borders of spans of 256 and of the kernels' widths, beyond registers
 SHAPES = [(1, 1, 1), (3, 5, 7), (2, 3, 8), (1, 17, 255), (2, 9, 256), (1, 4, 257), (5, 3, 520), (2, 7, 1001), (1, 33, 1024), (2, 2, 1032),
-          (1, 3, 4096), (1, 2, 4104), (1, 2, 8191), (1, 2, 8200), (1, 2, 16384), (2, 2, 16392), (1, 1, 40001), (32, 1, 64), (1, 700, 48)]
+          (1, 3, 4096), (1, 2, 4104), (1, 2, 8191), (1, 2, 8200), (1, 2, 16384), (2, 2, 16392), (1, 1, 40001), (32, 1, 64), (1, 700, 48), (3, 3001, 64), (2, 45, 72), (1, 261, 128), (2, 19, 16),
+          (1, 3, 4097), (1, 2, 6001)]
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
