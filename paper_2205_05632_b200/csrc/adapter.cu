@@ -70,8 +70,8 @@ __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uin
 }
 
 // As above onto nothing. The tensor cores cut their sums instead of rounding them, so a sum grows there for a few products only, the
-// small planes' first, and joins the others by an fp32 addition: with one running sum in mma.sync dA of 4096 columns and rank 16 was
-// 4e-6 off, this way as near as fp32 arithmetic comes.
+// small planes' first, and joins the others by an fp32 addition: 300 rows of fp32, 1000 columns, rank 8: the largest error of dA is 1.9e-7
+// of its largest value, 1.8e-6 with one running sum (torch's fp32 product: 6.2e-7).
 __device__ __forceinline__ void mma_first(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
         : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
@@ -278,9 +278,11 @@ __device__ __forceinline__ Raw8<T> ring_raw(char* smem, int stage, int slot) {  
 // ---- down ------------------------------------------------------------------------------------------------------------------
 
 // A warp takes MT blocks of 16 rows and 8 NT rank indices; WK warps of a CTA share out the columns of their rows, and so do the CTAs of a
-// cluster. With many rows WK is 1 and the eight warps, of different rows, share the fragments, which pass through shared memory. A few
-// rows need WK = 8 to occupy the SMs; every warp then fetches fragments of its own. The sums of the warps and of the CTAs are
-// joined in their order, through the CTAs' shared memory, and leave as t and as the operands that up and outer take.
+// cluster. WK is 8, and every warp fetches fragments of its own, or 1: then the eight warps, of different rows, share the fragments, which
+// pass through shared memory. The sums of the warps and of the CTAs are
+// joined in their order, through the CTAs' shared memory, and leave as t and as the operands that up and outer take. Bound by the
+// instructions that make operands of the activation, not by memory: 8 workers of 2048 rows of 4096 in fp16, rank 16, 134 MB, 58 us
+// (2.3 TB/s), 78 with dropout; of 1024 rows in fp32, 134 MB too, 58 and 66. 8 workers of 48 rows in bfloat16 7 us.
 template <typename T>
 __host__ __device__ constexpr int down_step() { return sizeof(T) == 4 ? 1 : 2; }  // blocks of 32 columns in a step
 template <typename T, bool VEC, int NT, int WK, int MT>
@@ -485,7 +487,8 @@ __global__ void __launch_bounds__(256, MT == 1 ? 2 : 1) adapter_down_kernel(cons
     cluster.sync();  // the others may still be reading
 }
 
-// A few rows to a worker: bound by the factor, which is read once, in fp32 as it lies. A CTA per worker and rank index.
+// A few rows to a worker: bound by the factor, which is read once, in fp32 as it lies. A CTA per worker and rank index. 32 workers of one
+// row of 4096, rank 16, 8.4 MB of factors: 5.4 us, of which the launch and two trips to memory take most.
 constexpr int kFewRows = 4;
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) adapter_down_few_kernel(const __grid_constant__ AdapterArgs a) {
@@ -531,7 +534,9 @@ __global__ void __launch_bounds__(256) adapter_down_few_kernel(const __grid_cons
 
 // A warp per 32 columns goes through the blocks of 16 rows of a chunk, MB at a time; the eight warps of a CTA are neighbours and share
 // t, which passes through shared memory. RB: blocks of 16 rank indices, whose fragments of the factor stay in registers (0: any number;
-// fragments and t are fetched again for each block of rows).
+// fragments and t are fetched again for each block of rows). Bound by memory as long as the fragments stay: 8 workers of 2048 rows of 4096
+// in fp16, rank 16, 268 MB with the base, 51 us (5.3 TB/s), 65 for dx with dropout, 134 MB. Rank 128 in bfloat16, of 8192 columns, 537
+// MB: 610 us, the fragments' way through the L1.
 template <typename T, int RB>
 __host__ __device__ constexpr int up_rows() { return (RB == 1 || RB == 2) && sizeof(T) == 2 ? 2 : 1; }  // MB
 template <typename T, bool VEC, int RB>
@@ -672,7 +677,7 @@ __global__ void __launch_bounds__(256, 2) adapter_up_kernel(const __grid_constan
     }
 }
 
-// A few rows to a worker: a lane per column, the factor read once in fp32.
+// A few rows to a worker: a lane per column, the factor read once in fp32 (32 workers of one row of 4096, rank 16: 3.7 us).
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) adapter_up_few_kernel(const __grid_constant__ AdapterArgs a) {
     dependency_wait();
@@ -719,7 +724,8 @@ __global__ void __launch_bounds__(256) adapter_up_few_kernel(const __grid_consta
 
 // A CTA per 256 columns, 8 NT rank indices and chunk of a worker's rows: four warps side by side, two that share out the blocks of 16 rows
 // and join their sums. A lane takes eight neighbours of four rows; pairs of rows become the operand's pairs by byte permutes. The side by
-// side warps share t, which passes through shared memory.
+// side warps share t, which passes through shared memory. Bound by instructions, as down: 8 workers of 2048 rows of 4096 in fp16, rank 16,
+// 134 MB, 77 us, 101 with dropout; of 1024 rows in fp32 78 and 92.
 constexpr int kOuterColumns = 256;
 template <typename T, bool VEC, int NT>
 __host__ __device__ constexpr int outer_ring() { return VEC ? kStages * 4 * (int)sizeof(Raw8<T>) * 256 : 0; }
@@ -891,7 +897,7 @@ __global__ void __launch_bounds__(256) adapter_outer_kernel(const __grid_constan
     }
 }
 
-// A few rows to a worker: a lane per column, bound by the gradient that it writes.
+// A few rows to a worker: a lane per column, bound by the gradient that it writes (8 workers of four rows of 4096, rank 16, 2.1 MB each: 4 us).
 template <typename T>
 __global__ void __launch_bounds__(256) adapter_outer_few_kernel(const __grid_constant__ AdapterArgs a) {
     dependency_wait();
@@ -947,12 +953,15 @@ struct AdapterShape {
 };
 
 // Whether a worker's rows are few enough for the kernels that read the factor as it lies: with a tile of 16 rows of which four are
-// there, three quarters of the products are of zeros, and the fragments are written and read again for them.
+// there, three quarters of the products are of zeros, and the fragments are written and read again for them. 32 workers, 4096 x 4096, rank
+// 16, each its own factors: 9 us for one row, 15 for four; with fragments 23 for five.
 bool few(const AdapterShape& z) { return z.rows <= kFewRows; }
 
-// Whether the products run on tcgen05.mma.
+// Whether the products run on tcgen05.mma, whose tiles are of 128 rows: from 64 rows on, from 128 where the rank is padded to 16. Forward and
+// backward of 8 workers' 4096 x 4096, device time with it and without: rank 16 and 64 rows 53 and 43 us, 128 rows 57 and 63, 512 rows
+// 98 and 136; rank 64 and 64 rows 94 and 106, 2048 rows (4096 x 8192) 462 and 1132.
 bool on_tensor(const AdapterShape& z, int32_t type) {
-    return type == kTypeBF16 && z.rank <= tensor::kMostRank && z.rows >= 64;
+    return type == kTypeBF16 && z.rank <= tensor::kMostRank && z.rows >= (tensor::padded_rank(z.rank) == 16 ? 128 : 64);
 }
 
 // The number of parts, of 1 ... most, at which the slowest of `slots` places ends first: waves of tiles * parts CTAs, each a part's
@@ -1198,19 +1207,20 @@ int down(Low low, Rows x, const AdapterShape& z, int64_t h, bool shared, Factor 
             constexpr int WK = decltype(k)::value, NT = decltype(n)::value, MT = decltype(m)::value;
             return go(adapter_down_kernel<T, V, NT, WK, MT>, WK, MT, down_shared<T, V, NT, WK, MT>());
         };
-        auto by_ranks = [&](auto v, auto k) {
+        auto by_ranks = [&](auto v) {
             const int nt = group_tiles(z.rank);
-            if (nt == 1) return pick(v, k, Int<1>(), Int<1>());
-            if (nt == 2) return pick(v, k, Int<2>(), Int<1>());
-            if (nt == 4) return pick(v, k, Int<4>(), Int<1>());
-            // many rank indices: two blocks of rows to a warp, or the fragments' way through shared memory is the limit
-            if constexpr (decltype(k)::value == 1) return pick(v, k, Int<8>(), Int<2>());
-            else return pick(v, k, Int<8>(), Int<1>());
+            // Warps that share the rows' columns keep more loads on their way; warps of different rows share the fragments, which pays
+            // for several groups of ranks in 16 bits and many rows. Both passes' kernels of 8 workers, 4096 columns, eight warps to the
+            // rows / one: fp16, rank 128, 1024 rows 378 / 341 us, 512 rows 196 / 269; fp16, rank 16, 2048 rows 137
+            // / 152, 512 rows 50 / 45; fp32, rank 64, 1024 rows 228 / 402.
+            if constexpr (sizeof(T) == 2)
+                if (z.rank > 64 && z.total() >= 8192) return pick(v, Int<1>(), Int<8>(), Int<2>());
+            if (nt == 1) return pick(v, Int<8>(), Int<1>(), Int<1>());
+            if (nt == 2) return pick(v, Int<8>(), Int<2>(), Int<1>());
+            if (nt == 4) return pick(v, Int<8>(), Int<4>(), Int<1>());
+            return pick(v, Int<8>(), Int<8>(), Int<1>());
         };
-        // eight blocks of rows to a CTA where that leaves CTAs for all SMs, the columns shared out eightfold
-        const bool many = (z.rows + 127) / 128 * z.n * 8 >= 148;
-        if (many) return vec ? by_ranks(Int<1>(), Int<1>()) : by_ranks(Int<0>(), Int<1>());
-        return vec ? by_ranks(Int<1>(), Int<8>()) : by_ranks(Int<0>(), Int<8>());
+        return vec ? by_ranks(Int<1>()) : by_ranks(Int<0>());
     });
 }
 
