@@ -535,8 +535,8 @@ __global__ void __launch_bounds__(256) adapter_down_few_kernel(const __grid_cons
 // A warp per 32 columns goes through the blocks of 16 rows of a chunk, MB at a time; the eight warps of a CTA are neighbours and share
 // t, which passes through shared memory. RB: blocks of 16 rank indices, whose fragments of the factor stay in registers (0: any number;
 // fragments and t are fetched again for each block of rows). Bound by memory as long as the fragments stay: 8 workers of 2048 rows of 4096
-// in fp16, rank 16, 268 MB with the base, 51 us (5.3 TB/s), 65 for dx with dropout, 134 MB. Rank 128 in bfloat16, of 8192 columns, 537
-// MB: 610 us, the fragments' way through the L1.
+// in fp16, rank 16, 268 MB with the base, 51 us (5.3 TB/s), 65 for dx with dropout, 134 MB. With rank 128 the fragments' way
+// through the L1 is the limit: 16384 bfloat16 rows of 8192, 537 MB, 610 us.
 template <typename T, int RB>
 __host__ __device__ constexpr int up_rows() { return (RB == 1 || RB == 2) && sizeof(T) == 2 ? 2 : 1; }  // MB
 template <typename T, bool VEC, int RB>
@@ -959,9 +959,10 @@ bool few(const AdapterShape& z) { return z.rows <= kFewRows; }
 
 // Whether the products run on tcgen05.mma, whose tiles are of 128 rows: from 64 rows on, from 128 where the rank is padded to 16. Forward and
 // backward of 8 workers' 4096 x 4096, device time with it and without: rank 16 and 64 rows 53 and 43 us, 128 rows 57 and 63, 512 rows
-// 98 and 136; rank 64 and 64 rows 94 and 106, 2048 rows (4096 x 8192) 462 and 1132.
+// 98 and 136; rank 64 and 64 rows 94 and 106, 2048 rows (4096 x 8192) 462 and 1132; rank 128 there
+// 939 and 2504.
 bool on_tensor(const AdapterShape& z, int32_t type) {
-    return type == kTypeBF16 && z.rank <= tensor::kMostRank && z.rows >= (tensor::padded_rank(z.rank) == 16 ? 128 : 64);
+    return type == kTypeBF16 && z.rows >= (tensor::padded_rank(z.rank) == 16 ? 128 : 64);
 }
 
 // The number of parts, of 1 ... most, at which the slowest of `slots` places ends first: waves of tiles * parts CTAs, each a part's
@@ -981,7 +982,8 @@ uint32_t outer_chunks(const AdapterShape& z, int64_t h, int32_t type) {
     if (few(z)) return 1;
     // (partial sums beyond the first cost as much as `rank` rows of bf16)
     if (on_tensor(z, type))
-        return (uint32_t)parts_of((h + 255) / 256 * z.n, 148, (z.rows + 63) / 64, 4.0, std::min<int64_t>(65535 / z.n, 8), false);
+        return (uint32_t)parts_of((h + 255) / 256 * z.n * tensor::groups_of(z.rank), 148, (z.rows + 63) / 64, 4.0,
+                                  std::min<int64_t>(65535 / z.n, 8), false);
     const int64_t tiles = (h + kOuterColumns - 1) / kOuterColumns * rank_groups(z.rank) * z.n;
     int64_t c = (148 * 2 + tiles - 1) / tiles;
     const int64_t most = (z.rows + 63) / 64;
@@ -1099,16 +1101,18 @@ bool box_map(CUtensorMap* map, Rows x, const AdapterShape& z, int64_t h, uint32_
 int tensor_prepare(const AdapterShape& z, bool shared, Factor down, int64_t down_h, void* down_image, Factor up, int64_t up_h, void* up_image,
                    const float* t, void* t_image, cudaStream_t stream) {
     tensor::PrepareArgs p = {down, up, (char*)down_image, (char*)up_image, t, (char*)t_image, (int32_t)down_h, (int32_t)up_h, z.rank,
-                             (uint32_t)z.rows, 0, 0, 0, shared};
-    const int r = tensor::padded_rank(z.rank);
-    if (down_image) p.down_count = (uint32_t)((down_h + 127) / 128 * 16 * r);
-    if (up_image) p.up_count = (uint32_t)((up_h + 127) / 128 * 16 * r);
-    if (t_image) p.t_count = (uint32_t)((z.rows + 63) / 64 * 8 * r);
-    const uint64_t ctas = ((uint64_t)p.down_count + p.up_count + p.t_count + 255) / 256;
-    if (ctas > 0x00ffffffu) return COMPAMS_ERR_TOO_LARGE;
+                             (uint32_t)z.rows, 0, 0, 0, 0, 0, 0, shared};
+    const int64_t r = tensor::padded_rank(z.rank), groups = tensor::groups_of(z.rank);
+    p.down_blocks = (uint32_t)((down_h + 127) / 128 * 2); p.up_blocks = (uint32_t)((up_h + 127) / 128); p.t_blocks = (uint32_t)((z.rows + 63) / 64);
+    const int64_t down_count = down_image ? groups * p.down_blocks * 8 * r : 0, up_count = up_image ? groups * p.up_blocks * 16 * r : 0;
+    const int64_t t_count = t_image ? groups * p.t_blocks * 8 * r : 0;
+    const int64_t ctas = (down_count + up_count + t_count + 255) / 256;
+    if (ctas > 0x00ffffff) return COMPAMS_ERR_TOO_LARGE;
+    p.down_count = (uint32_t)down_count; p.up_count = (uint32_t)up_count; p.t_count = (uint32_t)t_count;
     const uint32_t workers = shared && !t_image ? 1 : (uint32_t)z.n;
     return by_rank(z, [&](auto v) {
-        return launched(launch_next(tensor::prepare_kernel<decltype(v)::value>, dim3((uint32_t)ctas, workers), 1, 0, true, stream, p), "adapter_prepare");
+        return launched(launch_next(tensor::prepare_kernel<decltype(v)::value>, dim3((uint32_t)ctas, workers), 1, 0, true, stream, p),
+                        "adapter_prepare");
     });
 }
 
@@ -1122,12 +1126,13 @@ int tensor_down(Low low, Rows x, const AdapterShape& z, int64_t h, bool shared, 
         constexpr int R = decltype(v)::value;
         using P = tensor::Pipe<R, false>;
         a.tiles = (a.rows + P::kRows - 1) / P::kRows;
-        a.split = (int32_t)parts_of((int64_t)a.tiles * z.n, 148, (h + P::kStep - 1) / P::kStep, 4.0, 4, true);
+        const uint32_t groups = (uint32_t)tensor::groups_of(z.rank);
+        a.split = (int32_t)parts_of((int64_t)a.tiles * z.n * groups, 148, (h + P::kStep - 1) / P::kStep, 4.0, 4, true);
         const uint64_t ctas = (uint64_t)a.tiles * z.n * a.split;
         if (ctas > 0x7fffffffu) return (int)COMPAMS_ERR_TOO_LARGE;
         CUtensorMap map;
         auto kernel = box_map(&map, x, z, h, 128) ? tensor::down_kernel<R, true> : tensor::down_kernel<R, false>;
-        return launched(launch_sized(kernel, dim3((uint32_t)ctas), tensor::kThreads, a.split, P::kShared, false, stream, a, map),
+        return launched(launch_sized(kernel, dim3((uint32_t)ctas, groups), tensor::kThreads, a.split, P::kShared, false, stream, a, map),
                         "adapter_down");
     });
 }
@@ -1136,16 +1141,20 @@ int tensor_up(void* y, Rows base, Low low, const AdapterShape& z, int64_t h, boo
               cudaStream_t stream) {
     tensor::UpArgs a = {};
     a.base = base.p; a.y = y; a.image = (const char*)image; a.t_up = (const char*)low.up; a.base_ws = base.worker_stride;
-    a.base_rs = base.row_stride; a.image_ws = shared ? 0 : tensor::up_image(h, z.rank); a.rows = (uint32_t)z.rows; a.h = (int32_t)h; a.scale = scale;
-    a.drop = d;
+    a.base_rs = base.row_stride; a.image_ws = shared ? 0 : tensor::up_image(h, z.rank); a.rows = (uint32_t)z.rows; a.h = (int32_t)h; a.rank = z.rank;
+    a.scale = scale; a.drop = d;
+    const bool several = tensor::groups_of(z.rank) > 1;
     const int64_t wide = tensor::padded_rank(z.rank) == 64 ? tensor::up_columns<64>() : tensor::up_columns<16>();
     const int64_t columns = (h + wide - 1) / wide, blocks = (z.rows + 127) / 128;
-    a.chunks = (uint32_t)parts_of(columns * z.n, 2 * 148, blocks, 0.5, 65535 / z.n, false);
+    a.chunks = (uint32_t)parts_of(columns * z.n, several ? 148 : 2 * 148, blocks, 0.5, 65535 / z.n, false);
     const bool vec = h % 8 == 0 && (!base.p || base.aligned()) && packed(y, z.rows, h, base.type).aligned();
     return by_rank(z, [&](auto v) {
         constexpr int R = decltype(v)::value;
-        auto kernel = vec ? tensor::up_kernel<R, true> : tensor::up_kernel<R, false>;
-        return launched(launch_next(kernel, dim3((uint32_t)columns, (uint32_t)z.n * a.chunks), 1, tensor::up_shared<R>(), false, stream, a), "adapter_up");
+        auto kernel = vec ? tensor::up_kernel<R, true, false> : tensor::up_kernel<R, false, false>;
+        if constexpr (R == 64)
+            if (several) kernel = vec ? tensor::up_kernel<R, true, true> : tensor::up_kernel<R, false, true>;
+        return launched(launch_next(kernel, dim3((uint32_t)columns, (uint32_t)z.n * a.chunks), 1, tensor::up_shared<R>(several), false, stream, a),
+                        "adapter_up");
     });
 }
 
@@ -1157,8 +1166,8 @@ int tensor_outer(const AdapterArgs& b, Rows x, Low low, const AdapterShape& z, i
         constexpr int R = decltype(v)::value;
         CUtensorMap map;
         auto kernel = box_map(&map, x, z, h, 64) ? tensor::outer_kernel<R, true> : tensor::outer_kernel<R, false>;
-        return launched(launch_sized(kernel, dim3((uint32_t)((h + 255) / 256), (uint32_t)z.n * a.chunks), tensor::kThreads, 1, tensor::Pipe<R, true>::kShared,
-                                     first, stream, a, map),
+        const dim3 grid((uint32_t)((h + 255) / 256), (uint32_t)z.n * a.chunks, (uint32_t)tensor::groups_of(z.rank));
+        return launched(launch_sized(kernel, grid, tensor::kThreads, 1, tensor::Pipe<R, true>::kShared, first, stream, a, map),
                         "adapter_outer");
     });
 }

@@ -1,9 +1,10 @@
-// The adapters' three products on tcgen05.mma, for bfloat16 activations and ranks up to 64. mma.sync is bound by its own rate (550
-// TFLOP/s measured, a third of tcgen05's) from about rank 32 on, and below by the instructions that bring operands to registers.
+// The adapters' three products on tcgen05.mma, for bfloat16 activations. mma.sync is bound by its own rate (550 TFLOP/s measured, a third
+// of tcgen05's) from about rank 32 on, and below by the instructions that bring operands to registers. (fp16 would need planes in fp16,
+// whose range the factors' values leave, and fp32 three tiles of planes for each tile of the activation: both stay on mma.sync.)
 //
 // The planes of an fp32 operand are stacked along N: a tile of an activation, 128 x 64, is multiplied by [3 x R] rows of planes at
-// once (R: the rank, padded to 16, 32 or 64), so it is an operand once and the planes' sums stand beside each other in tensor memory.
-// Operands lie in shared memory in the 128-byte swizzle: rows of 128 bytes (64 elements), whose 16-byte chunk c lies at chunk
+// once (R: the rank, padded to 16, 32 or 64; higher ranks go in groups of 64), so it is an operand once for a group and the planes' sums
+// stand beside each other in tensor memory. Operands lie in shared memory in the 128-byte swizzle: rows of 128 bytes (64 elements), whose 16-byte chunk c lies at chunk
 // c ^ (row % 8). down: the rows are the activation's and the sum runs along them (K-major); outer: the sum runs over the rows, the tile
 // is read across them (MN-major), and t comes turned, [plane, rank][row].
 //
@@ -23,7 +24,6 @@ namespace compams {
 namespace {
 namespace tensor {
 
-constexpr int kMostRank = 64;
 constexpr int kTileBytes = 128 * 128;      // 128 rows of 64 elements, or 64 rows of 128
 // Tiles between two additions to the registers. The largest error of dA, 2048 rows x 4096, rank 64, against its largest value: 4.3e-7 with
 // 4, 8.8e-7 with 8, and 1.8e-6 for torch's fp32 product.
@@ -31,6 +31,7 @@ constexpr int kFlush = 8;
 
 // What goes by the padded rank.
 __host__ __device__ inline int padded_rank(int rank) { return rank <= 16 ? 16 : rank <= 32 ? 32 : 64; }
+__host__ __device__ inline int groups_of(int rank) { return rank <= 64 ? 1 : (rank + 63) / 64; }
 template <int R>
 struct By {
     static constexpr int kN = 3 * R;                       // planes side by side
@@ -58,12 +59,16 @@ struct Pipe {
 
 // ---- images of the fp32 operands in global memory, in the order of shared memory --------------------------------------------
 
-// A factor for down: [64 columns, an even number of times][plane, rank][64 columns]; for up: [128 columns][plane 0, 1][column][rank] (the planes within a column's
-// 128 bytes up to 32 ranks); bytes of a worker's.
-__host__ __device__ inline int64_t down_image(int64_t h, int rank) { return (h + 127) / 128 * (2 * 3 * 128 * padded_rank(rank)); }
-__host__ __device__ inline int64_t up_image(int64_t h, int rank) { return (h + 127) / 128 * (kTileBytes << (padded_rank(rank) == 64)); }
+// All begin with the group of ranks. A factor for down: [64 columns, an even number of times][plane, rank][64 columns]; for up: [128 columns]
+// [plane 0, 1][column][rank] (the planes within a column's 128 bytes up to 32 ranks). Bytes of a group, and of a worker's.
+__host__ __device__ inline int64_t down_group(int64_t h, int rank) { return (h + 127) / 128 * (2 * 3 * 128 * padded_rank(rank)); }
+__host__ __device__ inline int64_t up_group(int64_t h, int rank) { return (h + 127) / 128 * (kTileBytes << (padded_rank(rank) == 64)); }
+__host__ __device__ inline int64_t down_image(int64_t h, int rank) { return groups_of(rank) * down_group(h, rank); }
+__host__ __device__ inline int64_t up_image(int64_t h, int rank) { return groups_of(rank) * up_group(h, rank); }
 // t for outer: [64 rows][plane, rank][row]; for up: [128 rows], as a factor's columns.
-__host__ __device__ inline int64_t t_outer_image(int64_t rows, int rank) { return (rows + 63) / 64 * (3 * 128 * padded_rank(rank)); }
+__host__ __device__ inline int64_t t_outer_group(int64_t rows, int rank) { return (rows + 63) / 64 * (3 * 128 * padded_rank(rank)); }
+__host__ __device__ inline int64_t t_outer_image(int64_t rows, int rank) { return groups_of(rank) * t_outer_group(rows, rank); }
+__host__ __device__ inline int64_t t_up_group(int64_t rows, int rank) { return up_group(rows, rank); }
 __host__ __device__ inline int64_t t_up_image(int64_t rows, int rank) { return up_image(rows, rank); }
 
 __device__ __forceinline__ uint32_t swizzled(uint32_t row, uint32_t chunk) { return row * 128u + ((chunk ^ (row & 7u)) << 4); }
@@ -172,6 +177,7 @@ struct PrepareArgs {
     char* t_image;  // t for outer; may be null
     int32_t down_h, up_h, rank;
     uint32_t rows, down_count, up_count, t_count;  // chunks of a worker's images, of one plane
+    uint32_t down_blocks, up_blocks, t_blocks;     // of a group
     int32_t shared;
 };
 // A thread per chunk of 16 bytes. 2.4 us for the factors of 4096 x 4096 at rank 16, 7.5 for 4096 x 8192 at rank 64 with 16384 rows of t.
@@ -181,16 +187,16 @@ __global__ void __launch_bounds__(256) prepare_kernel(const __grid_constant__ Pr
     float v[8];
     uint4 w[3];
     if (at < a.t_count) {  // [64 rows][8 rows][rank]: neighbouring threads read neighbouring ranks
-        const uint32_t rank = at % R, c = at / R % 8u, block = at / (8 * R);
+        const uint32_t lane = at % R, c = at / R % 8u, all = at / (8 * R), block = all % a.t_blocks, rank = all / a.t_blocks * R + lane;
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
             const uint32_t row = block * 64 + c * 8 + k;
             v[k] = row < a.rows && (int)rank < a.rank ? __ldg(a.t + ((int64_t)blockIdx.y * a.rows + row) * a.rank + rank) : 0.0f;
         }
         planes8(v, w);
-        char* out = a.t_image + blockIdx.y * t_outer_image(a.rows, R) + (int64_t)block * By<R>::kPlanesBytes;
+        char* out = a.t_image + blockIdx.y * t_outer_image(a.rows, a.rank) + (int64_t)all * By<R>::kPlanesBytes;
 #pragma unroll
-        for (int p = 0; p < 3; ++p) *reinterpret_cast<uint4*>(out + swizzled(p * R + rank, c)) = w[p];
+        for (int p = 0; p < 3; ++p) *reinterpret_cast<uint4*>(out + swizzled(p * R + lane, c)) = w[p];
         return;
     }
     at -= a.t_count;
@@ -198,7 +204,8 @@ __global__ void __launch_bounds__(256) prepare_kernel(const __grid_constant__ Pr
     if (at < a.down_count) {
         // the faster index is the one along which the factor is packed
         const bool ranks_packed = a.down.sj == 1;
-        const uint32_t rank = ranks_packed ? at % R : at / 8 % R, c = ranks_packed ? at / R % 8u : at % 8u, block = at / (8 * R);
+        const uint32_t lane = ranks_packed ? at % R : at / 8 % R, c = ranks_packed ? at / R % 8u : at % 8u, all = at / (8 * R);
+        const uint32_t block = all % a.down_blocks, rank = all / a.down_blocks * R + lane;
         const float* f = a.down.p + (int64_t)blockIdx.y * a.down.ws;
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
@@ -206,25 +213,26 @@ __global__ void __launch_bounds__(256) prepare_kernel(const __grid_constant__ Pr
             v[k] = (int)rank < a.rank && col < a.down_h ? __ldg(f + rank * a.down.sj + col * a.down.sc) : 0.0f;
         }
         planes8(v, w);
-        char* out = a.down_image + blockIdx.y * down_image(a.down_h, R) + (int64_t)block * By<R>::kPlanesBytes;
+        char* out = a.down_image + blockIdx.y * down_image(a.down_h, a.rank) + (int64_t)all * By<R>::kPlanesBytes;
 #pragma unroll
-        for (int p = 0; p < 3; ++p) *reinterpret_cast<uint4*>(out + swizzled(p * R + rank, c)) = w[p];
+        for (int p = 0; p < 3; ++p) *reinterpret_cast<uint4*>(out + swizzled(p * R + lane, c)) = w[p];
         return;
     }
     at -= a.down_count;
     if (at >= a.up_count) return;
     const bool ranks_packed = a.up.sj == 1;
     constexpr uint32_t C = R / 8;  // chunks of a plane's row
-    const uint32_t col = ranks_packed ? at / C % 128u : at % 128u, c = ranks_packed ? at % C : at / 128 % C, block = at / (128 * C);
+    const uint32_t col = ranks_packed ? at / C % 128u : at % 128u, c = ranks_packed ? at % C : at / 128 % C, all = at / (128 * C);
+    const uint32_t block = all % a.up_blocks, group = all / a.up_blocks;
     const float* f = a.up.p + (int64_t)blockIdx.y * a.up.ws;
     const int64_t column = (int64_t)block * 128 + col;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-        const int rank = c * 8 + k;
+        const int rank = (int)(group * R + c * 8) + k;
         v[k] = rank < a.rank && column < a.up_h ? __ldg(f + rank * a.up.sj + column * a.up.sc) : 0.0f;
     }
     planes8(v, w);
-    store_up<R>(a.up_image + blockIdx.y * up_image(a.up_h, R) + (int64_t)block * By<R>::kUpBytes, col, c, w);
+    store_up<R>(a.up_image + blockIdx.y * up_image(a.up_h, a.rank) + (int64_t)all * By<R>::kUpBytes, col, c, w);
 }
 
 // ---- down and outer --------------------------------------------------------------------------------------------------------
@@ -275,6 +283,7 @@ __device__ __forceinline__ void tensor_end(uint32_t memory, uint32_t columns) {
 // What the parts walk: steps first, first + stride, ... below last along the columns (down: rows from row0 on) or along the rows (outer,
 // ACROSS: 256 columns from column0 on).
 struct Walk {
+    const char* image;  // of the factor or of t: the worker's, the group's
     uint32_t worker, row0;
     int column0, first, stride, last;
 };
@@ -283,7 +292,7 @@ struct Walk {
 template <int R, bool MAPPED, bool ACROSS>
 __device__ __forceinline__ void bring(const Args& a, const CUtensorMap* map, const Walk& k, char* smem, uint32_t bars) {
     using P = Pipe<R, ACROSS>;
-    const char* image = a.image + (int64_t)k.worker * a.image_ws;
+    const char* image = k.image;
     int stage = 0;
     uint32_t empty = 1;  // the phase to wait for: of a stage's first round none
     for (int step = k.first, turn = 0; step < k.last; step += k.stride, ++turn) {
@@ -302,7 +311,8 @@ __device__ __forceinline__ void bring(const Args& a, const CUtensorMap* map, con
             } else {
 #pragma unroll
                 for (int m = 0; m < 2; ++m)
-                    box_load(to + m * kTileBytes, map, step * P::kStep + (P::kWide ? m * 64 : 0), (int)k.row0 + (P::kWide ? 0 : m * 128), (int)k.worker, bar);
+                    box_load(to + m * kTileBytes, map, step * P::kStep + (P::kWide ? m * 64 : 0), (int)k.row0 + (P::kWide ? 0 : m * 128),
+                             (int)k.worker, bar);
             }
         }
         bulk_load(smem + stage * P::kStageBytes + 2 * kTileBytes, image + (int64_t)step * P::kPlanesBytes, P::kPlanesBytes, bar);
@@ -340,8 +350,8 @@ __device__ __forceinline__ void issue(const Args& a, const Walk& k, char* smem, 
         for (int q = 0; q < 4; ++q)  // 16 of the 64
 #pragma unroll
             for (int m = 0; m < 2; ++m)
-                product(memory + m * By<R>::kN, left + (m * kTileBytes + q * (ACROSS ? 2048 : 32)) / 16, right + (P::kWide ? m * By<R>::kPlanesBytes / 16 : 0) + q * 2, instruction(By<R>::kN, ACROSS, false),
-                        q > 0 || since > 0);
+                product(memory + m * By<R>::kN, left + (m * kTileBytes + q * (ACROSS ? 2048 : 32)) / 16,
+                        right + (P::kWide ? m * By<R>::kPlanesBytes / 16 : 0) + q * 2, instruction(By<R>::kN, ACROSS, false), q > 0 || since > 0);
         products_done(bars + 8 * (P::kEmpty + stage));
         if (++since == kFlush || step + k.stride >= k.last) {
             since = 0;
@@ -462,7 +472,8 @@ __global__ void __launch_bounds__(kThreads, 1) down_kernel(const __grid_constant
     const int part = (int)(blockIdx.x - tile * a.split), steps = (a.h + P::kStep - 1) / P::kStep;
     const bool main = threadIdx.x < 256;
     float sums[R];
-    const Walk walk = {i, row0, 0, part, a.split, steps};
+    const int group = (int)blockIdx.y;
+    const Walk walk = {a.image + (int64_t)i * a.image_ws + group * down_group(a.h, a.rank), i, row0, 0, part, a.split, steps};
     if (main) sum_tiles<R, MAPPED, false>(a, walk, smem, memory, shared_address(bars), sums);
     else feed<R, MAPPED, false>(a, &map, walk, smem, memory, shared_address(bars));
     tensor_end(memory, By<R>::kColumns);
@@ -493,7 +504,7 @@ __global__ void __launch_bounds__(kThreads, 1) down_kernel(const __grid_constant
     if (a.out)
         for (int e = threadIdx.x; e < share * R; e += kThreads) {
             const int r = e / R, j = e % R;
-            if (first + r < a.rows && j < a.rank) a.out[((int64_t)i * a.rows + first + r) * a.rank + j] = whole[r * L + j];
+            if (first + r < a.rows && group * R + j < a.rank) a.out[((int64_t)i * a.rows + first + r) * a.rank + group * R + j] = whole[r * L + j];
         }
     for (int e = threadIdx.x; e < share * (R / 8); e += kThreads) {  // a row's eight ranks
         const int r = e / (R / 8), c = e % (R / 8);
@@ -504,7 +515,8 @@ __global__ void __launch_bounds__(kThreads, 1) down_kernel(const __grid_constant
         for (int k = 0; k < 8; ++k) v[k] = whole[r * L + c * 8 + k];
         uint4 w[3];
         planes8(v, w);
-        store_up<R>(a.t_up + i * t_up_image(a.rows, R) + (int64_t)(row >> 7) * By<R>::kUpBytes, row & 127u, c, w);
+        char* out = a.t_up + i * t_up_image(a.rows, a.rank) + group * t_up_group(a.rows, a.rank) + (int64_t)(row >> 7) * By<R>::kUpBytes;
+        store_up<R>(out, row & 127u, c, w);
     }
     if (a.t_outer)
         for (int e = threadIdx.x; e < share / 8 * R; e += kThreads) {  // a rank's eight rows
@@ -516,7 +528,8 @@ __global__ void __launch_bounds__(kThreads, 1) down_kernel(const __grid_constant
             for (int k = 0; k < 8; ++k) v[k] = whole[(r + k) * L + j];
             uint4 w[3];
             planes8(v, w);
-            char* out = a.t_outer + i * t_outer_image(a.rows, R) + (int64_t)(row >> 6) * By<R>::kPlanesBytes;
+            char* out = a.t_outer + i * t_outer_image(a.rows, a.rank) + group * t_outer_group(a.rows, a.rank) +
+                        (int64_t)(row >> 6) * By<R>::kPlanesBytes;
 #pragma unroll
             for (int p = 0; p < 3; ++p) *reinterpret_cast<uint4*>(out + swizzled(p * R + j, (row >> 3) & 7u)) = w[p];
         }
@@ -538,23 +551,25 @@ __global__ void __launch_bounds__(kThreads, 1) outer_kernel(const __grid_constan
     const uint32_t i = blockIdx.y / a.chunks, chunk = blockIdx.y - i * a.chunks, blocks = (a.rows + 63) / 64;
     const int s0 = (int)((uint64_t)blocks * chunk / a.chunks), s1 = (int)((uint64_t)blocks * (chunk + 1) / a.chunks);
     float sums[R];
-    const Walk walk = {i, 0, (int)blockIdx.x * 256, s0, 1, s1};
+    const int group = (int)blockIdx.z;
+    const Walk walk = {a.image + (int64_t)i * a.image_ws + group * t_outer_group(a.rows, a.rank), i, 0, (int)blockIdx.x * 256, s0, 1, s1};
     if (threadIdx.x < 256) sum_tiles<R, MAPPED, true>(a, walk, smem, memory, shared_address(bars), sums);
     else feed<R, MAPPED, true>(a, &map, walk, smem, memory, shared_address(bars));
     tensor_end(memory, By<R>::kColumns);
     const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (threadIdx.x >= 256 || c >= a.h) return;
     const float scale = a.scale * (a.drop.on ? a.drop.factor : 1.0f);
-    float* out = a.out + (int64_t)blockIdx.y * a.rank * a.h + c * a.sc;
+    float* out = a.out + (int64_t)blockIdx.y * a.rank * a.h + c * a.sc + group * R * a.sj;
+    const int ranks = a.rank - group * R;
     if (a.sj == 1 && (a.rank & 3) == 0 && (reinterpret_cast<uintptr_t>(a.out) & 15u) == 0) {
 #pragma unroll
         for (int r = 0; r < R; r += 4)
-            if (r < a.rank)
+            if (r < ranks)
                 *reinterpret_cast<float4*>(out + r) = make_float4(scale * sums[r], scale * sums[r + 1], scale * sums[r + 2], scale * sums[r + 3]);
     } else {
 #pragma unroll
         for (int r = 0; r < R; ++r)
-            if (r < a.rank) out[r * a.sj] = scale * sums[r];
+            if (r < ranks) out[r * a.sj] = scale * sums[r];
     }
 }
 
@@ -566,10 +581,16 @@ __global__ void __launch_bounds__(kThreads, 1) outer_kernel(const __grid_constan
 // products the other's loads run. Rank 64, 8 workers of 2048 rows: 8192 columns, 537 MB with the base, 121 us (4.4 TB/s); 4096 for dx
 // with dropout, 134 MB, 77 us. Rank 8, 4096 columns: 46 us for 268 MB (5.9 TB/s), 66 for dx with dropout. Bound by memory with a base,
 // by the generator without one.
+//
+// GROUPS: of several groups of 64 ranks. A tile takes a round per group, whose products go onto the same sums, and the factor's planes come
+// with t's for every round; one CTA to an SM. Rank 128,
+// 8192 columns: 264 us (2.0 TB/s); 4096 for dx with dropout 159.
 template <int R>
 __host__ __device__ constexpr int up_columns() { return R == 64 ? 64 : 128; }  // CN: what two CTAs' shared memory holds
 template <int R>
-__host__ __device__ constexpr int up_shared() { return By<R>::kUpTiles * up_columns<R>() * 128 + 2 * By<R>::kUpBytes + 2 * 256 * up_columns<R>() + 256; }
+__host__ __device__ constexpr int up_shared(bool groups) {
+    return (groups ? 2 : 1) * By<R>::kUpTiles * up_columns<R>() * 128 + 2 * By<R>::kUpBytes + 2 * 256 * up_columns<R>() + 256;
+}
 
 struct UpArgs {
     const void* base;  // may be null
@@ -577,46 +598,58 @@ struct UpArgs {
     const char *image, *t_up;
     int64_t base_ws, base_rs, image_ws;
     uint32_t rows, chunks;
-    int32_t h;
+    int32_t h, rank;
     float scale;
     Drop drop;
 };
 
-template <int R, bool VEC>
-__global__ void __launch_bounds__(256, 2) up_kernel(const __grid_constant__ UpArgs a) {
+template <int R, bool VEC, bool GROUPS>
+__global__ void __launch_bounds__(256, GROUPS ? 1 : 2) up_kernel(const __grid_constant__ UpArgs a) {
     extern __shared__ __align__(1024) char smem[];  // (all of it: nothing static, so it starts on the boundary, and two CTAs fit)
     using B = By<R>;
     constexpr int CN = up_columns<R>(), kRow = 2 * CN, kPlaneBytes = CN * 128;  // bytes of a tile's row; of a plane of the factor (R = 64)
     constexpr uint32_t kMemory = CN;
     using P = Pipe<R, true>;
-    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + up_shared<R>() - 256);
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + up_shared<R>(GROUPS) - 256);
     uint32_t* word = reinterpret_cast<uint32_t*>(bars + P::kBars);
     bool lost = false;  // a wait gave up
     dependency_wait();
     uint32_t memory;
     tensor_begin<P>(bars, word, kMemory, memory);
     // tile: 128 rows, chunk c at c ^ (row % 8)
-    char *planes = smem, *t0 = smem + B::kUpTiles * kPlaneBytes, *tile0 = t0 + 2 * B::kUpBytes;
+    constexpr int kFactorBytes = B::kUpTiles * kPlaneBytes;  // bytes of the factor's
+    char *planes = smem, *t0 = smem + (GROUPS ? 2 : 1) * kFactorBytes, *tile0 = t0 + 2 * B::kUpBytes;
     const uint32_t i = blockIdx.y / a.chunks, chunk = blockIdx.y - i * a.chunks, blocks = (a.rows + 127) / 128;
     const uint32_t b0 = (uint32_t)((uint64_t)blocks * chunk / a.chunks), b1 = (uint32_t)((uint64_t)blocks * (chunk + 1) / a.chunks);
     const int c0 = (int)blockIdx.x * CN, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t call = drop_call(a.drop), bar = shared_address(bars + P::kReady);
     const __nv_bfloat16* base = (const __nv_bfloat16*)a.base + (int64_t)i * a.base_ws;
     __nv_bfloat16* y = (__nv_bfloat16*)a.y + (int64_t)i * a.rows * a.h;
-    const char* t_image = a.t_up + i * t_up_image(a.rows, R);
+    const int groups = GROUPS ? groups_of(a.rank) : 1;
+    const char* t_image = a.t_up + i * t_up_image(a.rows, a.rank);
+    const char* factor = a.image + (int64_t)i * a.image_ws + (int64_t)(c0 / 128) * B::kUpBytes + c0 % 128 * 128;
+    auto fetch_planes = [&](int group, char* to) {
+        const char* from = factor + group * up_group(a.h, a.rank);
+#pragma unroll
+        for (int p = 0; p < B::kUpTiles; ++p)
+#pragma unroll
+            for (int k = 0; k < kPlaneBytes / 16 / 256; ++k)
+                copy16(to + p * kPlaneBytes + (threadIdx.x + 256 * k) * 16, from + p * kTileBytes + (threadIdx.x + 256 * k) * 16);
+    };
     // What a thread brings to a tile it takes away too. VEC: a column of chunks, every (256 / chunks of a row)-th row's; elsewhere a warp has
     // every eighth row and a lane every 32nd element.
     constexpr uint32_t kChunks = CN / 8, kRows = 256 / kChunks;
     const uint32_t r0 = threadIdx.x / kChunks, q0 = threadIdx.x % kChunks, at0 = r0 * kRow + ((q0 ^ (r0 & 7u)) << 4);
     const int column = c0 + (int)q0 * 8;
     auto element = [&](uint32_t row, uint32_t c) { return row * kRow + (((c >> 3) ^ (row & 7u)) << 4) + (c & 7u) * 2; };
-    auto fetch = [&](uint32_t b, uint32_t turn) {
+    auto fetch = [&](uint32_t b, int group, uint32_t turn) {
         if (b < b1) {
-            char *t = t0 + (turn & 1u) * B::kUpBytes, *tile = tile0 + (turn & 1u) * (128 * kRow);
-            const char* from = t_image + (int64_t)b * B::kUpBytes;
+            char *t = t0 + (turn & 1u) * B::kUpBytes, *tile = tile0 + ((b - b0) & 1u) * (128 * kRow);
+            const char* from = t_image + group * t_up_group(a.rows, a.rank) + (int64_t)b * B::kUpBytes;
+            if (GROUPS) fetch_planes(group, planes + (turn & 1u) * kFactorBytes);
 #pragma unroll
             for (int k = 0; k < B::kUpBytes / 16 / 256; ++k) copy16(t + (threadIdx.x + 256 * k) * 16, from + (threadIdx.x + 256 * k) * 16);
-            if (a.base) {
+            if (a.base && group == 0) {
                 if constexpr (VEC) {
                     const __nv_bfloat16* x = base + (int64_t)(b * 128 + r0) * a.base_rs + column;
 #pragma unroll
@@ -635,33 +668,29 @@ __global__ void __launch_bounds__(256, 2) up_kernel(const __grid_constant__ UpAr
         }
         copies_commit();
     };
-    {
-        const char* from = a.image + (int64_t)i * a.image_ws + (int64_t)(c0 / 128) * B::kUpBytes + c0 % 128 * 128;
-#pragma unroll
-        for (int p = 0; p < B::kUpTiles; ++p)
-#pragma unroll
-            for (int k = 0; k < kPlaneBytes / 16 / 256; ++k)
-                copy16(planes + p * kPlaneBytes + (threadIdx.x + 256 * k) * 16, from + p * kTileBytes + (threadIdx.x + 256 * k) * 16);
-    }
-    fetch(b0, 0);
-    uint32_t turn = 0;
-    for (uint32_t b = b0; b < b1; ++b, ++turn) {
-        fetch(b + 1, turn + 1);
+    if (!GROUPS) fetch_planes(0, planes);
+    fetch(b0, 0, 0);
+    uint32_t turn = 0, b = b0;
+    for (int group = 0; b < b1; ++turn) {
+        const bool last = !GROUPS || group + 1 == groups;
+        fetch(last ? b + 1 : b, last ? 0 : group + 1, turn + 1);
         copies_wait<1>();
         fence_shared();
         fence_before();
         __syncthreads();
-        char* tile = tile0 + (turn & 1u) * (128 * kRow);
+        char* tile = tile0 + ((b - b0) & 1u) * (128 * kRow);
         if (threadIdx.x == 0) {
             fence_after();
-            const uint32_t left = shared_address(t0 + (turn & 1u) * B::kUpBytes), right = shared_address(planes);
+            const uint32_t left = shared_address(t0 + (turn & 1u) * B::kUpBytes);
+            const uint32_t right = shared_address(planes) + (GROUPS ? (turn & 1u) * kFactorBytes : 0);
             constexpr uint32_t kRightPlane = R == 64 ? kPlaneBytes : 2 * R;
 #pragma unroll
             for (int q = 0; q < 3; ++q) {  // (0, 1), (1, 0), (0, 0): the smallest first
                 const uint32_t l = left + (q == 1 ? B::kUpPlane : 0), r = right + (q == 0 ? kRightPlane : 0);
 #pragma unroll
                 for (int k = 0; k < R / 16; ++k)
-                    product(memory, operand(l + k * 32, 16), operand(r + k * 32, 16), instruction(CN, false, false), q > 0 || k > 0);
+                    product(memory, operand(l + k * 32, 16), operand(r + k * 32, 16), instruction(CN, false, false),
+                            q > 0 || k > 0 || (GROUPS && group > 0));
             }
             products_done(bar);
         }
@@ -669,6 +698,10 @@ __global__ void __launch_bounds__(256, 2) up_kernel(const __grid_constant__ UpAr
         const uint32_t r = (uint32_t)(warp & 3) * 32 + lane, row = b * 128 + r;
         lost = lost || !barrier_wait(bar, turn & 1u);
         fence_after();
+        if (!last) {
+            ++group;
+            continue;
+        }
 #pragma unroll
         for (int part = 0; part < CN / 64; ++part) {
             const int first = (warp >> 2) * (CN / 2) + part * 32;
@@ -704,6 +737,8 @@ __global__ void __launch_bounds__(256, 2) up_kernel(const __grid_constant__ UpAr
                     if (b * 128 + q < a.rows && c0 + c < a.h)
                         y[(int64_t)(b * 128 + q) * a.h + c0 + c] = *reinterpret_cast<const __nv_bfloat16*>(tile + element(q, c));
         }
+        ++b;
+        group = 0;
     }
     copies_wait<0>();
     if (lost) gave_up = 1;

@@ -847,7 +847,8 @@ int compams_norm_forward(void* y, void* s, float* stats, const void* x, const vo
     if (rows == 0) return COMPAMS_OK;
     const Rows in{x, x_worker_stride, x_row_stride, type}, out = packed(y, rows, h, type);
     const Rows res{residual, residual_worker_stride, residual_row_stride, residual_type}, sum = packed(s, rows, h, residual_type);
-    if (!in.strides_ok() || (add && !res.strides_ok()) || weight_stride < 0 || bias_stride < 0 || !x || !y || (add && !s) || !in.element_aligned() || !out.element_aligned() || !float_aligned(weight) || !float_aligned(bias) ||
+    if (!in.strides_ok() || (add && !res.strides_ok()) || weight_stride < 0 || bias_stride < 0 || !x || !y || (add && !s) ||
+        !in.element_aligned() || !out.element_aligned() || !float_aligned(weight) || !float_aligned(bias) ||
         (reinterpret_cast<uintptr_t>(stats) & 7u) || (add && (!res.element_aligned() || !sum.element_aligned())))
         return COMPAMS_ERR_INVALID_ARG;
     const bool vec = h % 8 == 0 && in.aligned() && out.aligned() && (!add || (res.aligned() && sum.aligned())) &&
@@ -897,7 +898,8 @@ int compams_norm_backward(void* dx, void* dresidual, float* dweight, float* dbia
     }
     const Rows gin{dy, dy_worker_stride, dy_row_stride, type}, gsum{ds, ds_worker_stride, ds_row_stride, v_type};
     const Rows vin{v, v_worker_stride, v_row_stride, v_type}, out = packed(dx, rows, h, type), rout = packed(dresidual, rows, h, v_type);
-    if (!gin.strides_ok() || (ds && !gsum.strides_ok()) || !vin.strides_ok() || weight_stride < 0 || !dy || !v || !stats || (reinterpret_cast<uintptr_t>(stats) & 7u) || !float_aligned(weight) || !gin.element_aligned() ||
+    if (!gin.strides_ok() || (ds && !gsum.strides_ok()) || !vin.strides_ok() || weight_stride < 0 || !dy || !v || !stats ||
+        (reinterpret_cast<uintptr_t>(stats) & 7u) || !float_aligned(weight) || !gin.element_aligned() ||
         !gsum.element_aligned() || !vin.element_aligned() || !out.element_aligned() || !rout.element_aligned())
         return COMPAMS_ERR_INVALID_ARG;
     const bool vec = h % 8 == 0 && gin.aligned() && vin.aligned() && (!ds || gsum.aligned()) && out.aligned() && rout.aligned() &&

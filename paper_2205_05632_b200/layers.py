@@ -21,6 +21,13 @@ program's uses of the generator, or a one-element int64 CUDA tensor that holds i
 to keep its value until the backward pass is done (add to it behind that).
 
 The operators run on the current stream of x's device. They are differentiable once; their outputs are packed.
+
+Forward and backward can be captured into a CUDA graph together. As with every torch backward pass, the leaves' gradient nodes belong to
+the stream on which they were first used: warm up on the capturing stream, and let no autograd graph of the same leaves from another
+stream live while capturing.
+
+Not finite: a row of a norm with an infinity or a NaN in it is NaN, and so are its gradients; a dropped element is 0 whatever it was. In
+an adapter what an infinity or a NaN reaches is infinite or NaN, as a sum over it is, but which of the two may differ from a plain product.
 """
 from __future__ import annotations
 
