@@ -74,10 +74,12 @@ template <int W>
 __host__ __device__ constexpr int norm_threads() { return W == 1 ? 32 * kRowsOfOneWarp : 32 * W; }
 
 // CTAs that the registers of an SM have to hold, so that their barriers fall at different times: 24 warps' (16 where the backward
-// pass with its third input would not fit 80 registers a thread, and where rows are read element by element).
-template <int W, int NG, bool VEC, bool MORE>
+// pass with its third input would not fit 80 registers a thread, and where rows are read element by element). One CTA of 16 warps; two in
+// the forward pass, where 64 registers a thread nearly do, but for aligned rows with a residual: 16384 bfloat16 rows of 4097 219 us
+// with one and 146 with two, of 8192 120 and 97, with the residual 207 and 222; backward, with spills, 155 and 221.
+template <int W, int NG, bool VEC, bool MORE, bool ADD>
 __host__ __device__ constexpr int norm_ctas() {
-    return W == 16 ? 1 : (VEC && !(MORE && NG > 1) ? 24 : 16) / (W == 1 ? kRowsOfOneWarp : W);
+    return W == 16 ? (!MORE && NG <= 2 && !(ADD && VEC) ? 2 : 1) : (VEC && !(MORE && NG > 1) ? 24 : 16) / (W == 1 ? kRowsOfOneWarp : W);
 }
 
 // ---- a CTA's rows ----------------------------------------------------------------------------------------------------------
@@ -137,7 +139,7 @@ __host__ __device__ constexpr int forward_slots() { return NG * (raw_slots<TX>()
 // 48 us (5.6 TB/s; a plain copy takes 42); with dropout and the residual, 32768 rows, 1.07 GB, 198 us (5.4 TB/s). One row of 4096 takes
 // 3 us, which is the latency of its loads and the barrier.
 template <typename TX, typename TR, int W, int NG, int L, bool VEC, bool ADD>
-__global__ void __launch_bounds__(norm_threads<W>(), norm_ctas<W, NG, VEC, false>()) norm_forward_kernel(const __grid_constant__ NormArgs a) {
+__global__ void __launch_bounds__(norm_threads<W>(), norm_ctas<W, NG, VEC, false, ADD>()) norm_forward_kernel(const __grid_constant__ NormArgs a) {
     extern __shared__ __align__(16) char smem[];
     constexpr int kRows = norm_rows<W, L>(), SLOTS = forward_slots<TX, TR, NG, ADD>(), kStages = row_stages<W, SLOTS, VEC>();
     constexpr bool RING = kStages > 0, kHold = NG <= 2;
@@ -304,7 +306,7 @@ __host__ __device__ constexpr int backward_slots() { return NG * (raw_slots<TX>(
 // and the residual's, 32768 rows, 1.34 GB, 230 us (5.8 TB/s). 8192 rows of 16000, four spans to a warp, take 427 us with the forward
 // pass, 2.6 times the bytes' time: the weights are read again from the L2 for each row.
 template <typename TX, typename TR, int W, int NG, int L, bool VEC, bool ADD>
-__global__ void __launch_bounds__(norm_threads<W>(), norm_ctas<W, NG, VEC, true>()) norm_backward_kernel(const __grid_constant__ NormArgs a) {
+__global__ void __launch_bounds__(norm_threads<W>(), norm_ctas<W, NG, VEC, true, ADD>()) norm_backward_kernel(const __grid_constant__ NormArgs a) {
     extern __shared__ __align__(16) char smem[];
     constexpr int kSlots = norm_rows<W, L>(), SX = raw_slots<TX>(), SR = raw_slots<TR>();
     constexpr int SLOTS = backward_slots<TX, TR, NG, ADD>(), kStages = row_stages<W, SLOTS, VEC>();
@@ -529,7 +531,7 @@ __global__ void __launch_bounds__(256) norm_columns_kernel(const __grid_constant
 }
 
 // Sums the chunks of a worker (or of all) in their order, so that the result does not depend on which CTA was first, as it would with
-// atomics: 32 columns by 8 shares of the chunks, the shares joined in shared memory. 8 workers of 4096 columns 5 us, some 20 MB from the L2.
+// atomics: 32 columns by 8 shares of the chunks, the shares joined in shared memory. 8 workers of 4096 columns 5 us, 10 MB from the L2.
 __global__ void __launch_bounds__(256) norm_join_kernel(const float* __restrict__ partial, float* dweight, float* dbias, int32_t h,
                                                         uint32_t chunks) {
     __shared__ float share[8][33];
@@ -715,7 +717,7 @@ uint32_t chunks_at_once(int count, int n, int64_t rows, int64_t per, int64_t mos
 // f(warps of a row, spans of a warp, aligned, lanes of a row): a span to a warp as far as eight warps go, so that few values are kept by
 // each thread; then two and four. A warp takes several aligned short rows: 262144 bfloat16 rows of 64, both passes, 41 us with eight
 // lanes to a row, 118 with 32; of 128, 74 us with 16 lanes; of 200, with 32 as their groups of eight need, 129. Rows that are not
-// aligned go the same way: 16384 of 4097, 427 us with two spans to 16 warps, 664 with four.
+// aligned go the same way: 16384 of 4097, 358 us with two spans to 16 warps, 664 with four.
 template <typename F>
 void by_width(int32_t h, bool vec, F f) {
     const int spans = (h + kSpan - 1) / kSpan;
