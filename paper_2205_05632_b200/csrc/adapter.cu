@@ -960,7 +960,7 @@ bool few(const AdapterShape& z) { return z.rows <= kFewRows; }
 // Whether the products run on tcgen05.mma, whose tiles are of 128 rows: from 64 rows on, from 128 where the rank is padded to 16. Forward and
 // backward of 8 workers' 4096 x 4096, device time with it and without: rank 16 and 64 rows 53 and 43 us, 128 rows 57 and 63, 512 rows
 // 98 and 136; rank 64 and 64 rows 94 and 106, 2048 rows (4096 x 8192) 462 and 1132; rank 128 there
-// 939 and 2504.
+// 851 and 2504.
 bool on_tensor(const AdapterShape& z, int32_t type) {
     return type == kTypeBF16 && z.rows >= (tensor::padded_rank(z.rank) == 16 ? 128 : 64);
 }
@@ -1144,16 +1144,20 @@ int tensor_up(void* y, Rows base, Low low, const AdapterShape& z, int64_t h, boo
     a.base_rs = base.row_stride; a.image_ws = shared ? 0 : tensor::up_image(h, z.rank); a.rows = (uint32_t)z.rows; a.h = (int32_t)h; a.rank = z.rank;
     a.scale = scale; a.drop = d;
     const bool several = tensor::groups_of(z.rank) > 1;
-    const int64_t wide = tensor::padded_rank(z.rank) == 64 ? tensor::up_columns<64>() : tensor::up_columns<16>();
+    const int64_t wide = tensor::padded_rank(z.rank) == 64 && !several ? tensor::up_columns<64, false>() : tensor::up_columns<16, false>();
     const int64_t columns = (h + wide - 1) / wide, blocks = (z.rows + 127) / 128;
     a.chunks = (uint32_t)parts_of(columns * z.n, several ? 148 : 2 * 148, blocks, 0.5, 65535 / z.n, false);
     const bool vec = h % 8 == 0 && (!base.p || base.aligned()) && packed(y, z.rows, h, base.type).aligned();
     return by_rank(z, [&](auto v) {
         constexpr int R = decltype(v)::value;
         auto kernel = vec ? tensor::up_kernel<R, true, false> : tensor::up_kernel<R, false, false>;
+        int shared_bytes = tensor::up_shared<R, false>();
         if constexpr (R == 64)
-            if (several) kernel = vec ? tensor::up_kernel<R, true, true> : tensor::up_kernel<R, false, true>;
-        return launched(launch_next(kernel, dim3((uint32_t)columns, (uint32_t)z.n * a.chunks), 1, tensor::up_shared<R>(several), false, stream, a),
+            if (several) {
+                kernel = vec ? tensor::up_kernel<R, true, true> : tensor::up_kernel<R, false, true>;
+                shared_bytes = tensor::up_shared<R, true>();
+            }
+        return launched(launch_next(kernel, dim3((uint32_t)columns, (uint32_t)z.n * a.chunks), 1, shared_bytes, false, stream, a),
                         "adapter_up");
     });
 }

@@ -583,13 +583,14 @@ __global__ void __launch_bounds__(kThreads, 1) outer_kernel(const __grid_constan
 // by the generator without one.
 //
 // GROUPS: of several groups of 64 ranks. A tile takes a round per group, whose products go onto the same sums, and the factor's planes come
-// with t's for every round; one CTA to an SM. Rank 128,
-// 8192 columns: 264 us (2.0 TB/s); 4096 for dx with dropout 159.
-template <int R>
-__host__ __device__ constexpr int up_columns() { return R == 64 ? 64 : 128; }  // CN: what two CTAs' shared memory holds
-template <int R>
-__host__ __device__ constexpr int up_shared(bool groups) {
-    return (groups ? 2 : 1) * By<R>::kUpTiles * up_columns<R>() * 128 + 2 * By<R>::kUpBytes + 2 * 256 * up_columns<R>() + 256;
+// with t's for every round; one CTA of 128 columns to an SM: rank 128, 8192 columns 206 us (2.6 TB/s), 4096 for dx with dropout 130; with
+// 64 columns 266 and 160. (One group, rank 64: two CTAs of 64 columns 123 and 78 us, one of 128 146 and 99.)
+template <int R, bool GROUPS>
+__host__ __device__ constexpr int up_columns() { return R == 64 && !GROUPS ? 64 : 128; }  // CN
+template <int R, bool GROUPS>
+__host__ __device__ constexpr int up_shared() {
+    constexpr int CN = up_columns<R, GROUPS>();
+    return (GROUPS ? 2 : 1) * By<R>::kUpTiles * CN * 128 + 2 * By<R>::kUpBytes + 2 * 256 * CN + 256;
 }
 
 struct UpArgs {
@@ -607,10 +608,10 @@ template <int R, bool VEC, bool GROUPS>
 __global__ void __launch_bounds__(256, GROUPS ? 1 : 2) up_kernel(const __grid_constant__ UpArgs a) {
     extern __shared__ __align__(1024) char smem[];  // (all of it: nothing static, so it starts on the boundary, and two CTAs fit)
     using B = By<R>;
-    constexpr int CN = up_columns<R>(), kRow = 2 * CN, kPlaneBytes = CN * 128;  // bytes of a tile's row; of a plane of the factor (R = 64)
+    constexpr int CN = up_columns<R, GROUPS>(), kRow = 2 * CN, kPlaneBytes = CN * 128;  // bytes of a tile's row; of a plane of the factor (R = 64)
     constexpr uint32_t kMemory = CN;
     using P = Pipe<R, true>;
-    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + up_shared<R>(GROUPS) - 256);
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + up_shared<R, GROUPS>() - 256);
     uint32_t* word = reinterpret_cast<uint32_t*>(bars + P::kBars);
     bool lost = false;  // a wait gave up
     dependency_wait();
