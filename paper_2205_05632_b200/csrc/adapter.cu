@@ -960,18 +960,20 @@ bool few(const AdapterShape& z) { return z.rows <= kFewRows; }
 // Whether the products run on tcgen05.mma, whose tiles are of 128 rows: from 64 rows on, from 128 where the rank is padded to 16. Forward and
 // backward of 8 workers' 4096 x 4096, device time with it and without: rank 16 and 64 rows 53 and 43 us, 128 rows 57 and 63, 512 rows
 // 98 and 136; rank 64 and 64 rows 94 and 106, 2048 rows (4096 x 8192) 462 and 1132; rank 128 there
-// 851 and 2504.
+// 808 and 2504.
 bool on_tensor(const AdapterShape& z, int32_t type) {
     return type == kTypeBF16 && z.rows >= (tensor::padded_rank(z.rank) == 16 ? 128 : 64);
 }
 
 // The number of parts, of 1 ... most, at which the slowest of `slots` places ends first: waves of tiles * parts CTAs, each a part's
-// share of `work` and `fixed` more.
-int64_t parts_of(int64_t tiles, int64_t slots, int64_t work, double fixed, int64_t most, bool powers) {
+// share of `work` and `fixed` more. join: what a part more of a tile costs the whole device afterwards, if there are several (and a
+// launch, 3); all in steps of a CTA.
+int64_t parts_of(int64_t tiles, int64_t slots, int64_t work, double fixed, int64_t most, bool powers, double join = 0.0) {
     int64_t best = 1;
     double least = 0.0;
     for (int64_t c = 1; c <= most && c <= work; c = powers ? 2 * c : c + 1) {
-        const double cost = (double)((tiles * c + slots - 1) / slots) * ((double)((work + c - 1) / c) + fixed);
+        const double cost = (double)((tiles * c + slots - 1) / slots) * ((double)((work + c - 1) / c) + fixed) +
+                            (join > 0.0 && c > 1 ? 3.0 + join * (double)(tiles * c) : 0.0);
         if (c == 1 || cost < least * 0.999) best = c, least = cost;
     }
     return best;
@@ -980,10 +982,11 @@ int64_t parts_of(int64_t tiles, int64_t slots, int64_t work, double fixed, int64
 // Chunks of a worker's rows: as many as give each SM about two CTAs, of 64 rows at least.
 uint32_t outer_chunks(const AdapterShape& z, int64_t h, int32_t type) {
     if (few(z)) return 1;
-    // (partial sums beyond the first cost as much as `rank` rows of bf16)
+    // (partial sums of 64 ranks and 256 columns, 64 KB written and read: 26 ns at 5 TB/s; a step takes 0.5 us. 16384 rows of 8192 at rank
+    // 128: 117 us with one chunk, 127 and 43 for the join with two; one worker's 512 rows of 1024 at rank 64: 11, 7.4 and 2.3 with eight)
     if (on_tensor(z, type))
         return (uint32_t)parts_of((h + 255) / 256 * z.n * tensor::groups_of(z.rank), 148, (z.rows + 63) / 64, 4.0,
-                                  std::min<int64_t>(65535 / z.n, 8), false);
+                                  std::min<int64_t>(65535 / z.n, 8), false, 0.05 * std::min(z.rank, 64) / 64);
     const int64_t tiles = (h + kOuterColumns - 1) / kOuterColumns * rank_groups(z.rank) * z.n;
     int64_t c = (148 * 2 + tiles - 1) / tiles;
     const int64_t most = (z.rows + 63) / 64;
