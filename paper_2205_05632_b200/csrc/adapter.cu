@@ -18,8 +18,8 @@
 //
 // Precision. mma.sync multiplies bf16 exactly and adds in fp32. An fp32 number is the sum of three bf16 numbers, its planes (8 bits
 // each, cut, not rounded: the rest after each cut is exact, nothing overflows); fp16 needs two and bf16 is one. Products of planes
-// i and j are formed for i + j <= 2, which leaves out less than 3 * 2^-24 of a product: as fp32 arithmetic does. Where the result is
-// a 16-bit number (y, dx) i + j <= 1 suffice: 3 * 2^-16 of a product, an eighth of half a step of fp16, 2^-6 of one of bf16.
+// i and j are formed for i + j <= 2, which leaves out less than 2^-21 of a product, also where the result is a 16-bit number (y, dx): base
+// and adapter may cancel, and a result near the border of two roundings should fall where fp32 arithmetic lets it fall.
 #include <cooperative_groups.h>
 #include <string.h>
 
@@ -159,15 +159,10 @@ __host__ __device__ inline int64_t up_frag_words(int64_t h, int rank) {
     return (h + kUpColumns - 1) / kUpColumns * ((rank + 15) / 16) * kPlanes * 64;
 }
 // t as an operand, 16 rows of a worker at a time:
-//   up:    [16 rows][16 ranks][plane][lane g, t] = rows g and g + 8, ranks 4 t ... 4 t + 3 (16 bytes); as many planes as up multiplies
+//   up:    [16 rows][16 ranks][plane][lane g, t] = rows g and g + 8, ranks 4 t ... 4 t + 3 (16 bytes)
 //   outer: [group][16 rows][tile][plane][lane g, t] = rows 4 t ... 4 t + 3, rank g (8 bytes)
-__host__ __device__ inline int64_t t_up_words(int64_t rows, int rank, int planes) {
-    return (rows + 15) / 16 * ((rank + 15) / 16) * planes * 32;
-}
+__host__ __device__ inline int64_t t_up_words(int64_t rows, int rank) { return (rows + 15) / 16 * ((rank + 15) / 16) * kPlanes * 32; }
 __host__ __device__ inline int64_t t_outer_words(int64_t rows, int rank) { return (rows + 15) / 16 * rank_tiles(rank) * kPlanes * 16; }
-template <typename T>
-__host__ __device__ constexpr int up_planes() { return sizeof(T) == 4 ? 3 : 2; }
-
 // Four numbers of t as an operand of outer.
 __device__ __forceinline__ void store_t_outer(uint2* at, const float (&v)[4]) {
     uint32_t lo[kPlanes], hi[kPlanes];
@@ -468,10 +463,9 @@ __global__ void __launch_bounds__(256, MT == 1 ? 2 : 1) adapter_down_kernel(cons
                     const float* at = whole + (g + half * 8) * L + j;
                     split2<kPlanes>(j < NT * 8 ? at[0] : 0.0f, j < NT * 8 ? at[1] : 0.0f, v[half][pair]);
                 }
-            constexpr int PT = up_planes<T>();
-            uint4* out = a.t_up + i * t_up_words(a.rows, a.rank, PT) + ((int64_t)block * ranks + n0 / 2 + q) * PT * 32 + lane;
+            uint4* out = a.t_up + i * t_up_words(a.rows, a.rank) + ((int64_t)block * ranks + n0 / 2 + q) * kPlanes * 32 + lane;
 #pragma unroll
-            for (int p = 0; p < PT; ++p) out[p * 32] = make_uint4(v[0][0][p], v[1][0][p], v[0][1][p], v[1][1][p]);
+            for (int p = 0; p < kPlanes; ++p) out[p * 32] = make_uint4(v[0][0][p], v[1][0][p], v[0][1][p], v[1][1][p]);
         }
         if (a.t_outer)
             for (int q = warp; q < NT; q += 8) {
@@ -534,20 +528,21 @@ __global__ void __launch_bounds__(256) adapter_down_few_kernel(const __grid_cons
 
 // A warp per 32 columns goes through the blocks of 16 rows of a chunk, MB at a time; the eight warps of a CTA are neighbours and share
 // t, which passes through shared memory. RB: blocks of 16 rank indices, whose fragments of the factor stay in registers (0: any number;
-// fragments and t are fetched again for each block of rows). Bound by memory as long as the fragments stay: 8 workers of 2048 rows of 4096
-// in fp16, rank 16, 268 MB with the base, 51 us (5.3 TB/s), 65 for dx with dropout, 134 MB. With rank 128 the fragments' way
-// through the L1 is the limit: 16384 bfloat16 rows of 8192, 537 MB, 610 us.
+// fragments and t are fetched again for each block of rows). 8 workers of 2048 rows of 4096 in fp16, rank 16, 268 MB with the base, take
+// 61 us (4.4 TB/s), 80 for dx with dropout, 134 MB; rank 32 89 and 118. Bound by the six products of planes from rank 64 on: 175 and 197 us,
+// with one CTA to an SM, whose registers hold the fragments (fetched again for each block of rows: 248 and 260). Rank 128, where the
+// fragments' way through the L1 is the limit: 431 and 448 us.
 template <typename T, int RB>
-__host__ __device__ constexpr int up_rows() { return (RB == 1 || RB == 2) && sizeof(T) == 2 ? 2 : 1; }  // MB
+__host__ __device__ constexpr int up_rows() { return RB == 1 && sizeof(T) == 2 ? 2 : 1; }  // MB
 template <typename T, bool VEC, int RB>
 __host__ __device__ constexpr int up_ring() { return VEC ? kStages * 2 * up_rows<T, RB>() * (int)sizeof(Raw8<T>) * 256 : 0; }
 template <typename T, bool VEC, int RB>
-__host__ __device__ constexpr int up_shared() { return up_ring<T, VEC, RB>() + kStages * up_rows<T, RB>() * RB * up_planes<T>() * 512; }
+__host__ __device__ constexpr int up_shared() { return up_ring<T, VEC, RB>() + kStages * up_rows<T, RB>() * RB * kPlanes * 512; }
 
 template <typename T, bool VEC, int RB>
-__global__ void __launch_bounds__(256, 2) adapter_up_kernel(const __grid_constant__ AdapterArgs a) {
+__global__ void __launch_bounds__(256, RB == 4 ? 1 : 2) adapter_up_kernel(const __grid_constant__ AdapterArgs a) {
     extern __shared__ __align__(16) char smem[];
-    constexpr int S16 = (int)sizeof(Raw8<T>) / 16, PT = up_planes<T>(), MB = up_rows<T, RB>(), SLOTS = 2 * MB * S16, STAGE = MB * RB * PT * 32;
+    constexpr int S16 = (int)sizeof(Raw8<T>) / 16, MB = up_rows<T, RB>(), SLOTS = 2 * MB * S16, STAGE = MB * RB * kPlanes * 32;
     dependency_wait();
     uint4* stages = reinterpret_cast<uint4*>(smem + up_ring<T, VEC, RB>());
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
@@ -559,11 +554,11 @@ __global__ void __launch_bounds__(256, 2) adapter_up_kernel(const __grid_constan
     const uint32_t b0 = (uint32_t)((uint64_t)blocks * chunk / a.tiles), b1 = (uint32_t)((uint64_t)blocks * (chunk + 1) / a.tiles);
     const uint32_t call = drop_call(a.drop);
     const uint4* frag = a.frag + (int64_t)i * a.frag_ws + (int64_t)(mine ? cb : 0) * ranks * kPlanes * 64 + lane;
-    const uint4* tt = a.t_up + i * t_up_words(a.rows, a.rank, PT);
-    uint4 f[RB ? RB : 1][PT][2];
-    auto factor = [&](int r, uint4 (&to)[PT][2]) {
+    const uint4* tt = a.t_up + i * t_up_words(a.rows, a.rank);
+    uint4 f[RB ? RB : 1][kPlanes][2];
+    auto factor = [&](int r, uint4 (&to)[kPlanes][2]) {
 #pragma unroll
-        for (int p = 0; p < PT; ++p) {
+        for (int p = 0; p < kPlanes; ++p) {
             to[p][0] = frag[((int64_t)r * kPlanes + p) * 64];
             to[p][1] = frag[((int64_t)r * kPlanes + p) * 64 + 32];
         }
@@ -576,8 +571,8 @@ __global__ void __launch_bounds__(256, 2) adapter_up_kernel(const __grid_constan
     Raw8<T> next[MB][2];
     auto fetch = [&](uint32_t b, int stage) {
         if constexpr (RB > 0) {
-            const uint4* from = tt + (int64_t)b * (RB * PT * 32);
-            const int have = b < b1 ? (b + MB <= b1 ? STAGE : RB * PT * 32) : 0;
+            const uint4* from = tt + (int64_t)b * (RB * kPlanes * 32);
+            const int have = b < b1 ? (b + MB <= b1 ? STAGE : RB * kPlanes * 32) : 0;
 #pragma unroll
             for (int e = threadIdx.x; e < STAGE; e += 256)
                 if (e < have) copy16(stages + stage * STAGE + e, from + e, true);
@@ -627,16 +622,16 @@ __global__ void __launch_bounds__(256, 2) adapter_up_kernel(const __grid_constan
         float acc[MB][4][4] = {};
 #pragma unroll(RB ? RB : 1)
         for (int r = 0; r < ranks; ++r) {
-            uint4 w[MB][PT];
+            uint4 w[MB][kPlanes];
             if constexpr (RB == 0) factor(r, f[0]);
 #pragma unroll
             for (int q = 0; q < MB; ++q)
 #pragma unroll
-                for (int p = 0; p < PT; ++p) w[q][p] = RB ? here[((q * RB + r) * PT + p) * 32] : tt[((int64_t)(b * ranks + r) * PT + p) * 32 + lane];
+                for (int p = 0; p < kPlanes; ++p) w[q][p] = RB ? here[((q * RB + r) * kPlanes + p) * 32] : tt[((int64_t)(b * ranks + r) * kPlanes + p) * 32 + lane];
             float d[MB][4][4] = {};
-            auto& sum = PT == 3 ? d : acc;  // a 16-bit result can stand one running sum
+            auto& sum = RB == 1 ? acc : d;  // (a sum grows for the products of 16 rank indices only)
 #pragma unroll
-            for (int both = PT - 1; both >= 0; --both)
+            for (int both = kPlanes - 1; both >= 0; --both)
 #pragma unroll
                 for (int pt = 0; pt <= both; ++pt)
 #pragma unroll
@@ -646,7 +641,7 @@ __global__ void __launch_bounds__(256, 2) adapter_up_kernel(const __grid_constan
                             const uint4 e = f[RB ? r : 0][both - pt][k >> 1];
                             mma(sum[q][k], w[q][pt].x, w[q][pt].y, w[q][pt].z, w[q][pt].w, k & 1 ? e.z : e.x, k & 1 ? e.w : e.y);
                         }
-            if (PT == 3)
+            if (RB != 1)
 #pragma unroll
                 for (int q = 0; q < MB; ++q)
 #pragma unroll
@@ -1146,22 +1141,20 @@ int tensor_up(void* y, Rows base, Low low, const AdapterShape& z, int64_t h, boo
     a.base = base.p; a.y = y; a.image = (const char*)image; a.t_up = (const char*)low.up; a.base_ws = base.worker_stride;
     a.base_rs = base.row_stride; a.image_ws = shared ? 0 : tensor::up_image(h, z.rank); a.rows = (uint32_t)z.rows; a.h = (int32_t)h; a.rank = z.rank;
     a.scale = scale; a.drop = d;
-    const bool several = tensor::groups_of(z.rank) > 1;
-    const int64_t wide = tensor::padded_rank(z.rank) == 64 && !several ? tensor::up_columns<64, false>() : tensor::up_columns<16, false>();
-    const int64_t columns = (h + wide - 1) / wide, blocks = (z.rows + 127) / 128;
-    a.chunks = (uint32_t)parts_of(columns * z.n, several ? 148 : 2 * 148, blocks, 0.5, 65535 / z.n, false);
-    const bool vec = h % 8 == 0 && (!base.p || base.aligned()) && packed(y, z.rows, h, base.type).aligned();
+    const bool several = tensor::groups_of(z.rank) > 1, vec = h % 8 == 0 && (!base.p || base.aligned()) && packed(y, z.rows, h, base.type).aligned();
     return by_rank(z, [&](auto v) {
         constexpr int R = decltype(v)::value;
-        auto kernel = vec ? tensor::up_kernel<R, true, false> : tensor::up_kernel<R, false, false>;
-        int shared_bytes = tensor::up_shared<R, false>();
+        auto go = [&](auto g) {
+            constexpr bool GROUPS = decltype(g)::value;
+            using U = tensor::Up<R, GROUPS>;
+            const int64_t columns = (h + U::kColumns - 1) / U::kColumns, blocks = (z.rows + 127) / 128;
+            a.chunks = (uint32_t)parts_of(columns * z.n, GROUPS ? 148 : 2 * 148, blocks, 0.5, 65535 / z.n, false);
+            auto kernel = vec ? tensor::up_kernel<R, true, GROUPS> : tensor::up_kernel<R, false, GROUPS>;
+            return launched(launch_next(kernel, dim3((uint32_t)columns, (uint32_t)z.n * a.chunks), 1, U::kShared, false, stream, a), "adapter_up");
+        };
         if constexpr (R == 64)
-            if (several) {
-                kernel = vec ? tensor::up_kernel<R, true, true> : tensor::up_kernel<R, false, true>;
-                shared_bytes = tensor::up_shared<R, true>();
-            }
-        return launched(launch_next(kernel, dim3((uint32_t)columns, (uint32_t)z.n * a.chunks), 1, shared_bytes, false, stream, a),
-                        "adapter_up");
+            if (several) return go(Int<1>());
+        return go(Int<0>());
     });
 }
 
@@ -1337,7 +1330,7 @@ Places places(const AdapterShape& z, bool shared, bool backward, bool sum_worker
     if (frags) {
         p.down = take(factors * either(down_frag_words(dh, z.rank), tensor::down_image(dh, z.rank)));
         p.up = take(factors * either(up_frag_words(uh, z.rank), tensor::up_image(uh, z.rank)));
-        p.t_up = take(z.n * either(t_up_words(z.rows, z.rank, kPlanes), tensor::t_up_image(z.rows, z.rank)));
+        p.t_up = take(z.n * either(t_up_words(z.rows, z.rank), tensor::t_up_image(z.rows, z.rank)));
     }
     if (frags && backward) {
         p.t_outer = take(z.n * either(t_outer_words(z.rows, z.rank), tensor::t_outer_image(z.rows, z.rank)));

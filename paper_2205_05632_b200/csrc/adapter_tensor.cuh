@@ -37,10 +37,14 @@ struct By {
     static constexpr int kN = 3 * R;                       // planes side by side
     static constexpr int kPlanesBytes = kN * 128;          // planes: rows of 64 elements
     static constexpr uint32_t kColumns = R == 64 ? 512 : R == 32 ? 256 : 128;  // of tensor memory: 2 kN used, a power of two taken
-    // up: two planes of 128 rows; up to 32 they share the rows' 128 bytes
-    static constexpr int kUpTiles = R == 64 ? 2 : 1, kUpBytes = kUpTiles * kTileBytes;
-    static constexpr uint32_t kUpPlane = R == 64 ? kTileBytes : 2 * R;  // from plane 0 to plane 1
+    // up: tiles of 128 rows for the three planes; they share a row's 128 bytes as far as they have room
+    static constexpr int kUpTiles = R == 64 ? 3 : R == 32 ? 2 : 1, kUpBytes = kUpTiles * kTileBytes;
 };
+// Where plane p of an operand of up lies: the tile and the byte of the row.
+template <int R>
+__host__ __device__ constexpr uint32_t up_tile(uint32_t p) { return p * 2 * R / 128; }
+template <int R>
+__host__ __device__ constexpr uint32_t up_byte(uint32_t p) { return p * 2 * R % 128; }
 // The stages of down (ACROSS = false) and outer: two tiles of the activation, which go to a sum each, and planes. outer: 64 rows of 256
 // columns. down: 64 columns of 256 rows, or, up to rank 32, 128 columns of 128 rows (WIDE), whose two sums are of the same rows and are
 // added in the end: twice as many CTAs for a few thousand rows (4096 x 4096, rank 16: 15.5 -> 13.7 us), for planes read twice as often.
@@ -60,9 +64,12 @@ struct Pipe {
 // ---- images of the fp32 operands in global memory, in the order of shared memory --------------------------------------------
 
 // All begin with the group of ranks. A factor for down: [64 columns, an even number of times][plane, rank][64 columns]; for up: [128 columns]
-// [plane 0, 1][column][rank] (the planes within a column's 128 bytes up to 32 ranks). Bytes of a group, and of a worker's.
+// [tile][column][plane, rank]: a column's 128 bytes hold a plane of 64 ranks, two of 32, all three of 16. Bytes of a group, and of a worker's.
 __host__ __device__ inline int64_t down_group(int64_t h, int rank) { return (h + 127) / 128 * (2 * 3 * 128 * padded_rank(rank)); }
-__host__ __device__ inline int64_t up_group(int64_t h, int rank) { return (h + 127) / 128 * (kTileBytes << (padded_rank(rank) == 64)); }
+__host__ __device__ inline int64_t up_group(int64_t h, int rank) {
+    const int r = padded_rank(rank);
+    return (h + 127) / 128 * kTileBytes * (r == 64 ? By<64>::kUpTiles : r == 32 ? By<32>::kUpTiles : By<16>::kUpTiles);
+}
 __host__ __device__ inline int64_t down_image(int64_t h, int rank) { return groups_of(rank) * down_group(h, rank); }
 __host__ __device__ inline int64_t up_image(int64_t h, int rank) { return groups_of(rank) * up_group(h, rank); }
 // t for outer: [64 rows][plane, rank][row]; for up: [128 rows], as a factor's columns.
@@ -160,12 +167,11 @@ __device__ __forceinline__ void planes8(const float (&v)[8], uint4 (&out)[3]) {
     for (int p = 0; p < 3; ++p) out[p] = make_uint4(w[0][p], w[1][p], w[2][p], w[3][p]);
 }
 
-// The first two planes of eight ranks of a row (a column of the factor) in an image for up.
+// The planes of eight ranks of a row (a column of the factor) in an image for up.
 template <int R>
 __device__ __forceinline__ void store_up(char* tile, uint32_t row, uint32_t c, const uint4 (&w)[3]) {
 #pragma unroll
-    for (uint32_t p = 0; p < 2; ++p)
-        *reinterpret_cast<uint4*>(tile + (R == 64 ? p * kTileBytes + swizzled(row, c) : swizzled(row, p * (R / 8) + c))) = w[p];
+    for (uint32_t p = 0; p < 3; ++p) *reinterpret_cast<uint4*>(tile + up_tile<R>(p) * kTileBytes + swizzled(row, up_byte<R>(p) / 16 + c)) = w[p];
 }
 
 // ---- prepare ---------------------------------------------------------------------------------------------------------------
@@ -577,21 +583,26 @@ __global__ void __launch_bounds__(kThreads, 1) outer_kernel(const __grid_constan
 
 // A CTA takes CN columns, whose planes of the factor stay in shared memory, and goes through the 128-row tiles of a chunk: the planes of t
 // and the base of the next tile are on their way while this one is done; products of 16 rank indices (the planes' indices together at
-// most 1); the result into the base's place in shared memory and from there to memory by rows. Two CTAs to an SM: while one waits for its
-// products the other's loads run. Rank 64, 8 workers of 2048 rows: 8192 columns, 537 MB with the base, 121 us (4.4 TB/s); 4096 for dx
-// with dropout, 134 MB, 77 us. Rank 8, 4096 columns: 46 us for 268 MB (5.9 TB/s), 66 for dx with dropout. Bound by memory with a base,
-// by the generator without one.
+// most 2, the smallest first); the result into the base's place in shared memory and from there to memory by rows. Two CTAs to an SM: while
+// one waits for its products the other's loads run. With 64 ranks there is room for one tile's planes of t: the next are asked for when the
+// products are done, so they come while the results leave.
 //
 // GROUPS: of several groups of 64 ranks. A tile takes a round per group, whose products go onto the same sums, and the factor's planes come
-// with t's for every round; one CTA of 128 columns to an SM: rank 128, 8192 columns 206 us (2.6 TB/s), 4096 for dx with dropout 130; with
-// 64 columns 266 and 160. (One group, rank 64: two CTAs of 64 columns 123 and 78 us, one of 128 146 and 99.)
+// with t's for every round; one CTA of 128 columns to an SM, and one tile of the base, asked for when the tile before it has left. The
+// small products (indices 1 and 2) have a sum of their own over all groups, so that the tensor cores' cuts of the sum are few.
+//
+// 8 workers of 2048 rows. Rank 16, 4096 columns: 47 us for 268 MB with the base (5.7 TB/s), 69 for dx with dropout, 134 MB: bound by
+// memory, and by the generator. Rank 64, 8192 columns: 160 us for 537 MB (3.4 TB/s), 4096 columns for dx with dropout 97; rank 32, 4096
+// columns 70 and 81: bound by shared memory, through which six products of planes and the planes of t pass for every tile (one CTA of 128
+// columns to an SM reads less and waits more: rank 64 190 and 117, rank 32 78 and 104). Rank 128, 8192 columns 272 us, dx 164.
 template <int R, bool GROUPS>
-__host__ __device__ constexpr int up_columns() { return R == 64 && !GROUPS ? 64 : 128; }  // CN
-template <int R, bool GROUPS>
-__host__ __device__ constexpr int up_shared() {
-    constexpr int CN = up_columns<R, GROUPS>();
-    return (GROUPS ? 2 : 1) * By<R>::kUpTiles * CN * 128 + 2 * By<R>::kUpBytes + 2 * 256 * CN + 256;
-}
+struct Up {
+    static constexpr int kColumns = R == 16 || GROUPS ? 128 : 64;                    // CN
+    static constexpr int kRow = 2 * kColumns;                                        // bytes of a row of the base's tile
+    static constexpr int kFactorTile = kColumns * 128, kFactorBytes = By<R>::kUpTiles * kFactorTile, kFactors = GROUPS ? 2 : 1;
+    static constexpr int kTs = R == 64 && !GROUPS ? 1 : 2, kBases = GROUPS ? 1 : 2;  // tiles of t and of the base
+    static constexpr int kShared = kFactors * kFactorBytes + kTs * By<R>::kUpBytes + kBases * 128 * kRow + 256;
+};
 
 struct UpArgs {
     const void* base;  // may be null
@@ -608,18 +619,18 @@ template <int R, bool VEC, bool GROUPS>
 __global__ void __launch_bounds__(256, GROUPS ? 1 : 2) up_kernel(const __grid_constant__ UpArgs a) {
     extern __shared__ __align__(1024) char smem[];  // (all of it: nothing static, so it starts on the boundary, and two CTAs fit)
     using B = By<R>;
-    constexpr int CN = up_columns<R, GROUPS>(), kRow = 2 * CN, kPlaneBytes = CN * 128;  // bytes of a tile's row; of a plane of the factor (R = 64)
-    constexpr uint32_t kMemory = CN;
+    using U = Up<R, GROUPS>;
+    constexpr int CN = U::kColumns, kRow = U::kRow;
+    constexpr uint32_t kMemory = GROUPS ? 2 * CN : CN;
     using P = Pipe<R, true>;
-    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + up_shared<R, GROUPS>() - 256);
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + U::kShared - 256);
     uint32_t* word = reinterpret_cast<uint32_t*>(bars + P::kBars);
     bool lost = false;  // a wait gave up
     dependency_wait();
     uint32_t memory;
     tensor_begin<P>(bars, word, kMemory, memory);
-    // tile: 128 rows, chunk c at c ^ (row % 8)
-    constexpr int kFactorBytes = B::kUpTiles * kPlaneBytes;  // bytes of the factor's
-    char *planes = smem, *t0 = smem + (GROUPS ? 2 : 1) * kFactorBytes, *tile0 = t0 + 2 * B::kUpBytes;
+    // a tile of the base: 128 rows, chunk c at c ^ (row % 8)
+    char *planes = smem, *t0 = smem + U::kFactors * U::kFactorBytes, *tile0 = t0 + U::kTs * B::kUpBytes;
     const uint32_t i = blockIdx.y / a.chunks, chunk = blockIdx.y - i * a.chunks, blocks = (a.rows + 127) / 128;
     const uint32_t b0 = (uint32_t)((uint64_t)blocks * chunk / a.chunks), b1 = (uint32_t)((uint64_t)blocks * (chunk + 1) / a.chunks);
     const int c0 = (int)blockIdx.x * CN, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -634,8 +645,8 @@ __global__ void __launch_bounds__(256, GROUPS ? 1 : 2) up_kernel(const __grid_co
 #pragma unroll
         for (int p = 0; p < B::kUpTiles; ++p)
 #pragma unroll
-            for (int k = 0; k < kPlaneBytes / 16 / 256; ++k)
-                copy16(to + p * kPlaneBytes + (threadIdx.x + 256 * k) * 16, from + p * kTileBytes + (threadIdx.x + 256 * k) * 16);
+            for (int k = 0; k < U::kFactorTile / 16 / 256; ++k)
+                copy16(to + p * U::kFactorTile + (threadIdx.x + 256 * k) * 16, from + p * kTileBytes + (threadIdx.x + 256 * k) * 16);
     };
     // What a thread brings to a tile it takes away too. VEC: a column of chunks, every (256 / chunks of a row)-th row's; elsewhere a warp has
     // every eighth row and a lane every 32nd element.
@@ -643,62 +654,83 @@ __global__ void __launch_bounds__(256, GROUPS ? 1 : 2) up_kernel(const __grid_co
     const uint32_t r0 = threadIdx.x / kChunks, q0 = threadIdx.x % kChunks, at0 = r0 * kRow + ((q0 ^ (r0 & 7u)) << 4);
     const int column = c0 + (int)q0 * 8;
     auto element = [&](uint32_t row, uint32_t c) { return row * kRow + (((c >> 3) ^ (row & 7u)) << 4) + (c & 7u) * 2; };
-    auto fetch = [&](uint32_t b, int group, uint32_t turn) {
-        if (b < b1) {
-            char *t = t0 + (turn & 1u) * B::kUpBytes, *tile = tile0 + ((b - b0) & 1u) * (128 * kRow);
-            const char* from = t_image + group * t_up_group(a.rows, a.rank) + (int64_t)b * B::kUpBytes;
-            if (GROUPS) fetch_planes(group, planes + (turn & 1u) * kFactorBytes);
+    auto tile_of = [&](uint32_t b) { return tile0 + (U::kBases == 2 ? ((b - b0) & 1u) * (128 * kRow) : 0); };
+    auto fetch_base = [&](uint32_t b) {
+        if (!a.base || b >= b1) return;
+        char* tile = tile_of(b);
+        if constexpr (VEC) {
+            const __nv_bfloat16* x = base + (int64_t)(b * 128 + r0) * a.base_rs + column;
 #pragma unroll
-            for (int k = 0; k < B::kUpBytes / 16 / 256; ++k) copy16(t + (threadIdx.x + 256 * k) * 16, from + (threadIdx.x + 256 * k) * 16);
-            if (a.base && group == 0) {
-                if constexpr (VEC) {
-                    const __nv_bfloat16* x = base + (int64_t)(b * 128 + r0) * a.base_rs + column;
-#pragma unroll
-                    for (uint32_t k = 0; k < 128 / kRows; ++k) {
-                        const bool in = column < a.h && b * 128 + r0 + kRows * k < a.rows;
-                        copy16(tile + at0 + k * kRows * kRow, in ? (const void*)(x + k * kRows * a.base_rs) : a.base, in);
-                    }
-                } else {
-                    for (uint32_t r = warp; r < 128; r += 8)
-#pragma unroll
-                        for (int c = lane; c < CN; c += 32)
-                            if (b * 128 + r < a.rows && c0 + c < a.h)
-                                *reinterpret_cast<__nv_bfloat16*>(tile + element(r, c)) = __ldg(base + (int64_t)(b * 128 + r) * a.base_rs + c0 + c);
-                }
+            for (uint32_t k = 0; k < 128 / kRows; ++k) {
+                const bool in = column < a.h && b * 128 + r0 + kRows * k < a.rows;
+                copy16(tile + at0 + k * kRows * kRow, in ? (const void*)(x + k * kRows * a.base_rs) : a.base, in);
             }
+        } else {
+            for (uint32_t r = warp; r < 128; r += 8)
+#pragma unroll
+                for (int c = lane; c < CN; c += 32)
+                    if (b * 128 + r < a.rows && c0 + c < a.h)
+                        *reinterpret_cast<__nv_bfloat16*>(tile + element(r, c)) = __ldg(base + (int64_t)(b * 128 + r) * a.base_rs + c0 + c);
         }
-        copies_commit();
+    };
+    auto fetch_t = [&](uint32_t b, int group, uint32_t turn) {
+        if (b >= b1) return;
+        char* t = t0 + (U::kTs == 2 ? (turn & 1u) * B::kUpBytes : 0);
+        const char* from = t_image + group * t_up_group(a.rows, a.rank) + (int64_t)b * B::kUpBytes;
+        if (GROUPS) fetch_planes(group, planes + (turn & 1u) * U::kFactorBytes);
+#pragma unroll
+        for (int k = 0; k < B::kUpBytes / 16 / 256; ++k) {
+            const uint32_t e = threadIdx.x + 256 * k;
+            if (R == 32 && k >= 4 && ((e ^ e >> 3) & 4u)) continue;  // the second tile's empty half
+            copy16(t + e * 16, from + e * 16);
+        }
     };
     if (!GROUPS) fetch_planes(0, planes);
-    fetch(b0, 0, 0);
+    fetch_t(b0, 0, 0);
+    fetch_base(b0);
+    copies_commit();
     uint32_t turn = 0, b = b0;
     for (int group = 0; b < b1; ++turn) {
         const bool last = !GROUPS || group + 1 == groups;
-        fetch(last ? b + 1 : b, last ? 0 : group + 1, turn + 1);
-        copies_wait<1>();
+        if constexpr (U::kTs == 2) {
+            fetch_t(last ? b + 1 : b, last ? 0 : group + 1, turn + 1);
+            if (!GROUPS) fetch_base(b + 1);
+            copies_commit();
+            copies_wait<1>();  // (GROUPS: the base was asked for in an earlier round than the tile's last)
+        } else {
+            copies_wait<0>();
+        }
         fence_shared();
         fence_before();
         __syncthreads();
-        char* tile = tile0 + ((b - b0) & 1u) * (128 * kRow);
+        char* tile = tile_of(b);
         if (threadIdx.x == 0) {
             fence_after();
-            const uint32_t left = shared_address(t0 + (turn & 1u) * B::kUpBytes);
-            const uint32_t right = shared_address(planes) + (GROUPS ? (turn & 1u) * kFactorBytes : 0);
-            constexpr uint32_t kRightPlane = R == 64 ? kPlaneBytes : 2 * R;
+            const uint32_t left = shared_address(t0) + (U::kTs == 2 ? (turn & 1u) * B::kUpBytes : 0);
+            const uint32_t right = shared_address(planes) + (GROUPS ? (turn & 1u) * U::kFactorBytes : 0);
 #pragma unroll
-            for (int q = 0; q < 3; ++q) {  // (0, 1), (1, 0), (0, 0): the smallest first
-                const uint32_t l = left + (q == 1 ? B::kUpPlane : 0), r = right + (q == 0 ? kRightPlane : 0);
+            for (int both = 2; both >= 0; --both)  // the planes' indices together
 #pragma unroll
-                for (int k = 0; k < R / 16; ++k)
-                    product(memory, operand(l + k * 32, 16), operand(r + k * 32, 16), instruction(CN, false, false),
-                            q > 0 || k > 0 || (GROUPS && group > 0));
-            }
+                for (int p = 0; p <= both; ++p) {
+                    const uint32_t l = left + up_tile<R>(p) * kTileBytes + up_byte<R>(p);
+                    const uint32_t r = right + up_tile<R>(both - p) * U::kFactorTile + up_byte<R>(both - p);
+                    const bool apart = GROUPS && both > 0, fresh = both == 2 ? p == 0 : GROUPS && both == 0;
+#pragma unroll
+                    for (int k = 0; k < R / 16; ++k)
+                        product(memory + (apart ? CN : 0), operand(l + k * 32, 16), operand(r + k * 32, 16), instruction(CN, false, false),
+                                !fresh || k > 0 || (GROUPS && group > 0));
+                }
             products_done(bar);
         }
+        if constexpr (U::kTs == 1) fetch_base(b + 1);
         // a lane's row: CN / 2 columns from CN / 2 (warp / 4) on
         const uint32_t r = (uint32_t)(warp & 3) * 32 + lane, row = b * 128 + r;
         lost = lost || !barrier_wait(bar, turn & 1u);
         fence_after();
+        if constexpr (U::kTs == 1) {
+            fetch_t(b + 1, 0, turn + 1);
+            copies_commit();
+        }
         if (!last) {
             ++group;
             continue;
@@ -709,6 +741,13 @@ __global__ void __launch_bounds__(256, GROUPS ? 1 : 2) up_kernel(const __grid_co
             float v[32];
             columns(memory + ((uint32_t)(warp & 3) << 21) + first, v);
             columns_wait(v);
+            if constexpr (GROUPS) {
+                float w[32];
+                columns(memory + ((uint32_t)(warp & 3) << 21) + CN + first, w);
+                columns_wait(w);
+#pragma unroll
+                for (int e = 0; e < 32; ++e) v[e] += w[e];
+            }
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const uint32_t c = (uint32_t)(first >> 3) + k;
@@ -739,12 +778,14 @@ __global__ void __launch_bounds__(256, GROUPS ? 1 : 2) up_kernel(const __grid_co
                         y[(int64_t)(b * 128 + q) * a.h + c0 + c] = *reinterpret_cast<const __nv_bfloat16*>(tile + element(q, c));
         }
         ++b;
+        if (GROUPS) fetch_base(b);  // (its copies are counted with the next round's)
         group = 0;
     }
     copies_wait<0>();
     if (lost) gave_up = 1;
     tensor_end(memory, kMemory);
 }
+
 
 }  // namespace tensor
 }  // namespace
