@@ -16,10 +16,12 @@
 // the places of the operand that this lane has to hold. No exchange between lanes stands between memory and mma.sync; the factors and t
 // wait in the order of the lanes' registers and come through the L1.
 //
-// Precision. mma.sync multiplies bf16 exactly and adds in fp32. An fp32 number is the sum of three bf16 numbers, its planes (8 bits
-// each, cut, not rounded: the rest after each cut is exact, nothing overflows); fp16 needs two and bf16 is one. Products of planes
-// i and j are formed for i + j <= 2, which leaves out less than 2^-21 of a product, also where the result is a 16-bit number (y, dx): base
-// and adapter may cancel, and a result near the border of two roundings should fall where fp32 arithmetic lets it fall.
+// Precision. mma.sync multiplies bf16 exactly and adds in fp32. An fp32 number is the sum of three bf16 numbers, its planes: each is the
+// rest of those before it, rounded, and every rest is exact (of numbers below 2^-110 what lies under 2^-133 is lost); fp16 needs two and
+// bf16 is one. Products of planes i and j are formed for i + j <= 2, which leaves out at most 2^-24 of a product, of either sign: as fp32
+// arithmetic does. (Planes that are cut instead of rounded leave out up to 2^-21, always towards zero.) So also where the result is a
+// 16-bit number (y, dx): base and adapter may cancel, and a result near the border of two roundings should fall where fp32 arithmetic
+// lets it fall.
 #include <cooperative_groups.h>
 #include <string.h>
 
@@ -78,16 +80,18 @@ __device__ __forceinline__ void mma_first(float (&c)[4], uint32_t a0, uint32_t a
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
 }
 
-// The first P planes of two numbers, packed. The rest of an infinity is 0, of what is not a number itself.
+// The first P planes of two numbers, packed. All but the last are held to finite numbers, so that the largest numbers are not rounded to an
+// infinity, whose rest would be the other; an infinity arrives in the last plane.
 template <int P>
 __device__ __forceinline__ void split2(float a, float b, uint32_t (&planes)[P]) {
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-        planes[p] = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
         if (p + 1 < P) {
-            const float ha = __uint_as_float(__float_as_uint(a) & 0xffff0000u), hb = __uint_as_float(__float_as_uint(b) & 0xffff0000u);
-            a = a == ha ? 0.0f : a - ha;
-            b = b == hb ? 0.0f : b - hb;
+            asm("cvt.rn.satfinite.bf16x2.f32 %0, %1, %2;" : "=r"(planes[p]) : "f"(b), "f"(a));
+            a -= __uint_as_float(planes[p] << 16);
+            b -= __uint_as_float(planes[p] & 0xffff0000u);
+        } else {
+            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(planes[p]) : "f"(b), "f"(a));
         }
     }
 }

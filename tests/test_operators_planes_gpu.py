@@ -3,9 +3,10 @@ product of two numbers with full significands, so an operand that lost a part of
 elsewhere.
 
 Tolerances, in units of E = 2^-24 of the product. An fp32 number is the sum of its three bf16 planes exactly, and products of planes
-are exact, so dt, t and what multiplies a one are exact. Left out are the products of planes i + j > 2: less than 8 (planes that are cut;
-2^-21). A sum of planes' products takes the small ones first: the last addition may cut 2 (a unit in the last place), those before it
-2^-6 of that each; fp32 additions and the scale, which is 1, round by 1 at most."""
+are exact, so dt, t and what multiplies a one are exact. Left out are the products of planes i + j > 2: at most 8 where planes are cut
+(2^-21), and 1 where they are rounded: with a in [1, 2) plane 1 is at most 2^-8 and plane 2 2^-17, so (1, 2) and (2, 1) are 2^-24
+together, and 0.89 is the largest that 4 million pairs give. A sum of planes' products takes the small ones first: the last addition may
+cut 2 (a unit in the last place), those before it 2^-6 of that each; fp32 additions and the scale, which is 1, round by 1 at most."""
 import pytest
 import torch
 
@@ -30,10 +31,10 @@ def ones_of_rows(n, rows, h, dtype, device):
     return torch.zeros(n, rows, h, dtype=dtype, device=device).scatter_(2, at[..., None], 1.0), at
 
 
-def one_of_columns(g, n, rows, h, dtype):
+def one_of_columns(g, n, rows, h, dtype, numbers=full):
     """[n, rows, h] with one number in every column, the row of it [n, h], and the numbers [n, h]."""
     at = (11 * torch.arange(h, device=g.device)[None] + torch.arange(n, device=g.device)[:, None]) % rows
-    v = full(g, n, h).to(dtype)
+    v = numbers(g, n, h).to(dtype)
     return torch.zeros(n, rows, h, dtype=dtype, device=g.device).scatter_(1, at[:, None], v[:, None]), at, v
 
 
@@ -95,6 +96,76 @@ def test_gradients_of_the_factors_use_t_and_dt_in_full(rows, rank, dtype):
     dt = pick(R.d(b), at.cpu())
     da, = torch.autograd.grad(low_rank_adapter(x, None, a, b), a, dy)
     check(da, (pick(dt, row.cpu()) * R.d(v)[..., None]).transpose(1, 2), 5, "dA")
+
+
+def hard(g, *shape):
+    """full(), but of every two numbers one with the significand 1 + 2^-7 - 2^-23, whose planes leave most when they are cut."""
+    v = full(g, *shape)
+    at = torch.arange(v.numel(), device=g.device).reshape(shape) % 2 == 0
+    return torch.where(at, torch.ldexp(torch.full_like(v, float(0x80ffff)), torch.frexp(v)[1] - 24) * v.sign(), v)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,rank", SIZES)
+def test_planes_leave_out_no_more_than_fp32_arithmetic(rows, rank):
+    """Products of two fp32 numbers, both with all of their planes. Left out 1, the last addition 2 or an fp32 one, before it 2^-5."""
+    n, h, out = 2, 136, 264
+    g = torch.Generator(device="cuda").manual_seed(4)
+    units = 3.1
+    # t: x has one number in a row, and B passes t on
+    x, at = ones_of_rows(n, rows, h, F32, g.device)
+    v = hard(g, n, rows, 1)
+    a = hard(g, n, rank, h)
+    which = (5 * torch.arange(out, device=g.device)[None] + torch.arange(n, device=g.device)[:, None]) % rank
+    b = torch.zeros(n, out, rank, device=g.device).scatter_(2, which[..., None], 1.0)
+    t = pick(R.d(a).transpose(1, 2), at.cpu()) * R.d(v)
+    check(low_rank_adapter(x * v, None, a, b), t.gather(2, which.cpu()[:, None].expand(n, rows, out)), units, "t")
+    # y, in all types: t is a column of A
+    b = torch.zeros(n, out, rank, device=g.device).scatter_(2, which[..., None], hard(g, n, out, 1))
+    want = pick(R.d(a).transpose(1, 2), at.cpu()) @ R.d(b).transpose(1, 2)
+    for dtype in (F32, BF16, F16):
+        check(low_rank_adapter(x.to(dtype), None, a, b), want, units, "y")
+    # dB, dA
+    a, b = a.requires_grad_(), hard(g, n, out, rank).requires_grad_()
+    dy, row, v = one_of_columns(g, n, rows, out, F32, hard)
+    t = pick(R.d(a).transpose(1, 2), at.cpu())
+    db, = torch.autograd.grad(low_rank_adapter(x, None, a, b), b, dy)
+    check(db, pick(t, row.cpu()) * R.d(v)[..., None], units, "dB")
+    dy, at = ones_of_rows(n, rows, out, F32, g.device)
+    x, row, v = one_of_columns(g, n, rows, h, F32, hard)
+    dt = pick(R.d(b), at.cpu())
+    da, = torch.autograd.grad(low_rank_adapter(x, None, a, b), a, dy)
+    check(da, (pick(dt, row.cpu()) * R.d(v)[..., None]).transpose(1, 2), units, "dA")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,rows", [(F32, 3), (F32, 40), (F16, 40), (BF16, 40), (BF16, 200)])
+def test_the_largest_numbers_and_infinities(dtype, rows):
+    """Numbers that a rounding to eight bits would take beyond the largest stay finite; an infinity in a factor reaches what it should."""
+    g = torch.Generator(device="cuda").manual_seed(5)
+    h, out, rank = 64, 72, 8
+    x, at = ones_of_rows(1, rows, h, dtype, g.device)
+    big = torch.finfo(F32).max
+    a, b = torch.zeros(1, rank, h, device=g.device), torch.zeros(1, out, rank, device=g.device)
+    a[0, 0], a[0, 0, ::2] = big, -big
+    b[0, :, 0] = 2.0 ** -126
+    want = R.d(a)[0, 0][at.cpu()][..., None] * 2.0 ** -126
+    check(low_rank_adapter(x, None, a, b), want.expand(1, rows, out), 3.1, "largest")
+    b[0, 5, 2] = float("-inf")  # of one column of y
+    a[0, 2] = 1.0
+    y = low_rank_adapter(x, None, a, b)
+    others = torch.arange(out, device=g.device) != 5
+    assert not torch.isfinite(y[0, :, 5]).any() and torch.isfinite(y[0][:, others]).all()
+    b[0, 5, 2] = 0.0
+    x[0, 1] *= float("inf")  # of one row; its zeros become NaN
+    y = low_rank_adapter(x, None, a, b)
+    others = torch.arange(rows, device=g.device) != 1
+    assert not torch.isfinite(y[0, 1]).any() and torch.isfinite(y[0, others]).all()
+    x[0, 1] = 0.0
+    x[0, 1, 4] = float("inf")
+    assert not torch.isfinite(low_rank_adapter(x, None, a, b)[0, 1]).any()
+    a[0, 1, 3] = float("inf")  # of a column of A: every row has it, times 0 or not
+    assert not torch.isfinite(low_rank_adapter(x, None, a, b)).any()
 
 
 def planes(v):
