@@ -302,8 +302,8 @@ __host__ __device__ constexpr int backward_slots() { return NG * (raw_slots<TX>(
 
 // The sums of dy xhat and dy of a chunk's rows stay in registers, the weight too. With several spans to a warp the values are taken
 // a second time behind the barrier instead of being held, and with four the weight is read again for each row: registers are what
-// bounds the CTAs of an SM. 16384 rows of 4096 in bfloat16, 403 MB, take 77 us (5.2 TB/s); with dropout, the second incoming gradient
-// and the residual's, 32768 rows, 1.34 GB, 230 us (5.8 TB/s). 8192 rows of 16000, four spans to a warp, take 427 us with the forward
+// bounds the CTAs of an SM. 16384 rows of 4096 in bfloat16, 403 MB, take 79 us (5.1 TB/s); with dropout, the second incoming gradient
+// and the residual's, 32768 rows, 1.34 GB, 237 us (5.7 TB/s). 8192 rows of 16000, four spans to a warp, take 427 us with the forward
 // pass, 2.6 times the bytes' time: the weights are read again from the L2 for each row.
 template <typename TX, typename TR, int W, int NG, int L, bool VEC, bool ADD>
 __global__ void __launch_bounds__(norm_threads<W>(), norm_ctas<W, NG, VEC, true, ADD>()) norm_backward_kernel(const __grid_constant__ NormArgs a) {
@@ -361,7 +361,7 @@ __global__ void __launch_bounds__(norm_threads<W>(), norm_ctas<W, NG, VEC, true,
             copies_wait<kStages - 1>();  // a lane's own
         }
         Pair g[4], xhat[4], sum1 = pair(0.0f), sum2 = pair(0.0f);
-        const Pair rstd = pair(st.y), shift = pair(-st.x * st.y);
+        const Pair rstd = pair(st.y), less_mean = pair(-st.x);
         // dy w and xhat of span q; the first time its share of the sums
         auto values = [&](int q, bool first) {
             const int c0 = (q * W + warp) * kSpan;
@@ -371,7 +371,7 @@ __global__ void __launch_bounds__(norm_threads<W>(), norm_ctas<W, NG, VEC, true,
             if (!kHoldWeight) weight(q, w);
 #pragma unroll
             for (int p = 0; p < 4; ++p) {
-                xhat[p] = fma(xhat[p], rstd, shift);
+                xhat[p] = mul(add(xhat[p], less_mean), rstd);  // (a product with the mean would leave its rounding in rows far from zero)
                 if (first) {
                     db[q][p] = add(db[q][p], g[p]);
                     dw[q][p] = fma(g[p], xhat[p], dw[q][p]);
