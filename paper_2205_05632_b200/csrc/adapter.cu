@@ -1434,6 +1434,7 @@ int compams_adapter_backward(void* dx, float* da, float* db, int32_t sum_workers
         !float_aligned(da) || !float_aligned(db) || !xin.element_aligned() || !gin.element_aligned() ||
         !packed(dx, rows, in, type).element_aligned())
         return COMPAMS_ERR_INVALID_ARG;
+    if (!dx && !da && !db) return COMPAMS_OK;
     const Factor fa{a, a_worker_stride, a_row_stride, 1}, fb{b, b_worker_stride, 1, b_row_stride};
     char* work = (char*)workspace;
     float* partial = (float*)(work + at.partial);
