@@ -503,9 +503,12 @@ int compams_adapter_backward(void* dx, float* da, float* db, int32_t sum_workers
                              int64_t a_worker_stride, int64_t a_row_stride, const float* b, int64_t b_worker_stride,
                              int64_t b_row_stride, float scale, double p, uint64_t seed, uint32_t call, const int64_t* call_device,
                              uint32_t first_worker, void* workspace, size_t workspace_bytes, void* cuda_stream);
-/* 1 if a kernel of the adapters gave up waiting for its own copies or products since the library was loaded (then a result was
-   worthless; no size or input should bring it about), else 0. Synchronises. */
+/* 1 if a kernel of the adapters gave up waiting for its own copies or products since this was last asked on the current device, else 0.
+   What such a kernel had to compute is NaN; no size or input should bring it about. Synchronises. */
 int compams_adapter_status(int32_t* gave_up);
+/* How often the waits of the adapters' kernels try, 0 to 16384, which is also what it is at first; each try may take microseconds. With 0
+   every wait gives up at once: for tests of what happens then. For calls from now on, of the whole process. */
+int compams_adapter_wait_tries(int32_t tries);
 /* shared: both worker strides of A and B are 0, or n is 1. sum_workers matters to the backward pass alone. */
 int compams_adapter_workspace_bytes(size_t* bytes, int32_t n, int64_t rows, int64_t in, int64_t out, int32_t rank, int32_t shared,
                                     int32_t backward, int32_t sum_workers);

@@ -137,6 +137,8 @@ def load_library() -> ctypes.CDLL:
                                            + [c.c_float] + drop + [P, c.c_size_t, P])
     L.compams_adapter_status.restype = c.c_int
     L.compams_adapter_status.argtypes = [c.POINTER(I32)]
+    L.compams_adapter_wait_tries.restype = c.c_int
+    L.compams_adapter_wait_tries.argtypes = [I32]
     L.compams_adapter_workspace_bytes.restype = c.c_int
     L.compams_adapter_workspace_bytes.argtypes = [c.POINTER(c.c_size_t), I32, I64, I64, I64, I32, I32, I32, I32]
     L.compams_error_string.restype = c.c_char_p

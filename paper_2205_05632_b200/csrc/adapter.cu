@@ -1099,6 +1099,9 @@ bool box_map(CUtensorMap* map, Rows x, const AdapterShape& z, int64_t h, uint32_
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Tries of a wait in the kernels on tcgen05.mma.
+std::atomic<uint32_t> wait_tries{tensor::kTries};
+
 // The three products on tcgen05.mma; the images stand where the fragments do.
 int tensor_prepare(const AdapterShape& z, bool shared, Factor down, int64_t down_h, void* down_image, Factor up, int64_t up_h, void* up_image,
                    const float* t, void* t_image, cudaStream_t stream) {
@@ -1123,7 +1126,7 @@ int tensor_down(Low low, Rows x, const AdapterShape& z, int64_t h, bool shared, 
     tensor::Args a = {};
     a.x = x.p; a.x_ws = x.worker_stride; a.x_rs = x.row_stride; a.image = (const char*)image; a.image_ws = shared ? 0 : tensor::down_image(h, z.rank);
     a.t_up = (char*)low.up; a.t_outer = (char*)low.outer; a.out = low.t; a.rows = (uint32_t)z.rows; a.h = (int32_t)h; a.rank = z.rank;
-    a.scale = scale; a.drop = d;
+    a.tries = wait_tries.load(std::memory_order_relaxed); a.scale = scale; a.drop = d;
     return by_rank(z, [&](auto v) {
         constexpr int R = decltype(v)::value;
         using P = tensor::Pipe<R, false>;
@@ -1144,7 +1147,7 @@ int tensor_up(void* y, Rows base, Low low, const AdapterShape& z, int64_t h, boo
     tensor::UpArgs a = {};
     a.base = base.p; a.y = y; a.image = (const char*)image; a.t_up = (const char*)low.up; a.base_ws = base.worker_stride;
     a.base_rs = base.row_stride; a.image_ws = shared ? 0 : tensor::up_image(h, z.rank); a.rows = (uint32_t)z.rows; a.h = (int32_t)h; a.rank = z.rank;
-    a.scale = scale; a.drop = d;
+    a.tries = wait_tries.load(std::memory_order_relaxed); a.scale = scale; a.drop = d;
     const bool several = tensor::groups_of(z.rank) > 1, vec = h % 8 == 0 && (!base.p || base.aligned()) && packed(y, z.rows, h, base.type).aligned();
     return by_rank(z, [&](auto v) {
         constexpr int R = decltype(v)::value;
@@ -1166,6 +1169,7 @@ int tensor_outer(const AdapterArgs& b, Rows x, Low low, const AdapterShape& z, i
     tensor::Args a = {};
     a.x = b.x; a.x_ws = b.x_ws; a.x_rs = b.x_rs; a.image = (const char*)low.outer; a.image_ws = tensor::t_outer_image(z.rows, z.rank); a.out = b.out;
     a.sj = b.f.sj; a.sc = b.f.sc; a.rows = b.rows; a.h = b.h; a.rank = b.rank; a.chunks = b.chunks; a.scale = b.scale; a.drop = b.drop;
+    a.tries = wait_tries.load(std::memory_order_relaxed);
     return by_rank(z, [&](auto v) {
         constexpr int R = decltype(v)::value;
         CUtensorMap map;
@@ -1359,7 +1363,18 @@ extern "C" {
 
 int compams_adapter_status(int32_t* gave_up) {
     if (!gave_up) return COMPAMS_ERR_INVALID_ARG;
-    return launched(cudaMemcpyFromSymbol(gave_up, tensor::gave_up, sizeof(int32_t)), "adapter_status");
+    cudaError_t e = cudaMemcpyFromSymbol(gave_up, tensor::gave_up, sizeof(int32_t));
+    if (e == cudaSuccess && *gave_up) {
+        const int32_t none = 0;
+        e = cudaMemcpyToSymbol(tensor::gave_up, &none, sizeof(none));
+    }
+    return launched(e, "adapter_status");
+}
+
+int compams_adapter_wait_tries(int32_t tries) {
+    if (tries < 0 || tries > (int32_t)tensor::kTries) return COMPAMS_ERR_INVALID_ARG;
+    wait_tries.store((uint32_t)tries, std::memory_order_relaxed);
+    return COMPAMS_OK;
 }
 
 int compams_adapter_workspace_bytes(size_t* bytes, int32_t n, int64_t rows, int64_t in, int64_t out, int32_t rank, int32_t shared,

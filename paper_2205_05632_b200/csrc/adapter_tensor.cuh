@@ -56,9 +56,9 @@ struct Pipe {
     static constexpr int kStages = kStageBytes * 5 > 225 * 1024 ? 4 : 5;  // what 227 KB hold
     static constexpr int kShared = 1024 + kStages * kStageBytes;
     // The barriers: what is brought to a stage has landed; 256 threads have done their part on it; its products are done; the sums are
-    // ready, and drained.
+    // ready, and drained; where someone gave up: all products are done.
     static constexpr int kLanded = 0, kTouched = kStages, kEmpty = 2 * kStages, kReady = 3 * kStages, kDrained = 3 * kStages + 1,
-                         kBars = 3 * kStages + 2;
+                         kStopped = 3 * kStages + 2, kBars = 3 * kStages + 3;
 };
 
 // ---- images of the fp32 operands in global memory, in the order of shared memory --------------------------------------------
@@ -88,15 +88,18 @@ __device__ __forceinline__ void barrier_init(uint32_t bar, uint32_t count) {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
 }
 __device__ __forceinline__ void barrier_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
-// Waits for the phase of this parity to end; gives up after a number of tries, each of which the hardware may hold for a while.
-__device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity) {
-    uint32_t there = 0;
-    for (int tries = 0; tries < (1 << 14) && !there; ++tries)
+// Waits for the phase of this parity to end; gives up after a number of tries, each of which the hardware may hold for a while (0:
+// at once, whatever is there).
+constexpr uint32_t kTries = 1u << 14;
+__device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity, uint32_t most) {
+    uint32_t there = 0, tries = 0;
+    do {
         asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
                      : "=r"(there)
                      : "r"(bar), "r"(parity)
                      : "memory");
-    return there != 0u;
+    } while (!there && ++tries < most);
+    return there && most;
 }
 __device__ __forceinline__ void memory_alloc(uint32_t to, uint32_t columns) {  // a whole warp
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(to), "r"(columns) : "memory");
@@ -155,8 +158,14 @@ __device__ __forceinline__ void columns(uint32_t at, float (&v)[N]) {
     }
 }
 
-// Set where a wait gave up, which no size or input should bring about; the results of that call are then worthless.
+// Waits that give up, which no size or input should bring about. Whoever gave up marks the CTA's shared word and this one, which stays until
+// it is asked for; nobody of the CTA waits in vain again. Before the tensor memory is given back the copies and products under way are
+// waited for, with a limit of their own, and the CTA's results are NaN, so that what is computed from them shows it.
 __device__ int32_t gave_up;
+__device__ __forceinline__ void give_up(uint32_t* lost) {
+    gave_up = 1;
+    *lost = 1u;
+}
 
 // Eight planes' neighbours as a chunk of 16 bytes each.
 __device__ __forceinline__ void planes8(const float (&v)[8], uint4 (&out)[3]) {
@@ -256,17 +265,19 @@ struct Args {
     uint32_t tiles;        // down: of 256 rows, a worker's
     int32_t split;         // down: CTAs of a cluster, which share out the columns
     uint32_t chunks;       // outer: of a worker's rows
+    uint32_t tries;        // of a wait
     float scale;
     Drop drop;
 };
 
 constexpr int kThreads = 320;
 
-// Tensor memory and the barriers. The shared word that takes the address is the caller's.
+// Tensor memory and the barriers. The shared words, one that takes the address and one for who gives up, are the caller's.
 template <typename P>
 __device__ __forceinline__ void tensor_begin(uint64_t* bars, uint32_t* word, uint32_t columns, uint32_t& memory) {
     if (threadIdx.x < 32) memory_alloc(shared_address(word), columns);
     if (threadIdx.x == 0) {
+        word[1] = 0u;
         for (int k = 0; k < P::kBars; ++k)
             barrier_init(shared_address(bars + k), (k >= P::kTouched && k < P::kEmpty) || k == P::kDrained ? 256u : 1u);
         fence_shared();
@@ -285,6 +296,28 @@ __device__ __forceinline__ void tensor_end(uint32_t memory, uint32_t columns) {
     fence_after();
     if (threadIdx.x < 32) memory_free(memory, columns);
 }
+// The same for down and outer: true if someone gave up. Then products and copies may still be under way, which nobody waited for: the
+// ninth warp's thread waits for the former, the tenth's for the latter, of which it brought `turns` stages.
+template <typename P>
+__device__ __forceinline__ bool tensor_end(uint32_t memory, uint32_t columns, const uint32_t* lost, uint32_t bars, int turns) {
+    fence_before();
+    __syncthreads();
+    const bool gone = *lost != 0u;
+    if (gone) {
+        if (threadIdx.x == 256) {
+            products_done(bars + 8 * P::kStopped);
+            barrier_wait(bars + 8 * P::kStopped, 0, kTries);
+        }
+        if (threadIdx.x == 288)
+            for (int s = 0; s < min(turns, P::kStages); ++s)
+                barrier_wait(bars + 8 * (P::kLanded + s), (uint32_t)((turns - s - 1) / P::kStages) & 1u, kTries);
+        fence_before();
+        __syncthreads();
+    }
+    fence_after();
+    if (threadIdx.x < 32) memory_free(memory, columns);
+    return gone;
+}
 
 // What the parts walk: steps first, first + stride, ... below last along the columns (down: rows from row0 on) or along the rows (outer,
 // ACROSS: 256 columns from column0 on).
@@ -294,19 +327,17 @@ struct Walk {
     int column0, first, stride, last;
 };
 
-// The tenth warp's part. MAPPED: the activation is brought by TMA.
+// The tenth warp's part; gives the number of stages that it brought. MAPPED: the activation is brought by TMA.
 template <int R, bool MAPPED, bool ACROSS>
-__device__ __forceinline__ void bring(const Args& a, const CUtensorMap* map, const Walk& k, char* smem, uint32_t bars) {
+__device__ __forceinline__ int bring(const Args& a, const CUtensorMap* map, const Walk& k, char* smem, uint32_t bars, uint32_t* lost) {
     using P = Pipe<R, ACROSS>;
     const char* image = k.image;
-    int stage = 0;
+    int stage = 0, turn = 0;
     uint32_t empty = 1;  // the phase to wait for: of a stage's first round none
-    for (int step = k.first, turn = 0; step < k.last; step += k.stride, ++turn) {
-        if (turn >= P::kStages && !barrier_wait(bars + 8 * (P::kEmpty + stage), empty)) {
-            gave_up = 1;
-            for (int s = 0; s < P::kStages; ++s)  // what is under way lands before the memory is given back
-                barrier_wait(bars + 8 * (P::kLanded + s), (uint32_t)(turn / P::kStages - (s < stage ? 0 : 1)) & 1u);
-            return;
+    for (int step = k.first; step < k.last; step += k.stride, ++turn) {
+        if (turn >= P::kStages && !barrier_wait(bars + 8 * (P::kEmpty + stage), empty, a.tries)) {
+            give_up(lost);
+            break;
         }
         const uint32_t bar = bars + 8 * (P::kLanded + stage), to = shared_address(smem + stage * P::kStageBytes);
         mbar_expect(bar, P::kPlanesBytes + (MAPPED ? 2 * kTileBytes : 0));
@@ -327,11 +358,12 @@ __device__ __forceinline__ void bring(const Args& a, const CUtensorMap* map, con
             empty ^= 1u;
         }
     }
+    return turn;
 }
 
 // The ninth warp's part.
 template <int R, bool MAPPED, bool ACROSS>
-__device__ __forceinline__ void issue(const Args& a, const Walk& k, char* smem, uint32_t memory, uint32_t bars) {
+__device__ __forceinline__ void issue(const Args& a, const Walk& k, char* smem, uint32_t memory, uint32_t bars, uint32_t* lost) {
     using P = Pipe<R, ACROSS>;
     const bool touched = !MAPPED || a.drop.on;
     const uint32_t tiles = shared_address(smem);
@@ -341,13 +373,14 @@ __device__ __forceinline__ void issue(const Args& a, const Walk& k, char* smem, 
     for (int step = k.first, turn = 0; step < k.last; step += k.stride, ++turn) {
         bool ok = true;
         if (since == 0) {
-            if (turn > 0) ok = barrier_wait(bars + 8 * P::kDrained, drained);
+            if (turn > 0) ok = barrier_wait(bars + 8 * P::kDrained, drained, a.tries);
             drained ^= 1u;
         }
-        ok = ok && barrier_wait(bars + 8 * (P::kLanded + stage), here) && (!touched || barrier_wait(bars + 8 * (P::kTouched + stage), here));
+        ok = ok && barrier_wait(bars + 8 * (P::kLanded + stage), here, a.tries) &&
+             (!touched || barrier_wait(bars + 8 * (P::kTouched + stage), here, a.tries));
         if (!ok) {
-            gave_up = 1;
-            return;
+            give_up(lost);
+            break;
         }
         fence_after();
         // addresses count 16 bytes in the operands' lowest bits
@@ -370,16 +403,20 @@ __device__ __forceinline__ void issue(const Args& a, const Walk& k, char* smem, 
     }
 }
 template <int R, bool MAPPED, bool ACROSS>
-__device__ __forceinline__ void feed(const Args& a, const CUtensorMap* map, const Walk& k, char* smem, uint32_t memory, uint32_t bars) {
-    if (threadIdx.x == 256) issue<R, MAPPED, ACROSS>(a, k, smem, memory, bars);
-    if (threadIdx.x == 288) bring<R, MAPPED, ACROSS>(a, map, k, smem, bars);
+__device__ __forceinline__ int feed(const Args& a, const CUtensorMap* map, const Walk& k, char* smem, uint32_t memory, uint32_t bars,
+                                     uint32_t* lost) {
+    int turns = 0;
+    if (threadIdx.x == 256) issue<R, MAPPED, ACROSS>(a, k, smem, memory, bars, lost);
+    if (threadIdx.x == 288) turns = bring<R, MAPPED, ACROSS>(a, map, k, smem, bars, lost);
     __syncwarp();
+    return turns;
 }
 
 // The first eight warps' part: sums[r] of a thread is rank r of row (outer: column) 32 (warp % 4) + lane of tile warp / 4. Where there is
 // something to do on the tiles a thread has a column of eight chunks, every 32nd row's (or 8th row's).
 template <int R, bool MAPPED, bool ACROSS>
-__device__ __forceinline__ void sum_tiles(const Args& a, const Walk& k, char* smem, uint32_t memory, uint32_t bars, float (&sums)[R]) {
+__device__ __forceinline__ void sum_tiles(const Args& a, const Walk& k, char* smem, uint32_t memory, uint32_t bars, uint32_t* given_up,
+                                          float (&sums)[R]) {
     using P = Pipe<R, ACROSS>;
     constexpr uint32_t kRows = ACROSS ? 8 : 32, kPlace = ACROSS ? 1024 : 4096;  // from one of a thread's chunks to the next
     const int warp = threadIdx.x >> 5;
@@ -417,9 +454,9 @@ __device__ __forceinline__ void sum_tiles(const Args& a, const Walk& k, char* sm
             const uint32_t row = (ACROSS ? (uint32_t)step * 64 : k.row0) + r0;
             const int64_t column0 = (ACROSS ? (int64_t)k.column0 : (int64_t)step * P::kStep) + c0 * 8;
             if (MAPPED) {
-                lost = lost || !barrier_wait(bars + 8 * (P::kLanded + stage), here >> stage & 1u);
+                lost = lost || !barrier_wait(bars + 8 * (P::kLanded + stage), here >> stage & 1u, a.tries);
             } else if (turn >= P::kStages) {
-                lost = lost || !barrier_wait(bars + 8 * (P::kEmpty + stage), empty >> stage & 1u);
+                lost = lost || !barrier_wait(bars + 8 * (P::kEmpty + stage), empty >> stage & 1u, a.tries);
                 empty ^= 1u << stage;
             }
             here ^= 1u << stage;
@@ -449,7 +486,7 @@ __device__ __forceinline__ void sum_tiles(const Args& a, const Walk& k, char* sm
         }
         if (++since == kFlush || step + k.stride >= k.last) {
             since = 0;
-            lost = lost || !barrier_wait(bars + 8 * P::kReady, ready);
+            lost = lost || !barrier_wait(bars + 8 * P::kReady, ready, a.tries);
             ready ^= 1u;
             fence_after();
             flush();
@@ -458,7 +495,7 @@ __device__ __forceinline__ void sum_tiles(const Args& a, const Walk& k, char* sm
         }
         stage = stage + 1 == P::kStages ? 0 : stage + 1;
     }
-    if (lost) gave_up = 1;
+    if (lost) give_up(given_up);
 }
 
 // A CTA takes 256 rows of a worker, or 128 (WIDE), and its share of the columns. Rank 64, 8 workers of 2048 rows: 8192 columns, 268 MB,
@@ -469,26 +506,27 @@ __global__ void __launch_bounds__(kThreads, 1) down_kernel(const __grid_constant
     extern __shared__ __align__(16) char dynamic[];
     using P = Pipe<R, false>;
     __shared__ uint64_t bars[P::kBars];
-    __shared__ uint32_t word;
+    __shared__ uint32_t word[2];
     dependency_wait();
     uint32_t memory;
     char* smem = aligned(dynamic);
-    tensor_begin<P>(bars, &word, By<R>::kColumns, memory);
+    tensor_begin<P>(bars, word, By<R>::kColumns, memory);
     const uint32_t tile = blockIdx.x / a.split, i = tile / a.tiles, row0 = (tile - i * a.tiles) * P::kRows;
     const int part = (int)(blockIdx.x - tile * a.split), steps = (a.h + P::kStep - 1) / P::kStep;
     const bool main = threadIdx.x < 256;
     float sums[R];
+    int turns = 0;
     const int group = (int)blockIdx.y;
     const Walk walk = {a.image + (int64_t)i * a.image_ws + group * down_group(a.h, a.rank), i, row0, 0, part, a.split, steps};
-    if (main) sum_tiles<R, MAPPED, false>(a, walk, smem, memory, shared_address(bars), sums);
-    else feed<R, MAPPED, false>(a, &map, walk, smem, memory, shared_address(bars));
-    tensor_end(memory, By<R>::kColumns);
+    if (main) sum_tiles<R, MAPPED, false>(a, walk, smem, memory, shared_address(bars), word + 1, sums);
+    else turns = feed<R, MAPPED, false>(a, &map, walk, smem, memory, shared_address(bars), word + 1);
+    const float worth = tensor_end<P>(memory, By<R>::kColumns, word + 1, shared_address(bars), turns) ? __int_as_float(0x7fffffff) : 1.0f;
     // this CTA's sums, then its share of the rows, joined over the cluster in order
     constexpr int L = R + 1;
     float *mine = reinterpret_cast<float*>(smem), *whole = mine + 256 * L;
     if (main)
 #pragma unroll
-        for (int r = 0; r < R; ++r) mine[threadIdx.x * L + r] = sums[r];
+        for (int r = 0; r < R; ++r) mine[threadIdx.x * L + r] = worth * sums[r];
     cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
     cluster.sync();
     const float scale = a.scale * (a.drop.on ? a.drop.factor : 1.0f);
@@ -549,22 +587,23 @@ __global__ void __launch_bounds__(kThreads, 1) outer_kernel(const __grid_constan
     extern __shared__ __align__(16) char dynamic[];
     using P = Pipe<R, true>;
     __shared__ uint64_t bars[P::kBars];
-    __shared__ uint32_t word;
+    __shared__ uint32_t word[2];
     dependency_wait();
     uint32_t memory;
     char* smem = aligned(dynamic);
-    tensor_begin<P>(bars, &word, By<R>::kColumns, memory);
+    tensor_begin<P>(bars, word, By<R>::kColumns, memory);
     const uint32_t i = blockIdx.y / a.chunks, chunk = blockIdx.y - i * a.chunks, blocks = (a.rows + 63) / 64;
     const int s0 = (int)((uint64_t)blocks * chunk / a.chunks), s1 = (int)((uint64_t)blocks * (chunk + 1) / a.chunks);
     float sums[R];
+    int turns = 0;
     const int group = (int)blockIdx.z;
     const Walk walk = {a.image + (int64_t)i * a.image_ws + group * t_outer_group(a.rows, a.rank), i, 0, (int)blockIdx.x * 256, s0, 1, s1};
-    if (threadIdx.x < 256) sum_tiles<R, MAPPED, true>(a, walk, smem, memory, shared_address(bars), sums);
-    else feed<R, MAPPED, true>(a, &map, walk, smem, memory, shared_address(bars));
-    tensor_end(memory, By<R>::kColumns);
+    if (threadIdx.x < 256) sum_tiles<R, MAPPED, true>(a, walk, smem, memory, shared_address(bars), word + 1, sums);
+    else turns = feed<R, MAPPED, true>(a, &map, walk, smem, memory, shared_address(bars), word + 1);
+    const bool gone = tensor_end<P>(memory, By<R>::kColumns, word + 1, shared_address(bars), turns);
     const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (threadIdx.x >= 256 || c >= a.h) return;
-    const float scale = a.scale * (a.drop.on ? a.drop.factor : 1.0f);
+    const float scale = gone ? __int_as_float(0x7fffffff) : a.scale * (a.drop.on ? a.drop.factor : 1.0f);
     float* out = a.out + (int64_t)blockIdx.y * a.rank * a.h + c * a.sc + group * R * a.sj;
     const int ranks = a.rank - group * R;
     if (a.sj == 1 && (a.rank & 3) == 0 && (reinterpret_cast<uintptr_t>(a.out) & 15u) == 0) {
@@ -611,6 +650,7 @@ struct UpArgs {
     int64_t base_ws, base_rs, image_ws;
     uint32_t rows, chunks;
     int32_t h, rank;
+    uint32_t tries;  // of a wait
     float scale;
     Drop drop;
 };
@@ -625,7 +665,7 @@ __global__ void __launch_bounds__(256, GROUPS ? 1 : 2) up_kernel(const __grid_co
     using P = Pipe<R, true>;
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + U::kShared - 256);
     uint32_t* word = reinterpret_cast<uint32_t*>(bars + P::kBars);
-    bool lost = false;  // a wait gave up
+    bool lost = false;  // a wait of this thread gave up, or one of the CTA's before the last barrier
     dependency_wait();
     uint32_t memory;
     tensor_begin<P>(bars, word, kMemory, memory);
@@ -689,7 +729,7 @@ __global__ void __launch_bounds__(256, GROUPS ? 1 : 2) up_kernel(const __grid_co
     fetch_t(b0, 0, 0);
     fetch_base(b0);
     copies_commit();
-    uint32_t turn = 0, b = b0;
+    uint32_t turn = 0, formed = 0, b = b0;
     for (int group = 0; b < b1; ++turn) {
         const bool last = !GROUPS || group + 1 == groups;
         if constexpr (U::kTs == 2) {
@@ -702,9 +742,10 @@ __global__ void __launch_bounds__(256, GROUPS ? 1 : 2) up_kernel(const __grid_co
         }
         fence_shared();
         fence_before();
-        __syncthreads();
+        lost = __syncthreads_or(lost);
         char* tile = tile_of(b);
-        if (threadIdx.x == 0) {
+        if (!lost) formed = turn;
+        if (threadIdx.x == 0 && !lost) {
             fence_after();
             const uint32_t left = shared_address(t0) + (U::kTs == 2 ? (turn & 1u) * B::kUpBytes : 0);
             const uint32_t right = shared_address(planes) + (GROUPS ? (turn & 1u) * U::kFactorBytes : 0);
@@ -725,7 +766,8 @@ __global__ void __launch_bounds__(256, GROUPS ? 1 : 2) up_kernel(const __grid_co
         if constexpr (U::kTs == 1) fetch_base(b + 1);
         // a lane's row: CN / 2 columns from CN / 2 (warp / 4) on
         const uint32_t r = (uint32_t)(warp & 3) * 32 + lane, row = b * 128 + r;
-        lost = lost || !barrier_wait(bar, turn & 1u);
+        lost = lost || !barrier_wait(bar, turn & 1u, a.tries);
+        const float scale = lost ? __int_as_float(0x7fffffff) : a.scale;  // (a thread that did not give up has its sums)
         fence_after();
         if constexpr (U::kTs == 1) {
             fetch_t(b + 1, 0, turn + 1);
@@ -755,7 +797,7 @@ __global__ void __launch_bounds__(256, GROUPS ? 1 : 2) up_kernel(const __grid_co
                 float x[8] = {};
                 if (a.base) raw_floats<__nv_bfloat16>({*at}, x);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = fmaf(a.scale, v[k * 8 + e], x[e]);
+                for (int e = 0; e < 8; ++e) x[e] = fmaf(scale, v[k * 8 + e], x[e]);
                 if (a.drop.on) drop8(a.drop, drop_words(a.drop, (uint32_t)(c0 >> 3) + c, row, a.drop.worker + i, call), x);
                 *at = make_uint4(pack(x[0], x[1], __nv_bfloat16()), pack(x[2], x[3], __nv_bfloat16()), pack(x[4], x[5], __nv_bfloat16()),
                                  pack(x[6], x[7], __nv_bfloat16()));
@@ -782,7 +824,10 @@ __global__ void __launch_bounds__(256, GROUPS ? 1 : 2) up_kernel(const __grid_co
         group = 0;
     }
     copies_wait<0>();
-    if (lost) gave_up = 1;
+    if (__syncthreads_or(lost)) {  // (or: the products of everyone's last wait are done)
+        barrier_wait(bar, formed & 1u, kTries);  // the last products, which someone did not wait for
+        gave_up = 1;
+    }
     tensor_end(memory, kMemory);
 }
 

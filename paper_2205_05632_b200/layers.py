@@ -28,6 +28,7 @@ stream live while capturing.
 
 Not finite: a row of a norm with an infinity or a NaN in it is NaN, and so are its gradients; a dropped element is 0 whatever it was. In
 an adapter what an infinity or a NaN reaches is infinite or NaN, as a sum over it is, but which of the two may differ from a plain product.
+NaN is also what an adapter's kernel leaves whose bounded waits run out (compams_adapter_status says so; nothing should bring it about).
 """
 from __future__ import annotations
 

@@ -20,3 +20,11 @@ def test_an_adapters_backward_pass_without_a_wanted_gradient(lib, rows, type_):
     if rows:
         assert lib.compams_adapter_backward(*adapter_backward_args(**dict(none, dy=None))) == -1  # arguments are looked at all the same
         assert lib.compams_adapter_backward(*adapter_backward_args(**dict(none, rank=0))) == -1
+
+
+def test_tries_of_a_wait(lib):
+    for bad in (-1, (1 << 14) + 1, 1 << 30):
+        assert lib.compams_adapter_wait_tries(bad) == -1
+    for good in (0, 1, 1 << 14):
+        assert lib.compams_adapter_wait_tries(good) == 0
+    assert lib.compams_adapter_status(None) == -1
