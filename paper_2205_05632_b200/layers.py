@@ -20,7 +20,9 @@ alone (x[None] with worker=i), and a run that is taken up again draws on as befo
 program's uses of the generator, or a one-element int64 CUDA tensor that holds it, which a captured graph reads at every replay; it has
 to keep its value until the backward pass is done (add to it behind that).
 
-The operators run on the current stream of x's device. They are differentiable once; their outputs are packed.
+The operators run on the current stream of x's device. They are differentiable once, backwards; their outputs are packed. Forward-mode
+derivatives, torch.func's transforms and recording by make_fx are refused; torch.jit.trace records the operator as a Python function.
+n is at most 65535.
 
 Forward and backward can be captured into a CUDA graph together. As with every torch backward pass, the leaves' gradient nodes belong to
 the stream on which they were first used: warm up on the capturing stream, and let no autograd graph of the same leaves from another
@@ -37,6 +39,7 @@ import functools
 from typing import Optional, Tuple, Union
 
 import torch
+from torch.autograd import forward_ad
 
 from .binding import CompAMSError, _check, load_library
 
@@ -161,6 +164,8 @@ def _once(backward):
     guarded = torch.autograd.function.once_differentiable(backward)
 
     def run(ctx, *grads):
+        if _has_tangent(grads):
+            raise CompAMSError("forward-mode derivatives of a backward pass are not offered")
         return guarded(ctx, *grads) if torch.is_grad_enabled() else backward(ctx, *grads)
 
     return run
@@ -177,8 +182,24 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
-def _wants_gradient(*tensors) -> bool:
-    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+def _has_tangent(tensors) -> bool:
+    return forward_ad._current_level >= 0 and any(t is not None and forward_ad.unpack_dual(t).tangent is not None for t in tensors)
+
+
+_pre_dispatch_modes = torch._ops.mode_stack_state_for_pre_dispatch().count
+
+
+def _through_autograd(*tensors) -> bool:
+    """Whether a call goes through its autograd function: where a gradient is wanted, but also where torch.jit.trace would otherwise record
+    the allocation of the result and nothing else (it records the function), and where a tensor carries a forward-mode tangent, which
+    would be lost (the function refuses it). make_fx sees neither, so it is refused here."""
+    if torch._C._len_torch_dispatch_stack() or _pre_dispatch_modes():
+        from torch.fx.experimental.proxy_tensor import get_proxy_mode
+        if get_proxy_mode() is not None:
+            raise CompAMSError("make_fx cannot record this operator: it would keep the allocation of the result alone")
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+        return True
+    return torch._C._is_tracing() or _has_tangent(tensors)
 
 
 # ---- dropout ---------------------------------------------------------------------------------------------------------------
@@ -212,7 +233,7 @@ def dropout(x: torch.Tensor, p: float, seed: int = 0, call: Call = 0, worker: in
     is kept. Dropped elements are 0 whatever they were, NaN included; p = 0 copies."""
     _activation(x)
     drop = _Drop(x, p, seed, call, worker)
-    return _DropoutFunction.apply(x, drop) if _wants_gradient(x) else _dropout(x, drop)
+    return _DropoutFunction.apply(x, drop) if _through_autograd(x) else _dropout(x, drop)
 
 
 # ---- layer norm ------------------------------------------------------------------------------------------------------------
@@ -311,7 +332,7 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
     [h] or [n, h]."""
     _activation(x)
     weight, bias, eps = _norm_parameters(x, weight, bias, eps)
-    if _wants_gradient(x, weight, bias):
+    if _through_autograd(x, weight, bias):
         return _LayerNormFunction.apply(x, weight, bias, eps)
     return _norm_forward(x, None, weight, bias, eps, _NOTHING, False)[0]
 
@@ -325,7 +346,7 @@ def dropout_add_layer_norm(x: torch.Tensor, residual: torch.Tensor, weight: Opti
     _like(residual, x, "residual", (x.dtype, torch.float32))
     weight, bias, eps = _norm_parameters(x, weight, bias, eps)
     drop = _Drop(x, p, seed, call, worker)
-    if _wants_gradient(x, residual, weight, bias):
+    if _through_autograd(x, residual, weight, bias):
         return _AddNormFunction.apply(x, residual, weight, bias, eps, drop)
     return _norm_forward(x, residual, weight, bias, eps, drop, False)[:2]
 
@@ -402,6 +423,6 @@ def low_rank_adapter(x: torch.Tensor, base: Optional[torch.Tensor], A: torch.Ten
                              or tuple(base.shape) != (*x.shape[:-1], out)):
         raise CompAMSError("base must be %s of type %s on %s" % ([*x.shape[:-1], out], x.dtype, x.device))
     drop, scale = _Drop(x, p, seed, call, worker), float(scale)
-    if _wants_gradient(x, base, A, B):
+    if _through_autograd(x, base, A, B):
         return _AdapterFunction.apply(x, base, A, B, scale, drop)
     return _adapter_forward(x, base, A, B, scale, drop)[0]
