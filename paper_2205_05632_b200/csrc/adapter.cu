@@ -956,12 +956,13 @@ struct AdapterShape {
 // 16, each its own factors: 9 us for one row, 15 for four; with fragments 23 for five.
 bool few(const AdapterShape& z) { return z.rows <= kFewRows; }
 
-// Whether the products run on tcgen05.mma, whose tiles are of 128 rows: from 64 rows on, from 128 where the rank is padded to 16. Forward and
-// backward of 8 workers' 4096 x 4096, device time with it and without: rank 16 and 64 rows 53 and 43 us, 128 rows 57 and 63, 512 rows
-// 98 and 136; rank 64 and 64 rows 94 and 106, 2048 rows (4096 x 8192) 462 and 1132; rank 128 there
-// 808 and 2504.
+// Whether the products run on tcgen05.mma, whose tiles are of 128 rows. Forward and backward of 8 workers' 4096 x 4096 in bfloat16, device time in
+// us with it and without: rank 16 and 64 rows 55 and 44, 128 rows 59 and 65, 512 rows 101 and 148; rank 32 and 64 rows 66 and 54, 96 rows 69
+// and 77, 512 rows 118 and 199; rank 64 and 64 rows 98 and 116, 512 rows 155 and 361; rank 128 and 64 rows 122 and 141, 512 rows 224 and 643.
+// With few tiles on the whole device mma.sync stays ahead for longer: one worker's 128 rows at rank 16 take 52 and 40.
 bool on_tensor(const AdapterShape& z, int32_t type) {
-    return type == kTypeBF16 && z.rows >= (tensor::padded_rank(z.rank) == 16 ? 128 : 64);
+    const int r = tensor::padded_rank(z.rank);
+    return type == kTypeBF16 && z.rows >= (r == 16 ? 128 : r == 32 ? 96 : 64);
 }
 
 // The number of parts, of 1 ... most, at which the slowest of `slots` places ends first: waves of tiles * parts CTAs, each a part's

@@ -141,3 +141,11 @@ def test_two_streams_at_once():
     torch.cuda.synchronize()
     for k, outs in got:
         assert all(torch.equal(p, q) for p, q in zip(outs, alone[k]))
+
+
+@pytest.mark.parametrize("rows", [95, 96, 100, 127, 129])
+@pytest.mark.parametrize("h,out", [(8, 8), (56, 64), (64, 120), (72, 128), (120, 136), (128, 256), (136, 264), (1000, 65), (257, 1), (1, 129)])
+def test_columns_around_the_tiles_at_ranks_of_17_to_32(h, out, rows):
+    g = gen(9)
+    x, base, dy = rand(g, 2, rows, h, dtype=BF16), rand(g, 2, rows, out, dtype=BF16), rand(g, 2, rows, out, dtype=BF16)
+    adapter(x, base, rand(g, 2, 30, h, sigma=h ** -0.5), rand(g, 2, out, 30, sigma=0.2), dy, p=0.25, seed=2)
