@@ -281,7 +281,7 @@ __device__ __forceinline__ Raw8<T> ring_raw(char* smem, int stage, int slot) {  
 // pass through shared memory. The sums of the warps and of the CTAs are
 // joined in their order, through the CTAs' shared memory, and leave as t and as the operands that up and outer take. Bound by the
 // instructions that make operands of the activation, not by memory: 8 workers of 2048 rows of 4096 in fp16, rank 16, 134 MB, 58 us
-// (2.3 TB/s), 78 with dropout; of 1024 rows in fp32, 134 MB too, 58 and 66. 8 workers of 48 rows in bfloat16 7 us.
+// (2.3 TB/s), 72 with dropout; of 1024 rows in fp32, 134 MB too, 58 and 63. 8 workers of 48 rows in bfloat16 7 us.
 template <typename T>
 __host__ __device__ constexpr int down_step() { return sizeof(T) == 4 ? 1 : 2; }  // blocks of 32 columns in a step
 template <typename T, bool VEC, int NT, int WK, int MT>
@@ -724,7 +724,7 @@ __global__ void __launch_bounds__(256) adapter_up_few_kernel(const __grid_consta
 // A CTA per 256 columns, 8 NT rank indices and chunk of a worker's rows: four warps side by side, two that share out the blocks of 16 rows
 // and join their sums. A lane takes eight neighbours of four rows; pairs of rows become the operand's pairs by byte permutes. The side by
 // side warps share t, which passes through shared memory. Bound by instructions, as down: 8 workers of 2048 rows of 4096 in fp16, rank 16,
-// 134 MB, 77 us, 101 with dropout; of 1024 rows in fp32 78 and 92.
+// 134 MB, 77 us, 98 with dropout; of 1024 rows in fp32 70 and 84.
 constexpr int kOuterColumns = 256;
 template <typename T, bool VEC, int NT>
 __host__ __device__ constexpr int outer_ring() { return VEC ? kStages * 4 * (int)sizeof(Raw8<T>) * 256 : 0; }
@@ -938,6 +938,7 @@ __global__ void __launch_bounds__(256) adapter_join_kernel(const float* __restri
 // ---- host ------------------------------------------------------------------------------------------------------------------
 
 constexpr int kMostRank = 1024;
+constexpr int kSms = 148;  // SMs of a B200, for which launches are laid out
 
 struct AdapterShape {
     int32_t n;
@@ -982,13 +983,14 @@ int64_t parts_of(int64_t tiles, int64_t slots, int64_t work, double fixed, int64
 // Chunks of a worker's rows: as many as give each SM about two CTAs, of 64 rows at least.
 uint32_t outer_chunks(const AdapterShape& z, int64_t h, int32_t type) {
     if (few(z)) return 1;
-    // (partial sums of 64 ranks and 256 columns, 64 KB written and read: 26 ns at 5 TB/s; a step takes 0.5 us. 16384 rows of 8192 at rank
-    // 128: 117 us with one chunk, 127 and 43 for the join with two; one worker's 512 rows of 1024 at rank 64: 11, 7.4 and 2.3 with eight)
+    // (partial sums of 64 ranks and 256 columns, 64 KB written and read: 26 ns at 5 TB/s, here 0.05 steps; a step takes 0.7 us at rank 16 and
+    // 0.9 at rank 64, so chunks are few rather than many. 16384 rows of 8192 at rank 128: 117 us with one chunk, 127 and 43 for the join with
+    // two; one worker's 512 rows of 1024 at rank 64: 11, 7.4 and 2.3 with eight)
     if (on_tensor(z, type))
-        return (uint32_t)parts_of((h + 255) / 256 * z.n * tensor::groups_of(z.rank), 148, (z.rows + 63) / 64, 4.0,
+        return (uint32_t)parts_of((h + 255) / 256 * z.n * tensor::groups_of(z.rank), kSms, (z.rows + 63) / 64, 4.0,
                                   std::min<int64_t>(65535 / z.n, 8), false, 0.05 * std::min(z.rank, 64) / 64);
     const int64_t tiles = (h + kOuterColumns - 1) / kOuterColumns * rank_groups(z.rank) * z.n;
-    int64_t c = (148 * 2 + tiles - 1) / tiles;
+    int64_t c = (kSms * 2 + tiles - 1) / tiles;
     const int64_t most = (z.rows + 63) / 64;
     if (c > most) c = most;
     if (c > 65535 / z.n) c = 65535 / z.n;
@@ -1133,7 +1135,7 @@ int tensor_down(Low low, Rows x, const AdapterShape& z, int64_t h, bool shared, 
         using P = tensor::Pipe<R, false>;
         a.tiles = (a.rows + P::kRows - 1) / P::kRows;
         const uint32_t groups = (uint32_t)tensor::groups_of(z.rank);
-        a.split = (int32_t)parts_of((int64_t)a.tiles * z.n * groups, 148, (h + P::kStep - 1) / P::kStep, 4.0, 4, true);
+        a.split = (int32_t)parts_of((int64_t)a.tiles * z.n * groups, kSms, (h + P::kStep - 1) / P::kStep, 4.0, tensor::kMostSplit, true);
         const uint64_t ctas = (uint64_t)a.tiles * z.n * a.split;
         if (ctas > 0x7fffffffu) return (int)COMPAMS_ERR_TOO_LARGE;
         CUtensorMap map;
@@ -1156,7 +1158,7 @@ int tensor_up(void* y, Rows base, Low low, const AdapterShape& z, int64_t h, boo
             constexpr bool GROUPS = decltype(g)::value;
             using U = tensor::Up<R, GROUPS>;
             const int64_t columns = (h + U::kColumns - 1) / U::kColumns, blocks = (z.rows + 127) / 128;
-            a.chunks = (uint32_t)parts_of(columns * z.n, GROUPS ? 148 : 2 * 148, blocks, 0.5, 65535 / z.n, false);
+            a.chunks = (uint32_t)parts_of(columns * z.n, GROUPS ? kSms : 2 * kSms, blocks, 0.5, 65535 / z.n, false);
             auto kernel = vec ? tensor::up_kernel<R, true, GROUPS> : tensor::up_kernel<R, false, GROUPS>;
             return launched(launch_next(kernel, dim3((uint32_t)columns, (uint32_t)z.n * a.chunks), 1, U::kShared, false, stream, a), "adapter_up");
         };
@@ -1214,7 +1216,7 @@ int down(Low low, Rows x, const AdapterShape& z, int64_t h, bool shared, Factor 
             const uint64_t tiles = (uint64_t)a.tiles * z.n * groups;
             const int64_t steps = (h + 32 * down_step<T>() - 1) / (32 * down_step<T>()) / wk;
             a.split = 1;
-            while (a.split < 8 && tiles * a.split < 2 * 148 / mt && steps >= 8 * a.split) a.split *= 2;
+            while (a.split < 8 && tiles * a.split < 2 * kSms / mt && steps >= 8 * a.split) a.split *= 2;
             const uint64_t ctas = (uint64_t)a.tiles * z.n * a.split;
             if (ctas > 0x7fffffffu) return (int)COMPAMS_ERR_TOO_LARGE;
             return launched(launch_next(kernel, dim3((uint32_t)ctas, groups), a.split, shared_bytes, false, stream, a),
@@ -1229,8 +1231,8 @@ int down(Low low, Rows x, const AdapterShape& z, int64_t h, bool shared, Factor 
             const int nt = group_tiles(z.rank);
             // Warps that share the rows' columns keep more loads on their way; warps of different rows share the fragments, which pays
             // for several groups of ranks in 16 bits and many rows. Both passes' kernels of 8 workers, 4096 columns, eight warps to the
-            // rows / one: fp16, rank 128, 1024 rows 378 / 341 us, 512 rows 196 / 269; fp16, rank 16, 2048 rows 137
-            // / 152, 512 rows 50 / 45; fp32, rank 64, 1024 rows 228 / 402.
+            // rows / one: fp16, rank 128, 1024 rows 371 / 321 us, 512 rows 190 / 254 (of 1024 columns 117 / 114 and 63 / 59, of 8192 836 /
+            // 596 and 420 / 459; rank 80 as 128); fp16, rank 16, 2048 rows 137 / 152, 512 rows 50 / 45; fp32, rank 64, 1024 rows 228 / 402.
             if constexpr (sizeof(T) == 2)
                 if (z.rank > 64 && z.total() >= 8192) return pick(v, Int<1>(), Int<8>(), Int<2>());
             if (nt == 1) return pick(v, Int<8>(), Int<1>(), Int<1>());
@@ -1257,7 +1259,7 @@ int up(void* y, Rows base, Low low, const AdapterShape& z, int64_t h, bool share
         }
         // row chunks: as many as give each SM about four CTAs
         const uint32_t blocks = (a.rows + 15) / 16, n = (uint32_t)z.n;
-        uint64_t c = 148 * 4 / ((uint64_t)columns * n) + 1;
+        uint64_t c = kSms * 4 / ((uint64_t)columns * n) + 1;
         if (c > blocks) c = blocks;
         if (c > 65535 / n) c = 65535 / n;
         a.tiles = (uint32_t)c;

@@ -1,6 +1,6 @@
 // The adapters' three products on tcgen05.mma, for bfloat16 activations. mma.sync is bound by its own rate (550 TFLOP/s measured, a third
-// of tcgen05's) from about rank 32 on, and below by the instructions that bring operands to registers. (fp16 would need planes in fp16,
-// whose range the factors' values leave, and fp32 three tiles of planes for each tile of the activation: both stay on mma.sync.)
+// of tcgen05's) from about rank 32 on, and below by the instructions that bring operands to registers. (fp16 would need two tiles of bf16
+// planes for each tile of the activation, which the eight warps would have to write, and fp32 three: both stay on mma.sync.)
 //
 // The planes of an fp32 operand are stacked along N: a tile of an activation, 128 x 64, is multiplied by [3 x R] rows of planes at
 // once (R: the rank, padded to 16, 32 or 64; higher ranks go in groups of 64), so it is an operand once for a group and the planes' sums
@@ -9,7 +9,7 @@
 // is read across them (MN-major), and t comes turned, [plane, rank][row].
 //
 // One thread of a ninth warp issues the products and one of a tenth brings the tiles (TMA, into the swizzle; the planes, already in its
-// order, in bulk): a stage costs the one 0.35 us and the other 0.2 us, whatever the rank. One thread for both, waits included, held
+// order, in bulk): a stage costs the one 0.35 us of issue and the other 0.2 us, whatever the rank; one thread for both, waits included, held
 // every stage to 0.8 to 1.1 us. They wait for nobody else unless dropout masks the activation, which the 256 threads of the other warps
 // do in place. The tensor cores cut their sums, so after every kFlush tiles of 64 the sums go to fp32 registers by rounded additions,
 // which is the other warps' work. Activations that TMA cannot address (odd widths, other strides) are brought by these warps, element by
@@ -262,7 +262,7 @@ struct Args {
     int64_t sj, sc;        // outer: of an element of out
     uint32_t rows;
     int32_t h, rank;
-    uint32_t tiles;        // down: of 256 rows, a worker's
+    uint32_t tiles;        // down: of 256 rows (WIDE: 128), a worker's
     int32_t split;         // down: CTAs of a cluster, which share out the columns
     uint32_t chunks;       // outer: of a worker's rows
     uint32_t tries;        // of a wait
@@ -271,6 +271,7 @@ struct Args {
 };
 
 constexpr int kThreads = 320;
+constexpr int kMostSplit = 4;  // CTAs of a cluster of down (with 8 no size was faster)
 
 // Tensor memory and the barriers. The shared words, one that takes the address and one for who gives up, are the caller's.
 template <typename P>
@@ -499,8 +500,8 @@ __device__ __forceinline__ void sum_tiles(const Args& a, const Walk& k, char* sm
 }
 
 // A CTA takes 256 rows of a worker, or 128 (WIDE), and its share of the columns. Rank 64, 8 workers of 2048 rows: 8192 columns, 268 MB,
-// 68 us (3.9 TB/s), bound by the products of a CTA's 64 columns and their waits, 0.5 us a step; 4096 columns with dropout, 134 MB, 70 us,
-// bound by the generator. Rank 16, 4096 columns: 34 and 53 us.
+// 69 us (3.9 TB/s): 128 CTAs of 64 steps, 1.1 us a step, of which the products take 0.4; 56 KB come to a stage, 24 of them planes from the
+// L2. 4096 columns with dropout, 134 MB, 69 us, bound by the generator. Rank 16, 4096 columns: 36 and 52 us.
 template <int R, bool MAPPED>
 __global__ void __launch_bounds__(kThreads, 1) down_kernel(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap map) {
     extern __shared__ __align__(16) char dynamic[];
@@ -530,17 +531,17 @@ __global__ void __launch_bounds__(kThreads, 1) down_kernel(const __grid_constant
     cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
     cluster.sync();
     const float scale = a.scale * (a.drop.on ? a.drop.factor : 1.0f);
-    const int share = P::kRows / a.split, from = part * share;  // split is a power of two up to 8: a share is 16 rows at least
+    const int share = P::kRows / a.split, from = part * share;  // split is a power of two: a share is 32 rows at least
     for (int e = threadIdx.x; e < share * R; e += kThreads) {
         const int r = e / R, j = e % R;
-        float sum[8], v = 0.0f;
+        float sum[kMostSplit], v = 0.0f;
 #pragma unroll
-        for (int s = 0; s < 8; ++s) {
+        for (int s = 0; s < kMostSplit; ++s) {
             const float* at = s < a.split ? cluster.map_shared_rank(mine, s) + (from + r) * L + j : nullptr;
             sum[s] = at ? (P::kWide ? at[0] + at[128 * L] : at[0]) : 0.0f;
         }
 #pragma unroll
-        for (int s = 0; s < 8; ++s) v += sum[s];
+        for (int s = 0; s < kMostSplit; ++s) v += sum[s];
         whole[r * L + j] = scale * v;
     }
     __syncthreads();
@@ -580,8 +581,8 @@ __global__ void __launch_bounds__(kThreads, 1) down_kernel(const __grid_constant
     cluster.sync();  // the others may still be reading
 }
 
-// A CTA takes 256 columns and a chunk of a worker's rows. Rank 64, 8 workers of 2048 rows: 8192 columns, 268 MB, 57 us (4.7 TB/s); 4096
-// with dropout, 134 MB, 57 us. Rank 16, 4096 columns: 22 us (6.2 TB/s), 49 with dropout.
+// A CTA takes 256 columns and a chunk of a worker's rows. Rank 64, 8 workers of 2048 rows: 8192 columns, 268 MB, 57 us (4.7 TB/s), 256 CTAs
+// of 32 steps in two waves, 0.9 us a step; 4096 with dropout, 134 MB, 57 us. Rank 16, 4096 columns: 22 us (6.2 TB/s), 49 with dropout.
 template <int R, bool MAPPED>
 __global__ void __launch_bounds__(kThreads, 1) outer_kernel(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap map) {
     extern __shared__ __align__(16) char dynamic[];

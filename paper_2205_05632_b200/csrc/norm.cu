@@ -76,7 +76,8 @@ __host__ __device__ constexpr int norm_threads() { return W == 1 ? 32 * kRowsOfO
 // CTAs that the registers of an SM have to hold, so that their barriers fall at different times: 24 warps' (16 where the backward
 // pass with its third input would not fit 80 registers a thread, and where rows are read element by element). One CTA of 16 warps; two in
 // the forward pass, where 64 registers a thread nearly do, but for aligned rows with a residual: 16384 bfloat16 rows of 4097 219 us
-// with one and 146 with two, of 8192 120 and 97, with the residual 207 and 222; backward, with spills, 155 and 221.
+// with one and 147 with two, with the residual, some of whose values spill then, 367 and 263; aligned rows of 8192 120 and 97, with the
+// residual 207 and 222; backward, with spills, 155 and 221.
 template <int W, int NG, bool VEC, bool MORE, bool ADD>
 __host__ __device__ constexpr int norm_ctas() {
     return W == 16 ? (!MORE && NG <= 2 && !(ADD && VEC) ? 2 : 1) : (VEC && !(MORE && NG > 1) ? 24 : 16) / (W == 1 ? kRowsOfOneWarp : W);
