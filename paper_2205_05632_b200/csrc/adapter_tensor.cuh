@@ -159,7 +159,7 @@ __device__ __forceinline__ void columns(uint32_t at, float (&v)[N]) {
 }
 
 // Waits that give up, which no size or input should bring about. Whoever gave up marks the CTA's shared word and this one, which stays until
-// it is asked for; nobody of the CTA waits in vain again. Before the tensor memory is given back the copies and products under way are
+// it is asked for; no thread waits in vain twice. Before the tensor memory is given back the copies and products under way are
 // waited for, with a limit of their own, and the CTA's results are NaN, so that what is computed from them shows it.
 __device__ int32_t gave_up;
 __device__ __forceinline__ void give_up(uint32_t* lost) {
