@@ -513,6 +513,48 @@ int compams_adapter_wait_tries(int32_t tries);
 int compams_adapter_workspace_bytes(size_t* bytes, int32_t n, int64_t rows, int64_t in, int64_t out, int32_t rank, int32_t shared,
                                     int32_t backward, int32_t sum_workers);
 
+/*
+ * The head of a language model: logits z = x W^T over a vocabulary and the softmax cross entropy with a target for each row,
+ * loss_j = log sum_v exp(z_jv) - z_j,target(j), without the logits in memory as a whole.
+ *   type            of x and dx; weight_type: of weight and dweight, the same or COMPAMS_F32.
+ *   weight          device, [vocab, h] with packed columns: worker i's row v at i * weight_worker_stride + v * weight_row_stride
+ *                   (weight_worker_stride 0: one for all).
+ *   target          device int64, packed [n, rows]: a column of the vocabulary, or `ignored`: the row's loss is 0 and it has no gradient. A
+ *                   row with any other number has a loss of NaN.
+ *   reduction       of the loss: 0 none, packed [n, rows]; 1 mean over each worker's rows that are not ignored (of none: 0), [n]; 2 sum, [n].
+ *   lse             device, packed fp32 [n, rows]: receives log sum_v exp(z_jv), which the backward pass takes.
+ *   workspace       device, 256-byte aligned, at least compams_head_workspace_bytes; used during the call's device work only.
+ * 1 <= vocab < 2^31 - 4096. A row whose logits hold a NaN or an infinity above zero has a loss of NaN.
+ */
+int compams_head_forward(float* loss, float* lse, const void* x, int32_t type, const void* weight, int32_t weight_type, const int64_t* target,
+                         int32_t n, int64_t rows, int64_t h, int64_t vocab, int64_t x_worker_stride, int64_t x_row_stride,
+                         int64_t weight_worker_stride, int64_t weight_row_stride, int64_t ignored, int32_t reduction, void* workspace,
+                         size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Its gradients.
+ *   dloss           device fp32, the loss's gradient: of worker i at i * dloss_worker_stride, without a reduction of its row j
+ *                   dloss_row_stride * j further (strides not negative, 0 repeats).
+ *   dx              packed [n, rows, h]; may be null: not wanted.
+ *   dweight         packed [n, vocab, h], worker i's rows alone; sum_workers: [vocab, h], over all workers, for a weight that all share;
+ *                   may be null: not wanted.
+ *   wanted          of the workspace: 0 the forward pass, else 1 (dx) + 2 (dweight).
+ *   x_copied, weight_copied   0 where TMA can read them as they lie: type is weight_type and has 16 bits, the address and the strides are
+ *                   multiples of 16 bytes (of axes longer than 1), rows do not overlap, and, for x beside a weight that all share, the
+ *                   workers' rows follow one another at one distance. Else 1, or 1 in any case: the workspace then has room for a copy.
+ *   shared          weight_worker_stride is 0, or n is 1.
+ */
+int compams_head_backward(void* dx, void* dweight, int32_t sum_workers, const float* dloss, int64_t dloss_worker_stride, int64_t dloss_row_stride,
+                          const void* x, int32_t type, const void* weight, int32_t weight_type, const int64_t* target, const float* lse, int32_t n,
+                          int64_t rows, int64_t h, int64_t vocab, int64_t x_worker_stride, int64_t x_row_stride, int64_t weight_worker_stride,
+                          int64_t weight_row_stride, int64_t ignored, int32_t reduction, void* workspace, size_t workspace_bytes,
+                          void* cuda_stream);
+int compams_head_workspace_bytes(size_t* bytes, int32_t n, int64_t rows, int64_t h, int64_t vocab, int32_t type, int32_t weight_type,
+                                 int32_t shared, int32_t x_copied, int32_t weight_copied, int32_t wanted);
+/* As compams_adapter_status and compams_adapter_wait_tries, for the head's kernels. */
+int compams_head_status(int32_t* gave_up);
+int compams_head_wait_tries(int32_t tries);
+
 /* Static strings (never null). */
 const char* compams_error_string(int status);
 const char* compams_kernel_name(int32_t kernel);

@@ -142,6 +142,16 @@ def load_library() -> ctypes.CDLL:
     L.compams_adapter_workspace_bytes.restype = c.c_int
     L.compams_adapter_workspace_bytes.argtypes = [c.POINTER(c.c_size_t), I32, I64, I64, I64, I32, I32, I32, I32]
     L.compams_error_string.restype = c.c_char_p
+    L.compams_head_forward.argtypes = [P, P, P, I32, P, I32, P, I32] + [I64] * 8 + [I32, P, c.c_size_t, P]
+    L.compams_head_forward.restype = c.c_int
+    L.compams_head_backward.argtypes = [P, P, I32, P, I64, I64, P, I32, P, I32, P, P, I32] + [I64] * 8 + [I32, P, c.c_size_t, P]
+    L.compams_head_backward.restype = c.c_int
+    L.compams_head_workspace_bytes.argtypes = [c.POINTER(c.c_size_t), I32, I64, I64, I64] + [I32] * 6
+    L.compams_head_workspace_bytes.restype = c.c_int
+    L.compams_head_status.argtypes = [c.POINTER(I32)]
+    L.compams_head_status.restype = c.c_int
+    L.compams_head_wait_tries.argtypes = [I32]
+    L.compams_head_wait_tries.restype = c.c_int
     L.compams_error_string.argtypes = [c.c_int]
     L.compams_kernel_name.restype = c.c_char_p
     L.compams_kernel_name.argtypes = [c.c_int32]

@@ -31,6 +31,7 @@
 
 #include "context.h"
 #include "rows.cuh"
+#include "tcgen05.cuh"
 
 namespace compams {
 namespace {
@@ -79,26 +80,6 @@ __device__ __forceinline__ void mma_first(float (&c)[4], uint32_t a0, uint32_t a
         : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
 }
-
-// The first P planes of two numbers, packed. All but the last are held to finite numbers, so that the largest numbers are not rounded to an
-// infinity, whose rest would be the other; an infinity arrives in the last plane.
-template <int P>
-__device__ __forceinline__ void split2(float a, float b, uint32_t (&planes)[P]) {
-#pragma unroll
-    for (int p = 0; p < P; ++p) {
-        if (p + 1 < P) {
-            asm("cvt.rn.satfinite.bf16x2.f32 %0, %1, %2;" : "=r"(planes[p]) : "f"(b), "f"(a));
-            a -= __uint_as_float(planes[p] << 16);
-            b -= __uint_as_float(planes[p] & 0xffff0000u);
-        } else {
-            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(planes[p]) : "f"(b), "f"(a));
-        }
-    }
-}
-
-template <typename T> struct Planes { static constexpr int count = 3; };
-template <> struct Planes<__nv_bfloat16> { static constexpr int count = 1; };
-template <> struct Planes<__half> { static constexpr int count = 2; };
 
 // A lane's eight neighbours of a row from column c on, 0 beyond h.
 template <typename T, bool VEC>
@@ -1007,52 +988,6 @@ template <typename F>
 int by_type(int32_t type, F f) {
     return type == kTypeF32 ? f(float()) : type == kTypeBF16 ? f(__nv_bfloat16()) : f(__half());
 }
-int launched(cudaError_t e, const char* what) { return e == cudaSuccess ? COMPAMS_OK : cuda_fail(e, what); }
-
-// Lets a kernel have more than 48 KB of shared memory: asked once for every kernel and device (a kernel's size is always the same).
-cudaError_t allow_shared(const void* kernel, size_t bytes) {
-    static std::atomic<uint64_t> known[1024];
-    int device = 0;
-    cudaError_t e = cudaGetDevice(&device);
-    if (e != cudaSuccess) return e;
-    const uint64_t key = (uint64_t)(uintptr_t)kernel ^ (uint64_t)(device + 1) << 56;
-    std::atomic<uint64_t>& slot = known[(key * 0x9E3779B97F4A7C15ull) >> 54];
-    if (slot.load(std::memory_order_relaxed) == key) return cudaSuccess;
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-    if (e == cudaSuccess) slot.store(key, std::memory_order_relaxed);
-    return e;
-}
-
-// A launch behind another of the same call (or the first), with dynamic shared memory and a cluster along x.
-template <typename... KArgs, typename... Args>
-cudaError_t launch_sized(void (*kernel)(KArgs...), dim3 grid, int threads, int cluster, size_t shared, bool first, cudaStream_t stream,
-                         Args... args) {
-    if (shared > 48 * 1024) {
-        const cudaError_t e = allow_shared((const void*)kernel, shared);
-        if (e != cudaSuccess) return e;
-    }
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3(threads);
-    cfg.dynamicSmemBytes = shared;
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[2];
-    int count = 0;
-    if (!first) {
-        attr[count].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attr[count++].val.programmaticStreamSerializationAllowed = 1;
-    }
-    if (cluster > 1) {
-        attr[count].id = cudaLaunchAttributeClusterDimension;
-        attr[count].val.clusterDim.x = (unsigned)cluster;
-        attr[count].val.clusterDim.y = 1;
-        attr[count++].val.clusterDim.z = 1;
-    }
-    cfg.attrs = attr;
-    cfg.numAttrs = count;
-    return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
-}
-
 template <typename... KArgs, typename... Args>
 cudaError_t launch_next(void (*kernel)(KArgs...), dim3 grid, int cluster, size_t shared, bool first, cudaStream_t stream, Args... args) {
     return launch_sized(kernel, grid, 256, cluster, shared, first, stream, args...);
@@ -1085,15 +1020,7 @@ bool box_map(CUtensorMap* map, Rows x, const AdapterShape& z, int64_t h, uint32_
     if (h % 8 != 0 || !x.aligned() || x.row_stride < h || (z.n > 1 && x.worker_stride < 1) || x.row_stride >= (int64_t)1 << 38 ||
         x.worker_stride >= (int64_t)1 << 38)
         return false;
-    // the encoder is the driver's; it is asked for once
-    using Encode = decltype(&cuTensorMapEncodeTiled);
-    static const Encode encode = [] {
-        void* f = nullptr;
-        cudaDriverEntryPointQueryResult found;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess)
-            f = nullptr;
-        return (Encode)f;
-    }();
+    const Encode encode = map_encoder();
     if (!encode) return false;
     const cuuint64_t size[3] = {(cuuint64_t)h, (cuuint64_t)z.rows, (cuuint64_t)z.n};
     const cuuint64_t stride[2] = {(cuuint64_t)x.row_stride * 2, (cuuint64_t)(z.n > 1 ? x.worker_stride : x.row_stride * z.rows) * 2};

@@ -16,9 +16,8 @@
 // element.
 #pragma once
 
-#include <cuda.h>  // CUtensorMap
-
 #include "rows.cuh"
+#include "tcgen05.cuh"
 
 namespace compams {
 namespace {
@@ -77,86 +76,6 @@ __host__ __device__ inline int64_t t_outer_group(int64_t rows, int rank) { retur
 __host__ __device__ inline int64_t t_outer_image(int64_t rows, int rank) { return groups_of(rank) * t_outer_group(rows, rank); }
 __host__ __device__ inline int64_t t_up_group(int64_t rows, int rank) { return up_group(rows, rank); }
 __host__ __device__ inline int64_t t_up_image(int64_t rows, int rank) { return up_image(rows, rank); }
-
-__device__ __forceinline__ uint32_t swizzled(uint32_t row, uint32_t chunk) { return row * 128u + ((chunk ^ (row & 7u)) << 4); }
-
-// ---- instructions ----------------------------------------------------------------------------------------------------------
-
-__device__ __forceinline__ uint32_t shared_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-
-__device__ __forceinline__ void barrier_init(uint32_t bar, uint32_t count) {
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
-}
-__device__ __forceinline__ void barrier_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
-// Waits for the phase of this parity to end; gives up after a number of tries, each of which the hardware may hold for a while (0:
-// at once, whatever is there).
-constexpr uint32_t kTries = 1u << 14;
-__device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity, uint32_t most) {
-    uint32_t there = 0, tries = 0;
-    do {
-        asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
-                     : "=r"(there)
-                     : "r"(bar), "r"(parity)
-                     : "memory");
-    } while (!there && ++tries < most);
-    return there && most;
-}
-__device__ __forceinline__ void memory_alloc(uint32_t to, uint32_t columns) {  // a whole warp
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(to), "r"(columns) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-}
-__device__ __forceinline__ void memory_free(uint32_t at, uint32_t columns) {
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(columns) : "memory");
-}
-__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void fence_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-
-// Of an operand in the 128-byte swizzle that starts at a shared address. `along`: bytes to the next 64 elements along M or N of an
-// MN-major operand; 8 rows of 128 bytes lie behind one another.
-__device__ __forceinline__ uint64_t operand(uint32_t at, uint32_t along) {
-    return (uint64_t)((at >> 4) & 0x3fffu) | (uint64_t)(along >> 4) << 16 | (uint64_t)(1024u >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
-}
-// bf16 x bf16 -> fp32; M = 128; which operands are MN-major.
-__host__ __device__ constexpr uint32_t instruction(int n, bool a_across, bool b_across) {
-    return 1u << 4 | 1u << 7 | 1u << 10 | (a_across ? 1u : 0u) << 15 | (b_across ? 1u : 0u) << 16 | (uint32_t)(n >> 3) << 17 | (128u >> 4) << 24;
-}
-__device__ __forceinline__ void product(uint32_t d, uint64_t a, uint64_t b, uint32_t what, bool onto) {
-    asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b),
-                 "r"(what), "r"((uint32_t)onto)
-                 : "memory");
-}
-__device__ __forceinline__ void products_done(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-}
-// A box of a 3-d map, which is in parameter space, to shared memory.
-__device__ __forceinline__ void box_load(uint32_t to, const CUtensorMap* map, int column, int row, int worker, uint32_t bar) {
-    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(to),
-                 "l"(map), "r"(column), "r"(row), "r"(worker), "r"(bar)
-                 : "memory");
-}
-// Behind it the values are there.
-template <int N>
-__device__ __forceinline__ void columns_wait(float (&v)[N]) {
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-    for (int k = 0; k < N; ++k) asm volatile("" : "+f"(v[k]));
-}
-
-// N columns of a lane's row, 16 at a time.
-template <int N>
-__device__ __forceinline__ void columns(uint32_t at, float (&v)[N]) {
-#pragma unroll
-    for (int k = 0; k < N; k += 16) {
-        uint32_t r[16];
-        asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-                     : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-                       "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-                     : "r"(at + k));
-#pragma unroll
-        for (int e = 0; e < 16; ++e) v[k + e] = __uint_as_float(r[e]);
-    }
-}
 
 // Waits that give up, which no size or input should bring about. Whoever gave up marks the CTA's shared word and this one, which stays until
 // it is asked for; no thread waits in vain twice. Before the tensor memory is given back the copies and products under way are

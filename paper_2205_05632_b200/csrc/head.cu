@@ -1,0 +1,809 @@
+// The head of a language model with the n workers' micro-batches in one batch: logits z = x W^T over a vocabulary, softmax cross entropy
+// with a target for each row, and the gradients of x and W, without the logits ever being in memory as a whole.
+//
+//   lse_j = log sum_v exp(z_jv)           loss_j = lse_j - z_j,target(j)     (0 where the target is ignored)
+//   d_jv  = (exp(z_jv - lse_j) - [v = target(j)]) g_j          g_j: the loss's gradient, for a mean divided by the worker's counted rows
+//   dx_j  = sum_v d_jv W_v                dW_v = sum_j d_jv x_j
+//
+// Forward: the products (head_tensor.cuh) leave a row's maximum and sum of exponentials for every 128 columns, 8 bytes in the place of
+// 512, which `join` brings together. Backward: the vocabulary goes by in pieces; a piece's logits are formed again and leave as d in 16
+// bits, as far as it fits a workspace that does not grow with the vocabulary, and the two products that read d follow. So a training
+// step does four products of 2 m h V operations where three would do for someone who keeps the logits: with m = 8192 rows, V = 100000 and
+// fp32 they would be 3.3 GB.
+//
+// A few rows (kFew) read W once, a warp taking rows of W whole, in fp32 arithmetic: bound by memory.
+//
+// Precision. Products of 16-bit numbers of one type are exact and their sums fp32. Beside an fp32 weight everything is bf16 planes: an fp32
+// number is three (each the rest of those before it, rounded), fp16 two; pairs of planes i + j <= 2 are formed, which leaves out at most
+// 2^-24 of a product. d is one plane (2^-9 of it at most left out) where the result has 8 bits, two for fp16 beside an fp32 weight, three
+// for an fp32 result; fp16 products take it in fp16, relative to the largest |g| rounded up to a power of two, as g may be a loss scale
+// or a ten-thousandth. For dx of 8 bits beside an fp32 weight two planes of W are taken. No atomics: results do not change from run to run.
+#include <string.h>
+
+#include <algorithm>
+#include <atomic>
+#include <type_traits>
+
+#include "context.h"
+#include "head_tensor.cuh"
+
+namespace compams {
+namespace {
+
+using head::power2;
+using head::kLog2e;
+
+constexpr float kInf = __builtin_inff();
+constexpr int kVocab = 128;  // columns of a statistic of head_tensor.cuh
+
+// (m, s) stands for s exp(m).
+__device__ __forceinline__ float2 merged(float2 a, float2 b) {
+    const float m = fmaxf(a.x, b.x), base = m == -kInf ? 0.0f : m;
+    return make_float2(m, fmaf(a.y, power2((a.x - base) * kLog2e), b.y * power2((b.x - base) * kLog2e)));
+}
+
+// ---- operands as 16-bit planes ---------------------------------------------------------------------------------------------
+
+struct PackArgs {
+    const void* src;
+    int64_t ws, rs;       // of src
+    int64_t rows, row0;   // rows of a batch that are taken, from row0 on
+    int64_t chunks;       // of all batches: eight columns each
+    int32_t h, per_row;   // columns; chunks of a row, the last padded with zeros
+    uint16_t* out;        // [plane][batch][rows][8 per_row]
+    int64_t plane;        // elements
+};
+template <typename T, int P, bool VEC>
+__global__ void __launch_bounds__(256) pack_kernel(const __grid_constant__ PackArgs a) {
+    dependency_wait();
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (at >= a.chunks) return;
+    const int64_t row = at / a.per_row, batch = row / a.rows;
+    const int c = (int)(at - row * a.per_row) * 8;
+    const T* x = (const T*)a.src + batch * a.ws + (a.row0 + row - batch * a.rows) * a.rs + c;
+    Raw8<T> raw;
+    float v[8];
+    if (VEC) {
+        raw = raw_load<T>(x);
+        raw_floats<T>(raw, v);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = c + k < a.h ? to_float(x[k]) : 0.0f;
+    }
+    uint4 out[P];
+    if constexpr (P == 1) {  // a copy: the type's own bits
+        out[0] = make_uint4(pack(v[0], v[1], T()), pack(v[2], v[3], T()), pack(v[4], v[5], T()), pack(v[6], v[7], T()));
+    } else {
+        uint32_t w[4][P];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) split2<P>(v[2 * q], v[2 * q + 1], w[q]);
+#pragma unroll
+        for (int p = 0; p < P; ++p) out[p] = make_uint4(w[0][p], w[1][p], w[2][p], w[3][p]);
+    }
+#pragma unroll
+    for (int p = 0; p < P; ++p) *reinterpret_cast<uint4*>(a.out + p * a.plane + at * 8) = out[p];
+}
+
+// ---- a few rows ------------------------------------------------------------------------------------------------------------
+
+constexpr int kFew = 4;                   // rows of a batch
+constexpr int64_t kFewShared = 96 * 1024;  // bytes that they take in shared memory: two CTAs to an SM
+
+struct FewArgs {
+    const void *x, *weight;
+    int64_t x_ws, x_rs, w_ws, w_rs;
+    int32_t h, vocab, rows, worker_rows;  // rows of a batch, and of a worker
+    int64_t all_rows;
+    const int64_t* target;
+    float* target_logit;
+    float2* stats;  // [CTA][all rows]
+};
+// A warp takes four rows of W at a time, a lane eight columns (or every 32nd) of each: 64 bytes of W for one reading of x.
+template <typename TX, typename TW, int MR, bool VEC>
+__global__ void __launch_bounds__(256) few_kernel(const __grid_constant__ FewArgs a) {
+    extern __shared__ __align__(16) float xs[];  // [MR][h up to a multiple of 8]
+    __shared__ float2 joint[8][MR];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pitch = (a.h + 7) & ~7;
+    const int64_t batch = blockIdx.y, number0 = batch * a.rows;
+    const TW* weight = (const TW*)a.weight + batch * a.w_ws;
+    for (int r = 0; r < MR; ++r) {
+        const TX* x = (const TX*)a.x + (batch + r / a.worker_rows) * a.x_ws + r % a.worker_rows * a.x_rs;
+        for (int c = threadIdx.x; c < pitch; c += 256) xs[r * pitch + c] = r < a.rows && c < a.h ? to_float(x[c]) : 0.0f;
+    }
+    __syncthreads();
+    int64_t target[MR];
+    float2 state[MR];
+#pragma unroll
+    for (int r = 0; r < MR; ++r) {
+        target[r] = r < a.rows ? a.target[number0 + r] : -1;
+        state[r] = make_float2(-kInf, 0.0f);
+    }
+    const int groups = (a.vocab + 3) / 4;
+    for (int g = blockIdx.x * 8 + warp; g < groups; g += gridDim.x * 8) {
+        float acc[4][MR] = {};
+        const TW* row[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) row[j] = weight + (int64_t)min(g * 4 + j, a.vocab - 1) * a.w_rs;
+        if constexpr (VEC) {
+#pragma unroll 2
+            for (int c = lane * 8; c < a.h; c += kSpan) {
+                Raw8<TW> raw[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) raw[j] = raw_load<TW>(row[j] + c);
+                float w[4][8];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) raw_floats<TW>(raw[j], w[j]);
+#pragma unroll
+                for (int r = 0; r < MR; ++r) {
+                    float v[8];
+                    *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(xs + r * pitch + c);
+                    *reinterpret_cast<float4*>(v + 4) = *reinterpret_cast<const float4*>(xs + r * pitch + c + 4);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) acc[j][r] = fmaf(w[j][k], v[k], acc[j][r]);
+                }
+            }
+        } else {
+#pragma unroll 4
+            for (int c = lane; c < a.h; c += 32) {
+                float w[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) w[j] = to_float(__ldg(row[j] + c));
+#pragma unroll
+                for (int r = 0; r < MR; ++r)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) acc[j][r] = fmaf(w[j], xs[r * pitch + c], acc[j][r]);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int r = 0; r < MR; ++r) {
+                float z = acc[j][r];
+#pragma unroll
+                for (int o = 16; o; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+                const int v = g * 4 + j;
+                if (v < a.vocab) {
+                    state[r] = merged(state[r], make_float2(z, 1.0f));
+                    if (lane == 0 && v == target[r]) a.target_logit[number0 + r] = z;
+                }
+            }
+    }
+#pragma unroll
+    for (int r = 0; r < MR; ++r)
+        if (lane == 0) joint[warp][r] = state[r];
+    __syncthreads();
+    if (threadIdx.x < a.rows) {
+        float2 v = joint[0][threadIdx.x];
+#pragma unroll
+        for (int w = 1; w < 8; ++w) v = merged(v, joint[w][threadIdx.x]);
+        a.stats[blockIdx.x * a.all_rows + number0 + threadIdx.x] = v;
+    }
+}
+
+// ---- losses ----------------------------------------------------------------------------------------------------------------
+
+enum Reduction : int32_t { kNone = 0, kMean = 1, kSum = 2 };
+
+struct JoinArgs {
+    const float2* stats;  // [part][all rows]
+    const float* target_logit;
+    const int64_t* target;
+    int64_t all_rows, rows, parts, ignored, vocab;
+    int32_t lanes;      // rows of a CTA, a power of two up to 32
+    int32_t whole;      // a CTA has a worker's rows, all of them
+    int32_t reduction;
+    float *lse, *row_loss, *loss;
+};
+__device__ __forceinline__ float sum_of_warp(float v) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+// 32 rows (fewer where there are fewer) by 1024 / rows shares of the parts.
+__global__ void __launch_bounds__(1024) join_kernel(const __grid_constant__ JoinArgs a) {
+    __shared__ float2 shares[1024];
+    dependency_wait();
+    const int r = threadIdx.x & (a.lanes - 1), share = threadIdx.x / a.lanes, count = 1024 / a.lanes;
+    const int64_t row = (int64_t)blockIdx.x * (a.whole ? a.rows : a.lanes) + r;
+    const bool there = a.whole ? r < a.rows : row < a.all_rows;
+    float2 v = make_float2(-kInf, 0.0f);
+    if (there)
+#pragma unroll 4
+        for (int64_t p = share; p < a.parts; p += count) v = merged(v, a.stats[p * a.all_rows + row]);
+    shares[threadIdx.x] = v;
+    for (int o = count / 2; o; o >>= 1) {
+        __syncthreads();
+        if (share < o) shares[threadIdx.x] = merged(shares[threadIdx.x], shares[threadIdx.x + o * a.lanes]);
+    }
+    if (threadIdx.x >= 32) return;
+    __syncwarp();
+    float loss = 0.0f, counted = 0.0f;
+    if (there && (int)threadIdx.x < a.lanes) {
+        v = shares[threadIdx.x];
+        const float lse = v.x + logf(v.y);
+        const int64_t t = a.target[row];
+        a.lse[row] = lse;
+        if (t != a.ignored) {
+            counted = 1.0f;
+            loss = t >= 0 && t < a.vocab ? lse - a.target_logit[row] : __int_as_float(0x7fffffff);  // no such column
+        }
+        if (a.reduction == kNone) a.loss[row] = loss;
+        else if (!a.whole) a.row_loss[row] = loss;
+    }
+    if (a.reduction == kNone || !a.whole) return;
+    loss = sum_of_warp(loss);
+    counted = sum_of_warp(counted);
+    if (threadIdx.x == 0) a.loss[blockIdx.x] = a.reduction == kMean ? loss / fmaxf(counted, 1.0f) : loss;
+}
+// A worker's loss from its rows'.
+__global__ void __launch_bounds__(256) reduce_kernel(const float* __restrict__ row_loss, const int64_t* __restrict__ target, int64_t rows,
+                                                     int64_t ignored, int32_t reduction, float* __restrict__ loss) {
+    __shared__ float sums[8], counts[8];
+    dependency_wait();
+    const int64_t row0 = blockIdx.x * rows;
+    float sum = 0.0f, count = 0.0f;
+    for (int64_t j = threadIdx.x; j < rows; j += 256) {
+        sum += row_loss[row0 + j];
+        count += target[row0 + j] != ignored ? 1.0f : 0.0f;
+    }
+    sum = sum_of_warp(sum);
+    count = sum_of_warp(count);
+    if ((threadIdx.x & 31) == 0) {
+        sums[threadIdx.x >> 5] = sum;
+        counts[threadIdx.x >> 5] = count;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < 8; ++w) {
+            sum += sums[w];
+            count += counts[w];
+        }
+        loss[blockIdx.x] = reduction == kMean ? sum / fmaxf(count, 1.0f) : sum;
+    }
+}
+
+// ---- the rows' gradients ---------------------------------------------------------------------------------------------------
+
+struct RowsArgs {
+    const float* dloss;
+    int64_t ws, rs;  // of dloss; rs counts without a reduction alone
+    const int64_t* target;
+    int64_t rows, ignored;
+    int32_t n, reduction, relative, together;
+    float2* worker;       // [n]: what g is multiplied by, the largest |g|
+    float *g, *scale;     // [all rows]
+};
+__device__ __forceinline__ float row_gradient(const RowsArgs& a, int64_t worker, int64_t row, float factor) {
+    if (a.target[worker * a.rows + row] == a.ignored) return 0.0f;
+    return factor * a.dloss[worker * a.ws + (a.reduction == kNone ? row * a.rs : 0)];
+}
+// A CTA per worker: its counted rows, and the largest |g| of them.
+__global__ void __launch_bounds__(256) worker_kernel(const __grid_constant__ RowsArgs a) {
+    __shared__ float counts[8], tops[8];
+    dependency_wait();
+    const int64_t i = blockIdx.x;
+    float count = 0.0f, top = 0.0f;
+    for (int64_t j = threadIdx.x; j < a.rows; j += 256)
+        if (a.target[i * a.rows + j] != a.ignored) {
+            count += 1.0f;
+            top = fmaxf(top, fabsf(a.dloss[i * a.ws + (a.reduction == kNone ? j * a.rs : 0)]));
+        }
+    count = sum_of_warp(count);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    if ((threadIdx.x & 31) == 0) {
+        counts[threadIdx.x >> 5] = count;
+        tops[threadIdx.x >> 5] = top;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < 8; ++w) {
+            count += counts[w];
+            top = fmaxf(top, tops[w]);
+        }
+        const float factor = a.reduction == kMean ? 1.0f / fmaxf(count, 1.0f) : 1.0f;
+        a.worker[i] = make_float2(factor, factor * top);
+    }
+}
+// g of every row; relative: to a power of two that no |g| of the worker (together: of all) is above, whose 2^-14th is the row's scale.
+__global__ void __launch_bounds__(256) rows_kernel(const __grid_constant__ RowsArgs a) {
+    dependency_wait();
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (at >= a.n * a.rows) return;
+    const int64_t i = at / a.rows;
+    float g = row_gradient(a, i, at - i * a.rows, a.worker[i].x);
+    if (a.relative) {
+        float top = a.worker[i].y;
+        if (a.together)
+            for (int k = 0; k < a.n; ++k) top = fmaxf(top, a.worker[k].y);
+        int e = 0;
+        if (top > 0.0f && top < kInf) frexpf(top, &e);
+        e = max(e, -100);  // (2^-e is finite; below, g is 0 but for rounding)
+        g = ldexpf(g, -e);
+        a.scale[at] = ldexpf(1.0f / head::kF16Scale, e);
+    }
+    a.g[at] = g;
+}
+
+// dx from the parts' sums.
+struct PartsArgs {
+    const float* parts;  // [parts][all rows][pitch]
+    int64_t part, all_rows, chunks;
+    int32_t count, h, per_row, pitch;
+    const float* scale;  // of a row; may be null
+    void* out;           // [all rows][h]
+};
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(256) parts_kernel(const __grid_constant__ PartsArgs a) {
+    dependency_wait();
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (at >= a.chunks) return;
+    const int64_t row = at / a.per_row;
+    const int c = (int)(at - row * a.per_row) * 8;
+    float v[8] = {};
+    for (int s = 0; s < a.count; ++s) {
+        const float* from = a.parts + s * a.part + row * a.pitch + c;
+        const float4 p = *reinterpret_cast<const float4*>(from), q = *reinterpret_cast<const float4*>(from + 4);
+        v[0] += p.x; v[1] += p.y; v[2] += p.z; v[3] += p.w;
+        v[4] += q.x; v[5] += q.y; v[6] += q.z; v[7] += q.w;
+    }
+    const float scale = a.scale ? a.scale[row] : 1.0f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] *= scale;
+    T* out = (T*)a.out + row * a.h + c;
+    if (VEC) {
+        store8<T>(out, v);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (c + k < a.h) out[k] = from_float<T>(v[k]);
+    }
+}
+
+// ---- host ------------------------------------------------------------------------------------------------------------------
+
+std::atomic<uint32_t> wait_tries{tensor::kTries};
+
+struct HeadShape {
+    int32_t n;
+    int64_t rows, h, vocab;
+    int32_t type, weight_type;
+    bool shared;  // one weight for all workers
+    bool ok() const {
+        return n >= 1 && n <= 65535 && rows >= 0 && rows <= (int64_t)0x7fffffff / n && h >= 1 && h < ((int64_t)1 << 31) - 4096 && vocab >= 1 &&
+               vocab < ((int64_t)1 << 31) - 4096 && type_known(type) && type_known(weight_type) && (type == weight_type || weight_type == kTypeF32);
+    }
+    bool copies() const { return weight_type == kTypeF32; }  // operands are planes, never the caller's own memory
+    bool f16() const { return type == kTypeF16 && !copies(); }
+    int x_planes() const { return !copies() || type == kTypeBF16 ? 1 : type == kTypeF16 ? 2 : 3; }
+    int w_planes() const { return copies() ? 3 : 1; }
+    int64_t batches() const { return shared ? 1 : n; }
+    int64_t batch_rows() const { return shared ? n * rows : rows; }
+    int64_t all_rows() const { return n * rows; }
+    int64_t pitch() const { return (h + 7) / 8 * 8; }
+    bool few() const { return batch_rows() <= kFew && batch_rows() * pitch() * 4 <= kFewShared; }
+    // planes of d: for dx, for dW
+    int x_probs() const { return type == kTypeF32 ? 3 : type == kTypeF16 && copies() ? 2 : 1; }
+    int w_probs() const { return copies() ? 3 : 1; }
+};
+
+// Rows on 16-byte boundaries and one behind the other, as TMA takes them; where there is but one row or batch its stride does not count.
+struct Matrix {
+    const void* p;
+    int64_t row_stride, batch_stride;  // elements
+};
+bool lies_well(const Matrix& m, int64_t rows, int64_t batches, int64_t h) {
+    return ((reinterpret_cast<uintptr_t>(m.p) & 15u) == 0) && (rows == 1 || (m.row_stride % 8 == 0 && m.row_stride >= h && m.row_stride < (int64_t)1 << 38)) &&
+           (batches == 1 || (m.batch_stride % 8 == 0 && m.batch_stride >= 1 && m.batch_stride < (int64_t)1 << 38));
+}
+// x as one batch of all workers' rows; false where the workers do not lie so.
+bool flat(const HeadShape& z, int64_t ws, int64_t rs, int64_t& stride) {
+    stride = z.rows == 1 ? ws : rs;
+    return z.rows == 1 || z.n == 1 || ws == z.rows * rs;
+}
+bool x_lies_well(const HeadShape& z, const void* x, int64_t ws, int64_t rs, Matrix& m) {
+    if (z.copies() || z.type == kTypeF32) return false;
+    int64_t stride = rs;
+    if (z.shared) {
+        if (!flat(z, ws, rs, stride)) return false;
+        m = {x, stride, 0};
+        return lies_well(m, z.all_rows(), 1, z.h);
+    }
+    m = {x, rs, ws};
+    return lies_well(m, z.rows, z.n, z.h);
+}
+bool w_lies_well(const HeadShape& z, const void* w, int64_t ws, int64_t rs, Matrix& m) {
+    if (z.copies() || z.weight_type == kTypeF32) return false;
+    m = {w, rs, ws};
+    return lies_well(m, z.vocab, z.batches(), z.h);
+}
+
+// How the vocabulary goes by, and where things lie in the workspace.
+struct Plan {
+    int64_t piece, pieces;  // columns, a multiple of 256 unless it is all of them
+    int64_t width;          // columns of d
+    int32_t probs, parts;   // planes of d; parts of the vocabulary's sum of dx
+    bool sums;              // dx is added up in fp32
+    int64_t x_copy, w_copy, stats, stat_parts, target_logit, row_loss, worker, g, scale, d, dx_sums, bytes;
+};
+constexpr int64_t kCopyBytes = 64ll << 20;   // of a piece's copy of W: it stays in the L2 between its writing and its reading
+constexpr int64_t kProbsBytes = 512ll << 20;  // of a piece's d
+constexpr int64_t kSumsBytes = 256ll << 20;   // of the parts' sums of dx
+constexpr int kFewWaves = 4;                  // CTAs of few_kernel to an SM
+
+int64_t up_to(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+int64_t few_ctas(const HeadShape& z) {
+    return std::max<int64_t>(1, std::min<int64_t>((z.vocab + 31) / 32, ((int64_t)multiprocessors() * kFewWaves + z.batches() - 1) / z.batches()));
+}
+
+// Parts of the vocabulary's sum of dx: as many as take the pairs of CTAs the shortest time, in tiles of 64 (0.3 us), with what adding up
+// the parts costs.
+int32_t parts_of(const HeadShape& z, int64_t steps, int pairs) {
+    const int64_t m = z.batch_rows(), tiles = (m + 255) / 256 * ((z.h + 255) / 256) * z.batches(), at_once = std::max(1, multiprocessors() / 2);
+    int32_t best = 1;
+    double least = 1e30;
+    for (int32_t s = 1; s <= 32 && s * 4 <= std::max<int64_t>(steps, 4) && (s == 1 || s * z.all_rows() * z.pitch() * 4 <= kSumsBytes); ++s) {
+        const double waves = (double)((tiles * s + at_once - 1) / at_once);
+        const double t = waves * (0.3 * pairs * (double)((steps + s - 1) / s) + 2.0) +
+                         (s > 1 ? 3.0 + s * (double)z.all_rows() * z.pitch() * 8e-6 / 5.0 : 0.0);
+        if (t < 0.98 * least) {
+            least = t;
+            best = s;
+        }
+    }
+    return best;
+}
+
+Plan plan_of(const HeadShape& z, bool x_copied, bool w_copied, int wanted) {  // wanted: 0 forward, else 1 dx + 2 dW
+    Plan p = {};
+    const int64_t m = z.all_rows();
+    p.probs = std::max(wanted & 1 ? z.x_probs() : 0, wanted & 2 ? z.w_probs() : 0);
+    p.piece = z.vocab;
+    const bool few = !wanted && z.few();
+    if (!few) {
+        int64_t most = up_to(z.vocab, 256);
+        if (w_copied) most = std::min(most, std::max<int64_t>(256, kCopyBytes / (z.w_planes() * z.batches() * z.pitch() * 2) / 256 * 256));
+        if (wanted) most = std::min(most, std::max<int64_t>(256, kProbsBytes / (p.probs * m * 2) / 256 * 256));
+        p.pieces = (z.vocab + most - 1) / most;
+        p.piece = std::min(z.vocab, up_to((z.vocab + p.pieces - 1) / p.pieces, 256));
+    }
+    p.pieces = (z.vocab + p.piece - 1) / p.piece;
+    p.width = up_to(p.piece, 256);
+    int64_t at = 0;
+    auto take = [&](int64_t bytes) {
+        const int64_t here = at;
+        at += up_to(bytes, 256);
+        return here;
+    };
+    if (x_copied && !few) p.x_copy = take(z.x_planes() * m * z.pitch() * 2);
+    if (w_copied && !few) p.w_copy = take(z.w_planes() * z.batches() * p.piece * z.pitch() * 2);
+    if (!wanted) {
+        p.stat_parts = few ? few_ctas(z) : (z.vocab + kVocab - 1) / kVocab;
+        p.stats = take(p.stat_parts * m * 8);
+        p.target_logit = take(m * 4);
+        p.row_loss = take(m * 4);
+    } else {
+        p.worker = take(z.n * 8);
+        p.g = take(m * 4);
+        p.scale = take(m * 4);
+        p.d = take(p.probs * m * p.width * 2);
+        p.parts = wanted & 1 ? parts_of(z, (p.piece + 63) / 64, z.x_probs() == 3 ? 6 : z.x_probs() == 2 ? 3 : z.copies() ? 2 : 1) : 1;
+        p.sums = (wanted & 1) && (p.parts > 1 || p.pieces > 1);
+        if (p.sums) p.dx_sums = take(p.parts * m * z.pitch() * 4);
+    }
+    p.bytes = at;
+    return p;
+}
+
+// An operand: 16-bit planes, [plane][batch][rows][columns].
+struct Operand {
+    const void* p;
+    int64_t columns, rows, batches, planes;
+    int64_t row_stride, batch_stride;  // elements; plane after plane
+};
+bool operand_map(CUtensorMap* map, const Operand& o, bool f16, uint32_t box_rows) {
+    const Encode encode = map_encoder();
+    if (!encode) return false;
+    const int64_t row = o.rows > 1 ? o.row_stride : up_to(o.columns, 8), batch = o.batches * o.planes > 1 ? o.batch_stride : row * o.rows;
+    const cuuint64_t size[3] = {(cuuint64_t)o.columns, (cuuint64_t)o.rows, (cuuint64_t)(o.batches * o.planes)};
+    const cuuint64_t stride[2] = {(cuuint64_t)row * 2, (cuuint64_t)batch * 2};
+    const cuuint32_t extent[3] = {64, box_rows, 1}, every[3] = {1, 1, 1};
+    return encode(map, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(o.p), size, stride, extent,
+                  every, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Pairs of planes whose indices together are at most `order`, small ones first.
+void pairs_of(head::Args& a, int left, int right, int order) {
+    a.pairs = 0;
+    for (int both = order; both >= 0; --both)
+        for (int i = 0; i <= both; ++i)
+            if (i < left && both - i < right) {
+                a.left_plane[a.pairs] = (uint8_t)i;
+                a.right_plane[a.pairs++] = (uint8_t)(both - i);
+            }
+}
+
+template <int FORM>
+int product(head::Args& a, const Operand& left, const Operand& right, bool f16, cudaStream_t stream, const char* what) {
+    using O = head::Order<FORM>;
+    CUtensorMap l = {}, r = {};
+    if (!operand_map(&l, left, f16, O::kLeftAcross ? 64 : 128) || !operand_map(&r, right, f16, O::kRightAcross ? 64 : 128))
+        return COMPAMS_ERR_INVALID_ARG;
+    a.left_planes = (int32_t)left.batches;
+    a.right_planes = (int32_t)right.batches;
+    a.left_batch = left.batches > 1;
+    a.right_batch = right.batches > 1;
+    a.f16 = f16;
+    a.tries = wait_tries.load(std::memory_order_relaxed);
+    const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n * a.batches * a.parts;
+    if (tiles > 0x3fffffff) return COMPAMS_ERR_TOO_LARGE;
+    const int64_t at_once = std::max(1, multiprocessors() / 2);
+    return launched(launch_sized(head::head_kernel<FORM>, dim3((uint32_t)(2 * std::min(tiles, at_once))), head::kThreads, 2, head::kShared, false,
+                                 stream, a, l, r),
+                    what);
+}
+
+template <typename T, int P>
+int pack(const Matrix& m, int64_t rows, int64_t row0, int64_t batches, int64_t h, uint16_t* out, cudaStream_t stream) {
+    PackArgs a = {};
+    a.src = m.p; a.ws = m.batch_stride; a.rs = m.row_stride; a.rows = rows; a.row0 = row0; a.h = (int32_t)h;
+    a.per_row = (int32_t)((h + 7) / 8);
+    a.chunks = batches * rows * a.per_row;
+    a.out = out; a.plane = a.chunks * 8;
+    const int64_t ctas = (a.chunks + 255) / 256;
+    if (ctas > 0x7fffffff) return COMPAMS_ERR_TOO_LARGE;
+    const bool vec = h % 8 == 0 && ((reinterpret_cast<uintptr_t>(m.p) | (uint64_t)(m.row_stride * (int64_t)sizeof(T)) |
+                                     (uint64_t)(m.batch_stride * (int64_t)sizeof(T))) & 15u) == 0;
+    const auto kernel = vec ? pack_kernel<T, P, true> : pack_kernel<T, P, false>;
+    return launched(launch_sized(kernel, dim3((uint32_t)ctas), 256, 1, 0, false, stream, a), "head_pack");
+}
+int pack_operand(const HeadShape& z, int32_t type, int planes, const Matrix& m, int64_t rows, int64_t row0, int64_t batches, void* out,
+                 cudaStream_t stream) {
+    uint16_t* to = (uint16_t*)out;
+    if (type == kTypeF32) return pack<float, 3>(m, rows, row0, batches, z.h, to, stream);
+    if (type == kTypeBF16) return pack<__nv_bfloat16, 1>(m, rows, row0, batches, z.h, to, stream);
+    return planes == 2 ? pack<__half, 2>(m, rows, row0, batches, z.h, to, stream) : pack<__half, 1>(m, rows, row0, batches, z.h, to, stream);
+}
+
+// x as an operand, the caller's memory or a copy: [plane][batch][rows of a batch][h].
+int x_operand(const HeadShape& z, const void* x, int64_t ws, int64_t rs, const Plan& p, char* work, Operand& o, cudaStream_t stream) {
+    Matrix m;
+    o = {nullptr, z.h, z.batch_rows(), z.batches(), z.x_planes(), 0, 0};
+    if (x_lies_well(z, x, ws, rs, m)) {
+        o.p = m.p; o.row_stride = m.row_stride; o.batch_stride = m.batch_stride;
+        return COMPAMS_OK;
+    }
+    o.p = work + p.x_copy; o.row_stride = z.pitch(); o.batch_stride = z.batch_rows() * z.pitch();
+    o.columns = z.pitch();
+    return pack_operand(z, z.type, z.x_planes(), {x, rs, ws}, z.rows, 0, z.n, work + p.x_copy, stream);
+}
+// Rows v0 ... of the weight: the caller's memory, whose row v0 is row `first`, or a copy of the piece.
+int w_operand(const HeadShape& z, const void* w, int64_t ws, int64_t rs, const Plan& p, int64_t v0, int64_t count, char* work, Operand& o,
+              int32_t& first, cudaStream_t stream) {
+    Matrix m;
+    o = {nullptr, z.h, z.vocab, z.batches(), z.w_planes(), 0, 0};
+    if (w_lies_well(z, w, ws, rs, m)) {
+        o.p = m.p; o.row_stride = m.row_stride; o.batch_stride = m.batch_stride;
+        first = (int32_t)v0;
+        return COMPAMS_OK;
+    }
+    first = 0;
+    o.p = work + p.w_copy; o.rows = count; o.columns = z.pitch(); o.row_stride = z.pitch(); o.batch_stride = count * z.pitch();
+    return pack_operand(z, z.weight_type, z.w_planes(), {w, rs, ws}, count, v0, z.batches(), work + p.w_copy, stream);
+}
+
+template <typename TX, typename TW, int MR>
+int few_rows(const HeadShape& z, FewArgs& a, bool vec, int64_t ctas, cudaStream_t stream) {
+    const auto kernel = vec ? few_kernel<TX, TW, MR, true> : few_kernel<TX, TW, MR, false>;
+    return launched(launch_sized(kernel, dim3((uint32_t)ctas, (uint32_t)z.batches()), 256, 1, (size_t)(MR * z.pitch() * 4), true, stream, a),
+                    "head_few");
+}
+template <typename TX, typename TW>
+int few_rows(const HeadShape& z, FewArgs& a, int64_t ctas, cudaStream_t stream) {
+    const bool vec = z.h % 8 == 0 && ((reinterpret_cast<uintptr_t>(a.weight) | (uint64_t)(a.w_rs * (int64_t)sizeof(TW)) |
+                                       (uint64_t)(a.w_ws * (int64_t)sizeof(TW))) & 15u) == 0;
+    return a.rows == 1 ? few_rows<TX, TW, 1>(z, a, vec, ctas, stream)
+                       : a.rows == 2 ? few_rows<TX, TW, 2>(z, a, vec, ctas, stream) : few_rows<TX, TW, 4>(z, a, vec, ctas, stream);
+}
+
+bool float_aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+bool element_aligned(const void* p, int32_t type) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(type_bytes(type) - 1)) == 0; }
+
+}  // namespace
+}  // namespace compams
+
+using namespace compams;
+
+extern "C" {
+
+int compams_head_status(int32_t* gave_up) {
+    if (!gave_up) return COMPAMS_ERR_INVALID_ARG;
+    int32_t none = 0;
+    cudaError_t e = cudaMemcpyFromSymbol(gave_up, head::gave_up, sizeof(int32_t));
+    if (e == cudaSuccess && *gave_up) e = cudaMemcpyToSymbol(head::gave_up, &none, sizeof(int32_t));
+    return launched(e, "head_status");
+}
+
+int compams_head_wait_tries(int32_t tries) {
+    if (tries < 0 || tries > (int32_t)tensor::kTries) return COMPAMS_ERR_INVALID_ARG;
+    wait_tries.store((uint32_t)tries, std::memory_order_relaxed);
+    return COMPAMS_OK;
+}
+
+int compams_head_workspace_bytes(size_t* bytes, int32_t n, int64_t rows, int64_t h, int64_t vocab, int32_t type, int32_t weight_type,
+                                 int32_t shared, int32_t x_copied, int32_t weight_copied, int32_t wanted) {
+    const HeadShape z{n, rows, h, vocab, type, weight_type, shared != 0 || n == 1};
+    if (!bytes || !z.ok() || wanted < 0 || wanted > 3) return COMPAMS_ERR_INVALID_ARG;
+    *bytes = rows ? (size_t)plan_of(z, x_copied || z.copies(), weight_copied || z.copies(), wanted).bytes : 0;
+    return COMPAMS_OK;
+}
+
+int compams_head_forward(float* loss, float* lse, const void* x, int32_t type, const void* weight, int32_t weight_type, const int64_t* target,
+                         int32_t n, int64_t rows, int64_t h, int64_t vocab, int64_t x_worker_stride, int64_t x_row_stride,
+                         int64_t weight_worker_stride, int64_t weight_row_stride, int64_t ignored, int32_t reduction, void* workspace,
+                         size_t workspace_bytes, void* cuda_stream) {
+    const HeadShape z{n, rows, h, vocab, type, weight_type, weight_worker_stride == 0 || n == 1};
+    if (!z.ok() || reduction < kNone || reduction > kSum || x_worker_stride < 0 || x_row_stride < 0 || weight_worker_stride < 0 ||
+        weight_row_stride < 0 || !float_aligned(loss) || (!loss && (rows || reduction)))
+        return COMPAMS_ERR_INVALID_ARG;
+    const cudaStream_t stream = (cudaStream_t)cuda_stream;
+    if (rows == 0) return reduction == kNone ? COMPAMS_OK : launched(cudaMemsetAsync(loss, 0, (size_t)n * 4, stream), "head_forward");
+    Matrix m;
+    const Plan p = plan_of(z, !x_lies_well(z, x, x_worker_stride, x_row_stride, m),
+                           !w_lies_well(z, weight, weight_worker_stride, weight_row_stride, m), 0);
+    if (!lse || !x || !weight || !target || !workspace || workspace_bytes < (size_t)p.bytes || (reinterpret_cast<uintptr_t>(workspace) & 255u) ||
+        !float_aligned(lse) || !element_aligned(x, type) || !element_aligned(weight, weight_type) || (reinterpret_cast<uintptr_t>(target) & 7u))
+        return COMPAMS_ERR_INVALID_ARG;
+    char* work = (char*)workspace;
+    float2* stats = (float2*)(work + p.stats);
+    float* target_logit = (float*)(work + p.target_logit);
+    int rc = COMPAMS_OK;
+    if (z.few()) {
+        FewArgs a = {};
+        a.x = x; a.weight = weight; a.x_ws = x_worker_stride; a.x_rs = x_row_stride; a.w_ws = z.shared ? 0 : weight_worker_stride; a.w_rs = weight_row_stride; a.h = (int32_t)h; a.vocab = (int32_t)vocab;
+        a.rows = (int32_t)z.batch_rows(); a.all_rows = z.all_rows(); a.target = target; a.target_logit = target_logit; a.stats = stats;
+        a.worker_rows = (int32_t)rows;
+        const int64_t ctas = p.stat_parts;
+        const bool wide = weight_type == kTypeF32;
+        rc = type == kTypeF32 ? few_rows<float, float>(z, a, ctas, stream)
+             : type == kTypeBF16 ? (wide ? few_rows<__nv_bfloat16, float>(z, a, ctas, stream) : few_rows<__nv_bfloat16, __nv_bfloat16>(z, a, ctas, stream))
+                                 : (wide ? few_rows<__half, float>(z, a, ctas, stream) : few_rows<__half, __half>(z, a, ctas, stream));
+    } else {
+        Operand xo, wo;
+        rc = x_operand(z, x, x_worker_stride, x_row_stride, p, work, xo, stream);
+        for (int64_t v0 = 0; v0 < vocab && rc == COMPAMS_OK; v0 += p.piece) {
+            const int64_t count = std::min(p.piece, vocab - v0);
+            head::Args a = {};
+            rc = w_operand(z, weight, weight_worker_stride, weight_row_stride, p, v0, count, work, wo, a.right_row, stream);
+            if (rc != COMPAMS_OK) break;
+            a.tiles_m = (int32_t)((z.batch_rows() + 255) / 256); a.tiles_n = (int32_t)((count + 255) / 256);
+            a.batches = (int32_t)z.batches(); a.parts = 1;
+            a.steps = a.part_steps = (int32_t)((h + 63) / 64);
+            pairs_of(a, z.x_planes(), z.w_planes(), 2);
+            a.rows = z.batch_rows(); a.columns = (int32_t)vocab; a.first = (int32_t)v0;
+            a.target = target; a.target_logit = target_logit; a.stats = stats; a.all_rows = z.all_rows();
+            rc = product<head::kForward>(a, xo, wo, z.f16(), stream, "head_forward");
+        }
+    }
+    if (rc != COMPAMS_OK) return rc;
+    JoinArgs j = {};
+    j.stats = stats; j.target_logit = target_logit; j.target = target; j.all_rows = z.all_rows(); j.rows = rows; j.parts = p.stat_parts;
+    j.ignored = ignored; j.vocab = vocab; j.reduction = reduction; j.lse = lse; j.row_loss = (float*)(work + p.row_loss); j.loss = loss;
+    j.whole = reduction != kNone && rows <= 32;
+    const int64_t most = j.whole ? rows : std::min<int64_t>(32, j.all_rows);
+    for (j.lanes = 1; j.lanes < most;) j.lanes *= 2;
+    const int64_t ctas = j.whole ? n : (j.all_rows + j.lanes - 1) / j.lanes;
+    rc = launched(launch_sized(join_kernel, dim3((uint32_t)ctas), 1024, 1, 0, false, stream, j), "head_join");
+    if (rc != COMPAMS_OK || j.whole || reduction == kNone) return rc;
+    return launched(launch_sized(reduce_kernel, dim3((uint32_t)n), 256, 1, 0, false, stream, (const float*)j.row_loss, target, rows, ignored,
+                                 reduction, loss),
+                    "head_reduce");
+}
+
+int compams_head_backward(void* dx, void* dweight, int32_t sum_workers, const float* dloss, int64_t dloss_worker_stride, int64_t dloss_row_stride,
+                          const void* x, int32_t type, const void* weight, int32_t weight_type, const int64_t* target, const float* lse, int32_t n,
+                          int64_t rows, int64_t h, int64_t vocab, int64_t x_worker_stride, int64_t x_row_stride, int64_t weight_worker_stride,
+                          int64_t weight_row_stride, int64_t ignored, int32_t reduction, void* workspace, size_t workspace_bytes,
+                          void* cuda_stream) {
+    const HeadShape z{n, rows, h, vocab, type, weight_type, weight_worker_stride == 0 || n == 1};
+    const bool together = sum_workers != 0;
+    if (!z.ok() || reduction < kNone || reduction > kSum || x_worker_stride < 0 || x_row_stride < 0 || weight_worker_stride < 0 ||
+        weight_row_stride < 0 || dloss_worker_stride < 0 || dloss_row_stride < 0 || (together && dweight && !z.shared) ||
+        !element_aligned(dx, type) || !element_aligned(dweight, weight_type))
+        return COMPAMS_ERR_INVALID_ARG;
+    const cudaStream_t stream = (cudaStream_t)cuda_stream;
+    const int64_t gradients = together ? 1 : n;
+    if (rows == 0)
+        return dweight ? launched(cudaMemsetAsync(dweight, 0, (size_t)(gradients * vocab * h * type_bytes(weight_type)), stream), "head_backward")
+                       : COMPAMS_OK;
+    const int wanted = (dx ? 1 : 0) | (dweight ? 2 : 0);
+    if (!wanted) return COMPAMS_OK;
+    Matrix m;
+    const Plan p = plan_of(z, !x_lies_well(z, x, x_worker_stride, x_row_stride, m),
+                           !w_lies_well(z, weight, weight_worker_stride, weight_row_stride, m), wanted);
+    if (!dloss || !lse || !x || !weight || !target || !workspace || workspace_bytes < (size_t)p.bytes ||
+        (reinterpret_cast<uintptr_t>(workspace) & 255u) || !float_aligned(lse) || !float_aligned(dloss) || !element_aligned(x, type) ||
+        !element_aligned(weight, weight_type) || (reinterpret_cast<uintptr_t>(target) & 7u))
+        return COMPAMS_ERR_INVALID_ARG;
+    char* work = (char*)workspace;
+    const int64_t all = z.all_rows();
+    RowsArgs r = {};
+    r.dloss = dloss; r.ws = dloss_worker_stride; r.rs = dloss_row_stride; r.target = target; r.rows = rows; r.ignored = ignored; r.n = n;
+    r.reduction = reduction; r.relative = z.f16(); r.together = together && dweight; r.worker = (float2*)(work + p.worker);
+    r.g = (float*)(work + p.g); r.scale = (float*)(work + p.scale);
+    int rc = launched(launch_sized(worker_kernel, dim3((uint32_t)n), 256, 1, 0, true, stream, r), "head_worker");
+    if (rc == COMPAMS_OK)
+        rc = launched(launch_sized(rows_kernel, dim3((uint32_t)((all + 255) / 256)), 256, 1, 0, false, stream, r), "head_rows");
+    Operand xo, wo;
+    if (rc == COMPAMS_OK) rc = x_operand(z, x, x_worker_stride, x_row_stride, p, work, xo, stream);
+    const float* scale = z.f16() ? r.scale : nullptr;
+    uint16_t* d = (uint16_t*)(work + p.d);
+    const int32_t tiles_h = (int32_t)((h + 255) / 256), tiles_rows = (int32_t)((z.batch_rows() + 255) / 256);
+    for (int64_t v0 = 0; v0 < vocab && rc == COMPAMS_OK; v0 += p.piece) {
+        const int64_t count = std::min(p.piece, vocab - v0);
+        int32_t first = 0;
+        rc = w_operand(z, weight, weight_worker_stride, weight_row_stride, p, v0, count, work, wo, first, stream);
+        if (rc != COMPAMS_OK) break;
+        {
+            head::Args a = {};
+            a.tiles_m = tiles_rows; a.tiles_n = (int32_t)((count + 255) / 256); a.batches = (int32_t)z.batches(); a.parts = 1;
+            a.steps = a.part_steps = (int32_t)((h + 63) / 64);
+            pairs_of(a, z.x_planes(), z.w_planes(), 2);
+            a.right_row = first; a.rows = z.batch_rows(); a.columns = (int32_t)vocab; a.first = (int32_t)v0; a.target = target;
+            a.all_rows = all; a.lse = lse; a.row_gradient = r.g; a.probs = d; a.probs_plane = all * p.width; a.width = (int32_t)p.width;
+            a.probs_planes = p.probs;
+            rc = product<head::kProbs>(a, xo, wo, z.f16(), stream, "head_probs");
+        }
+        const Operand by_batch{d, p.width, z.batch_rows(), z.batches(), p.probs, p.width, z.batch_rows() * p.width};
+        if (rc == COMPAMS_OK && dx) {
+            head::Args a = {};
+            a.tiles_m = tiles_rows; a.tiles_n = tiles_h; a.batches = (int32_t)z.batches(); a.parts = p.parts;
+            a.steps = (int32_t)((count + 63) / 64); a.part_steps = (a.steps + p.parts - 1) / p.parts;
+            // 8 bits beside an fp32 weight: two of its planes; 11 bits: to the same order
+            pairs_of(a, z.x_probs(), z.copies() && type != kTypeF32 ? 2 : z.w_planes(), type == kTypeF32 ? 2 : 1);
+            a.right_sum = first; a.rows = z.batch_rows();
+            if (p.sums) {
+                a.out = work + p.dx_sums; a.out_type = kTypeF32; a.out_row = z.pitch(); a.columns = (int32_t)z.pitch();
+                a.out_part = all * z.pitch(); a.add = v0 > 0;
+            } else {
+                a.out = dx; a.out_type = type; a.out_row = h; a.columns = (int32_t)h; a.row_scale = scale;
+            }
+            a.out_batch = z.batch_rows() * a.out_row;
+            rc = product<head::kInput>(a, by_batch, wo, z.f16(), stream, "head_input");
+        }
+        if (rc == COMPAMS_OK && dweight) {
+            // together: one sum over all workers' rows; else a batch for every worker
+            const int64_t batches = together ? 1 : n, sum = together ? all : rows;
+            head::Args a = {};
+            a.tiles_m = (int32_t)((count + 255) / 256); a.tiles_n = tiles_h; a.batches = (int32_t)batches; a.parts = 1;
+            a.steps = a.part_steps = (int32_t)((sum + 63) / 64);
+            pairs_of(a, z.w_probs(), z.x_planes(), 2);
+            a.rows = count; a.columns = (int32_t)h; a.out_type = weight_type; a.out_row = h; a.out_batch = vocab * h;
+            a.out = (char*)dweight + v0 * h * type_bytes(weight_type);
+            a.row_scale = scale; a.scale_batch = together ? 0 : rows;
+            const Operand left{d, p.width, sum, batches, p.probs, p.width, sum * p.width};
+            Operand right = xo;
+            right.rows = sum; right.batches = batches;
+            if (z.shared) right.batch_stride = sum * (all > 1 ? xo.row_stride : z.pitch());
+            rc = product<head::kWeight>(a, left, right, z.f16(), stream, "head_weight");
+        }
+    }
+    if (rc != COMPAMS_OK || !p.sums || !dx) return rc;
+    PartsArgs a = {};
+    a.parts = (const float*)(work + p.dx_sums); a.part = all * z.pitch(); a.all_rows = all; a.count = p.parts; a.h = (int32_t)h;
+    a.per_row = (int32_t)(z.pitch() / 8); a.pitch = (int32_t)z.pitch(); a.chunks = all * a.per_row; a.scale = scale; a.out = dx;
+    const int64_t ctas = (a.chunks + 255) / 256;
+    if (ctas > 0x7fffffff) return COMPAMS_ERR_TOO_LARGE;
+    const bool vec = h % 8 == 0 && (reinterpret_cast<uintptr_t>(dx) & 15u) == 0;
+    auto go = [&](auto t) {
+        using T = decltype(t);
+        const auto kernel = vec ? parts_kernel<T, true> : parts_kernel<T, false>;
+        return launched(launch_sized(kernel, dim3((uint32_t)ctas), 256, 1, 0, false, stream, a), "head_parts");
+    };
+    return type == kTypeF32 ? go(float()) : type == kTypeBF16 ? go(__nv_bfloat16()) : go(__half());
+}
+
+}  // extern "C"

@@ -1,0 +1,503 @@
+// The head's products on tcgen05.mma: one kernel in four forms, which differ in the order of their operands and in what becomes of a tile.
+//
+//   FORWARD   z = x W^T        x and W along the sum (K-major)      a row's maximum and sum of exponentials in the tile, the target's logit
+//   PROBS     z = x W^T        again                                d = (softmax(z) - [target]) g, written as 16-bit planes
+//   INPUT     dx = d W         d along the sum, W across it         added up over the pieces and parts of the vocabulary
+//   WEIGHT    dW = d^T x       both across the sum                  written
+//
+// A pair of CTAs takes tiles of 256 x 256 (cta_group::2): each holds 128 rows of the left operand and 128 of the right in shared memory,
+// half of what two CTAs of 128 x 256 would read from it and fetch from the L2, and has the sums of its 128 rows in its tensor memory,
+// twice (2 x 256 columns): while eight warps take the sums of one stretch, the products of the next go to the other. The tensor cores cut
+// their sums, so a stretch is kFlush tiles of 64 long and joins the fp32 registers by rounded additions.
+//
+// Operands are bf16 or fp16. fp32 numbers are three bf16 planes, and fp16 ones beside fp32 two: the sum then runs over pairs of planes as
+// well, listed in the arguments, small ones first.
+//
+// A tenth warp's thread brings tiles by TMA into the 128-byte swizzle, in both CTAs, to the first CTA's barriers; a ninth's, in the first
+// CTA, issues the products. All waits are bounded: who gives up marks the CTA, whose results then are NaN.
+#pragma once
+
+#include "rows.cuh"
+#include "tcgen05.cuh"
+
+namespace compams {
+namespace {
+namespace head {
+
+using namespace tensor;
+
+// Whoever's wait gave up marks the CTA's shared word and this one, which stays until it is asked for. No size or input should bring it about.
+__device__ int32_t gave_up;
+__device__ __forceinline__ void give_up(uint32_t* lost) {
+    gave_up = 1;
+    *lost = 1u;
+}
+
+enum Form : int { kForward, kProbs, kInput, kWeight };
+
+constexpr int kTile = 256;                     // rows and columns of a pair's tile
+constexpr int kHalf = 128 * 128;               // bytes of a CTA's 128 x 64 of an operand
+constexpr int kStages = 6, kStage = 2 * kHalf;  // 32 KB a stage
+constexpr int kStaging = 8 * 4096;             // 32 rows of 128 bytes for each of the eight warps
+constexpr int kShared = 1024 + kStages * kStage + kStaging;
+// Three groups of four warps at 168 registers; the two that keep sums take 216 and the third keeps 40: no more than the launch has.
+constexpr int kThreads = 384;
+constexpr int kSumRegisters = 216, kOtherRegisters = 40;
+static_assert(256 * kSumRegisters + 128 * kOtherRegisters <= kThreads * 168, "registers of the launch");
+constexpr int kFlush = 8;  // tiles of 64 between two additions to the registers
+constexpr int kMostPairs = 6;
+// The barriers: a stage has landed (of both CTAs, at the first); its products are done; the sums are ready, and drained (at the first).
+constexpr int kFull = 0, kEmpty = kStages, kReady = 2 * kStages, kDrained = kReady + 2, kStopped = kDrained + 2, kBars = kStopped + 1;
+
+struct Args {
+    // the tiles, in this order: batch, part of the sum, row and column in groups of kRaster rows
+    int32_t tiles_m, tiles_n, batches, parts;
+    int32_t steps, part_steps;  // tiles of 64 along the sum: of a batch, and of a part
+    // operands: the third coordinate is plane * planes apart + batch * batch apart; where rows and the sum begin
+    int32_t pairs;
+    uint8_t left_plane[kMostPairs], right_plane[kMostPairs];
+    int32_t left_planes, left_batch, left_row, left_sum;
+    int32_t right_planes, right_batch, right_row, right_sum;
+    int32_t f16;    // operands are fp16 (else bf16)
+    uint32_t tries;  // of a wait
+    int64_t rows;   // of a batch: rows of the result
+    int32_t columns;  // of the result; FORWARD, PROBS: the vocabulary
+    int32_t first;  // FORWARD, PROBS: the piece's first column
+    // FORWARD, PROBS; rows are numbered through the batches
+    const int64_t* target;
+    float* target_logit;
+    float2* stats;         // FORWARD: [half tile of the vocabulary][all rows]: maximum, sum of exp(z - maximum)
+    int64_t all_rows;
+    const float *lse, *row_gradient;
+    uint16_t* probs;       // PROBS: [plane][all rows][width]
+    int64_t probs_plane;   // elements of a plane
+    int32_t width, probs_planes;
+    // INPUT, WEIGHT
+    void* out;             // fp32, or of out_type where it is final
+    int64_t out_part, out_batch, out_row;  // elements from part to part, batch to batch, row to row
+    int32_t out_type, add;                 // add: onto what is there (fp32)
+    const float* row_scale;                // INPUT: of a row, WEIGHT: of a batch's first row; null: 1
+    int64_t scale_batch;                   // WEIGHT: rows from batch to batch
+};
+
+constexpr int kRaster = 8;
+
+struct Place {
+    int32_t batch, part, m, n;
+};
+__device__ __forceinline__ Place place_of(const Args& a, uint32_t t) {
+    Place p;
+    const uint32_t plane = (uint32_t)a.tiles_m * a.tiles_n, whole = t / plane, in = t - whole * plane;
+    p.batch = (int32_t)(whole / a.parts);
+    p.part = (int32_t)(whole - (uint32_t)p.batch * a.parts);
+    const uint32_t band = kRaster * (uint32_t)a.tiles_n, group = in / band, left = in - group * band;
+    const uint32_t high = min((uint32_t)kRaster, (uint32_t)a.tiles_m - group * kRaster);
+    p.n = (int32_t)(left / high);
+    p.m = (int32_t)(group * kRaster + (left - (uint32_t)p.n * high));
+    return p;
+}
+
+// ---- instructions of a pair of CTAs ------------------------------------------------------------------------------------------
+
+__device__ __forceinline__ void pair_alloc(uint32_t to) {  // a whole warp of each CTA
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(to) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void pair_free(uint32_t at) {
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(at) : "memory");
+}
+__device__ __forceinline__ uint32_t cta_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+// A shared address of this CTA as the first CTA's.
+__device__ __forceinline__ uint32_t at_first(uint32_t address) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(address));
+    return r;
+}
+__device__ __forceinline__ void arrive_at(uint32_t cluster_bar) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+__device__ __forceinline__ void pair_box(uint32_t to, const CUtensorMap* map, int x, int y, int z, uint32_t cluster_bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(to),
+        "l"(map), "r"(x), "r"(y), "r"(z), "r"(cluster_bar)
+        : "memory");
+}
+__device__ __forceinline__ void pair_product(uint32_t d, uint64_t a, uint64_t b, uint32_t what, bool onto) {
+    asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b),
+                 "r"(what), "r"((uint32_t)onto)
+                 : "memory");
+}
+// Tells the barrier at this place in both CTAs when the products so far are done.
+__device__ __forceinline__ void pair_done(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3)
+                 : "memory");
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// M = 256, N = 256.
+__host__ __device__ constexpr uint32_t pair_instruction(bool bf16, bool left_across, bool right_across) {
+    return 1u << 4 | (bf16 ? 1u << 7 | 1u << 10 : 0u) | (left_across ? 1u : 0u) << 15 | (right_across ? 1u : 0u) << 16 | (256u >> 3) << 17 |
+           (256u >> 4) << 24;
+}
+
+template <int FORM> struct Order {
+    static constexpr bool kLeftAcross = FORM == kWeight, kRightAcross = FORM == kInput || FORM == kWeight;
+};
+
+// ---- the parts ---------------------------------------------------------------------------------------------------------------
+
+__device__ __forceinline__ void steps_of(const Args& a, const Place& p, int& k0, int& k1) {
+    k0 = p.part * a.part_steps;
+    k1 = min(a.steps, k0 + a.part_steps);
+}
+
+// The tenth warp's thread, in both CTAs.
+template <int FORM>
+__device__ __forceinline__ void bring(const Args& a, const CUtensorMap* left, const CUtensorMap* right, uint32_t tiles, char* smem, uint32_t bars,
+                                      uint32_t rank, uint32_t* lost) {
+    using O = Order<FORM>;
+    const uint32_t bars0 = at_first(bars), mem = shared_address(smem);
+    int stage = 0;
+    uint32_t phase = 1;  // of a stage's first round there is nothing to wait for: the phase before it counts as ended
+    for (uint32_t t = blockIdx.x / 2; t < tiles; t += gridDim.x / 2) {
+        const Place p = place_of(a, t);
+        int k0, k1;
+        steps_of(a, p, k0, k1);
+        const int m = a.left_row + p.m * kTile + (int)rank * 128, n = a.right_row + p.n * kTile + (int)rank * 128;
+        const int lz = p.batch * a.left_batch, rz = p.batch * a.right_batch;
+        for (int k = k0; k < k1; ++k) {
+            const int ls = a.left_sum + k * 64, rs = a.right_sum + k * 64;
+            for (int pair = 0; pair < a.pairs; ++pair) {
+                if (!barrier_wait(bars + 8 * (kEmpty + stage), phase, a.tries)) {
+                    give_up(lost);
+                    return;
+                }
+                const uint32_t bar = bars0 + 8 * (kFull + stage), to = mem + stage * kStage;
+                if (rank == 0) mbar_expect(bars + 8 * (kFull + stage), 2 * kStage);
+                const int lp = lz + a.left_plane[pair] * a.left_planes, rp = rz + a.right_plane[pair] * a.right_planes;
+                if (O::kLeftAcross) {
+                    pair_box(to, left, m, ls, lp, bar);
+                    pair_box(to + 8192, left, m + 64, ls, lp, bar);
+                } else {
+                    pair_box(to, left, ls, m, lp, bar);
+                }
+                if (O::kRightAcross) {
+                    pair_box(to + kHalf, right, n, rs, rp, bar);
+                    pair_box(to + kHalf + 8192, right, n + 64, rs, rp, bar);
+                } else {
+                    pair_box(to + kHalf, right, rs, n, rp, bar);
+                }
+                if (++stage == kStages) {
+                    stage = 0;
+                    phase ^= 1u;
+                }
+            }
+        }
+    }
+}
+
+// The ninth warp's thread, in the first CTA.
+template <int FORM>
+__device__ __forceinline__ void issue(const Args& a, uint32_t tiles, char* smem, uint32_t memory, uint32_t bars, uint32_t* lost) {
+    using O = Order<FORM>;
+    const uint32_t mem = shared_address(smem);
+    const uint64_t left0 = operand(mem, O::kLeftAcross ? 8192 : 16), right0 = operand(mem + kHalf, O::kRightAcross ? 8192 : 16);
+    constexpr uint32_t kLeft = (O::kLeftAcross ? 2048 : 32) / 16, kRight = (O::kRightAcross ? 2048 : 32) / 16;  // to the next 16 of the sum
+    const uint32_t what = pair_instruction(!a.f16, O::kLeftAcross, O::kRightAcross);
+    int stage = 0;
+    uint32_t phase = 0, buffer = 0, drained = 3;  // a bit for each half of the tensor memory; nothing is to be drained at first
+    for (uint32_t t = blockIdx.x / 2; t < tiles; t += gridDim.x / 2) {
+        const Place p = place_of(a, t);
+        int k0, k1;
+        steps_of(a, p, k0, k1);
+        const int all = (k1 - k0) * a.pairs;
+        for (int done = 0; done < all;) {
+            const int end = min(done + kFlush, all);
+            if (!barrier_wait(bars + 8 * (kDrained + buffer), drained >> buffer & 1u, a.tries)) {
+                give_up(lost);
+                return;
+            }
+            drained ^= 1u << buffer;
+            fence_after();
+            for (bool onto = false; done < end; ++done) {
+                if (!barrier_wait(bars + 8 * (kFull + stage), phase, a.tries)) {
+                    give_up(lost);
+                    return;
+                }
+                fence_after();
+                const uint64_t l = left0 + (uint32_t)(stage * (kStage / 16)), r = right0 + (uint32_t)(stage * (kStage / 16));
+#pragma unroll
+                for (uint32_t q = 0; q < 4; ++q) {
+                    pair_product(memory + buffer * kTile, l + q * kLeft, r + q * kRight, what, onto);
+                    onto = true;
+                }
+                pair_done(bars + 8 * (kEmpty + stage));
+                if (++stage == kStages) {
+                    stage = 0;
+                    phase ^= 1u;
+                }
+            }
+            pair_done(bars + 8 * (kReady + buffer));
+            buffer ^= 1u;
+        }
+    }
+}
+
+// 32 rows of 128 bytes that a warp has in its staging, chunk c of row r at c ^ (r % 8), to memory. Row r goes to out + r * row (bytes);
+// rows: how many there are, bytes: of a row; fast: rows start on 16-byte boundaries and have whole chunks, else element by element.
+template <typename T, bool ADD>
+__device__ __forceinline__ void leave(const char* staging, char* out, int64_t row, int rows, int bytes, bool fast) {
+    const int lane = threadIdx.x & 31;
+    if (fast) {
+        const int c = lane & 7;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = i * 4 + (lane >> 3);
+            if (r < rows && c * 16 < bytes) {
+                uint4 v = *reinterpret_cast<const uint4*>(staging + swizzled(r, c));
+                uint4* to = reinterpret_cast<uint4*>(out + r * row + c * 16);
+                if (ADD) {
+                    const float4 was = *reinterpret_cast<const float4*>(to);
+                    v = make_uint4(__float_as_uint(__uint_as_float(v.x) + was.x), __float_as_uint(__uint_as_float(v.y) + was.y),
+                                   __float_as_uint(__uint_as_float(v.z) + was.z), __float_as_uint(__uint_as_float(v.w) + was.w));
+                }
+                *to = v;
+            }
+        }
+    } else {
+        constexpr int N = 128 / (int)sizeof(T);
+        for (int r = 0; r < rows; ++r)
+#pragma unroll
+            for (int e = lane; e < N; e += 32)
+                if (e * (int)sizeof(T) < bytes) {
+                    T v = *reinterpret_cast<const T*>(staging + swizzled(r, e * sizeof(T) / 16) + e * sizeof(T) % 16);
+                    T* to = reinterpret_cast<T*>(out + r * row) + e;
+                    if constexpr (ADD) v = v + *to;
+                    *to = v;
+                }
+    }
+}
+
+// Two values as one plane of the 16-bit type; what the plane leaves out stays in them.
+__device__ __forceinline__ uint32_t plane_of(float& a, float& b, bool f16, bool last) {
+    if (f16) return pack(a, b, __half());
+    if (last) return pack(a, b, __nv_bfloat16());
+    const uint32_t w = pack(a, b, __nv_bfloat16());
+    a -= __uint_as_float(w << 16);
+    b -= __uint_as_float(w & 0xffff0000u);
+    return w;
+}
+
+constexpr float kLog2e = 1.4426950408889634f;
+__device__ __forceinline__ float power2(float x) {  // within two units of the last place; 0 below 2^-126
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// fp16 holds d times this, so that probabilities down to 2^-38 are there; |d| <= 1.
+constexpr float kF16Scale = 16384.0f;
+
+// The first eight warps. A thread has row 32 (warp % 4) + lane of the CTA's 128 and 128 columns, from 128 (warp / 4) on.
+template <int FORM>
+__device__ __forceinline__ void finish(const Args& a, uint32_t tiles, char* staging0, uint32_t memory, uint32_t bars, uint32_t rank, uint32_t* given_up) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, half = warp >> 2;
+    const uint32_t at = memory + ((uint32_t)(warp & 3) << 21) + (uint32_t)half * 128;
+    const uint32_t drained0 = at_first(bars + 8 * kDrained);
+    char* staging = staging0 + warp * 4096;
+    uint32_t buffer = 0, ready = 0;  // a bit for each half of the tensor memory
+    bool lost = false;
+    for (uint32_t t = blockIdx.x / 2; t < tiles; t += gridDim.x / 2) {
+        const Place p = place_of(a, t);
+        int k0, k1;
+        steps_of(a, p, k0, k1);
+        const int all = (k1 - k0) * a.pairs;
+        float sum[128];
+        if (all <= 0)  // a part of the sum behind its end
+#pragma unroll
+            for (int c = 0; c < 128; ++c) sum[c] = 0.0f;
+        for (int done = 0; done < all; done += kFlush) {
+            lost = lost || !barrier_wait(bars + 8 * (kReady + buffer), ready >> buffer & 1u, a.tries);
+            ready ^= 1u << buffer;
+            __syncwarp();
+            fence_after();
+#pragma unroll
+            for (int c = 0; c < 128; c += 32) {
+                float v[32];
+                columns(at + buffer * kTile + c, v);
+                columns_wait(v);
+                if (done == 0) {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) sum[c + e] = v[e];
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) sum[c + e] += v[e];
+                }
+            }
+            fence_before();
+            __syncwarp();
+            if (lane == 0) arrive_at(drained0 + 8 * buffer);
+            buffer ^= 1u;
+        }
+        const int row0 = p.m * kTile + (int)rank * 128 + (warp & 3) * 32;  // of the warp, in the batch
+        const int64_t row = row0 + lane;
+        const int column0 = p.n * kTile + half * 128;  // in the piece, or of the result
+        const bool there = row < a.rows;
+        const float nan = __int_as_float(0x7fffffff);
+        if constexpr (FORM == kForward || FORM == kProbs) {
+            const int64_t number = (int64_t)p.batch * a.rows + row;
+            const int left = a.columns - (a.first + column0);  // columns from here on
+            const int64_t wanted_at = there ? a.target[number] - a.first - column0 : -1;
+            const int mine = wanted_at >= 0 && wanted_at < min(left, 128) ? (int)wanted_at : -1;
+            if constexpr (FORM == kForward) {
+                float top = __int_as_float(0xff800000);
+#pragma unroll
+                for (int c = 0; c < 128; ++c) top = fmaxf(top, c < left ? sum[c] : top);
+                const float base = top == __int_as_float(0xff800000) ? 0.0f : top;  // nothing but -inf here: a sum of 0
+                float total = 0.0f, wanted = 0.0f;
+#pragma unroll
+                for (int c = 0; c < 128; ++c) {
+                    total += c < left ? power2((sum[c] - base) * kLog2e) : 0.0f;
+                    if (c == mine) wanted = sum[c];
+                }
+                if (there && left > 0) {
+                    a.stats[((a.first + column0) >> 7) * a.all_rows + number] = lost ? make_float2(nan, nan) : make_float2(top, total);
+                    if (mine >= 0) a.target_logit[number] = wanted;
+                }
+            } else {
+                const float lse = there ? a.lse[number] : 0.0f, g = !there ? 0.0f : lost ? nan : a.row_gradient[number];
+                const float scale = a.f16 ? g * kF16Scale : g;
+#pragma unroll
+                for (int c = 0; c < 128; ++c) {
+                    const float d = power2((sum[c] - lse) * kLog2e) - (c == mine ? 1.0f : 0.0f);
+                    sum[c] = c < left && g != 0.0f ? d * scale : 0.0f;
+                }
+                for (int plane = 0; plane < a.probs_planes; ++plane) {
+                    const bool last = plane + 1 == a.probs_planes;
+#pragma unroll
+                    for (int part = 0; part < 2; ++part) {
+                        __syncwarp();
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) {
+                            uint32_t w[4];
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) {
+                                const int e = part * 64 + c * 8 + q * 2;
+                                w[q] = plane_of(sum[e], sum[e + 1], a.f16, last);
+                            }
+                            *reinterpret_cast<uint4*>(staging + swizzled(lane, c)) = make_uint4(w[0], w[1], w[2], w[3]);
+                        }
+                        __syncwarp();
+                        const int64_t first = (int64_t)p.batch * a.rows + row0;
+                        const int rows = (int)min((int64_t)32, a.rows - row0);
+                        char* out = reinterpret_cast<char*>(a.probs + plane * a.probs_plane + first * a.width + column0 + part * 64);
+                        leave<uint16_t, false>(staging, out, (int64_t)a.width * 2, rows, 128, true);
+                    }
+                }
+            }
+        } else {
+            float scale = 1.0f;
+            if (a.row_scale) {
+                if (FORM == kInput) scale = there ? a.row_scale[(int64_t)p.batch * a.rows + row] : 0.0f;
+                else scale = a.row_scale[p.batch * a.scale_batch];
+            }
+            if (lost) scale = nan;
+            const int rows = (int)min((int64_t)32, a.rows - row0), left = a.columns - column0;
+            const int size = a.out_type == kTypeF32 ? 4 : 2;
+            char* out = static_cast<char*>(a.out) + (p.part * a.out_part + p.batch * a.out_batch + row0 * a.out_row + column0) * size;
+            const bool fast = ((reinterpret_cast<uintptr_t>(a.out) | (uint64_t)(a.out_part * size) | (uint64_t)(a.out_batch * size) |
+                                (uint64_t)(a.out_row * size) | (uint64_t)((int64_t)a.columns * size)) & 15u) == 0;
+            if (a.out_type == kTypeF32) {
+#pragma unroll
+                for (int part = 0; part < 4; ++part) {
+                    __syncwarp();
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) {
+                        const float* v = &sum[part * 32 + c * 4];
+                        *reinterpret_cast<float4*>(staging + swizzled(lane, c)) = make_float4(scale * v[0], scale * v[1], scale * v[2], scale * v[3]);
+                    }
+                    __syncwarp();
+                    const int bytes = (left - part * 32) * 4;
+                    if (a.add) leave<float, true>(staging, out + part * 128, a.out_row * 4, rows, bytes, fast);
+                    else leave<float, false>(staging, out + part * 128, a.out_row * 4, rows, bytes, fast);
+                }
+            } else {
+#pragma unroll
+                for (int part = 0; part < 2; ++part) {
+                    __syncwarp();
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const float x = scale * sum[part * 64 + c * 8 + q * 2], y = scale * sum[part * 64 + c * 8 + q * 2 + 1];
+                            w[q] = a.out_type == kTypeBF16 ? pack(x, y, __nv_bfloat16()) : pack(x, y, __half());
+                        }
+                        *reinterpret_cast<uint4*>(staging + swizzled(lane, c)) = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                    __syncwarp();
+                    leave<uint16_t, false>(staging, out + part * 128, a.out_row * 2, rows, (left - part * 64) * 2, fast);
+                }
+            }
+        }
+    }
+    if (lost) give_up(given_up);
+}
+
+template <int FORM>
+__global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap left,
+                                                           const __grid_constant__ CUtensorMap right) {
+    extern __shared__ __align__(16) char dynamic[];
+    __shared__ uint64_t barriers[kBars];
+    __shared__ uint32_t word[2];  // the tensor memory's address; whether someone gave up
+    char* smem = dynamic + ((1024u - (shared_address(dynamic) & 1023u)) & 1023u);
+    const uint32_t bars = shared_address(barriers), rank = cta_rank();
+    if (threadIdx.x < 32) pair_alloc(shared_address(word));
+    if (threadIdx.x == 32) {
+        word[1] = 0u;
+        for (int k = 0; k < kBars; ++k) barrier_init(bars + 8 * k, k >= kDrained && k < kStopped ? 16u : 1u);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_shared();
+    }
+    fence_before();
+    __syncthreads();
+    cluster_sync();
+    fence_after();
+    const uint32_t memory = word[0];
+    const uint32_t tiles = (uint32_t)a.tiles_m * a.tiles_n * a.batches * a.parts;
+    dependency_wait();
+    if (threadIdx.x < 256) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSumRegisters));
+        finish<FORM>(a, tiles, smem + kStages * kStage, memory, bars, rank, word + 1);
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegisters));
+        if (threadIdx.x == 256 && rank == 0) issue<FORM>(a, tiles, smem, memory, bars, word + 1);
+        else if (threadIdx.x == 288) bring<FORM>(a, &left, &right, tiles, smem, bars, rank, word + 1);
+    }
+    __syncwarp();
+    fence_before();
+    __syncthreads();
+    if (word[1]) {
+        // products and copies may be under way that nobody waited for: the products are waited for, with a limit, and the copies are given
+        // a millisecond, a hundred times what they take
+        if (threadIdx.x == 256 && rank == 0) {
+            pair_done(bars + 8 * kStopped);
+            barrier_wait(bars + 8 * kStopped, 0, kTries);
+        }
+        if (threadIdx.x == 288)
+            for (int k = 0; k < 1000; ++k) __nanosleep(1000);
+        __syncwarp();
+        __syncthreads();
+    }
+    cluster_sync();  // the other CTA's barriers and tensor memory are used until here
+    fence_after();
+    if (threadIdx.x < 32) pair_free(memory);
+}
+
+}  // namespace head
+}  // namespace
+}  // namespace compams

@@ -662,12 +662,6 @@ struct Shape {
     }
 };
 
-int multiprocessors() {
-    int device = 0, sms = 148;
-    if (cudaGetDevice(&device) == cudaSuccess) cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
-    cudaGetLastError();
-    return sms;
-}
 // CTAs of a kernel that an SM holds at once. Asked once for every kernel and device.
 template <auto kernel>
 cudaError_t resident(int threads, int shared, int* count) {

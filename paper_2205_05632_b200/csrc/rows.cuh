@@ -322,6 +322,13 @@ inline bool make_drop(Drop& d, double p, uint64_t seed, uint32_t call, const int
 
 enum : int32_t { kTypeF32 = 0, kTypeBF16 = 1, kTypeF16 = 2 };
 
+inline int multiprocessors() {
+    int device = 0, sms = 148;
+    if (cudaGetDevice(&device) == cudaSuccess) cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
+    cudaGetLastError();
+    return sms;
+}
+
 inline int type_bytes(int32_t type) { return type == kTypeF32 ? 4 : 2; }
 inline bool type_known(int32_t type) { return type >= kTypeF32 && type <= kTypeF16; }
 

@@ -426,3 +426,107 @@ def low_rank_adapter(x: torch.Tensor, base: Optional[torch.Tensor], A: torch.Ten
     if _through_autograd(x, base, A, B):
         return _AdapterFunction.apply(x, base, A, B, scale, drop)
     return _adapter_forward(x, base, A, B, scale, drop)[0]
+
+
+# ---- the head: cross entropy over a vocabulary -----------------------------------------------------------------------------
+
+_REDUCTIONS = {"none": 0, "mean": 1, "sum": 2}
+
+
+def _as_it_lies(p: int, h: int, rows: int, row_stride: int, batches: int, batch_stride: int) -> bool:
+    """Whether TMA can read 16-bit rows where they are."""
+    return (p % 16 == 0 and (rows == 1 or (row_stride % 8 == 0 and row_stride >= h))
+            and (batches == 1 or (batch_stride % 8 == 0 and batch_stride >= 1)))
+
+
+class _Head:
+    """x, weight and target of a call as the library takes them."""
+    __slots__ = ("x", "weight", "rows", "shape", "strides", "copied", "shared", "reduction", "ignored")
+
+    def __init__(self, x, weight, reduction, ignored):
+        n, h, vocab = x.shape[0], x.shape[-1], weight.shape[-2]
+        self.x, self.rows, ws, rs = _rows(x)
+        self.weight, self.reduction, self.ignored = weight, reduction, ignored
+        wws = weight.stride(0) if weight.dim() == 3 and n > 1 else 0
+        self.shared = wws == 0
+        self.strides = (ws, rs, wws, weight.stride(-2))
+        self.shape = (n, self.rows, h, vocab)
+        x_copied = w_copied = True
+        if x.dtype == weight.dtype and x.dtype != torch.float32:
+            if self.shared:
+                stride = ws if self.rows == 1 else rs
+                x_copied = not ((self.rows == 1 or n == 1 or ws == self.rows * rs)
+                                and _as_it_lies(self.x.data_ptr(), h, n * self.rows, stride, 1, 0))
+            else:
+                x_copied = not _as_it_lies(self.x.data_ptr(), h, self.rows, rs, n, ws)
+            w_copied = not _as_it_lies(weight.data_ptr(), h, vocab, weight.stride(-2), 1 if self.shared else n, wws)
+        self.copied = (int(x_copied), int(w_copied))
+
+    def workspace(self, wanted: int) -> torch.Tensor:
+        return _workspace("compams_head_workspace_bytes", self.x, *self.shape, _TYPES[self.x.dtype], _TYPES[self.weight.dtype],
+                          int(self.shared), *self.copied, wanted)
+
+
+def _head_forward(x, weight, target, reduction, ignored):
+    lse = x.new_empty(target.shape, dtype=torch.float32)
+    make = x.new_empty if x.numel() else x.new_zeros
+    loss = make(target.shape if reduction == 0 else x.shape[:1], dtype=torch.float32)
+    if x.numel():
+        z = _Head(x, weight, reduction, ignored)
+        work = z.workspace(0)
+        _run("compams_head_forward", x.device, loss.data_ptr(), lse.data_ptr(), z.x.data_ptr(), _TYPES[x.dtype], weight.data_ptr(),
+             _TYPES[weight.dtype], target.data_ptr(), *z.shape, *z.strides, ignored, reduction, work.data_ptr(), work.numel())
+    return loss, lse
+
+
+class _HeadFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, target, reduction, ignored):
+        loss, lse = _head_forward(x, weight, target, reduction, ignored)
+        ctx.save_for_backward(x, weight, target, lse)
+        ctx.reduction, ctx.ignored = reduction, ignored
+        return loss
+
+    @staticmethod
+    @_once
+    def backward(ctx, dloss):
+        x, weight, target, lse = ctx.saved_tensors
+        needs_x, needs_w = ctx.needs_input_grad[:2]
+        dx = _empty(x) if needs_x else None
+        dw = (weight.new_empty if x.numel() else weight.new_zeros)(weight.shape) if needs_w else None
+        if x.numel() and (needs_x or needs_w):
+            z = _Head(x, weight, ctx.reduction, ctx.ignored)
+            g = dloss.resolve_neg()
+            g = g if ctx.reduction else g.reshape(x.shape[0], -1)
+            work = z.workspace((1 if needs_x else 0) + (2 if needs_w else 0))
+            _run("compams_head_backward", x.device, _ptr(dx), _ptr(dw), 1 if weight.dim() == 2 else 0, g.data_ptr(), g.stride(0),
+                 0 if ctx.reduction else g.stride(1), z.x.data_ptr(), _TYPES[x.dtype], weight.data_ptr(), _TYPES[weight.dtype],
+                 target.data_ptr(), lse.data_ptr(), *z.shape, *z.strides, ctx.ignored, ctx.reduction, work.data_ptr(), work.numel())
+        return dx, dw, None, None, None
+
+
+def linear_cross_entropy(x: torch.Tensor, weight: torch.Tensor, target: torch.Tensor, reduction: str = "mean",
+                         ignore_index: int = -100) -> torch.Tensor:
+    """Softmax cross entropy of the logits x W^T with target, without the logits in memory as a whole: x is [n, ..., h], weight, which
+    has x's type or float32, [vocab, h] for all workers or [n, vocab, h], target int64 [n, ...]. float32 results: "mean", [n], is over
+    each worker's targets that are not ignore_index (0 where all are), "sum", [n], and "none", [n, ...], where an ignored target has 0.
+    A target outside the vocabulary makes the loss NaN, and with it the gradients that it reaches.
+
+    A float32 weight is taken as it is, in three products of bfloat16 for one (six where x is float32); a 16-bit weight in one."""
+    _activation(x)
+    if reduction not in _REDUCTIONS:
+        raise CompAMSError("reduction must be one of %s: got %r" % (sorted(_REDUCTIONS), reduction))
+    n, h = x.shape[0], x.shape[-1]
+    if (not isinstance(weight, torch.Tensor) or weight.device != x.device or weight.dtype not in (x.dtype, torch.float32)
+            or weight.dim() not in (2, 3) or weight.shape[-1] != h or weight.shape[-2] < 1 or (weight.dim() == 3 and weight.shape[0] != n)):
+        raise CompAMSError("weight must be [vocab, %d] or [%d, vocab, %d] of type %s or float32 on %s" % (h, n, h, x.dtype, x.device))
+    if not isinstance(target, torch.Tensor) or target.device != x.device or target.dtype != torch.int64 or target.shape != x.shape[:-1]:
+        raise CompAMSError("target must be an int64 tensor %s on %s" % (list(x.shape[:-1]), x.device))
+    if not -(1 << 63) <= int(ignore_index) < 1 << 63:
+        raise CompAMSError("ignore_index must be a 64-bit number")
+    if weight.is_neg():
+        weight = weight.resolve_neg()
+    if weight.stride(-1) != 1 and h > 1:
+        weight = weight.contiguous()
+    args = (x, weight, target.contiguous(), _REDUCTIONS[reduction], int(ignore_index))
+    return _HeadFunction.apply(*args) if _through_autograd(x, weight) else _head_forward(*args)[0]
