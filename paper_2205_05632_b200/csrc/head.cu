@@ -16,8 +16,11 @@
 // Precision. Products of 16-bit numbers of one type are exact and their sums fp32. Beside an fp32 weight everything is bf16 planes: an fp32
 // number is three (each the rest of those before it, rounded), fp16 two; pairs of planes i + j <= 2 are formed, which leaves out at most
 // 2^-24 of a product. d is one plane (2^-9 of it at most left out) where the result has 8 bits, two for fp16 beside an fp32 weight, three
-// for an fp32 result; fp16 products take it in fp16, relative to the largest |g| rounded up to a power of two, as g may be a loss scale
-// or a ten-thousandth. For dx of 8 bits beside an fp32 weight two planes of W are taken. No atomics: results do not change from run to run.
+// for an fp32 result. The rows' factors g are taken relative to their worker's: a mean's and a sum's g, the same for all rows of a worker,
+// stays out of d altogether and joins in fp32, so that d of the target, p - 1, is not rounded the same way in every row (8192 rows,
+// 100000 columns: 2.9e-3 off with g inside, 2.2e-3 now, of which rounding the result is 1.7e-3); without a reduction it is taken relative
+// to a power of two above the largest, as fp16 could not hold a loss scale or a ten-thousandth. For dx of 8 bits beside an fp32 weight two
+// planes of W are taken. No atomics: results do not change from run to run.
 #include <string.h>
 
 #include <algorithm>
@@ -271,24 +274,21 @@ struct RowsArgs {
     int64_t ws, rs;  // of dloss; rs counts without a reduction alone
     const int64_t* target;
     int64_t rows, ignored;
-    int32_t n, reduction, relative, together;
-    float2* worker;       // [n]: what g is multiplied by, the largest |g|
-    float *g, *scale;     // [all rows]
+    int32_t n, reduction, f16;
+    float *g, *scale;     // [all rows], [n]
 };
-__device__ __forceinline__ float row_gradient(const RowsArgs& a, int64_t worker, int64_t row, float factor) {
-    if (a.target[worker * a.rows + row] == a.ignored) return 0.0f;
-    return factor * a.dloss[worker * a.ws + (a.reduction == kNone ? row * a.rs : 0)];
-}
-// A CTA per worker: its counted rows, and the largest |g| of them.
-__global__ void __launch_bounds__(256) worker_kernel(const __grid_constant__ RowsArgs a) {
+// A CTA per worker: its rows' g relative to the worker's scale.
+__global__ void __launch_bounds__(256) rows_kernel(const __grid_constant__ RowsArgs a) {
     __shared__ float counts[8], tops[8];
     dependency_wait();
     const int64_t i = blockIdx.x;
+    const int64_t* target = a.target + i * a.rows;
+    const float* dloss = a.dloss + i * a.ws;
     float count = 0.0f, top = 0.0f;
     for (int64_t j = threadIdx.x; j < a.rows; j += 256)
-        if (a.target[i * a.rows + j] != a.ignored) {
+        if (target[j] != a.ignored) {
             count += 1.0f;
-            top = fmaxf(top, fabsf(a.dloss[i * a.ws + (a.reduction == kNone ? j * a.rs : 0)]));
+            if (a.reduction == kNone) top = fmaxf(top, fabsf(dloss[j * a.rs]));
         }
     count = sum_of_warp(count);
 #pragma unroll
@@ -298,33 +298,25 @@ __global__ void __launch_bounds__(256) worker_kernel(const __grid_constant__ Row
         tops[threadIdx.x >> 5] = top;
     }
     __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int w = 1; w < 8; ++w) {
-            count += counts[w];
-            top = fmaxf(top, tops[w]);
-        }
-        const float factor = a.reduction == kMean ? 1.0f / fmaxf(count, 1.0f) : 1.0f;
-        a.worker[i] = make_float2(factor, factor * top);
+    count = top = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) {
+        count += counts[w];
+        top = fmaxf(top, tops[w]);
     }
-}
-// g of every row; relative: to a power of two that no |g| of the worker (together: of all) is above, whose 2^-14th is the row's scale.
-__global__ void __launch_bounds__(256) rows_kernel(const __grid_constant__ RowsArgs a) {
-    dependency_wait();
-    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (at >= a.n * a.rows) return;
-    const int64_t i = at / a.rows;
-    float g = row_gradient(a, i, at - i * a.rows, a.worker[i].x);
-    if (a.relative) {
-        float top = a.worker[i].y;
-        if (a.together)
-            for (int k = 0; k < a.n; ++k) top = fmaxf(top, a.worker[k].y);
+    float scale = 1.0f, inverse = 1.0f;
+    if (a.reduction == kNone) {
         int e = 0;
         if (top > 0.0f && top < kInf) frexpf(top, &e);
-        e = max(e, -100);  // (2^-e is finite; below, g is 0 but for rounding)
-        g = ldexpf(g, -e);
-        a.scale[at] = ldexpf(1.0f / head::kF16Scale, e);
+        e = max(e, -100);  // 2^-e is finite
+        scale = ldexpf(1.0f, e);
+        inverse = ldexpf(1.0f, -e);
+    } else {
+        scale = a.reduction == kMean ? dloss[0] / fmaxf(count, 1.0f) : dloss[0];
     }
-    a.g[at] = g;
+    if (threadIdx.x == 0) a.scale[i] = a.f16 ? scale * (1.0f / head::kF16Scale) : scale;
+    for (int64_t j = threadIdx.x; j < a.rows; j += 256)
+        a.g[i * a.rows + j] = target[j] == a.ignored ? 0.0f : a.reduction == kNone ? inverse * dloss[j * a.rs] : 1.0f;
 }
 
 // dx from the parts' sums.
@@ -332,7 +324,8 @@ struct PartsArgs {
     const float* parts;  // [parts][all rows][pitch]
     int64_t part, all_rows, chunks;
     int32_t count, h, per_row, pitch;
-    const float* scale;  // of a row; may be null
+    const float* scale;  // of a worker
+    int64_t worker_rows;
     void* out;           // [all rows][h]
 };
 template <typename T, bool VEC>
@@ -349,7 +342,7 @@ __global__ void __launch_bounds__(256) parts_kernel(const __grid_constant__ Part
         v[0] += p.x; v[1] += p.y; v[2] += p.z; v[3] += p.w;
         v[4] += q.x; v[5] += q.y; v[6] += q.z; v[7] += q.w;
     }
-    const float scale = a.scale ? a.scale[row] : 1.0f;
+    const float scale = a.scale[row / a.worker_rows];
 #pragma unroll
     for (int k = 0; k < 8; ++k) v[k] *= scale;
     T* out = (T*)a.out + row * a.h + c;
@@ -426,7 +419,7 @@ struct Plan {
     int64_t width;          // columns of d
     int32_t probs, parts;   // planes of d; parts of the vocabulary's sum of dx
     bool sums;              // dx is added up in fp32
-    int64_t x_copy, w_copy, stats, stat_parts, target_logit, row_loss, worker, g, scale, d, dx_sums, bytes;
+    int64_t x_copy, w_copy, stats, stat_parts, target_logit, row_loss, g, scale, d, dx_sums, bytes;
 };
 constexpr int64_t kCopyBytes = 64ll << 20;   // of a piece's copy of W: it stays in the L2 between its writing and its reading
 constexpr int64_t kProbsBytes = 512ll << 20;  // of a piece's d
@@ -485,9 +478,8 @@ Plan plan_of(const HeadShape& z, bool x_copied, bool w_copied, int wanted) {  //
         p.target_logit = take(m * 4);
         p.row_loss = take(m * 4);
     } else {
-        p.worker = take(z.n * 8);
         p.g = take(m * 4);
-        p.scale = take(m * 4);
+        p.scale = take(z.n * 4);
         p.d = take(p.probs * m * p.width * 2);
         p.parts = wanted & 1 ? parts_of(z, (p.piece + 63) / 64, z.x_probs() == 3 ? 6 : z.x_probs() == 2 ? 3 : z.copies() ? 2 : 1) : 1;
         p.sums = (wanted & 1) && (p.parts > 1 || p.pieces > 1);
@@ -681,7 +673,7 @@ int compams_head_forward(float* loss, float* lse, const void* x, int32_t type, c
             if (rc != COMPAMS_OK) break;
             a.tiles_m = (int32_t)((z.batch_rows() + 255) / 256); a.tiles_n = (int32_t)((count + 255) / 256);
             a.batches = (int32_t)z.batches(); a.parts = 1;
-            a.steps = a.part_steps = (int32_t)((h + 63) / 64);
+            a.segments = 1; a.steps = a.part_steps = (int32_t)((h + 63) / 64);
             pairs_of(a, z.x_planes(), z.w_planes(), 2);
             a.rows = z.batch_rows(); a.columns = (int32_t)vocab; a.first = (int32_t)v0;
             a.target = target; a.target_logit = target_logit; a.stats = stats; a.all_rows = z.all_rows();
@@ -732,14 +724,11 @@ int compams_head_backward(void* dx, void* dweight, int32_t sum_workers, const fl
     const int64_t all = z.all_rows();
     RowsArgs r = {};
     r.dloss = dloss; r.ws = dloss_worker_stride; r.rs = dloss_row_stride; r.target = target; r.rows = rows; r.ignored = ignored; r.n = n;
-    r.reduction = reduction; r.relative = z.f16(); r.together = together && dweight; r.worker = (float2*)(work + p.worker);
-    r.g = (float*)(work + p.g); r.scale = (float*)(work + p.scale);
-    int rc = launched(launch_sized(worker_kernel, dim3((uint32_t)n), 256, 1, 0, true, stream, r), "head_worker");
-    if (rc == COMPAMS_OK)
-        rc = launched(launch_sized(rows_kernel, dim3((uint32_t)((all + 255) / 256)), 256, 1, 0, false, stream, r), "head_rows");
+    r.reduction = reduction; r.f16 = z.f16(); r.g = (float*)(work + p.g); r.scale = (float*)(work + p.scale);
+    int rc = launched(launch_sized(rows_kernel, dim3((uint32_t)n), 256, 1, 0, true, stream, r), "head_rows");
     Operand xo, wo;
     if (rc == COMPAMS_OK) rc = x_operand(z, x, x_worker_stride, x_row_stride, p, work, xo, stream);
-    const float* scale = z.f16() ? r.scale : nullptr;
+    const float* scale = r.scale;
     uint16_t* d = (uint16_t*)(work + p.d);
     const int32_t tiles_h = (int32_t)((h + 255) / 256), tiles_rows = (int32_t)((z.batch_rows() + 255) / 256);
     for (int64_t v0 = 0; v0 < vocab && rc == COMPAMS_OK; v0 += p.piece) {
@@ -750,7 +739,7 @@ int compams_head_backward(void* dx, void* dweight, int32_t sum_workers, const fl
         {
             head::Args a = {};
             a.tiles_m = tiles_rows; a.tiles_n = (int32_t)((count + 255) / 256); a.batches = (int32_t)z.batches(); a.parts = 1;
-            a.steps = a.part_steps = (int32_t)((h + 63) / 64);
+            a.segments = 1; a.steps = a.part_steps = (int32_t)((h + 63) / 64);
             pairs_of(a, z.x_planes(), z.w_planes(), 2);
             a.right_row = first; a.rows = z.batch_rows(); a.columns = (int32_t)vocab; a.first = (int32_t)v0; a.target = target;
             a.all_rows = all; a.lse = lse; a.row_gradient = r.g; a.probs = d; a.probs_plane = all * p.width; a.width = (int32_t)p.width;
@@ -761,7 +750,7 @@ int compams_head_backward(void* dx, void* dweight, int32_t sum_workers, const fl
         if (rc == COMPAMS_OK && dx) {
             head::Args a = {};
             a.tiles_m = tiles_rows; a.tiles_n = tiles_h; a.batches = (int32_t)z.batches(); a.parts = p.parts;
-            a.steps = (int32_t)((count + 63) / 64); a.part_steps = (a.steps + p.parts - 1) / p.parts;
+            a.segments = 1; a.steps = (int32_t)((count + 63) / 64); a.part_steps = (a.steps + p.parts - 1) / p.parts;
             // 8 bits beside an fp32 weight: two of its planes; 11 bits: to the same order
             pairs_of(a, z.x_probs(), z.copies() && type != kTypeF32 ? 2 : z.w_planes(), type == kTypeF32 ? 2 : 1);
             a.right_sum = first; a.rows = z.batch_rows();
@@ -769,32 +758,31 @@ int compams_head_backward(void* dx, void* dweight, int32_t sum_workers, const fl
                 a.out = work + p.dx_sums; a.out_type = kTypeF32; a.out_row = z.pitch(); a.columns = (int32_t)z.pitch();
                 a.out_part = all * z.pitch(); a.add = v0 > 0;
             } else {
-                a.out = dx; a.out_type = type; a.out_row = h; a.columns = (int32_t)h; a.row_scale = scale;
+                a.out = dx; a.out_type = type; a.out_row = h; a.columns = (int32_t)h; a.scale = scale; a.worker_rows = rows;
             }
             a.out_batch = z.batch_rows() * a.out_row;
             rc = product<head::kInput>(a, by_batch, wo, z.f16(), stream, "head_input");
         }
         if (rc == COMPAMS_OK && dweight) {
-            // together: one sum over all workers' rows; else a batch for every worker
-            const int64_t batches = together ? 1 : n, sum = together ? all : rows;
+            // together: the workers are segments of one sum; else each is a batch
             head::Args a = {};
-            a.tiles_m = (int32_t)((count + 255) / 256); a.tiles_n = tiles_h; a.batches = (int32_t)batches; a.parts = 1;
-            a.steps = a.part_steps = (int32_t)((sum + 63) / 64);
+            a.tiles_m = (int32_t)((count + 255) / 256); a.tiles_n = tiles_h; a.batches = together ? 1 : n; a.parts = 1;
+            a.segments = together ? n : 1; a.steps = a.part_steps = (int32_t)((rows + 63) / 64);
             pairs_of(a, z.w_probs(), z.x_planes(), 2);
             a.rows = count; a.columns = (int32_t)h; a.out_type = weight_type; a.out_row = h; a.out_batch = vocab * h;
             a.out = (char*)dweight + v0 * h * type_bytes(weight_type);
-            a.row_scale = scale; a.scale_batch = together ? 0 : rows;
-            const Operand left{d, p.width, sum, batches, p.probs, p.width, sum * p.width};
+            a.scale = scale;
+            const Operand left{d, p.width, rows, n, p.probs, p.width, rows * p.width};
             Operand right = xo;
-            right.rows = sum; right.batches = batches;
-            if (z.shared) right.batch_stride = sum * (all > 1 ? xo.row_stride : z.pitch());
+            right.rows = rows; right.batches = n;
+            if (z.shared) right.batch_stride = rows * (all > 1 ? xo.row_stride : z.pitch());
             rc = product<head::kWeight>(a, left, right, z.f16(), stream, "head_weight");
         }
     }
     if (rc != COMPAMS_OK || !p.sums || !dx) return rc;
     PartsArgs a = {};
     a.parts = (const float*)(work + p.dx_sums); a.part = all * z.pitch(); a.all_rows = all; a.count = p.parts; a.h = (int32_t)h;
-    a.per_row = (int32_t)(z.pitch() / 8); a.pitch = (int32_t)z.pitch(); a.chunks = all * a.per_row; a.scale = scale; a.out = dx;
+    a.per_row = (int32_t)(z.pitch() / 8); a.pitch = (int32_t)z.pitch(); a.chunks = all * a.per_row; a.scale = scale; a.worker_rows = rows; a.out = dx;
     const int64_t ctas = (a.chunks + 255) / 256;
     if (ctas > 0x7fffffff) return COMPAMS_ERR_TOO_LARGE;
     const bool vec = h % 8 == 0 && (reinterpret_cast<uintptr_t>(dx) & 15u) == 0;

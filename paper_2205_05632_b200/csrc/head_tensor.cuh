@@ -52,7 +52,9 @@ constexpr int kFull = 0, kEmpty = kStages, kReady = 2 * kStages, kDrained = kRea
 struct Args {
     // the tiles, in this order: batch, part of the sum, row and column in groups of kRaster rows
     int32_t tiles_m, tiles_n, batches, parts;
-    int32_t steps, part_steps;  // tiles of 64 along the sum: of a batch, and of a part
+    // tiles of 64 along the sum: of a segment, and of a part. WEIGHT of all workers together: a worker's rows are a segment; else there is
+    // one. A stretch ends with its segment.
+    int32_t segments, steps, part_steps;
     // operands: the third coordinate is plane * planes apart + batch * batch apart; where rows and the sum begin
     int32_t pairs;
     uint8_t left_plane[kMostPairs], right_plane[kMostPairs];
@@ -76,8 +78,8 @@ struct Args {
     void* out;             // fp32, or of out_type where it is final
     int64_t out_part, out_batch, out_row;  // elements from part to part, batch to batch, row to row
     int32_t out_type, add;                 // add: onto what is there (fp32)
-    const float* row_scale;                // INPUT: of a row, WEIGHT: of a batch's first row; null: 1
-    int64_t scale_batch;                   // WEIGHT: rows from batch to batch
+    const float* scale;                    // of a worker; null: 1
+    int64_t worker_rows;
 };
 
 constexpr int kRaster = 8;
@@ -169,9 +171,9 @@ __device__ __forceinline__ void bring(const Args& a, const CUtensorMap* left, co
         int k0, k1;
         steps_of(a, p, k0, k1);
         const int m = a.left_row + p.m * kTile + (int)rank * 128, n = a.right_row + p.n * kTile + (int)rank * 128;
-        const int lz = p.batch * a.left_batch, rz = p.batch * a.right_batch;
-        for (int k = k0; k < k1; ++k) {
+        for (int segment = 0, k = k0; segment < a.segments && k < k1; k + 1 < k1 ? ++k : (k = k0, ++segment)) {
             const int ls = a.left_sum + k * 64, rs = a.right_sum + k * 64;
+            const int lz = (p.batch + segment) * a.left_batch, rz = (p.batch + segment) * a.right_batch;
             for (int pair = 0; pair < a.pairs; ++pair) {
                 if (!barrier_wait(bars + 8 * (kEmpty + stage), phase, a.tries)) {
                     give_up(lost);
@@ -216,7 +218,7 @@ __device__ __forceinline__ void issue(const Args& a, uint32_t tiles, char* smem,
         int k0, k1;
         steps_of(a, p, k0, k1);
         const int all = (k1 - k0) * a.pairs;
-        for (int done = 0; done < all;) {
+        for (int segment = 0, done = 0; segment < a.segments && all > 0; done < all ? 0 : (done = 0, ++segment)) {
             const int end = min(done + kFlush, all);
             if (!barrier_wait(bars + 8 * (kDrained + buffer), drained >> buffer & 1u, a.tries)) {
                 give_up(lost);
@@ -299,7 +301,7 @@ __device__ __forceinline__ float power2(float x) {  // within two units of the l
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// fp16 holds d times this, so that probabilities down to 2^-38 are there; |d| <= 1.
+// fp16 holds d times this, so that probabilities down to 2^-38 are there; |d| <= 1. (The workers' scales have its inverse.)
 constexpr float kF16Scale = 16384.0f;
 
 // The first eight warps. A thread has row 32 (warp % 4) + lane of the CTA's 128 and 128 columns, from 128 (warp / 4) on.
@@ -320,7 +322,8 @@ __device__ __forceinline__ void finish(const Args& a, uint32_t tiles, char* stag
         if (all <= 0)  // a part of the sum behind its end
 #pragma unroll
             for (int c = 0; c < 128; ++c) sum[c] = 0.0f;
-        for (int done = 0; done < all; done += kFlush) {
+        for (int segment = 0, done = 0; segment < a.segments && all > 0; done + kFlush < all ? done += kFlush : (done = 0, ++segment)) {
+            const float worth = FORM == kWeight && a.scale ? a.scale[p.batch + segment] : 1.0f;
             lost = lost || !barrier_wait(bars + 8 * (kReady + buffer), ready >> buffer & 1u, a.tries);
             ready ^= 1u << buffer;
             __syncwarp();
@@ -330,7 +333,10 @@ __device__ __forceinline__ void finish(const Args& a, uint32_t tiles, char* stag
                 float v[32];
                 columns(at + buffer * kTile + c, v);
                 columns_wait(v);
-                if (done == 0) {
+                if (FORM == kWeight) {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) sum[c + e] = done + segment == 0 ? worth * v[e] : fmaf(worth, v[e], sum[c + e]);
+                } else if (done == 0) {
 #pragma unroll
                     for (int e = 0; e < 32; ++e) sum[c + e] = v[e];
                 } else {
@@ -401,10 +407,7 @@ __device__ __forceinline__ void finish(const Args& a, uint32_t tiles, char* stag
             }
         } else {
             float scale = 1.0f;
-            if (a.row_scale) {
-                if (FORM == kInput) scale = there ? a.row_scale[(int64_t)p.batch * a.rows + row] : 0.0f;
-                else scale = a.row_scale[p.batch * a.scale_batch];
-            }
+            if (FORM == kInput && a.scale) scale = there ? a.scale[((int64_t)p.batch * a.rows + row) / a.worker_rows] : 0.0f;
             if (lost) scale = nan;
             const int rows = (int)min((int64_t)32, a.rows - row0), left = a.columns - column0;
             const int size = a.out_type == kTypeF32 ? 4 : 2;
