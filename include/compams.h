@@ -422,6 +422,30 @@ int compams_blocksign_sweep_static_limits(int64_t* max_workers, int64_t* max_til
  */
 int compams_collect(float* row, const float* const* tensors, const int64_t* offsets, int32_t count, void* cuda_stream);
 
+enum compams_type { COMPAMS_F32 = 0, COMPAMS_BF16 = 1, COMPAMS_F16 = 2 };
+
+/*
+ * compams_collect_workers - all n workers' gradients, one tensor per parameter with a worker in each row, gathered as the rows of the
+ * [n, d] gradient buffer; each worker's global norm over all its tensors; rows above max_norm scaled to it:
+ *   norm_i = sqrt(sum g^2), G_i = min(1, max_norm / (norm_i + eps)) g_i (an infinite norm's factor is 0, that of no number none).
+ *
+ *   rows         device; fp32, worker i's row at i * row_stride (at least offsets[count] elements); coordinates offsets[0] ...
+ *                offsets[count] - 1 of each are written. Null: the tensors are scaled where they lie, in their own type.
+ *   norms        device; [n] fp32, receives the norms as they were; may be null: not wanted.
+ *   tensors      host; count DEVICE pointers; tensor k's elements of worker i are packed from i * strides[k] elements on, aligned to
+ *                their element. Null: no gradient, zeros. They may not overlap rows.
+ *   types        host; compams_type of each tensor.
+ *   offsets      host; count + 1 entries, offsets[0] >= 0, strictly increasing. All host arrays are read during the call.
+ *   max_norm     infinity: nothing is scaled. A row whose factor is 1 is copied bit for bit (in place: not touched).
+ *   workspace    device, 8-byte aligned, at least compams_collect_workers_workspace_bytes; used during the call's device work only. Not
+ *                needed where norms is null and max_norm infinity.
+ * Sums run in a fixed order, in binary64 beyond four elements. Errors: INVALID_ARG, TOO_LARGE, CUDA.
+ */
+int compams_collect_workers(float* rows, int64_t row_stride, float* norms, const void* const* tensors, const int64_t* strides,
+                            const int32_t* types, const int64_t* offsets, int32_t count, int32_t n, double max_norm, double eps, void* workspace,
+                            size_t workspace_bytes, void* cuda_stream);
+int compams_collect_workers_workspace_bytes(size_t* bytes, int32_t n, int32_t count);
+
 /*
  * Operators for the layers of a model whose n workers' micro-batches run as one batch: activations are [n, rows, h] with the worker on
  * the leading axis, and a weight's gradient stays apart by worker, as the rows of the gradient buffer that compams_step takes.
@@ -439,7 +463,6 @@ int compams_collect(float* row, const float* const* tensors, const int64_t* offs
  * call_device, if not null, points to one device int64 that is added to it (modulo 2^32), so that a captured graph draws anew at
  * each replay; it has to hold the same value in a backward pass as in its forward pass.
  */
-enum compams_type { COMPAMS_F32 = 0, COMPAMS_BF16 = 1, COMPAMS_F16 = 2 };
 
 /* y = dropout(x); also dx = dropout(dy). 0 <= p <= 1. */
 int compams_dropout(void* y, const void* x, int32_t type, int32_t n, int64_t rows, int64_t h, int64_t worker_stride,

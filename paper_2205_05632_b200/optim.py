@@ -16,12 +16,113 @@ torch is used for the model and its autograd; the optimizer step itself runs in 
 from __future__ import annotations
 
 import ctypes
-from typing import Iterable, List
+import functools
+import itertools
+from typing import Iterable, List, Optional, Sequence, Tuple, Union
 
 import numpy as np
 import torch
 
 from .binding import RANDK, TOPK, CompAMS, CompAMSError, _check, load_library
+
+_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_INFINITY = float("inf")
+
+
+@functools.lru_cache(maxsize=256)
+def _workspace_bytes(n: int, count: int) -> int:
+    need = ctypes.c_size_t(0)
+    _check(load_library().compams_collect_workers_workspace_bytes(ctypes.byref(need), n, count), "compams_collect_workers_workspace_bytes")
+    return need.value
+
+
+@functools.lru_cache(maxsize=64)
+def _arrays(count: int):
+    """Types of the host arrays of a call."""
+    return ctypes.c_void_p * count, ctypes.c_int64 * count, ctypes.c_int32 * count, ctypes.c_int64 * (count + 1)
+
+
+def _limit(max_norm: Optional[float], eps: float) -> Tuple[float, float]:
+    limit, eps = _INFINITY if max_norm is None else float(max_norm), float(eps)
+    if not limit >= 0.0 or not eps >= 0.0:
+        raise CompAMSError("max_norm and eps must not be negative: got %r, %r" % (max_norm, eps))
+    return limit, eps
+
+
+def _collect_workers(rows: Optional[torch.Tensor], device: torch.device, n: int, pieces, norms: bool, max_norm: float,
+                     eps: float) -> Optional[torch.Tensor]:
+    """compams_collect_workers on (address or None, elements from worker to worker, elements of a worker, type) of each tensor."""
+    pieces = [p for p in pieces if p[2]]
+    got = torch.empty(n, dtype=torch.float32, device=device) if norms else None
+    if not pieces:
+        return None if got is None else got.zero_()
+    count = len(pieces)
+    pointers, longs, ints, ends = _arrays(count)
+    addresses, strides, sizes, types = zip(*pieces)
+    work = torch.empty(_workspace_bytes(n, count), dtype=torch.uint8, device=device) if norms or max_norm < _INFINITY else None
+    with torch.cuda.device(device):
+        _check(load_library().compams_collect_workers(
+            None if rows is None else rows.data_ptr(), 0 if rows is None else rows.stride(0), None if got is None else got.data_ptr(),
+            pointers(*addresses), longs(*strides), ints(*types), ends(*itertools.accumulate(sizes, initial=0)), count, n, max_norm, eps,
+            None if work is None else work.data_ptr(), 0 if work is None else work.numel(), torch._C._cuda_getCurrentRawStream(device.index)),
+            "compams_collect_workers")
+    return got
+
+
+def _changed(tensors) -> None:
+    """Tells autograd, which would not know, that they are written."""
+    tensors = [t for t in tensors if not t.is_inference()]
+    if tensors:
+        torch.autograd.graph.increment_version(tensors)
+
+
+def _gradients(grads, what: str) -> Tuple[List[torch.Tensor], int, torch.device]:
+    grads = [grads] if isinstance(grads, torch.Tensor) else list(grads)
+    if not grads or not all(isinstance(g, torch.Tensor) for g in grads):
+        raise CompAMSError("%s takes tensors, one at least" % what)
+    device, n = grads[0].device, grads[0].shape[0] if grads[0].dim() else 0
+    if device.type != "cuda" or not 1 <= n <= 65535:
+        raise CompAMSError("gradients must be CUDA tensors with the workers, at most 65535, on the leading axis")
+    for g in grads:
+        if g.dtype not in _TYPES or g.device != device or g.dim() == 0 or g.shape[0] != n:
+            raise CompAMSError("gradients must be float32, bfloat16 or float16 tensors [%d, ...] on %s: got %s of type %s on %s" % (
+                n, device, list(g.shape), g.dtype, g.device))
+    return grads, n, device
+
+
+def collect_gradients(grads: Union[torch.Tensor, Sequence[torch.Tensor]], out: Optional[torch.Tensor] = None,
+                      max_norm: Optional[float] = None, eps: float = 1e-6) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(G, norms): the workers' gradients, one tensor [n, *shape] per parameter in float32, bfloat16 or float16, gathered as the rows of a
+    float32 tensor [n, d], `out` where given, and each worker's global norm over all of them, [n], as it was. Rows whose norm is above
+    max_norm are multiplied by max_norm / (norm + eps). The tensors may not overlap out."""
+    grads, n, device = _gradients(grads, "collect_gradients")
+    max_norm, eps = _limit(max_norm, eps)
+    d = sum(g.numel() for g in grads) // n
+    if out is None:
+        out = torch.empty(n, d, dtype=torch.float32, device=device)
+    elif (not isinstance(out, torch.Tensor) or out.dtype != torch.float32 or out.device != device or out.shape != (n, d)
+          or (d > 1 and out.stride(1) != 1) or (n > 1 and out.stride(0) < d) or out.is_neg() or out.requires_grad):
+        raise CompAMSError("out must be a float32 tensor [%d, %d] with packed rows on %s" % (n, d, device))
+    _changed([out])
+    kept = [g if g.is_contiguous() and not g.is_neg() else g.resolve_neg().contiguous() for g in grads]  # until the kernel is enqueued
+    norms = _collect_workers(out, device, n, [(g.data_ptr(), g.numel() // n, g.numel() // n, _TYPES[g.dtype]) for g in kept], True, max_norm, eps)
+    return out, norms
+
+
+def clip_gradients(grads: Union[torch.Tensor, Sequence[torch.Tensor]], max_norm: float, eps: float = 1e-6) -> torch.Tensor:
+    """Each worker's global norm, [n], over tensors [n, *shape] (G itself, or one tensor per parameter; every worker's part packed), which are
+    scaled in place, worker by worker, by min(1, max_norm / (norm + eps)). A worker that is not above max_norm is not touched."""
+    grads, n, device = _gradients(grads, "clip_gradients")
+    max_norm, eps = _limit(max_norm, eps)
+    pieces = []
+    for g in grads:
+        if g.is_neg() or not g[0].is_contiguous() or (n > 1 and g.stride(0) < g[0].numel()):
+            raise CompAMSError("gradients that are clipped in place must be packed for every worker, and the workers' parts apart")
+        if g.requires_grad and torch.is_grad_enabled() and g.is_leaf:
+            raise CompAMSError("a leaf that requires a gradient cannot be scaled in place")
+        pieces.append((g.data_ptr(), g.stride(0), g[0].numel(), _TYPES[g.dtype]))
+    _changed(grads)
+    return _collect_workers(None, device, n, pieces, True, max_norm, eps)
 
 
 class CompAMSOptimizer:
@@ -46,6 +147,7 @@ class CompAMSOptimizer:
         self.G = torch.zeros(self.n, self.d, dtype=torch.float32, device=dev)
         # collect(): the tensors that have elements, their places in a row, and room for their gradients' addresses
         self._pieces = [(p, 4 * size) for p, size in zip(self.params, sizes) if size]
+        self._sizes = sizes
         places = [int(o) for o, size in zip(self.offsets, sizes) if size] + [self.d]
         self._places = (ctypes.c_int64 * len(places))(*places)
         self._addresses = (ctypes.c_void_p * len(self._pieces))()
@@ -92,24 +194,31 @@ class CompAMSOptimizer:
                             for p, lo, hi in zip(self.params, self.offsets[:-1], self.offsets[1:])]
         return self._leaves
 
-    def collect_all(self) -> None:
-        """All rows of G <- the gradients that worker_parameters() accumulated since the last call; they are cleared."""
+    def collect_all(self, max_norm: Optional[float] = None, eps: float = 1e-6) -> Optional[torch.Tensor]:
+        """All rows of G <- the gradients that worker_parameters() accumulated since the last call; they are cleared. With max_norm every
+        worker's row whose norm over all parameters is above it is multiplied by max_norm / (norm + eps), and the norms, [n], are the
+        result."""
+        limit, eps = _limit(max_norm, eps)
         leaves = self.worker_parameters()
         dev = self.G.device
         grads = []
-        for leaf, (_, nbytes) in zip((w for w in leaves if w.numel()), self._pieces):
+        for leaf in leaves:
             g = leaf.grad
             if g is not None and (g.dtype != torch.float32 or g.device != dev or not g.is_contiguous() or g.is_neg()):
                 g = g.to(dev, torch.float32).resolve_neg().contiguous()
-            grads.append((g, nbytes))
-        with torch.cuda.device(dev):
-            stream = torch.cuda.current_stream(dev).cuda_stream
-            for i in range(self.n):
-                self._addresses[:] = [None if g is None else g.data_ptr() + i * nbytes for g, nbytes in grads]
-                _check(load_library().compams_collect(self.G.data_ptr() + 4 * self.d * i, self._addresses, self._places,
-                                                      len(grads), stream), "compams_collect")
+            grads.append(g)
+        pieces = []
+        for g, size in zip(grads, self._sizes):
+            pieces.append((None if g is None else g.data_ptr(), size, size, 0))
+        norms = _collect_workers(self.G, dev, self.n, pieces, max_norm is not None, limit, eps)
         for leaf in leaves:
             leaf.grad = None
+        return norms
+
+    def clip(self, max_norm: float, eps: float = 1e-6) -> torch.Tensor:
+        """Between collect() of the workers and step(): rows of G whose norm is above max_norm are multiplied by max_norm / (norm + eps).
+        The norms, [n], as they were."""
+        return clip_gradients(self.G, max_norm, eps)
 
     def step(self) -> None:
         self.opt.step(self.G, self.theta)
