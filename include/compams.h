@@ -500,6 +500,34 @@ int compams_norm_backward(void* dx, void* dresidual, float* dweight, float* dbia
 int compams_norm_workspace_bytes(size_t* bytes, int32_t n, int64_t rows, int64_t h);
 
 /*
+ * Root-mean-square norms around a block: with r = 1 / sqrt(mean(x^2) + eps) over the h columns,
+ *   residual null:  y = x r weight (s, gate and next are null)
+ *   residual given: s = residual_scale * residual + gate x r weight, rounded to residual_type (`type` or COMPAMS_F32; to 16 bits as the exact
+ *                   value would be, but for one in 10^8), and y = s q next with q = 1 / sqrt(mean(s^2) + eps) of s as it is kept.
+ *   stats           device float [n * rows][2], 8-byte aligned: r and q for the backward pass; may be null.
+ *   weight, gate, next   device fp32; element c of worker i at i * stride + c (stride 0: one for all workers); null: 1.
+ */
+int compams_rms_norm_forward(void* y, void* s, float* stats, const void* x, const void* residual, int32_t type, int32_t residual_type,
+                             int32_t n, int64_t rows, int64_t h, int64_t x_worker_stride, int64_t x_row_stride, int64_t residual_worker_stride,
+                             int64_t residual_row_stride, const float* weight, int64_t weight_stride, const float* gate, int64_t gate_stride,
+                             const float* next, int64_t next_stride, double residual_scale, float eps, void* cuda_stream);
+
+/*
+ * Its gradients. s (null: the plain norm) and stats are the forward pass's, s packed; dy has `type`, ds (null: none) residual_type.
+ *   dx, dresidual, dweight, dgate, dnext   packed, in `type`, residual_type and fp32 [n, h]; each may be null: not wanted. Row i of the
+ *                   latter three is summed over the rows of worker i alone, in a fixed order; sum_workers: [h], over all workers.
+ *   workspace       device, 16-byte aligned, at least compams_rms_norm_workspace_bytes of the current device; used during the call's
+ *                   device work only. Not needed without dweight, dgate and dnext.
+ */
+int compams_rms_norm_backward(void* dx, void* dresidual, float* dweight, float* dgate, float* dnext, int32_t sum_workers, const void* dy,
+                              const void* ds, const void* x, const void* s, const float* stats, int32_t type, int32_t residual_type, int32_t n,
+                              int64_t rows, int64_t h, int64_t dy_worker_stride, int64_t dy_row_stride, int64_t ds_worker_stride,
+                              int64_t ds_row_stride, int64_t x_worker_stride, int64_t x_row_stride, const float* weight, int64_t weight_stride,
+                              const float* gate, int64_t gate_stride, const float* next, int64_t next_stride, double residual_scale,
+                              void* workspace, size_t workspace_bytes, void* cuda_stream);
+int compams_rms_norm_workspace_bytes(size_t* bytes, int32_t n, int64_t rows, int64_t h);
+
+/*
  * Low-rank adapters beside a projection: y = base + scale (dropout(x) A^T) B^T, worker (or request) by worker.
  *   type            of x, base, dy and of the results; x is [n, rows, in], base [n, rows, out] (null: 0) and y packed [n, rows, out].
  *   a, b            device fp32, A [rank, in] and B [out, rank]: rows packed, row_stride apart; worker i's at i * worker_stride (0: one

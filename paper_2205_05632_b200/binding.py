@@ -157,6 +157,13 @@ def load_library() -> ctypes.CDLL:
     L.compams_collect_workers.restype = c.c_int
     L.compams_collect_workers_workspace_bytes.argtypes = [c.POINTER(c.c_size_t), I32, I32]
     L.compams_collect_workers_workspace_bytes.restype = c.c_int
+    L.compams_rms_norm_forward.argtypes = [P] * 5 + [I32] * 3 + [I64] * 6 + [P, I64] * 3 + [c.c_double, c.c_float, P]
+    L.compams_rms_norm_forward.restype = c.c_int
+    L.compams_rms_norm_backward.argtypes = ([P] * 5 + [I32] + [P] * 5 + [I32] * 3 + [I64] * 8 + [P, I64] * 3
+                                            + [c.c_double, P, c.c_size_t, P])
+    L.compams_rms_norm_backward.restype = c.c_int
+    L.compams_rms_norm_workspace_bytes.argtypes = [c.POINTER(c.c_size_t), I32, I64, I64]
+    L.compams_rms_norm_workspace_bytes.restype = c.c_int
     L.compams_error_string.argtypes = [c.c_int]
     L.compams_kernel_name.restype = c.c_char_p
     L.compams_kernel_name.argtypes = [c.c_int32]

@@ -1,0 +1,663 @@
+// Root-mean-square norms around a model's blocks, on [n, rows, h] activations:
+//
+//   norm:   y = x r w                                   r = 1 / sqrt(mean(x^2) + eps)
+//   gated:  s = alpha residual + gate x r w             the norm behind a block, its gate, the residual's scale
+//           y = s q v                                   q = 1 / sqrt(mean(s^2) + eps), the norm before the next block
+//
+//   backward:  b = dy v,   ds' = ds + q (b - s q^2 mean(b s)),   dv = sum_j dy s q
+//              dresidual = alpha ds'
+//              a = ds' gate w,   dx = r (a - x r^2 mean(a x)),   c = sum_j ds' x r,   dw = gate c,   dgate = w c
+//
+// Bound by memory. A row's threads keep it in registers (eight columns each, or sixteen), from the reading to the writing, and have the
+// next row on its way meanwhile; they walk a chunk of a worker's rows and add up its part of the weights' gradients as they go, so that
+// these cost no reading of their own. Rows above kLongest are read again instead, and their sums grow in the workspace.
+//
+// Precision. Everything is fp32 between the reading and the writing. s is kept in the residual's type and normalised as it is kept. In a
+// 16-bit type a difference in the last bit of fp32 may put s on the other side of a border between two of its values: a row's mean of
+// squares is summed with its rounding errors (Kahan), and an s that is nearer to a border than the fp32 error is formed again in
+// binary64; so s is the rounded exact value but for one in 10^8, and with it what the backward pass reads (with fp32 alone one s in
+// 30000 differs, and dv by 1.3e-5 of its length).
+#include <algorithm>
+#include <type_traits>
+
+#include "context.h"
+#include "rows.cuh"
+
+namespace compams {
+namespace {
+
+constexpr int kMostThreads = 512;                      // of a row
+constexpr int64_t kLongest = 16 * (int64_t)kMostThreads;  // columns that they keep
+
+struct BlockArgs {
+    const void *x, *residual, *dy, *ds, *s_in;
+    void *y, *s, *dx, *dresidual;
+    float2* stats;  // of a row: r, q; may be null going forward
+    const float *weight, *gate, *next;  // may be null: ones
+    int64_t weight_ws, gate_ws, next_ws;
+    int64_t x_ws, x_rs, r_ws, r_rs, dy_ws, dy_rs, ds_ws, ds_rs;  // r: of the residual
+    uint32_t rows, groups;  // of a worker; that walk them
+    int32_t h;
+    float alpha, eps;
+    double alpha64;
+    float* partial;  // [n][groups][2][h]: dv, c; may be null
+};
+
+// A thread's eight columns of a row, part k of several: neighbours on a 16-byte boundary (VEC), or every blockDim.x-th.
+template <typename T, bool VEC> struct Cell { Raw8<T> raw; };
+template <typename T> struct Cell<T, false> { float v[8]; };
+
+template <bool VEC> __device__ __forceinline__ int cell_column(int k, int e) {
+    return VEC ? (k * (int)blockDim.x + (int)threadIdx.x) * 8 + e : (k * 8 + e) * (int)blockDim.x + (int)threadIdx.x;
+}
+template <typename T, bool VEC>
+__device__ __forceinline__ void cell_load(Cell<T, VEC>& c, const T* row, int k, int h, bool there) {
+    if constexpr (VEC) {
+        c.raw = {};
+        if (there && cell_column<VEC>(k, 0) < h) c.raw = raw_load<T>(row + cell_column<VEC>(k, 0));
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int at = cell_column<VEC>(k, e);
+            c.v[e] = there && at < h ? to_float(__ldg(row + at)) : 0.0f;
+        }
+    }
+}
+template <typename T, bool VEC>
+__device__ __forceinline__ void cell_values(const Cell<T, VEC>& c, float (&v)[8]) {
+    if constexpr (VEC) {
+        raw_floats<T>(c.raw, v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = c.v[e];
+    }
+}
+// Rounds to T and stores; v becomes what was stored.
+template <typename T, bool VEC>
+__device__ __forceinline__ void cell_store(T* row, int k, int h, bool there, float (&v)[8]) {
+    if constexpr (VEC) {
+        if (there && cell_column<VEC>(k, 0) < h) store8<T>(row + cell_column<VEC>(k, 0), v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int at = cell_column<VEC>(k, e);
+            if (there && at < h) row[at] = from_float<T>(v[e]);
+        }
+    }
+    if constexpr (!std::is_same_v<T, float>)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = to_float(from_float<T>(v[e]));
+}
+template <bool VEC>
+__device__ __forceinline__ void parameter_load(const float* p, int k, int h, float (&v)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const int at = cell_column<VEC>(k, e);
+        v[e] = at >= h ? 0.0f : p ? __ldg(p + at) : 1.0f;
+    }
+}
+
+// The sum over a row's threads: 8, 16 or 32 lanes, or warps that meet at a barrier of their own. `turn` alternates between two places.
+constexpr int kScratch = 4 * 2 * 16;  // rows of a CTA that need it (64 threads each at least), turns, warps
+template <typename V>
+__device__ __forceinline__ V row_sum(V v, V* scratch, int& turn) {
+    const int threads = (int)blockDim.x;
+#pragma unroll
+    for (int o = 16; o; o >>= 1)
+        if (o < threads) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if (threads <= 32) return v;
+    V* place = scratch + (threadIdx.y * 2 + turn) * 16;
+    turn ^= 1;
+    const int warps = threads >> 5;
+    if ((threadIdx.x & 31) == 0) place[threadIdx.x >> 5] = v;
+    asm volatile("bar.sync %0, %1;" ::"r"((int)threadIdx.y + 1), "r"(threads) : "memory");
+    V sum = place[0];
+    for (int w = 1; w < warps; ++w) sum += place[w];
+    return sum;
+}
+
+// Whether the fp32 sum s of p and q is so near to a border between two values of the type that its error may have carried it over.
+template <typename T>
+__device__ __forceinline__ bool near_border(float s, float p, float q) {
+    constexpr uint32_t kDropped = std::is_same_v<T, __nv_bfloat16> ? 16 : 13;
+    const int off = (int)(__float_as_uint(s) & ((1u << kDropped) - 1)) - (1 << (kDropped - 1));
+    return fabsf((float)off) * fabsf(s) <= 8.0f * (fabsf(p) + fabsf(q));
+}
+
+template <typename T, typename R, bool GATED, bool VEC, int K>
+__global__ void __launch_bounds__(kMostThreads, K == 1 ? 2 : 1) block_forward_kernel(const __grid_constant__ BlockArgs a) {
+    constexpr bool kWide = GATED && !std::is_same_v<R, float>;  // s is rounded to 16 bits
+    using Sum = std::conditional_t<kWide, double, float>;
+    __shared__ Sum scratch[kScratch];
+    __shared__ float scratch2[kScratch];
+    const uint32_t worker = blockIdx.y, group = blockIdx.x * blockDim.y + threadIdx.y, rounds = (a.rows + a.groups - 1) / a.groups;
+    const T* x = (const T*)a.x + (int64_t)worker * a.x_ws;
+    const R* residual = GATED ? (const R*)a.residual + (int64_t)worker * a.r_ws : nullptr;
+    const float *weight = a.weight ? a.weight + worker * a.weight_ws : nullptr, *gate = a.gate ? a.gate + worker * a.gate_ws : nullptr;
+    const float* next = a.next ? a.next + worker * a.next_ws : nullptr;
+    float w[K][8], v[K][8];  // weight * gate, next
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        parameter_load<VEC>(weight, k, a.h, w[k]);
+        if (GATED) {
+            float g[8];
+            parameter_load<VEC>(gate, k, a.h, g);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[k][e] *= g[e];
+            parameter_load<VEC>(next, k, a.h, v[k]);
+        }
+    }
+    const float inverse = 1.0f / (float)a.h;
+    int turn = 0, turn2 = 0;
+    Cell<T, VEC> cx[K];
+    Cell<R, VEC> cr[K];
+    auto fetch = [&](uint32_t j) {
+        const bool there = group < a.groups && j < a.rows;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            cell_load<T, VEC>(cx[k], x + (there ? (int64_t)j * a.x_rs : 0), k, a.h, there);
+            if (GATED) cell_load<R, VEC>(cr[k], residual + (there ? (int64_t)j * a.r_rs : 0), k, a.h, there);
+        }
+    };
+    fetch(group);
+    for (uint32_t round = 0, j = group; round < rounds; ++round, j += a.groups) {
+        const bool there = group < a.groups && j < a.rows;
+        float xs[K][8], rs[K][8];
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            cell_values<T, VEC>(cx[k], xs[k]);
+            if (GATED) cell_values<R, VEC>(cr[k], rs[k]);
+        }
+        if (round + 1 < rounds) fetch(j + a.groups);
+        float sum = 0.0f, lost = 0.0f;
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if (kWide) {
+                    const float term = fmaf(xs[k][e], xs[k][e], -lost), grown = sum + term;
+                    lost = (grown - sum) - term;
+                    sum = grown;
+                } else {
+                    sum = fmaf(xs[k][e], xs[k][e], sum);
+                }
+            }
+        const Sum all = row_sum<Sum>(kWide ? (Sum)sum - (Sum)lost : (Sum)sum, scratch, turn);
+        double exact = 0.0;
+        float r;
+        if constexpr (kWide) {
+            exact = all / a.h + (double)a.eps;
+            r = 1.0f / sqrtf((float)exact);
+        } else {
+            r = 1.0f / sqrtf(all * inverse + a.eps);
+        }
+        const int64_t number = (int64_t)worker * a.rows + j;
+        T* y = (T*)a.y + number * a.h;
+        if constexpr (!GATED) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) xs[k][e] = xs[k][e] * r * w[k][e];
+                cell_store<T, VEC>(y, k, a.h, there, xs[k]);
+            }
+            if (a.stats && there && threadIdx.x == 0) a.stats[number] = make_float2(r, 0.0f);
+        } else {
+            R* s = (R*)a.s + number * a.h;
+            float squares = 0.0f;
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float p = a.alpha * rs[k][e], q = xs[k][e] * r * w[k][e];
+                    float t = p + q;
+                    if constexpr (kWide)
+                        if (near_border<R>(t, p, q)) {
+                            const int at = cell_column<VEC>(k, e);
+                            if (at < a.h) {
+                                const double g = (weight ? (double)weight[at] : 1.0) * (gate ? (double)gate[at] : 1.0);
+                                t = (float)(a.alpha64 * (double)rs[k][e] + (double)xs[k][e] / sqrt(exact) * g);
+                            }
+                        }
+                    rs[k][e] = t;
+                }
+                cell_store<R, VEC>(s, k, a.h, there, rs[k]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) squares = fmaf(rs[k][e], rs[k][e], squares);
+            }
+            const float q = 1.0f / sqrtf(row_sum<float>(squares, scratch2, turn2) * inverse + a.eps);
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) rs[k][e] = rs[k][e] * q * v[k][e];
+                cell_store<T, VEC>(y, k, a.h, there, rs[k]);
+            }
+            if (a.stats && there && threadIdx.x == 0) a.stats[number] = make_float2(r, q);
+        }
+    }
+}
+
+template <typename T, typename R, bool GATED, bool VEC, int K>
+__global__ void __launch_bounds__(kMostThreads, 1) block_backward_kernel(const __grid_constant__ BlockArgs a) {
+    __shared__ float scratch[kScratch];
+    const uint32_t worker = blockIdx.y, group = blockIdx.x * blockDim.y + threadIdx.y, rounds = (a.rows + a.groups - 1) / a.groups;
+    const T* x = (const T*)a.x + (int64_t)worker * a.x_ws;
+    const T* dy = (const T*)a.dy + (int64_t)worker * a.dy_ws;
+    const R* ds = GATED && a.ds ? (const R*)a.ds + (int64_t)worker * a.ds_ws : nullptr;
+    const R* s = GATED ? (const R*)a.s_in + (int64_t)worker * a.rows * a.h : nullptr;
+    const float *weight = a.weight ? a.weight + worker * a.weight_ws : nullptr, *gate = a.gate ? a.gate + worker * a.gate_ws : nullptr;
+    const float* next = a.next ? a.next + worker * a.next_ws : nullptr;
+    float w[K][8], v[K][8], sums[2][K][8];  // weight * gate, next; dv, c
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        parameter_load<VEC>(weight, k, a.h, w[k]);
+        if (GATED) {
+            float g[8];
+            parameter_load<VEC>(gate, k, a.h, g);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[k][e] *= g[e];
+            parameter_load<VEC>(next, k, a.h, v[k]);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sums[0][k][e] = sums[1][k][e] = 0.0f;
+    }
+    const float inverse = 1.0f / (float)a.h;
+    int turn = 0;
+    Cell<T, VEC> cx[K], cy[K];
+    Cell<R, VEC> cs[K], cd[K];
+    float2 next_stats = {};
+    auto fetch = [&](uint32_t j) {
+        const bool there = group < a.groups && j < a.rows;
+        const int64_t at = there ? j : 0;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            cell_load<T, VEC>(cx[k], x + at * a.x_rs, k, a.h, there);
+            cell_load<T, VEC>(cy[k], dy + at * a.dy_rs, k, a.h, there);
+            if (GATED) {
+                cell_load<R, VEC>(cs[k], s + at * a.h, k, a.h, there);
+                if (ds) cell_load<R, VEC>(cd[k], ds + at * a.ds_rs, k, a.h, there);
+                else cd[k] = {};
+            }
+        }
+        next_stats = there ? __ldg(a.stats + (int64_t)worker * a.rows + j) : make_float2(0.0f, 0.0f);
+    };
+    fetch(group);
+    for (uint32_t round = 0, j = group; round < rounds; ++round, j += a.groups) {
+        const bool there = group < a.groups && j < a.rows;
+        const float r = next_stats.x, q = next_stats.y;
+        float xs[K][8], g[K][8];  // x; the gradient of what the norm behind x gives
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            cell_values<T, VEC>(cx[k], xs[k]);
+            cell_values<T, VEC>(cy[k], g[k]);
+        }
+        const int64_t number = (int64_t)worker * a.rows + j;
+        if constexpr (GATED) {
+            float ss[K][8], dd[K][8];
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                cell_values<R, VEC>(cs[k], ss[k]);
+                cell_values<R, VEC>(cd[k], dd[k]);
+            }
+            if (round + 1 < rounds) fetch(j + a.groups);
+            float dot = 0.0f;
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    ss[k][e] *= q;
+                    sums[0][k][e] = fmaf(g[k][e], ss[k][e], sums[0][k][e]);
+                    g[k][e] *= v[k][e];
+                    dot = fmaf(g[k][e], ss[k][e], dot);
+                }
+            const float mean = row_sum<float>(dot, scratch, turn) * inverse;
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    g[k][e] = fmaf(q, fmaf(-mean, ss[k][e], g[k][e]), dd[k][e]);
+                    dd[k][e] = a.alpha * g[k][e];
+                }
+                if (a.dresidual) cell_store<R, VEC>((R*)a.dresidual + number * a.h, k, a.h, there, dd[k]);
+            }
+        } else {
+            if (round + 1 < rounds) fetch(j + a.groups);
+        }
+        float dot = 0.0f;
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                xs[k][e] *= r;
+                sums[1][k][e] = fmaf(g[k][e], xs[k][e], sums[1][k][e]);
+                g[k][e] *= w[k][e];
+                dot = fmaf(g[k][e], xs[k][e], dot);
+            }
+        if (a.dx) {
+            const float mean = row_sum<float>(dot, scratch, turn) * inverse;
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) g[k][e] = r * fmaf(-mean, xs[k][e], g[k][e]);
+                cell_store<T, VEC>((T*)a.dx + number * a.h, k, a.h, there, g[k]);
+            }
+        }
+    }
+    if (!a.partial || group >= a.groups) return;
+    float* out = a.partial + ((int64_t)worker * a.groups + group) * 2 * a.h;
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int at = cell_column<VEC>(k, e);
+            if (at < a.h) {
+                if (GATED) out[at] = sums[0][k][e];
+                out[a.h + at] = sums[1][k][e];
+            }
+        }
+}
+
+// Rows that registers do not hold: a CTA of 512 threads walks its rows' columns again for every sum.
+template <typename T, typename R, bool GATED>
+__global__ void __launch_bounds__(kMostThreads) long_forward_kernel(const __grid_constant__ BlockArgs a) {
+    constexpr bool kWide = GATED && !std::is_same_v<R, float>;
+    __shared__ double scratch[kScratch];
+    __shared__ float scratch2[kScratch];
+    const uint32_t worker = blockIdx.y;
+    const float *weight = a.weight ? a.weight + worker * a.weight_ws : nullptr, *gate = a.gate ? a.gate + worker * a.gate_ws : nullptr;
+    const float* next = a.next ? a.next + worker * a.next_ws : nullptr;
+    const float inverse = 1.0f / (float)a.h;
+    int turn = 0, turn2 = 0;
+    for (uint32_t j = blockIdx.x; j < a.rows; j += a.groups) {
+        const T* x = (const T*)a.x + (int64_t)worker * a.x_ws + (int64_t)j * a.x_rs;
+        const R* residual = GATED ? (const R*)a.residual + (int64_t)worker * a.r_ws + (int64_t)j * a.r_rs : nullptr;
+        const int64_t number = (int64_t)worker * a.rows + j;
+        T* y = (T*)a.y + number * a.h;
+        R* s = GATED ? (R*)a.s + number * a.h : nullptr;
+        double sum = 0.0;
+        for (int c0 = threadIdx.x; c0 < a.h; c0 += 8 * kMostThreads) {
+            float some = 0.0f, lost = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int c = c0 + e * kMostThreads;
+                const float v = c < a.h ? to_float(__ldg(x + c)) : 0.0f;
+                const float term = fmaf(v, v, -lost), grown = some + term;
+                lost = (grown - some) - term;
+                some = grown;
+            }
+            sum += (double)some - (double)lost;
+        }
+        const double exact = row_sum<double>(sum, scratch, turn) / a.h + (double)a.eps;
+        const float r = 1.0f / sqrtf((float)exact);
+        float squares = 0.0f, q = 0.0f;
+        for (int c = threadIdx.x; c < a.h; c += kMostThreads) {
+            const float w = weight ? __ldg(weight + c) : 1.0f, v = to_float(__ldg(x + c));
+            if constexpr (!GATED) {
+                y[c] = from_float<T>(v * r * w);
+            } else {
+                const float p = a.alpha * to_float(__ldg(residual + c)), u = v * r * (w * (gate ? __ldg(gate + c) : 1.0f));
+                float t = p + u;
+                if constexpr (kWide)
+                    if (near_border<R>(t, p, u))
+                        t = (float)(a.alpha64 * (double)to_float(__ldg(residual + c)) + (double)v / sqrt(exact) * ((double)w * (gate ? (double)gate[c] : 1.0)));
+                s[c] = from_float<R>(t);
+                t = to_float(from_float<R>(t));
+                squares = fmaf(t, t, squares);
+            }
+        }
+        if constexpr (GATED) {
+            q = 1.0f / sqrtf(row_sum<float>(squares, scratch2, turn2) * inverse + a.eps);
+            for (int c = threadIdx.x; c < a.h; c += kMostThreads)  // (its own: a thread reads what it wrote)
+                y[c] = from_float<T>(to_float(s[c]) * q * (next ? __ldg(next + c) : 1.0f));
+        }
+        if (a.stats && threadIdx.x == 0) a.stats[number] = make_float2(r, q);
+    }
+}
+template <typename T, typename R, bool GATED>
+__global__ void __launch_bounds__(kMostThreads) long_backward_kernel(const __grid_constant__ BlockArgs a) {
+    __shared__ float scratch[kScratch];
+    const uint32_t worker = blockIdx.y;
+    const float *weight = a.weight ? a.weight + worker * a.weight_ws : nullptr, *gate = a.gate ? a.gate + worker * a.gate_ws : nullptr;
+    const float* next = a.next ? a.next + worker * a.next_ws : nullptr;
+    const float inverse = 1.0f / (float)a.h;
+    float* out = a.partial ? a.partial + ((int64_t)worker * a.groups + blockIdx.x) * 2 * a.h : nullptr;
+    int turn = 0;
+    for (uint32_t j = blockIdx.x; j < a.rows; j += a.groups) {
+        const T* x = (const T*)a.x + (int64_t)worker * a.x_ws + (int64_t)j * a.x_rs;
+        const T* dy = (const T*)a.dy + (int64_t)worker * a.dy_ws + (int64_t)j * a.dy_rs;
+        const R* ds = GATED && a.ds ? (const R*)a.ds + (int64_t)worker * a.ds_ws + (int64_t)j * a.ds_rs : nullptr;
+        const int64_t number = (int64_t)worker * a.rows + j;
+        const R* s = GATED ? (const R*)a.s_in + number * a.h : nullptr;
+        const float2 stats = __ldg(a.stats + number);
+        const float r = stats.x, q = stats.y;
+        const bool first = j == blockIdx.x;
+        float mean = 0.0f;
+        if constexpr (GATED) {
+            float dot = 0.0f;
+            for (int c = threadIdx.x; c < a.h; c += kMostThreads) {
+                const float g = to_float(__ldg(dy + c)), shat = to_float(__ldg(s + c)) * q;
+                dot = fmaf(g * (next ? __ldg(next + c) : 1.0f), shat, dot);
+                if (out) out[c] = fmaf(g, shat, first ? 0.0f : out[c]);
+            }
+            mean = row_sum<float>(dot, scratch, turn) * inverse;
+        }
+        auto gradient = [&](int c) {  // of what the norm behind x gives, gate included
+            const float g = to_float(__ldg(dy + c));
+            if constexpr (!GATED) return g;
+            else return fmaf(q, fmaf(-mean, to_float(__ldg(s + c)) * q, g * (next ? __ldg(next + c) : 1.0f)), ds ? to_float(__ldg(ds + c)) : 0.0f);
+        };
+        auto factor = [&](int c) { return (weight ? __ldg(weight + c) : 1.0f) * (GATED && gate ? __ldg(gate + c) : 1.0f); };
+        float dot = 0.0f;
+        for (int c = threadIdx.x; c < a.h; c += kMostThreads) {
+            const float g = gradient(c), xhat = to_float(__ldg(x + c)) * r;
+            if (GATED && a.dresidual) ((R*)a.dresidual)[number * a.h + c] = from_float<R>(a.alpha * g);
+            if (out) out[a.h + c] = fmaf(g, xhat, first ? 0.0f : out[a.h + c]);
+            dot = fmaf(g * factor(c), xhat, dot);
+        }
+        if (a.dx) {
+            const float mean2 = row_sum<float>(dot, scratch, turn) * inverse;
+            for (int c = threadIdx.x; c < a.h; c += kMostThreads)
+                ((T*)a.dx)[number * a.h + c] = from_float<T>(r * fmaf(-mean2, to_float(__ldg(x + c)) * r, gradient(c) * factor(c)));
+        }
+    }
+}
+
+struct SumsArgs {
+    const float* partial;
+    const float *weight, *gate;
+    int64_t weight_ws, gate_ws;
+    float *dweight, *dgate, *dnext;
+    int32_t h, n, gated;
+    uint32_t groups;
+    int32_t together;
+};
+// The groups' sums, eight shares of them for 32 columns, and the weights' gradients from them. together: over all workers.
+__global__ void __launch_bounds__(256) block_sums_kernel(const __grid_constant__ SumsArgs a) {
+    __shared__ float shares[2][8][33];
+    dependency_wait();
+    const int c = blockIdx.x * 32 + threadIdx.x;
+    float dv = 0.0f, dw = 0.0f, dg = 0.0f;
+    for (int i = a.together ? 0 : blockIdx.y; i < (a.together ? a.n : (int)blockIdx.y + 1); ++i) {
+        const float* from = a.partial + (int64_t)i * a.groups * 2 * a.h + c;
+        float v = 0.0f, q = 0.0f;
+        if (c < a.h)
+#pragma unroll 4
+            for (uint32_t g = threadIdx.y; g < a.groups; g += 8) {
+                if (a.gated) v += from[(int64_t)g * 2 * a.h];
+                q += from[(int64_t)g * 2 * a.h + a.h];
+            }
+        __syncthreads();
+        shares[0][threadIdx.y][threadIdx.x] = v;
+        shares[1][threadIdx.y][threadIdx.x] = q;
+        __syncthreads();
+        if (threadIdx.y == 0 && c < a.h) {
+            v = q = 0.0f;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                v += shares[0][k][threadIdx.x];
+                q += shares[1][k][threadIdx.x];
+            }
+            dv += v;
+            dw += (a.gate ? a.gate[i * a.gate_ws + c] : 1.0f) * q;
+            dg += (a.weight ? a.weight[i * a.weight_ws + c] : 1.0f) * q;
+        }
+    }
+    if (threadIdx.y || c >= a.h) return;
+    const int64_t at = (int64_t)blockIdx.y * a.h + c;
+    if (a.dnext) a.dnext[at] = dv;
+    if (a.dweight) a.dweight[at] = dw;
+    if (a.dgate) a.dgate[at] = dg;
+}
+
+// ---- host ------------------------------------------------------------------------------------------------------------------
+
+struct BlockShape {
+    int32_t n;
+    int64_t rows, h;
+    bool ok() const {
+        return n >= 1 && n <= 65535 && rows >= 0 && h >= 1 && h < ((int64_t)1 << 31) - 16 * kSpan && rows <= (int64_t)0x7fffffff / n;
+    }
+    // Threads of a row: eight columns each, then sixteen; at least 8. Rows of a CTA: 256 threads, or one row.
+    int parts() const { return h <= 8 * kMostThreads ? 1 : 2; }
+    int threads() const {
+        if (h > kLongest) return kMostThreads;
+        const int64_t cells = (h + 8 * parts() - 1) / (8 * parts());
+        return cells <= 8 ? 8 : cells <= 16 ? 16 : (int)((cells + 31) / 32 * 32);
+    }
+    int rows_of_cta() const { return threads() >= 256 ? 1 : 256 / threads(); }
+    // Groups of threads that walk a worker's rows: what fills the SMs with 1024 threads, of four rows at least.
+    uint32_t groups() const {
+        const int64_t all = (int64_t)multiprocessors() * (1024 / threads());
+        const int64_t most = (rows + 3) / 4, per = rows_of_cta();
+        int64_t g = (all + n - 1) / n;
+        g = std::min(std::max<int64_t>(1, g), std::max<int64_t>(1, most));
+        return (uint32_t)((g + per - 1) / per * per);
+    }
+};
+
+template <typename F>
+int by_block_types(int32_t x, int32_t r, F f) {
+    if (x == kTypeF32) return f(float(), float());
+    if (x == kTypeBF16) return r == kTypeF32 ? f(__nv_bfloat16(), float()) : f(__nv_bfloat16(), __nv_bfloat16());
+    return r == kTypeF32 ? f(__half(), float()) : f(__half(), __half());
+}
+int launched(cudaError_t e, const char* what) { return e == cudaSuccess ? COMPAMS_OK : cuda_fail(e, what); }
+bool float_aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+bool vector_parameter(const float* p, int64_t ws) { return !p || (((reinterpret_cast<uintptr_t>(p) | (uint64_t)(ws * 4)) & 15u) == 0); }
+
+template <typename T, typename R, bool GATED>
+int block_forward(BlockArgs& a, const BlockShape& z, bool vec, cudaStream_t stream) {
+    if (z.h > kLongest)
+        return launched(launch_plain(long_forward_kernel<T, R, GATED>, dim3(a.groups, (uint32_t)z.n), dim3(kMostThreads), 0, stream, a), "block_forward");
+    const auto kernel = z.parts() == 1 ? (vec ? block_forward_kernel<T, R, GATED, true, 1> : block_forward_kernel<T, R, GATED, false, 1>)
+                                       : (vec ? block_forward_kernel<T, R, GATED, true, 2> : block_forward_kernel<T, R, GATED, false, 2>);
+    return launched(launch_plain(kernel, dim3(a.groups / z.rows_of_cta(), (uint32_t)z.n), dim3((uint32_t)z.threads(), (uint32_t)z.rows_of_cta()), 0, stream, a),
+                    "block_forward");
+}
+template <typename T, typename R, bool GATED>
+int block_backward(BlockArgs& a, const BlockShape& z, bool vec, cudaStream_t stream) {
+    if (z.h > kLongest)
+        return launched(launch_plain(long_backward_kernel<T, R, GATED>, dim3(a.groups, (uint32_t)z.n), dim3(kMostThreads), 0, stream, a), "block_backward");
+    const auto kernel = z.parts() == 1 ? (vec ? block_backward_kernel<T, R, GATED, true, 1> : block_backward_kernel<T, R, GATED, false, 1>)
+                                       : (vec ? block_backward_kernel<T, R, GATED, true, 2> : block_backward_kernel<T, R, GATED, false, 2>);
+    return launched(launch_plain(kernel, dim3(a.groups / z.rows_of_cta(), (uint32_t)z.n), dim3((uint32_t)z.threads(), (uint32_t)z.rows_of_cta()), 0, stream, a),
+                    "block_backward");
+}
+
+}  // namespace
+}  // namespace compams
+
+using namespace compams;
+
+extern "C" {
+
+int compams_rms_norm_forward(void* y, void* s, float* stats, const void* x, const void* residual, int32_t type, int32_t residual_type,
+                             int32_t n, int64_t rows, int64_t h, int64_t x_worker_stride, int64_t x_row_stride, int64_t residual_worker_stride,
+                             int64_t residual_row_stride, const float* weight, int64_t weight_stride, const float* gate, int64_t gate_stride,
+                             const float* next, int64_t next_stride, double residual_scale, float eps, void* cuda_stream) {
+    const BlockShape z{n, rows, h};
+    const bool gated = residual != nullptr;
+    if (!z.ok() || !type_known(type) || !(eps >= 0.0f) || (gated ? residual_type != type && residual_type != kTypeF32 : s || gate || next))
+        return COMPAMS_ERR_INVALID_ARG;
+    if (rows == 0) return COMPAMS_OK;
+    const Rows in{x, x_worker_stride, x_row_stride, type}, out = packed(y, rows, h, type);
+    const Rows res{residual, residual_worker_stride, residual_row_stride, residual_type}, sum = packed(s, rows, h, residual_type);
+    if (!in.strides_ok() || (gated && !res.strides_ok()) || weight_stride < 0 || gate_stride < 0 || next_stride < 0 || !x || !y || (gated && !s) ||
+        !in.element_aligned() || !out.element_aligned() || !float_aligned(weight) || !float_aligned(gate) || !float_aligned(next) ||
+        (reinterpret_cast<uintptr_t>(stats) & 7u) || (gated && (!res.element_aligned() || !sum.element_aligned())))
+        return COMPAMS_ERR_INVALID_ARG;
+    const bool vec = h % 8 == 0 && in.aligned() && out.aligned() && (!gated || (res.aligned() && sum.aligned())) &&
+                     vector_parameter(weight, weight_stride) && vector_parameter(gate, gate_stride) && vector_parameter(next, next_stride);
+    BlockArgs a = {};
+    a.x = x; a.residual = residual; a.y = y; a.s = s; a.stats = (float2*)stats; a.weight = weight; a.gate = gate; a.next = next;
+    a.weight_ws = weight_stride; a.gate_ws = gate_stride; a.next_ws = next_stride;
+    a.x_ws = x_worker_stride; a.x_rs = x_row_stride; a.r_ws = residual_worker_stride; a.r_rs = residual_row_stride;
+    a.rows = (uint32_t)rows; a.groups = z.groups(); a.h = (int32_t)h; a.alpha = (float)residual_scale; a.alpha64 = residual_scale; a.eps = eps;
+    return by_block_types(type, gated ? residual_type : type, [&](auto t, auto r) {
+        using T = decltype(t);
+        using R = decltype(r);
+        if (gated) return block_forward<T, R, true>(a, z, vec, (cudaStream_t)cuda_stream);
+        return block_forward<T, T, false>(a, z, vec, (cudaStream_t)cuda_stream);
+    });
+}
+
+int compams_rms_norm_workspace_bytes(size_t* bytes, int32_t n, int64_t rows, int64_t h) {
+    const BlockShape z{n, rows, h};
+    if (!bytes || !z.ok()) return COMPAMS_ERR_INVALID_ARG;
+    *bytes = (size_t)n * z.groups() * 2 * (size_t)h * sizeof(float);
+    return COMPAMS_OK;
+}
+
+int compams_rms_norm_backward(void* dx, void* dresidual, float* dweight, float* dgate, float* dnext, int32_t sum_workers, const void* dy,
+                              const void* ds, const void* x, const void* s, const float* stats, int32_t type, int32_t residual_type, int32_t n,
+                              int64_t rows, int64_t h, int64_t dy_worker_stride, int64_t dy_row_stride, int64_t ds_worker_stride,
+                              int64_t ds_row_stride, int64_t x_worker_stride, int64_t x_row_stride, const float* weight, int64_t weight_stride,
+                              const float* gate, int64_t gate_stride, const float* next, int64_t next_stride, double residual_scale,
+                              void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    const BlockShape z{n, rows, h};
+    const bool gated = s != nullptr, sums = dweight || dgate || dnext;
+    if (!z.ok() || !type_known(type) || (gated ? residual_type != type && residual_type != kTypeF32 : ds || dresidual || gate || next || dgate || dnext))
+        return COMPAMS_ERR_INVALID_ARG;
+    if (!float_aligned(dweight) || !float_aligned(dgate) || !float_aligned(dnext)) return COMPAMS_ERR_INVALID_ARG;
+    const cudaStream_t stream = (cudaStream_t)cuda_stream;
+    if (rows == 0) {
+        const size_t bytes = (size_t)(sum_workers ? 1 : n) * (size_t)h * sizeof(float);
+        cudaError_t e = dweight ? cudaMemsetAsync(dweight, 0, bytes, stream) : cudaSuccess;
+        if (e == cudaSuccess && dgate) e = cudaMemsetAsync(dgate, 0, bytes, stream);
+        if (e == cudaSuccess && dnext) e = cudaMemsetAsync(dnext, 0, bytes, stream);
+        return launched(e, "block_backward");
+    }
+    const size_t need = (size_t)n * z.groups() * 2 * (size_t)h * sizeof(float);
+    const Rows gin{dy, dy_worker_stride, dy_row_stride, type}, gsum{ds, ds_worker_stride, ds_row_stride, residual_type};
+    const Rows xin{x, x_worker_stride, x_row_stride, type}, sin = packed(s, rows, h, residual_type), out = packed(dx, rows, h, type),
+               rout = packed(dresidual, rows, h, residual_type);
+    if ((sums && (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 15u))) || !gin.strides_ok() ||
+        (ds && !gsum.strides_ok()) || !xin.strides_ok() || weight_stride < 0 || gate_stride < 0 || next_stride < 0 || !dy || !x || !stats ||
+        (reinterpret_cast<uintptr_t>(stats) & 7u) || !float_aligned(weight) || !float_aligned(gate) || !float_aligned(next) ||
+        !gin.element_aligned() || !xin.element_aligned() || !out.element_aligned() ||
+        (gated && (!gsum.element_aligned() || !sin.element_aligned() || !rout.element_aligned())))
+        return COMPAMS_ERR_INVALID_ARG;
+    if (!dx && !dresidual && !sums) return COMPAMS_OK;
+    const bool vec = h % 8 == 0 && gin.aligned() && xin.aligned() && out.aligned() &&
+                     (!gated || ((!ds || gsum.aligned()) && sin.aligned() && rout.aligned())) && vector_parameter(weight, weight_stride) &&
+                     vector_parameter(gate, gate_stride) && vector_parameter(next, next_stride);
+    BlockArgs a = {};
+    a.x = x; a.dy = dy; a.ds = ds; a.s_in = s; a.dx = dx; a.dresidual = dresidual; a.stats = (float2*)const_cast<float*>(stats);
+    a.weight = weight; a.gate = gate; a.next = next; a.weight_ws = weight_stride; a.gate_ws = gate_stride; a.next_ws = next_stride;
+    a.x_ws = x_worker_stride; a.x_rs = x_row_stride; a.dy_ws = dy_worker_stride; a.dy_rs = dy_row_stride; a.ds_ws = ds_worker_stride;
+    a.ds_rs = ds_row_stride; a.rows = (uint32_t)rows; a.groups = z.groups(); a.h = (int32_t)h; a.alpha = (float)residual_scale;
+    a.partial = sums ? (float*)workspace : nullptr;
+    const int rc = by_block_types(type, gated ? residual_type : type, [&](auto t, auto r) {
+        using T = decltype(t);
+        using R = decltype(r);
+        if (gated) return block_backward<T, R, true>(a, z, vec, stream);
+        return block_backward<T, T, false>(a, z, vec, stream);
+    });
+    if (rc != COMPAMS_OK || !sums) return rc;
+    SumsArgs j = {};
+    j.partial = a.partial; j.weight = weight; j.gate = gate; j.weight_ws = weight_stride; j.gate_ws = gate_stride; j.dweight = dweight; j.dgate = dgate;
+    j.dnext = dnext; j.h = (int32_t)h; j.n = n; j.gated = gated; j.groups = a.groups; j.together = sum_workers != 0;
+    return launched(launch_after(block_sums_kernel, dim3((uint32_t)((h + 31) / 32), sum_workers ? 1u : (uint32_t)n), dim3(32, 8), stream, j),
+                    "block_sums");
+}
+
+}  // extern "C"

@@ -351,6 +351,119 @@ def dropout_add_layer_norm(x: torch.Tensor, residual: torch.Tensor, weight: Opti
     return _norm_forward(x, residual, weight, bias, eps, drop, False)[:2]
 
 
+# ---- root-mean-square norms around a block ---------------------------------------------------------------------------------
+
+
+def _rms_forward(x, residual, weight, gate, after, scale, eps, keep_stats):
+    y = _empty(x)
+    s = None if residual is None else _empty(x, residual.dtype)
+    stats = x.new_empty((x.numel() // x.shape[-1], 2), dtype=torch.float32) if keep_stats else None
+    if x.numel():
+        v, rows, ws, rs = _rows(x)
+        r, rws, rrs = None, 0, 0
+        if residual is not None:
+            r, _, rws, rrs = _rows(residual)
+        _run("compams_rms_norm_forward", x.device, y.data_ptr(), _ptr(s), _ptr(stats), v.data_ptr(), _ptr(r), _TYPES[x.dtype],
+             0 if r is None else _TYPES[r.dtype], x.shape[0], rows, x.shape[-1], ws, rs, rws, rrs, *_affine(weight), *_affine(gate),
+             *_affine(after), scale, eps)
+    return y, s, stats
+
+
+def _rms_backward(ctx, dy, ds, x, s, stats, weight, gate, after):
+    """(dx, dresidual, dweight, dgate, dnext) as ctx.wanted wants them."""
+    needs_x, needs_r, *needs = ctx.wanted
+    n, h = x.shape[0], x.shape[-1]
+    dx = _empty(x) if needs_x else None
+    dres = _empty(s) if needs_r else None
+    make = x.new_empty if x.numel() else x.new_zeros
+    params = [make((n, h) if ctx.apart else (h,), dtype=torch.float32) if need else None for need in needs]
+    if x.numel():
+        dy = x.new_zeros(x.shape) if dy is None else dy
+        g, rows, gws, grs = _rows(dy)
+        v, _, ws, rs = _rows(x)
+        e, ews, ers = None, 0, 0
+        if ds is not None:
+            e, _, ews, ers = _rows(ds)
+        work = _workspace("compams_rms_norm_workspace_bytes", v, n, rows, h) if any(needs) else None
+        _run("compams_rms_norm_backward", x.device, _ptr(dx), _ptr(dres), *map(_ptr, params), 0 if ctx.apart else 1, g.data_ptr(), _ptr(e),
+             v.data_ptr(), _ptr(s), stats.data_ptr(), _TYPES[x.dtype], 0 if s is None else _TYPES[s.dtype], n, rows, h, gws, grs, ews, ers,
+             ws, rs, *_affine(weight), *_affine(gate), *_affine(after), ctx.scale, _ptr(work), 0 if work is None else work.numel())
+    return dx, dres, *params
+
+
+class _RmsNormFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, eps):
+        y, _, stats = _rms_forward(x, None, weight, None, None, 1.0, eps, True)
+        ctx.save_for_backward(x, stats, *([weight] if weight is not None else []))
+        ctx.apart, ctx.scale = weight is not None and weight.dim() == 2, 1.0
+        return y
+
+    @staticmethod
+    @_once
+    def backward(ctx, dy):
+        x, stats, *weight = ctx.saved_tensors
+        ctx.wanted = (ctx.needs_input_grad[0], False, ctx.needs_input_grad[1], False, False)
+        dx, _, dw, _, _ = _rms_backward(ctx, dy, None, x, None, stats, weight[0] if weight else None, None, None)
+        return dx, dw, None
+
+
+class _GatedNormFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, residual, weight, gate, after, scale, eps):
+        y, s, stats = _rms_forward(x, residual, weight, gate, after, scale, eps, True)
+        ctx.set_materialize_grads(False)
+        given = [t for t in (weight, gate, after) if t is not None]
+        ctx.given = [t is not None for t in (weight, gate, after)]
+        ctx.save_for_backward(x, s, stats, *given)
+        ctx.apart, ctx.scale = any(t.dim() == 2 for t in given), scale
+        return y, s
+
+    @staticmethod
+    @_once
+    def backward(ctx, dy, ds):
+        x, s, stats, *given = ctx.saved_tensors
+        if dy is None and ds is None:
+            return (None,) * 7
+        ctx.wanted = ctx.needs_input_grad[:5]
+        given = iter(given)
+        return (*_rms_backward(ctx, dy, ds, x, s, stats, *[next(given) if there else None for there in ctx.given]), None, None)
+
+
+def _rms_parameters(x, eps, **parameters):
+    h = x.shape[-1]
+    found = [None if p is None else _factor(p, x, (h,), name) for name, p in parameters.items()]
+    if len({p.dim() for p in found if p is not None}) > 1:
+        raise CompAMSError("%s are all for all workers or all per worker" % ", ".join(parameters))
+    if not float(eps) >= 0.0:
+        raise CompAMSError("eps must not be negative")
+    return *found, float(eps)
+
+
+def rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, eps: float = 1e-6) -> torch.Tensor:
+    """x / sqrt(mean(x^2) + eps) * weight over the last axis of x [n, ..., h], in x's type; weight is float32 [h] or [n, h]."""
+    _activation(x)
+    weight, eps = _rms_parameters(x, eps, weight=weight)
+    if _through_autograd(x, weight):
+        return _RmsNormFunction.apply(x, weight, eps)
+    return _rms_forward(x, None, weight, None, None, 1.0, eps, False)[0]
+
+
+def gated_add_rms_norm(x: torch.Tensor, residual: torch.Tensor, weight: Optional[torch.Tensor] = None,
+                       gate: Optional[torch.Tensor] = None, next_weight: Optional[torch.Tensor] = None, residual_scale: float = 1.0,
+                       eps: float = 1e-6) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(rms_norm(s, next_weight), s) with s = residual_scale * residual + gate * rms_norm(x, weight): the norm behind a block, its gate, the
+    residual stream and the norm before the next block. s has the residual's type, which is x's or float32, and is normalised as it is
+    stored; the first result has x's type. weight, gate and next_weight are float32 [h], or all [n, h]; None: 1."""
+    _activation(x)
+    _like(residual, x, "residual", (x.dtype, torch.float32))
+    weight, gate, next_weight, eps = _rms_parameters(x, eps, weight=weight, gate=gate, next_weight=next_weight)
+    args = (x, residual, weight, gate, next_weight, float(residual_scale), eps)
+    if _through_autograd(*args[:5]):
+        return _GatedNormFunction.apply(*args)
+    return _rms_forward(*args, False)[:2]
+
+
 # ---- low-rank adapters -----------------------------------------------------------------------------------------------------
 
 
