@@ -14,9 +14,9 @@
 //
 // Precision. Everything is fp32 between the reading and the writing. s is kept in the residual's type and normalised as it is kept. In a
 // 16-bit type a difference in the last bit of fp32 may put s on the other side of a border between two of its values: a row's mean of
-// squares is summed with its rounding errors (Kahan), and an s that is nearer to a border than the fp32 error is formed again in
-// binary64; so s is the rounded exact value but for one in 10^8, and with it what the backward pass reads (with fp32 alone one s in
-// 30000 differs, and dv by 1.3e-5 of its length).
+// squares is summed with its rounding errors, and an s that is nearer to a border than the fp32 error is formed again in binary64; so s is
+// the exact sum, rounded to fp32 and then to 16 bits, but for one in 10^8, and with it what the backward pass reads (with fp32 alone one s
+// in 30000 differs, and dv by 1.3e-5 of its length).
 #include <algorithm>
 #include <type_traits>
 
@@ -124,6 +124,13 @@ __device__ __forceinline__ bool near_border(float s, float p, float q) {
     return fabsf((float)off) * fabsf(s) <= 8.0f * (fabsf(p) + fabsf(q));
 }
 
+// Adds a square, exact in fp32 for 16-bit numbers, to a sum, and what the sum's rounding leaves out to `lost` (Knuth's two-sum).
+__device__ __forceinline__ void add_square(float x, float& sum, float& lost) {
+    const float term = x * x, grown = sum + term, part = grown - sum;
+    lost += (sum - (grown - part)) + (term - part);
+    sum = grown;
+}
+
 template <typename T, typename R, bool GATED, bool VEC, int K>
 __global__ void __launch_bounds__(kMostThreads, K == 1 ? 2 : 1) block_forward_kernel(const __grid_constant__ BlockArgs a) {
     constexpr bool kWide = GATED && !std::is_same_v<R, float>;  // s is rounded to 16 bits
@@ -174,15 +181,10 @@ __global__ void __launch_bounds__(kMostThreads, K == 1 ? 2 : 1) block_forward_ke
         for (int k = 0; k < K; ++k)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                if (kWide) {
-                    const float term = fmaf(xs[k][e], xs[k][e], -lost), grown = sum + term;
-                    lost = (grown - sum) - term;
-                    sum = grown;
-                } else {
-                    sum = fmaf(xs[k][e], xs[k][e], sum);
-                }
+                if (kWide) add_square(xs[k][e], sum, lost);
+                else sum = fmaf(xs[k][e], xs[k][e], sum);
             }
-        const Sum all = row_sum<Sum>(kWide ? (Sum)sum - (Sum)lost : (Sum)sum, scratch, turn);
+        const Sum all = row_sum<Sum>(kWide ? (Sum)sum + (Sum)lost : (Sum)sum, scratch, turn);
         double exact = 0.0;
         float r;
         if constexpr (kWide) {
@@ -379,12 +381,9 @@ __global__ void __launch_bounds__(kMostThreads) long_forward_kernel(const __grid
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const int c = c0 + e * kMostThreads;
-                const float v = c < a.h ? to_float(__ldg(x + c)) : 0.0f;
-                const float term = fmaf(v, v, -lost), grown = some + term;
-                lost = (grown - some) - term;
-                some = grown;
+                add_square(c < a.h ? to_float(__ldg(x + c)) : 0.0f, some, lost);
             }
-            sum += (double)some - (double)lost;
+            sum += (double)some + (double)lost;
         }
         const double exact = row_sum<double>(sum, scratch, turn) / a.h + (double)a.eps;
         const float r = 1.0f / sqrtf((float)exact);

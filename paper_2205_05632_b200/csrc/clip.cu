@@ -146,7 +146,7 @@ __global__ void __launch_bounds__(256) clip_kernel(const __grid_constant__ List 
         for (int p = threadIdx.x; p < a.pitch; p += 256) sum += a.partials[worker * a.pitch + p];
         const double norm = sqrt(block_sum_double<8>(sum, scratch));
         if (threadIdx.x == 0) {
-            const double f = a.max_norm / (norm + a.eps);
+            const double f = isinf(a.max_norm) ? 1.0 : a.max_norm / (norm + a.eps);
             shared_factor = f >= 1.0 ? 1.0f : (float)f;  // (no number stays none)
             if (a.norms && piece == 0) a.norms[worker] = (float)norm;
         }

@@ -273,7 +273,7 @@ struct RowsArgs {
     const float* dloss;
     int64_t ws, rs;  // of dloss; rs counts without a reduction alone
     const int64_t* target;
-    int64_t rows, ignored;
+    int64_t rows, ignored, vocab;
     int32_t n, reduction, f16;
     float *g, *scale;     // [all rows], [n]
 };
@@ -315,8 +315,11 @@ __global__ void __launch_bounds__(256) rows_kernel(const __grid_constant__ RowsA
         scale = a.reduction == kMean ? dloss[0] / fmaxf(count, 1.0f) : dloss[0];
     }
     if (threadIdx.x == 0) a.scale[i] = a.f16 ? scale * (1.0f / head::kF16Scale) : scale;
-    for (int64_t j = threadIdx.x; j < a.rows; j += 256)
-        a.g[i * a.rows + j] = target[j] == a.ignored ? 0.0f : a.reduction == kNone ? inverse * dloss[j * a.rs] : 1.0f;
+    for (int64_t j = threadIdx.x; j < a.rows; j += 256) {
+        const int64_t t = target[j];
+        const float g = a.reduction == kNone ? inverse * dloss[j * a.rs] : 1.0f;
+        a.g[i * a.rows + j] = t == a.ignored ? 0.0f : t >= 0 && t < a.vocab ? g : __int_as_float(0x7fffffff);  // no such column
+    }
 }
 
 // dx from the parts' sums.
@@ -723,7 +726,7 @@ int compams_head_backward(void* dx, void* dweight, int32_t sum_workers, const fl
     char* work = (char*)workspace;
     const int64_t all = z.all_rows();
     RowsArgs r = {};
-    r.dloss = dloss; r.ws = dloss_worker_stride; r.rs = dloss_row_stride; r.target = target; r.rows = rows; r.ignored = ignored; r.n = n;
+    r.dloss = dloss; r.ws = dloss_worker_stride; r.rs = dloss_row_stride; r.target = target; r.rows = rows; r.ignored = ignored; r.vocab = vocab; r.n = n;
     r.reduction = reduction; r.f16 = z.f16(); r.g = (float*)(work + p.g); r.scale = (float*)(work + p.scale);
     int rc = launched(launch_sized(rows_kernel, dim3((uint32_t)n), 256, 1, 0, true, stream, r), "head_rows");
     Operand xo, wo;
