@@ -521,8 +521,22 @@ void pairs_of(head::Args& a, int left, int right, int order) {
             }
 }
 
+// What a form writes: fp32 or 16-bit rows [batches][rows][columns] for boxes of 64 bytes and 32 rows; false where TMA cannot address them.
+bool result_map(CUtensorMap* map, void* p, int32_t type, int64_t columns, int64_t rows, int64_t batches, int64_t row, int64_t batch) {
+    const Encode encode = map_encoder();
+    const int64_t e = type_bytes(type);
+    if (!encode || (reinterpret_cast<uintptr_t>(p) & 15u) || (row * e) % 16 || (batch * e) % 16 || row * e >= (int64_t)1 << 40 || batch * e >= (int64_t)1 << 40)
+        return false;
+    const cuuint64_t size[3] = {(cuuint64_t)columns, (cuuint64_t)rows, (cuuint64_t)batches};
+    const cuuint64_t stride[2] = {(cuuint64_t)(row * e), (cuuint64_t)(batch * e)};
+    const cuuint32_t extent[3] = {(cuuint32_t)(64 / e), 32, 1}, every[3] = {1, 1, 1};
+    const auto kind = type == kTypeF32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : type == kTypeBF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    return encode(map, kind, 3, p, size, stride, extent, every, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B,
+                  CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int FORM>
-int product(head::Args& a, const Operand& left, const Operand& right, bool f16, cudaStream_t stream, const char* what) {
+int product(head::Args& a, const Operand& left, const Operand& right, const CUtensorMap& out, bool f16, cudaStream_t stream, const char* what) {
     using O = head::Order<FORM>;
     CUtensorMap l = {}, r = {};
     if (!operand_map(&l, left, f16, O::kLeftAcross ? 64 : 128) || !operand_map(&r, right, f16, O::kRightAcross ? 64 : 128))
@@ -531,13 +545,19 @@ int product(head::Args& a, const Operand& left, const Operand& right, bool f16, 
     a.right_planes = (int32_t)right.batches;
     a.left_batch = left.batches > 1;
     a.right_batch = right.batches > 1;
+    for (int k = 0; k < a.pairs; ++k) {
+        a.left_count = std::max(a.left_count, a.left_plane[k] + 1);
+        a.right_count = std::max(a.right_count, a.right_plane[k] + 1);
+    }
+    a.stages = std::min(head::kMostStages, head::kHalves / (a.left_count + a.right_count));
+    a.stretch = std::max(1, head::kFlush / a.pairs);
     a.f16 = f16;
     a.tries = wait_tries.load(std::memory_order_relaxed);
     const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n * a.batches * a.parts;
     if (tiles > 0x3fffffff) return COMPAMS_ERR_TOO_LARGE;
     const int64_t at_once = std::max(1, multiprocessors() / 2);
     return launched(launch_sized(head::head_kernel<FORM>, dim3((uint32_t)(2 * std::min(tiles, at_once))), head::kThreads, 2, head::kShared, false,
-                                 stream, a, l, r),
+                                 stream, a, l, r, out),
                     what);
 }
 
@@ -680,7 +700,7 @@ int compams_head_forward(float* loss, float* lse, const void* x, int32_t type, c
             pairs_of(a, z.x_planes(), z.w_planes(), 2);
             a.rows = z.batch_rows(); a.columns = (int32_t)vocab; a.first = (int32_t)v0;
             a.target = target; a.target_logit = target_logit; a.stats = stats; a.all_rows = z.all_rows();
-            rc = product<head::kForward>(a, xo, wo, z.f16(), stream, "head_forward");
+            rc = product<head::kForward>(a, xo, wo, {}, z.f16(), stream, "head_forward");
         }
     }
     if (rc != COMPAMS_OK) return rc;
@@ -745,9 +765,11 @@ int compams_head_backward(void* dx, void* dweight, int32_t sum_workers, const fl
             a.segments = 1; a.steps = a.part_steps = (int32_t)((h + 63) / 64);
             pairs_of(a, z.x_planes(), z.w_planes(), 2);
             a.right_row = first; a.rows = z.batch_rows(); a.columns = (int32_t)vocab; a.first = (int32_t)v0; a.target = target;
-            a.all_rows = all; a.lse = lse; a.row_gradient = r.g; a.probs = d; a.probs_plane = all * p.width; a.width = (int32_t)p.width;
-            a.probs_planes = p.probs;
-            rc = product<head::kProbs>(a, xo, wo, z.f16(), stream, "head_probs");
+            a.all_rows = all; a.lse = lse; a.row_gradient = r.g; a.probs_planes = p.probs;
+            CUtensorMap out = {};
+            if (!result_map(&out, d, z.f16() ? kTypeF16 : kTypeBF16, p.width, z.batch_rows(), z.batches() * p.probs, p.width, z.batch_rows() * p.width))
+                return COMPAMS_ERR_INVALID_ARG;
+            rc = product<head::kProbs>(a, xo, wo, out, z.f16(), stream, "head_probs");
         }
         const Operand by_batch{d, p.width, z.batch_rows(), z.batches(), p.probs, p.width, z.batch_rows() * p.width};
         if (rc == COMPAMS_OK && dx) {
@@ -757,14 +779,14 @@ int compams_head_backward(void* dx, void* dweight, int32_t sum_workers, const fl
             // 8 bits beside an fp32 weight: two of its planes; 11 bits: to the same order
             pairs_of(a, z.x_probs(), z.copies() && type != kTypeF32 ? 2 : z.w_planes(), type == kTypeF32 ? 2 : 1);
             a.right_sum = first; a.rows = z.batch_rows();
-            if (p.sums) {
-                a.out = work + p.dx_sums; a.out_type = kTypeF32; a.out_row = z.pitch(); a.columns = (int32_t)z.pitch();
-                a.out_part = all * z.pitch(); a.add = v0 > 0;
-            } else {
-                a.out = dx; a.out_type = type; a.out_row = h; a.columns = (int32_t)h; a.scale = scale; a.worker_rows = rows;
-            }
-            a.out_batch = z.batch_rows() * a.out_row;
-            rc = product<head::kInput>(a, by_batch, wo, z.f16(), stream, "head_input");
+            void* to = p.sums ? (void*)(work + p.dx_sums) : dx;
+            a.out_row = p.sums ? z.pitch() : h;
+            a.columns = (int32_t)a.out_row; a.out_type = p.sums ? kTypeF32 : type; a.out_batch = z.batch_rows() * a.out_row;
+            if (p.sums) a.add = v0 > 0;
+            else { a.scale = scale; a.worker_rows = rows; }
+            CUtensorMap out = {};
+            if (!result_map(&out, to, a.out_type, a.out_row, z.batch_rows(), z.batches() * p.parts, a.out_row, a.out_batch)) a.out = to;
+            rc = product<head::kInput>(a, by_batch, wo, out, z.f16(), stream, "head_input");
         }
         if (rc == COMPAMS_OK && dweight) {
             // together: the workers are segments of one sum; else each is a batch
@@ -772,14 +794,15 @@ int compams_head_backward(void* dx, void* dweight, int32_t sum_workers, const fl
             a.tiles_m = (int32_t)((count + 255) / 256); a.tiles_n = tiles_h; a.batches = together ? 1 : n; a.parts = 1;
             a.segments = together ? n : 1; a.steps = a.part_steps = (int32_t)((rows + 63) / 64);
             pairs_of(a, z.w_probs(), z.x_planes(), 2);
-            a.rows = count; a.columns = (int32_t)h; a.out_type = weight_type; a.out_row = h; a.out_batch = vocab * h;
-            a.out = (char*)dweight + v0 * h * type_bytes(weight_type);
+            a.rows = count; a.columns = (int32_t)h; a.out_type = weight_type; a.out_row = h; a.out_batch = vocab * h; a.out_first = (int32_t)v0;
             a.scale = scale;
+            CUtensorMap out = {};
+            if (!result_map(&out, dweight, weight_type, h, vocab, together ? 1 : n, h, vocab * h)) a.out = dweight;
             const Operand left{d, p.width, rows, n, p.probs, p.width, rows * p.width};
             Operand right = xo;
             right.rows = rows; right.batches = n;
             if (z.shared) right.batch_stride = rows * (all > 1 ? xo.row_stride : z.pitch());
-            rc = product<head::kWeight>(a, left, right, z.f16(), stream, "head_weight");
+            rc = product<head::kWeight>(a, left, right, out, z.f16(), stream, "head_weight");
         }
     }
     if (rc != COMPAMS_OK || !p.sums || !dx) return rc;

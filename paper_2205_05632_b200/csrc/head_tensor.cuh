@@ -35,19 +35,20 @@ __device__ __forceinline__ void give_up(uint32_t* lost) {
 
 enum Form : int { kForward, kProbs, kInput, kWeight };
 
-constexpr int kTile = 256;                     // rows and columns of a pair's tile
-constexpr int kHalf = 128 * 128;               // bytes of a CTA's 128 x 64 of an operand
-constexpr int kStages = 6, kStage = 2 * kHalf;  // 32 KB a stage
-constexpr int kStaging = 8 * 4096;             // 32 rows of 128 bytes for each of the eight warps
-constexpr int kShared = 1024 + kStages * kStage + kStaging;
+constexpr int kTile = 256;          // rows and columns of a pair's tile
+constexpr int kHalf = 128 * 128;    // bytes of a CTA's 128 x 64 of an operand's plane
+constexpr int kHalves = 12;         // of them there is room for: six stages of one plane each, three of 1 + 3, two of 3 + 3
+constexpr int kMostStages = 6;
+constexpr int kStaging = 8 * 4096;  // for each of the eight warps two times 32 rows of 64 bytes
+constexpr int kShared = 1024 + kHalves * kHalf + kStaging;
 // Three groups of four warps at 168 registers; the two that keep sums take 216 and the third keeps 40: no more than the launch has.
 constexpr int kThreads = 384;
-constexpr int kSumRegisters = 216, kOtherRegisters = 40;
+constexpr int kSumRegisters = 224, kOtherRegisters = 32;
 static_assert(256 * kSumRegisters + 128 * kOtherRegisters <= kThreads * 168, "registers of the launch");
-constexpr int kFlush = 8;  // tiles of 64 between two additions to the registers
+constexpr int kFlush = 8;  // products of 64 between two additions to the registers, at most (or those of one stage)
 constexpr int kMostPairs = 6;
 // The barriers: a stage has landed (of both CTAs, at the first); its products are done; the sums are ready, and drained (at the first).
-constexpr int kFull = 0, kEmpty = kStages, kReady = 2 * kStages, kDrained = kReady + 2, kStopped = kDrained + 2, kBars = kStopped + 1;
+constexpr int kFull = 0, kEmpty = kMostStages, kReady = 2 * kMostStages, kDrained = kReady + 2, kStopped = kDrained + 2, kBars = kStopped + 1;
 
 struct Args {
     // the tiles, in this order: batch, part of the sum, row and column in groups of kRaster rows
@@ -56,6 +57,8 @@ struct Args {
     // one. A stretch ends with its segment.
     int32_t segments, steps, part_steps;
     // operands: the third coordinate is plane * planes apart + batch * batch apart; where rows and the sum begin
+    int32_t left_count, right_count;  // planes of a stage
+    int32_t stages, stretch;          // stages there is room for; stages between two additions to the registers
     int32_t pairs;
     uint8_t left_plane[kMostPairs], right_plane[kMostPairs];
     int32_t left_planes, left_batch, left_row, left_sum;
@@ -71,13 +74,12 @@ struct Args {
     float2* stats;         // FORWARD: [half tile of the vocabulary][all rows]: maximum, sum of exp(z - maximum)
     int64_t all_rows;
     const float *lse, *row_gradient;
-    uint16_t* probs;       // PROBS: [plane][all rows][width]
-    int64_t probs_plane;   // elements of a plane
-    int32_t width, probs_planes;
-    // INPUT, WEIGHT
-    void* out;             // fp32, or of out_type where it is final
-    int64_t out_part, out_batch, out_row;  // elements from part to part, batch to batch, row to row
-    int32_t out_type, add;                 // add: onto what is there (fp32)
+    int32_t probs_planes;
+    // PROBS, INPUT, WEIGHT: the third map is of what is written, [plane or part][batch][row][column] from out_first's row on
+    int32_t out_type, add;  // add: onto what is there (fp32)
+    int32_t out_first;
+    void* out;              // where the third map does not serve (rows off 16-byte boundaries); else null
+    int64_t out_batch, out_row;  // elements
     const float* scale;                    // of a worker; null: 1
     int64_t worker_rows;
 };
@@ -120,7 +122,9 @@ __device__ __forceinline__ uint32_t at_first(uint32_t address) {
     return r;
 }
 __device__ __forceinline__ void arrive_at(uint32_t cluster_bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+    // (what it orders is the reading of tensor memory, which a fence of its own stands in front of; a release for the cluster would wait
+    // for the warp's global stores as well)
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
 __device__ __forceinline__ void pair_box(uint32_t to, const CUtensorMap* map, int x, int y, int z, uint32_t cluster_bar) {
     asm volatile(
@@ -173,31 +177,33 @@ __device__ __forceinline__ void bring(const Args& a, const CUtensorMap* left, co
         const int m = a.left_row + p.m * kTile + (int)rank * 128, n = a.right_row + p.n * kTile + (int)rank * 128;
         for (int segment = 0, k = k0; segment < a.segments && k < k1; k + 1 < k1 ? ++k : (k = k0, ++segment)) {
             const int ls = a.left_sum + k * 64, rs = a.right_sum + k * 64;
-            const int lz = (p.batch + segment) * a.left_batch, rz = (p.batch + segment) * a.right_batch;
-            for (int pair = 0; pair < a.pairs; ++pair) {
-                if (!barrier_wait(bars + 8 * (kEmpty + stage), phase, a.tries)) {
-                    give_up(lost);
-                    return;
-                }
-                const uint32_t bar = bars0 + 8 * (kFull + stage), to = mem + stage * kStage;
-                if (rank == 0) mbar_expect(bars + 8 * (kFull + stage), 2 * kStage);
-                const int lp = lz + a.left_plane[pair] * a.left_planes, rp = rz + a.right_plane[pair] * a.right_planes;
+            int lz = (p.batch + segment) * a.left_batch, rz = (p.batch + segment) * a.right_batch;
+            if (!barrier_wait(bars + 8 * (kEmpty + stage), phase, a.tries)) {
+                give_up(lost);
+                return;
+            }
+            const uint32_t bar = bars0 + 8 * (kFull + stage);
+            uint32_t to = mem + stage * (a.left_count + a.right_count) * kHalf;
+            if (rank == 0) mbar_expect(bars + 8 * (kFull + stage), 2 * (a.left_count + a.right_count) * kHalf);
+            for (int c = 0; c < a.left_count; ++c, lz += a.left_planes, to += kHalf) {
                 if (O::kLeftAcross) {
-                    pair_box(to, left, m, ls, lp, bar);
-                    pair_box(to + 8192, left, m + 64, ls, lp, bar);
+                    pair_box(to, left, m, ls, lz, bar);
+                    pair_box(to + 8192, left, m + 64, ls, lz, bar);
                 } else {
-                    pair_box(to, left, ls, m, lp, bar);
+                    pair_box(to, left, ls, m, lz, bar);
                 }
+            }
+            for (int c = 0; c < a.right_count; ++c, rz += a.right_planes, to += kHalf) {
                 if (O::kRightAcross) {
-                    pair_box(to + kHalf, right, n, rs, rp, bar);
-                    pair_box(to + kHalf + 8192, right, n + 64, rs, rp, bar);
+                    pair_box(to, right, n, rs, rz, bar);
+                    pair_box(to + 8192, right, n + 64, rs, rz, bar);
                 } else {
-                    pair_box(to + kHalf, right, rs, n, rp, bar);
+                    pair_box(to, right, rs, n, rz, bar);
                 }
-                if (++stage == kStages) {
-                    stage = 0;
-                    phase ^= 1u;
-                }
+            }
+            if (++stage == a.stages) {
+                stage = 0;
+                phase ^= 1u;
             }
         }
     }
@@ -207,8 +213,8 @@ __device__ __forceinline__ void bring(const Args& a, const CUtensorMap* left, co
 template <int FORM>
 __device__ __forceinline__ void issue(const Args& a, uint32_t tiles, char* smem, uint32_t memory, uint32_t bars, uint32_t* lost) {
     using O = Order<FORM>;
-    const uint32_t mem = shared_address(smem);
-    const uint64_t left0 = operand(mem, O::kLeftAcross ? 8192 : 16), right0 = operand(mem + kHalf, O::kRightAcross ? 8192 : 16);
+    const uint32_t mem = shared_address(smem), size = (a.left_count + a.right_count) * (kHalf / 16);
+    const uint64_t left0 = operand(mem, O::kLeftAcross ? 8192 : 16), right0 = operand(mem + a.left_count * kHalf, O::kRightAcross ? 8192 : 16);
     constexpr uint32_t kLeft = (O::kLeftAcross ? 2048 : 32) / 16, kRight = (O::kRightAcross ? 2048 : 32) / 16;  // to the next 16 of the sum
     const uint32_t what = pair_instruction(!a.f16, O::kLeftAcross, O::kRightAcross);
     int stage = 0;
@@ -217,9 +223,9 @@ __device__ __forceinline__ void issue(const Args& a, uint32_t tiles, char* smem,
         const Place p = place_of(a, t);
         int k0, k1;
         steps_of(a, p, k0, k1);
-        const int all = (k1 - k0) * a.pairs;
+        const int all = k1 - k0;
         for (int segment = 0, done = 0; segment < a.segments && all > 0; done < all ? 0 : (done = 0, ++segment)) {
-            const int end = min(done + kFlush, all);
+            const int end = min(done + a.stretch, all);
             if (!barrier_wait(bars + 8 * (kDrained + buffer), drained >> buffer & 1u, a.tries)) {
                 give_up(lost);
                 return;
@@ -232,14 +238,17 @@ __device__ __forceinline__ void issue(const Args& a, uint32_t tiles, char* smem,
                     return;
                 }
                 fence_after();
-                const uint64_t l = left0 + (uint32_t)(stage * (kStage / 16)), r = right0 + (uint32_t)(stage * (kStage / 16));
+                for (int pair = 0; pair < a.pairs; ++pair) {
+                    const uint64_t l = left0 + (uint32_t)(stage * size + a.left_plane[pair] * (kHalf / 16));
+                    const uint64_t r = right0 + (uint32_t)(stage * size + a.right_plane[pair] * (kHalf / 16));
 #pragma unroll
-                for (uint32_t q = 0; q < 4; ++q) {
-                    pair_product(memory + buffer * kTile, l + q * kLeft, r + q * kRight, what, onto);
-                    onto = true;
+                    for (uint32_t q = 0; q < 4; ++q) {
+                        pair_product(memory + buffer * kTile, l + q * kLeft, r + q * kRight, what, onto);
+                        onto = true;
+                    }
                 }
                 pair_done(bars + 8 * (kEmpty + stage));
-                if (++stage == kStages) {
+                if (++stage == a.stages) {
                     stage = 0;
                     phase ^= 1u;
                 }
@@ -250,40 +259,59 @@ __device__ __forceinline__ void issue(const Args& a, uint32_t tiles, char* smem,
     }
 }
 
-// 32 rows of 128 bytes that a warp has in its staging, chunk c of row r at c ^ (r % 8), to memory. Row r goes to out + r * row (bytes);
-// rows: how many there are, bytes: of a row; fast: rows start on 16-byte boundaries and have whole chunks, else element by element.
-template <typename T, bool ADD>
-__device__ __forceinline__ void leave(const char* staging, char* out, int64_t row, int rows, int bytes, bool fast) {
-    const int lane = threadIdx.x & 31;
-    if (fast) {
-        const int c = lane & 7;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int r = i * 4 + (lane >> 3);
-            if (r < rows && c * 16 < bytes) {
-                uint4 v = *reinterpret_cast<const uint4*>(staging + swizzled(r, c));
-                uint4* to = reinterpret_cast<uint4*>(out + r * row + c * 16);
-                if (ADD) {
-                    const float4 was = *reinterpret_cast<const float4*>(to);
-                    v = make_uint4(__float_as_uint(__uint_as_float(v.x) + was.x), __float_as_uint(__uint_as_float(v.y) + was.y),
-                                   __float_as_uint(__uint_as_float(v.z) + was.z), __float_as_uint(__uint_as_float(v.w) + was.w));
-                }
-                *to = v;
+// 32 rows of 64 bytes of a warp's staging, chunk c of row r at c ^ (r / 2 % 4): the order of TMA's 64-byte swizzle.
+__device__ __forceinline__ uint32_t staged(uint32_t row, uint32_t chunk) { return row * 64u + ((chunk ^ (row >> 1 & 3u)) << 4); }
+
+// How the warps' results leave: 64 bytes of each of a warp's 32 rows at a time, from two places by turns.
+struct Exit {
+    char* places;
+    const CUtensorMap* map;
+    uint32_t turn;
+    // The place to write to next; what was brought from it before is gone.
+    __device__ __forceinline__ char* place() {
+        if ((threadIdx.x & 31) == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+        __syncwarp();
+        return places + turn * 2048;
+    }
+    __device__ __forceinline__ void leave(int column, int row, int z, bool add) {
+        fence_shared();
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) {
+            const uint32_t from = shared_address(places + turn * 2048);
+            if (add)
+                asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(map),
+                             "r"(column), "r"(row), "r"(z), "r"(from)
+                             : "memory");
+            else
+                asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(map), "r"(column), "r"(row),
+                             "r"(z), "r"(from)
+                             : "memory");
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        }
+        turn ^= 1u;
+    }
+    // Element by element, for rows that TMA cannot address: `count` of the columns and `rows` of the rows are there.
+    template <typename T>
+    __device__ __forceinline__ void leave_slowly(T* out, int64_t row, int rows, int count, bool add) {
+        __syncwarp();
+        constexpr int N = 64 / (int)sizeof(T);
+        const char* from = places + turn * 2048;
+        for (int e = threadIdx.x & 31; e < 32 * N; e += 32) {
+            const int r = e / N, c = e % N;
+            if (r < rows && c < count) {
+                T v = *reinterpret_cast<const T*>(from + staged(r, c * sizeof(T) / 16) + c * sizeof(T) % 16);
+                if constexpr (sizeof(T) == 4)
+                    if (add) v += out[r * row + c];
+                out[r * row + c] = v;
             }
         }
-    } else {
-        constexpr int N = 128 / (int)sizeof(T);
-        for (int r = 0; r < rows; ++r)
-#pragma unroll
-            for (int e = lane; e < N; e += 32)
-                if (e * (int)sizeof(T) < bytes) {
-                    T v = *reinterpret_cast<const T*>(staging + swizzled(r, e * sizeof(T) / 16) + e * sizeof(T) % 16);
-                    T* to = reinterpret_cast<T*>(out + r * row) + e;
-                    if constexpr (ADD) v = v + *to;
-                    *to = v;
-                }
+        __syncwarp();
     }
-}
+    __device__ __forceinline__ void end() {
+        if ((threadIdx.x & 31) == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        __syncwarp();
+    }
+};
 
 // Two values as one plane of the 16-bit type; what the plane leaves out stays in them.
 __device__ __forceinline__ uint32_t plane_of(float& a, float& b, bool f16, bool last) {
@@ -306,23 +334,22 @@ constexpr float kF16Scale = 16384.0f;
 
 // The first eight warps. A thread has row 32 (warp % 4) + lane of the CTA's 128 and 128 columns, from 128 (warp / 4) on.
 template <int FORM>
-__device__ __forceinline__ void finish(const Args& a, uint32_t tiles, char* staging0, uint32_t memory, uint32_t bars, uint32_t rank, uint32_t* given_up) {
+__device__ __forceinline__ void finish(const Args& a, const CUtensorMap* map, uint32_t tiles, char* staging0, uint32_t memory, uint32_t bars, uint32_t rank, uint32_t* given_up) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, half = warp >> 2;
     const uint32_t at = memory + ((uint32_t)(warp & 3) << 21) + (uint32_t)half * 128;
     const uint32_t drained0 = at_first(bars + 8 * kDrained);
-    char* staging = staging0 + warp * 4096;
+    Exit exit = {staging0 + warp * 4096, map, 0u};
     uint32_t buffer = 0, ready = 0;  // a bit for each half of the tensor memory
     bool lost = false;
     for (uint32_t t = blockIdx.x / 2; t < tiles; t += gridDim.x / 2) {
         const Place p = place_of(a, t);
         int k0, k1;
         steps_of(a, p, k0, k1);
-        const int all = (k1 - k0) * a.pairs;
+        const int all = k1 - k0;
         float sum[128];
-        if (all <= 0)  // a part of the sum behind its end
 #pragma unroll
-            for (int c = 0; c < 128; ++c) sum[c] = 0.0f;
-        for (int segment = 0, done = 0; segment < a.segments && all > 0; done + kFlush < all ? done += kFlush : (done = 0, ++segment)) {
+        for (int c = 0; c < 128; ++c) sum[c] = 0.0f;
+        for (int segment = 0, done = 0; segment < a.segments && all > 0; done + a.stretch < all ? done += a.stretch : (done = 0, ++segment)) {
             const float worth = FORM == kWeight && a.scale ? a.scale[p.batch + segment] : 1.0f;
             lost = lost || !barrier_wait(bars + 8 * (kReady + buffer), ready >> buffer & 1u, a.tries);
             ready ^= 1u << buffer;
@@ -333,16 +360,8 @@ __device__ __forceinline__ void finish(const Args& a, uint32_t tiles, char* stag
                 float v[32];
                 columns(at + buffer * kTile + c, v);
                 columns_wait(v);
-                if (FORM == kWeight) {
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) sum[c + e] = done + segment == 0 ? worth * v[e] : fmaf(worth, v[e], sum[c + e]);
-                } else if (done == 0) {
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) sum[c + e] = v[e];
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) sum[c + e] += v[e];
-                }
+                for (int e = 0; e < 32; ++e) sum[c + e] = FORM == kWeight ? fmaf(worth, v[e], sum[c + e]) : sum[c + e] + v[e];
             }
             fence_before();
             __syncwarp();
@@ -382,26 +401,23 @@ __device__ __forceinline__ void finish(const Args& a, uint32_t tiles, char* stag
                     const float d = power2((sum[c] - lse) * kLog2e) - (c == mine ? 1.0f : 0.0f);
                     sum[c] = c < left && g != 0.0f ? d * scale : 0.0f;
                 }
+                if (row0 >= a.rows) continue;
                 for (int plane = 0; plane < a.probs_planes; ++plane) {
                     const bool last = plane + 1 == a.probs_planes;
 #pragma unroll
-                    for (int part = 0; part < 2; ++part) {
-                        __syncwarp();
+                    for (int part = 0; part < 4; ++part) {
+                        char* place = exit.place();
 #pragma unroll
-                        for (int c = 0; c < 8; ++c) {
+                        for (int c = 0; c < 4; ++c) {
                             uint32_t w[4];
 #pragma unroll
                             for (int q = 0; q < 4; ++q) {
-                                const int e = part * 64 + c * 8 + q * 2;
+                                const int e = part * 32 + c * 8 + q * 2;
                                 w[q] = plane_of(sum[e], sum[e + 1], a.f16, last);
                             }
-                            *reinterpret_cast<uint4*>(staging + swizzled(lane, c)) = make_uint4(w[0], w[1], w[2], w[3]);
+                            *reinterpret_cast<uint4*>(place + staged(lane, c)) = make_uint4(w[0], w[1], w[2], w[3]);
                         }
-                        __syncwarp();
-                        const int64_t first = (int64_t)p.batch * a.rows + row0;
-                        const int rows = (int)min((int64_t)32, a.rows - row0);
-                        char* out = reinterpret_cast<char*>(a.probs + plane * a.probs_plane + first * a.width + column0 + part * 64);
-                        leave<uint16_t, false>(staging, out, (int64_t)a.width * 2, rows, 128, true);
+                        exit.leave(column0 + part * 32, row0, plane * a.batches + p.batch, false);
                     }
                 }
             }
@@ -409,51 +425,50 @@ __device__ __forceinline__ void finish(const Args& a, uint32_t tiles, char* stag
             float scale = 1.0f;
             if (FORM == kInput && a.scale) scale = there ? a.scale[((int64_t)p.batch * a.rows + row) / a.worker_rows] : 0.0f;
             if (lost) scale = nan;
-            const int rows = (int)min((int64_t)32, a.rows - row0), left = a.columns - column0;
-            const int size = a.out_type == kTypeF32 ? 4 : 2;
-            char* out = static_cast<char*>(a.out) + (p.part * a.out_part + p.batch * a.out_batch + row0 * a.out_row + column0) * size;
-            const bool fast = ((reinterpret_cast<uintptr_t>(a.out) | (uint64_t)(a.out_part * size) | (uint64_t)(a.out_batch * size) |
-                                (uint64_t)(a.out_row * size) | (uint64_t)((int64_t)a.columns * size)) & 15u) == 0;
+            const int rows = (int)min((int64_t)32, a.rows - row0), left = a.columns - column0, z = p.part * a.batches + p.batch;
+            const int64_t first = z * a.out_batch + (row0 + a.out_first) * a.out_row + column0;
+            if (rows <= 0) continue;
             if (a.out_type == kTypeF32) {
 #pragma unroll
-                for (int part = 0; part < 4; ++part) {
-                    __syncwarp();
+                for (int part = 0; part < 8; ++part) {
+                    if (part * 16 >= left) break;
+                    char* place = exit.place();
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) {
-                        const float* v = &sum[part * 32 + c * 4];
-                        *reinterpret_cast<float4*>(staging + swizzled(lane, c)) = make_float4(scale * v[0], scale * v[1], scale * v[2], scale * v[3]);
+                    for (int c = 0; c < 4; ++c) {
+                        const float* v = &sum[part * 16 + c * 4];
+                        *reinterpret_cast<float4*>(place + staged(lane, c)) = make_float4(scale * v[0], scale * v[1], scale * v[2], scale * v[3]);
                     }
-                    __syncwarp();
-                    const int bytes = (left - part * 32) * 4;
-                    if (a.add) leave<float, true>(staging, out + part * 128, a.out_row * 4, rows, bytes, fast);
-                    else leave<float, false>(staging, out + part * 128, a.out_row * 4, rows, bytes, fast);
+                    if (!a.out) exit.leave(column0 + part * 16, row0 + a.out_first, z, a.add);
+                    else exit.leave_slowly((float*)a.out + first + part * 16, a.out_row, rows, left - part * 16, a.add);
                 }
             } else {
 #pragma unroll
-                for (int part = 0; part < 2; ++part) {
-                    __syncwarp();
+                for (int part = 0; part < 4; ++part) {
+                    if (part * 32 >= left) break;
+                    char* place = exit.place();
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) {
+                    for (int c = 0; c < 4; ++c) {
                         uint32_t w[4];
 #pragma unroll
                         for (int q = 0; q < 4; ++q) {
-                            const float x = scale * sum[part * 64 + c * 8 + q * 2], y = scale * sum[part * 64 + c * 8 + q * 2 + 1];
+                            const float x = scale * sum[part * 32 + c * 8 + q * 2], y = scale * sum[part * 32 + c * 8 + q * 2 + 1];
                             w[q] = a.out_type == kTypeBF16 ? pack(x, y, __nv_bfloat16()) : pack(x, y, __half());
                         }
-                        *reinterpret_cast<uint4*>(staging + swizzled(lane, c)) = make_uint4(w[0], w[1], w[2], w[3]);
+                        *reinterpret_cast<uint4*>(place + staged(lane, c)) = make_uint4(w[0], w[1], w[2], w[3]);
                     }
-                    __syncwarp();
-                    leave<uint16_t, false>(staging, out + part * 128, a.out_row * 2, rows, (left - part * 64) * 2, fast);
+                    if (!a.out) exit.leave(column0 + part * 32, row0 + a.out_first, z, false);
+                    else exit.leave_slowly((uint16_t*)a.out + first + part * 32, a.out_row, rows, left - part * 32, false);
                 }
             }
         }
     }
+    if (FORM != kForward) exit.end();
     if (lost) give_up(given_up);
 }
 
 template <int FORM>
 __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap left,
-                                                           const __grid_constant__ CUtensorMap right) {
+                                                           const __grid_constant__ CUtensorMap right, const __grid_constant__ CUtensorMap out) {
     extern __shared__ __align__(16) char dynamic[];
     __shared__ uint64_t barriers[kBars];
     __shared__ uint32_t word[2];  // the tensor memory's address; whether someone gave up
@@ -475,7 +490,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
     dependency_wait();
     if (threadIdx.x < 256) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSumRegisters));
-        finish<FORM>(a, tiles, smem + kStages * kStage, memory, bars, rank, word + 1);
+        finish<FORM>(a, &out, tiles, smem + kHalves * kHalf, memory, bars, rank, word + 1);
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegisters));
         if (threadIdx.x == 256 && rank == 0) issue<FORM>(a, tiles, smem, memory, bars, word + 1);
