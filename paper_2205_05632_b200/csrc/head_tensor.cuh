@@ -45,7 +45,9 @@ constexpr int kShared = 1024 + kHalves * kHalf + kStaging;
 constexpr int kThreads = 384;
 constexpr int kSumRegisters = 224, kOtherRegisters = 32;
 static_assert(256 * kSumRegisters + 128 * kOtherRegisters <= kThreads * 168, "registers of the launch");
-constexpr int kFlush = 8;  // products of 64 between two additions to the registers, at most (or those of one stage)
+// Products of 64 between two additions to the registers, at most (or those of one stage). With 32 nothing is faster, and dx of fp32 is
+// 1.4e-6 off its length instead of 2.1e-7 (4 workers of 100 rows, 512 columns, a vocabulary of 8000).
+constexpr int kFlush = 8;
 constexpr int kMostPairs = 6;
 // The barriers: a stage has landed (of both CTAs, at the first); its products are done; the sums are ready, and drained (at the first).
 constexpr int kFull = 0, kEmpty = kMostStages, kReady = 2 * kMostStages, kDrained = kReady + 2, kStopped = kDrained + 2, kBars = kStopped + 1;
@@ -84,7 +86,7 @@ struct Args {
     int64_t worker_rows;
 };
 
-constexpr int kRaster = 8;
+constexpr int kRaster = 16;  // (8192 rows, 4096 columns, 100000: 19.7 ms for both passes; 4: 21.1, 8: 20.0, 32: 21.0)
 
 struct Place {
     int32_t batch, part, m, n;
@@ -155,6 +157,18 @@ template <int FORM> struct Order {
     static constexpr bool kLeftAcross = FORM == kWeight, kRightAcross = FORM == kInput || FORM == kWeight;
 };
 
+// One lane of a warp whose lanes are together.
+__device__ __forceinline__ bool elected() {
+    uint32_t is;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(is));
+    return is != 0u;
+}
+
+// A wait of a warp, which gives up as one.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, uint32_t tries) {
+    return __all_sync(0xffffffffu, barrier_wait(bar, parity, tries));
+}
+
 // ---- the parts ---------------------------------------------------------------------------------------------------------------
 
 __device__ __forceinline__ void steps_of(const Args& a, const Place& p, int& k0, int& k1) {
@@ -162,7 +176,9 @@ __device__ __forceinline__ void steps_of(const Args& a, const Place& p, int& k0,
     k1 = min(a.steps, k0 + a.part_steps);
 }
 
-// The tenth warp's thread, in both CTAs.
+// The tenth warp, in both CTAs. (It and the ninth stay together and elect a lane for what one thread does: so all that the instructions
+// take is the same for the warp and is held in its uniform registers. With one thread on its own a stage's four products cost 700 cycles to
+// issue, where the products take 512.)
 template <int FORM>
 __device__ __forceinline__ void bring(const Args& a, const CUtensorMap* left, const CUtensorMap* right, uint32_t tiles, char* smem, uint32_t bars,
                                       uint32_t rank, uint32_t* lost) {
@@ -178,29 +194,32 @@ __device__ __forceinline__ void bring(const Args& a, const CUtensorMap* left, co
         for (int segment = 0, k = k0; segment < a.segments && k < k1; k + 1 < k1 ? ++k : (k = k0, ++segment)) {
             const int ls = a.left_sum + k * 64, rs = a.right_sum + k * 64;
             int lz = (p.batch + segment) * a.left_batch, rz = (p.batch + segment) * a.right_batch;
-            if (!barrier_wait(bars + 8 * (kEmpty + stage), phase, a.tries)) {
+            if (!warp_wait(bars + 8 * (kEmpty + stage), phase, a.tries)) {
                 give_up(lost);
                 return;
             }
             const uint32_t bar = bars0 + 8 * (kFull + stage);
             uint32_t to = mem + stage * (a.left_count + a.right_count) * kHalf;
-            if (rank == 0) mbar_expect(bars + 8 * (kFull + stage), 2 * (a.left_count + a.right_count) * kHalf);
-            for (int c = 0; c < a.left_count; ++c, lz += a.left_planes, to += kHalf) {
-                if (O::kLeftAcross) {
-                    pair_box(to, left, m, ls, lz, bar);
-                    pair_box(to + 8192, left, m + 64, ls, lz, bar);
-                } else {
-                    pair_box(to, left, ls, m, lz, bar);
+            if (elected()) {
+                if (rank == 0) mbar_expect(bars + 8 * (kFull + stage), 2 * (a.left_count + a.right_count) * kHalf);
+                for (int c = 0; c < a.left_count; ++c, lz += a.left_planes, to += kHalf) {
+                    if (O::kLeftAcross) {
+                        pair_box(to, left, m, ls, lz, bar);
+                        pair_box(to + 8192, left, m + 64, ls, lz, bar);
+                    } else {
+                        pair_box(to, left, ls, m, lz, bar);
+                    }
+                }
+                for (int c = 0; c < a.right_count; ++c, rz += a.right_planes, to += kHalf) {
+                    if (O::kRightAcross) {
+                        pair_box(to, right, n, rs, rz, bar);
+                        pair_box(to + 8192, right, n + 64, rs, rz, bar);
+                    } else {
+                        pair_box(to, right, rs, n, rz, bar);
+                    }
                 }
             }
-            for (int c = 0; c < a.right_count; ++c, rz += a.right_planes, to += kHalf) {
-                if (O::kRightAcross) {
-                    pair_box(to, right, n, rs, rz, bar);
-                    pair_box(to + 8192, right, n + 64, rs, rz, bar);
-                } else {
-                    pair_box(to, right, rs, n, rz, bar);
-                }
-            }
+            __syncwarp();
             if (++stage == a.stages) {
                 stage = 0;
                 phase ^= 1u;
@@ -209,7 +228,7 @@ __device__ __forceinline__ void bring(const Args& a, const CUtensorMap* left, co
     }
 }
 
-// The ninth warp's thread, in the first CTA.
+// The ninth warp, in the first CTA.
 template <int FORM>
 __device__ __forceinline__ void issue(const Args& a, uint32_t tiles, char* smem, uint32_t memory, uint32_t bars, uint32_t* lost) {
     using O = Order<FORM>;
@@ -226,34 +245,37 @@ __device__ __forceinline__ void issue(const Args& a, uint32_t tiles, char* smem,
         const int all = k1 - k0;
         for (int segment = 0, done = 0; segment < a.segments && all > 0; done < all ? 0 : (done = 0, ++segment)) {
             const int end = min(done + a.stretch, all);
-            if (!barrier_wait(bars + 8 * (kDrained + buffer), drained >> buffer & 1u, a.tries)) {
+            if (!warp_wait(bars + 8 * (kDrained + buffer), drained >> buffer & 1u, a.tries)) {
                 give_up(lost);
                 return;
             }
             drained ^= 1u << buffer;
             fence_after();
             for (bool onto = false; done < end; ++done) {
-                if (!barrier_wait(bars + 8 * (kFull + stage), phase, a.tries)) {
+                if (!warp_wait(bars + 8 * (kFull + stage), phase, a.tries)) {
                     give_up(lost);
                     return;
                 }
                 fence_after();
-                for (int pair = 0; pair < a.pairs; ++pair) {
-                    const uint64_t l = left0 + (uint32_t)(stage * size + a.left_plane[pair] * (kHalf / 16));
-                    const uint64_t r = right0 + (uint32_t)(stage * size + a.right_plane[pair] * (kHalf / 16));
+                if (elected()) {
+                    for (int pair = 0; pair < a.pairs; ++pair) {
+                        const uint64_t l = left0 + (uint32_t)(stage * size + a.left_plane[pair] * (kHalf / 16));
+                        const uint64_t r = right0 + (uint32_t)(stage * size + a.right_plane[pair] * (kHalf / 16));
 #pragma unroll
-                    for (uint32_t q = 0; q < 4; ++q) {
-                        pair_product(memory + buffer * kTile, l + q * kLeft, r + q * kRight, what, onto);
-                        onto = true;
+                        for (uint32_t q = 0; q < 4; ++q)
+                            pair_product(memory + buffer * kTile, l + q * kLeft, r + q * kRight, what, onto || pair > 0 || q > 0);
                     }
+                    pair_done(bars + 8 * (kEmpty + stage));
                 }
-                pair_done(bars + 8 * (kEmpty + stage));
+                __syncwarp();
+                onto = true;
                 if (++stage == a.stages) {
                     stage = 0;
                     phase ^= 1u;
                 }
             }
-            pair_done(bars + 8 * (kReady + buffer));
+            if (elected()) pair_done(bars + 8 * (kReady + buffer));
+            __syncwarp();
             buffer ^= 1u;
         }
     }
@@ -473,7 +495,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
     __shared__ uint64_t barriers[kBars];
     __shared__ uint32_t word[2];  // the tensor memory's address; whether someone gave up
     char* smem = dynamic + ((1024u - (shared_address(dynamic) & 1023u)) & 1023u);
-    const uint32_t bars = shared_address(barriers), rank = cta_rank();
+    const uint32_t bars = shared_address(barriers), rank = cta_rank(), warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
     if (threadIdx.x < 32) pair_alloc(shared_address(word));
     if (threadIdx.x == 32) {
         word[1] = 0u;
@@ -493,8 +515,8 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
         finish<FORM>(a, &out, tiles, smem + kHalves * kHalf, memory, bars, rank, word + 1);
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegisters));
-        if (threadIdx.x == 256 && rank == 0) issue<FORM>(a, tiles, smem, memory, bars, word + 1);
-        else if (threadIdx.x == 288) bring<FORM>(a, &left, &right, tiles, smem, bars, rank, word + 1);
+        if (warp == 8 && rank == 0) issue<FORM>(a, tiles, smem, memory, bars, word + 1);
+        else if (warp == 9) bring<FORM>(a, &left, &right, tiles, smem, bars, rank, word + 1);
     }
     __syncwarp();
     fence_before();
@@ -502,8 +524,9 @@ __global__ void __launch_bounds__(kThreads, 1) head_kernel(const __grid_constant
     if (word[1]) {
         // products and copies may be under way that nobody waited for: the products are waited for, with a limit, and the copies are given
         // a millisecond, a hundred times what they take
-        if (threadIdx.x == 256 && rank == 0) {
-            pair_done(bars + 8 * kStopped);
+        if (warp == 8 && rank == 0) {
+            if (elected()) pair_done(bars + 8 * kStopped);
+            __syncwarp();
             barrier_wait(bars + 8 * kStopped, 0, kTries);
         }
         if (threadIdx.x == 288)
