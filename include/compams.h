@@ -503,7 +503,7 @@ int compams_norm_workspace_bytes(size_t* bytes, int32_t n, int64_t rows, int64_t
  * Root-mean-square norms around a block: with r = 1 / sqrt(mean(x^2) + eps) over the h columns,
  *   residual null:  y = x r weight (s, gate and next are null)
  *   residual given: s = residual_scale * residual + gate x r weight, rounded to residual_type (`type` or COMPAMS_F32; to 16 bits as the exact
- *                   value, rounded to fp32, would be, but for one in 10^8), and y = s q next with q = 1 / sqrt(mean(s^2) + eps) of s as it is kept.
+ *                   value, rounded to fp32, would be, but for one in a million), and y = s q next with q = 1 / sqrt(mean(s^2) + eps) of s as it is kept.
  *   stats           device float [n * rows][2], 8-byte aligned: r and q for the backward pass; may be null.
  *   weight, gate, next   device fp32; element c of worker i at i * stride + c (stride 0: one for all workers); null: 1.
  */

@@ -13,11 +13,12 @@
 // these cost no reading of their own. Rows above kLongest are read again instead, and their sums grow in the workspace.
 //
 // Precision. Everything is fp32 between the reading and the writing. s is kept in the residual's type and normalised as it is kept. In a
-// 16-bit type a difference in the last bit of fp32 may put s on the other side of a border between two of its values: a row's mean of
-// squares is summed with its rounding errors, and an s that is nearer to a border than the fp32 error is formed again in binary64; so s is
-// the exact sum, rounded to fp32 and then to 16 bits, but for one in 10^8, and with it what the backward pass reads (with fp32 alone one s
-// in 30000 differs, and dv by 1.3e-5 of its length).
+// 16-bit type a difference in the last bit of fp32 may put s on the other side of a border between two of its values: a row's squares are
+// summed in binary64, and an s that is nearer to a border than the fp32 error is formed again in binary64; so s is the exact sum,
+// rounded to fp32 and then to 16 bits, but for one in a million, and with it what the backward pass reads (with fp32 alone one s in 30000
+// differs, and dv by 1.3e-5 of its length).
 #include <algorithm>
+#include <atomic>
 #include <type_traits>
 
 #include "context.h"
@@ -27,6 +28,7 @@ namespace compams {
 namespace {
 
 constexpr int kMostThreads = 512;                      // of a row
+constexpr int kForwardBytes = 96 * 1024, kBackwardBytes = 200 * 1024;  // of a CTA's rows that come ahead: two CTAs to an SM, and one
 constexpr int64_t kLongest = 16 * (int64_t)kMostThreads;  // columns that they keep
 
 struct BlockArgs {
@@ -44,32 +46,43 @@ struct BlockArgs {
 };
 
 // A thread's eight columns of a row, part k of several: neighbours on a 16-byte boundary (VEC), or every blockDim.x-th.
-template <typename T, bool VEC> struct Cell { Raw8<T> raw; };
-template <typename T> struct Cell<T, false> { float v[8]; };
-
 template <bool VEC> __device__ __forceinline__ int cell_column(int k, int e) {
     return VEC ? (k * (int)blockDim.x + (int)threadIdx.x) * 8 + e : (k * 8 + e) * (int)blockDim.x + (int)threadIdx.x;
 }
-template <typename T, bool VEC>
-__device__ __forceinline__ void cell_load(Cell<T, VEC>& c, const T* row, int k, int h, bool there) {
-    if constexpr (VEC) {
-        c.raw = {};
-        if (there && cell_column<VEC>(k, 0) < h) c.raw = raw_load<T>(row + cell_column<VEC>(k, 0));
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int at = cell_column<VEC>(k, e);
-            c.v[e] = there && at < h ? to_float(__ldg(row + at)) : 0.0f;
-        }
-    }
+// Rows come ahead. VEC: by asynchronous copies into places of a thread's own in shared memory, `depth` rows of them, of which it waits for
+// the oldest; a row's cells stand there until its turn is over. Elsewhere the next row waits in registers.
+template <typename T> constexpr int kChunks = (int)sizeof(T) / 2;  // of 16 bytes, for eight columns
+__host__ __device__ constexpr int depth_of(int chunks, int bytes) {  // of rows whose threads hold so many chunks each
+    const int d = bytes / (chunks * 16 * kMostThreads);
+    return d < 1 ? 1 : d > 4 ? 4 : d;
 }
-template <typename T, bool VEC>
-__device__ __forceinline__ void cell_values(const Cell<T, VEC>& c, float (&v)[8]) {
-    if constexpr (VEC) {
-        raw_floats<T>(c.raw, v);
-    } else {
+// A tensor's cells of a row: `first` chunks stand in front of them in a thread's place.
+template <typename T>
+__device__ __forceinline__ void cell_fetch(uint4* place, int first, const T* row, int k, int h, bool there, int pitch) {
+    const int at = cell_column<true>(k, 0);
+    const bool in = there && at < h;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = c.v[e];
+    for (int c = 0; c < kChunks<T>; ++c)
+        copy16(place + (first + k * kChunks<T> + c) * pitch, in ? (const void*)(row + at + c * (8 / kChunks<T>)) : (const void*)row, in);
+}
+template <typename T>
+__device__ __forceinline__ void cell_take(const uint4* place, int first, int k, int pitch, float (&v)[8]) {
+    Raw8<T> raw;
+    const uint4* at = place + (first + k * kChunks<T>) * pitch;
+    if constexpr (std::is_same_v<T, float>) {
+        raw.a = *reinterpret_cast<const float4*>(at);
+        raw.b = *reinterpret_cast<const float4*>(at + pitch);
+    } else {
+        raw.q = *at;
+    }
+    raw_floats<T>(raw, v);
+}
+template <typename T>
+__device__ __forceinline__ void cell_load(const T* row, int k, int h, bool there, float (&v)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const int at = cell_column<false>(k, e);
+        v[e] = there && at < h ? to_float(__ldg(row + at)) : 0.0f;
     }
 }
 // Rounds to T and stores; v becomes what was stored.
@@ -108,35 +121,45 @@ __device__ __forceinline__ V row_sum(V v, V* scratch, int& turn) {
     if (threads <= 32) return v;
     V* place = scratch + (threadIdx.y * 2 + turn) * 16;
     turn ^= 1;
-    const int warps = threads >> 5;
     if ((threadIdx.x & 31) == 0) place[threadIdx.x >> 5] = v;
     asm volatile("bar.sync %0, %1;" ::"r"((int)threadIdx.y + 1), "r"(threads) : "memory");
-    V sum = place[0];
-    for (int w = 1; w < warps; ++w) sum += place[w];
-    return sum;
+    V some[4];  // (places without a warp hold zeros)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) some[k] = (place[4 * k] + place[4 * k + 1]) + (place[4 * k + 2] + place[4 * k + 3]);
+    return (some[0] + some[1]) + (some[2] + some[3]);
+}
+template <typename V>
+__device__ __forceinline__ void clear_scratch(V* scratch) {
+    for (int k = threadIdx.y * blockDim.x + threadIdx.x; k < kScratch; k += blockDim.x * blockDim.y) scratch[k] = V(0);
 }
 
-// Whether the fp32 sum s of p and q is so near to a border between two values of the type that its error may have carried it over.
+// Whether the fp32 sum s of p and q, which is `rounded` in the 16-bit type, is so near to a border between two of its values that its
+// error, 7 2^-24 of |p| + |q| at most, may have carried it over: its distance from `rounded` is then half a step.
 template <typename T>
-__device__ __forceinline__ bool near_border(float s, float p, float q) {
-    constexpr uint32_t kDropped = std::is_same_v<T, __nv_bfloat16> ? 16 : 13;
-    const int off = (int)(__float_as_uint(s) & ((1u << kDropped) - 1)) - (1 << (kDropped - 1));
-    return fabsf((float)off) * fabsf(s) <= 8.0f * (fabsf(p) + fabsf(q));
+__device__ __forceinline__ bool near_border(float s, float rounded, float p, float q) {
+    constexpr bool kHalfType = std::is_same_v<T, __half>;
+    float half_step = __uint_as_float(__float_as_uint(s) & 0x7f800000u) * (kHalfType ? 0x1p-11f : 0x1p-8f);
+    if (kHalfType) half_step = fmaxf(half_step, 0x1p-25f);
+    return fabsf(fabsf(s - rounded) - half_step) <= 0x1p-21f * (fabsf(p) + fabsf(q));
 }
 
-// Adds a square, exact in fp32 for 16-bit numbers, to a sum, and what the sum's rounding leaves out to `lost` (Knuth's two-sum).
-__device__ __forceinline__ void add_square(float x, float& sum, float& lost) {
-    const float term = x * x, grown = sum + term, part = grown - sum;
-    lost += (sum - (grown - part)) + (term - part);
-    sum = grown;
+// 1 / sqrt(v) in binary64 from its fp32 approximation, by a step of Newton's: off by about 2^-46.
+__device__ __forceinline__ double root64(double v, float r) { return (double)r * (1.5 - 0.5 * v * ((double)r * (double)r)); }
+// The sum of eight squares of 16-bit numbers, which are exact in fp32, in binary64. (Pairs of bf16's in fp32, which halves the conversions,
+// are off by 2^-33 of the sum: enough for three of 4 million s.)
+__device__ __forceinline__ double squares8(const float (&v)[8]) {
+    double s[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) s[k] = (double)(v[2 * k] * v[2 * k]) + (double)(v[2 * k + 1] * v[2 * k + 1]);
+    return (s[0] + s[1]) + (s[2] + s[3]);
 }
 
 template <typename T, typename R, bool GATED, bool VEC, int K>
 __global__ void __launch_bounds__(kMostThreads, K == 1 ? 2 : 1) block_forward_kernel(const __grid_constant__ BlockArgs a) {
     constexpr bool kWide = GATED && !std::is_same_v<R, float>;  // s is rounded to 16 bits
     using Sum = std::conditional_t<kWide, double, float>;
-    __shared__ Sum scratch[kScratch];
-    __shared__ float scratch2[kScratch];
+    __shared__ __align__(16) Sum scratch[kScratch];
+    __shared__ __align__(16) float scratch2[kScratch];
     const uint32_t worker = blockIdx.y, group = blockIdx.x * blockDim.y + threadIdx.y, rounds = (a.rows + a.groups - 1) / a.groups;
     const T* x = (const T*)a.x + (int64_t)worker * a.x_ws;
     const R* residual = GATED ? (const R*)a.residual + (int64_t)worker * a.r_ws : nullptr;
@@ -155,40 +178,66 @@ __global__ void __launch_bounds__(kMostThreads, K == 1 ? 2 : 1) block_forward_ke
         }
     }
     const float inverse = 1.0f / (float)a.h;
+    const double inverse64 = 1.0 / (double)a.h;
     int turn = 0, turn2 = 0;
-    Cell<T, VEC> cx[K];
-    Cell<R, VEC> cr[K];
-    auto fetch = [&](uint32_t j) {
-        const bool there = group < a.groups && j < a.rows;
+    clear_scratch(scratch);
+    clear_scratch(scratch2);
+    __syncthreads();
+    constexpr int kRowChunks = K * (kChunks<T> + (GATED ? kChunks<R> : 0)), kDepth = depth_of(kRowChunks, kForwardBytes);
+    extern __shared__ __align__(16) uint4 ring[];
+    const int pitch = (int)(blockDim.x * blockDim.y), tid = (int)(threadIdx.y * blockDim.x + threadIdx.x);
+    float nx[K][8], nr[K][8];  // the next row, where it waits in registers
+    auto fetch = [&](uint32_t round) {
+        const uint32_t j = group + round * a.groups;
+        const bool there = round < rounds && j < a.rows;
+        const T* from = x + (there ? (int64_t)j * a.x_rs : 0);
+        const R* also = GATED ? residual + (there ? (int64_t)j * a.r_rs : 0) : nullptr;
+        uint4* place = ring + (round % kDepth) * kRowChunks * pitch + tid;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            cell_load<T, VEC>(cx[k], x + (there ? (int64_t)j * a.x_rs : 0), k, a.h, there);
-            if (GATED) cell_load<R, VEC>(cr[k], residual + (there ? (int64_t)j * a.r_rs : 0), k, a.h, there);
-        }
-    };
-    fetch(group);
-    for (uint32_t round = 0, j = group; round < rounds; ++round, j += a.groups) {
-        const bool there = group < a.groups && j < a.rows;
-        float xs[K][8], rs[K][8];
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-            cell_values<T, VEC>(cx[k], xs[k]);
-            if (GATED) cell_values<R, VEC>(cr[k], rs[k]);
-        }
-        if (round + 1 < rounds) fetch(j + a.groups);
-        float sum = 0.0f, lost = 0.0f;
-#pragma unroll
-        for (int k = 0; k < K; ++k)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                if (kWide) add_square(xs[k][e], sum, lost);
-                else sum = fmaf(xs[k][e], xs[k][e], sum);
+            if constexpr (VEC) {
+                cell_fetch<T>(place, 0, from, k, a.h, there, pitch);
+                if (GATED) cell_fetch<R>(place, K * kChunks<T>, also, k, a.h, there, pitch);
+            } else {
+                cell_load<T>(from, k, a.h, there, nx[k]);
+                if (GATED) cell_load<R>(also, k, a.h, there, nr[k]);
             }
-        const Sum all = row_sum<Sum>(kWide ? (Sum)sum + (Sum)lost : (Sum)sum, scratch, turn);
+        }
+        if (VEC) copies_commit();
+    };
+    for (uint32_t round = 0; round < (VEC ? kDepth - 1 : 1); ++round) fetch(round);
+    for (uint32_t round = 0, j = group; round < rounds; ++round, j += a.groups) {
+        const bool there = j < a.rows;
+        float xs[K][8], rs[K][8];
+        if (VEC) {
+            fetch(round + kDepth - 1);
+            copies_wait<kDepth - 1>();
+        }
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            if constexpr (VEC) {
+                cell_take<T>(ring + (round % kDepth) * kRowChunks * pitch + tid, 0, k, pitch, xs[k]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) xs[k][e] = nx[k][e], rs[k][e] = GATED ? nr[k][e] : 0.0f;
+            }
+        }
+        if (!VEC) fetch(round + 1);
+        Sum sum = 0;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            if constexpr (kWide) {
+                sum += squares8(xs[k]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum = fmaf(xs[k][e], xs[k][e], sum);
+            }
+        }
+        const Sum all = row_sum<Sum>(sum, scratch, turn);
         double exact = 0.0;
         float r;
         if constexpr (kWide) {
-            exact = all / a.h + (double)a.eps;
+            exact = all * inverse64 + (double)a.eps;
             r = 1.0f / sqrtf((float)exact);
         } else {
             r = 1.0f / sqrtf(all * inverse + a.eps);
@@ -208,16 +257,17 @@ __global__ void __launch_bounds__(kMostThreads, K == 1 ? 2 : 1) block_forward_ke
             float squares = 0.0f;
 #pragma unroll
             for (int k = 0; k < K; ++k) {
+                if (VEC) cell_take<R>(ring + (round % kDepth) * kRowChunks * pitch + tid, K * kChunks<T>, k, pitch, rs[k]);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const float p = a.alpha * rs[k][e], q = xs[k][e] * r * w[k][e];
                     float t = p + q;
                     if constexpr (kWide)
-                        if (near_border<R>(t, p, q)) {
+                        if (near_border<R>(t, to_float(from_float<R>(t)), p, q)) {
                             const int at = cell_column<VEC>(k, e);
                             if (at < a.h) {
                                 const double g = (weight ? (double)weight[at] : 1.0) * (gate ? (double)gate[at] : 1.0);
-                                t = (float)(a.alpha64 * (double)rs[k][e] + (double)xs[k][e] / sqrt(exact) * g);
+                                t = (float)(a.alpha64 * (double)rs[k][e] + (double)xs[k][e] * root64(exact, r) * g);
                             }
                         }
                     rs[k][e] = t;
@@ -264,43 +314,70 @@ __global__ void __launch_bounds__(kMostThreads, 1) block_backward_kernel(const _
     }
     const float inverse = 1.0f / (float)a.h;
     int turn = 0;
-    Cell<T, VEC> cx[K], cy[K];
-    Cell<R, VEC> cs[K], cd[K];
+    clear_scratch(scratch);
+    __syncthreads();
+    // chunks of a row: dy, x, then s and ds
+    constexpr int kY = 0, kX = K * kChunks<T>, kS = 2 * kX, kD = kS + K * kChunks<R>;
+    constexpr int kRowChunks = GATED ? kD + K * kChunks<R> : kS, kDepth = depth_of(kRowChunks, kBackwardBytes);
+    extern __shared__ __align__(16) uint4 ring[];
+    const int pitch = (int)(blockDim.x * blockDim.y), tid = (int)(threadIdx.y * blockDim.x + threadIdx.x);
+    float nx[K][8], ny[K][8], ns[K][8], nd[K][8];  // the next row, where it waits in registers
     float2 next_stats = {};
-    auto fetch = [&](uint32_t j) {
-        const bool there = group < a.groups && j < a.rows;
+    auto stats_of = [&](uint32_t j) { return j < a.rows ? __ldg(a.stats + (int64_t)worker * a.rows + j) : make_float2(0.0f, 0.0f); };
+    auto fetch = [&](uint32_t round) {
+        const uint32_t j = group + round * a.groups;
+        const bool there = round < rounds && j < a.rows;
         const int64_t at = there ? j : 0;
+        uint4* place = ring + (round % kDepth) * kRowChunks * pitch + tid;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            cell_load<T, VEC>(cx[k], x + at * a.x_rs, k, a.h, there);
-            cell_load<T, VEC>(cy[k], dy + at * a.dy_rs, k, a.h, there);
-            if (GATED) {
-                cell_load<R, VEC>(cs[k], s + at * a.h, k, a.h, there);
-                if (ds) cell_load<R, VEC>(cd[k], ds + at * a.ds_rs, k, a.h, there);
-                else cd[k] = {};
+            if constexpr (VEC) {
+                cell_fetch<T>(place, kY, dy + at * a.dy_rs, k, a.h, there, pitch);
+                cell_fetch<T>(place, kX, x + at * a.x_rs, k, a.h, there, pitch);
+                if (GATED) {
+                    cell_fetch<R>(place, kS, s + at * a.h, k, a.h, there, pitch);
+                    cell_fetch<R>(place, kD, ds ? ds + at * a.ds_rs : s, k, a.h, there && ds, pitch);
+                }
+            } else {
+                cell_load<T>(dy + at * a.dy_rs, k, a.h, there, ny[k]);
+                cell_load<T>(x + at * a.x_rs, k, a.h, there, nx[k]);
+                if (GATED) {
+                    cell_load<R>(s + at * a.h, k, a.h, there, ns[k]);
+                    cell_load<R>(ds ? ds + at * a.ds_rs : s, k, a.h, there && ds, nd[k]);
+                }
             }
         }
-        next_stats = there ? __ldg(a.stats + (int64_t)worker * a.rows + j) : make_float2(0.0f, 0.0f);
+        if (VEC) copies_commit();
     };
-    fetch(group);
+    for (uint32_t round = 0; round < (VEC ? kDepth - 1 : 1); ++round) fetch(round);
+    next_stats = stats_of(group);
     for (uint32_t round = 0, j = group; round < rounds; ++round, j += a.groups) {
-        const bool there = group < a.groups && j < a.rows;
+        const bool there = j < a.rows;
         const float r = next_stats.x, q = next_stats.y;
-        float xs[K][8], g[K][8];  // x; the gradient of what the norm behind x gives
+        next_stats = stats_of(j + a.groups);
+        float xs[K][8], g[K][8], ss[K][8], dd[K][8];  // x; the gradient of what the norm behind x gives; s; ds
+        const uint4* place = ring + (round % kDepth) * kRowChunks * pitch + tid;
+        if (VEC) {
+            fetch(round + kDepth - 1);
+            copies_wait<kDepth - 1>();
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            cell_values<T, VEC>(cx[k], xs[k]);
-            cell_values<T, VEC>(cy[k], g[k]);
+            for (int k = 0; k < K; ++k) {
+                cell_take<T>(place, kY, k, pitch, g[k]);
+                if (GATED) cell_take<R>(place, kS, k, pitch, ss[k]);
+                else cell_take<T>(place, kX, k, pitch, xs[k]);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    xs[k][e] = nx[k][e], g[k][e] = ny[k][e];
+                    if (GATED) ss[k][e] = ns[k][e], dd[k][e] = nd[k][e];
+                }
+            fetch(round + 1);
         }
         const int64_t number = (int64_t)worker * a.rows + j;
         if constexpr (GATED) {
-            float ss[K][8], dd[K][8];
-#pragma unroll
-            for (int k = 0; k < K; ++k) {
-                cell_values<R, VEC>(cs[k], ss[k]);
-                cell_values<R, VEC>(cd[k], dd[k]);
-            }
-            if (round + 1 < rounds) fetch(j + a.groups);
             float dot = 0.0f;
 #pragma unroll
             for (int k = 0; k < K; ++k)
@@ -314,6 +391,10 @@ __global__ void __launch_bounds__(kMostThreads, 1) block_backward_kernel(const _
             const float mean = row_sum<float>(dot, scratch, turn) * inverse;
 #pragma unroll
             for (int k = 0; k < K; ++k) {
+                if (VEC) {
+                    cell_take<R>(place, kD, k, pitch, dd[k]);
+                    cell_take<T>(place, kX, k, pitch, xs[k]);
+                }
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     g[k][e] = fmaf(q, fmaf(-mean, ss[k][e], g[k][e]), dd[k][e]);
@@ -321,8 +402,6 @@ __global__ void __launch_bounds__(kMostThreads, 1) block_backward_kernel(const _
                 }
                 if (a.dresidual) cell_store<R, VEC>((R*)a.dresidual + number * a.h, k, a.h, there, dd[k]);
             }
-        } else {
-            if (round + 1 < rounds) fetch(j + a.groups);
         }
         float dot = 0.0f;
 #pragma unroll
@@ -344,7 +423,7 @@ __global__ void __launch_bounds__(kMostThreads, 1) block_backward_kernel(const _
             }
         }
     }
-    if (!a.partial || group >= a.groups) return;
+    if (!a.partial) return;
     float* out = a.partial + ((int64_t)worker * a.groups + group) * 2 * a.h;
 #pragma unroll
     for (int k = 0; k < K; ++k)
@@ -362,8 +441,11 @@ __global__ void __launch_bounds__(kMostThreads, 1) block_backward_kernel(const _
 template <typename T, typename R, bool GATED>
 __global__ void __launch_bounds__(kMostThreads) long_forward_kernel(const __grid_constant__ BlockArgs a) {
     constexpr bool kWide = GATED && !std::is_same_v<R, float>;
-    __shared__ double scratch[kScratch];
-    __shared__ float scratch2[kScratch];
+    __shared__ __align__(16) double scratch[kScratch];
+    __shared__ __align__(16) float scratch2[kScratch];
+    clear_scratch(scratch);
+    clear_scratch(scratch2);
+    __syncthreads();
     const uint32_t worker = blockIdx.y;
     const float *weight = a.weight ? a.weight + worker * a.weight_ws : nullptr, *gate = a.gate ? a.gate + worker * a.gate_ws : nullptr;
     const float* next = a.next ? a.next + worker * a.next_ws : nullptr;
@@ -377,13 +459,13 @@ __global__ void __launch_bounds__(kMostThreads) long_forward_kernel(const __grid
         R* s = GATED ? (R*)a.s + number * a.h : nullptr;
         double sum = 0.0;
         for (int c0 = threadIdx.x; c0 < a.h; c0 += 8 * kMostThreads) {
-            float some = 0.0f, lost = 0.0f;
+            float v[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const int c = c0 + e * kMostThreads;
-                add_square(c < a.h ? to_float(__ldg(x + c)) : 0.0f, some, lost);
+                v[e] = c < a.h ? to_float(__ldg(x + c)) : 0.0f;
             }
-            sum += (double)some + (double)lost;
+            sum += squares8(v);
         }
         const double exact = row_sum<double>(sum, scratch, turn) / a.h + (double)a.eps;
         const float r = 1.0f / sqrtf((float)exact);
@@ -396,8 +478,8 @@ __global__ void __launch_bounds__(kMostThreads) long_forward_kernel(const __grid
                 const float p = a.alpha * to_float(__ldg(residual + c)), u = v * r * (w * (gate ? __ldg(gate + c) : 1.0f));
                 float t = p + u;
                 if constexpr (kWide)
-                    if (near_border<R>(t, p, u))
-                        t = (float)(a.alpha64 * (double)to_float(__ldg(residual + c)) + (double)v / sqrt(exact) * ((double)w * (gate ? (double)gate[c] : 1.0)));
+                    if (near_border<R>(t, to_float(from_float<R>(t)), p, u))
+                        t = (float)(a.alpha64 * (double)to_float(__ldg(residual + c)) + (double)v * root64(exact, r) * ((double)w * (gate ? (double)gate[c] : 1.0)));
                 s[c] = from_float<R>(t);
                 t = to_float(from_float<R>(t));
                 squares = fmaf(t, t, squares);
@@ -413,7 +495,9 @@ __global__ void __launch_bounds__(kMostThreads) long_forward_kernel(const __grid
 }
 template <typename T, typename R, bool GATED>
 __global__ void __launch_bounds__(kMostThreads) long_backward_kernel(const __grid_constant__ BlockArgs a) {
-    __shared__ float scratch[kScratch];
+    __shared__ __align__(16) float scratch[kScratch];
+    clear_scratch(scratch);
+    __syncthreads();
     const uint32_t worker = blockIdx.y;
     const float *weight = a.weight ? a.weight + worker * a.weight_ws : nullptr, *gate = a.gate ? a.gate + worker * a.gate_ws : nullptr;
     const float* next = a.next ? a.next + worker * a.next_ws : nullptr;
@@ -543,23 +627,51 @@ int launched(cudaError_t e, const char* what) { return e == cudaSuccess ? COMPAM
 bool float_aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 bool vector_parameter(const float* p, int64_t ws) { return !p || (((reinterpret_cast<uintptr_t>(p) | (uint64_t)(ws * 4)) & 15u) == 0); }
 
+// Shared memory for rows of so many 16-byte chunks a thread.
+int ring_bytes(const BlockShape& z, bool vec, int chunks, int bytes) {
+    return vec ? depth_of(chunks, bytes) * chunks * 16 * z.threads() * z.rows_of_cta() : 0;
+}
+template <auto kernel>
+cudaError_t allow(int bytes) {  // more than 48 KB, the static part included: asked once for every device
+    static std::atomic<uint64_t> known{0};
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess || bytes <= 40 * 1024 || (device < 64 && known.load(std::memory_order_relaxed) >> device & 1u)) return e;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024);
+    if (e == cudaSuccess && device < 64) known.fetch_or((uint64_t)1 << device, std::memory_order_relaxed);
+    return e;
+}
+template <typename T, typename R, bool GATED, bool VEC, int K>
+int block_forward(BlockArgs& a, const BlockShape& z, cudaStream_t stream) {
+    constexpr auto kernel = block_forward_kernel<T, R, GATED, VEC, K>;
+    const int bytes = ring_bytes(z, VEC, K * (kChunks<T> + (GATED ? kChunks<R> : 0)), kForwardBytes);
+    cudaError_t e = allow<kernel>(bytes);
+    if (e == cudaSuccess)
+        e = launch_plain(kernel, dim3(a.groups / z.rows_of_cta(), (uint32_t)z.n), dim3((uint32_t)z.threads(), (uint32_t)z.rows_of_cta()), bytes, stream, a);
+    return launched(e, "block_forward");
+}
+template <typename T, typename R, bool GATED, bool VEC, int K>
+int block_backward(BlockArgs& a, const BlockShape& z, cudaStream_t stream) {
+    constexpr auto kernel = block_backward_kernel<T, R, GATED, VEC, K>;
+    const int bytes = ring_bytes(z, VEC, 2 * K * (kChunks<T> + (GATED ? kChunks<R> : 0)), kBackwardBytes);
+    cudaError_t e = allow<kernel>(bytes);
+    if (e == cudaSuccess)
+        e = launch_plain(kernel, dim3(a.groups / z.rows_of_cta(), (uint32_t)z.n), dim3((uint32_t)z.threads(), (uint32_t)z.rows_of_cta()), bytes, stream, a);
+    return launched(e, "block_backward");
+}
 template <typename T, typename R, bool GATED>
 int block_forward(BlockArgs& a, const BlockShape& z, bool vec, cudaStream_t stream) {
     if (z.h > kLongest)
         return launched(launch_plain(long_forward_kernel<T, R, GATED>, dim3(a.groups, (uint32_t)z.n), dim3(kMostThreads), 0, stream, a), "block_forward");
-    const auto kernel = z.parts() == 1 ? (vec ? block_forward_kernel<T, R, GATED, true, 1> : block_forward_kernel<T, R, GATED, false, 1>)
-                                       : (vec ? block_forward_kernel<T, R, GATED, true, 2> : block_forward_kernel<T, R, GATED, false, 2>);
-    return launched(launch_plain(kernel, dim3(a.groups / z.rows_of_cta(), (uint32_t)z.n), dim3((uint32_t)z.threads(), (uint32_t)z.rows_of_cta()), 0, stream, a),
-                    "block_forward");
+    if (z.parts() == 1) return vec ? block_forward<T, R, GATED, true, 1>(a, z, stream) : block_forward<T, R, GATED, false, 1>(a, z, stream);
+    return vec ? block_forward<T, R, GATED, true, 2>(a, z, stream) : block_forward<T, R, GATED, false, 2>(a, z, stream);
 }
 template <typename T, typename R, bool GATED>
 int block_backward(BlockArgs& a, const BlockShape& z, bool vec, cudaStream_t stream) {
     if (z.h > kLongest)
         return launched(launch_plain(long_backward_kernel<T, R, GATED>, dim3(a.groups, (uint32_t)z.n), dim3(kMostThreads), 0, stream, a), "block_backward");
-    const auto kernel = z.parts() == 1 ? (vec ? block_backward_kernel<T, R, GATED, true, 1> : block_backward_kernel<T, R, GATED, false, 1>)
-                                       : (vec ? block_backward_kernel<T, R, GATED, true, 2> : block_backward_kernel<T, R, GATED, false, 2>);
-    return launched(launch_plain(kernel, dim3(a.groups / z.rows_of_cta(), (uint32_t)z.n), dim3((uint32_t)z.threads(), (uint32_t)z.rows_of_cta()), 0, stream, a),
-                    "block_backward");
+    if (z.parts() == 1) return vec ? block_backward<T, R, GATED, true, 1>(a, z, stream) : block_backward<T, R, GATED, false, 1>(a, z, stream);
+    return vec ? block_backward<T, R, GATED, true, 2>(a, z, stream) : block_backward<T, R, GATED, false, 2>(a, z, stream);
 }
 
 }  // namespace

@@ -11,6 +11,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 namespace compams {
 
 constexpr int kSpan = 256;
@@ -322,9 +324,16 @@ inline bool make_drop(Drop& d, double p, uint64_t seed, uint32_t call, const int
 
 enum : int32_t { kTypeF32 = 0, kTypeBF16 = 1, kTypeF16 = 2 };
 
+// SMs of the current device; asked once for every device.
 inline int multiprocessors() {
+    static std::atomic<int> known[64];
     int device = 0, sms = 148;
-    if (cudaGetDevice(&device) == cudaSuccess) cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
+    if (cudaGetDevice(&device) == cudaSuccess) {
+        const int here = device < 64 ? known[device].load(std::memory_order_relaxed) : 0;
+        if (here) return here;
+        if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) == cudaSuccess && device < 64)
+            known[device].store(sms, std::memory_order_relaxed);
+    }
     cudaGetLastError();
     return sms;
 }
