@@ -27,8 +27,10 @@
 namespace compams {
 namespace {
 
+constexpr float kInf = __builtin_inff();
 constexpr int kMostThreads = 512;                      // of a row
-constexpr int kForwardBytes = 96 * 1024, kBackwardBytes = 200 * 1024;  // of a CTA's rows that come ahead: two CTAs to an SM, and one
+constexpr int kForwardBytes = 96 * 1024, kBackwardBytes = 200 * 1024;  // of the rows that come ahead, for 512 threads
+constexpr int kNarrow = 1024;                          // columns up to which a thread keeps eight of them, else sixteen
 constexpr int64_t kLongest = 16 * (int64_t)kMostThreads;  // columns that they keep
 
 struct BlockArgs {
@@ -66,7 +68,7 @@ __device__ __forceinline__ void cell_fetch(uint4* place, int first, const T* row
         copy16(place + (first + k * kChunks<T> + c) * pitch, in ? (const void*)(row + at + c * (8 / kChunks<T>)) : (const void*)row, in);
 }
 template <typename T>
-__device__ __forceinline__ void cell_take(const uint4* place, int first, int k, int pitch, float (&v)[8]) {
+__device__ __forceinline__ void cell_take(const uint4* place, int first, int k, int pitch, Pair (&v)[4]) {
     Raw8<T> raw;
     const uint4* at = place + (first + k * kChunks<T>) * pitch;
     if constexpr (std::is_same_v<T, float>) {
@@ -75,39 +77,47 @@ __device__ __forceinline__ void cell_take(const uint4* place, int first, int k, 
     } else {
         raw.q = *at;
     }
-    raw_floats<T>(raw, v);
+    raw_pairs<T>(raw, v);
 }
 template <typename T>
-__device__ __forceinline__ void cell_load(const T* row, int k, int h, bool there, float (&v)[8]) {
+__device__ __forceinline__ void cell_load(const T* row, int k, int h, bool there, Pair (&v)[4]) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const int at = cell_column<false>(k, e);
-        v[e] = there && at < h ? to_float(__ldg(row + at)) : 0.0f;
+    for (int p = 0; p < 4; ++p) {
+        const int at = cell_column<false>(k, 2 * p), next = cell_column<false>(k, 2 * p + 1);
+        v[p] = pair(there && at < h ? to_float(__ldg(row + at)) : 0.0f, there && next < h ? to_float(__ldg(row + next)) : 0.0f);
     }
 }
-// Rounds to T and stores; v becomes what was stored.
-template <typename T, bool VEC>
-__device__ __forceinline__ void cell_store(T* row, int k, int h, bool there, float (&v)[8]) {
+// Rounds to T and stores; v becomes what was stored where KEEP.
+template <typename T, bool VEC, bool KEEP = false>
+__device__ __forceinline__ void cell_store(T* row, int k, int h, bool there, Pair (&v)[4]) {
+    const Raw8<T> raw = pack_pairs<T>(v);
     if constexpr (VEC) {
-        if (there && cell_column<VEC>(k, 0) < h) store8<T>(row + cell_column<VEC>(k, 0), v);
+        if (there && cell_column<VEC>(k, 0) < h) raw_store<T>(row + cell_column<VEC>(k, 0), raw);
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int at = cell_column<VEC>(k, e);
-            if (there && at < h) row[at] = from_float<T>(v[e]);
+        for (int p = 0; p < 4; ++p) {
+            float x[2];
+            halves(v[p], x[0], x[1]);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int at = cell_column<VEC>(k, 2 * p + e);
+                if (there && at < h) row[at] = from_float<T>(x[e]);
+            }
         }
     }
-    if constexpr (!std::is_same_v<T, float>)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = to_float(from_float<T>(v[e]));
+    if (KEEP) raw_pairs<T>(raw, v);
 }
 template <bool VEC>
-__device__ __forceinline__ void parameter_load(const float* p, int k, int h, float (&v)[8]) {
+__device__ __forceinline__ void parameter_load(const float* p, int k, int h, Pair (&v)[4]) {
+    auto one = [&](int at) { return at >= h ? 0.0f : p ? __ldg(p + at) : 1.0f; };
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const int at = cell_column<VEC>(k, e);
-        v[e] = at >= h ? 0.0f : p ? __ldg(p + at) : 1.0f;
-    }
+    for (int q = 0; q < 4; ++q) v[q] = pair(one(cell_column<VEC>(k, 2 * q)), one(cell_column<VEC>(k, 2 * q + 1)));
+}
+__device__ __forceinline__ Pair minus(Pair a, Pair b) { return fma(b, pair(-1.0f), a); }  // exact where a - b is
+// 1 / sqrt(v), to the last bit or the one before: a step of Newton's behind the fast one.
+__device__ __forceinline__ float root(float v) {
+    const float r = rsqrtf(v), off = fmaf(-v * r, r, 1.0f);
+    return v < kInf && v > 0.0f ? fmaf(0.5f * r, off, r) : r;
 }
 
 // The sum over a row's threads: 8, 16 or 32 lanes, or warps that meet at a barrier of their own. `turn` alternates between two places.
@@ -133,29 +143,33 @@ __device__ __forceinline__ void clear_scratch(V* scratch) {
     for (int k = threadIdx.y * blockDim.x + threadIdx.x; k < kScratch; k += blockDim.x * blockDim.y) scratch[k] = V(0);
 }
 
-// Whether the fp32 sum s of p and q, which is `rounded` in the 16-bit type, is so near to a border between two of its values that its
-// error, 7 2^-24 of |p| + |q| at most, may have carried it over: its distance from `rounded` is then half a step.
+// Whether the fp32 sum s of p and q, which is s + off in the 16-bit type, is so near to a border between two of its values that its error,
+// 7 2^-24 of |p| + |q| at most, may have carried it over: off is then half a step.
 template <typename T>
-__device__ __forceinline__ bool near_border(float s, float rounded, float p, float q) {
+__device__ __forceinline__ bool near_border(float s, float off, float p, float q) {
     constexpr bool kHalfType = std::is_same_v<T, __half>;
     float half_step = __uint_as_float(__float_as_uint(s) & 0x7f800000u) * (kHalfType ? 0x1p-11f : 0x1p-8f);
     if (kHalfType) half_step = fmaxf(half_step, 0x1p-25f);
-    return fabsf(fabsf(s - rounded) - half_step) <= 0x1p-21f * (fabsf(p) + fabsf(q));
+    return fabsf(fabsf(off) - half_step) <= 0x1p-21f * (fabsf(p) + fabsf(q));
 }
 
 // 1 / sqrt(v) in binary64 from its fp32 approximation, by a step of Newton's: off by about 2^-46.
 __device__ __forceinline__ double root64(double v, float r) { return (double)r * (1.5 - 0.5 * v * ((double)r * (double)r)); }
 // The sum of eight squares of 16-bit numbers, which are exact in fp32, in binary64. (Pairs of bf16's in fp32, which halves the conversions,
 // are off by 2^-33 of the sum: enough for three of 4 million s.)
-__device__ __forceinline__ double squares8(const float (&v)[8]) {
+__device__ __forceinline__ double squares8(const Pair (&v)[4]) {
     double s[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) s[k] = (double)(v[2 * k] * v[2 * k]) + (double)(v[2 * k + 1] * v[2 * k + 1]);
+    for (int k = 0; k < 4; ++k) {
+        float a, b;
+        halves(mul(v[k], v[k]), a, b);
+        s[k] = (double)a + (double)b;
+    }
     return (s[0] + s[1]) + (s[2] + s[3]);
 }
 
 template <typename T, typename R, bool GATED, bool VEC, int K>
-__global__ void __launch_bounds__(kMostThreads, K == 1 ? 2 : 1) block_forward_kernel(const __grid_constant__ BlockArgs a) {
+__global__ void __launch_bounds__(K == 1 ? 256 : kMostThreads, K == 1 ? 2 : 1) block_forward_kernel(const __grid_constant__ BlockArgs a) {
     constexpr bool kWide = GATED && !std::is_same_v<R, float>;  // s is rounded to 16 bits
     using Sum = std::conditional_t<kWide, double, float>;
     __shared__ __align__(16) Sum scratch[kScratch];
@@ -165,28 +179,40 @@ __global__ void __launch_bounds__(kMostThreads, K == 1 ? 2 : 1) block_forward_ke
     const R* residual = GATED ? (const R*)a.residual + (int64_t)worker * a.r_ws : nullptr;
     const float *weight = a.weight ? a.weight + worker * a.weight_ws : nullptr, *gate = a.gate ? a.gate + worker * a.gate_ws : nullptr;
     const float* next = a.next ? a.next + worker * a.next_ws : nullptr;
-    float w[K][8], v[K][8];  // weight * gate, next
+    constexpr int kRowChunks = K * (kChunks<T> + (GATED ? kChunks<R> : 0)), kDepth = depth_of(kRowChunks, kForwardBytes);
+    extern __shared__ __align__(16) uint4 ring[];
+    const int pitch = (int)(blockDim.x * blockDim.y), tid = (int)(threadIdx.y * blockDim.x + threadIdx.x);
+    // a thread's weights and gates, for what is formed in binary64
+    float2* parameters = reinterpret_cast<float2*>(ring + (VEC ? kDepth * kRowChunks * pitch : 0)) + tid;
+    Pair w[K][4], v[K][4];  // weight * gate, next
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         parameter_load<VEC>(weight, k, a.h, w[k]);
         if (GATED) {
-            float g[8];
+            Pair g[4];
             parameter_load<VEC>(gate, k, a.h, g);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) w[k][e] *= g[e];
+            for (int p = 0; p < 4; ++p) {
+                if (kWide) {
+                    float x0, x1, g0, g1;
+                    halves(w[k][p], x0, x1);
+                    halves(g[p], g0, g1);
+                    parameters[(k * 8 + 2 * p) * pitch] = make_float2(x0, g0);
+                    parameters[(k * 8 + 2 * p + 1) * pitch] = make_float2(x1, g1);
+                }
+                w[k][p] = mul(w[k][p], g[p]);
+            }
             parameter_load<VEC>(next, k, a.h, v[k]);
         }
     }
     const float inverse = 1.0f / (float)a.h;
     const double inverse64 = 1.0 / (double)a.h;
+    const Pair alpha = pair(a.alpha);
     int turn = 0, turn2 = 0;
     clear_scratch(scratch);
     clear_scratch(scratch2);
     __syncthreads();
-    constexpr int kRowChunks = K * (kChunks<T> + (GATED ? kChunks<R> : 0)), kDepth = depth_of(kRowChunks, kForwardBytes);
-    extern __shared__ __align__(16) uint4 ring[];
-    const int pitch = (int)(blockDim.x * blockDim.y), tid = (int)(threadIdx.y * blockDim.x + threadIdx.x);
-    float nx[K][8], nr[K][8];  // the next row, where it waits in registers
+    Pair nx[K][4], nr[K][4];  // the next row, where it waits in registers
     auto fetch = [&](uint32_t round) {
         const uint32_t j = group + round * a.groups;
         const bool there = round < rounds && j < a.rows;
@@ -208,39 +234,43 @@ __global__ void __launch_bounds__(kMostThreads, K == 1 ? 2 : 1) block_forward_ke
     for (uint32_t round = 0; round < (VEC ? kDepth - 1 : 1); ++round) fetch(round);
     for (uint32_t round = 0, j = group; round < rounds; ++round, j += a.groups) {
         const bool there = j < a.rows;
-        float xs[K][8], rs[K][8];
+        Pair xs[K][4], rs[K][4];
+        const uint4* place = ring + (round % kDepth) * kRowChunks * pitch + tid;
         if (VEC) {
             fetch(round + kDepth - 1);
             copies_wait<kDepth - 1>();
-        }
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            if constexpr (VEC) {
-                cell_take<T>(ring + (round % kDepth) * kRowChunks * pitch + tid, 0, k, pitch, xs[k]);
-            } else {
+            for (int k = 0; k < K; ++k) cell_take<T>(place, 0, k, pitch, xs[k]);
+        } else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) xs[k][e] = nx[k][e], rs[k][e] = GATED ? nr[k][e] : 0.0f;
-            }
+            for (int k = 0; k < K; ++k)
+#pragma unroll
+                for (int p = 0; p < 4; ++p) {
+                    xs[k][p] = nx[k][p];
+                    if (GATED) rs[k][p] = nr[k][p];
+                }
+            fetch(round + 1);
         }
-        if (!VEC) fetch(round + 1);
         Sum sum = 0;
+        if constexpr (kWide) {
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            if constexpr (kWide) {
-                sum += squares8(xs[k]);
-            } else {
+            for (int k = 0; k < K; ++k) sum += squares8(xs[k]);
+        } else {
+            Pair some = pair(0.0f);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sum = fmaf(xs[k][e], xs[k][e], sum);
-            }
+            for (int k = 0; k < K; ++k)
+#pragma unroll
+                for (int p = 0; p < 4; ++p) some = fma(xs[k][p], xs[k][p], some);
+            sum = joint(some);
         }
         const Sum all = row_sum<Sum>(sum, scratch, turn);
         double exact = 0.0;
         float r;
         if constexpr (kWide) {
             exact = all * inverse64 + (double)a.eps;
-            r = 1.0f / sqrtf((float)exact);
+            r = root((float)exact);
         } else {
-            r = 1.0f / sqrtf(all * inverse + a.eps);
+            r = root(all * inverse + a.eps);
         }
         const int64_t number = (int64_t)worker * a.rows + j;
         T* y = (T*)a.y + number * a.h;
@@ -248,39 +278,75 @@ __global__ void __launch_bounds__(kMostThreads, K == 1 ? 2 : 1) block_forward_ke
 #pragma unroll
             for (int k = 0; k < K; ++k) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) xs[k][e] = xs[k][e] * r * w[k][e];
+                for (int p = 0; p < 4; ++p) xs[k][p] = mul(mul(xs[k][p], pair(r)), w[k][p]);
                 cell_store<T, VEC>(y, k, a.h, there, xs[k]);
             }
             if (a.stats && there && threadIdx.x == 0) a.stats[number] = make_float2(r, 0.0f);
         } else {
             R* s = (R*)a.s + number * a.h;
-            float squares = 0.0f;
+            Pair squares = pair(0.0f);
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                if (VEC) cell_take<R>(ring + (round % kDepth) * kRowChunks * pitch + tid, K * kChunks<T>, k, pitch, rs[k]);
+                if (VEC) cell_take<R>(place, K * kChunks<T>, k, pitch, rs[k]);
+                Pair one[4], other[4], t[4];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float p = a.alpha * rs[k][e], q = xs[k][e] * r * w[k][e];
-                    float t = p + q;
-                    if constexpr (kWide)
-                        if (near_border<R>(t, to_float(from_float<R>(t)), p, q)) {
-                            const int at = cell_column<VEC>(k, e);
-                            if (at < a.h) {
-                                const double g = (weight ? (double)weight[at] : 1.0) * (gate ? (double)gate[at] : 1.0);
-                                t = (float)(a.alpha64 * (double)rs[k][e] + (double)xs[k][e] * root64(exact, r) * g);
-                            }
-                        }
-                    rs[k][e] = t;
+                for (int p = 0; p < 4; ++p) {
+                    one[p] = mul(alpha, rs[k][p]);
+                    other[p] = mul(mul(xs[k][p], pair(r)), w[k][p]);
+                    t[p] = add(one[p], other[p]);
                 }
-                cell_store<R, VEC>(s, k, a.h, there, rs[k]);
+                if constexpr (kWide) {
+                    Pair off[4];
+                    raw_pairs<R>(pack_pairs<R>(t), off);
+                    float sv[8], ov[8], pv[8], qv[8];
+                    bool any = false;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) squares = fmaf(rs[k][e], rs[k][e], squares);
+                    for (int p = 0; p < 4; ++p) {
+                        halves(t[p], sv[2 * p], sv[2 * p + 1]);
+                        halves(minus(off[p], t[p]), ov[2 * p], ov[2 * p + 1]);
+                        halves(one[p], pv[2 * p], pv[2 * p + 1]);
+                        halves(other[p], qv[2 * p], qv[2 * p + 1]);
+                    }
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) any = any || near_border<R>(sv[e], ov[e], pv[e], qv[e]);
+                    if (any) {  // one thread in a hundred
+                        uint32_t which = 0;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) which |= near_border<R>(sv[e], ov[e], pv[e], qv[e]) ? 1u << e : 0u;
+                        const double r64 = root64(exact, r);
+                        while (which) {
+                            const int e = __ffs(which) - 1;
+                            which &= which - 1;
+                            const float2 factors = parameters[(k * 8 + e) * pitch];
+                            double xv, rv;
+                            if (VEC) {
+                                xv = to_float(reinterpret_cast<const T*>(place + k * pitch)[e]);
+                                rv = to_float(reinterpret_cast<const R*>(place + (K + k) * pitch)[e]);
+                            } else {
+                                const int at = cell_column<VEC>(k, e);
+                                xv = there && at < a.h ? to_float(x[(int64_t)j * a.x_rs + at]) : 0.0f;
+                                rv = there && at < a.h ? to_float(residual[(int64_t)j * a.r_rs + at]) : 0.0f;
+                            }
+                            const float exactly = (float)(a.alpha64 * rv + xv * r64 * ((double)factors.x * (double)factors.y));
+#pragma unroll
+                            for (int c = 0; c < 8; ++c) sv[c] = c == e ? exactly : sv[c];
+                        }
+#pragma unroll
+                        for (int p = 0; p < 4; ++p) t[p] = pair(sv[2 * p], sv[2 * p + 1]);
+                    }
+                }
+                cell_store<R, VEC, true>(s, k, a.h, there, t);
+#pragma unroll
+                for (int p = 0; p < 4; ++p) {
+                    rs[k][p] = t[p];
+                    squares = fma(t[p], t[p], squares);
+                }
             }
-            const float q = 1.0f / sqrtf(row_sum<float>(squares, scratch2, turn2) * inverse + a.eps);
+            const float q = root(row_sum<float>(joint(squares), scratch2, turn2) * inverse + a.eps);
 #pragma unroll
             for (int k = 0; k < K; ++k) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) rs[k][e] = rs[k][e] * q * v[k][e];
+                for (int p = 0; p < 4; ++p) rs[k][p] = mul(mul(rs[k][p], pair(q)), v[k][p]);
                 cell_store<T, VEC>(y, k, a.h, there, rs[k]);
             }
             if (a.stats && there && threadIdx.x == 0) a.stats[number] = make_float2(r, q);
@@ -289,8 +355,10 @@ __global__ void __launch_bounds__(kMostThreads, K == 1 ? 2 : 1) block_forward_ke
 }
 
 template <typename T, typename R, bool GATED, bool VEC, int K>
-__global__ void __launch_bounds__(kMostThreads, 1) block_backward_kernel(const __grid_constant__ BlockArgs a) {
-    __shared__ float scratch[kScratch];
+__global__ void __launch_bounds__(K == 1 ? 256 : kMostThreads, K == 1 ? 2 : 1) block_backward_kernel(const __grid_constant__ BlockArgs a) {
+    __shared__ __align__(16) float scratch[kScratch];
+    clear_scratch(scratch);
+    __syncthreads();
     const uint32_t worker = blockIdx.y, group = blockIdx.x * blockDim.y + threadIdx.y, rounds = (a.rows + a.groups - 1) / a.groups;
     const T* x = (const T*)a.x + (int64_t)worker * a.x_ws;
     const T* dy = (const T*)a.dy + (int64_t)worker * a.dy_ws;
@@ -298,30 +366,28 @@ __global__ void __launch_bounds__(kMostThreads, 1) block_backward_kernel(const _
     const R* s = GATED ? (const R*)a.s_in + (int64_t)worker * a.rows * a.h : nullptr;
     const float *weight = a.weight ? a.weight + worker * a.weight_ws : nullptr, *gate = a.gate ? a.gate + worker * a.gate_ws : nullptr;
     const float* next = a.next ? a.next + worker * a.next_ws : nullptr;
-    float w[K][8], v[K][8], sums[2][K][8];  // weight * gate, next; dv, c
+    Pair w[K][4], v[K][4], sums[2][K][4];  // weight * gate, next; dv, c
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         parameter_load<VEC>(weight, k, a.h, w[k]);
         if (GATED) {
-            float g[8];
+            Pair g[4];
             parameter_load<VEC>(gate, k, a.h, g);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) w[k][e] *= g[e];
+            for (int p = 0; p < 4; ++p) w[k][p] = mul(w[k][p], g[p]);
             parameter_load<VEC>(next, k, a.h, v[k]);
         }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sums[0][k][e] = sums[1][k][e] = 0.0f;
+        for (int p = 0; p < 4; ++p) sums[0][k][p] = sums[1][k][p] = pair(0.0f);
     }
     const float inverse = 1.0f / (float)a.h;
     int turn = 0;
-    clear_scratch(scratch);
-    __syncthreads();
     // chunks of a row: dy, x, then s and ds
     constexpr int kY = 0, kX = K * kChunks<T>, kS = 2 * kX, kD = kS + K * kChunks<R>;
     constexpr int kRowChunks = GATED ? kD + K * kChunks<R> : kS, kDepth = depth_of(kRowChunks, kBackwardBytes);
     extern __shared__ __align__(16) uint4 ring[];
     const int pitch = (int)(blockDim.x * blockDim.y), tid = (int)(threadIdx.y * blockDim.x + threadIdx.x);
-    float nx[K][8], ny[K][8], ns[K][8], nd[K][8];  // the next row, where it waits in registers
+    Pair nx[K][4], ny[K][4], ns[K][4], nd[K][4];  // the next row, where it waits in registers
     float2 next_stats = {};
     auto stats_of = [&](uint32_t j) { return j < a.rows ? __ldg(a.stats + (int64_t)worker * a.rows + j) : make_float2(0.0f, 0.0f); };
     auto fetch = [&](uint32_t round) {
@@ -355,7 +421,7 @@ __global__ void __launch_bounds__(kMostThreads, 1) block_backward_kernel(const _
         const bool there = j < a.rows;
         const float r = next_stats.x, q = next_stats.y;
         next_stats = stats_of(j + a.groups);
-        float xs[K][8], g[K][8], ss[K][8], dd[K][8];  // x; the gradient of what the norm behind x gives; s; ds
+        Pair xs[K][4], g[K][4], ss[K][4], dd[K][4];  // x; the gradient of what the norm behind x gives; s; ds
         const uint4* place = ring + (round % kDepth) * kRowChunks * pitch + tid;
         if (VEC) {
             fetch(round + kDepth - 1);
@@ -370,25 +436,25 @@ __global__ void __launch_bounds__(kMostThreads, 1) block_backward_kernel(const _
 #pragma unroll
             for (int k = 0; k < K; ++k)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    xs[k][e] = nx[k][e], g[k][e] = ny[k][e];
-                    if (GATED) ss[k][e] = ns[k][e], dd[k][e] = nd[k][e];
+                for (int p = 0; p < 4; ++p) {
+                    xs[k][p] = nx[k][p], g[k][p] = ny[k][p];
+                    if (GATED) ss[k][p] = ns[k][p], dd[k][p] = nd[k][p];
                 }
             fetch(round + 1);
         }
         const int64_t number = (int64_t)worker * a.rows + j;
         if constexpr (GATED) {
-            float dot = 0.0f;
+            Pair dot = pair(0.0f);
 #pragma unroll
             for (int k = 0; k < K; ++k)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    ss[k][e] *= q;
-                    sums[0][k][e] = fmaf(g[k][e], ss[k][e], sums[0][k][e]);
-                    g[k][e] *= v[k][e];
-                    dot = fmaf(g[k][e], ss[k][e], dot);
+                for (int p = 0; p < 4; ++p) {
+                    ss[k][p] = mul(ss[k][p], pair(q));
+                    sums[0][k][p] = fma(g[k][p], ss[k][p], sums[0][k][p]);
+                    g[k][p] = mul(g[k][p], v[k][p]);
+                    dot = fma(g[k][p], ss[k][p], dot);
                 }
-            const float mean = row_sum<float>(dot, scratch, turn) * inverse;
+            const float mean = row_sum<float>(joint(dot), scratch, turn) * inverse;
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 if (VEC) {
@@ -396,29 +462,29 @@ __global__ void __launch_bounds__(kMostThreads, 1) block_backward_kernel(const _
                     cell_take<T>(place, kX, k, pitch, xs[k]);
                 }
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    g[k][e] = fmaf(q, fmaf(-mean, ss[k][e], g[k][e]), dd[k][e]);
-                    dd[k][e] = a.alpha * g[k][e];
+                for (int p = 0; p < 4; ++p) {
+                    g[k][p] = fma(pair(q), fma(pair(-mean), ss[k][p], g[k][p]), dd[k][p]);
+                    dd[k][p] = mul(pair(a.alpha), g[k][p]);
                 }
                 if (a.dresidual) cell_store<R, VEC>((R*)a.dresidual + number * a.h, k, a.h, there, dd[k]);
             }
         }
-        float dot = 0.0f;
+        Pair dot = pair(0.0f);
 #pragma unroll
         for (int k = 0; k < K; ++k)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                xs[k][e] *= r;
-                sums[1][k][e] = fmaf(g[k][e], xs[k][e], sums[1][k][e]);
-                g[k][e] *= w[k][e];
-                dot = fmaf(g[k][e], xs[k][e], dot);
+            for (int p = 0; p < 4; ++p) {
+                xs[k][p] = mul(xs[k][p], pair(r));
+                sums[1][k][p] = fma(g[k][p], xs[k][p], sums[1][k][p]);
+                g[k][p] = mul(g[k][p], w[k][p]);
+                dot = fma(g[k][p], xs[k][p], dot);
             }
         if (a.dx) {
-            const float mean = row_sum<float>(dot, scratch, turn) * inverse;
+            const float mean = row_sum<float>(joint(dot), scratch, turn) * inverse;
 #pragma unroll
             for (int k = 0; k < K; ++k) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) g[k][e] = r * fmaf(-mean, xs[k][e], g[k][e]);
+                for (int p = 0; p < 4; ++p) g[k][p] = mul(pair(r), fma(pair(-mean), xs[k][p], g[k][p]));
                 cell_store<T, VEC>((T*)a.dx + number * a.h, k, a.h, there, g[k]);
             }
         }
@@ -428,11 +494,17 @@ __global__ void __launch_bounds__(kMostThreads, 1) block_backward_kernel(const _
 #pragma unroll
     for (int k = 0; k < K; ++k)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int at = cell_column<VEC>(k, e);
-            if (at < a.h) {
-                if (GATED) out[at] = sums[0][k][e];
-                out[a.h + at] = sums[1][k][e];
+        for (int p = 0; p < 4; ++p) {
+            float dv[2], c[2];
+            halves(sums[0][k][p], dv[0], dv[1]);
+            halves(sums[1][k][p], c[0], c[1]);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int at = cell_column<VEC>(k, 2 * p + e);
+                if (at < a.h) {
+                    if (GATED) out[at] = dv[e];
+                    out[a.h + at] = c[e];
+                }
             }
         }
 }
@@ -459,16 +531,14 @@ __global__ void __launch_bounds__(kMostThreads) long_forward_kernel(const __grid
         R* s = GATED ? (R*)a.s + number * a.h : nullptr;
         double sum = 0.0;
         for (int c0 = threadIdx.x; c0 < a.h; c0 += 8 * kMostThreads) {
-            float v[8];
+            Pair v[4];
+            auto one = [&](int c) { return c < a.h ? to_float(__ldg(x + c)) : 0.0f; };
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int c = c0 + e * kMostThreads;
-                v[e] = c < a.h ? to_float(__ldg(x + c)) : 0.0f;
-            }
+            for (int p = 0; p < 4; ++p) v[p] = pair(one(c0 + 2 * p * kMostThreads), one(c0 + (2 * p + 1) * kMostThreads));
             sum += squares8(v);
         }
         const double exact = row_sum<double>(sum, scratch, turn) / a.h + (double)a.eps;
-        const float r = 1.0f / sqrtf((float)exact);
+        const float r = root((float)exact);
         float squares = 0.0f, q = 0.0f;
         for (int c = threadIdx.x; c < a.h; c += kMostThreads) {
             const float w = weight ? __ldg(weight + c) : 1.0f, v = to_float(__ldg(x + c));
@@ -478,7 +548,7 @@ __global__ void __launch_bounds__(kMostThreads) long_forward_kernel(const __grid
                 const float p = a.alpha * to_float(__ldg(residual + c)), u = v * r * (w * (gate ? __ldg(gate + c) : 1.0f));
                 float t = p + u;
                 if constexpr (kWide)
-                    if (near_border<R>(t, to_float(from_float<R>(t)), p, u))
+                    if (near_border<R>(t, to_float(from_float<R>(t)) - t, p, u))
                         t = (float)(a.alpha64 * (double)to_float(__ldg(residual + c)) + (double)v * root64(exact, r) * ((double)w * (gate ? (double)gate[c] : 1.0)));
                 s[c] = from_float<R>(t);
                 t = to_float(from_float<R>(t));
@@ -486,7 +556,7 @@ __global__ void __launch_bounds__(kMostThreads) long_forward_kernel(const __grid
             }
         }
         if constexpr (GATED) {
-            q = 1.0f / sqrtf(row_sum<float>(squares, scratch2, turn2) * inverse + a.eps);
+            q = root(row_sum<float>(squares, scratch2, turn2) * inverse + a.eps);
             for (int c = threadIdx.x; c < a.h; c += kMostThreads)  // (its own: a thread reads what it wrote)
                 y[c] = from_float<T>(to_float(s[c]) * q * (next ? __ldg(next + c) : 1.0f));
         }
@@ -600,16 +670,16 @@ struct BlockShape {
         return n >= 1 && n <= 65535 && rows >= 0 && h >= 1 && h < ((int64_t)1 << 31) - 16 * kSpan && rows <= (int64_t)0x7fffffff / n;
     }
     // Threads of a row: eight columns each, then sixteen; at least 8. Rows of a CTA: 256 threads, or one row.
-    int parts() const { return h <= 8 * kMostThreads ? 1 : 2; }
+    int parts() const { return h <= kNarrow ? 1 : 2; }
     int threads() const {
         if (h > kLongest) return kMostThreads;
         const int64_t cells = (h + 8 * parts() - 1) / (8 * parts());
         return cells <= 8 ? 8 : cells <= 16 ? 16 : (int)((cells + 31) / 32 * 32);
     }
     int rows_of_cta() const { return threads() >= 256 ? 1 : 256 / threads(); }
-    // Groups of threads that walk a worker's rows: what fills the SMs with 1024 threads, of four rows at least.
-    uint32_t groups() const {
-        const int64_t all = (int64_t)multiprocessors() * (1024 / threads());
+    // Groups of threads that walk a worker's rows: what the SMs hold at once with so many threads, of four rows at least.
+    uint32_t groups(int resident = 512) const {
+        const int64_t all = (int64_t)multiprocessors() * std::max(1, resident / threads());
         const int64_t most = (rows + 3) / 4, per = rows_of_cta();
         int64_t g = (all + n - 1) / n;
         g = std::min(std::max<int64_t>(1, g), std::max<int64_t>(1, most));
@@ -644,7 +714,8 @@ cudaError_t allow(int bytes) {  // more than 48 KB, the static part included: as
 template <typename T, typename R, bool GATED, bool VEC, int K>
 int block_forward(BlockArgs& a, const BlockShape& z, cudaStream_t stream) {
     constexpr auto kernel = block_forward_kernel<T, R, GATED, VEC, K>;
-    const int bytes = ring_bytes(z, VEC, K * (kChunks<T> + (GATED ? kChunks<R> : 0)), kForwardBytes);
+    const int bytes = ring_bytes(z, VEC, K * (kChunks<T> + (GATED ? kChunks<R> : 0)), kForwardBytes) +
+                      (GATED && !std::is_same_v<R, float> ? K * 64 * z.threads() * z.rows_of_cta() : 0);
     cudaError_t e = allow<kernel>(bytes);
     if (e == cudaSuccess)
         e = launch_plain(kernel, dim3(a.groups / z.rows_of_cta(), (uint32_t)z.n), dim3((uint32_t)z.threads(), (uint32_t)z.rows_of_cta()), bytes, stream, a);
@@ -702,7 +773,7 @@ int compams_rms_norm_forward(void* y, void* s, float* stats, const void* x, cons
     a.x = x; a.residual = residual; a.y = y; a.s = s; a.stats = (float2*)stats; a.weight = weight; a.gate = gate; a.next = next;
     a.weight_ws = weight_stride; a.gate_ws = gate_stride; a.next_ws = next_stride;
     a.x_ws = x_worker_stride; a.x_rs = x_row_stride; a.r_ws = residual_worker_stride; a.r_rs = residual_row_stride;
-    a.rows = (uint32_t)rows; a.groups = z.groups(); a.h = (int32_t)h; a.alpha = (float)residual_scale; a.alpha64 = residual_scale; a.eps = eps;
+    a.rows = (uint32_t)rows; a.groups = z.groups(gated ? 512 : 768); a.h = (int32_t)h; a.alpha = (float)residual_scale; a.alpha64 = residual_scale; a.eps = eps;
     return by_block_types(type, gated ? residual_type : type, [&](auto t, auto r) {
         using T = decltype(t);
         using R = decltype(r);
