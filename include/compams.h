@@ -590,9 +590,10 @@ int compams_head_forward(float* loss, float* lse, const void* x, int32_t type, c
  *   dweight         packed [n, vocab, h], worker i's rows alone; sum_workers: [vocab, h], over all workers, for a weight that all share;
  *                   may be null: not wanted.
  *   wanted          of the workspace: 0 the forward pass, else 1 (dx) + 2 (dweight).
- *   x_copied, weight_copied   0 where TMA can read them as they lie: type is weight_type and has 16 bits, the address and the strides are
- *                   multiples of 16 bytes (of axes longer than 1), rows do not overlap, and, for x beside a weight that all share, the
- *                   workers' rows follow one another at one distance. Else 1, or 1 in any case: the workspace then has room for a copy.
+ *   x_copied, weight_copied   0 where TMA can read them as they lie: both have one 16-bit type (or, for x, type is COMPAMS_BF16), the
+ *                   address and the strides are multiples of 16 bytes (of axes longer than 1), rows do not overlap, and, for x beside a
+ *                   weight that all share, the workers' rows follow one another at one distance. Else 1, or 1 in any case: the workspace
+ *                   then has room for a copy.
  *   shared          weight_worker_stride is 0, or n is 1.
  */
 int compams_head_backward(void* dx, void* dweight, int32_t sum_workers, const float* dloss, int64_t dloss_worker_stride, int64_t dloss_row_stride,

@@ -152,8 +152,7 @@ def load_library() -> ctypes.CDLL:
     L.compams_head_status.restype = c.c_int
     L.compams_head_wait_tries.argtypes = [I32]
     L.compams_head_wait_tries.restype = c.c_int
-    L.compams_collect_workers.argtypes = [P, I64, P, c.POINTER(P), c.POINTER(I64), c.POINTER(I32), c.POINTER(I64), I32, I32, c.c_double,
-                                          c.c_double, P, c.c_size_t, P]
+    L.compams_collect_workers.argtypes = [P, I64, P, P, P, P, P, I32, I32, c.c_double, c.c_double, P, c.c_size_t, P]
     L.compams_collect_workers.restype = c.c_int
     L.compams_collect_workers_workspace_bytes.argtypes = [c.POINTER(c.c_size_t), I32, I32]
     L.compams_collect_workers_workspace_bytes.restype = c.c_int

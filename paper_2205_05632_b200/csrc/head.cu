@@ -56,11 +56,15 @@ struct PackArgs {
     uint16_t* out;        // [plane][batch][rows][8 per_row]
     int64_t plane;        // elements
 };
+// Of up to two tensors of a type: the second's chunks are numbered behind the first's.
 template <typename T, int P, bool VEC>
-__global__ void __launch_bounds__(256) pack_kernel(const __grid_constant__ PackArgs a) {
+__global__ void __launch_bounds__(256) pack_kernel(const __grid_constant__ PackArgs first, const __grid_constant__ PackArgs second) {
     dependency_wait();
-    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (at >= a.chunks) return;
+    int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (at >= first.chunks + second.chunks) return;
+    const bool behind = at >= first.chunks;
+    const PackArgs& a = behind ? second : first;
+    if (behind) at -= first.chunks;
     const int64_t row = at / a.per_row, batch = row / a.rows;
     const int c = (int)(at - row * a.per_row) * 8;
     const T* x = (const T*)a.src + batch * a.ws + (a.row0 + row - batch * a.rows) * a.rs + c;
@@ -121,12 +125,14 @@ __global__ void __launch_bounds__(256) few_kernel(const __grid_constant__ FewArg
         target[r] = r < a.rows ? a.target[number0 + r] : -1;
         state[r] = make_float2(-kInf, 0.0f);
     }
-    const int groups = (a.vocab + 3) / 4;
-    for (int g = blockIdx.x * 8 + warp; g < groups; g += gridDim.x * 8) {
+    // a warp's rows, as many as any other's but for one
+    const int64_t warps = (int64_t)gridDim.x * 8, mine = (int64_t)blockIdx.x * 8 + warp;
+    const int last = (int)(a.vocab * (mine + 1) / warps);
+    for (int v0 = (int)(a.vocab * mine / warps); v0 < last; v0 += 4) {
         float acc[4][MR] = {};
         const TW* row[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) row[j] = weight + (int64_t)min(g * 4 + j, a.vocab - 1) * a.w_rs;
+        for (int j = 0; j < 4; ++j) row[j] = weight + (int64_t)min(v0 + j, last - 1) * a.w_rs;
         if constexpr (VEC) {
 #pragma unroll 2
             for (int c = lane * 8; c < a.h; c += kSpan) {
@@ -166,8 +172,8 @@ __global__ void __launch_bounds__(256) few_kernel(const __grid_constant__ FewArg
                 float z = acc[j][r];
 #pragma unroll
                 for (int o = 16; o; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
-                const int v = g * 4 + j;
-                if (v < a.vocab) {
+                const int v = v0 + j;
+                if (v < last) {
                     state[r] = merged(state[r], make_float2(z, 1.0f));
                     if (lane == 0 && v == target[r]) a.target_logit[number0 + r] = z;
                 }
@@ -400,7 +406,7 @@ bool flat(const HeadShape& z, int64_t ws, int64_t rs, int64_t& stride) {
     return z.rows == 1 || z.n == 1 || ws == z.rows * rs;
 }
 bool x_lies_well(const HeadShape& z, const void* x, int64_t ws, int64_t rs, Matrix& m) {
-    if (z.copies() || z.type == kTypeF32) return false;
+    if (z.x_planes() > 1) return false;
     int64_t stride = rs;
     if (z.shared) {
         if (!flat(z, ws, rs, stride)) return false;
@@ -411,7 +417,7 @@ bool x_lies_well(const HeadShape& z, const void* x, int64_t ws, int64_t rs, Matr
     return lies_well(m, z.rows, z.n, z.h);
 }
 bool w_lies_well(const HeadShape& z, const void* w, int64_t ws, int64_t rs, Matrix& m) {
-    if (z.copies() || z.weight_type == kTypeF32) return false;
+    if (z.copies()) return false;
     m = {w, rs, ws};
     return lies_well(m, z.vocab, z.batches(), z.h);
 }
@@ -561,53 +567,65 @@ int product(head::Args& a, const Operand& left, const Operand& right, const CUte
                     what);
 }
 
+// What is to be brought into planes: rows row0 ... row0 + rows of every batch of a matrix.
+struct Job {
+    Matrix m;
+    int64_t rows, row0, batches;
+    void* out;
+};
 template <typename T, int P>
-int pack(const Matrix& m, int64_t rows, int64_t row0, int64_t batches, int64_t h, uint16_t* out, cudaStream_t stream) {
-    PackArgs a = {};
-    a.src = m.p; a.ws = m.batch_stride; a.rs = m.row_stride; a.rows = rows; a.row0 = row0; a.h = (int32_t)h;
-    a.per_row = (int32_t)((h + 7) / 8);
-    a.chunks = batches * rows * a.per_row;
-    a.out = out; a.plane = a.chunks * 8;
-    const int64_t ctas = (a.chunks + 255) / 256;
+int pack(const Job* jobs, int count, int64_t h, cudaStream_t stream) {
+    PackArgs a[2] = {};
+    bool vec = h % 8 == 0;
+    for (int k = 0; k < count; ++k) {
+        const Job& j = jobs[k];
+        a[k].src = j.m.p; a[k].ws = j.m.batch_stride; a[k].rs = j.m.row_stride; a[k].rows = j.rows; a[k].row0 = j.row0; a[k].h = (int32_t)h;
+        a[k].per_row = (int32_t)((h + 7) / 8);
+        a[k].chunks = j.batches * j.rows * a[k].per_row;
+        a[k].out = (uint16_t*)j.out; a[k].plane = a[k].chunks * 8;
+        vec = vec && ((reinterpret_cast<uintptr_t>(j.m.p) | (uint64_t)(j.m.row_stride * (int64_t)sizeof(T)) |
+                       (uint64_t)(j.m.batch_stride * (int64_t)sizeof(T))) & 15u) == 0;
+    }
+    const int64_t ctas = (a[0].chunks + a[1].chunks + 255) / 256;
     if (ctas > 0x7fffffff) return COMPAMS_ERR_TOO_LARGE;
-    const bool vec = h % 8 == 0 && ((reinterpret_cast<uintptr_t>(m.p) | (uint64_t)(m.row_stride * (int64_t)sizeof(T)) |
-                                     (uint64_t)(m.batch_stride * (int64_t)sizeof(T))) & 15u) == 0;
     const auto kernel = vec ? pack_kernel<T, P, true> : pack_kernel<T, P, false>;
-    return launched(launch_sized(kernel, dim3((uint32_t)ctas), 256, 1, 0, false, stream, a), "head_pack");
+    return launched(launch_sized(kernel, dim3((uint32_t)ctas), 256, 1, 0, false, stream, a[0], a[1]), "head_pack");
 }
-int pack_operand(const HeadShape& z, int32_t type, int planes, const Matrix& m, int64_t rows, int64_t row0, int64_t batches, void* out,
-                 cudaStream_t stream) {
-    uint16_t* to = (uint16_t*)out;
-    if (type == kTypeF32) return pack<float, 3>(m, rows, row0, batches, z.h, to, stream);
-    if (type == kTypeBF16) return pack<__nv_bfloat16, 1>(m, rows, row0, batches, z.h, to, stream);
-    return planes == 2 ? pack<__half, 2>(m, rows, row0, batches, z.h, to, stream) : pack<__half, 1>(m, rows, row0, batches, z.h, to, stream);
+int pack(int32_t type, int planes, const Job* jobs, int count, int64_t h, cudaStream_t stream) {
+    if (type == kTypeF32) return pack<float, 3>(jobs, count, h, stream);
+    if (type == kTypeBF16) return pack<__nv_bfloat16, 1>(jobs, count, h, stream);
+    return planes == 2 ? pack<__half, 2>(jobs, count, h, stream) : pack<__half, 1>(jobs, count, h, stream);
 }
 
-// x as an operand, the caller's memory or a copy: [plane][batch][rows of a batch][h].
-int x_operand(const HeadShape& z, const void* x, int64_t ws, int64_t rs, const Plan& p, char* work, Operand& o, cudaStream_t stream) {
+// x and the piece of the weight from row v0 on as operands: the caller's memory, or copies, [plane][batch][rows][columns]. The weight's piece
+// starts at row `first` of its operand. x_too: x has not been copied yet.
+int operands(const HeadShape& z, const void* x, int64_t x_ws, int64_t x_rs, const void* w, int64_t w_ws, int64_t w_rs, const Plan& p, int64_t v0,
+             int64_t count, bool x_too, char* work, Operand& xo, Operand& wo, int32_t& first, cudaStream_t stream) {
+    Job jobs[2];
+    int much = 0;
     Matrix m;
-    o = {nullptr, z.h, z.batch_rows(), z.batches(), z.x_planes(), 0, 0};
-    if (x_lies_well(z, x, ws, rs, m)) {
-        o.p = m.p; o.row_stride = m.row_stride; o.batch_stride = m.batch_stride;
-        return COMPAMS_OK;
+    xo = {nullptr, z.h, z.batch_rows(), z.batches(), z.x_planes(), 0, 0};
+    if (x_lies_well(z, x, x_ws, x_rs, m)) {
+        xo.p = m.p; xo.row_stride = m.row_stride; xo.batch_stride = m.batch_stride;
+    } else {
+        xo.p = work + p.x_copy; xo.row_stride = z.pitch(); xo.batch_stride = z.batch_rows() * z.pitch(); xo.columns = z.pitch();
+        if (x_too) jobs[much++] = {{x, x_rs, x_ws}, z.rows, 0, z.n, work + p.x_copy};
     }
-    o.p = work + p.x_copy; o.row_stride = z.pitch(); o.batch_stride = z.batch_rows() * z.pitch();
-    o.columns = z.pitch();
-    return pack_operand(z, z.type, z.x_planes(), {x, rs, ws}, z.rows, 0, z.n, work + p.x_copy, stream);
-}
-// Rows v0 ... of the weight: the caller's memory, whose row v0 is row `first`, or a copy of the piece.
-int w_operand(const HeadShape& z, const void* w, int64_t ws, int64_t rs, const Plan& p, int64_t v0, int64_t count, char* work, Operand& o,
-              int32_t& first, cudaStream_t stream) {
-    Matrix m;
-    o = {nullptr, z.h, z.vocab, z.batches(), z.w_planes(), 0, 0};
-    if (w_lies_well(z, w, ws, rs, m)) {
-        o.p = m.p; o.row_stride = m.row_stride; o.batch_stride = m.batch_stride;
-        first = (int32_t)v0;
-        return COMPAMS_OK;
+    wo = {nullptr, z.h, z.vocab, z.batches(), z.w_planes(), 0, 0};
+    first = (int32_t)v0;
+    if (w_lies_well(z, w, w_ws, w_rs, m)) {
+        wo.p = m.p; wo.row_stride = m.row_stride; wo.batch_stride = m.batch_stride;
+        return much ? pack(z.type, z.x_planes(), jobs, 1, z.h, stream) : (int)COMPAMS_OK;
     }
     first = 0;
-    o.p = work + p.w_copy; o.rows = count; o.columns = z.pitch(); o.row_stride = z.pitch(); o.batch_stride = count * z.pitch();
-    return pack_operand(z, z.weight_type, z.w_planes(), {w, rs, ws}, count, v0, z.batches(), work + p.w_copy, stream);
+    wo.p = work + p.w_copy; wo.rows = count; wo.columns = z.pitch(); wo.row_stride = z.pitch(); wo.batch_stride = count * z.pitch();
+    const Job weight{{w, w_rs, w_ws}, count, v0, z.batches(), work + p.w_copy};
+    if (much && z.type == z.weight_type) {  // both at once
+        jobs[much++] = weight;
+        return pack(z.type, z.x_planes(), jobs, 2, z.h, stream);
+    }
+    const int rc = much ? pack(z.type, z.x_planes(), jobs, 1, z.h, stream) : (int)COMPAMS_OK;
+    return rc == COMPAMS_OK ? pack(z.weight_type, z.w_planes(), &weight, 1, z.h, stream) : rc;
 }
 
 template <typename TX, typename TW, int MR>
@@ -652,7 +670,7 @@ int compams_head_workspace_bytes(size_t* bytes, int32_t n, int64_t rows, int64_t
                                  int32_t shared, int32_t x_copied, int32_t weight_copied, int32_t wanted) {
     const HeadShape z{n, rows, h, vocab, type, weight_type, shared != 0 || n == 1};
     if (!bytes || !z.ok() || wanted < 0 || wanted > 3) return COMPAMS_ERR_INVALID_ARG;
-    *bytes = rows ? (size_t)plan_of(z, x_copied || z.copies(), weight_copied || z.copies(), wanted).bytes : 0;
+    *bytes = rows ? (size_t)plan_of(z, x_copied || z.x_planes() > 1, weight_copied || z.copies(), wanted).bytes : 0;
     return COMPAMS_OK;
 }
 
@@ -688,11 +706,11 @@ int compams_head_forward(float* loss, float* lse, const void* x, int32_t type, c
                                  : (wide ? few_rows<__half, float>(z, a, ctas, stream) : few_rows<__half, __half>(z, a, ctas, stream));
     } else {
         Operand xo, wo;
-        rc = x_operand(z, x, x_worker_stride, x_row_stride, p, work, xo, stream);
         for (int64_t v0 = 0; v0 < vocab && rc == COMPAMS_OK; v0 += p.piece) {
             const int64_t count = std::min(p.piece, vocab - v0);
             head::Args a = {};
-            rc = w_operand(z, weight, weight_worker_stride, weight_row_stride, p, v0, count, work, wo, a.right_row, stream);
+            rc = operands(z, x, x_worker_stride, x_row_stride, weight, weight_worker_stride, weight_row_stride, p, v0, count, v0 == 0, work, xo, wo,
+                          a.right_row, stream);
             if (rc != COMPAMS_OK) break;
             a.tiles_m = (int32_t)((z.batch_rows() + 255) / 256); a.tiles_n = (int32_t)((count + 255) / 256);
             a.batches = (int32_t)z.batches(); a.parts = 1;
@@ -750,14 +768,14 @@ int compams_head_backward(void* dx, void* dweight, int32_t sum_workers, const fl
     r.reduction = reduction; r.f16 = z.f16(); r.g = (float*)(work + p.g); r.scale = (float*)(work + p.scale);
     int rc = launched(launch_sized(rows_kernel, dim3((uint32_t)n), 256, 1, 0, true, stream, r), "head_rows");
     Operand xo, wo;
-    if (rc == COMPAMS_OK) rc = x_operand(z, x, x_worker_stride, x_row_stride, p, work, xo, stream);
     const float* scale = r.scale;
     uint16_t* d = (uint16_t*)(work + p.d);
     const int32_t tiles_h = (int32_t)((h + 255) / 256), tiles_rows = (int32_t)((z.batch_rows() + 255) / 256);
     for (int64_t v0 = 0; v0 < vocab && rc == COMPAMS_OK; v0 += p.piece) {
         const int64_t count = std::min(p.piece, vocab - v0);
         int32_t first = 0;
-        rc = w_operand(z, weight, weight_worker_stride, weight_row_stride, p, v0, count, work, wo, first, stream);
+        rc = operands(z, x, x_worker_stride, x_row_stride, weight, weight_worker_stride, weight_row_stride, p, v0, count, v0 == 0, work, xo, wo, first,
+                      stream);
         if (rc != COMPAMS_OK) break;
         {
             head::Args a = {};

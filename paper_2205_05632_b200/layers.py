@@ -129,7 +129,7 @@ _NOTHING = _Nothing()
 def _run(name: str, device: torch.device, *args) -> None:
     fn = getattr(load_library(), name)
     index = device.index
-    if torch.cuda.current_device() == index:
+    if torch._C._cuda_getDevice() == index:
         rc = fn(*args, _stream(index))
     else:
         with torch.cuda.device(device):
@@ -430,20 +430,29 @@ class _GatedNormFunction(torch.autograd.Function):
         return (*_rms_backward(ctx, dy, ds, x, s, stats, *[next(given) if there else None for there in ctx.given]), None, None)
 
 
-def _rms_parameters(x, eps, **parameters):
-    h = x.shape[-1]
-    found = [None if p is None else _factor(p, x, (h,), name) for name, p in parameters.items()]
-    if len({p.dim() for p in found if p is not None}) > 1:
-        raise CompAMSError("%s are all for all workers or all per worker" % ", ".join(parameters))
-    if not float(eps) >= 0.0:
+def _rms_parameters(x, weight, gate, after):
+    inner = x.shape[-1:]
+    weight = None if weight is None else _factor(weight, x, inner, "weight")
+    gate = None if gate is None else _factor(gate, x, inner, "gate")
+    after = None if after is None else _factor(after, x, inner, "next_weight")
+    dims = [p.dim() for p in (weight, gate, after) if p is not None]
+    if dims and min(dims) != max(dims):
+        raise CompAMSError("weight, gate and next_weight are all for all workers or all per worker")
+    return weight, gate, after
+
+
+def _epsilon(eps: float) -> float:
+    eps = float(eps)
+    if not eps >= 0.0:
         raise CompAMSError("eps must not be negative")
-    return *found, float(eps)
+    return eps
 
 
 def rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, eps: float = 1e-6) -> torch.Tensor:
     """x / sqrt(mean(x^2) + eps) * weight over the last axis of x [n, ..., h], in x's type; weight is float32 [h] or [n, h]."""
     _activation(x)
-    weight, eps = _rms_parameters(x, eps, weight=weight)
+    weight = None if weight is None else _factor(weight, x, x.shape[-1:], "weight")
+    eps = _epsilon(eps)
     if _through_autograd(x, weight):
         return _RmsNormFunction.apply(x, weight, eps)
     return _rms_forward(x, None, weight, None, None, 1.0, eps, False)[0]
@@ -457,8 +466,7 @@ def gated_add_rms_norm(x: torch.Tensor, residual: torch.Tensor, weight: Optional
     stored; the first result has x's type. weight, gate and next_weight are float32 [h], or all [n, h]; None: 1."""
     _activation(x)
     _like(residual, x, "residual", (x.dtype, torch.float32))
-    weight, gate, next_weight, eps = _rms_parameters(x, eps, weight=weight, gate=gate, next_weight=next_weight)
-    args = (x, residual, weight, gate, next_weight, float(residual_scale), eps)
+    args = (x, residual, *_rms_parameters(x, weight, gate, next_weight), float(residual_scale), _epsilon(eps))
     if _through_autograd(*args[:5]):
         return _GatedNormFunction.apply(*args)
     return _rms_forward(*args, False)[:2]
@@ -565,13 +573,14 @@ class _Head:
         self.strides = (ws, rs, wws, weight.stride(-2))
         self.shape = (n, self.rows, h, vocab)
         x_copied = w_copied = True
-        if x.dtype == weight.dtype and x.dtype != torch.float32:
+        if x.dtype == torch.bfloat16 or (x.dtype == weight.dtype == torch.float16):
             if self.shared:
                 stride = ws if self.rows == 1 else rs
                 x_copied = not ((self.rows == 1 or n == 1 or ws == self.rows * rs)
                                 and _as_it_lies(self.x.data_ptr(), h, n * self.rows, stride, 1, 0))
             else:
                 x_copied = not _as_it_lies(self.x.data_ptr(), h, self.rows, rs, n, ws)
+        if x.dtype == weight.dtype != torch.float32:
             w_copied = not _as_it_lies(weight.data_ptr(), h, vocab, weight.stride(-2), 1 if self.shared else n, wws)
         self.copied = (int(x_copied), int(w_copied))
 

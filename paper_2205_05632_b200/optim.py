@@ -15,6 +15,7 @@ torch is used for the model and its autograd; the optimizer step itself runs in 
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import functools
 import itertools
@@ -36,12 +37,6 @@ def _workspace_bytes(n: int, count: int) -> int:
     return need.value
 
 
-@functools.lru_cache(maxsize=64)
-def _arrays(count: int):
-    """Types of the host arrays of a call."""
-    return ctypes.c_void_p * count, ctypes.c_int64 * count, ctypes.c_int32 * count, ctypes.c_int64 * (count + 1)
-
-
 def _limit(max_norm: Optional[float], eps: float) -> Tuple[float, float]:
     limit, eps = _INFINITY if max_norm is None else float(max_norm), float(eps)
     if not limit >= 0.0 or not eps >= 0.0:
@@ -49,23 +44,27 @@ def _limit(max_norm: Optional[float], eps: float) -> Tuple[float, float]:
     return limit, eps
 
 
-def _collect_workers(rows: Optional[torch.Tensor], device: torch.device, n: int, pieces, norms: bool, max_norm: float,
+def _collect_workers(rows: Optional[torch.Tensor], device: torch.device, n: int, addresses, strides, sizes, types, norms: bool, max_norm: float,
                      eps: float) -> Optional[torch.Tensor]:
-    """compams_collect_workers on (address or None, elements from worker to worker, elements of a worker, type) of each tensor."""
-    pieces = [p for p in pieces if p[2]]
+    """compams_collect_workers on lists of the tensors' addresses (0: no gradient), elements from worker to worker, elements of a worker
+    (none of them 0) and types."""
     got = torch.empty(n, dtype=torch.float32, device=device) if norms else None
-    if not pieces:
+    if not sizes:
         return None if got is None else got.zero_()
-    count = len(pieces)
-    pointers, longs, ints, ends = _arrays(count)
-    addresses, strides, sizes, types = zip(*pieces)
+    count, index = len(sizes), device.index
     work = torch.empty(_workspace_bytes(n, count), dtype=torch.uint8, device=device) if norms or max_norm < _INFINITY else None
-    with torch.cuda.device(device):
-        _check(load_library().compams_collect_workers(
-            None if rows is None else rows.data_ptr(), 0 if rows is None else rows.stride(0), None if got is None else got.data_ptr(),
-            pointers(*addresses), longs(*strides), ints(*types), ends(*itertools.accumulate(sizes, initial=0)), count, n, max_norm, eps,
-            None if work is None else work.data_ptr(), 0 if work is None else work.numel(), torch._C._cuda_getCurrentRawStream(device.index)),
-            "compams_collect_workers")
+    lists = (array.array("Q", addresses), array.array("q", strides), array.array("i", types),
+             array.array("q", itertools.accumulate(sizes, initial=0)))
+    args = (None if rows is None else rows.data_ptr(), 0 if rows is None else rows.stride(0), None if got is None else got.data_ptr(),
+            *[a.buffer_info()[0] for a in lists], count, n, max_norm, eps, None if work is None else work.data_ptr(),
+            0 if work is None else work.numel(), torch._C._cuda_getCurrentRawStream(index))
+    if torch._C._cuda_getDevice() == index:
+        rc = load_library().compams_collect_workers(*args)
+    else:
+        with torch.cuda.device(device):
+            rc = load_library().compams_collect_workers(*args)
+    if rc:
+        _check(rc, "compams_collect_workers")
     return got
 
 
@@ -76,18 +75,27 @@ def _changed(tensors) -> None:
         torch.autograd.graph.increment_version(tensors)
 
 
-def _gradients(grads, what: str) -> Tuple[List[torch.Tensor], int, torch.device]:
+_T = torch.Tensor
+
+
+def _gradients(grads, what: str) -> Tuple[Sequence[torch.Tensor], int, torch.device, List[int]]:
+    """The tensors, the number of workers, the device and the tensors' types. (Calls are mapped over the list: a model has hundreds.)"""
     grads = [grads] if isinstance(grads, torch.Tensor) else list(grads)
-    if not grads or not all(isinstance(g, torch.Tensor) for g in grads):
+    if not grads or not all([isinstance(g, torch.Tensor) for g in grads]):
         raise CompAMSError("%s takes tensors, one at least" % what)
     device, n = grads[0].device, grads[0].shape[0] if grads[0].dim() else 0
     if device.type != "cuda" or not 1 <= n <= 65535:
         raise CompAMSError("gradients must be CUDA tensors with the workers, at most 65535, on the leading axis")
-    for g in grads:
-        if g.dtype not in _TYPES or g.device != device or g.dim() == 0 or g.shape[0] != n:
-            raise CompAMSError("gradients must be float32, bfloat16 or float16 tensors [%d, ...] on %s: got %s of type %s on %s" % (
-                n, device, list(g.shape), g.dtype, g.device))
-    return grads, n, device
+    types = [_TYPES.get(g.dtype, -1) for g in grads]
+    if min(types) < 0 or set(map(_T.get_device, grads)) != {device.index} or not all(map(_T.dim, grads)) or not all([g.size(0) == n for g in grads]):
+        raise CompAMSError("gradients must be float32, bfloat16 or float16 tensors [%d, ...] on %s: got %s" % (
+            n, device, ", ".join("%s of type %s on %s" % (list(g.shape), g.dtype, g.device) for g in grads)))
+    return grads, n, device, types
+
+
+def _with_elements(sizes: List[int], *lists):
+    """The lists without what belongs to tensors of no elements."""
+    return [sizes, *lists] if all(sizes) else [[v for v, size in zip(of, sizes) if size] for of in (sizes, *lists)]
 
 
 def collect_gradients(grads: Union[torch.Tensor, Sequence[torch.Tensor]], out: Optional[torch.Tensor] = None,
@@ -95,34 +103,36 @@ def collect_gradients(grads: Union[torch.Tensor, Sequence[torch.Tensor]], out: O
     """(G, norms): the workers' gradients, one tensor [n, *shape] per parameter in float32, bfloat16 or float16, gathered as the rows of a
     float32 tensor [n, d], `out` where given, and each worker's global norm over all of them, [n], as it was. Rows whose norm is above
     max_norm are multiplied by max_norm / (norm + eps). The tensors may not overlap out."""
-    grads, n, device = _gradients(grads, "collect_gradients")
+    grads, n, device, types = _gradients(grads, "collect_gradients")
     max_norm, eps = _limit(max_norm, eps)
-    d = sum(g.numel() for g in grads) // n
+    if not all(map(_T.is_contiguous, grads)) or any(map(_T.is_neg, grads)):
+        grads = [g if g.is_contiguous() and not g.is_neg() else g.resolve_neg().contiguous() for g in grads]
+    sizes = [k // n for k in map(_T.numel, grads)]
+    d = sum(sizes)
     if out is None:
         out = torch.empty(n, d, dtype=torch.float32, device=device)
     elif (not isinstance(out, torch.Tensor) or out.dtype != torch.float32 or out.device != device or out.shape != (n, d)
           or (d > 1 and out.stride(1) != 1) or (n > 1 and out.stride(0) < d) or out.is_neg() or out.requires_grad):
         raise CompAMSError("out must be a float32 tensor [%d, %d] with packed rows on %s" % (n, d, device))
-    _changed([out])
-    kept = [g if g.is_contiguous() and not g.is_neg() else g.resolve_neg().contiguous() for g in grads]  # until the kernel is enqueued
-    norms = _collect_workers(out, device, n, [(g.data_ptr(), g.numel() // n, g.numel() // n, _TYPES[g.dtype]) for g in kept], True, max_norm, eps)
-    return out, norms
+    else:
+        _changed([out])
+    sizes, addresses, types = _with_elements(sizes, list(map(_T.data_ptr, grads)), types)
+    return out, _collect_workers(out, device, n, addresses, sizes, sizes, types, True, max_norm, eps)
 
 
 def clip_gradients(grads: Union[torch.Tensor, Sequence[torch.Tensor]], max_norm: float, eps: float = 1e-6) -> torch.Tensor:
     """Each worker's global norm, [n], over tensors [n, *shape] (G itself, or one tensor per parameter; every worker's part packed), which are
     scaled in place, worker by worker, by min(1, max_norm / (norm + eps)). A worker that is not above max_norm is not touched."""
-    grads, n, device = _gradients(grads, "clip_gradients")
+    grads, n, device, types = _gradients(grads, "clip_gradients")
     max_norm, eps = _limit(max_norm, eps)
-    pieces = []
     for g in grads:
         if g.is_neg() or not g[0].is_contiguous() or (n > 1 and g.stride(0) < g[0].numel()):
             raise CompAMSError("gradients that are clipped in place must be packed for every worker, and the workers' parts apart")
         if g.requires_grad and torch.is_grad_enabled() and g.is_leaf:
             raise CompAMSError("a leaf that requires a gradient cannot be scaled in place")
-        pieces.append((g.data_ptr(), g.stride(0), g[0].numel(), _TYPES[g.dtype]))
     _changed(grads)
-    return _collect_workers(None, device, n, pieces, True, max_norm, eps)
+    sizes, addresses, strides, types = _with_elements([g.numel() // n for g in grads], [g.data_ptr() for g in grads], [g.stride(0) for g in grads], types)
+    return _collect_workers(None, device, n, addresses, strides, sizes, types, True, max_norm, eps)
 
 
 class CompAMSOptimizer:
@@ -207,10 +217,8 @@ class CompAMSOptimizer:
             if g is not None and (g.dtype != torch.float32 or g.device != dev or not g.is_contiguous() or g.is_neg()):
                 g = g.to(dev, torch.float32).resolve_neg().contiguous()
             grads.append(g)
-        pieces = []
-        for g, size in zip(grads, self._sizes):
-            pieces.append((None if g is None else g.data_ptr(), size, size, 0))
-        norms = _collect_workers(self.G, dev, self.n, pieces, max_norm is not None, limit, eps)
+        sizes, addresses = _with_elements(self._sizes, [0 if g is None else g.data_ptr() for g in grads])
+        norms = _collect_workers(self.G, dev, self.n, addresses, sizes, sizes, [0] * len(sizes), max_norm is not None, limit, eps)
         for leaf in leaves:
             leaf.grad = None
         return norms
