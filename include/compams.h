@@ -573,7 +573,8 @@ int compams_adapter_workspace_bytes(size_t* bytes, int32_t n, int64_t rows, int6
  *   target          device int64, packed [n, rows]: a column of the vocabulary, or `ignored`: the row's loss is 0 and it has no gradient. A
  *                   row with any other number has a loss of NaN.
  *   reduction       of the loss: 0 none, packed [n, rows]; 1 mean over each worker's rows that are not ignored (of none: 0), [n]; 2 sum, [n].
- *   lse             device, packed fp32 [n, rows]: receives log sum_v exp(z_jv), which the backward pass takes.
+ *   lse             device, fp32, n * rows + n elements: receives log sum_v exp(z_jv) of every row and, with a reduction, what each worker's
+ *                   rows count for (a mean's 1 / counted rows, a sum's 1), which the backward pass takes.
  *   workspace       device, 256-byte aligned, at least compams_head_workspace_bytes; used during the call's device work only.
  * 1 <= vocab < 2^31 - 4096. A row whose logits hold a NaN or an infinity above zero has a loss of NaN.
  */

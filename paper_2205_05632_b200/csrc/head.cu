@@ -200,19 +200,19 @@ struct JoinArgs {
     const float* target_logit;
     const int64_t* target;
     int64_t all_rows, rows, parts, ignored, vocab;
-    int32_t lanes;      // rows of a CTA, a power of two up to 32
+    int32_t lanes;      // rows of a CTA, a power of two up to 256
     int32_t whole;      // a CTA has a worker's rows, all of them
     int32_t reduction;
-    float *lse, *row_loss, *loss;
+    float *lse, *row_loss, *loss, *inverse;  // the last: a mean's 1 / counted rows, a sum's 1
 };
 __device__ __forceinline__ float sum_of_warp(float v) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
-// 32 rows (fewer where there are fewer) by 1024 / rows shares of the parts.
+// 32 rows (fewer where there are fewer, a worker's up to 256 where the parts are few) by 1024 / rows shares of the parts.
 __global__ void __launch_bounds__(1024) join_kernel(const __grid_constant__ JoinArgs a) {
-    __shared__ float2 shares[1024];
+    __shared__ float2 shares[1024], joint[8];
     dependency_wait();
     const int r = threadIdx.x & (a.lanes - 1), share = threadIdx.x / a.lanes, count = 1024 / a.lanes;
     const int64_t row = (int64_t)blockIdx.x * (a.whole ? a.rows : a.lanes) + r;
@@ -226,7 +226,7 @@ __global__ void __launch_bounds__(1024) join_kernel(const __grid_constant__ Join
         __syncthreads();
         if (share < o) shares[threadIdx.x] = merged(shares[threadIdx.x], shares[threadIdx.x + o * a.lanes]);
     }
-    if (threadIdx.x >= 32) return;
+    if (threadIdx.x >= 32 && (int)threadIdx.x >= a.lanes) return;  // (whole warps)
     __syncwarp();
     float loss = 0.0f, counted = 0.0f;
     if (there && (int)threadIdx.x < a.lanes) {
@@ -244,11 +244,25 @@ __global__ void __launch_bounds__(1024) join_kernel(const __grid_constant__ Join
     if (a.reduction == kNone || !a.whole) return;
     loss = sum_of_warp(loss);
     counted = sum_of_warp(counted);
-    if (threadIdx.x == 0) a.loss[blockIdx.x] = a.reduction == kMean ? loss / fmaxf(counted, 1.0f) : loss;
+    const int warps = (a.lanes + 31) / 32;
+    if (warps > 1) {
+        if ((threadIdx.x & 31) == 0) joint[threadIdx.x >> 5] = make_float2(loss, counted);
+        asm volatile("bar.sync 1, %0;" ::"r"(warps * 32) : "memory");
+        loss = counted = 0.0f;
+        for (int w = 0; w < warps; ++w) {
+            loss += joint[w].x;
+            counted += joint[w].y;
+        }
+    }
+    if (threadIdx.x == 0) {
+        const float inverse = a.reduction == kMean ? 1.0f / fmaxf(counted, 1.0f) : 1.0f;
+        a.inverse[blockIdx.x] = inverse;
+        a.loss[blockIdx.x] = a.reduction == kMean ? loss / fmaxf(counted, 1.0f) : loss;
+    }
 }
 // A worker's loss from its rows'.
 __global__ void __launch_bounds__(256) reduce_kernel(const float* __restrict__ row_loss, const int64_t* __restrict__ target, int64_t rows,
-                                                     int64_t ignored, int32_t reduction, float* __restrict__ loss) {
+                                                     int64_t ignored, int32_t reduction, float* __restrict__ loss, float* __restrict__ inverse) {
     __shared__ float sums[8], counts[8];
     dependency_wait();
     const int64_t row0 = blockIdx.x * rows;
@@ -270,6 +284,7 @@ __global__ void __launch_bounds__(256) reduce_kernel(const float* __restrict__ r
             count += counts[w];
         }
         loss[blockIdx.x] = reduction == kMean ? sum / fmaxf(count, 1.0f) : sum;
+        inverse[blockIdx.x] = reduction == kMean ? 1.0f / fmaxf(count, 1.0f) : 1.0f;
     }
 }
 
@@ -277,54 +292,36 @@ __global__ void __launch_bounds__(256) reduce_kernel(const float* __restrict__ r
 
 struct RowsArgs {
     const float* dloss;
-    int64_t ws, rs;  // of dloss; rs counts without a reduction alone
+    int64_t ws, rs;
     const int64_t* target;
     int64_t rows, ignored, vocab;
-    int32_t n, reduction, f16;
+    int32_t f16;
     float *g, *scale;     // [all rows], [n]
 };
-// A CTA per worker: its rows' g relative to the worker's scale.
+// Without a reduction: a CTA per worker, its rows' g relative to the power of two above the largest.
 __global__ void __launch_bounds__(256) rows_kernel(const __grid_constant__ RowsArgs a) {
-    __shared__ float counts[8], tops[8];
+    __shared__ float tops[8];
     dependency_wait();
     const int64_t i = blockIdx.x;
     const int64_t* target = a.target + i * a.rows;
     const float* dloss = a.dloss + i * a.ws;
-    float count = 0.0f, top = 0.0f;
+    float top = 0.0f;
     for (int64_t j = threadIdx.x; j < a.rows; j += 256)
-        if (target[j] != a.ignored) {
-            count += 1.0f;
-            if (a.reduction == kNone) top = fmaxf(top, fabsf(dloss[j * a.rs]));
-        }
-    count = sum_of_warp(count);
+        if (target[j] != a.ignored) top = fmaxf(top, fabsf(dloss[j * a.rs]));
 #pragma unroll
     for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    if ((threadIdx.x & 31) == 0) {
-        counts[threadIdx.x >> 5] = count;
-        tops[threadIdx.x >> 5] = top;
-    }
+    if ((threadIdx.x & 31) == 0) tops[threadIdx.x >> 5] = top;
     __syncthreads();
-    count = top = 0.0f;
 #pragma unroll
-    for (int w = 0; w < 8; ++w) {
-        count += counts[w];
-        top = fmaxf(top, tops[w]);
-    }
-    float scale = 1.0f, inverse = 1.0f;
-    if (a.reduction == kNone) {
-        int e = 0;
-        if (top > 0.0f && top < kInf) frexpf(top, &e);
-        e = max(e, -100);  // 2^-e is finite
-        scale = ldexpf(1.0f, e);
-        inverse = ldexpf(1.0f, -e);
-    } else {
-        scale = a.reduction == kMean ? dloss[0] / fmaxf(count, 1.0f) : dloss[0];
-    }
-    if (threadIdx.x == 0) a.scale[i] = a.f16 ? scale * (1.0f / head::kF16Scale) : scale;
+    for (int w = 0; w < 8; ++w) top = fmaxf(top, tops[w]);
+    int e = 0;
+    if (top > 0.0f && top < kInf) frexpf(top, &e);
+    e = max(e, -100);  // 2^-e is finite
+    const float inverse = ldexpf(1.0f, -e);
+    if (threadIdx.x == 0) a.scale[i] = ldexpf(a.f16 ? 1.0f / head::kF16Scale : 1.0f, e);
     for (int64_t j = threadIdx.x; j < a.rows; j += 256) {
         const int64_t t = target[j];
-        const float g = a.reduction == kNone ? inverse * dloss[j * a.rs] : 1.0f;
-        a.g[i * a.rows + j] = t == a.ignored ? 0.0f : t >= 0 && t < a.vocab ? g : __int_as_float(0x7fffffff);  // no such column
+        a.g[i * a.rows + j] = t == a.ignored ? 0.0f : t >= 0 && t < a.vocab ? inverse * dloss[j * a.rs] : __int_as_float(0x7fffffff);  // no such column
     }
 }
 
@@ -333,7 +330,7 @@ struct PartsArgs {
     const float* parts;  // [parts][all rows][pitch]
     int64_t part, all_rows, chunks;
     int32_t count, h, per_row, pitch;
-    const float* scale;  // of a worker
+    head::Scale scale;   // of a worker
     int64_t worker_rows;
     void* out;           // [all rows][h]
 };
@@ -351,7 +348,7 @@ __global__ void __launch_bounds__(256) parts_kernel(const __grid_constant__ Part
         v[0] += p.x; v[1] += p.y; v[2] += p.z; v[3] += p.w;
         v[4] += q.x; v[5] += q.y; v[6] += q.z; v[7] += q.w;
     }
-    const float scale = a.scale[row / a.worker_rows];
+    const float scale = head::scale_of(a.scale, row / a.worker_rows);
 #pragma unroll
     for (int k = 0; k < 8; ++k) v[k] *= scale;
     T* out = (T*)a.out + row * a.h + c;
@@ -725,14 +722,16 @@ int compams_head_forward(float* loss, float* lse, const void* x, int32_t type, c
     JoinArgs j = {};
     j.stats = stats; j.target_logit = target_logit; j.target = target; j.all_rows = z.all_rows(); j.rows = rows; j.parts = p.stat_parts;
     j.ignored = ignored; j.vocab = vocab; j.reduction = reduction; j.lse = lse; j.row_loss = (float*)(work + p.row_loss); j.loss = loss;
-    j.whole = reduction != kNone && rows <= 32;
+    j.inverse = lse + j.all_rows;
+    // (256 rows of 250 parts: 16 us by one CTA a worker, 6 + 2 by two kernels; 100 of 63: 4.5, and a launch less)
+    j.whole = reduction != kNone && (rows <= 32 || (rows <= 256 && rows * p.stat_parts <= 16384));
     const int64_t most = j.whole ? rows : std::min<int64_t>(32, j.all_rows);
     for (j.lanes = 1; j.lanes < most;) j.lanes *= 2;
     const int64_t ctas = j.whole ? n : (j.all_rows + j.lanes - 1) / j.lanes;
     rc = launched(launch_sized(join_kernel, dim3((uint32_t)ctas), 1024, 1, 0, false, stream, j), "head_join");
     if (rc != COMPAMS_OK || j.whole || reduction == kNone) return rc;
     return launched(launch_sized(reduce_kernel, dim3((uint32_t)n), 256, 1, 0, false, stream, (const float*)j.row_loss, target, rows, ignored,
-                                 reduction, loss),
+                                 reduction, loss, j.inverse),
                     "head_reduce");
 }
 
@@ -763,12 +762,19 @@ int compams_head_backward(void* dx, void* dweight, int32_t sum_workers, const fl
         return COMPAMS_ERR_INVALID_ARG;
     char* work = (char*)workspace;
     const int64_t all = z.all_rows();
-    RowsArgs r = {};
-    r.dloss = dloss; r.ws = dloss_worker_stride; r.rs = dloss_row_stride; r.target = target; r.rows = rows; r.ignored = ignored; r.vocab = vocab; r.n = n;
-    r.reduction = reduction; r.f16 = z.f16(); r.g = (float*)(work + p.g); r.scale = (float*)(work + p.scale);
-    int rc = launched(launch_sized(rows_kernel, dim3((uint32_t)n), 256, 1, 0, true, stream, r), "head_rows");
+    // a mean's and a sum's rows have d by itself, and the worker's factor is found where it is needed; without a reduction each has its own
+    head::Scale scale = {nullptr, dloss, lse + all, dloss_worker_stride, z.f16() ? 1.0f / head::kF16Scale : 1.0f};
+    const float* row_gradient = nullptr;
+    int rc = COMPAMS_OK;
+    if (reduction == kNone) {
+        RowsArgs r = {};
+        r.dloss = dloss; r.ws = dloss_worker_stride; r.rs = dloss_row_stride; r.target = target; r.rows = rows; r.ignored = ignored; r.vocab = vocab;
+        r.f16 = z.f16(); r.g = (float*)(work + p.g); r.scale = (float*)(work + p.scale);
+        rc = launched(launch_sized(rows_kernel, dim3((uint32_t)n), 256, 1, 0, true, stream, r), "head_rows");
+        scale.own = r.scale;
+        row_gradient = r.g;
+    }
     Operand xo, wo;
-    const float* scale = r.scale;
     uint16_t* d = (uint16_t*)(work + p.d);
     const int32_t tiles_h = (int32_t)((h + 255) / 256), tiles_rows = (int32_t)((z.batch_rows() + 255) / 256);
     for (int64_t v0 = 0; v0 < vocab && rc == COMPAMS_OK; v0 += p.piece) {
@@ -783,7 +789,7 @@ int compams_head_backward(void* dx, void* dweight, int32_t sum_workers, const fl
             a.segments = 1; a.steps = a.part_steps = (int32_t)((h + 63) / 64);
             pairs_of(a, z.x_planes(), z.w_planes(), 2);
             a.right_row = first; a.rows = z.batch_rows(); a.columns = (int32_t)vocab; a.first = (int32_t)v0; a.target = target;
-            a.all_rows = all; a.lse = lse; a.row_gradient = r.g; a.probs_planes = p.probs;
+            a.all_rows = all; a.lse = lse; a.row_gradient = row_gradient; a.ignored = ignored; a.probs_planes = p.probs;
             CUtensorMap out = {};
             if (!result_map(&out, d, z.f16() ? kTypeF16 : kTypeBF16, p.width, z.batch_rows(), z.batches() * p.probs, p.width, z.batch_rows() * p.width))
                 return COMPAMS_ERR_INVALID_ARG;
@@ -800,8 +806,9 @@ int compams_head_backward(void* dx, void* dweight, int32_t sum_workers, const fl
             void* to = p.sums ? (void*)(work + p.dx_sums) : dx;
             a.out_row = p.sums ? z.pitch() : h;
             a.columns = (int32_t)a.out_row; a.out_type = p.sums ? kTypeF32 : type; a.out_batch = z.batch_rows() * a.out_row;
-            if (p.sums) a.add = v0 > 0;
-            else { a.scale = scale; a.worker_rows = rows; }
+            a.add = p.sums && v0 > 0;
+            a.scale = scale; a.worker_rows = rows;
+            if (p.sums) a.scale.factor = 0.0f;  // later
             CUtensorMap out = {};
             if (!result_map(&out, to, a.out_type, a.out_row, z.batch_rows(), z.batches() * p.parts, a.out_row, a.out_batch)) a.out = to;
             rc = product<head::kInput>(a, by_batch, wo, out, z.f16(), stream, "head_input");

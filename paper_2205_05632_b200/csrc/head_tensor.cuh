@@ -52,6 +52,16 @@ constexpr int kMostPairs = 6;
 // The barriers: a stage has landed (of both CTAs, at the first); its products are done; the sums are ready, and drained (at the first).
 constexpr int kFull = 0, kEmpty = kMostStages, kReady = 2 * kMostStages, kDrained = kReady + 2, kStopped = kDrained + 2, kBars = kStopped + 1;
 
+// What a worker's rows of d are multiplied by: a number of its own, or its loss's gradient times `inverse`.
+struct Scale {
+    const float *own, *dloss, *inverse;
+    int64_t stride;  // of dloss
+    float factor;
+};
+__device__ __forceinline__ float scale_of(const Scale& s, int64_t worker) {
+    return s.own ? s.own[worker] : s.factor * (s.dloss[worker * s.stride] * s.inverse[worker]);
+}
+
 struct Args {
     // the tiles, in this order: batch, part of the sum, row and column in groups of kRaster rows
     int32_t tiles_m, tiles_n, batches, parts;
@@ -75,14 +85,15 @@ struct Args {
     float* target_logit;
     float2* stats;         // FORWARD: [half tile of the vocabulary][all rows]: maximum, sum of exp(z - maximum)
     int64_t all_rows;
-    const float *lse, *row_gradient;
+    int64_t ignored;
+    const float *lse, *row_gradient;  // PROBS: the latter is null where all rows' are 1, 0 for an ignored target
     int32_t probs_planes;
     // PROBS, INPUT, WEIGHT: the third map is of what is written, [plane or part][batch][row][column] from out_first's row on
     int32_t out_type, add;  // add: onto what is there (fp32)
     int32_t out_first;
     void* out;              // where the third map does not serve (rows off 16-byte boundaries); else null
     int64_t out_batch, out_row;  // elements
-    const float* scale;                    // of a worker; null: 1
+    Scale scale;            // of a worker
     int64_t worker_rows;
 };
 
@@ -372,7 +383,7 @@ __device__ __forceinline__ void finish(const Args& a, const CUtensorMap* map, ui
 #pragma unroll
         for (int c = 0; c < 128; ++c) sum[c] = 0.0f;
         for (int segment = 0, done = 0; segment < a.segments && all > 0; done + a.stretch < all ? done += a.stretch : (done = 0, ++segment)) {
-            const float worth = FORM == kWeight && a.scale ? a.scale[p.batch + segment] : 1.0f;
+            const float worth = FORM == kWeight ? scale_of(a.scale, p.batch + segment) : 1.0f;
             lost = lost || !barrier_wait(bars + 8 * (kReady + buffer), ready >> buffer & 1u, a.tries);
             ready ^= 1u << buffer;
             __syncwarp();
@@ -398,8 +409,8 @@ __device__ __forceinline__ void finish(const Args& a, const CUtensorMap* map, ui
         if constexpr (FORM == kForward || FORM == kProbs) {
             const int64_t number = (int64_t)p.batch * a.rows + row;
             const int left = a.columns - (a.first + column0);  // columns from here on
-            const int64_t wanted_at = there ? a.target[number] - a.first - column0 : -1;
-            const int mine = wanted_at >= 0 && wanted_at < min(left, 128) ? (int)wanted_at : -1;
+            const int64_t target = there ? a.target[number] : -1, wanted_at = target - a.first - column0;
+            const int mine = target >= 0 && wanted_at >= 0 && wanted_at < min(left, 128) ? (int)wanted_at : -1;
             if constexpr (FORM == kForward) {
                 float top = __int_as_float(0xff800000);
 #pragma unroll
@@ -416,7 +427,10 @@ __device__ __forceinline__ void finish(const Args& a, const CUtensorMap* map, ui
                     if (mine >= 0) a.target_logit[number] = wanted;
                 }
             } else {
-                const float lse = there ? a.lse[number] : 0.0f, g = !there ? 0.0f : lost ? nan : a.row_gradient[number];
+                const float lse = there ? a.lse[number] : 0.0f;
+                float g = 0.0f;
+                if (there) g = a.row_gradient ? a.row_gradient[number] : target == a.ignored ? 0.0f : target >= 0 && target < a.columns ? 1.0f : nan;
+                if (lost) g = nan;
                 const float scale = a.f16 ? g * kF16Scale : g;
 #pragma unroll
                 for (int c = 0; c < 128; ++c) {
@@ -445,7 +459,7 @@ __device__ __forceinline__ void finish(const Args& a, const CUtensorMap* map, ui
             }
         } else {
             float scale = 1.0f;
-            if (FORM == kInput && a.scale) scale = there ? a.scale[((int64_t)p.batch * a.rows + row) / a.worker_rows] : 0.0f;
+            if (FORM == kInput && a.scale.factor != 0.0f) scale = there ? scale_of(a.scale, ((int64_t)p.batch * a.rows + row) / a.worker_rows) : 0.0f;
             if (lost) scale = nan;
             const int rows = (int)min((int64_t)32, a.rows - row0), left = a.columns - column0, z = p.part * a.batches + p.batch;
             const int64_t first = z * a.out_batch + (row0 + a.out_first) * a.out_row + column0;

@@ -132,6 +132,10 @@ Encode map_encoder() {
             f = nullptr;
         return (Encode)f;
     }();
+    // It wants the device's context current in its thread, which the first launch sees to; this may come before one.
+    static thread_local int bound = -1;
+    int device = 0;
+    if (cudaGetDevice(&device) == cudaSuccess && device != bound && cudaSetDevice(device) == cudaSuccess) bound = device;
     return encode;
 }
 

@@ -590,7 +590,7 @@ class _Head:
 
 
 def _head_forward(x, weight, target, reduction, ignored):
-    lse = x.new_empty(target.shape, dtype=torch.float32)
+    lse = x.new_empty(target.numel() + x.shape[0], dtype=torch.float32)  # and what each worker's rows count for
     make = x.new_empty if x.numel() else x.new_zeros
     loss = make(target.shape if reduction == 0 else x.shape[:1], dtype=torch.float32)
     if x.numel():
