@@ -172,6 +172,26 @@ def load_library() -> ctypes.CDLL:
     return L
 
 
+_ops = None
+
+
+def load_operators():
+    """The extension with the operators' usual calls (built in-tree beside the library, whose addresses it gets)."""
+    global _ops
+    if _ops is None:
+        L = load_library()
+        try:
+            from . import _torch_ops
+        except ImportError as e:
+            raise CompAMSError("the extension of %s cannot be loaded (%s): build it with `python -m paper_2205_05632_b200.build`" % (
+                _HERE, e)) from e
+        _torch_ops.bind(*[ctypes.cast(getattr(L, "compams_" + name), ctypes.c_void_p).value for name in (
+            "rms_norm_forward", "rms_norm_backward", "rms_norm_workspace_bytes", "head_forward", "head_backward", "head_workspace_bytes",
+            "collect_workers", "collect_workers_workspace_bytes", "error_string", "last_cuda_error")], CompAMSError)
+        _ops = _torch_ops
+    return _ops
+
+
 def _check(rc: int, what: str) -> None:
     if rc != 0:
         L = load_library()

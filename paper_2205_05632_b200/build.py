@@ -18,6 +18,11 @@ NVCC_FLAGS = [
 ]
 
 
+# The operators' usual calls for torch: a Python extension beside the library, which it reaches through its addresses.
+EXTENSION = os.path.join(HERE, "_torch_ops.so")
+EXTENSION_SOURCE = os.path.join(CSRC, "torch_ops.cpp")
+
+
 def _nvcc() -> str:
     for cand in (os.environ.get("NVCC"), "/usr/local/cuda/bin/nvcc", "nvcc"):
         if cand and (os.path.sep not in cand or os.path.exists(cand)):
@@ -33,7 +38,27 @@ def _stale() -> bool:
     return any(os.path.getmtime(p) > t for p in deps)
 
 
+def build_extension(force: bool = False) -> str:
+    deps = [EXTENSION_SOURCE, os.path.join(HERE, "..", "include", "compams.h"), os.path.abspath(__file__)]
+    if not force and os.path.exists(EXTENSION) and all(os.path.getmtime(p) <= os.path.getmtime(EXTENSION) for p in deps):
+        return EXTENSION
+    import sysconfig
+
+    import torch
+    root = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(_nvcc())) if os.path.sep in _nvcc() else "/usr/local/cuda"
+    tmp = EXTENSION + ".tmp.%d" % os.getpid()
+    subprocess.run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared",
+                    "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI), "-isystem", os.path.join(root, "include"), "-isystem",
+                    os.path.join(root, "include", "torch", "csrc", "api", "include"), "-isystem", os.path.join(cuda, "include"), "-isystem",
+                    sysconfig.get_paths()["include"], EXTENSION_SOURCE, "-o", tmp, "-L" + os.path.join(root, "lib"), "-lc10", "-lc10_cuda",
+                    "-ltorch_cpu", "-ltorch_python"], check=True)
+    os.replace(tmp, EXTENSION)
+    return EXTENSION
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
+    build_extension(force)
     if not force and not _stale():
         return LIB
     tmp = LIB + ".tmp.%d" % os.getpid()

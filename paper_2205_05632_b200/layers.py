@@ -41,7 +41,7 @@ from typing import Optional, Tuple, Union
 import torch
 from torch.autograd import forward_ad
 
-from .binding import CompAMSError, _check, load_library
+from .binding import CompAMSError, _check, load_library, load_operators
 
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 Call = Union[int, torch.Tensor]
@@ -450,6 +450,9 @@ def _epsilon(eps: float) -> float:
 
 def rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, eps: float = 1e-6) -> torch.Tensor:
     """x / sqrt(mean(x^2) + eps) * weight over the last axis of x [n, ..., h], in x's type; weight is float32 [h] or [n, h]."""
+    y = None if forward_ad._current_level >= 0 else load_operators().rms_norm(x, weight, eps)
+    if y is not None:  # a usual call; the others go through this file
+        return y
     _activation(x)
     weight = None if weight is None else _factor(weight, x, x.shape[-1:], "weight")
     eps = _epsilon(eps)
@@ -464,6 +467,9 @@ def gated_add_rms_norm(x: torch.Tensor, residual: torch.Tensor, weight: Optional
     """(rms_norm(s, next_weight), s) with s = residual_scale * residual + gate * rms_norm(x, weight): the norm behind a block, its gate, the
     residual stream and the norm before the next block. s has the residual's type, which is x's or float32, and is normalised as it is
     stored; the first result has x's type. weight, gate and next_weight are float32 [h], or all [n, h]; None: 1."""
+    got = None if forward_ad._current_level >= 0 else load_operators().gated_add_rms_norm(x, residual, weight, gate, next_weight, residual_scale, eps)
+    if got is not None:
+        return got
     _activation(x)
     _like(residual, x, "residual", (x.dtype, torch.float32))
     args = (x, residual, *_rms_parameters(x, weight, gate, next_weight), float(residual_scale), _epsilon(eps))
@@ -635,8 +641,12 @@ def linear_cross_entropy(x: torch.Tensor, weight: torch.Tensor, target: torch.Te
     A target outside the vocabulary makes the loss NaN, and with it the gradients that it reaches.
 
     A float32 weight is taken as it is, in three products of bfloat16 for one (six where x is float32); a 16-bit weight in one."""
+    number = _REDUCTIONS.get(reduction) if type(reduction) is str else None
+    loss = None if forward_ad._current_level >= 0 else load_operators().linear_cross_entropy(x, weight, target, number, ignore_index)
+    if loss is not None:
+        return loss
     _activation(x)
-    if reduction not in _REDUCTIONS:
+    if number is None:
         raise CompAMSError("reduction must be one of %s: got %r" % (sorted(_REDUCTIONS), reduction))
     n, h = x.shape[0], x.shape[-1]
     if (not isinstance(weight, torch.Tensor) or weight.device != x.device or weight.dtype not in (x.dtype, torch.float32)
@@ -650,5 +660,5 @@ def linear_cross_entropy(x: torch.Tensor, weight: torch.Tensor, target: torch.Te
         weight = weight.resolve_neg()
     if weight.stride(-1) != 1 and h > 1:
         weight = weight.contiguous()
-    args = (x, weight, target.contiguous(), _REDUCTIONS[reduction], int(ignore_index))
+    args = (x, weight, target.contiguous(), number, int(ignore_index))
     return _HeadFunction.apply(*args) if _through_autograd(x, weight) else _head_forward(*args)[0]

@@ -24,7 +24,7 @@ from typing import Iterable, List, Optional, Sequence, Tuple, Union
 import numpy as np
 import torch
 
-from .binding import RANDK, TOPK, CompAMS, CompAMSError, _check, load_library
+from .binding import RANDK, TOPK, CompAMS, CompAMSError, _check, load_library, load_operators
 
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _INFINITY = float("inf")
@@ -103,6 +103,9 @@ def collect_gradients(grads: Union[torch.Tensor, Sequence[torch.Tensor]], out: O
     """(G, norms): the workers' gradients, one tensor [n, *shape] per parameter in float32, bfloat16 or float16, gathered as the rows of a
     float32 tensor [n, d], `out` where given, and each worker's global norm over all of them, [n], as it was. Rows whose norm is above
     max_norm are multiplied by max_norm / (norm + eps). The tensors may not overlap out."""
+    got = load_operators().collect_gradients(grads, out, _INFINITY if max_norm is None else max_norm, eps)
+    if got is not None:  # a usual call: a list of packed tensors
+        return got
     grads, n, device, types = _gradients(grads, "collect_gradients")
     max_norm, eps = _limit(max_norm, eps)
     if not all(map(_T.is_contiguous, grads)) or any(map(_T.is_neg, grads)):

@@ -109,3 +109,26 @@ def test_a_second_derivative_is_refused():
         dx, = torch.autograd.grad(y, x, create_graph=True)
         with pytest.raises(RuntimeError):
             dx.sum().backward()
+
+
+def test_tangents_are_refused_and_tracing_records():
+    from torch.autograd import forward_ad
+    x, w = torch.randn(2, 3, 8, device="cuda"), torch.randn(5, 8, device="cuda")
+    t = torch.zeros(2, 3, dtype=torch.int64, device="cuda")
+    calls = (lambda v: linear_cross_entropy(v, w, t), rms_norm, lambda v: gated_add_rms_norm(v, v)[0])
+    for call in calls:
+        with forward_ad.dual_level():
+            dual = forward_ad.make_dual(x, torch.ones_like(x))
+            with pytest.raises(Exception):
+                call(dual)
+            assert torch.equal(call(x), call(x.clone()))  # without a tangent a level changes nothing
+        traced = torch.jit.trace(call, (x,), check_trace=False)
+        other = torch.randn(2, 3, 8, device="cuda")
+        assert torch.equal(traced(other), call(other))
+
+
+def test_a_library_error_is_the_bindings_own():
+    # a size that the library refuses and no check before it: 2^31 pieces of gradients cannot be had, a vocabulary of 2^31 rows can, of none
+    w = torch.zeros(1, 8, device="cuda").expand(1 << 31, 8)
+    with pytest.raises(CompAMSError):
+        linear_cross_entropy(torch.zeros(2, 3, 8, device="cuda"), w, torch.zeros(2, 3, dtype=torch.int64, device="cuda"))
