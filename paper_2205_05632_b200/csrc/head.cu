@@ -105,14 +105,23 @@ struct FewArgs {
     float* target_logit;
     float2* stats;  // [CTA][all rows]
 };
-// A warp takes four rows of W at a time, a lane eight columns (or every 32nd) of each: 64 bytes of W for one reading of x.
+// A warp takes a share of the rows of W, for one row of x a row at a time and eight CTAs to an SM (32000 rows of 4096 bfloat16 columns, 262 MB:
+// 46 us; four rows at a time and four CTAs 49, two and six 51), for more of them four, so that x is read once for four; a lane has eight
+// columns (or every 32nd) of each.
+__host__ __device__ constexpr int rows_at_once(int rows) { return rows == 1 ? 1 : 4; }
+__host__ __device__ constexpr int ctas_at_once(int rows) { return rows == 1 ? 8 : 4; }
 template <typename TX, typename TW, int MR, bool VEC>
-__global__ void __launch_bounds__(256) few_kernel(const __grid_constant__ FewArgs a) {
+__global__ void __launch_bounds__(256, MR == 1 ? ctas_at_once(MR) : 1) few_kernel(const __grid_constant__ FewArgs a) {
     extern __shared__ __align__(16) float xs[];  // [MR][h up to a multiple of 8]
     __shared__ float2 joint[8][MR];
+    constexpr int kRows = rows_at_once(MR);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pitch = (a.h + 7) & ~7;
     const int64_t batch = blockIdx.y, number0 = batch * a.rows;
     const TW* weight = (const TW*)a.weight + batch * a.w_ws;
+    // a warp's rows, as many as any other's but for one
+    const int64_t warps = (int64_t)gridDim.x * 8, mine = (int64_t)blockIdx.x * 8 + warp;
+    const int last = (int)(a.vocab * (mine + 1) / warps);
+    const int start = (int)(a.vocab * mine / warps);
     for (int r = 0; r < MR; ++r) {
         const TX* x = (const TX*)a.x + (batch + r / a.worker_rows) * a.x_ws + r % a.worker_rows * a.x_rs;
         for (int c = threadIdx.x; c < pitch; c += 256) xs[r * pitch + c] = r < a.rows && c < a.h ? to_float(x[c]) : 0.0f;
@@ -125,30 +134,27 @@ __global__ void __launch_bounds__(256) few_kernel(const __grid_constant__ FewArg
         target[r] = r < a.rows ? a.target[number0 + r] : -1;
         state[r] = make_float2(-kInf, 0.0f);
     }
-    // a warp's rows, as many as any other's but for one
-    const int64_t warps = (int64_t)gridDim.x * 8, mine = (int64_t)blockIdx.x * 8 + warp;
-    const int last = (int)(a.vocab * (mine + 1) / warps);
-    for (int v0 = (int)(a.vocab * mine / warps); v0 < last; v0 += 4) {
-        float acc[4][MR] = {};
-        const TW* row[4];
+    for (int v0 = start; v0 < last; v0 += kRows) {
+        float acc[kRows][MR] = {};
+        const TW* row[kRows];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) row[j] = weight + (int64_t)min(v0 + j, last - 1) * a.w_rs;
+        for (int j = 0; j < kRows; ++j) row[j] = weight + (int64_t)min(v0 + j, last - 1) * a.w_rs;
         if constexpr (VEC) {
 #pragma unroll 2
             for (int c = lane * 8; c < a.h; c += kSpan) {
-                Raw8<TW> raw[4];
+                Raw8<TW> raw[kRows];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) raw[j] = raw_load<TW>(row[j] + c);
-                float w[4][8];
+                for (int j = 0; j < kRows; ++j) raw[j] = raw_load<TW>(row[j] + c);
+                float w[kRows][8];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) raw_floats<TW>(raw[j], w[j]);
+                for (int j = 0; j < kRows; ++j) raw_floats<TW>(raw[j], w[j]);
 #pragma unroll
                 for (int r = 0; r < MR; ++r) {
                     float v[8];
                     *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(xs + r * pitch + c);
                     *reinterpret_cast<float4*>(v + 4) = *reinterpret_cast<const float4*>(xs + r * pitch + c + 4);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
+                    for (int j = 0; j < kRows; ++j)
 #pragma unroll
                         for (int k = 0; k < 8; ++k) acc[j][r] = fmaf(w[j][k], v[k], acc[j][r]);
                 }
@@ -156,17 +162,17 @@ __global__ void __launch_bounds__(256) few_kernel(const __grid_constant__ FewArg
         } else {
 #pragma unroll 4
             for (int c = lane; c < a.h; c += 32) {
-                float w[4];
+                float w[kRows];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) w[j] = to_float(__ldg(row[j] + c));
+                for (int j = 0; j < kRows; ++j) w[j] = to_float(__ldg(row[j] + c));
 #pragma unroll
                 for (int r = 0; r < MR; ++r)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) acc[j][r] = fmaf(w[j], xs[r * pitch + c], acc[j][r]);
+                    for (int j = 0; j < kRows; ++j) acc[j][r] = fmaf(w[j], xs[r * pitch + c], acc[j][r]);
             }
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < kRows; ++j)
 #pragma unroll
             for (int r = 0; r < MR; ++r) {
                 float z = acc[j][r];
@@ -430,11 +436,10 @@ struct Plan {
 constexpr int64_t kCopyBytes = 64ll << 20;   // of a piece's copy of W: it stays in the L2 between its writing and its reading
 constexpr int64_t kProbsBytes = 512ll << 20;  // of a piece's d
 constexpr int64_t kSumsBytes = 256ll << 20;   // of the parts' sums of dx
-constexpr int kFewWaves = 4;                  // CTAs of few_kernel to an SM
 
 int64_t up_to(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 int64_t few_ctas(const HeadShape& z) {
-    return std::max<int64_t>(1, std::min<int64_t>((z.vocab + 31) / 32, ((int64_t)multiprocessors() * kFewWaves + z.batches() - 1) / z.batches()));
+    return std::max<int64_t>(1, std::min<int64_t>((z.vocab + 31) / 32, ((int64_t)multiprocessors() * ctas_at_once((int)z.batch_rows()) + z.batches() - 1) / z.batches()));
 }
 
 // Parts of the vocabulary's sum of dx: as many as take the pairs of CTAs the shortest time, in tiles of 64 (0.3 us), with what adding up
@@ -628,6 +633,10 @@ int operands(const HeadShape& z, const void* x, int64_t x_ws, int64_t x_rs, cons
 template <typename TX, typename TW, int MR>
 int few_rows(const HeadShape& z, FewArgs& a, bool vec, int64_t ctas, cudaStream_t stream) {
     const auto kernel = vec ? few_kernel<TX, TW, MR, true> : few_kernel<TX, TW, MR, false>;
+    if (MR * z.pitch() * 4 > 48 * 1024) {  // the most that a call may want, as it is asked for once
+        const cudaError_t e = allow_shared((const void*)kernel, kFewShared);
+        if (e != cudaSuccess) return launched(e, "head_few");
+    }
     return launched(launch_sized(kernel, dim3((uint32_t)ctas, (uint32_t)z.batches()), 256, 1, (size_t)(MR * z.pitch() * 4), true, stream, a),
                     "head_few");
 }

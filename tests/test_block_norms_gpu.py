@@ -188,6 +188,28 @@ def test_no_rows():
     assert y.shape == s.shape == x.shape and not dw.any()
 
 
+@pytest.mark.parametrize("h", [96, 97])
+def test_some_gradients_alone_are_the_same(h):
+    g = gen(9)
+    values = [rand(g, 3, 10, h, dtype=BF16), rand(g, 3, 10, h)] + [1 + 0.2 * rand(g, 3, h) for _ in range(3)]
+    dy, ds = rand(g, 3, 10, h, dtype=BF16), rand(g, 3, 10, h)
+
+    def gradients(wanted, given=(1, 1, 1, 1, 1)):
+        leaves = [(v.clone().requires_grad_() if k in wanted else v) if given[k] else None for k, v in enumerate(values)]
+        out = gated_add_rms_norm(*leaves)
+        return torch.autograd.grad(out, [leaves[k] for k in wanted], (dy, ds))
+
+    everything = gradients((0, 1, 2, 3, 4))
+    for wanted in ((0,), (1,), (2,), (3,), (4,), (0, 4), (1, 3), (2, 3)):
+        assert all(torch.equal(a, everything[k]) for a, k in zip(gradients(wanted), wanted))
+    without = gradients((0, 1, 3), (1, 1, 0, 1, 1))  # a parameter that is not given in front of one that is
+    assert all(torch.equal(a, b) for a, b in zip(gradients((3,), (1, 1, 0, 1, 1)), without[2:]))
+    x, w = values[0].clone().requires_grad_(), values[2].clone().requires_grad_()
+    dx, dw = torch.autograd.grad(rms_norm(x, w), (x, w), dy)
+    assert torch.equal(torch.autograd.grad(rms_norm(x, values[2]), x, dy)[0], dx)
+    assert torch.equal(torch.autograd.grad(rms_norm(values[0], w), w, dy)[0], dw)
+
+
 def test_the_same_tensor_everywhere():
     g = gen(6)
     x, w = rand(g, 2, 6, 96).requires_grad_(), (1 + 0.2 * rand(g, 2, 96)).requires_grad_()

@@ -209,6 +209,15 @@ def test_gradients_against_differences():
     assert abs(float(up - down) / (2 * e) - along) < 30 * e * e + 1e-3
 
 
+@pytest.mark.parametrize("kinds", TYPES, ids=str)
+def test_a_few_rows_of_growing_width(kinds):
+    # more shared memory from call to call, up to what a few rows may have, and beyond, where other kernels take over
+    for rows, h in ((1, 12800), (1, 16000), (1, 24576), (1, 24577), (2, 8000), (2, 12288), (4, 4000), (4, 6144), (4, 6145)):
+        x, w, t, g = inputs(rows + h, 1, rows, h, 40, *kinds, "shared", 0.0)
+        want, tol = B.head(x, w, t, "none")
+        B.check(linear_cross_entropy(x, w, t, "none"), want, tol, "loss")
+
+
 @pytest.mark.parametrize("rows", [1, 130])
 def test_offsets_beyond_32_bits(rows):
     vocab, h = 140000, 16384  # 2.3 G elements
