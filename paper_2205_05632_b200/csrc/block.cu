@@ -168,8 +168,11 @@ __device__ __forceinline__ double squares8(const Pair (&v)[4]) {
     return (s[0] + s[1]) + (s[2] + s[3]);
 }
 
+// 16384 bfloat16 rows: norm of 2048 columns 22 us (6.1 TB/s) with registers for 1024 threads to an SM, 28 with them for 768; gated of 4096
+// 144 us (3.7 TB/s) with registers for 512, 219 and spills for 768: the two sums, one in binary64, and what a row's rounding takes are 300
+// instructions a thread, and 16 warps do not cover the barriers between them.
 template <typename T, typename R, bool GATED, bool VEC, int K>
-__global__ void __launch_bounds__(K == 1 ? 256 : kMostThreads, K == 1 ? 2 : 1) block_forward_kernel(const __grid_constant__ BlockArgs a) {
+__global__ void __launch_bounds__(K == 1 ? 256 : kMostThreads, GATED ? (K == 1 ? 2 : 1) : (K == 1 ? 4 : 2)) block_forward_kernel(const __grid_constant__ BlockArgs a) {
     constexpr bool kWide = GATED && !std::is_same_v<R, float>;  // s is rounded to 16 bits
     using Sum = std::conditional_t<kWide, double, float>;
     __shared__ __align__(16) Sum scratch[kScratch];
@@ -354,6 +357,7 @@ __global__ void __launch_bounds__(K == 1 ? 256 : kMostThreads, K == 1 ? 2 : 1) b
     }
 }
 
+// The same rows: norm of 2048 columns 40 us (5.0 TB/s), gated of 4096 158 us (5.1 TB/s); more threads to an SM spill (47, 247).
 template <typename T, typename R, bool GATED, bool VEC, int K>
 __global__ void __launch_bounds__(K == 1 ? 256 : kMostThreads, K == 1 ? 2 : 1) block_backward_kernel(const __grid_constant__ BlockArgs a) {
     __shared__ __align__(16) float scratch[kScratch];
@@ -773,7 +777,7 @@ int compams_rms_norm_forward(void* y, void* s, float* stats, const void* x, cons
     a.x = x; a.residual = residual; a.y = y; a.s = s; a.stats = (float2*)stats; a.weight = weight; a.gate = gate; a.next = next;
     a.weight_ws = weight_stride; a.gate_ws = gate_stride; a.next_ws = next_stride;
     a.x_ws = x_worker_stride; a.x_rs = x_row_stride; a.r_ws = residual_worker_stride; a.r_rs = residual_row_stride;
-    a.rows = (uint32_t)rows; a.groups = z.groups(gated ? 512 : 768); a.h = (int32_t)h; a.alpha = (float)residual_scale; a.alpha64 = residual_scale; a.eps = eps;
+    a.rows = (uint32_t)rows; a.groups = z.groups(gated ? 512 : 1024); a.h = (int32_t)h; a.alpha = (float)residual_scale; a.alpha64 = residual_scale; a.eps = eps;
     return by_block_types(type, gated ? residual_type : type, [&](auto t, auto r) {
         using T = decltype(t);
         using R = decltype(r);
