@@ -10,8 +10,9 @@ the optimizer's parameter vector, and collect_all() makes their gradients the ro
         y, s = dropout_add_layer_norm(x, residual, w, b, p=0.1, seed=seed, call=2 * t)
         z = low_rank_adapter(y, project(y), A, B, scale=2.0, p=0.1, seed=seed, call=2 * t + 1)
         ...
-        loss.backward()
-        opt.collect_all()
+        loss = linear_cross_entropy(z, head, targets)   # [n], each worker's mean
+        loss.sum().backward()
+        opt.collect_all(max_norm=1.0)                   # every worker's gradient clipped by itself
         opt.step()
 
 Dropout draws from a counter-based generator, Philox4x32-10: the bit of element (worker + i, row j, column c) of use number `call`
@@ -22,7 +23,8 @@ to keep its value until the backward pass is done (add to it behind that).
 
 The operators run on the current stream of x's device. They are differentiable once, backwards; their outputs are packed. Forward-mode
 derivatives, torch.func's transforms and recording by make_fx are refused; torch.jit.trace records the operator as a Python function.
-n is at most 65535.
+n is at most 65535. rms_norm, gated_add_rms_norm and linear_cross_entropy take their usual calls, packed tensors that nobody traces, through
+an extension (binding.load_operators) and the others through this file: the same kernels and results, at a third of the host's time.
 
 Forward and backward can be captured into a CUDA graph together. As with every torch backward pass, the leaves' gradient nodes belong to
 the stream on which they were first used: warm up on the capturing stream, and let no autograd graph of the same leaves from another
@@ -30,7 +32,8 @@ stream live while capturing.
 
 Not finite: a row of a norm with an infinity or a NaN in it is NaN, and so are its gradients; a dropped element is 0 whatever it was. In
 an adapter what an infinity or a NaN reaches is infinite or NaN, as a sum over it is, but which of the two may differ from a plain product.
-NaN is also what an adapter's kernel leaves whose bounded waits run out (compams_adapter_status says so; nothing should bring it about).
+NaN is also what a kernel of an adapter or of the head leaves whose bounded waits run out (compams_adapter_status, compams_head_status say so;
+nothing should bring it about). In the head a row's NaN or infinity stays in its own loss and dx, and reaches all of its worker's dweight.
 """
 from __future__ import annotations
 
