@@ -144,13 +144,14 @@ __device__ __forceinline__ void clear_scratch(V* scratch) {
 }
 
 // Whether the fp32 sum s of p and q, which is s + off in the 16-bit type, is so near to a border between two of its values that its error,
-// 7 2^-24 of |p| + |q| at most, may have carried it over: off is then half a step.
+// 6.5 2^-24 of |p| + |q| at most (5.5 of q: the root 2.5, three products; 2 of p: alpha and a product; the sum), may have carried it over:
+// off is then half a step.
 template <typename T>
 __device__ __forceinline__ bool near_border(float s, float off, float p, float q) {
     constexpr bool kHalfType = std::is_same_v<T, __half>;
     float half_step = __uint_as_float(__float_as_uint(s) & 0x7f800000u) * (kHalfType ? 0x1p-11f : 0x1p-8f);
     if (kHalfType) half_step = fmaxf(half_step, 0x1p-25f);
-    return fabsf(fabsf(off) - half_step) <= 0x1p-21f * (fabsf(p) + fabsf(q));
+    return fabsf(fabsf(off) - half_step) <= 0x1.ap-22f * (fabsf(p) + fabsf(q));
 }
 
 // 1 / sqrt(v) in binary64 from its fp32 approximation, by a step of Newton's: off by about 2^-46.

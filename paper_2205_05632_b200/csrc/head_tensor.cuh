@@ -89,7 +89,7 @@ struct Args {
     const float *lse, *row_gradient;  // PROBS: the latter is null where all rows' are 1, 0 for an ignored target
     int32_t probs_planes;
     // PROBS, INPUT, WEIGHT: the third map is of what is written, [plane or part][batch][row][column] from out_first's row on
-    int32_t out_type, add;  // add: onto what is there (fp32)
+    int32_t out_type, add;  // add: onto what is there (fp32, where the map serves)
     int32_t out_first;
     void* out;              // where the third map does not serve (rows off 16-byte boundaries); else null
     int64_t out_batch, out_row;  // elements
@@ -325,17 +325,14 @@ struct Exit {
     }
     // Element by element, for rows that TMA cannot address: `count` of the columns and `rows` of the rows are there.
     template <typename T>
-    __device__ __forceinline__ void leave_slowly(T* out, int64_t row, int rows, int count, bool add) {
+    __device__ __forceinline__ void leave_slowly(T* out, int64_t row, int rows, int count) {
         __syncwarp();
         constexpr int N = 64 / (int)sizeof(T);
         const char* from = places + turn * 2048;
         for (int e = threadIdx.x & 31; e < 32 * N; e += 32) {
             const int r = e / N, c = e % N;
             if (r < rows && c < count) {
-                T v = *reinterpret_cast<const T*>(from + staged(r, c * sizeof(T) / 16) + c * sizeof(T) % 16);
-                if constexpr (sizeof(T) == 4)
-                    if (add) v += out[r * row + c];
-                out[r * row + c] = v;
+                out[r * row + c] = *reinterpret_cast<const T*>(from + staged(r, c * sizeof(T) / 16) + c * sizeof(T) % 16);
             }
         }
         __syncwarp();
@@ -475,7 +472,7 @@ __device__ __forceinline__ void finish(const Args& a, const CUtensorMap* map, ui
                         *reinterpret_cast<float4*>(place + staged(lane, c)) = make_float4(scale * v[0], scale * v[1], scale * v[2], scale * v[3]);
                     }
                     if (!a.out) exit.leave(column0 + part * 16, row0 + a.out_first, z, a.add);
-                    else exit.leave_slowly((float*)a.out + first + part * 16, a.out_row, rows, left - part * 16, a.add);
+                    else exit.leave_slowly((float*)a.out + first + part * 16, a.out_row, rows, left - part * 16);
                 }
             } else {
 #pragma unroll
@@ -493,7 +490,7 @@ __device__ __forceinline__ void finish(const Args& a, const CUtensorMap* map, ui
                         *reinterpret_cast<uint4*>(place + staged(lane, c)) = make_uint4(w[0], w[1], w[2], w[3]);
                     }
                     if (!a.out) exit.leave(column0 + part * 32, row0 + a.out_first, z, false);
-                    else exit.leave_slowly((uint16_t*)a.out + first + part * 32, a.out_row, rows, left - part * 32, false);
+                    else exit.leave_slowly((uint16_t*)a.out + first + part * 32, a.out_row, rows, left - part * 32);
                 }
             }
         }
