@@ -558,7 +558,7 @@ int product(head::Args& a, const Operand& left, const Operand& right, const CUte
         a.right_count = std::max(a.right_count, a.right_plane[k] + 1);
     }
     a.stages = std::min(head::kMostStages, head::kHalves / (a.left_count + a.right_count));
-    a.stretch = std::max(1, head::kFlush / a.pairs);
+    a.stretch = std::max(1, head::flush_after(a.pairs) / a.pairs);
     a.f16 = f16;
     a.tries = wait_tries.load(std::memory_order_relaxed);
     const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n * a.batches * a.parts;

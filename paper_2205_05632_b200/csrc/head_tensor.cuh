@@ -8,7 +8,7 @@
 // A pair of CTAs takes tiles of 256 x 256 (cta_group::2): each holds 128 rows of the left operand and 128 of the right in shared memory,
 // half of what two CTAs of 128 x 256 would read from it and fetch from the L2, and has the sums of its 128 rows in its tensor memory,
 // twice (2 x 256 columns): while eight warps take the sums of one stretch, the products of the next go to the other. The tensor cores cut
-// their sums, so a stretch is kFlush tiles of 64 long and joins the fp32 registers by rounded additions.
+// their sums, so a stretch is 8 or 16 tiles of 64 long and joins the fp32 registers by rounded additions.
 //
 // Operands are bf16 or fp16. fp32 numbers are three bf16 planes, and fp16 ones beside fp32 two: the sum then runs over pairs of planes as
 // well, listed in the arguments, small ones first.
@@ -45,9 +45,10 @@ constexpr int kShared = 1024 + kHalves * kHalf + kStaging;
 constexpr int kThreads = 384;
 constexpr int kSumRegisters = 224, kOtherRegisters = 32;
 static_assert(256 * kSumRegisters + 128 * kOtherRegisters <= kThreads * 168, "registers of the launch");
-// Products of 64 between two additions to the registers, at most (or those of one stage). With 32 nothing is faster, and dx of fp32 is
-// 1.4e-6 off its length instead of 2.1e-7 (4 workers of 100 rows, 512 columns, a vocabulary of 8000).
-constexpr int kFlush = 8;
+// Products of 64 between two additions to the registers, at most (or those of one stage): what is drained of one half of the tensor memory,
+// and at a tile's end written, has as long as the products that go to the other. Beside an fp32 weight, 8 workers of 256 bfloat16 rows: 1475 us
+// with 8, 1400 with 16; with six pairs of planes nothing is faster and dx is 5.4e-7 off its length instead of 2.1e-7 (1.4e-6 with 32).
+__host__ __device__ constexpr int flush_after(int pairs) { return pairs <= 3 ? 16 : 8; }
 constexpr int kMostPairs = 6;
 // The barriers: a stage has landed (of both CTAs, at the first); its products are done; the sums are ready, and drained (at the first).
 constexpr int kFull = 0, kEmpty = kMostStages, kReady = 2 * kMostStages, kDrained = kReady + 2, kStopped = kDrained + 2, kBars = kStopped + 1;

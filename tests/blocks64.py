@@ -2,7 +2,7 @@
 one final rounding may be off. Shares no code with the library. Runs where its inputs are.
 
 Tolerances. A rounding is off by at most half a step, U = finfo(t).eps / 2 relative. A sum of products by fp32 fused operations or by the
-tensor cores, which cut what they add to 2^-23 of the largest, in stretches of at most 32 additions that join by rounded ones, is off by at
+tensor cores, which cut what they add to 2^-23 of the largest, in stretches of at most 64 additions that join by rounded ones, is off by at
 most g = (h / 512 + 64) 2^-23 of the sum of the terms' magnitudes. An exponential of a difference is off by 2^-21 and by the difference's
 own error.
 
