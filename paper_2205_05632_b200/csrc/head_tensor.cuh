@@ -41,7 +41,7 @@ constexpr int kHalves = 12;         // of them there is room for: six stages of 
 constexpr int kMostStages = 6;
 constexpr int kStaging = 8 * 4096;  // for each of the eight warps two times 32 rows of 64 bytes
 constexpr int kShared = 1024 + kHalves * kHalf + kStaging;
-// Three groups of four warps at 168 registers; the two that keep sums take 216 and the third keeps 40: no more than the launch has.
+// Three groups of four warps at 168 registers; the two that keep sums take 224 and the third keeps 32: no more than the launch has.
 constexpr int kThreads = 384;
 constexpr int kSumRegisters = 224, kOtherRegisters = 32;
 static_assert(256 * kSumRegisters + 128 * kOtherRegisters <= kThreads * 168, "registers of the launch");
