@@ -417,6 +417,11 @@ PyObject* collect_gradients(PyObject*, PyObject* const* args, Py_ssize_t count) 
     if (G.defined()) {
         if (!usual(G) || G.scalar_type() != at::kFloat || G.device() != device || G.dim() != 2 || G.size(0) != n || G.size(1) != ends[many] || G.requires_grad())
             NOT_USUAL;
+        const char* lo = (const char*)G.const_data_ptr();
+        for (Py_ssize_t k = 0; k < many; ++k) {
+            const char* g = (const char*)addresses[k];
+            if (g < lo + G.nbytes() && lo < g + n * sizes[k] * (types[k] == 0 ? 4 : 2)) NOT_USUAL;  // a gradient that lies in G: refused there
+        }
         if (!G.is_inference()) G.unsafeGetTensorImpl()->bump_version();
     } else {
         G = at::empty({n, ends[many]}, options);

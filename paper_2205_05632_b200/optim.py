@@ -75,6 +75,22 @@ def _changed(tensors) -> None:
         torch.autograd.graph.increment_version(tensors)
 
 
+def _overlap(n: int, addresses, strides, sizes, widths) -> bool:
+    """Whether two of the workers' parts (n of each tensor, its stride and size in elements of its width) have bytes in common."""
+    if len(sizes) < 2:
+        return False  # a tensor's own parts are apart: its stride has been looked at
+    widths, starts = np.array(widths, dtype=np.int64), np.array(addresses, dtype=np.int64)
+    steps, lengths = np.array(strides, dtype=np.int64) * widths, np.array(sizes, dtype=np.int64) * widths
+
+    def meet(lo, length):
+        order = np.argsort(lo)
+        return bool((lo[order][1:] < (lo + length)[order][:-1]).any())
+
+    if not meet(starts, (n - 1) * steps + lengths):
+        return False
+    return meet((starts[:, None] + steps[:, None] * np.arange(n)).ravel(), np.repeat(lengths, n))  # parts of one G, beside one another
+
+
 _T = torch.Tensor
 
 
@@ -102,7 +118,7 @@ def collect_gradients(grads: Union[torch.Tensor, Sequence[torch.Tensor]], out: O
                       max_norm: Optional[float] = None, eps: float = 1e-6) -> Tuple[torch.Tensor, torch.Tensor]:
     """(G, norms): the workers' gradients, one tensor [n, *shape] per parameter in float32, bfloat16 or float16, gathered as the rows of a
     float32 tensor [n, d], `out` where given, and each worker's global norm over all of them, [n], as it was. Rows whose norm is above
-    max_norm are multiplied by max_norm / (norm + eps). The tensors may not overlap out."""
+    max_norm are multiplied by max_norm / (norm + eps). The tensors may not lie between out's first and last element."""
     got = load_operators().collect_gradients(grads, out, _INFINITY if max_norm is None else max_norm, eps)
     if got is not None:  # a usual call: a list of packed tensors
         return got
@@ -118,6 +134,10 @@ def collect_gradients(grads: Union[torch.Tensor, Sequence[torch.Tensor]], out: O
           or (d > 1 and out.stride(1) != 1) or (n > 1 and out.stride(0) < d) or out.is_neg() or out.requires_grad):
         raise CompAMSError("out must be a float32 tensor [%d, %d] with packed rows on %s" % (n, d, device))
     else:
+        lo = out.data_ptr()
+        hi = lo + 4 * ((n - 1) * out.stride(0) + d)
+        if any([g.data_ptr() < hi and lo < g.data_ptr() + g.numel() * g.element_size() for g in grads]):
+            raise CompAMSError("the gradients must be apart from out")
         _changed([out])
     sizes, addresses, types = _with_elements(sizes, list(map(_T.data_ptr, grads)), types)
     return out, _collect_workers(out, device, n, addresses, sizes, sizes, types, True, max_norm, eps)
@@ -125,7 +145,8 @@ def collect_gradients(grads: Union[torch.Tensor, Sequence[torch.Tensor]], out: O
 
 def clip_gradients(grads: Union[torch.Tensor, Sequence[torch.Tensor]], max_norm: float, eps: float = 1e-6) -> torch.Tensor:
     """Each worker's global norm, [n], over tensors [n, *shape] (G itself, or one tensor per parameter; every worker's part packed), which are
-    scaled in place, worker by worker, by min(1, max_norm / (norm + eps)). A worker that is not above max_norm is not touched."""
+    scaled in place, worker by worker, by min(1, max_norm / (norm + eps)). A worker that is not above max_norm is not touched. No two tensors
+    may have elements in common."""
     grads, n, device, types = _gradients(grads, "clip_gradients")
     max_norm, eps = _limit(max_norm, eps)
     for g in grads:
@@ -133,8 +154,11 @@ def clip_gradients(grads: Union[torch.Tensor, Sequence[torch.Tensor]], max_norm:
             raise CompAMSError("gradients that are clipped in place must be packed for every worker, and the workers' parts apart")
         if g.requires_grad and torch.is_grad_enabled() and g.is_leaf:
             raise CompAMSError("a leaf that requires a gradient cannot be scaled in place")
+    sizes, addresses, strides, types, widths = _with_elements([g.numel() // n for g in grads], [g.data_ptr() for g in grads],
+                                                              [g.stride(0) for g in grads], types, [g.element_size() for g in grads])
+    if _overlap(n, addresses, strides, sizes, widths):
+        raise CompAMSError("gradients that are clipped in place must be apart from one another")
     _changed(grads)
-    sizes, addresses, strides, types = _with_elements([g.numel() // n for g in grads], [g.data_ptr() for g in grads], [g.stride(0) for g in grads], types)
     return _collect_workers(None, device, n, addresses, strides, sizes, types, True, max_norm, eps)
 
 

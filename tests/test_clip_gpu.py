@@ -225,3 +225,20 @@ def test_refusals():
             clip_gradients([t], limit)
     with pytest.raises(CompAMSError):
         clip_gradients([t], 1.0, eps=-1.0)
+
+
+def test_tensors_that_overlap():
+    wide = torch.randn(3, 40, device="cuda")
+    want = wide.double()
+    norms = want.norm(dim=1)
+    for bad in ([wide, wide], [wide[:, :21], wide[:, 20:]], [wide, wide[:1].expand(3, 40)[:, :0], wide]):
+        with pytest.raises(CompAMSError):
+            clip_gradients(bad, 1.0)
+    for bad in ([wide], [wide[1, :3], wide.new_zeros(3, 39)], (wide.new_zeros(3, 39), wide.view(-1)[117:])):
+        with pytest.raises(CompAMSError):
+            collect_gradients(bad, out=wide)
+    assert torch.equal(wide.double(), want)
+    G, all_norms = collect_gradients([wide, wide])  # read only: it may stand there twice
+    assert torch.equal(G, torch.cat([wide, wide], 1)) and close(all_norms, norms * 2 ** 0.5, 4)
+    got = clip_gradients([wide[:, :21], wide[:, 21:]], 1.0, eps=0.0)  # beside one another
+    assert close(got, norms, 4) and close(wide, want * (1.0 / norms).clamp(max=1.0)[:, None], 9)

@@ -146,3 +146,17 @@ def test_collect_refuses_what_is_missing(lib):
     assert lib.compams_collect_workers_workspace_bytes(ctypes.byref(b), 4, 1000) == 0 and b.value > 0
     assert lib.compams_collect_workers_workspace_bytes(ctypes.byref(b), 0, 1) == INVALID
     assert lib.compams_collect_workers_workspace_bytes(None, 1, 1) == INVALID
+
+
+@pytest.mark.parametrize("parts, meet", [([(0, 8, 8, 4)], False), ([(0, 8, 8, 4), (0, 8, 8, 4)], True), ([(0, 8, 8, 4), (64, 8, 8, 4)], False),
+                                         ([(64, 8, 8, 4), (0, 8, 8, 4)], False), ([(0, 8, 8, 4), (60, 8, 8, 4)], True),
+                                         ([(0, 8, 5, 4), (20, 8, 3, 4)], False), ([(20, 8, 3, 4), (0, 8, 5, 4)], False),
+                                         ([(0, 8, 6, 4), (20, 8, 3, 4)], True), ([(0, 8, 5, 4), (20, 16, 3, 2)], False),
+                                         ([(0, 8, 5, 4), (20, 16, 7, 2)], True), ([(0, 8, 5, 4), (20, 9, 1, 4), (28, 8, 1, 4)], False),
+                                         ([(0, 100, 50, 4), (200, 10, 3, 4)], False), ([], False)], ids=str)
+def test_parts_that_overlap(parts, meet):
+    """(address, elements from worker to worker, elements, bytes of one) of two workers' parts against every byte of them."""
+    from paper_2205_05632_b200.optim import _overlap
+    every = [b for a, stride, size, width in parts for i in range(2) for b in range(a + i * stride * width, a + (i * stride + size) * width)]
+    assert (len(set(every)) < len(every)) == meet
+    assert _overlap(2, *[[p[k] for p in parts] for k in range(4)]) == meet
