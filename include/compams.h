@@ -433,7 +433,7 @@ enum compams_type { COMPAMS_F32 = 0, COMPAMS_BF16 = 1, COMPAMS_F16 = 2 };
  *                offsets[count] - 1 of each are written. Null: the tensors are scaled where they lie, in their own type.
  *   norms        device; [n] fp32, receives the norms as they were; may be null: not wanted.
  *   tensors      host; count DEVICE pointers; tensor k's elements of worker i are packed from i * strides[k] elements on, aligned to
- *                their element. Null: no gradient, zeros. They may not overlap rows.
+ *                their element. Null: no gradient, zeros. They may not overlap rows, nor one another where rows is null.
  *   types        host; compams_type of each tensor.
  *   offsets      host; count + 1 entries, offsets[0] >= 0, strictly increasing. All host arrays are read during the call.
  *   max_norm     infinity: nothing is scaled. A row whose factor is 1 is copied bit for bit (in place: not touched).
