@@ -139,8 +139,9 @@ variable_list norm_backward(Tensor dy, Tensor ds, const Tensor& x, const Tensor&
                             double scale) {
     const Shape z = shape_of(x);
     const c10::DeviceGuard guard(x.device());
-    dy = dy.defined() ? dy.contiguous() : at::zeros(x.sizes(), x.options().requires_grad(false));
-    if (ds.defined()) ds = ds.contiguous();
+    // (a packed tensor may be the negative of what lies in memory)
+    dy = dy.defined() ? dy.resolve_neg().contiguous() : at::zeros(x.sizes(), x.options().requires_grad(false));
+    if (ds.defined()) ds = ds.resolve_neg().contiguous();
     variable_list got(5);
     if (wanted[0]) got[0] = packed_like(x);
     if (wanted[1]) got[1] = packed_like(s);

@@ -1,0 +1,68 @@
+"""Edges of the operators around a block and at the two ends of the backward pass: gradients that are the negative of what lies in memory, on
+the path of the extension and on Python's."""
+import pytest
+import torch
+
+import paper_2205_05632_b200.binding as binding
+from paper_2205_05632_b200.layers import gated_add_rms_norm, linear_cross_entropy, rms_norm
+
+pytestmark = pytest.mark.gpu
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+TYPES = [(BF16, BF16), (F16, F16), (F32, F32), (BF16, F32), (F16, F32)]
+
+
+class _Nothing:
+    """No call is a usual one."""
+
+    def __getattr__(self, name):
+        return lambda *args: None
+
+
+@pytest.fixture(params=["extension", "python"])
+def path(request, monkeypatch):
+    binding.load_operators()
+    if request.param == "python":
+        monkeypatch.setattr(binding, "_ops", _Nothing())
+    return request.param
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def rand(g, *shape, dtype=F32):
+    return torch.randn(*shape, generator=g, device="cuda").to(dtype)
+
+
+def same(a, b):
+    return all(torch.equal(p, q) for p, q in zip(a, b))
+
+
+@pytest.mark.parametrize("kinds", TYPES, ids=str)
+@pytest.mark.parametrize("h", [64, 1001, 8200])
+def test_gradients_that_are_negatives_of_what_lies_in_memory(h, kinds, path):
+    g = gen(h)
+    x, dy, res, ds = rand(g, 2, 5, h, dtype=kinds[0]), rand(g, 2, 5, h, dtype=kinds[0]), rand(g, 2, 5, h, dtype=kinds[1]), rand(g, 2, 5, h, dtype=kinds[1])
+    p = [1.0 + 0.2 * rand(g, 2, h) for _ in range(3)]
+    w, t = rand(g, 30, h, dtype=kinds[1]), torch.randint(0, 30, (2, 5), generator=g, device="cuda")
+    negative = torch._neg_view
+    assert negative(dy).is_neg() and negative(dy).is_contiguous()
+
+    def norm(dy):
+        a = [v.detach().requires_grad_() for v in (x, p[0])]
+        return torch.autograd.grad(rms_norm(*a), a, dy)
+
+    def gated(dy, ds):
+        a = [v.detach().requires_grad_() for v in (x, res, *p)]
+        return torch.autograd.grad(gated_add_rms_norm(*a), a, (dy, ds))
+
+    def head(dloss, reduction):
+        a = [v.detach().requires_grad_() for v in (x, w)]
+        return torch.autograd.grad(linear_cross_entropy(*a, t, reduction), a, dloss)
+
+    assert same(norm(negative(dy)), norm(-dy))
+    assert same(gated(negative(dy), ds), gated(-dy, ds))
+    assert same(gated(dy, negative(ds)), gated(dy, -ds))
+    for reduction, shape in (("mean", (2,)), ("none", (2, 5))):
+        dloss = rand(g, *shape)
+        assert same(head(negative(dloss), reduction), head(-dloss, reduction))
