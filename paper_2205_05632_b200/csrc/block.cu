@@ -154,8 +154,11 @@ __device__ __forceinline__ bool near_border(float s, float off, float p, float q
     return fabsf(fabsf(off) - half_step) <= 0x1.ap-22f * (fabsf(p) + fabsf(q));
 }
 
-// 1 / sqrt(v) in binary64 from its fp32 approximation, by a step of Newton's: off by about 2^-46.
-__device__ __forceinline__ double root64(double v, float r) { return (double)r * (1.5 - 0.5 * v * ((double)r * (double)r)); }
+// 1 / sqrt(v) in binary64 from its fp32 approximation, by a step of Newton's: off by about 2^-46. (Of an infinity it is 0 and of 0 infinite, as in
+// fp32: the step would make either NaN.)
+__device__ __forceinline__ double root64(double v, float r) {
+    return r > 0.0f && r < kInf ? (double)r * (1.5 - 0.5 * v * ((double)r * (double)r)) : (double)r;
+}
 // The sum of eight squares of 16-bit numbers, which are exact in fp32, in binary64. (Pairs of bf16's in fp32, which halves the conversions,
 // are off by 2^-33 of the sum: enough for three of 4 million s.)
 __device__ __forceinline__ double squares8(const Pair (&v)[4]) {

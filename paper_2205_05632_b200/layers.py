@@ -30,7 +30,10 @@ Forward and backward can be captured into a CUDA graph together. As with every t
 the stream on which they were first used: warm up on the capturing stream, and let no autograd graph of the same leaves from another
 stream live while capturing.
 
-Not finite: a row of a norm with an infinity or a NaN in it is NaN, and so are its gradients; a dropped element is 0 whatever it was. In
+Not finite: a row of a norm with a NaN in it is NaN, and so are its gradients. An infinity makes a row of layer_norm NaN, too. In rms_norm its
+reciprocal root is 0, as is that of a row whose squares are more than float32 holds (elements of 2^64): the row is 0, but NaN at the infinity; its
+dx is NaN. gated_add_rms_norm keeps s = residual_scale * residual + 0 of such a row, NaN at the infinity, and where there is a NaN in s all of
+the first result and the row's gradients are. A dropped element is 0 whatever it was. In
 an adapter what an infinity or a NaN reaches is infinite or NaN, as a sum over it is, but which of the two may differ from a plain product.
 NaN is also what a kernel of an adapter or of the head leaves whose bounded waits run out (compams_adapter_status, compams_head_status say so;
 nothing should bring it about). In the head a row's NaN or infinity stays in its own loss and dx, and reaches all of its worker's dweight.

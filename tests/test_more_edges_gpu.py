@@ -1,8 +1,9 @@
-"""Edges of the operators around a block and at the two ends of the backward pass: gradients that are the negative of what lies in memory, on
-the path of the extension and on Python's."""
+"""Edges of the operators around a block and at the two ends of the backward pass: gradients that are the negative of what lies in memory, rows
+with infinities; on the path of the extension and on Python's."""
 import pytest
 import torch
 
+import blocks64 as B
 import paper_2205_05632_b200.binding as binding
 from paper_2205_05632_b200.layers import gated_add_rms_norm, linear_cross_entropy, rms_norm
 
@@ -66,3 +67,28 @@ def test_gradients_that_are_negatives_of_what_lies_in_memory(h, kinds, path):
     for reduction, shape in (("mean", (2,)), ("none", (2, 5))):
         dloss = rand(g, *shape)
         assert same(head(negative(dloss), reduction), head(-dloss, reduction))
+
+
+@pytest.mark.parametrize("kind", [BF16, F16, F32])
+@pytest.mark.parametrize("h", [500, 512, 1000, 2001, 4096, 9000])
+def test_rows_with_an_infinity(h, kind, path):
+    # 1 / sqrt(infinity) is 0: a norm's row is 0 but for 0 * infinity, and the stream is what the residual is, the 16-bit ones' borders included
+    g = gen(h)
+    x, res, dy = (rand(g, 3, 60, h, dtype=kind) for _ in range(3))
+    w, gate = 1.0 + 0.2 * rand(g, 3, h), 0.5 + 0.2 * rand(g, 3, h)
+    x[:, ::2, 7], x[:, 1::2, 9] = float("inf"), -float("inf")
+    if kind != F16:
+        x[:, 2, 7] = 1e30  # its square is beyond fp32, itself it is not
+    at = torch.isinf(x)
+    a = [v.detach().requires_grad_() for v in (x, res, w, gate)]
+    y, s = gated_add_rms_norm(*a, None, residual_scale=0.9)
+    want = torch.where(at, float("nan"), 0.9 * res.double())
+    B.check(s, want, 4 * B.E * want.abs(), "s")  # alpha, the product and the sum with 0 are rounded
+    rows = at.any(-1)
+    assert torch.isnan(y[rows]).all() and torch.isfinite(y[~rows]).all()
+    dx, = torch.autograd.grad(y, a[0], dy)
+    assert torch.isnan(dx[rows]).all()
+    y = rms_norm(a[0], a[2])
+    assert torch.equal(torch.isnan(y), at) and not y.nan_to_num().any()
+    dx, dw = torch.autograd.grad(y, (a[0], a[2]), dy)
+    assert torch.isnan(dx[rows]).all() and torch.equal(torch.isnan(dw), at.any(1))
