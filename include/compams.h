@@ -427,7 +427,8 @@ enum compams_type { COMPAMS_F32 = 0, COMPAMS_BF16 = 1, COMPAMS_F16 = 2 };
 /*
  * compams_collect_workers - all n workers' gradients, one tensor per parameter with a worker in each row, gathered as the rows of the
  * [n, d] gradient buffer; each worker's global norm over all its tensors; rows above max_norm scaled to it:
- *   norm_i = sqrt(sum g^2), G_i = min(1, max_norm / (norm_i + eps)) g_i (an infinite norm's factor is 0, that of no number none).
+ *   norm_i = sqrt(sum g^2), G_i = max_norm / (norm_i + eps) g_i where norm_i + eps is above max_norm, else g_i (an infinite norm's factor is 0,
+ *   that of no number none).
  *
  *   rows         device; fp32, worker i's row at i * row_stride (at least offsets[count] elements); coordinates offsets[0] ...
  *                offsets[count] - 1 of each are written. Null: the tensors are scaled where they lie, in their own type.

@@ -148,8 +148,8 @@ __device__ __forceinline__ float factor_of(const ClipArgs& a, int64_t worker, in
     for (int p = threadIdx.x; p < a.pitch; p += 256) sum += a.partials[worker * a.pitch + p];
     const double norm = sqrt(block_sum_double<8>(sum, scratch));
     if (threadIdx.x == 0) {
-        const double f = isinf(a.max_norm) ? 1.0 : a.max_norm / (norm + a.eps);
-        shared_factor = f >= 1.0 ? 1.0f : (float)f;  // (no number stays none)
+        const double over = norm + a.eps;  // (no number makes the factor none; a gradient of zeros has 1 where max_norm and eps are 0, too)
+        shared_factor = isinf(a.max_norm) || over <= a.max_norm ? 1.0f : (float)(a.max_norm / over);
         if (a.norms && piece == 0) a.norms[worker] = (float)norm;
     }
     __syncthreads();

@@ -117,8 +117,8 @@ def _with_elements(sizes: List[int], *lists):
 def collect_gradients(grads: Union[torch.Tensor, Sequence[torch.Tensor]], out: Optional[torch.Tensor] = None,
                       max_norm: Optional[float] = None, eps: float = 1e-6) -> Tuple[torch.Tensor, torch.Tensor]:
     """(G, norms): the workers' gradients, one tensor [n, *shape] per parameter in float32, bfloat16 or float16, gathered as the rows of a
-    float32 tensor [n, d], `out` where given, and each worker's global norm over all of them, [n], as it was. Rows whose norm is above
-    max_norm are multiplied by max_norm / (norm + eps). The tensors may not lie between out's first and last element."""
+    float32 tensor [n, d], `out` where given, and each worker's global norm over all of them, [n], as it was. Rows whose norm + eps is
+    above max_norm are multiplied by max_norm / (norm + eps). The tensors may not lie between out's first and last element."""
     got = load_operators().collect_gradients(grads, out, _INFINITY if max_norm is None else max_norm, eps)
     if got is not None:  # a usual call: a list of packed tensors
         return got
@@ -145,8 +145,8 @@ def collect_gradients(grads: Union[torch.Tensor, Sequence[torch.Tensor]], out: O
 
 def clip_gradients(grads: Union[torch.Tensor, Sequence[torch.Tensor]], max_norm: float, eps: float = 1e-6) -> torch.Tensor:
     """Each worker's global norm, [n], over tensors [n, *shape] (G itself, or one tensor per parameter; every worker's part packed), which are
-    scaled in place, worker by worker, by min(1, max_norm / (norm + eps)). A worker that is not above max_norm is not touched. No two tensors
-    may have elements in common."""
+    scaled in place, worker by worker, by max_norm / (norm + eps) where norm + eps is above max_norm; the other workers' are not touched. No two
+    tensors may have elements in common."""
     grads, n, device, types = _gradients(grads, "clip_gradients")
     max_norm, eps = _limit(max_norm, eps)
     for g in grads:
@@ -233,8 +233,8 @@ class CompAMSOptimizer:
 
     def collect_all(self, max_norm: Optional[float] = None, eps: float = 1e-6) -> Optional[torch.Tensor]:
         """All rows of G <- the gradients that worker_parameters() accumulated since the last call; they are cleared. With max_norm every
-        worker's row whose norm over all parameters is above it is multiplied by max_norm / (norm + eps), and the norms, [n], are the
-        result."""
+        worker's row whose norm over all parameters, with eps added, is above it is multiplied by max_norm / (norm + eps), and the norms, [n],
+        are the result."""
         limit, eps = _limit(max_norm, eps)
         leaves = self.worker_parameters()
         dev = self.G.device
@@ -251,8 +251,8 @@ class CompAMSOptimizer:
         return norms
 
     def clip(self, max_norm: float, eps: float = 1e-6) -> torch.Tensor:
-        """Between collect() of the workers and step(): rows of G whose norm is above max_norm are multiplied by max_norm / (norm + eps).
-        The norms, [n], as they were."""
+        """Between collect() of the workers and step(): rows of G whose norm + eps is above max_norm are multiplied by max_norm / (norm +
+        eps). The norms, [n], as they were."""
         return clip_gradients(self.G, max_norm, eps)
 
     def step(self) -> None:

@@ -1,11 +1,12 @@
 """Edges of the operators around a block and at the two ends of the backward pass: gradients that are the negative of what lies in memory, rows
-with infinities; on the path of the extension and on Python's."""
+with infinities, clipping at its borders; on the path of the extension and on Python's."""
 import pytest
 import torch
 
 import blocks64 as B
 import paper_2205_05632_b200.binding as binding
 from paper_2205_05632_b200.layers import gated_add_rms_norm, linear_cross_entropy, rms_norm
+from paper_2205_05632_b200.optim import clip_gradients, collect_gradients
 
 pytestmark = pytest.mark.gpu
 F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
@@ -92,3 +93,19 @@ def test_rows_with_an_infinity(h, kind, path):
     assert torch.equal(torch.isnan(y), at) and not y.nan_to_num().any()
     dx, dw = torch.autograd.grad(y, (a[0], a[2]), dy)
     assert torch.isnan(dx[rows]).all() and torch.equal(torch.isnan(dw), at.any(1))
+
+
+@pytest.mark.parametrize("kind", [F32, BF16, F16])
+def test_clipping_at_its_borders(kind, path):
+    t = torch.zeros(3, 100, dtype=kind, device="cuda")
+    t[1], t[2, 5] = 2.0, 4.0  # norms 0, 20 and 4
+    for max_norm, eps, factors in ((0.0, 0.0, (1.0, 0.0, 0.0)), (0.0, 1.0, (0.0, 0.0, 0.0)), (4.0, 0.0, (1.0, 0.2, 1.0)), (4.0, 4.0, (1.0, 4 / 24, 0.5)),
+                                   (20.0, 0.0, (1.0, 1.0, 1.0)), (float("inf"), 1.0, (1.0, 1.0, 1.0))):
+        G, norms = collect_gradients([t], max_norm=max_norm, eps=eps)
+        assert norms.tolist() == [0.0, 20.0, 4.0]
+        f = torch.tensor(factors, dtype=torch.float64, device="cuda")[:, None]
+        B.check(G, t.double() * f, 2 * B.E * t.double().abs(), "G")  # the factor is rounded, and the product
+        kept = t.clone()
+        clip_gradients([kept], max_norm, eps)
+        B.check(kept, t.double() * f, 2 * B.E * t.double().abs(), "in place")
+        assert torch.equal(kept[f[:, 0] == 1.0], t[f[:, 0] == 1.0])
