@@ -108,6 +108,7 @@ struct FewArgs {
 // A warp takes a share of the rows of W, for one row of x a row at a time and eight CTAs to an SM (32000 rows of 4096 bfloat16 columns, 262 MB:
 // 46 us; four rows at a time and four CTAs 49, two and six 51), for more of them four, so that x is read once for four; a lane has eight
 // columns (or every 32nd) of each.
+constexpr int staged_rows(int rows) { return rows == 3 ? 4 : rows; }  // the kernel's MR: three rows are taken as four
 __host__ __device__ constexpr int rows_at_once(int rows) { return rows == 1 ? 1 : 4; }
 __host__ __device__ constexpr int ctas_at_once(int rows) { return rows == 1 ? 8 : 4; }
 template <typename TX, typename TW, int MR, bool VEC>
@@ -388,7 +389,7 @@ struct HeadShape {
     int64_t batch_rows() const { return shared ? n * rows : rows; }
     int64_t all_rows() const { return n * rows; }
     int64_t pitch() const { return (h + 7) / 8 * 8; }
-    bool few() const { return batch_rows() <= kFew && batch_rows() * pitch() * 4 <= kFewShared; }
+    bool few() const { return batch_rows() <= kFew && staged_rows((int)batch_rows()) * pitch() * 4 <= kFewShared; }
     // planes of d: for dx, for dW
     int x_probs() const { return type == kTypeF32 ? 3 : type == kTypeF16 && copies() ? 2 : 1; }
     int w_probs() const { return copies() ? 3 : 1; }
@@ -633,19 +634,17 @@ int operands(const HeadShape& z, const void* x, int64_t x_ws, int64_t x_rs, cons
 template <typename TX, typename TW, int MR>
 int few_rows(const HeadShape& z, FewArgs& a, bool vec, int64_t ctas, cudaStream_t stream) {
     const auto kernel = vec ? few_kernel<TX, TW, MR, true> : few_kernel<TX, TW, MR, false>;
-    if (MR * z.pitch() * 4 > 48 * 1024) {  // the most that a call may want, as it is asked for once
-        const cudaError_t e = allow_shared((const void*)kernel, kFewShared);
-        if (e != cudaSuccess) return launched(e, "head_few");
-    }
-    return launched(launch_sized(kernel, dim3((uint32_t)ctas, (uint32_t)z.batches()), 256, 1, (size_t)(MR * z.pitch() * 4), true, stream, a),
+    return launched(launch_sized(kernel, dim3((uint32_t)ctas, (uint32_t)z.batches()), 256, 1, Shared((size_t)(MR * z.pitch() * 4), kFewShared), true,
+                                 stream, a),
                     "head_few");
 }
 template <typename TX, typename TW>
 int few_rows(const HeadShape& z, FewArgs& a, int64_t ctas, cudaStream_t stream) {
     const bool vec = z.h % 8 == 0 && ((reinterpret_cast<uintptr_t>(a.weight) | (uint64_t)(a.w_rs * (int64_t)sizeof(TW)) |
                                        (uint64_t)(a.w_ws * (int64_t)sizeof(TW))) & 15u) == 0;
-    return a.rows == 1 ? few_rows<TX, TW, 1>(z, a, vec, ctas, stream)
-                       : a.rows == 2 ? few_rows<TX, TW, 2>(z, a, vec, ctas, stream) : few_rows<TX, TW, 4>(z, a, vec, ctas, stream);
+    const int staged = staged_rows(a.rows);
+    return staged == 1 ? few_rows<TX, TW, 1>(z, a, vec, ctas, stream)
+                       : staged == 2 ? few_rows<TX, TW, 2>(z, a, vec, ctas, stream) : few_rows<TX, TW, 4>(z, a, vec, ctas, stream);
 }
 
 bool float_aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }

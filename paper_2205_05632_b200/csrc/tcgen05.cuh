@@ -141,7 +141,7 @@ Encode map_encoder() {
 
 int launched(cudaError_t e, const char* what) { return e == cudaSuccess ? COMPAMS_OK : cuda_fail(e, what); }
 
-// Lets a kernel have more than 48 KB of shared memory: asked once for every kernel and device (a kernel's size is always the same).
+// Lets a kernel have more than 48 KB of shared memory: asked once for every kernel and device, so always for the most that it may want.
 cudaError_t allow_shared(const void* kernel, size_t bytes) {
     static std::atomic<uint64_t> known[1024];
     int device = 0;
@@ -155,18 +155,24 @@ cudaError_t allow_shared(const void* kernel, size_t bytes) {
     return e;
 }
 
+// Dynamic shared memory of a launch, and the most that the kernel's launches have, where that differs.
+struct Shared {
+    size_t bytes, most;
+    Shared(size_t all) : bytes(all), most(all) {}
+    Shared(size_t some, size_t at_most) : bytes(some), most(at_most) {}
+};
 // A launch behind another of the same call (or the first), with dynamic shared memory and a cluster along x.
 template <typename... KArgs, typename... Args>
-cudaError_t launch_sized(void (*kernel)(KArgs...), dim3 grid, int threads, int cluster, size_t shared, bool first, cudaStream_t stream,
+cudaError_t launch_sized(void (*kernel)(KArgs...), dim3 grid, int threads, int cluster, Shared shared, bool first, cudaStream_t stream,
                          Args... args) {
-    if (shared > 48 * 1024) {
-        const cudaError_t e = allow_shared((const void*)kernel, shared);
+    if (shared.bytes > 40 * 1024) {  // (the 48 KB are for a kernel's static part as well)
+        const cudaError_t e = allow_shared((const void*)kernel, shared.most);
         if (e != cudaSuccess) return e;
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = dim3(threads);
-    cfg.dynamicSmemBytes = shared;
+    cfg.dynamicSmemBytes = shared.bytes;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
     int count = 0;

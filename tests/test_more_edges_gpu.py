@@ -1,5 +1,5 @@
 """Edges of the operators around a block and at the two ends of the backward pass: gradients that are the negative of what lies in memory, rows
-with infinities, clipping at its borders; on the path of the extension and on Python's."""
+with infinities, clipping at its borders, a few rows of every width; on the path of the extension and on Python's."""
 import pytest
 import torch
 
@@ -109,3 +109,18 @@ def test_clipping_at_its_borders(kind, path):
         clip_gradients([kept], max_norm, eps)
         B.check(kept, t.double() * f, 2 * B.E * t.double().abs(), "in place")
         assert torch.equal(kept[f[:, 0] == 1.0], t[f[:, 0] == 1.0])
+
+
+@pytest.mark.parametrize("kinds", TYPES, ids=str)
+@pytest.mark.parametrize("rows,h", [(1, 12264), (1, 12280), (1, 12288), (1, 12296), (2, 6120), (2, 6136), (2, 6144), (3, 3064), (3, 6144), (3, 6145), (3, 7168),
+                                    (3, 8192), (3, 8193), (4, 3058), (4, 3064), (4, 6144)])
+def test_a_few_rows_of_every_width(rows, h, kinds):
+    # x takes up to 96 KB of shared memory, three rows as much as four; from 48 KB on, the kernel's own arrays counted, it has to be asked for
+    g = gen(rows + h)
+    x, t = rand(g, rows, h, dtype=kinds[0]), torch.randint(0, 40, (rows,), generator=g, device="cuda")
+    w = (2.0 * h ** -0.5 * rand(g, 2, 40, h)).to(kinds[1])
+    one_worker, one_row_each, weights_of_their_own = (x[None], w[0], t[None]), (x[:, None], w[0], t[:, None]), (
+        torch.stack([x, x.flip(0)]), w, torch.stack([t, t]))
+    for call in (one_worker, one_row_each, weights_of_their_own):
+        want, tol = B.head(*call, "none")
+        B.check(linear_cross_entropy(*call, "none"), want, tol, "loss")
