@@ -14,7 +14,9 @@
 // well, listed in the arguments, small ones first.
 //
 // A tenth warp's thread brings tiles by TMA into the 128-byte swizzle, in both CTAs, to the first CTA's barriers; a ninth's, in the first
-// CTA, issues the products. All waits are bounded: who gives up marks the CTA, whose results then are NaN.
+// CTA, issues the products. All waits are bounded. Who gives up marks the CTA, and a warp of results whose wait ran out leaves NaN from there on
+// and says no more that it has drained anything: so no product goes to sums that another warp has still to take, the products come to an end,
+// and with them every other warp's waits. What is finite then is as it would have been.
 #pragma once
 
 #include "rows.cuh"
@@ -382,9 +384,8 @@ __device__ __forceinline__ void finish(const Args& a, const CUtensorMap* map, ui
         for (int c = 0; c < 128; ++c) sum[c] = 0.0f;
         for (int segment = 0, done = 0; segment < a.segments && all > 0; done + a.stretch < all ? done += a.stretch : (done = 0, ++segment)) {
             const float worth = FORM == kWeight ? scale_of(a.scale, p.batch + segment) : 1.0f;
-            lost = lost || !barrier_wait(bars + 8 * (kReady + buffer), ready >> buffer & 1u, a.tries);
+            lost = lost || !warp_wait(bars + 8 * (kReady + buffer), ready >> buffer & 1u, a.tries);
             ready ^= 1u << buffer;
-            __syncwarp();
             fence_after();
 #pragma unroll
             for (int c = 0; c < 128; c += 32) {
@@ -396,7 +397,7 @@ __device__ __forceinline__ void finish(const Args& a, const CUtensorMap* map, ui
             }
             fence_before();
             __syncwarp();
-            if (lane == 0) arrive_at(drained0 + 8 * buffer);
+            if (lane == 0 && !lost) arrive_at(drained0 + 8 * buffer);
             buffer ^= 1u;
         }
         const int row0 = p.m * kTile + (int)rank * 128 + (warp & 3) * 32;  // of the warp, in the batch
