@@ -151,7 +151,8 @@ __device__ __forceinline__ bool near_border(float s, float off, float p, float q
     constexpr bool kHalfType = std::is_same_v<T, __half>;
     float half_step = __uint_as_float(__float_as_uint(s) & 0x7f800000u) * (kHalfType ? 0x1p-11f : 0x1p-8f);
     if (kHalfType) half_step = fmaxf(half_step, 0x1p-25f);
-    return fabsf(fabsf(off) - half_step) <= 0x1.ap-22f * (fabsf(p) + fabsf(q));
+    // (less, not also equal: 0 + 0 is no sum to form again, of a row of zeros and of the threads behind a row's end)
+    return fabsf(fabsf(off) - half_step) < 0x1.ap-22f * (fabsf(p) + fabsf(q));
 }
 
 // 1 / sqrt(v) in binary64 from its fp32 approximation, by a step of Newton's: off by about 2^-46. (Of an infinity it is 0 and of 0 infinite, as in

@@ -124,3 +124,20 @@ def test_a_few_rows_of_every_width(rows, h, kinds):
     for call in (one_worker, one_row_each, weights_of_their_own):
         want, tol = B.head(*call, "none")
         B.check(linear_cross_entropy(*call, "none"), want, tol, "loss")
+
+
+@pytest.mark.parametrize("kinds", [(BF16, BF16), (F16, F16), (BF16, F32)], ids=str)
+@pytest.mark.parametrize("h", [72, 1000, 1001, 4104, 9000])
+def test_a_padded_batch(h, kinds, path):
+    # rows of zeros: their sum is 0 and their gradient what the norm's slope at 0 makes of it; the others do not notice. Sums that cancel to 0
+    g = gen(h)
+    x, res = rand(g, 3, 20, h, dtype=kinds[0]), rand(g, 3, 20, h, dtype=kinds[1])
+    w, gate, v = (1.0 + 0.2 * rand(g, 3, h) for _ in range(3))
+    y0, s0 = gated_add_rms_norm(x, res, w, gate, v, residual_scale=0.7)
+    x[:, 11:], res[:, 11:] = 0.0, 0.0
+    y, s = gated_add_rms_norm(x, res, w, gate, v, residual_scale=0.7)
+    assert not s[:, 11:].any() and not y[:, 11:].any()
+    assert torch.equal(s[:, :11], s0[:, :11]) and torch.equal(y[:, :11], y0[:, :11])
+    one = torch.ones_like(x)
+    y, s = gated_add_rms_norm(one, -one.to(kinds[1]), eps=0.0)  # 1 / sqrt(1) - 1
+    assert not s.any()
