@@ -595,7 +595,7 @@ int compams_head_forward(float* loss, float* lse, const void* x, int32_t type, c
  *   x_copied, weight_copied   0 where TMA can read them as they lie: both have one 16-bit type (or, for x, type is COMPAMS_BF16), the
  *                   address and the strides are multiples of 16 bytes (of axes longer than 1), rows do not overlap, and, for x beside a
  *                   weight that all share, the workers' rows follow one another at one distance. Else 1, or 1 in any case: the workspace
- *                   then has room for a copy.
+ *                   then has room either way.
  *   shared          weight_worker_stride is 0, or n is 1.
  */
 int compams_head_backward(void* dx, void* dweight, int32_t sum_workers, const float* dloss, int64_t dloss_worker_stride, int64_t dloss_row_stride,

@@ -675,7 +675,14 @@ int compams_head_workspace_bytes(size_t* bytes, int32_t n, int64_t rows, int64_t
                                  int32_t shared, int32_t x_copied, int32_t weight_copied, int32_t wanted) {
     const HeadShape z{n, rows, h, vocab, type, weight_type, shared != 0 || n == 1};
     if (!bytes || !z.ok() || wanted < 0 || wanted > 3) return COMPAMS_ERR_INVALID_ARG;
-    *bytes = rows ? (size_t)plan_of(z, x_copied || z.x_planes() > 1, weight_copied || z.copies(), wanted).bytes : 0;
+    *bytes = 0;
+    if (rows == 0) return COMPAMS_OK;
+    // Who says "copied" may find that a call reads it where it lies: a weight's copy makes pieces smaller, and with them d, so that either may
+    // take more. (x's copy only adds to the others.)
+    const bool x = x_copied || z.x_planes() > 1;
+    int64_t most = plan_of(z, x, weight_copied || z.copies(), wanted).bytes;
+    if (weight_copied && !z.copies()) most = std::max(most, plan_of(z, x, false, wanted).bytes);
+    *bytes = (size_t)most;
     return COMPAMS_OK;
 }
 
