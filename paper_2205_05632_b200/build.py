@@ -18,7 +18,8 @@ NVCC_FLAGS = [
 ]
 
 
-# The operators' usual calls for torch: a Python extension beside the library, which it reaches through its addresses.
+# The operators' usual calls for torch: a Python extension beside the library, which it reaches through its addresses. It is built for one torch
+# and one Python, whose versions stand beside it.
 EXTENSION = os.path.join(HERE, "_torch_ops.so")
 EXTENSION_SOURCE = os.path.join(CSRC, "torch_ops.cpp")
 
@@ -38,13 +39,27 @@ def _stale() -> bool:
     return any(os.path.getmtime(p) > t for p in deps)
 
 
-def build_extension(force: bool = False) -> str:
+def _extension_stale(versions: str) -> bool:
     deps = [EXTENSION_SOURCE, os.path.join(HERE, "..", "include", "compams.h"), os.path.abspath(__file__)]
-    if not force and os.path.exists(EXTENSION) and all(os.path.getmtime(p) <= os.path.getmtime(EXTENSION) for p in deps):
-        return EXTENSION
+    if not os.path.exists(EXTENSION) or any(os.path.getmtime(p) > os.path.getmtime(EXTENSION) for p in deps):
+        return True
+    try:
+        with open(EXTENSION + ".versions") as f:
+            return f.read() != versions
+    except OSError:
+        return True
+
+
+def build_extension(force: bool = False) -> None:
     import sysconfig
 
-    import torch
+    try:
+        import torch
+    except ImportError:
+        return  # the library is for programs without torch as well, the extension is not
+    versions = "torch %s, Python %s" % (torch.__version__, sysconfig.get_config_var("SOABI"))
+    if not force and not _extension_stale(versions):
+        return
     root = os.path.dirname(torch.__file__)
     cuda = os.path.dirname(os.path.dirname(_nvcc())) if os.path.sep in _nvcc() else "/usr/local/cuda"
     tmp = EXTENSION + ".tmp.%d" % os.getpid()
@@ -54,18 +69,18 @@ def build_extension(force: bool = False) -> str:
                     sysconfig.get_paths()["include"], EXTENSION_SOURCE, "-o", tmp, "-L" + os.path.join(root, "lib"), "-lc10", "-lc10_cuda",
                     "-ltorch_cpu", "-ltorch_python"], check=True)
     os.replace(tmp, EXTENSION)
-    return EXTENSION
+    with open(EXTENSION + ".versions", "w") as f:
+        f.write(versions)
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    build_extension(force)
-    if not force and not _stale():
-        return LIB
-    tmp = LIB + ".tmp.%d" % os.getpid()
-    cmd = [_nvcc(), *NVCC_FLAGS, *(["-Xptxas", "-v"] if verbose else []),
-           *[os.path.join(CSRC, s) for s in SOURCES], "-o", tmp]
-    subprocess.run(cmd, check=True)
-    os.replace(tmp, LIB)
+    if force or _stale():
+        tmp = LIB + ".tmp.%d" % os.getpid()
+        cmd = [_nvcc(), *NVCC_FLAGS, *(["-Xptxas", "-v"] if verbose else []),
+               *[os.path.join(CSRC, s) for s in SOURCES], "-o", tmp]
+        subprocess.run(cmd, check=True)
+        os.replace(tmp, LIB)
+    build_extension(force)  # (behind the library, which needs neither torch's headers nor a C++ compiler beside nvcc's)
     return LIB
 
 
