@@ -86,8 +86,8 @@ bool activation(const Tensor& x) { return usual(x) && type_of(x) >= 0 && x.dim()
 bool parameter(const Tensor& w, const Tensor& x) {
     if (!w.defined()) return true;
     const auto keys = w.key_set();
-    return w.is_cuda() && w.scalar_type() == at::kFloat && w.layout() == c10::kStrided && w.device() == x.device() && w.size(-1) == x.size(-1) &&
-           (w.dim() == 1 || (w.dim() == 2 && w.size(0) == x.size(0))) && w.stride(-1) == 1 && !keys.has(c10::DispatchKey::Python) &&
+    return w.is_cuda() && w.scalar_type() == at::kFloat && w.layout() == c10::kStrided && w.device() == x.device() &&
+           (w.dim() == 1 || (w.dim() == 2 && w.size(0) == x.size(0))) && w.size(-1) == x.size(-1) && w.stride(-1) == 1 && !keys.has(c10::DispatchKey::Python) &&
            !keys.has(c10::DispatchKey::Negative) && !keys.has(c10::DispatchKey::FuncTorchBatched) &&
            !keys.has(c10::DispatchKey::FuncTorchGradWrapper);
 }

@@ -1,10 +1,12 @@
 """Edges of the operators around a block and at the two ends of the backward pass: gradients that are the negative of what lies in memory, rows
-with infinities, clipping at its borders, a few rows of every width; on the path of the extension and on Python's."""
+with infinities, clipping at its borders, a few rows of every width, tensors
+without axes; on the path of the extension and on Python's."""
 import pytest
 import torch
 
 import blocks64 as B
 import paper_2205_05632_b200.binding as binding
+from paper_2205_05632_b200 import CompAMSError
 from paper_2205_05632_b200.layers import gated_add_rms_norm, linear_cross_entropy, rms_norm
 from paper_2205_05632_b200.optim import clip_gradients, collect_gradients
 
@@ -141,3 +143,13 @@ def test_a_padded_batch(h, kinds, path):
     one = torch.ones_like(x)
     y, s = gated_add_rms_norm(one, -one.to(kinds[1]), eps=0.0)  # 1 / sqrt(1) - 1
     assert not s.any()
+
+
+def test_tensors_without_axes_are_refused(path):
+    x, one, t = torch.zeros(2, 3, 8, device="cuda"), torch.ones((), device="cuda"), torch.zeros(2, 3, dtype=torch.int64, device="cuda")
+    for call in (lambda: rms_norm(x, one), lambda: rms_norm(one), lambda: gated_add_rms_norm(x, x, one), lambda: gated_add_rms_norm(x, x, gate=one),
+                 lambda: gated_add_rms_norm(x, x, next_weight=one), lambda: gated_add_rms_norm(x, one), lambda: linear_cross_entropy(x, one, t),
+                 lambda: linear_cross_entropy(x, torch.ones(5, 8, device="cuda"), t[0, 0]), lambda: collect_gradients([one]),
+                 lambda: collect_gradients([x], out=one), lambda: clip_gradients([one], 1.0)):
+        with pytest.raises(CompAMSError):
+            call()
