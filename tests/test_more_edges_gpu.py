@@ -1,6 +1,6 @@
 """Edges of the operators around a block and at the two ends of the backward pass: gradients that are the negative of what lies in memory, rows
-with infinities, clipping at its borders, a few rows of every width, tensors
-without axes; on the path of the extension and on Python's."""
+with infinities, clipping at its borders, a few rows of every width, tensors without axes, streams that cancel; on the path of the extension
+and on Python's."""
 import pytest
 import torch
 
@@ -153,3 +153,19 @@ def test_tensors_without_axes_are_refused(path):
                  lambda: collect_gradients([x], out=one), lambda: clip_gradients([one], 1.0)):
         with pytest.raises(CompAMSError):
             call()
+
+
+@pytest.mark.parametrize("kind", [BF16, F16])
+@pytest.mark.parametrize("h", [2048, 1001])
+def test_a_stream_that_cancels_is_rounded_as_the_exact_sum(h, kind):
+    # down to the smallest numbers of the type: a third of the sums is below 2^-14, where fp16 has no more bits
+    g = gen(4)
+    x, w = rand(g, 4, 300, h, dtype=kind), 1.0 + 0.3 * rand(g, 4, h)
+    gate = rand(g, 4, h) * 10.0 ** (4 * torch.rand(4, h, generator=g, device="cuda") - 3)
+    u = B.rms(x.double(), w.double()[:, None], 1e-6)[0] * gate.double()[:, None]
+    res = (-u / 0.7 * (1.0 + 0.01 * torch.randn(u.shape, generator=g, device="cuda"))).to(kind)
+    _, s = gated_add_rms_norm(x, res, w, gate, None, residual_scale=0.7)
+    want = 0.7 * res.double() + u
+    assert int((want.abs() < 2.0 ** -14).sum()) > want.numel() // 4
+    off = s.double() != want.float().to(kind).double()
+    assert int(off.sum()) <= 2 + 1e-6 * off.numel()
