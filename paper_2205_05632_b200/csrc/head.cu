@@ -323,7 +323,7 @@ __global__ void __launch_bounds__(256) rows_kernel(const __grid_constant__ RowsA
     for (int w = 0; w < 8; ++w) top = fmaxf(top, tops[w]);
     int e = 0;
     if (top > 0.0f && top < kInf) frexpf(top, &e);
-    e = max(e, -100);  // 2^-e is finite
+    e = min(max(e, -100), 127);  // 2^-e and 2^e are finite
     const float inverse = ldexpf(1.0f, -e);
     if (threadIdx.x == 0) a.scale[i] = ldexpf(a.f16 ? 1.0f / head::kF16Scale : 1.0f, e);
     for (int64_t j = threadIdx.x; j < a.rows; j += 256) {

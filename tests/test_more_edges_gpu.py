@@ -1,6 +1,6 @@
 """Edges of the operators around a block and at the two ends of the backward pass: gradients that are the negative of what lies in memory, rows
-with infinities, clipping at its borders, a few rows of every width, tensors without axes, streams that cancel; on the path of the extension
-and on Python's."""
+with infinities, clipping at its borders, a few rows of every width, tensors without axes, streams that cancel, rows' gradients far
+apart or large; on the path of the extension and on Python's."""
 import pytest
 import torch
 
@@ -169,3 +169,17 @@ def test_a_stream_that_cancels_is_rounded_as_the_exact_sum(h, kind):
     assert int((want.abs() < 2.0 ** -14).sum()) > want.numel() // 4
     off = s.double() != want.float().to(kind).double()
     assert int(off.sum()) <= 2 + 1e-6 * off.numel()
+
+
+@pytest.mark.parametrize("kinds", [(BF16, BF16), (F32, F32), (BF16, F32)], ids=str)
+@pytest.mark.parametrize("top", [1e-38, 1.5e38, 3e38])
+def test_rows_gradients_at_the_ends_of_the_range(top, kinds):
+    g = gen(1)
+    x, w = (1e-2 * rand(g, 2, 9, 64)).to(kinds[0]).requires_grad_(), (1e-2 * rand(g, 200, 64)).to(kinds[1]).requires_grad_()
+    t = torch.randint(0, 200, (2, 9), generator=g, device="cuda")
+    dloss = torch.full((2, 9), top, device="cuda")
+    dloss[0, 3], dloss[1, 4], dloss[1, 5] = 1e-3 * top, -top, 0.0
+    got = torch.autograd.grad(linear_cross_entropy(x, w, t, "none"), (x, w), dloss)
+    _, _, wx, tx, ww, tw = B.head(x.detach(), w.detach(), t, "none", -100, dloss)
+    B.check(got[0], wx, tx, "dx")
+    B.check(got[1], ww, tw, "dweight")
