@@ -19,7 +19,8 @@
 // for an fp32 result. The rows' factors g are taken relative to their worker's: a mean's and a sum's g, the same for all rows of a worker,
 // stays out of d altogether and joins in fp32, so that d of the target, p - 1, is not rounded the same way in every row (8192 rows,
 // 100000 columns: 2.9e-3 off with g inside, 2.2e-3 now, of which rounding the result is 1.7e-3); without a reduction it is taken relative
-// to a power of two above the largest, as fp16 could not hold a loss scale or a ten-thousandth. For dx of 8 bits beside an fp32 weight two
+// to a power of two above the worker's largest, and where d is fp16, which could not hold rows far below it, to one of the row's own: dx
+// then has its row's, and d is brought to the worker's before the sum over the rows. For dx of 8 bits beside an fp32 weight two
 // planes of W are taken. No atomics: results do not change from run to run.
 #include <string.h>
 
@@ -302,10 +303,17 @@ struct RowsArgs {
     int64_t ws, rs;
     const int64_t* target;
     int64_t rows, ignored, vocab;
-    int32_t f16;
-    float *g, *scale;     // [all rows], [n]
+    float *g, *scale;         // [all rows], [n]
+    float *row_scale, *back;  // [all rows], where d is fp16; else null
 };
-// Without a reduction: a CTA per worker, its rows' g relative to the power of two above the largest.
+// The exponent of the power of two above v, as far as it and its inverse are finite.
+__device__ __forceinline__ int exponent_above(float v) {
+    int e = 0;
+    if (v > 0.0f && v < kInf) frexpf(v, &e);
+    return min(max(e, -100), 127);
+}
+// Without a reduction: a CTA per worker, its rows' g relative to the power of two above the largest; where d is fp16, to that above the row's
+// own, with what takes it from there to the result and to the worker's.
 __global__ void __launch_bounds__(256) rows_kernel(const __grid_constant__ RowsArgs a) {
     __shared__ float tops[8];
     dependency_wait();
@@ -321,15 +329,36 @@ __global__ void __launch_bounds__(256) rows_kernel(const __grid_constant__ RowsA
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < 8; ++w) top = fmaxf(top, tops[w]);
-    int e = 0;
-    if (top > 0.0f && top < kInf) frexpf(top, &e);
-    e = min(max(e, -100), 127);  // 2^-e and 2^e are finite
-    const float inverse = ldexpf(1.0f, -e);
-    if (threadIdx.x == 0) a.scale[i] = ldexpf(a.f16 ? 1.0f / head::kF16Scale : 1.0f, e);
+    const int e = exponent_above(top);
+    const float inverse = ldexpf(1.0f, -e), result = a.row_scale ? 1.0f / head::kF16Scale : 1.0f;
+    if (threadIdx.x == 0) a.scale[i] = ldexpf(result, e);
     for (int64_t j = threadIdx.x; j < a.rows; j += 256) {
-        const int64_t t = target[j];
-        a.g[i * a.rows + j] = t == a.ignored ? 0.0f : t >= 0 && t < a.vocab ? inverse * dloss[j * a.rs] : __int_as_float(0x7fffffff);  // no such column
+        const int64_t t = target[j], number = i * a.rows + j;
+        const float v = t == a.ignored ? 0.0f : dloss[j * a.rs];
+        float by = inverse;
+        if (a.row_scale) {
+            const int own = v != 0.0f ? exponent_above(fabsf(v)) : e;
+            by = ldexpf(1.0f, -own);
+            a.row_scale[number] = ldexpf(result, own);
+            a.back[number] = ldexpf(1.0f, own - e);
+        }
+        a.g[number] = t == a.ignored ? 0.0f : t >= 0 && t < a.vocab ? by * v : __int_as_float(0x7fffffff);  // no such column
     }
+}
+// A piece's d from the rows' own powers of two to their workers'.
+__global__ void __launch_bounds__(256) back_kernel(uint4* __restrict__ d, const float* __restrict__ back, int64_t chunks, int32_t per_row, int64_t pitch) {
+    dependency_wait();
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (at >= chunks) return;
+    const int64_t row = at / per_row;
+    const float by = back[row];
+    if (by == 1.0f) return;
+    uint4& place = d[row * pitch + (at - row * per_row)];
+    float v[8];
+    raw_floats<__half>(Raw8<__half>{place}, v);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] *= by;
+    store8<__half>(reinterpret_cast<__half*>(&place), v);
 }
 
 // dx from the parts' sums.
@@ -432,7 +461,7 @@ struct Plan {
     int64_t width;          // columns of d
     int32_t probs, parts;   // planes of d; parts of the vocabulary's sum of dx
     bool sums;              // dx is added up in fp32
-    int64_t x_copy, w_copy, stats, stat_parts, target_logit, row_loss, g, scale, d, dx_sums, bytes;
+    int64_t x_copy, w_copy, stats, stat_parts, target_logit, row_loss, g, row_scale, back, scale, d, dx_sums, bytes;
 };
 constexpr int64_t kCopyBytes = 64ll << 20;   // of a piece's copy of W: it stays in the L2 between its writing and its reading
 constexpr int64_t kProbsBytes = 512ll << 20;  // of a piece's d
@@ -491,6 +520,10 @@ Plan plan_of(const HeadShape& z, bool x_copied, bool w_copied, int wanted) {  //
         p.row_loss = take(m * 4);
     } else {
         p.g = take(m * 4);
+        if (z.f16()) {
+            p.row_scale = take(m * 4);
+            p.back = take(m * 4);
+        }
         p.scale = take(z.n * 4);
         p.d = take(p.probs * m * p.width * 2);
         p.parts = wanted & 1 ? parts_of(z, (p.piece + 63) / 64, z.x_probs() == 3 ? 6 : z.x_probs() == 2 ? 3 : z.copies() ? 2 : 1) : 1;
@@ -784,10 +817,19 @@ int compams_head_backward(void* dx, void* dweight, int32_t sum_workers, const fl
     if (reduction == kNone) {
         RowsArgs r = {};
         r.dloss = dloss; r.ws = dloss_worker_stride; r.rs = dloss_row_stride; r.target = target; r.rows = rows; r.ignored = ignored; r.vocab = vocab;
-        r.f16 = z.f16(); r.g = (float*)(work + p.g); r.scale = (float*)(work + p.scale);
+        r.g = (float*)(work + p.g); r.scale = (float*)(work + p.scale);
+        if (z.f16()) { r.row_scale = (float*)(work + p.row_scale); r.back = (float*)(work + p.back); }
         rc = launched(launch_sized(rows_kernel, dim3((uint32_t)n), 256, 1, 0, true, stream, r), "head_rows");
         scale.own = r.scale;
         row_gradient = r.g;
+    }
+    head::Scale scale_x = scale;  // of dx: a worker's, or a row's own
+    int64_t scale_rows = rows;
+    const float* back = nullptr;
+    if (reduction == kNone && z.f16()) {
+        scale_x.own = (const float*)(work + p.row_scale);
+        scale_rows = 1;
+        back = (const float*)(work + p.back);
     }
     Operand xo, wo;
     uint16_t* d = (uint16_t*)(work + p.d);
@@ -822,11 +864,18 @@ int compams_head_backward(void* dx, void* dweight, int32_t sum_workers, const fl
             a.out_row = p.sums ? z.pitch() : h;
             a.columns = (int32_t)a.out_row; a.out_type = p.sums ? kTypeF32 : type; a.out_batch = z.batch_rows() * a.out_row;
             a.add = p.sums && v0 > 0;
-            a.scale = scale; a.worker_rows = rows;
+            a.scale = scale_x; a.worker_rows = scale_rows;
             if (p.sums) a.scale.factor = 0.0f;  // later
             CUtensorMap out = {};
             if (!result_map(&out, to, a.out_type, a.out_row, z.batch_rows(), z.batches() * p.parts, a.out_row, a.out_batch)) a.out = to;
             rc = product<head::kInput>(a, by_batch, wo, out, z.f16(), stream, "head_input");
+        }
+        if (rc == COMPAMS_OK && dweight && back) {
+            const int32_t per_row = (int32_t)(up_to(count, 256) / 8);
+            const int64_t ctas = (all * per_row + 255) / 256;
+            if (ctas > 0x7fffffff) return COMPAMS_ERR_TOO_LARGE;
+            rc = launched(launch_sized(back_kernel, dim3((uint32_t)ctas), 256, 1, 0, false, stream, (uint4*)d, back, all * per_row, per_row, p.width / 8),
+                          "head_back");
         }
         if (rc == COMPAMS_OK && dweight) {
             // together: the workers are segments of one sum; else each is a batch
@@ -848,7 +897,7 @@ int compams_head_backward(void* dx, void* dweight, int32_t sum_workers, const fl
     if (rc != COMPAMS_OK || !p.sums || !dx) return rc;
     PartsArgs a = {};
     a.parts = (const float*)(work + p.dx_sums); a.part = all * z.pitch(); a.all_rows = all; a.count = p.parts; a.h = (int32_t)h;
-    a.per_row = (int32_t)(z.pitch() / 8); a.pitch = (int32_t)z.pitch(); a.chunks = all * a.per_row; a.scale = scale; a.worker_rows = rows; a.out = dx;
+    a.per_row = (int32_t)(z.pitch() / 8); a.pitch = (int32_t)z.pitch(); a.chunks = all * a.per_row; a.scale = scale_x; a.worker_rows = scale_rows; a.out = dx;
     const int64_t ctas = (a.chunks + 255) / 256;
     if (ctas > 0x7fffffff) return COMPAMS_ERR_TOO_LARGE;
     const bool vec = h % 8 == 0 && (reinterpret_cast<uintptr_t>(dx) & 15u) == 0;

@@ -1,6 +1,6 @@
 """Edges of the operators around a block and at the two ends of the backward pass: gradients that are the negative of what lies in memory, rows
-with infinities, clipping at its borders, a few rows of every width, tensors without axes, streams that cancel, rows' gradients far
-apart or large; on the path of the extension and on Python's."""
+with infinities, clipping at its borders, a few rows of every width, tensors without axes, streams that cancel, rows' gradients that are large
+or far apart; on the path of the extension and on Python's."""
 import pytest
 import torch
 
@@ -183,3 +183,35 @@ def test_rows_gradients_at_the_ends_of_the_range(top, kinds):
     _, _, wx, tx, ww, tw = B.head(x.detach(), w.detach(), t, "none", -100, dloss)
     B.check(got[0], wx, tx, "dx")
     B.check(got[1], ww, tw, "dweight")
+
+
+@pytest.mark.parametrize("kinds", TYPES, ids=str)
+@pytest.mark.parametrize("n,rows,h,vocab,form", [(1, 64, 128, 5000, "shared"), (2, 40, 72, 700, "own"), (3, 33, 1001, 300, "apart"), (2, 300, 512, 40000, "shared"),
+                                                   (3, 10000, 64, 20000, "shared")])
+@pytest.mark.parametrize("span", [6, 24])
+def test_rows_gradients_far_apart(span, n, rows, h, vocab, form, kinds):
+    # each row's dx is as good as by itself: the weights of some rows are a millionth of the others'
+    g = gen(span + h)
+    x = rand(g, n, rows, h, dtype=kinds[0]).requires_grad_()
+    w = (2.0 * h ** -0.5 * rand(g, *((n,) if form == "own" else ()), vocab, h)).to(kinds[1])
+    w = (w.expand(n, vocab, h) if form == "apart" else w).detach().requires_grad_()
+    t = torch.randint(0, vocab, (n, rows), generator=g, device="cuda")
+    t[:, 1] = -100
+    dloss = 4096.0 * 2.0 ** (-span * torch.rand(n, rows, generator=g, device="cuda"))
+    dloss[:, 2], dloss[:, 3], dloss[:, 0] = 0.0, -dloss[:, 3], 4096.0
+    dloss[:, 4:7] = 4096.0 * 2.0 ** -span
+
+    def both(x, w):
+        return torch.autograd.grad(linear_cross_entropy(x, w, t, "none"), [v for v in (x, w) if v.requires_grad], dloss)
+
+    dx, dw = both(x, w)
+    _, _, wx, tx, ww, tw = B.head(x.detach(), w.detach(), t, "none", -100, dloss)
+    B.check(dx, wx, tx, "dx")
+    # dweight is a sum over the rows, where fp16's d is relative to the worker's largest: off by up to 2^-39 of 8192, the power of two above it
+    lost = x.detach().abs().double().sum((0, 1) if form == "shared" else 1).unsqueeze(-2) * (2.0 ** -38 * 4096.0 if kinds == (F16, F16) else 0.0)
+    B.check(dw, ww, tw + lost, "dweight")
+    if span == 6 or kinds != (F16, F16):
+        for i in range(n):
+            B.near(dx[i], wx[i], max(2 * B.U[kinds[0]], 2e-6), "dx")
+    if rows < 10000:  # a piece of the vocabulary; of several, each gradient alone may have fewer, and sums in another order
+        assert torch.equal(both(x, w.detach())[0], dx) and torch.equal(both(x.detach(), w)[0], dw)
