@@ -100,6 +100,11 @@ Tensor bytes(const Tensor& like, size_t count) { return at::empty({(int64_t)coun
 Tensor floats(const Tensor& like, at::IntArrayRef shape) { return at::empty(shape, like.options().dtype(at::kFloat).requires_grad(false)); }
 Tensor packed_like(const Tensor& t) { return at::empty(t.sizes(), t.options().requires_grad(false)); }
 
+// A backward pass of gradients with forward-mode tangents would lose them.
+void no_tangents(const variable_list& grads) {
+    for (const Tensor& g : grads)
+        if (g.defined() && g._fw_grad(0).defined()) throw LibraryError("forward-mode derivatives of a backward pass are not offered");
+}
 // The gradients of a backward pass, which is not differentiable itself: said where someone tries, as the Python functions do.
 variable_list once(variable_list grads) {
     if (!at::GradMode::is_enabled()) return grads;
@@ -182,6 +187,7 @@ struct RmsNorm : torch::autograd::Function<RmsNorm> {
         return y;
     }
     static variable_list backward(AutogradContext* ctx, variable_list grads) {
+        no_tangents(grads);
         const variable_list saved = ctx->get_saved_variables();
         const Tensor parameters[3] = {saved[1], Tensor(), Tensor()};
         const bool wanted[5] = {ctx->needs_input_grad(0), false, saved[1].defined() && ctx->needs_input_grad(1), false, false};
@@ -204,6 +210,7 @@ struct GatedNorm : torch::autograd::Function<GatedNorm> {
     }
     static variable_list backward(AutogradContext* ctx, variable_list grads) {
         if (!grads[0].defined() && !grads[1].defined()) return variable_list(7);
+        no_tangents(grads);
         const variable_list saved = ctx->get_saved_variables();
         const Tensor parameters[3] = {saved[3], saved[4], saved[5]};
         bool wanted[5] = {ctx->needs_input_grad(0), ctx->needs_input_grad(1), false, false, false};
@@ -261,6 +268,7 @@ struct Head : torch::autograd::Function<Head> {
         return loss;
     }
     static variable_list backward(AutogradContext* ctx, variable_list grads) {
+        no_tangents(grads);
         const variable_list saved = ctx->get_saved_variables();
         const Tensor &x = saved[0], &weight = saved[1];
         const c10::DeviceGuard guard(x.device());

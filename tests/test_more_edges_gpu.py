@@ -1,6 +1,6 @@
 """Edges of the operators around a block and at the two ends of the backward pass: gradients that are the negative of what lies in memory, rows
 with infinities, clipping at its borders, a few rows of every width, tensors without axes, streams that cancel, rows' gradients that are large
-or far apart; on the path of the extension and on Python's."""
+or far apart, tangents of gradients; on the path of the extension and on Python's."""
 import pytest
 import torch
 
@@ -215,3 +215,16 @@ def test_rows_gradients_far_apart(span, n, rows, h, vocab, form, kinds):
             B.near(dx[i], wx[i], max(2 * B.U[kinds[0]], 2e-6), "dx")
     if rows < 10000:  # a piece of the vocabulary; of several, each gradient alone may have fewer, and sums in another order
         assert torch.equal(both(x, w.detach())[0], dx) and torch.equal(both(x.detach(), w)[0], dw)
+
+
+def test_tangents_of_gradients_are_refused(path):
+    from torch.autograd import forward_ad
+    g = gen(1)
+    x, w, t = rand(g, 2, 5, 16).requires_grad_(), rand(g, 30, 16).requires_grad_(), torch.randint(0, 30, (2, 5), generator=g, device="cuda")
+    for y in (rms_norm(x), *gated_add_rms_norm(x, x), linear_cross_entropy(x, w, t)):
+        with forward_ad.dual_level():
+            dy = torch.ones_like(y)
+            want, = torch.autograd.grad(y, x, dy, retain_graph=True)  # without a tangent a level changes nothing
+            with pytest.raises(RuntimeError, match="forward-mode"):
+                torch.autograd.grad(y, x, forward_ad.make_dual(dy, dy), retain_graph=True)
+        assert torch.equal(torch.autograd.grad(y, x, dy, retain_graph=True)[0], want)
