@@ -119,6 +119,10 @@ variable_list once(variable_list grads) {
     return error->apply(std::move(grads));
 }
 
+// Saved tensors come as a hook unpacks them (torch.autograd.graph.saved_tensors_hooks): the same values, but perhaps not as they lay.
+Tensor packed(const Tensor& t) { return t.defined() ? t.resolve_neg().contiguous() : t; }
+Tensor packed_columns(const Tensor& t) { return t.defined() && (t.is_neg() || t.stride(-1) != 1) ? packed(t) : t; }
+
 struct Shape {
     int32_t n;
     int64_t rows, h;
@@ -189,9 +193,9 @@ struct RmsNorm : torch::autograd::Function<RmsNorm> {
     static variable_list backward(AutogradContext* ctx, variable_list grads) {
         no_tangents(grads);
         const variable_list saved = ctx->get_saved_variables();
-        const Tensor parameters[3] = {saved[1], Tensor(), Tensor()};
+        const Tensor parameters[3] = {packed_columns(saved[1]), Tensor(), Tensor()};
         const bool wanted[5] = {ctx->needs_input_grad(0), false, saved[1].defined() && ctx->needs_input_grad(1), false, false};
-        const variable_list got = norm_backward(grads[0], {}, saved[0], {}, saved[2], parameters, wanted, 1.0);
+        const variable_list got = norm_backward(grads[0], {}, packed(saved[0]), {}, packed(saved[2]), parameters, wanted, 1.0);
         return once({got[0], got[2], Tensor()});
     }
 };
@@ -212,10 +216,10 @@ struct GatedNorm : torch::autograd::Function<GatedNorm> {
         if (!grads[0].defined() && !grads[1].defined()) return variable_list(7);
         no_tangents(grads);
         const variable_list saved = ctx->get_saved_variables();
-        const Tensor parameters[3] = {saved[3], saved[4], saved[5]};
+        const Tensor parameters[3] = {packed_columns(saved[3]), packed_columns(saved[4]), packed_columns(saved[5])};
         bool wanted[5] = {ctx->needs_input_grad(0), ctx->needs_input_grad(1), false, false, false};
         for (int k = 0, edge = 2; k < 3; ++k) wanted[2 + k] = parameters[k].defined() && ctx->needs_input_grad(edge++);
-        const variable_list got = norm_backward(grads[0], grads[1], saved[0], saved[1], saved[2], parameters, wanted,
+        const variable_list got = norm_backward(grads[0], grads[1], packed(saved[0]), packed(saved[1]), packed(saved[2]), parameters, wanted,
                                                 ctx->saved_data["scale"].toDouble());
         return once({got[0], got[1], got[2], got[3], got[4], Tensor(), Tensor()});
     }
@@ -270,7 +274,7 @@ struct Head : torch::autograd::Function<Head> {
     static variable_list backward(AutogradContext* ctx, variable_list grads) {
         no_tangents(grads);
         const variable_list saved = ctx->get_saved_variables();
-        const Tensor &x = saved[0], &weight = saved[1];
+        const Tensor x = packed(saved[0]), weight = packed_columns(saved[1]), target = packed(saved[2]), lse = packed(saved[3]);
         const c10::DeviceGuard guard(x.device());
         const int reduction = (int)ctx->saved_data["reduction"].toInt();
         const HeadCall c = head_call(x, weight);
@@ -283,7 +287,7 @@ struct Head : torch::autograd::Function<Head> {
             const Tensor work = head_workspace(c, x, weight, (dx.defined() ? 1 : 0) | (dweight.defined() ? 2 : 0), need);
             check(entry.head_backward(out(dx), out(dweight), weight.dim() == 2 ? 1 : 0, (const float*)g.const_data_ptr(), g.stride(0),
                                       reduction ? 0 : g.stride(1), x.const_data_ptr(), type_of(x), weight.const_data_ptr(), type_of(weight),
-                                      (const int64_t*)saved[2].const_data_ptr(), (const float*)saved[3].const_data_ptr(), c.z.n, c.z.rows, c.z.h,
+                                      (const int64_t*)target.const_data_ptr(), (const float*)lse.const_data_ptr(), c.z.n, c.z.rows, c.z.h,
                                       c.vocab, c.z.rows * c.z.h, c.z.h, c.weight_worker, c.weight_row, ctx->saved_data["ignored"].toInt(), reduction,
                                       out(work), need, stream_of(x)),
                   "compams_head_backward");

@@ -360,6 +360,16 @@ def dropout_add_layer_norm(x: torch.Tensor, residual: torch.Tensor, weight: Opti
 # ---- root-mean-square norms around a block ---------------------------------------------------------------------------------
 
 
+def _unpacked(t: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
+    """A saved tensor that was packed: a hook of torch.autograd.graph.saved_tensors_hooks may give it back with other strides."""
+    return None if t is None else t.resolve_neg().contiguous()
+
+
+def _unpacked_columns(w: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
+    """A saved parameter whose last axis was packed."""
+    return _unpacked(w) if w is not None and (w.is_neg() or w.stride(-1) != 1) else w
+
+
 def _rms_forward(x, residual, weight, gate, after, scale, eps, keep_stats):
     y = _empty(x)
     s = None if residual is None else _empty(x, residual.dtype)
@@ -410,7 +420,8 @@ class _RmsNormFunction(torch.autograd.Function):
     def backward(ctx, dy):
         x, stats, *weight = ctx.saved_tensors
         ctx.wanted = (ctx.needs_input_grad[0], False, ctx.needs_input_grad[1], False, False)
-        dx, _, dw, _, _ = _rms_backward(ctx, dy, None, x, None, stats, weight[0] if weight else None, None, None)
+        weight = _unpacked_columns(weight[0]) if weight else None
+        dx, _, dw, _, _ = _rms_backward(ctx, dy, None, x, None, _unpacked(stats), weight, None, None)
         return dx, dw, None
 
 
@@ -432,8 +443,8 @@ class _GatedNormFunction(torch.autograd.Function):
         if dy is None and ds is None:
             return (None,) * 7
         ctx.wanted = ctx.needs_input_grad[:5]
-        given = iter(given)
-        return (*_rms_backward(ctx, dy, ds, x, s, stats, *[next(given) if there else None for there in ctx.given]), None, None)
+        given = map(_unpacked_columns, given)
+        return (*_rms_backward(ctx, dy, ds, x, _unpacked(s), _unpacked(stats), *[next(given) if there else None for there in ctx.given]), None, None)
 
 
 def _rms_parameters(x, weight, gate, after):
@@ -625,6 +636,7 @@ class _HeadFunction(torch.autograd.Function):
     @_once
     def backward(ctx, dloss):
         x, weight, target, lse = ctx.saved_tensors
+        weight, target, lse = _unpacked_columns(weight), _unpacked(target), _unpacked(lse)
         needs_x, needs_w = ctx.needs_input_grad[:2]
         dx = _empty(x) if needs_x else None
         dw = (weight.new_empty if x.numel() else weight.new_zeros)(weight.shape) if needs_w else None

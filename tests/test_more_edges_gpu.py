@@ -1,6 +1,6 @@
 """Edges of the operators around a block and at the two ends of the backward pass: gradients that are the negative of what lies in memory, rows
 with infinities, clipping at its borders, a few rows of every width, tensors without axes, streams that cancel, rows' gradients that are large
-or far apart, tangents of gradients; on the path of the extension and on Python's."""
+or far apart, tangents of gradients, saved tensors that hooks give back in another order; on the path of the extension and on Python's."""
 import pytest
 import torch
 
@@ -228,3 +228,33 @@ def test_tangents_of_gradients_are_refused(path):
             with pytest.raises(RuntimeError, match="forward-mode"):
                 torch.autograd.grad(y, x, forward_ad.make_dual(dy, dy), retain_graph=True)
         assert torch.equal(torch.autograd.grad(y, x, dy, retain_graph=True)[0], want)
+
+
+@pytest.mark.parametrize("kinds", [(BF16, BF16), (F32, F32), (BF16, F32)], ids=str)
+def test_saved_tensors_that_hooks_unpack(kinds, path):
+    g = gen(2)
+    x, res = (rand(g, 3, 7, 72, dtype=k).requires_grad_() for k in kinds)
+    w, p = rand(g, 40, 72, dtype=kinds[1]).requires_grad_(), [(1.0 + 0.2 * rand(g, 3, 72)).requires_grad_() for _ in range(3)]
+    t = torch.randint(0, 40, (3, 7), generator=g, device="cuda")
+
+    def otherwise(v):  # the same values, the first axis innermost
+        return v.movedim(0, -1).contiguous().movedim(-1, 0) if v.dim() > 1 else torch.stack([v, v], 1)[:, 0]
+
+    def negative(v):
+        return torch._neg_view(-v) if v.is_floating_point() else v
+
+    calls = ((lambda: (rms_norm(x, p[0]),), (x, p[0])), (lambda: (rms_norm(x, p[0][0]),), (x, p[0])), (lambda: gated_add_rms_norm(x, res, *p), (x, res, *p)),
+             (lambda: (linear_cross_entropy(x, w, t),), (x, w)), (lambda: (linear_cross_entropy(x, w.expand(3, 40, 72), t, "none"),), (x, w)))
+    def gradients(out, leaves):
+        return torch.autograd.grad([y.float().square().sum() for y in out], leaves)
+
+    hooks = [torch.autograd.graph.saved_tensors_hooks(lambda v: v, otherwise), torch.autograd.graph.saved_tensors_hooks(lambda v: v, negative),
+             torch.autograd.graph.save_on_cpu()]
+    for call, leaves in calls:
+        want = gradients(call(), leaves)
+        for hook in hooks:
+            with hook:
+                out = call()
+            # (a weight that all share may come back as one of each worker's own: its sums then run in another order)
+            for a, b in zip(gradients(out, leaves), want):
+                B.near(a, b.double(), 2 * B.U[a.dtype] + 2.0 ** -20, "gradient")
