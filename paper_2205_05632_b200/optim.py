@@ -118,7 +118,8 @@ def collect_gradients(grads: Union[torch.Tensor, Sequence[torch.Tensor]], out: O
                       max_norm: Optional[float] = None, eps: float = 1e-6) -> Tuple[torch.Tensor, torch.Tensor]:
     """(G, norms): the workers' gradients, one tensor [n, *shape] per parameter in float32, bfloat16 or float16, gathered as the rows of a
     float32 tensor [n, d], `out` where given, and each worker's global norm over all of them, [n], as it was. Rows whose norm + eps is
-    above max_norm are multiplied by max_norm / (norm + eps). The tensors may not lie between out's first and last element."""
+    above max_norm are multiplied by max_norm / (norm + eps). The tensors may not lie between out's first and last element.
+    Not recorded: as under torch.no_grad()."""
     got = load_operators().collect_gradients(grads, out, _INFINITY if max_norm is None else max_norm, eps)
     if got is not None:  # a usual call: a list of packed tensors
         return got
@@ -146,14 +147,14 @@ def collect_gradients(grads: Union[torch.Tensor, Sequence[torch.Tensor]], out: O
 def clip_gradients(grads: Union[torch.Tensor, Sequence[torch.Tensor]], max_norm: float, eps: float = 1e-6) -> torch.Tensor:
     """Each worker's global norm, [n], over tensors [n, *shape] (G itself, or one tensor per parameter; every worker's part packed), which are
     scaled in place, worker by worker, by max_norm / (norm + eps) where norm + eps is above max_norm; the other workers' are not touched. No two
-    tensors may have elements in common."""
+    tensors may have elements in common. Not recorded: as under torch.no_grad()."""
     grads, n, device, types = _gradients(grads, "clip_gradients")
     max_norm, eps = _limit(max_norm, eps)
     for g in grads:
         if g.is_neg() or not g[0].is_contiguous() or (n > 1 and g.stride(0) < g[0].numel()):
             raise CompAMSError("gradients that are clipped in place must be packed for every worker, and the workers' parts apart")
-        if g.requires_grad and torch.is_grad_enabled() and g.is_leaf:
-            raise CompAMSError("a leaf that requires a gradient cannot be scaled in place")
+        if g.requires_grad and torch.is_grad_enabled() and (g.is_leaf or (g._base is not None and g._base.is_leaf)):
+            raise CompAMSError("a leaf that requires a gradient, or a view of one, cannot be scaled in place")
     sizes, addresses, strides, types, widths = _with_elements([g.numel() // n for g in grads], [g.data_ptr() for g in grads],
                                                               [g.stride(0) for g in grads], types, [g.element_size() for g in grads])
     if _overlap(n, addresses, strides, sizes, widths):

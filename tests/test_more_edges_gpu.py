@@ -258,3 +258,17 @@ def test_saved_tensors_that_hooks_unpack(kinds, path):
             # (a weight that all share may come back as one of each worker's own: its sums then run in another order)
             for a, b in zip(gradients(out, leaves), want):
                 B.near(a, b.double(), 2 * B.U[a.dtype] + 2.0 ** -20, "gradient")
+
+
+def test_leaves_and_their_views_are_not_scaled_in_place():
+    x = torch.ones(2, 3, 4, device="cuda", requires_grad=True)
+    for bad in (x, x.view(2, 12), x[:, 1], x[:1]):
+        with pytest.raises(CompAMSError):
+            clip_gradients([bad], 0.01)
+    assert torch.equal(x, torch.ones_like(x))
+    with torch.no_grad():
+        clip_gradients([x.view(2, 12)], 0.01, eps=0.0)
+    B.near(x, x.detach().double().fill_(0.01 / 12 ** 0.5), 4 * B.E, "x")
+    clip_gradients([x.detach()], 0.001)
+    G, norms = collect_gradients([x, x * 2.0])  # a copy, which knows nothing of where it is from
+    assert not G.requires_grad and not norms.requires_grad
