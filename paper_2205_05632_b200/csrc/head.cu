@@ -108,7 +108,9 @@ struct FewArgs {
 };
 // A warp takes a share of the rows of W, for one row of x a row at a time and eight CTAs to an SM (32000 rows of 4096 bfloat16 columns, 262 MB:
 // 46 us; four rows at a time and four CTAs 49, two and six 51), for more of them four, so that x is read once for four; a lane has eight
-// columns (or every 32nd) of each.
+// columns (or every 32nd) of each. Two to four rows of x: shares for four CTAs to an SM, of which the registers let two (two rows of x) or one
+// be there at a time. 32000 rows of W in shares for four / three / two: two rows of 4096 65 / 76 / 61 us, of 8192 110 / 137 / 113, four of 1024
+// 46 / 48 / 42, of 4096 113 / 117 / 105, of 6144 155 / 159 / 141.
 constexpr int staged_rows(int rows) { return rows == 3 ? 4 : rows; }  // the kernel's MR: three rows are taken as four
 __host__ __device__ constexpr int rows_at_once(int rows) { return rows == 1 ? 1 : 4; }
 __host__ __device__ constexpr int ctas_at_once(int rows) { return rows == 1 ? 8 : 4; }

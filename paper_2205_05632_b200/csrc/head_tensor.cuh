@@ -8,7 +8,8 @@
 // A pair of CTAs takes tiles of 256 x 256 (cta_group::2): each holds 128 rows of the left operand and 128 of the right in shared memory,
 // half of what two CTAs of 128 x 256 would read from it and fetch from the L2, and has the sums of its 128 rows in its tensor memory,
 // twice (2 x 256 columns): while eight warps take the sums of one stretch, the products of the next go to the other. The tensor cores cut
-// their sums, so a stretch is 8 or 16 tiles of 64 long and joins the fp32 registers by rounded additions.
+// their sums, so a stretch is at most 16 products of 64 (up to three pairs of planes) or 8 (more), which are 16, 8, 5 or 1 tiles along the sum,
+// one at least, and joins the fp32 registers by rounded additions.
 //
 // Operands are bf16 or fp16. fp32 numbers are three bf16 planes, and fp16 ones beside fp32 two: the sum then runs over pairs of planes as
 // well, listed in the arguments, small ones first.
