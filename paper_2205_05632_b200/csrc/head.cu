@@ -105,6 +105,12 @@ struct FewArgs {
     const int64_t* target;
     float* target_logit;
     float2* stats;  // [CTA][all rows]
+    // PROBS: of the columns from `first` on, the first `vocab` (weight is that of `first`)
+    const float *lse, *row_gradient;
+    int64_t ignored;
+    int32_t first, all_columns, probs, f16;
+    uint16_t* d;           // [plane][all rows][width]; zeros behind the last column up to a multiple of 64
+    int64_t width;
 };
 // A warp takes a share of the rows of W, for one row of x a row at a time and eight CTAs to an SM (32000 rows of 4096 bfloat16 columns, 262 MB:
 // 46 us; four rows at a time and four CTAs 49, two and six 51), for more of them four, so that x is read once for four; a lane has eight
@@ -114,7 +120,9 @@ struct FewArgs {
 constexpr int staged_rows(int rows) { return rows == 3 ? 4 : rows; }  // the kernel's MR: three rows are taken as four
 __host__ __device__ constexpr int rows_at_once(int rows) { return rows == 1 ? 1 : 4; }
 __host__ __device__ constexpr int ctas_at_once(int rows) { return rows == 1 ? 8 : 4; }
-template <typename TX, typename TW, int MR, bool VEC>
+// PROBS: the same logits, to the last bit, and d from them: a target that is nearly certain has d = p - 1, which another order of the sums
+// would be in the place of.
+template <typename TX, typename TW, int MR, bool VEC, bool PROBS>
 __global__ void __launch_bounds__(256, MR == 1 ? ctas_at_once(MR) : 1) few_kernel(const __grid_constant__ FewArgs a) {
     extern __shared__ __align__(16) float xs[];  // [MR][h up to a multiple of 8]
     __shared__ float2 joint[8][MR];
@@ -137,6 +145,23 @@ __global__ void __launch_bounds__(256, MR == 1 ? ctas_at_once(MR) : 1) few_kerne
     for (int r = 0; r < MR; ++r) {
         target[r] = r < a.rows ? a.target[number0 + r] : -1;
         state[r] = make_float2(-kInf, 0.0f);
+    }
+    // PROBS: a lane's row of x, and which of the rows of W it writes
+    const int own = lane % MR, own_j = lane / MR;
+    const bool writes = PROBS && own < a.rows && own_j < kRows;
+    float lse = 0.0f, g = 0.0f;
+    int64_t own_target = -1;
+    uint16_t* d = nullptr;
+    if (writes) {
+        const int64_t number = number0 + own;
+        own_target = a.target[number];
+        lse = a.lse[number];
+        g = a.row_gradient ? a.row_gradient[number]
+                           : own_target == a.ignored ? 0.0f : own_target >= 0 && own_target < a.all_columns ? 1.0f : __int_as_float(0x7fffffff);
+        d = a.d + number * a.width;
+        if (blockIdx.x == 0 && warp == 0 && own_j == 0)
+            for (int p = 0; p < a.probs; ++p)
+                for (int c = a.vocab; c < (a.vocab + 63) / 64 * 64; ++c) d[p * a.all_rows * a.width + c] = 0;
     }
     for (int v0 = start; v0 < last; v0 += kRows) {
         float acc[kRows][MR] = {};
@@ -175,6 +200,7 @@ __global__ void __launch_bounds__(256, MR == 1 ? ctas_at_once(MR) : 1) few_kerne
                     for (int j = 0; j < kRows; ++j) acc[j][r] = fmaf(w[j], xs[r * pitch + c], acc[j][r]);
             }
         }
+        float mine = 0.0f;
 #pragma unroll
         for (int j = 0; j < kRows; ++j)
 #pragma unroll
@@ -183,12 +209,24 @@ __global__ void __launch_bounds__(256, MR == 1 ? ctas_at_once(MR) : 1) few_kerne
 #pragma unroll
                 for (int o = 16; o; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
                 const int v = v0 + j;
-                if (v < last) {
+                if (PROBS) {
+                    if (lane == j * MR + r) mine = z;
+                } else if (v < last) {
                     state[r] = merged(state[r], make_float2(z, 1.0f));
                     if (lane == 0 && v == target[r]) a.target_logit[number0 + r] = z;
                 }
             }
+        if (PROBS && writes && v0 + own_j < last) {
+            const int v = v0 + own_j;
+            float rest = 0.0f;
+            if (g != 0.0f) rest = (power2((mine - lse) * kLog2e) - (a.first + v == own_target ? 1.0f : 0.0f)) * (a.f16 ? g * head::kF16Scale : g);
+            for (int p = 0; p < a.probs; ++p) {
+                float none = 0.0f;
+                d[p * a.all_rows * a.width + v] = (uint16_t)head::plane_of(rest, none, a.f16 != 0, p + 1 == a.probs);
+            }
+        }
     }
+    if (PROBS) return;
 #pragma unroll
     for (int r = 0; r < MR; ++r)
         if (lane == 0) joint[warp][r] = state[r];
@@ -470,8 +508,8 @@ constexpr int64_t kProbsBytes = 512ll << 20;  // of a piece's d
 constexpr int64_t kSumsBytes = 256ll << 20;   // of the parts' sums of dx
 
 int64_t up_to(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
-int64_t few_ctas(const HeadShape& z) {
-    return std::max<int64_t>(1, std::min<int64_t>((z.vocab + 31) / 32, ((int64_t)multiprocessors() * ctas_at_once((int)z.batch_rows()) + z.batches() - 1) / z.batches()));
+int64_t few_ctas(const HeadShape& z, int64_t columns) {
+    return std::max<int64_t>(1, std::min<int64_t>((columns + 31) / 32, ((int64_t)multiprocessors() * ctas_at_once((int)z.batch_rows()) + z.batches() - 1) / z.batches()));
 }
 
 // Parts of the vocabulary's sum of dx: as many as take the pairs of CTAs the shortest time, in tiles of 64 (0.3 us), with what adding up
@@ -516,7 +554,7 @@ Plan plan_of(const HeadShape& z, bool x_copied, bool w_copied, int wanted) {  //
     if (x_copied && !few) p.x_copy = take(z.x_planes() * m * z.pitch() * 2);
     if (w_copied && !few) p.w_copy = take(z.w_planes() * z.batches() * p.piece * z.pitch() * 2);
     if (!wanted) {
-        p.stat_parts = few ? few_ctas(z) : (z.vocab + kVocab - 1) / kVocab;
+        p.stat_parts = few ? few_ctas(z, z.vocab) : (z.vocab + kVocab - 1) / kVocab;
         p.stats = take(p.stat_parts * m * 8);
         p.target_logit = take(m * 4);
         p.row_loss = take(m * 4);
@@ -667,19 +705,31 @@ int operands(const HeadShape& z, const void* x, int64_t x_ws, int64_t x_rs, cons
 }
 
 template <typename TX, typename TW, int MR>
-int few_rows(const HeadShape& z, FewArgs& a, bool vec, int64_t ctas, cudaStream_t stream) {
-    const auto kernel = vec ? few_kernel<TX, TW, MR, true> : few_kernel<TX, TW, MR, false>;
+int few_rows(const HeadShape& z, const FewArgs& a, bool vec, int64_t ctas, cudaStream_t stream) {
+    const auto kernel = a.d ? (vec ? few_kernel<TX, TW, MR, true, true> : few_kernel<TX, TW, MR, false, true>)
+                            : (vec ? few_kernel<TX, TW, MR, true, false> : few_kernel<TX, TW, MR, false, false>);
     return launched(launch_sized(kernel, dim3((uint32_t)ctas, (uint32_t)z.batches()), 256, 1, Shared((size_t)(MR * z.pitch() * 4), kFewShared), true,
                                  stream, a),
                     "head_few");
 }
 template <typename TX, typename TW>
-int few_rows(const HeadShape& z, FewArgs& a, int64_t ctas, cudaStream_t stream) {
+int few_rows(const HeadShape& z, const FewArgs& a, int64_t ctas, cudaStream_t stream) {
     const bool vec = z.h % 8 == 0 && ((reinterpret_cast<uintptr_t>(a.weight) | (uint64_t)(a.w_rs * (int64_t)sizeof(TW)) |
                                        (uint64_t)(a.w_ws * (int64_t)sizeof(TW))) & 15u) == 0;
     const int staged = staged_rows(a.rows);
     return staged == 1 ? few_rows<TX, TW, 1>(z, a, vec, ctas, stream)
                        : staged == 2 ? few_rows<TX, TW, 2>(z, a, vec, ctas, stream) : few_rows<TX, TW, 4>(z, a, vec, ctas, stream);
+}
+
+// The logits of a few rows for `columns` rows of the weight, a.weight on.
+int few_rows(const HeadShape& z, FewArgs& a, const void* x, int64_t x_ws, int64_t x_rs, int64_t w_ws, int64_t w_rs, int64_t columns, cudaStream_t stream) {
+    a.x = x; a.x_ws = x_ws; a.x_rs = x_rs; a.w_ws = z.shared ? 0 : w_ws; a.w_rs = w_rs; a.h = (int32_t)z.h; a.vocab = (int32_t)columns;
+    a.rows = (int32_t)z.batch_rows(); a.worker_rows = (int32_t)z.rows; a.all_rows = z.all_rows();
+    const int64_t ctas = few_ctas(z, columns);
+    const bool wide = z.weight_type == kTypeF32;
+    return z.type == kTypeF32 ? few_rows<float, float>(z, a, ctas, stream)
+           : z.type == kTypeBF16 ? (wide ? few_rows<__nv_bfloat16, float>(z, a, ctas, stream) : few_rows<__nv_bfloat16, __nv_bfloat16>(z, a, ctas, stream))
+                                 : (wide ? few_rows<__half, float>(z, a, ctas, stream) : few_rows<__half, __half>(z, a, ctas, stream));
 }
 
 bool float_aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
@@ -743,14 +793,8 @@ int compams_head_forward(float* loss, float* lse, const void* x, int32_t type, c
     int rc = COMPAMS_OK;
     if (z.few()) {
         FewArgs a = {};
-        a.x = x; a.weight = weight; a.x_ws = x_worker_stride; a.x_rs = x_row_stride; a.w_ws = z.shared ? 0 : weight_worker_stride; a.w_rs = weight_row_stride; a.h = (int32_t)h; a.vocab = (int32_t)vocab;
-        a.rows = (int32_t)z.batch_rows(); a.all_rows = z.all_rows(); a.target = target; a.target_logit = target_logit; a.stats = stats;
-        a.worker_rows = (int32_t)rows;
-        const int64_t ctas = p.stat_parts;
-        const bool wide = weight_type == kTypeF32;
-        rc = type == kTypeF32 ? few_rows<float, float>(z, a, ctas, stream)
-             : type == kTypeBF16 ? (wide ? few_rows<__nv_bfloat16, float>(z, a, ctas, stream) : few_rows<__nv_bfloat16, __nv_bfloat16>(z, a, ctas, stream))
-                                 : (wide ? few_rows<__half, float>(z, a, ctas, stream) : few_rows<__half, __half>(z, a, ctas, stream));
+        a.weight = weight; a.target = target; a.target_logit = target_logit; a.stats = stats;
+        rc = few_rows(z, a, x, x_worker_stride, x_row_stride, weight_worker_stride, weight_row_stride, vocab, stream);
     } else {
         Operand xo, wo;
         for (int64_t v0 = 0; v0 < vocab && rc == COMPAMS_OK; v0 += p.piece) {
@@ -842,7 +886,13 @@ int compams_head_backward(void* dx, void* dweight, int32_t sum_workers, const fl
         rc = operands(z, x, x_worker_stride, x_row_stride, weight, weight_worker_stride, weight_row_stride, p, v0, count, v0 == 0, work, xo, wo, first,
                       stream);
         if (rc != COMPAMS_OK) break;
-        {
+        if (z.few()) {  // (launched behind what still reads the last piece's d, all of it)
+            FewArgs a = {};
+            a.weight = (const char*)weight + v0 * weight_row_stride * type_bytes(weight_type); a.target = target;
+            a.lse = lse; a.row_gradient = row_gradient; a.ignored = ignored; a.first = (int32_t)v0; a.all_columns = (int32_t)vocab;
+            a.probs = p.probs; a.f16 = z.f16(); a.d = d; a.width = p.width;
+            rc = few_rows(z, a, x, x_worker_stride, x_row_stride, weight_worker_stride, weight_row_stride, count, stream);
+        } else {
             head::Args a = {};
             a.tiles_m = tiles_rows; a.tiles_n = (int32_t)((count + 255) / 256); a.batches = (int32_t)z.batches(); a.parts = 1;
             a.segments = 1; a.steps = a.part_steps = (int32_t)((h + 63) / 64);

@@ -272,3 +272,45 @@ def test_leaves_and_their_views_are_not_scaled_in_place():
     clip_gradients([x.detach()], 0.001)
     G, norms = collect_gradients([x, x * 2.0])  # a copy, which knows nothing of where it is from
     assert not G.requires_grad and not norms.requires_grad
+
+
+@pytest.mark.parametrize("kinds", TYPES, ids=str)
+@pytest.mark.parametrize("n,rows,form", [(1, 1, "shared"), (1, 2, "shared"), (3, 1, "shared"), (1, 4, "apart"), (2, 3, "own"), (1, 6, "shared"), (2, 200, "own")])
+@pytest.mark.parametrize("h,vocab", [(1024, 700), (1002, 9001)])
+def test_rows_whose_target_is_nearly_certain(h, vocab, n, rows, form, kinds):
+    # Logits of a few units from products that sum to thousands in magnitude: of another order, they are another 1e-3. d of the target is p - 1, of a
+    # millionth; it is as exact as the statistics are as long as both passes have the same logits, whatever these are off by.
+    g = gen(h + rows)
+    half = rand(g, n, rows, h // 2).abs() + 0.1
+    x = torch.cat([half, half], -1).to(kinds[0])
+    along = torch.cat([torch.ones(h // 2, device="cuda"), -torch.ones(h // 2, device="cuda")])
+    t = torch.full((n, rows), 7, device="cuda")
+    to = torch.full((vocab, 1), -20.0, device="cuda")
+    to[7] = 3.0
+    w = (7.5 * along + 0.05 * rand(g, *((n,) if form == "own" else ()), vocab, h) + to / (0.9 * h)).to(kinds[1])
+    w = (w.expand(n, vocab, h) if form == "apart" else w).detach().requires_grad_()
+    x.requires_grad_()
+    loss = linear_cross_entropy(x, w, t, "none")
+    got = torch.autograd.grad(loss.sum(), (x, w))
+    together, dws, tws = w.dim() == 2, [], []
+    for i in range(n):
+        x64, w64 = x[i].detach().double(), (w if together else w[i]).detach().double()
+        z, dz = x64 @ w64.T, (h / 512 + 64) * 2 * B.E * (x64.abs() @ w64.abs().T)
+        lse = torch.logsumexp(z, -1, keepdim=True)
+        p = torch.exp(z - lse)
+        assert float((1.0 - p[:, 7]).max()) < 1e-3
+        # lse and its logarithm are rounded, the sum of exponentials at most 16 times beside 1; logits that are off shift p against p, of 1 - p
+        off = 2 * B.E * (lse.abs() + z.amax(-1, keepdim=True).abs()) + 2.0 ** -20
+        rest = 2 * dz.amax(-1, keepdim=True) + 2.0 ** -19
+        d, err = p.clone(), p * (rest + off)
+        d[:, 7] = -p[:, torch.arange(vocab, device="cuda") != 7].sum(1)
+        err[:, 7] = (off - d[:, 7:8] * rest)[:, 0]
+        planes = {BF16: B.U[BF16], F16: B.U[F16] if kinds[1] == F16 else 2.0 ** -17, F32: B.E}[kinds[0]] + (2.0 ** -16 if kinds[0] != kinds[1] else 3 * B.E)
+        if kinds == (F16, F16):
+            err = err + 2.0 ** -38
+        B.check(got[0][i], d @ w64, err @ w64.abs() + (planes + (vocab / 512 + 64) * 2 * B.E) * (d.abs() @ w64.abs()), "dx")
+        dws.append(d.T @ x64)
+        planes = (B.E if kinds[1] == F32 else B.U[kinds[1]]) + 3 * B.E
+        tws.append(err.T @ x64.abs() + (planes + (rows / 512 + 64) * 2 * B.E) * (d.T.abs() @ x64.abs()))
+    dw, tw = torch.stack(dws), torch.stack(tws)
+    B.check(got[1], dw.sum(0) if together else dw, tw.sum(0) if together else tw, "dweight")
