@@ -11,7 +11,8 @@
 // step does four products of 2 m h V operations where three would do for someone who keeps the logits: with m = 8192 rows, V = 100000 and
 // fp32 they would be 3.3 GB.
 //
-// A few rows (kFew) read W once, a warp taking rows of W whole, in fp32 arithmetic: bound by memory.
+// A few rows (kFew) read W once, a warp taking rows of W whole, in fp32 arithmetic: bound by memory; backward for d as well, so that the logits
+// of both passes are the same.
 //
 // Precision. Products of 16-bit numbers of one type are exact and their sums fp32. Beside an fp32 weight everything is bf16 planes: an fp32
 // number is three (each the rest of those before it, rounded), fp16 two; pairs of planes i + j <= 2 are formed, which leaves out at most
@@ -21,7 +22,8 @@
 // 100000 columns: 2.9e-3 off with g inside, 2.2e-3 now, of which rounding the result is 1.7e-3); without a reduction it is taken relative
 // to a power of two above the worker's largest, and where d is fp16, which could not hold rows far below it, to one of the row's own: dx
 // then has its row's, and d is brought to the worker's before the sum over the rows. For dx of 8 bits beside an fp32 weight two
-// planes of W are taken. No atomics: results do not change from run to run.
+// planes of W are taken. lse is one fp32 number, so every p, and the target's p - 1, is off by up to half a step of it (1e-6 for 16 to 32).
+// No atomics: results do not change from run to run.
 #include <string.h>
 
 #include <algorithm>
@@ -279,12 +281,13 @@ __global__ void __launch_bounds__(1024) join_kernel(const __grid_constant__ Join
     float loss = 0.0f, counted = 0.0f;
     if (there && (int)threadIdx.x < a.lanes) {
         v = shares[threadIdx.x];
-        const float lse = v.x + logf(v.y);
+        const float log_sum = logf(v.y), lse = v.x + log_sum;
         const int64_t t = a.target[row];
         a.lse[row] = lse;
         if (t != a.ignored) {
             counted = 1.0f;
-            loss = t >= 0 && t < a.vocab ? lse - a.target_logit[row] : __int_as_float(0x7fffffff);  // no such column
+            // (the logits' difference first: where the target is nearly certain lse has rounded away what the loss is)
+            loss = t >= 0 && t < a.vocab ? (v.x - a.target_logit[row]) + log_sum : __int_as_float(0x7fffffff);  // no such column
         }
         if (a.reduction == kNone) a.loss[row] = loss;
         else if (!a.whole) a.row_loss[row] = loss;

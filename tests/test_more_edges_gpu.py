@@ -314,3 +314,23 @@ def test_rows_whose_target_is_nearly_certain(h, vocab, n, rows, form, kinds):
         tws.append(err.T @ x64.abs() + (planes + (rows / 512 + 64) * 2 * B.E) * (d.T.abs() @ x64.abs()))
     dw, tw = torch.stack(dws), torch.stack(tws)
     B.check(got[1], dw.sum(0) if together else dw, tw.sum(0) if together else tw, "dweight")
+
+
+@pytest.mark.parametrize("kinds", TYPES, ids=str)
+@pytest.mark.parametrize("rows", [1, 3, 40, 300])
+def test_small_losses_of_large_logits(rows, kinds):
+    # a target's logit of 320 in front of others of about 300: a loss of a ten-thousandth or less, of which a rounding of the logits' size, up to
+    # 2^-16, would leave little
+    g = gen(rows)
+    x = torch.ones(2, rows, 64, dtype=kinds[0], device="cuda")
+    w = (torch.randint(296, 305, (500, 1), generator=g, device="cuda").float() / 64).expand(500, 64).contiguous()
+    w[3] = 5.0
+    w = w.to(kinds[1])
+    t = torch.full((2, rows), 3, device="cuda")
+    z = x.double() @ w.double().T
+    want = torch.logsumexp(z, -1) - z[..., 3]
+    assert 1e-7 < float(want.min()) and float(want.max()) < 1e-3
+    # z is a sum of 64 equal numbers of 10 bits at most: exact. Beside the target's 1 the sum of exponentials is rounded, by 2^-24 at most, at each
+    # of the 127 other columns of a tile, as they are added one after another, and where tiles or warps are joined, 16 times at most; the
+    # exponentials themselves are 2^-21 off and their arguments, of 24, 2^-20
+    B.check(linear_cross_entropy(x, w, t, "none"), want, (127 + 16) * B.E + 2.0 ** -18 * want, "loss")
